@@ -64,7 +64,9 @@ typedef enum ebs_layout {
 typedef enum ebs_dtype {
     EBS_F32 = 0,      /* real values; quantized inside the call (Eq. 1b / 1c) */
     EBS_I8_CODES = 1, /* signed 8-bit integer codes (weights) */
-    EBS_U8_CODES = 2  /* unsigned 8-bit integer codes (activations) */
+    EBS_U8_CODES = 2, /* unsigned 8-bit integer codes (activations) */
+    EBS_F16 = 3,      /* IEEE half precision (real-valued layers below) */
+    EBS_BF16 = 4      /* bfloat16 (real-valued layers below) */
 } ebs_dtype;
 
 /* One convolution layer (Sec. 3: weight tensor c_i x c_o x k x k; Sec. 4.3: per-layer M and K). */
@@ -348,6 +350,78 @@ int ebs_search_weight_forward(const float *w_dev, size_t n, const int *bits, con
                               float *w_hat_dev, void *scratch_dev, void *stream);
 int ebs_search_act_forward(const float *x_dev, size_t n, float alpha, const int *bits, const float *coeff,
                            int n_cand, float *x_hat_dev, void *stream);
+
+/*
+ * Real-valued layers: what the search stage multiplies between ebs_search_weight_forward / ebs_search_act_forward and
+ * what the layers that stay unquantized (classifier; App. B) need, forward and backward.  The paper trains with an
+ * ordinary framework here and has no counterpart.
+ *
+ *   forward    z = x W^T + bias          x [m][k], W [n][k], bias [n] (nullable)
+ *              y = act(z) + residual     residual [m][n] (nullable); y, z [m][n]
+ *   backward   dz = dy * act'(z)         dy, z [m][n] (z: what the forward call kept; unused without an activation)
+ *              dx = dz W,  dW = dz^T x,  dbias = sum over the rows of dz        (residual's gradient is dy itself)
+ *
+ * All tensors have the element type `dtype` (EBS_F32, EBS_F16 or EBS_BF16); products are summed in fp32 (EBS_F32: from
+ * operands of 22 bits or more, see csrc/gemm.cuh), activation and residual are applied to the fp32 sums, and each output
+ * is rounded once.  The backward call of a 16-bit type with an activation rounds dz to that type before the products,
+ * not before the sum that gives dbias.
+ *   EBS_ACT_RELU       z > 0 ? z : 0 (NaN gives 0, as in the convolution's epilogue); slope 1 where z > 0, else 0
+ *   EBS_ACT_GELU       z/2 (1 + erf(z / sqrt 2))
+ *   EBS_ACT_GELU_TANH  z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))
+ *   EBS_ACT_SILU       z / (1 + exp(-z))
+ * Infinities and NaN in x, W and dy reach exactly the outputs whose sums contain them.
+ *
+ * Rows may be strided: ld* = elements from one row to the next (0: dense, that is k for x and W, n for the others); what
+ * lies between the rows is neither read nor written.  dx has the stride of x, dW of W, dy of y.  Base addresses are
+ * 16-byte aligned, the strides need not be (strides whose rows all start on 16 bytes save a copy of that operand).
+ * m = 0 is an empty batch: nothing is read, dW and dbias become zero.  No output may overlap another tensor of the call,
+ * except that y may be the residual itself (same address and stride).
+ * Results do not depend on anything but the arguments: sums are taken in a fixed order.
+ *
+ * workspace_dev: ebs_linear_workspace_bytes(desc, backward) bytes of device memory (0 bytes: may be NULL).  A call leaves
+ * nothing in it that another one reads; two calls whose GPU work overlaps need one each.
+ * Backward: any of dx, dW, dbias may be NULL, at least one is wanted.  x is needed for dW, W for dx.
+ */
+typedef enum ebs_act {
+    EBS_ACT_NONE = 0,
+    EBS_ACT_RELU = 1,
+    EBS_ACT_GELU = 2,
+    EBS_ACT_GELU_TANH = 3,
+    EBS_ACT_SILU = 4
+} ebs_act;
+
+typedef struct ebs_linear_desc {
+    int m, n, k;   /* rows of x, output features, input features; m >= 0, n and k >= 1 */
+    int dtype;     /* EBS_F32, EBS_F16, EBS_BF16 */
+    int act;       /* ebs_act */
+    long long ldx, ldw, ldy, ldr, ldz; /* row strides of x (and dx), W (and dW), y (and dy), residual, z; 0: dense */
+} ebs_linear_desc;
+
+size_t ebs_linear_workspace_bytes(const ebs_linear_desc *desc, int backward);
+int ebs_linear_forward(const void *x_dev, const void *w_dev, const void *bias_dev, const void *residual_dev,
+                       const ebs_linear_desc *desc, void *y_dev, void *z_dev, void *workspace_dev, size_t workspace_bytes,
+                       void *stream);
+int ebs_linear_backward(const void *dy_dev, const void *x_dev, const void *w_dev, const void *z_dev,
+                        const ebs_linear_desc *desc, void *dx_dev, void *dw_dev, void *dbias_dev, void *workspace_dev,
+                        size_t workspace_bytes, void *stream);
+
+/*
+ * Orthogonalised update: `batch` matrices G [rows][cols] (dense, one behind the other), each replaced by a Newton-Schulz
+ * iterate of itself (the paper trains with SGD and has no counterpart):
+ *   X_0 = G / (|G|_F + eps)
+ *   X <- a X + b (X X^T) X + c (X X^T)^2 X        `steps` times; (a, b, c) = coeff
+ *   out = scale * X
+ * The iteration acts on the singular values alone, s <- a s + b s^3 + c s^5: with the coefficients 3.4445, -4.7750,
+ * 2.0315 all but the smallest end in about 0.7 .. 1.2.  A zero matrix gives zero (eps > 0); a matrix with a NaN or an
+ * infinity gives NaN throughout.  |G|_F is summed in 64 bits.  The products are summed in fp32 from operands kept to 22
+ * bits, for every type: a steep polynomial multiplies early roundings by up to a^steps.
+ * dtype (EBS_F32, EBS_F16, EBS_BF16) is the type of G and out.  steps 0 .. 64, coefficients and scale finite, eps >= 0;
+ * EBS_ERR_UNSUPPORTED if the singular values could leave 2^-60 .. 2^60 under these coefficients.  coeff is a HOST array of
+ * three floats.  out may be G itself, and may not overlap it otherwise; workspace_dev as above.
+ */
+size_t ebs_orthogonalize_workspace_bytes(int batch, int rows, int cols, int dtype, int steps);
+int ebs_orthogonalize(const void *g_dev, int batch, int rows, int cols, int dtype, int steps, const float *coeff, float eps,
+                      float scale, void *out_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
  * Expected operation count of a layer during the search (Eq. 11):

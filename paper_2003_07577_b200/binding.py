@@ -23,7 +23,8 @@ LIB_PATH = os.path.join(_PKG, "libebs_checked.so" if os.environ.get("EBS_LIBRARY
 EBS_OK, EBS_ERR_INVALID_ARG, EBS_ERR_UNSUPPORTED, EBS_ERR_OVERFLOW, EBS_ERR_CUDA, EBS_ERR_TIMEOUT = 0, -1, -2, -3, -4, -5
 EBS_ERR_SCRATCH_TOO_SMALL = -6
 EBS_NCHW, EBS_NHWC = 0, 1
-EBS_F32, EBS_I8_CODES, EBS_U8_CODES = 0, 1, 2
+EBS_F32, EBS_I8_CODES, EBS_U8_CODES, EBS_F16, EBS_BF16 = 0, 1, 2, 3, 4
+EBS_ACT_NONE, EBS_ACT_RELU, EBS_ACT_GELU, EBS_ACT_GELU_TANH, EBS_ACT_SILU = 0, 1, 2, 3, 4
 
 EXPORTS = [
     "ebs_version", "ebs_status_string", "ebs_last_cuda_error", "ebs_conv_out_shape", "ebs_packed_weight_bytes",
@@ -35,6 +36,8 @@ EXPORTS = [
     "ebs_conv2d_i8", "ebs_maxpool_packed", "ebs_combined_scale", "ebs_reciprocal_step",
     "ebs_checked_build", "ebs_checked_status", "ebs_test_checked_shrink", "ebs_pack_acts_s2d", "ebs_test_conv_route",
     "ebs_graph_begin", "ebs_graph_end", "ebs_graph_launch", "ebs_graph_destroy",
+    "ebs_linear_workspace_bytes", "ebs_linear_forward", "ebs_linear_backward",
+    "ebs_orthogonalize_workspace_bytes", "ebs_orthogonalize",
 ]
 
 
@@ -50,6 +53,12 @@ class ebs_epilogue(ctypes.Structure):
                 ("residual_dev", ctypes.c_void_p), ("relu", ctypes.c_int), ("next_a_bits", ctypes.c_int),
                 ("next_a_scale", ctypes.c_float), ("y_layout", ctypes.c_int), ("res_packed_dev", ctypes.c_void_p),
                 ("res_bits", ctypes.c_int), ("res_scale", ctypes.c_float)]
+
+
+class ebs_linear_desc(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_int), ("n", ctypes.c_int), ("k", ctypes.c_int), ("dtype", ctypes.c_int), ("act", ctypes.c_int),
+                ("ldx", ctypes.c_longlong), ("ldw", ctypes.c_longlong), ("ldy", ctypes.c_longlong),
+                ("ldr", ctypes.c_longlong), ("ldz", ctypes.c_longlong)]
 
 
 class EbsError(RuntimeError):
@@ -125,6 +134,14 @@ def lib() -> ctypes.CDLL:
         L.ebs_graph_end.argtypes = [p, ctypes.POINTER(p)]
         L.ebs_graph_launch.argtypes = [p, p]
         L.ebs_graph_destroy.argtypes = [p]
+        LD = ctypes.POINTER(ebs_linear_desc)
+        L.ebs_linear_workspace_bytes.argtypes = [LD, i]
+        L.ebs_linear_workspace_bytes.restype = z
+        L.ebs_linear_forward.argtypes = [p, p, p, p, LD, p, p, p, z, p]
+        L.ebs_linear_backward.argtypes = [p, p, p, p, LD, p, p, p, p, z, p]
+        L.ebs_orthogonalize_workspace_bytes.argtypes = [i, i, i, i, i]
+        L.ebs_orthogonalize_workspace_bytes.restype = z
+        L.ebs_orthogonalize.argtypes = [p, i, i, i, i, i, fp, f, f, p, p, z, p]
         _lib = L
     return _lib
 
@@ -140,10 +157,11 @@ def _native():
         L = lib()
         names = ("ebs_pack_acts", "ebs_pack_acts_s2d", "ebs_conv2d_mixed", "ebs_conv2d_mixed_variant", "ebs_dequant",
                  "ebs_global_avgpool", "ebs_maxpool_packed", "ebs_resnet_cifar_forward", "ebs_search_weight_forward",
-                 "ebs_search_act_forward", "ebs_graph_launch")
+                 "ebs_search_act_forward", "ebs_graph_launch", "ebs_linear_forward", "ebs_linear_backward", "ebs_orthogonalize")
         torch.cuda.init()                                  # the stream lookups below need torch's CUDA state
         _fastcall.bind({k: ctypes.cast(getattr(L, k), ctypes.c_void_p).value for k in names},
-                       torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, ebs_conv_desc, ebs_epilogue, ebs_fused_head)
+                       torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, ebs_conv_desc, ebs_epilogue, ebs_fused_head,
+                       ebs_linear_desc)
         _fast = _fastcall
     return _fast
 
@@ -406,6 +424,39 @@ def ebs_combined_scale(w_scale: float, a_scale: float) -> float:
 
 def ebs_reciprocal_step(step: float) -> float:
     return float(lib().ebs_reciprocal_step(step))
+
+
+def linear_desc(m, n, k, dtype=EBS_F32, act=EBS_ACT_NONE, ldx=0, ldw=0, ldy=0, ldr=0, ldz=0) -> ebs_linear_desc:
+    return ebs_linear_desc(m, n, k, dtype, act, ldx, ldw, ldy, ldr, ldz)
+
+
+def ebs_linear_workspace_bytes(desc: ebs_linear_desc, backward=False) -> int:
+    return lib().ebs_linear_workspace_bytes(ctypes.byref(desc), int(bool(backward)))
+
+
+def ebs_linear_forward(x_dev, w_dev, bias_dev, residual_dev, desc: ebs_linear_desc, y_dev, z_dev=None, workspace_dev=None,
+                       stream=None) -> None:
+    rc = (_fast or _native()).linear_forward(x_dev, w_dev, bias_dev, residual_dev, desc, y_dev, z_dev, workspace_dev, stream)
+    if rc:
+        _check(rc, "ebs_linear_forward")
+
+
+def ebs_linear_backward(dy_dev, x_dev, w_dev, z_dev, desc: ebs_linear_desc, dx_dev=None, dw_dev=None, dbias_dev=None,
+                        workspace_dev=None, stream=None) -> None:
+    rc = (_fast or _native()).linear_backward(dy_dev, x_dev, w_dev, z_dev, desc, dx_dev, dw_dev, dbias_dev, workspace_dev, stream)
+    if rc:
+        _check(rc, "ebs_linear_backward")
+
+
+def ebs_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int, dtype: int, steps: int = 5) -> int:
+    return lib().ebs_orthogonalize_workspace_bytes(batch, rows, cols, dtype, steps)
+
+
+def ebs_orthogonalize(g_dev, batch: int, rows: int, cols: int, dtype: int, steps: int, coeff, eps: float, scale: float, out_dev,
+                      workspace_dev, stream=None) -> None:
+    rc = (_fast or _native()).orthogonalize(g_dev, batch, rows, cols, dtype, steps, coeff, eps, scale, out_dev, workspace_dev, stream)
+    if rc:
+        _check(rc, "ebs_orthogonalize")
 
 
 class CaptureStream:

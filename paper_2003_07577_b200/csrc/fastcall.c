@@ -12,7 +12,7 @@
 
 #include "ebs.h"
 
-static PyObject *s_data_ptr, *s_cuda_stream, *f_raw_stream, *f_get_device, *t_desc, *t_epilogue, *t_head;
+static PyObject *s_data_ptr, *s_cuda_stream, *s_nbytes, *f_raw_stream, *f_get_device, *t_desc, *t_epilogue, *t_head, *t_linear;
 
 #define EACH_ENTRY(X)                                                                                                 \
     X(ebs_pack_acts) X(ebs_pack_acts_s2d) X(ebs_conv2d_mixed) X(ebs_conv2d_mixed_variant) X(ebs_dequant)              \
@@ -20,6 +20,9 @@ static PyObject *s_data_ptr, *s_cuda_stream, *f_raw_stream, *f_get_device, *t_de
     X(ebs_search_act_forward) X(ebs_graph_launch)
 #define DECLARE_ENTRY(name) static __typeof__(&name) p_##name;
 EACH_ENTRY(DECLARE_ENTRY)
+/* The real-valued operators: bound where `bind` is given their descriptor type and addresses. */
+#define EACH_REAL_ENTRY(X) X(ebs_linear_forward) X(ebs_linear_backward) X(ebs_orthogonalize)
+EACH_REAL_ENTRY(DECLARE_ENTRY)
 
 /* Device or host address of a tensor argument; None is the null pointer. */
 static int as_ptr(PyObject *o, void **out) {
@@ -240,6 +243,69 @@ FAST(graph_launch) {
     CALL(p_ebs_graph_launch(exec, st));
 }
 
+static int bound(const void *entry) {
+    if (!entry) PyErr_SetString(PyExc_RuntimeError, "entry point is not bound");
+    return entry != NULL;
+}
+/* Address and size in bytes of a workspace tensor; None is no workspace. */
+static int as_workspace(PyObject *o, void **ptr, size_t *bytes) {
+    *bytes = 0;
+    if (!as_ptr(o, ptr)) return 0;
+    if (o == Py_None) return 1;
+    PyObject *v = PyObject_GetAttr(o, s_nbytes);
+    if (!v) return 0;
+    const int ok = as_size(v, bytes);
+    Py_DECREF(v);
+    return ok;
+}
+
+FAST(linear_forward) {
+    void *p[6], *ws, *st;
+    size_t bytes;
+    ebs_linear_desc d;
+    if (!arg_count(n, 9) || !bound(p_ebs_linear_forward)) return NULL;
+    for (int k = 0; k < 4; ++k)
+        if (!as_ptr(a[k], &p[k])) return NULL;
+    if (!as_struct(a[4], t_linear, &d, sizeof(d)) || !as_ptr(a[5], &p[4]) || !as_ptr(a[6], &p[5]) || !as_workspace(a[7], &ws, &bytes) ||
+        !as_stream(a[8], &st))
+        return NULL;
+    CALL(p_ebs_linear_forward(p[0], p[1], p[2], p[3], &d, p[4], p[5], ws, bytes, st));
+}
+
+FAST(linear_backward) {
+    void *p[7], *ws, *st;
+    size_t bytes;
+    ebs_linear_desc d;
+    if (!arg_count(n, 10) || !bound(p_ebs_linear_backward)) return NULL;
+    for (int k = 0; k < 4; ++k)
+        if (!as_ptr(a[k], &p[k])) return NULL;
+    if (!as_struct(a[4], t_linear, &d, sizeof(d))) return NULL;
+    for (int k = 4; k < 7; ++k)
+        if (!as_ptr(a[k + 1], &p[k])) return NULL;
+    if (!as_workspace(a[8], &ws, &bytes) || !as_stream(a[9], &st)) return NULL;
+    CALL(p_ebs_linear_backward(p[0], p[1], p[2], p[3], &d, p[4], p[5], p[6], ws, bytes, st));
+}
+
+FAST(orthogonalize) {
+    void *g, *out, *ws, *st;
+    int i[5];
+    size_t bytes;
+    float c[3], eps, scale;
+    if (!arg_count(n, 12) || !bound(p_ebs_orthogonalize) || !as_ptr(a[0], &g)) return NULL;
+    for (int k = 0; k < 5; ++k)
+        if (!as_int(a[1 + k], &i[k])) return NULL;
+    PyObject *seq = PySequence_Fast(a[6], "coeff is not a sequence");
+    if (!seq) return NULL;
+    int ok = PySequence_Fast_GET_SIZE(seq) == 3;
+    if (!ok) PyErr_SetString(PyExc_ValueError, "coeff has three entries");
+    for (int k = 0; ok && k < 3; ++k) ok = as_float(PySequence_Fast_GET_ITEM(seq, k), &c[k]);
+    Py_DECREF(seq);
+    if (!ok || !as_float(a[7], &eps) || !as_float(a[8], &scale) || !as_ptr(a[9], &out) || !as_workspace(a[10], &ws, &bytes) ||
+        !as_stream(a[11], &st))
+        return NULL;
+    CALL(p_ebs_orthogonalize(g, i[0], i[1], i[2], i[3], i[4], c, eps, scale, out, ws, bytes, st));
+}
+
 /* same_bytes(structs, bytes): whether the concatenated contents of the structures are exactly `bytes`. */
 FAST(same_bytes) {
     if (!arg_count(n, 2)) return NULL;
@@ -281,12 +347,12 @@ FAST(same_addresses) {
     return same < 0 ? NULL : PyBool_FromLong(same);
 }
 
-/* bind(addresses, raw_stream, get_device, desc, epilogue, head): library entry points by name, torch's raw current stream of
- * a device, torch's current device and the ctypes structure types. */
+/* bind(addresses, raw_stream, get_device, desc, epilogue, head[, linear]): library entry points by name, torch's raw current
+ * stream of a device, torch's current device and the ctypes structure types (linear: with the real-valued operators). */
 static PyObject *bind(PyObject *self, PyObject *args) {
-    PyObject *addr, *raw, *dev, *desc, *epi, *head;
-    if (!PyArg_ParseTuple(args, "O!OOO!O!O!", &PyDict_Type, &addr, &raw, &dev, &PyType_Type, &desc, &PyType_Type, &epi,
-                          &PyType_Type, &head))
+    PyObject *addr, *raw, *dev, *desc, *epi, *head, *linear = NULL;
+    if (!PyArg_ParseTuple(args, "O!OOO!O!O!|O!", &PyDict_Type, &addr, &raw, &dev, &PyType_Type, &desc, &PyType_Type, &epi,
+                          &PyType_Type, &head, &PyType_Type, &linear))
         return NULL;
 #define BIND_ENTRY(name)                                                                                              \
     {                                                                                                                 \
@@ -296,6 +362,11 @@ static PyObject *bind(PyObject *self, PyObject *args) {
         if (!p_##name) return PyErr_Occurred() ? NULL : PyErr_Format(PyExc_ValueError, "null address: %s", #name);    \
     }
     EACH_ENTRY(BIND_ENTRY)
+    if (linear) {
+        EACH_REAL_ENTRY(BIND_ENTRY)
+        Py_INCREF(linear);
+        Py_XSETREF(t_linear, linear);
+    }
     Py_INCREF(raw);
     Py_XSETREF(f_raw_stream, raw);
     Py_INCREF(dev);
@@ -321,6 +392,9 @@ static PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, NULL},
                                 FAST_METHOD(search_weight_forward),
                                 FAST_METHOD(search_act_forward),
                                 FAST_METHOD(graph_launch),
+                                FAST_METHOD(linear_forward),
+                                FAST_METHOD(linear_backward),
+                                FAST_METHOD(orthogonalize),
                                 FAST_METHOD(same_bytes),
                                 FAST_METHOD(same_addresses),
                                 {NULL, NULL, 0, NULL}};
@@ -330,6 +404,7 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1
 PyMODINIT_FUNC PyInit__fastcall(void) {
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    if (!s_data_ptr || !s_cuda_stream) return NULL;
+    s_nbytes = PyUnicode_InternFromString("nbytes");
+    if (!s_data_ptr || !s_cuda_stream || !s_nbytes) return NULL;
     return PyModule_Create(&module);
 }
