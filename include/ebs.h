@@ -362,7 +362,7 @@ int ebs_search_act_forward(const float *x_dev, size_t n, float alpha, const int 
  *              dx = dz W,  dW = dz^T x,  dbias = sum over the rows of dz        (residual's gradient is dy itself)
  *
  * All tensors have the element type `dtype` (EBS_F32, EBS_F16 or EBS_BF16); products are summed in fp32 (EBS_F32: from
- * operands of 22 bits or more, see csrc/gemm.cuh), activation and residual are applied to the fp32 sums, and each output
+ * operands kept to 22 bits), activation and residual are applied to the fp32 sums, and each output
  * is rounded once.  The backward call of a 16-bit type with an activation rounds dz to that type before the products,
  * not before the sum that gives dbias.
  *   EBS_ACT_RELU       z > 0 ? z : 0 (NaN gives 0, as in the convolution's epilogue); slope 1 where z > 0, else 0
@@ -416,7 +416,7 @@ int ebs_linear_backward(const void *dy_dev, const void *x_dev, const void *w_dev
  * infinity gives NaN throughout.  |G|_F is summed in 64 bits.  The products are summed in fp32 from operands kept to 22
  * bits, for every type: a steep polynomial multiplies early roundings by up to a^steps.
  * dtype (EBS_F32, EBS_F16, EBS_BF16) is the type of G and out.  steps 0 .. 64, coefficients and scale finite, eps >= 0;
- * EBS_ERR_UNSUPPORTED if the singular values could leave 2^-60 .. 2^60 under these coefficients.  coeff is a HOST array of
+ * EBS_ERR_UNSUPPORTED if the singular values could leave 2^-20 .. 2^20 under these coefficients.  coeff is a HOST array of
  * three floats.  out may be G itself, and may not overlap it otherwise; workspace_dev as above.
  */
 size_t ebs_orthogonalize_workspace_bytes(int batch, int rows, int cols, int dtype, int steps);

@@ -4,6 +4,10 @@
 #include "ebs_internal.cuh"
 
 namespace ebs {
+unsigned long long gemm_tile_timeouts();   // gemm_tile.cu
+}
+
+namespace ebs {
 
 static thread_local char g_cuda_error[256] = "";
 
@@ -45,13 +49,16 @@ const ConvVariant* conv_mma_variant(int w_bits, int a_bits, int variant) {
 
 unsigned long long conv_umma_timeouts() {
     return conv_umma_tile_timeouts() +
-           conv_umma_strip_timeouts() + conv_umma_resident_timeouts() + conv_umma_pipe_timeouts() + fused_net_timeouts();
+           conv_umma_strip_timeouts() + conv_umma_resident_timeouts() + conv_umma_pipe_timeouts() + fused_net_timeouts() +
+           gemm_tile_timeouts();
 }
 
 // Polls a bounded device-side wait makes before it gives up (about 40 ns each), and test flags; process-wide,
 // changed only by ebs_test_set_device_wait.
 static unsigned g_wait_limit = 1u << 20;
 static int g_test_flags = 0;
+unsigned device_wait_limit() { return g_wait_limit; }
+int device_test_flags() { return g_test_flags; }
 static long long g_check_shrink = 0;      // range-checked build, tests only: result extents declared this much too short
 
 // Range-checked build only: the device words the kernels record their first out-of-range index in.

@@ -51,40 +51,126 @@ __device__ __forceinline__ float activation_slope(float z, int act) {
     }
 }
 
-// What becomes of the sum v of output (row, col).
-//   linear:  z = v + bias[col]; y = act(z) + residual
-//   otherwise: y = alpha * v + beta * c   (c fp32, read at the output's place)
+// Powers of two that fp32 operands are scaled by before they are split (linear.cu): one exponent a row or column.
+constexpr int SCALE_NAN = 1 << 20;         // the row holds a NaN: so do all its results
+constexpr int SCALE_INF = 1 << 21;         // it holds an infinity: its results are summed once more from the fp32 operands
+
+// fp32 operands of a split product, for rows and columns with infinities: a[i * a_row + r * a_red], b[j * b_col + r * b_red].
+struct GemmFp32 {
+    const float *a = nullptr, *b = nullptr;
+    long long a_row = 0, a_red = 0, b_col = 0, b_red = 0;
+    int red = 0;
+};
+
+// What becomes of the sum v of output (row, col):
+//   v *= 2^(row_exp[row] + col_exp[col])       (split fp32 operands)
+//   z = alpha * v + bias[col];  y = act(z) + residual
 struct GemmOut {
     const void* bias = nullptr;
     const void* residual = nullptr;
     void* z = nullptr;
     void* y = nullptr;
-    const float* c = nullptr;
-    long long ldr = 0, ldz = 0, ldy = 0, batch_y = 0;   // batch_y: elements between the matrices of a batch (y and c)
-    float alpha = 1.0f, beta = 0.0f;
+    const int* row_exp = nullptr;
+    const int* col_exp = nullptr;
+    GemmFp32 fp32;
+    long long ldr = 0, ldz = 0, ldy = 0;
+    float alpha = 1.0f;
     int act = EBS_ACT_NONE;
 };
 
+// v * 2^e without an overflow on the way.
+__device__ __forceinline__ float scale_pow2(float v, int e) {
+    e = e < -252 ? -252 : e;                               // (nothing of a sum below 2^100 is left there)
+    const int h = e >> 1;
+    return v * __int_as_float((h + 127) << 23) * __int_as_float((e - h + 127) << 23);
+}
+static __device__ __noinline__ float fp32_dot(const GemmFp32& g, long long row, int col) {
+    float v = 0.0f;
+    for (int r = 0; r < g.red; ++r) v = fmaf(g.a[row * g.a_row + r * g.a_red], g.b[col * g.b_col + r * g.b_red], v);
+    return v;
+}
+__device__ __forceinline__ float gemm_unscale(const GemmOut& o, long long row, int col, int row_exp, int col_exp, float v) {
+    const int e = row_exp + col_exp;
+    if (e < SCALE_NAN / 2) return scale_pow2(v, e);
+    if (row_exp == SCALE_NAN || col_exp == SCALE_NAN) return __int_as_float(0x7fffffff);
+    return fp32_dot(o.fp32, row, col);
+}
+
+// One element: the path of ragged or unaligned outputs.
 template <typename T>
-__device__ __forceinline__ void gemm_store(const GemmOut& o, int batch, long long row, int col, float v) {
-    const long long at = batch * o.batch_y + row * o.ldy + col;
-    if (o.c) v = o.alpha * v + o.beta * o.c[at];
-    else if (o.alpha != 1.0f) v *= o.alpha;
+__device__ __forceinline__ void gemm_store(const GemmOut& o, long long row, int col, float v) {
+    if (o.row_exp) v = gemm_unscale(o, row, col, o.row_exp[row], o.col_exp[col], v);
+    v *= o.alpha;
     if (o.bias) v += to_f32(static_cast<const T*>(o.bias)[col]);
     if (o.z) static_cast<T*>(o.z)[row * o.ldz + col] = from_f32<T>(v);
     if (o.act) v = activation(v, o.act);
     if (o.residual) v += to_f32(static_cast<const T*>(o.residual)[row * o.ldr + col]);
-    static_cast<T*>(o.y)[at] = from_f32<T>(v);
+    static_cast<T*>(o.y)[row * o.ldy + col] = from_f32<T>(v);
 }
 
-// D[i][j] = sum_r A(i, r) B(r, j) over elements at a[i * a_row + r * a_red] and b[j * b_col + r * b_red].
-struct GemmIn {
-    const void *a, *b;
-    long long a_row, a_red, b_col, b_red, batch_a = 0, batch_b = 0;
-    int rows, cols, red, batch = 1;
-};
+// 16 bytes of elements.
+template <typename T> struct Pack { static constexpr int N = 16 / sizeof(T); };
+template <typename T>
+__device__ __forceinline__ void load_pack(const T* p, float (&v)[16 / sizeof(T)]) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    const T* e = reinterpret_cast<const T*>(&u);
+#pragma unroll
+    for (int i = 0; i < Pack<T>::N; ++i) v[i] = to_f32(e[i]);
+}
+template <typename T>
+__device__ __forceinline__ void store_pack(T* p, const float (&v)[16 / sizeof(T)]) {
+    uint4 u;
+    T* e = reinterpret_cast<T*>(&u);
+#pragma unroll
+    for (int i = 0; i < Pack<T>::N; ++i) e[i] = from_f32<T>(v[i]);
+    *reinterpret_cast<uint4*>(p) = u;
+}
+// 16 bytes of neighbouring columns of one row, every address 16-byte aligned.
+template <typename T>
+__device__ __forceinline__ void gemm_store_pack(const GemmOut& o, long long row, int col, float (&v)[16 / sizeof(T)]) {
+    constexpr int N = Pack<T>::N;
+    float t[N];
+    if (o.row_exp) {
+        const int re = o.row_exp[row];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = gemm_unscale(o, row, col + i, re, o.col_exp[col + i], v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= o.alpha;
+    if (o.bias) {
+        load_pack(static_cast<const T*>(o.bias) + col, t);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += t[i];
+    }
+    if (o.z) store_pack(static_cast<T*>(o.z) + row * o.ldz + col, v);
+    switch (o.act) {                                        // (outside the loop: one branch a pack)
+#define EBS_ACT_CASE(A) case A: _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = activation(v[i], A); break;
+        EBS_ACT_CASE(EBS_ACT_RELU) EBS_ACT_CASE(EBS_ACT_GELU) EBS_ACT_CASE(EBS_ACT_GELU_TANH) EBS_ACT_CASE(EBS_ACT_SILU)
+#undef EBS_ACT_CASE
+        default: break;
+    }
+    if (o.residual) {
+        load_pack(static_cast<const T*>(o.residual) + row * o.ldr + col, t);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += t[i];
+    }
+    store_pack(static_cast<T*>(o.y) + row * o.ldy + col, v);
+}
+// Whether every row of the outputs and of the residual starts on 16 bytes.
+inline bool packs_ok(const GemmOut& o, size_t size) {
+    auto ok = [&](const void* p, long long ld) { return !p || (((uintptr_t)p & 15) == 0 && (ld * (long long)size) % 16 == 0); };
+    return ok(o.y, o.ldy) && ok(o.z, o.ldz) && ok(o.residual, o.ldr) && ok(o.bias, 0);
+}
 
-// dtype: type of both operands, out_dtype: of y, z, bias and residual.
-int launch_gemm(const GemmIn& in, const GemmOut& out, int dtype, int out_dtype, cudaStream_t st);
+// An operand in memory for the tensor cores: `planes` 16-bit matrices (one behind the other, plane_stride elements apart) for
+// each of `batch` (batch_stride apart), with the reduction along a row (mn_major = false: rows = the result's rows or columns) or
+// across rows (mn_major = true: rows = reduction).  Base and strides are multiples of 16 bytes.
+struct GemmOperand {
+    const void* p;
+    long long ld;
+    bool mn_major;
+    int planes = 1;
+    long long plane_stride = 0, batch_stride = 0;
+};
 
 }  // namespace ebs

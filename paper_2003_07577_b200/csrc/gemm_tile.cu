@@ -1,0 +1,326 @@
+// Tile kernel of the real-valued products: one 128 x TN tile of results a thread block, or a cluster of thread blocks that share
+// its reduction.
+//
+// Warp 8 fetches operand tiles by TMA, warp 9 issues the MMAs, warps 0-7 take the sums out of tensor memory.
+//  - Split products (PL = 2: operands as two fp16 planes hi + lo): three MMAs a step, hi*hi + hi*lo + lo*hi.  The tensor core
+//    truncates when it adds to an accumulator, so that long sums drift by their length; every GEMM_CHUNK stages the accumulator
+//    is therefore taken out and added up in registers, rounded to nearest, while the MMAs go on in a second one.
+//  - Few result rows (SWAP): the operand with many rows takes the 128 lanes, the few rows the N side of the MMA.  Such products
+//    are bound by the bytes of the large operand.
+//  - Few tiles and a long reduction: up to eight thread blocks of a cluster take a part of the reduction each; the sums meet in
+//    shared memory, each block adds a share of the tile over all parts in block order and writes it.
+#include "gemm_umma.cuh"
+#include "gemm_tile.cuh"
+
+namespace ebs {
+
+static __device__ unsigned long long g_gemm_tile_timeouts = 0ull;
+
+template <int TN, int PL>
+__host__ __device__ constexpr int tile_stage_bytes() { return PL * (128 + TN) * GEMM_ROW_BYTES; }
+
+template <class EPI, int TN, int PL, bool SWAP>
+__global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                           const TileArgs g, const EPI epi) {
+    // A is the operand on the 128 lanes, B the one on the TN columns; SWAP: lanes are the result's columns
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full[8], empty[8], acc_full[2], acc_empty[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    constexpr int STAGE = tile_stage_bytes<TN, PL>();
+    constexpr int A_BYTES = 128 * GEMM_ROW_BYTES, B_BYTES = TN * GEMM_ROW_BYTES;
+    constexpr int COLS = PL * TN < 32 ? 32 : PL * TN;            // TMEM columns: one accumulator, or two taken in turn
+    uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int split = g.split, part = (int)(blockIdx.x % split);
+    const int a0 = (int)(blockIdx.x / split) * 128, b0 = (int)blockIdx.y * TN, batch = (int)blockIdx.z;
+    const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK;
+    const int kb0 = (int)((long long)blocks * part / split), kb1 = (int)((long long)blocks * (part + 1) / split);
+    const int nkb = kb1 - kb0;
+    const int chunk = PL == 2 ? GEMM_CHUNK : (nkb > 0 ? nkb : 1);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < g.stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 8); }
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_slot)), "r"((uint32_t)COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    const uint32_t tmem = uni(tmem_slot);
+
+    float acc[PL == 2 ? TN / 2 : 1];                              // (split products: this thread's sums)
+    if (warp == 8) {
+        const bool leader = elect_one();
+        for (int i = 0; i < nkb; ++i) {
+            const int s = i % g.stages, k = (kb0 + i) * GEMM_BK;
+            if (!mbar_wait_warp(&empty[s], ((i / g.stages) & 1) ^ 1, &abort_flag, g.wait_limit)) break;
+            if (leader) {
+                const uint32_t base = smem_u32(tiles) + s * STAGE, bar = smem_u32(&full[s]);
+                mbar_expect_tx(&full[s], STAGE);
+#pragma unroll
+                for (int p = 0; p < PL; ++p) {
+                    const uint32_t at = base + p * A_BYTES, bt = base + PL * A_BYTES + p * B_BYTES;
+                    const int z = batch * PL + p;
+                    if (!g.a_mn) tma_load_3d(at, &map_a, k, a0, z, bar);
+                    else { tma_load_3d(at, &map_a, a0, k, z, bar); tma_load_3d(at + 8192, &map_a, a0 + 64, k, z, bar); }
+                    if (!g.b_mn) tma_load_3d(bt, &map_b, k, b0, z, bar);
+                    else
+#pragma unroll
+                        for (int h = 0; h < (TN + 63) / 64; ++h) tma_load_3d(bt + h * 8192, &map_b, b0 + h * 64, k, z, bar);
+                }
+            }
+            __syncwarp();
+        }
+    } else if (warp == 9) {
+        const uint32_t leader = elect_one() ? 1u : 0u;
+        const uint32_t idesc = gemm_idesc(128, TN, g.bf16, g.a_mn, g.b_mn);
+        const uint32_t a_step = g.a_mn ? 2048 >> 4 : 32 >> 4, b_step = g.b_mn ? 2048 >> 4 : 32 >> 4;
+        for (int i = 0; i < nkb; ++i) {
+            const int s = i % g.stages, c = i / chunk, in_chunk = i - c * chunk;
+            if (PL == 2 && in_chunk == 0 && c >= 2 && !mbar_wait_warp(&acc_empty[c & 1], ((c >> 1) & 1) ^ 1, &abort_flag, g.wait_limit)) break;
+            if (!mbar_wait_warp(&full[s], (i / g.stages) & 1, &abort_flag, g.wait_limit)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+            if (g.test_flags & 1) continue;                       // (give-up test: nothing is ever issued)
+            const uint32_t d = tmem + (PL == 2 ? (uint32_t)((c & 1) * TN) : 0u);
+            const uint32_t base = smem_u32(tiles) + s * STAGE;
+            const uint32_t ah = tile_desc_lo(base, g.a_mn), bh = tile_desc_lo(base + PL * A_BYTES, g.b_mn);
+#pragma unroll
+            for (int k = 0; k < GEMM_BK / 16; ++k) {
+                const uint32_t a = ah + k * a_step, b = bh + k * b_step;
+                umma_f16(leader, d, a, b, idesc, (in_chunk | k) != 0);
+                if (PL == 2) {
+                    umma_f16(leader, d, a, b + (B_BYTES >> 4), idesc, 1u);
+                    umma_f16(leader, d, a + (A_BYTES >> 4), b, idesc, 1u);
+                }
+            }
+            umma_commit_pred(leader, &empty[s]);
+            if (in_chunk == chunk - 1 || i == nkb - 1) umma_commit_pred(leader, &acc_full[c & 1]);
+        }
+    } else {
+        const uint32_t row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * (TN / 2);
+        bool ok = true;
+        if (PL == 2) {
+#pragma unroll
+            for (int j = 0; j < TN / 2; ++j) acc[j] = 0.0f;
+            const int chunks = (nkb + chunk - 1) / chunk;
+            for (int c = 0; c < chunks && ok; ++c) {
+                ok = mbar_wait_bounded(&acc_full[c & 1], (c >> 1) & 1, &abort_flag, g.wait_limit);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+#pragma unroll
+                for (int j = 0; j < TN / 2; j += 8) {
+                    uint32_t v[8];
+                    tmem_ld8(row + (c & 1) * TN + j, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[j + e] += __uint_as_float(v[e]);
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+                if (lane == 0) mbar_arrive(&acc_empty[c & 1]);
+            }
+        } else if (nkb > 0) {
+            ok = mbar_wait_bounded(&acc_full[0], 0, &abort_flag, g.wait_limit);
+            asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+        }
+    }
+    __syncthreads();                                              // every MMA is done: the stages become the exchange of sums
+    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    // exchange[outer][inner]: inner runs along a row of the results
+    float* exchange = reinterpret_cast<float*>(tiles);
+    constexpr int INNER = SWAP ? 128 : TN, OUTER = SWAP ? TN : 128, PITCH = INNER + 4;
+    if (warp < 8 && !abort_flag) {
+        const uint32_t row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * (TN / 2);
+        const int l = (warp & 3) * 32 + lane, n0 = (warp >> 2) * (TN / 2);
+#pragma unroll
+        for (int j = 0; j < TN / 2; j += 8) {
+            float f[8];
+            if (PL == 2) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = acc[j + e];
+            } else {
+                uint32_t v[8];
+                tmem_ld8(row + j, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = nkb > 0 ? __uint_as_float(v[e]) : 0.0f;
+            }
+            if (SWAP) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) exchange[(n0 + j + e) * PITCH + l] = f[e];
+            } else {
+                *reinterpret_cast<float4*>(exchange + l * PITCH + n0 + j) = make_float4(f[0], f[1], f[2], f[3]);
+                *reinterpret_cast<float4*>(exchange + l * PITCH + n0 + j + 4) = make_float4(f[4], f[5], f[6], f[7]);
+            }
+        }
+    }
+    if (split > 1) cluster_sync_all();
+    else __syncthreads();
+    const bool gave_up = abort_flag != 0;
+    bool skip = gave_up;
+    for (int q = 0; q < split && split > 1; ++q) {                // (a part that gave up leaves no sums)
+        int f;
+        asm volatile("ld.shared::cluster.s32 %0, [%1];\n" : "=r"(f) : "r"(cluster_addr((const void*)&abort_flag, q)));
+        skip |= f != 0;
+    }
+    if (!skip) {
+        const int outer0 = SWAP ? b0 : a0, inner0 = SWAP ? a0 : b0;
+        const int o_begin = OUTER * part / split, o_end = OUTER * (part + 1) / split;
+        constexpr int N = EPI::N;
+        const bool packs = g.packs != 0;
+        for (int i = threadIdx.x; i < (o_end - o_begin) * (INNER / N); i += 320) {
+            const int o = o_begin + i / (INNER / N), n = (i % (INNER / N)) * N;
+            const int orow = outer0 + o, ocol = inner0 + n;
+            if (orow >= g.out_rows || ocol >= g.out_cols) continue;
+            float v[N];
+            const float* at = exchange + o * PITCH + n;
+            if (split == 1) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = at[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = 0.0f;
+                for (int q = 0; q < split; ++q) {
+                    const uint32_t addr = cluster_addr(at, q);
+#pragma unroll
+                    for (int e = 0; e < N; e += 4) {
+                        float4 t;
+                        asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];\n" : "=f"(t.x), "=f"(t.y), "=f"(t.z), "=f"(t.w) : "r"(addr + 4 * e));
+                        v[e] += t.x; v[e + 1] += t.y; v[e + 2] += t.z; v[e + 3] += t.w;
+                    }
+                }
+            }
+            if (packs && ocol + N <= g.out_cols) epi.pack(batch, orow, ocol, v);
+            else
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (ocol + e < g.out_cols) epi.one(batch, orow, ocol + e, v[e]);
+        }
+    }
+    if (split > 1) cluster_sync_all();                            // no block leaves while another reads its sums
+    if (gave_up) {
+        giveup_drain();
+        if (threadIdx.x == 0) atomicAdd(&g_gemm_tile_timeouts, 1ull);
+    }
+    __syncthreads();
+    if (warp == 9)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"((uint32_t)COLS) : "memory");
+}
+
+unsigned long long gemm_tile_timeouts() {
+    unsigned long long n = 0;
+    return cudaMemcpyFromSymbol(&n, g_gemm_tile_timeouts, sizeof(n)) == cudaSuccess ? n : 0;
+}
+
+template <class EPI, int TN, int PL, bool SWAP>
+static int launch_tile(const CUtensorMap& a, const CUtensorMap& b, TileArgs g, const EPI& epi, int batch, int lanes, int columns, cudaStream_t st) {
+    constexpr int STAGE = tile_stage_bytes<TN, PL>();
+    constexpr int EXCHANGE = (SWAP ? TN * 132 : 128 * (TN + 4)) * 4;
+    const int most = (220 * 1024) / STAGE;
+    g.stages = most < 8 ? most : 8;
+    const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK, mine = (blocks + g.split - 1) / g.split;
+    if (g.stages > mine) g.stages = mine;
+    const int bytes = (g.stages * STAGE > EXCHANGE ? g.stages * STAGE : EXCHANGE) + 1024;
+    auto kern = gemm_tile_kernel<EPI, TN, PL, SWAP>;
+    static bool attr_set[64] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+        if (check_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024))) return EBS_ERR_CUDA;
+        if (dev >= 0 && dev < 64) attr_set[dev] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((lanes + 127) / 128 * g.split), (unsigned)((columns + TN - 1) / TN), (unsigned)batch);
+    cfg.blockDim = dim3(320, 1, 1);
+    cfg.dynamicSmemBytes = (size_t)bytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)g.split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return check_cuda(cudaLaunchKernelEx(&cfg, kern, a, b, g, epi));
+}
+
+template <class EPI, int PL>
+static int launch_tile_form(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, bool packs, cudaStream_t st) {
+    const int sms = gemm_sm_count();
+    TileArgs g = {};
+    const bool swap = s.rows <= 64 && !A.mn_major;
+    const int tn = swap ? (s.rows <= 16 ? 16 : s.rows <= 32 ? 32 : 64) : (s.cols <= 64 ? 64 : 128);
+    const int lanes = swap ? s.cols : s.rows, columns = swap ? s.rows : s.cols;
+    const GemmOperand &la = swap ? B : A, &lb = swap ? A : B;
+    const long long tiles = (long long)((lanes + 127) / 128) * ((columns + tn - 1) / tn) * s.batch;
+    const int blocks = (s.red + GEMM_BK - 1) / GEMM_BK;
+    g.split = 1;
+    while (g.split < 8 && tiles * g.split * 2 <= sms && blocks >= 4 * g.split) g.split *= 2;
+    g.red = s.red;
+    g.out_rows = s.rows;
+    g.out_cols = s.cols;
+    g.a_mn = la.mn_major;
+    g.b_mn = lb.mn_major;
+    g.bf16 = bf16;
+    g.packs = packs;
+    g.wait_limit = device_wait_limit();
+    g.test_flags = device_test_flags();
+    if ((columns + tn - 1) / tn > 65535 || s.batch > 65535) return EBS_ERR_OVERFLOW;
+    CUtensorMap a, b;
+    if (!gemm_operand_map(la, lanes, s.red, s.batch, 128, bf16, &a) || !gemm_operand_map(lb, columns, s.red, s.batch, tn, bf16, &b)) return EBS_ERR_CUDA;
+    if (swap) {
+        if (tn == 16) return launch_tile<EPI, 16, PL, true>(a, b, g, epi, s.batch, lanes, columns, st);
+        if (tn == 32) return launch_tile<EPI, 32, PL, true>(a, b, g, epi, s.batch, lanes, columns, st);
+        return launch_tile<EPI, 64, PL, true>(a, b, g, epi, s.batch, lanes, columns, st);
+    }
+    if (tn == 64) return launch_tile<EPI, 64, PL, false>(a, b, g, epi, s.batch, lanes, columns, st);
+    return launch_tile<EPI, 128, PL, false>(a, b, g, epi, s.batch, lanes, columns, st);
+}
+
+int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmOut& out, int dtype, cudaStream_t st) {
+    const bool packs = packs_ok(out, element_size(dtype));
+    if (dtype == EBS_F32) return launch_tile_form<LinearOut<float>, 2>(A, B, s, {out}, false, packs, st);
+    if (dtype == EBS_F16) return launch_tile_form<LinearOut<__half>, 1>(A, B, s, {out}, false, packs, st);
+    return launch_tile_form<LinearOut<__nv_bfloat16>, 1>(A, B, s, {out}, true, packs, st);
+}
+
+int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st) {
+    return launch_tile_form<PlanesOut, 2>(A, B, s, out, false, out.ld % 4 == 0, st);
+}
+
+bool gemm_operand_map(const GemmOperand& o, int mn, int red, int batch, int box_mn, bool bf16, CUtensorMap* map) {
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        return cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) == cudaSuccess &&
+                       found == cudaDriverEntryPointSuccess
+                   ? reinterpret_cast<Encode>(fn)
+                   : nullptr;
+    }();
+    if (!encode) return false;
+    const cuuint64_t inner = o.mn_major ? mn : red, outer = o.mn_major ? red : mn;
+    const long long slice = o.planes > 1 ? o.plane_stride : (batch > 1 ? o.batch_stride : o.ld * (long long)outer);
+    const cuuint64_t dims[3] = {inner, outer, (cuuint64_t)batch * o.planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)slice * 2};
+    const cuuint32_t box[3] = {64, o.mn_major ? 64u : (cuuint32_t)box_mn, 1}, one[3] = {1, 1, 1};
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(o.p), dims, strides, box, one,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int gemm_sm_count() {
+    static int counts[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+    if (!counts[dev]) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 148;
+        counts[dev] = n;
+    }
+    return counts[dev];
+}
+
+}  // namespace ebs

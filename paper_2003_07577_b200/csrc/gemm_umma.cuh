@@ -1,0 +1,141 @@
+// Matrix products of 16-bit operands on tcgen05.mma, operands by TMA: pieces shared by the tile kernel (gemm_tile.cu) and the
+// persistent pair kernel (gemm_pair.cu).
+//
+// Shared-memory tiles are 64 elements (128 bytes) wide with the 128-byte swizzle, whichever way an operand lies in memory:
+//  - reduction along a row (K-major): [rows][64 k], 8-row groups 1024 bytes apart; the 16-element step of one MMA is 32 bytes;
+//  - reduction across rows (MN-major): blocks of [64 k][64 rows], a block 8192 bytes, 8-k groups 1024 bytes apart; the step is
+//    16 rows of the block, 2048 bytes.  No operand is ever transposed in memory.
+#pragma once
+
+#include <cuda.h>
+
+#include "conv_frame.cuh"
+#include "conv_umma.cuh"
+#include "gemm.cuh"
+
+namespace ebs {
+
+constexpr int GEMM_BK = 64;                     // reduction elements of a stage
+constexpr int GEMM_ROW_BYTES = 128;
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst), "l"(map),
+                 "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+// Bounded wait of a converged warp that has nothing else to do: no sleep between polls.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned limit) {
+    const uint32_t addr = smem_u32(bar);
+    for (unsigned it = 0; it < limit; ++it) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}\n"
+            : "=r"(done) : "r"(addr), "r"(parity) : "memory");
+        if (__all_sync(0xffffffffu, done != 0)) return true;
+        if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
+    }
+    *abort_flag = 1;
+    return false;
+}
+
+// Descriptor words of a 128-byte-swizzled tile: the low word takes the start address, the high word is constant.
+__device__ __forceinline__ uint32_t tile_desc_lo(uint32_t smem_addr, bool mn_major) {
+    return ((smem_addr >> 4) & 0x3FFFu) | ((mn_major ? 8192u >> 4 : 1u) << 16);      // leading offset: next 64-row block
+}
+constexpr uint32_t TILE_DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);           // 8-row groups, descriptor version, 128-byte swizzle
+
+// 8 columns of this warp's 32 lanes.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(taddr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;\n" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]) :: "memory");
+}
+
+// Instruction descriptor: fp32 sums, both operands fp16 (0) or bf16 (1).
+__host__ __device__ constexpr uint32_t gemm_idesc(int m, int n, bool bf16, bool a_mn, bool b_mn) {
+    return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void umma_f16(uint32_t leader, uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %3};\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}\n"
+        :: "r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(TILE_DESC_HI), "r"(idesc), "r"(accumulate), "r"(leader)
+        : "memory");
+}
+
+// Host side: tensor map of an operand.  mn: its rows or columns in the result, red: the reduction; box_mn: rows a K-major box takes.
+// False: the driver has no tensor maps, or refused this one.
+bool gemm_operand_map(const GemmOperand& o, int mn, int red, int batch, int box_mn, bool bf16, CUtensorMap* map);
+
+// Shape of a product D = A B over `red`; D has `rows` x `cols` (row-major results) as the caller sees them.
+struct GemmShape {
+    int rows, cols, red, batch;
+};
+
+int gemm_sm_count();
+
+// The results of a linear layer or of its gradients.
+template <typename T>
+struct LinearOut {
+    static constexpr int N = Pack<T>::N;
+    GemmOut o;
+    __device__ __forceinline__ void pack(int, long long row, int col, float (&v)[N]) const { gemm_store_pack<T>(o, row, col, v); }
+    __device__ __forceinline__ void one(int, long long row, int col, float v) const { gemm_store<T>(o, row, col, v); }
+};
+
+// Results kept for further products: v = alpha * sum + beta * (c_hi + c_lo), as two fp16 planes hi + lo (value: times 2^-e of the
+// caller's choice, folded into alpha and beta).  c and y: planes `plane` elements apart, matrices of a batch `batch` apart.
+struct PlanesOut {
+    static constexpr int N = 4;
+    __half* y;
+    const __half* c;
+    long long ld, plane, batch;
+    long long c_ld, c_plane, c_batch;
+    float alpha, beta;
+    __device__ __forceinline__ void one(int b, long long row, int col, float v) const {
+        v *= alpha;
+        if (c) {
+            const __half* p = c + b * c_batch + row * c_ld + col;
+            v = fmaf(beta, __half2float(p[0]) + __half2float(p[c_plane]), v);
+        }
+        __half* q = y + b * batch + row * ld + col;
+        const __half hi = __float2half_rn(v);
+        q[0] = hi;
+        q[plane] = __float2half_rn(v - __half2float(hi));
+    }
+    __device__ __forceinline__ void pack(int b, long long row, int col, float (&v)[N]) const {
+        __half hi[4], lo[4], ch[4], cl[4];
+        if (c) {
+            const __half* p = c + b * c_batch + row * c_ld + col;
+            *reinterpret_cast<uint2*>(ch) = *reinterpret_cast<const uint2*>(p);
+            *reinterpret_cast<uint2*>(cl) = *reinterpret_cast<const uint2*>(p + c_plane);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float t = v[i] * alpha;
+            if (c) t = fmaf(beta, __half2float(ch[i]) + __half2float(cl[i]), t);
+            hi[i] = __float2half_rn(t);
+            lo[i] = __float2half_rn(t - __half2float(hi[i]));
+        }
+        __half* q = y + b * batch + row * ld + col;
+        *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(hi);
+        *reinterpret_cast<uint2*>(q + plane) = *reinterpret_cast<const uint2*>(lo);
+    }
+};
+
+// ebs_test_set_device_wait's settings.
+unsigned device_wait_limit();
+int device_test_flags();
+
+}  // namespace ebs

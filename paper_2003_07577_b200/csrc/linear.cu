@@ -1,5 +1,5 @@
 // Real-valued layers: y = act(x W^T + bias) + residual and its gradients.  See include/ebs.h.
-#include "gemm.cuh"
+#include "gemm_tile.cuh"
 
 namespace ebs {
 
@@ -55,12 +55,147 @@ static int check_tensors(const Rows* t, int count, size_t size, const Rows* same
     return EBS_OK;
 }
 
+// ---------------------------------------------------------------------------------------------------- operands
+// Takes buffers out of the workspace one behind the other; without a base it only counts.
+struct Carver {
+    char* base;
+    size_t used = 0;
+    template <typename T> T* take(size_t count) {
+        char* p = base ? base + used : nullptr;
+        used += round256(count * sizeof(T));
+        return reinterpret_cast<T*>(p);
+    }
+};
+static long long round8(long long v) { return (v + 7) & ~7LL; }
+
+// A copy of 16-bit rows whose stride is a multiple of 16 bytes.
+__global__ void __launch_bounds__(256) copy_rows_kernel(const uint16_t* __restrict__ src, long long ld, long long rows, int cols, uint16_t* __restrict__ dst, long long ldd) {
+    for (long long r = blockIdx.y; r < rows; r += gridDim.y)
+        for (int c = blockIdx.x * 256 + threadIdx.x; c < cols; c += gridDim.x * 256) dst[r * ldd + c] = src[r * ld + c];
+}
+
+// The power of two that brings values of magnitude up to the one with these bits below 2^15, and what is remembered of it: its
+// negated exponent, or what kind of row this is.
+__device__ __forceinline__ int split_exponent(unsigned top_bits) { return 141 - (int)(top_bits >> 23); }
+__device__ __forceinline__ int split_record(unsigned top_bits) {
+    if (top_bits > 0x7f800000u) return SCALE_NAN;
+    if (top_bits == 0x7f800000u) return SCALE_INF;
+    return top_bits == 0u ? 0 : -split_exponent(top_bits);
+}
+// x = (hi + lo) 2^-e: both halves rounded to nearest, 22 bits where hi is a normal number and lo has its 11 bits (values within 2^-17
+// of the largest of the row), an absolute error of 2^-40 of the largest below.  Non-finite values are 0: their rows are flagged.
+__device__ __forceinline__ void split_value(float x, int e, __half& hi, __half& lo) {
+    const float v = (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? 0.0f : scale_pow2(x, e);
+    hi = __float2half_rn(v);
+    lo = __float2half_rn(v - __half2float(hi));
+}
+
+// Planes of a matrix whose reduction runs along its rows: one exponent a row, a warp a row.
+__global__ void __launch_bounds__(256) split_rows_kernel(const float* __restrict__ src, long long ld, long long rows, int cols, __half* __restrict__ dst,
+                                                         long long ldd, int* __restrict__ exps) {
+    const int lane = threadIdx.x & 31;
+    for (long long r = blockIdx.x * 8LL + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8LL) {
+        const float* x = src + r * ld;
+        unsigned top = 0u;
+        for (int c = lane; c < cols; c += 32) top = max(top, __float_as_uint(x[c]) & 0x7fffffffu);
+        top = __reduce_max_sync(0xffffffffu, top);
+        const int e = top < 0x7f800000u && top != 0u ? split_exponent(top) : 0;
+        if (lane == 0) exps[r] = split_record(top);
+        for (int c = lane; c < cols; c += 32) split_value(x[c], e, dst[r * ldd + c], dst[rows * ldd + r * ldd + c]);
+    }
+}
+// The largest magnitudes of the columns (their bits, in `top`, which starts at zero).
+__global__ void __launch_bounds__(256) column_top_kernel(const float* __restrict__ src, long long ld, long long rows, int cols, unsigned* __restrict__ top) {
+    __shared__ unsigned part[8][32];
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), y = threadIdx.x >> 5;
+    unsigned m = 0u;
+    if (c < cols)
+        for (long long r = blockIdx.y * 8LL + y; r < rows; r += gridDim.y * 8LL) m = max(m, __float_as_uint(src[r * ld + c]) & 0x7fffffffu);
+    part[y][threadIdx.x & 31] = m;
+    __syncthreads();
+    if (y == 0 && c < cols) {
+        for (int i = 1; i < 8; ++i) m = max(m, part[i][threadIdx.x]);
+        atomicMax(top + c, m);
+    }
+}
+// Planes of a matrix whose reduction runs across its rows: one exponent a column, from column_top_kernel.
+__global__ void __launch_bounds__(256) split_columns_kernel(const float* __restrict__ src, long long ld, long long rows, int cols, const unsigned* __restrict__ top,
+                                                            __half* __restrict__ dst, long long ldd, int* __restrict__ exps) {
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), y = threadIdx.x >> 5;
+    if (c >= cols) return;
+    const unsigned t = top[c];
+    const int e = t < 0x7f800000u && t != 0u ? split_exponent(t) : 0;
+    if (blockIdx.y == 0 && y == 0) exps[c] = split_record(t);
+    for (long long r = blockIdx.y * 8LL + y; r < rows; r += gridDim.y * 8LL) split_value(src[r * ld + c], e, dst[r * ldd + c], dst[rows * ldd + r * ldd + c]);
+}
+
+// An operand of a product: 16-bit rows as they are, or copied where their starts are not on 16 bytes; fp32 rows split.
+struct Prepared {
+    GemmOperand op;
+    const int* exps = nullptr;
+};
+struct Matrix {
+    const void* p;
+    long long rows, ld;
+    int cols;
+};
+static unsigned row_blocks(long long rows, int per) { const long long b = (rows + per - 1) / per; return (unsigned)(b < 2048 ? b : 2048); }
+
+static int prepare_operand(const Matrix& m, int dtype, bool across, Carver& ws, bool run, cudaStream_t st, Prepared* out) {
+    out->op = GemmOperand{m.p, m.ld, across};
+    if (dtype != EBS_F32) {
+        if ((m.ld & 7) == 0) return EBS_OK;
+        const long long ldd = round8(m.cols);
+        uint16_t* copy = ws.take<uint16_t>((size_t)m.rows * ldd);
+        out->op.p = copy;
+        out->op.ld = ldd;
+        if (!run) return EBS_OK;
+        copy_rows_kernel<<<dim3((m.cols + 255) / 256, row_blocks(m.rows, 1)), 256, 0, st>>>(static_cast<const uint16_t*>(m.p), m.ld, m.rows, m.cols, copy, ldd);
+        return check_cuda(cudaGetLastError());
+    }
+    const long long ldd = round8(m.cols);
+    __half* planes = ws.take<__half>(2 * (size_t)m.rows * ldd);
+    int* exps = ws.take<int>(across ? m.cols : m.rows);
+    unsigned* top = across ? ws.take<unsigned>(m.cols) : nullptr;
+    out->op = GemmOperand{planes, ldd, across, 2, m.rows * ldd, 2 * m.rows * ldd};
+    out->exps = exps;
+    if (!run) return EBS_OK;
+    const float* src = static_cast<const float*>(m.p);
+    if (!across) {
+        split_rows_kernel<<<row_blocks(m.rows, 8), 256, 0, st>>>(src, m.ld, m.rows, m.cols, planes, ldd, exps);
+    } else {
+        if (check_cuda(cudaMemsetAsync(top, 0, (size_t)m.cols * 4, st))) return EBS_ERR_CUDA;
+        const dim3 grid((m.cols + 31) / 32, row_blocks(m.rows, 64));
+        column_top_kernel<<<grid, 256, 0, st>>>(src, m.ld, m.rows, m.cols, top);
+        split_columns_kernel<<<grid, 256, 0, st>>>(src, m.ld, m.rows, m.cols, top, planes, ldd, exps);
+    }
+    return check_cuda(cudaGetLastError());
+}
+
+// One product with its operands prepared; a: its rows are the result's (across: its columns), likewise b for the result's columns.
+static int product(const Prepared& a, const Matrix& am, const Prepared& b, const Matrix& bm, int red, GemmOut o, int dtype, cudaStream_t st) {
+    GemmShape s{(int)(a.op.mn_major ? am.cols : am.rows), (int)(b.op.mn_major ? bm.cols : bm.rows), red, 1};
+    if (dtype == EBS_F32) {
+        o.row_exp = a.exps;
+        o.col_exp = b.exps;
+        o.fp32.a = static_cast<const float*>(am.p);
+        o.fp32.b = static_cast<const float*>(bm.p);
+        o.fp32.a_row = a.op.mn_major ? 1 : am.ld;
+        o.fp32.a_red = a.op.mn_major ? am.ld : 1;
+        o.fp32.b_col = b.op.mn_major ? 1 : bm.ld;
+        o.fp32.b_red = b.op.mn_major ? bm.ld : 1;
+        o.fp32.red = red;
+    }
+    return launch_gemm_tile(a.op, b.op, s, o, dtype, st);
+}
+
+// ---------------------------------------------------------------------------------------------------- dz and dbias
 // A half-precision dz is kept halved: the steepest slope (1.13) times the type's largest value would not fit.
 static float dz_store_scale(const ebs_linear_desc& d) { return d.dtype == EBS_F16 && d.act ? 0.5f : 1.0f; }
 
 // dz = dy * act'(z), stored times `store`, and the column sums of dz before its rounding: 32 columns a thread block, every row.
 template <typename T>
-__global__ void __launch_bounds__(256) linear_dz_kernel(const T* dy, long long ldy, const T* z, long long ldz, int m, int n, int act, float store, T* dz, T* dbias) {
+__global__ void __launch_bounds__(256) linear_dz_kernel(const T* dy, long long ldy, const T* z, long long ldz, int m, int n, int act, float store, T* dz, long long lddz, T* dbias) {
     __shared__ float part[8][33];
     const int col = blockIdx.x * 32 + (threadIdx.x & 31), lane_row = threadIdx.x >> 5;
     float sum = 0.0f;
@@ -68,7 +203,7 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const T* dy, long long l
         for (long long r = lane_row; r < m; r += 8) {
             float v = to_f32(dy[r * ldy + col]);
             if (act) v *= activation_slope(to_f32(z[r * ldz + col]), act);
-            if (dz) dz[r * n + col] = from_f32<T>(v * store);
+            if (dz) dz[r * lddz + col] = from_f32<T>(v * store);
             sum += v;
         }
     }
@@ -79,15 +214,83 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const T* dy, long long l
         dbias[col] = from_f32<T>(sum);
     }
 }
-
 template <typename T>
-static int launch_dz(const void* dy, const void* z, const ebs_linear_desc& d, void* dz, void* dbias, cudaStream_t st) {
-    linear_dz_kernel<T><<<(d.n + 31) / 32, 256, 0, st>>>(static_cast<const T*>(dy), d.ldy, static_cast<const T*>(z), d.ldz, d.m, d.n, d.act, dz_store_scale(d), static_cast<T*>(dz), static_cast<T*>(dbias));
+static int launch_dz(const void* dy, const void* z, const ebs_linear_desc& d, void* dz, long long lddz, void* dbias, cudaStream_t st) {
+    linear_dz_kernel<T><<<(d.n + 31) / 32, 256, 0, st>>>(static_cast<const T*>(dy), d.ldy, static_cast<const T*>(z), d.ldz, d.m, d.n, d.act, dz_store_scale(d), static_cast<T*>(dz), lddz,
+                                                         static_cast<T*>(dbias));
     return check_cuda(cudaGetLastError());
 }
 
-static size_t linear_workspace(const ebs_linear_desc& d, bool backward) {
-    return backward && d.act ? round256((size_t)d.m * d.n * element_size(d.dtype)) : 0;
+// ---------------------------------------------------------------------------------------------------- the calls
+struct LinearTensors {
+    const void *x, *w, *bias, *residual, *dy, *z;
+    void *y, *keep, *dx, *dw, *dbias;
+};
+// Runs the call, or (run = false) counts its workspace.
+static int forward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws, bool run, cudaStream_t st) {
+    if (d.m == 0) return EBS_OK;
+    const Matrix xm{t.x, d.m, d.ldx, d.k}, wm{t.w, d.n, d.ldw, d.k};
+    Prepared x, w;
+    int rc;
+    if ((rc = prepare_operand(xm, d.dtype, false, ws, run, st, &x)) || (rc = prepare_operand(wm, d.dtype, false, ws, run, st, &w)) || !run) return rc;
+    GemmOut o;
+    o.bias = t.bias; o.residual = t.residual; o.z = t.keep; o.y = t.y; o.act = d.act;
+    o.ldr = d.ldr; o.ldz = d.ldz; o.ldy = d.ldy;
+    return product(x, xm, w, wm, d.k, o, d.dtype, st);
+}
+static int backward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws, bool run, cudaStream_t st) {
+    int rc;
+    if (d.m == 0) {
+        if (!run) return EBS_OK;
+        const size_t size = element_size(d.dtype);
+        if (t.dw && check_cuda(cudaMemset2DAsync(t.dw, d.ldw * size, 0, d.k * size, d.n, st))) return EBS_ERR_CUDA;
+        if (t.dbias && check_cuda(cudaMemsetAsync(t.dbias, 0, d.n * size, st))) return EBS_ERR_CUDA;
+        return EBS_OK;
+    }
+    Matrix dm{t.dy, d.m, d.ldy, d.n};
+    if (d.act || t.dbias || !run) {
+        void* dz = nullptr;
+        if (d.act) {
+            const long long ld = round8(d.n);
+            dz = d.dtype == EBS_F32 ? (void*)ws.take<float>((size_t)d.m * ld) : (void*)ws.take<uint16_t>((size_t)d.m * ld);
+            dm.p = dz;
+            dm.ld = ld;
+        }
+        if (run) {
+            if (d.dtype == EBS_F32) rc = launch_dz<float>(t.dy, t.z, d, dz, dm.ld, t.dbias, st);
+            else if (d.dtype == EBS_F16) rc = launch_dz<__half>(t.dy, t.z, d, dz, dm.ld, t.dbias, st);
+            else rc = launch_dz<__nv_bfloat16>(t.dy, t.z, d, dz, dm.ld, t.dbias, st);
+            if (rc) return rc;
+        }
+    }
+    GemmOut o;
+    o.alpha = 1.0f / dz_store_scale(d);
+    Prepared g, other;
+    const bool shared = d.dtype != EBS_F32;                  // one 16-bit copy serves both products
+    if (shared && (rc = prepare_operand(dm, d.dtype, false, ws, run && (t.dx || t.dw), st, &g))) return rc;
+    if (t.dx || !run) {
+        const Matrix wm{t.w, d.n, d.ldw, d.k};
+        if (!shared && (rc = prepare_operand(dm, d.dtype, false, ws, run, st, &g))) return rc;
+        if ((rc = prepare_operand(wm, d.dtype, true, ws, run, st, &other))) return rc;
+        o.y = t.dx; o.ldy = d.ldx;
+        if (run && (rc = product(g, dm, other, wm, d.n, o, d.dtype, st))) return rc;
+    }
+    if (t.dw || !run) {
+        const Matrix xm{t.x, d.m, d.ldx, d.k};
+        if (!shared) { if ((rc = prepare_operand(dm, d.dtype, true, ws, run, st, &g))) return rc; }
+        else g.op.mn_major = true;
+        if ((rc = prepare_operand(xm, d.dtype, true, ws, run, st, &other))) return rc;
+        o.y = t.dw; o.ldy = d.ldw;
+        if (run && (rc = product(g, dm, other, xm, d.m, o, d.dtype, st))) return rc;
+    }
+    return EBS_OK;
+}
+static size_t linear_workspace(const ebs_linear_desc& d, bool back) {
+    Carver count{nullptr};
+    const LinearTensors none{};
+    if (back) backward(d, none, count, false, nullptr);
+    else forward(d, none, count, false, nullptr);
+    return count.used;
 }
 
 }  // namespace ebs
@@ -113,18 +316,14 @@ int ebs_linear_forward(const void* x, const void* w, const void* bias, const voi
     const Rows t[] = {{x, d.m, d.k, d.ldx, false}, {w, d.n, d.k, d.ldw, false}, {bias, 1, d.n, d.n, false}, {residual, d.m, d.n, d.ldr, false},
                       {y, d.m, d.n, d.ldy, true}, {z, d.m, d.n, d.ldz, true}, {need ? workspace : nullptr, 1, (long long)(need / size), (long long)(need / size), true}};
     if (check_tensors(t, 7, size, &t[3], &t[4])) return EBS_ERR_INVALID_ARG;
-    if (d.m == 0) return EBS_OK;
-    GemmIn in{x, w, d.ldx, 1, d.ldw, 1, 0, 0, d.m, d.n, d.k};
-    GemmOut o;
-    o.bias = bias; o.residual = residual; o.z = z; o.y = y; o.act = d.act;
-    o.ldr = d.ldr; o.ldz = d.ldz; o.ldy = d.ldy;
-    return launch_gemm(in, o, d.dtype, d.dtype, static_cast<cudaStream_t>(stream));
+    Carver ws{static_cast<char*>(workspace)};
+    return forward(d, LinearTensors{x, w, bias, residual, nullptr, nullptr, y, z, nullptr, nullptr, nullptr}, ws, true, static_cast<cudaStream_t>(stream));
 }
 
 int ebs_linear_backward(const void* dy, const void* x, const void* w, const void* z, const ebs_linear_desc* desc, void* dx, void* dw, void* dbias,
                         void* workspace, size_t workspace_bytes, void* stream) {
     ebs_linear_desc d;
-    int rc = complete(desc, &d);
+    const int rc = complete(desc, &d);
     if (rc) return rc;
     if (!dx && !dw && !dbias && d.m > 0) return EBS_ERR_INVALID_ARG;
     if (d.m > 0 && (!dy || (dx && !w) || (dw && !x) || (d.act && !z))) return EBS_ERR_INVALID_ARG;
@@ -134,30 +333,8 @@ int ebs_linear_backward(const void* dy, const void* x, const void* w, const void
                       {dx, d.m, d.k, d.ldx, true}, {dw, d.n, d.k, d.ldw, true}, {dbias, 1, d.n, d.n, true},
                       {need ? workspace : nullptr, 1, (long long)(need / size), (long long)(need / size), true}};
     if (check_tensors(t, 8, size, nullptr, nullptr)) return EBS_ERR_INVALID_ARG;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const void* dz = dy;
-    long long lddz = d.ldy;
-    if (dbias || d.act) {
-        void* out = d.act ? workspace : nullptr;
-        if (d.dtype == EBS_F32) rc = launch_dz<float>(dy, z, d, out, dbias, st);
-        else if (d.dtype == EBS_F16) rc = launch_dz<__half>(dy, z, d, out, dbias, st);
-        else rc = launch_dz<__nv_bfloat16>(dy, z, d, out, dbias, st);
-        if (rc) return rc;
-        if (out) { dz = out; lddz = d.n; }
-    }
-    GemmOut o;
-    o.alpha = 1.0f / dz_store_scale(d);
-    if (dx && d.m > 0) {
-        GemmIn in{dz, w, lddz, 1, 1, d.ldw, 0, 0, d.m, d.k, d.n};
-        o.y = dx; o.ldy = d.ldx;
-        if ((rc = launch_gemm(in, o, d.dtype, d.dtype, st))) return rc;
-    }
-    if (dw) {
-        GemmIn in{dz, x, 1, lddz, 1, d.ldx, 0, 0, d.n, d.k, d.m};
-        o.y = dw; o.ldy = d.ldw;
-        if ((rc = launch_gemm(in, o, d.dtype, d.dtype, st))) return rc;
-    }
-    return EBS_OK;
+    Carver ws{static_cast<char*>(workspace)};
+    return backward(d, LinearTensors{x, w, nullptr, nullptr, dy, z, nullptr, nullptr, dx, dw, dbias}, ws, true, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

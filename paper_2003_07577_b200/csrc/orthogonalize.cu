@@ -1,18 +1,22 @@
 // Newton-Schulz orthogonalisation of update matrices.  See include/ebs.h.
 #include <math.h>
 
-#include "gemm.cuh"
+#include "gemm_tile.cuh"
 
 namespace ebs {
 
 static size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
 
+// Matrices are kept as two fp16 planes hi + lo (22 bits) times a power of two: X by 2^-ex, its Gram matrix A by 2^-ea and
+// B = b A + c A^2 by 2^-eb, chosen from bounds of the singular values so that no entry leaves fp16 (an entry is at most the
+// largest singular value).
 // X = G / (|G|_F + eps), one thread block a matrix, the sum of squares in 64 bits in a fixed order.
 template <typename T>
-__global__ void __launch_bounds__(1024) normalize_kernel(const T* g, long long count, float eps, float* x) {
+__global__ void __launch_bounds__(1024) normalize_kernel(const T* g, int rows, int cols, float eps, float store, __half* x, long long ld, long long plane) {
     __shared__ double part[1024];
+    const long long count = (long long)rows * cols;
     g += blockIdx.x * count;
-    x += blockIdx.x * count;
+    x += blockIdx.x * 2 * plane;
     double s = 0.0;
     for (long long i = threadIdx.x; i < count; i += 1024) { const double v = to_f32(g[i]); s += v * v; }
     part[threadIdx.x] = s;
@@ -21,37 +25,51 @@ __global__ void __launch_bounds__(1024) normalize_kernel(const T* g, long long c
         if (threadIdx.x < o) part[threadIdx.x] += part[threadIdx.x + o];
         __syncthreads();
     }
-    const double inv = 1.0 / (sqrt(part[0]) + (double)eps);
-    for (long long i = threadIdx.x; i < count; i += 1024) x[i] = (float)(to_f32(g[i]) * inv);
+    const double inv = store / (sqrt(part[0]) + (double)eps);
+    for (long long i = threadIdx.x; i < count; i += 1024) {
+        const long long at = i / cols * ld + i % cols;
+        const float v = (float)(to_f32(g[i]) * inv);
+        const __half hi = __float2half_rn(v);
+        x[at] = hi;
+        x[plane + at] = __float2half_rn(v - __half2float(hi));
+    }
 }
 template <typename T>
-__global__ void __launch_bounds__(256) scale_out_kernel(const float* x, long long count, float scale, T* out) {
-    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < count; i += gridDim.x * 256LL) out[i] = from_f32<T>(scale * x[i]);
+__global__ void __launch_bounds__(256) scale_out_kernel(const __half* x, long long ld, long long plane, int rows, int cols, int batch, float scale, T* out) {
+    const long long count = (long long)rows * cols, total = count * batch;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < total; i += gridDim.x * 256LL) {
+        const long long b = i / count, r = i % count, at = b * 2 * plane + r / cols * ld + r % cols;
+        out[i] = from_f32<T>(scale * (__half2float(x[at]) + __half2float(x[plane + at])));
+    }
 }
 
-// Bounds of the singular values after every step; false if they could leave 2^-60 .. 2^60.
-static bool bounded(int steps, const float* c) {
-    double s = 1.0;
-    for (int i = 0; i < steps; ++i) {
-        double top = 0.0;
-        for (int j = 1; j <= 4096; ++j) {
-            const double v = s * j / 4096.0, v2 = v * v, p = fabs(v * (c[0] + v2 * (c[1] + v2 * (double)c[2])));
-            top = p > top ? p : top;
-        }
-        s = top;
-        if (!(s < 0x1p60 && s > 0x1p-60)) return false;
+// The largest singular value a step can give from singular values in 0 .. s, and the largest of |b v + c v^2|, v in 0 .. s^2 (b A + c A^2).
+static void step_bounds(const float* c, double s, double* next, double* inner) {
+    double top = 0.0, in = 0.0;
+    for (int j = 1; j <= 4096; ++j) {
+        const double v = s * j / 4096.0, v2 = v * v, q = fabs(v2 * (c[1] + v2 * (double)c[2])), p = fabs(v * (c[0] + v2 * (c[1] + v2 * (double)c[2])));
+        top = p > top ? p : top;
+        in = q > in ? q : in;
     }
-    return true;
+    *next = top;
+    *inner = in;
 }
+// The exponent e with v * 2^e in [2^13, 2^14): a factor of four below fp16's largest value for what roundings add to the bounds.
+static int headroom(double v) { int e; frexp(v > 0.0 ? v : 1.0, &e); return 14 - e; }
 
 struct OrthoBuffers {
+    long long ld, plane, side_ld, side_plane;
     size_t x, a, total;
 };
 static OrthoBuffers ortho_buffers(int batch, int rows, int cols) {
-    const size_t side = rows < cols ? rows : cols;
+    const long long side = rows < cols ? rows : cols;
     OrthoBuffers b;
-    b.x = round256((size_t)batch * rows * cols * 4);
-    b.a = round256((size_t)batch * side * side * 4);
+    b.ld = (cols + 7) & ~7LL;
+    b.plane = b.ld * rows;
+    b.side_ld = (side + 7) & ~7LL;
+    b.side_plane = b.side_ld * side;
+    b.x = round256((size_t)batch * 2 * b.plane * 2);
+    b.a = round256((size_t)batch * 2 * b.side_plane * 2);
     b.total = 2 * b.x + 2 * b.a;
     return b;
 }
@@ -80,7 +98,18 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     if (((uintptr_t)g & 15) || ((uintptr_t)out & 15) || ((uintptr_t)workspace & 15)) return EBS_ERR_INVALID_ARG;
     for (int i = 0; i < 3; ++i)
         if (!isfinite(coeff[i])) return EBS_ERR_INVALID_ARG;
-    if (!bounded(steps, coeff)) return EBS_ERR_UNSUPPORTED;
+    // singular values before each step, and the exponents of X, A and B
+    double bound = 1.0;
+    int ex[65], eb[64];
+    for (int i = 0; i <= steps; ++i) {
+        if (!(bound < 0x1p20 && bound > 0x1p-20)) return EBS_ERR_UNSUPPORTED;
+        ex[i] = headroom(bound);
+        if (i == steps) break;
+        double next, inner;
+        step_bounds(coeff, bound, &next, &inner);
+        eb[i] = headroom(inner) < 60 ? headroom(inner) : 60;
+        bound = next;
+    }
     const OrthoBuffers b = ortho_buffers(batch, rows, cols);
     if (workspace_bytes < b.total) return EBS_ERR_INVALID_ARG;
     const size_t bytes = (size_t)batch * rows * cols * element_size(dtype);
@@ -88,39 +117,38 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     if (pg != po && pg < po + bytes && po < pg + bytes) return EBS_ERR_INVALID_ARG;
     if ((pw < pg + bytes && pg < pw + b.total) || (pw < po + bytes && po < pw + b.total)) return EBS_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    float* x = static_cast<float*>(workspace);
-    float* x2 = reinterpret_cast<float*>(static_cast<char*>(workspace) + b.x);
-    float* A = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * b.x);
-    float* B = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * b.x + b.a);
-    const long long count = (long long)rows * cols;
-    if (dtype == EBS_F32) normalize_kernel<float><<<batch, 1024, 0, st>>>(static_cast<const float*>(g), count, eps, x);
-    else if (dtype == EBS_F16) normalize_kernel<__half><<<batch, 1024, 0, st>>>(static_cast<const __half*>(g), count, eps, x);
-    else normalize_kernel<__nv_bfloat16><<<batch, 1024, 0, st>>>(static_cast<const __nv_bfloat16*>(g), count, eps, x);
+    __half* x = static_cast<__half*>(workspace);
+    __half* x2 = reinterpret_cast<__half*>(static_cast<char*>(workspace) + b.x);
+    __half* A = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x);
+    __half* B = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x + b.a);
+    const float first = ldexpf(1.0f, ex[0]);
+    if (dtype == EBS_F32) normalize_kernel<float><<<batch, 1024, 0, st>>>(static_cast<const float*>(g), rows, cols, eps, first, x, b.ld, b.plane);
+    else if (dtype == EBS_F16) normalize_kernel<__half><<<batch, 1024, 0, st>>>(static_cast<const __half*>(g), rows, cols, eps, first, x, b.ld, b.plane);
+    else normalize_kernel<__nv_bfloat16><<<batch, 1024, 0, st>>>(static_cast<const __nv_bfloat16*>(g), rows, cols, eps, first, x, b.ld, b.plane);
     if ((rc = check_cuda(cudaGetLastError()))) return rc;
     const bool tall = rows > cols;                            // then X X^T X is taken as X (X^T X): the smaller product
     const int m = tall ? cols : rows, n = tall ? rows : cols;
-    const long long sq = (long long)m * m;
     for (int s = 0; s < steps; ++s) {
-        const long long mi = tall ? 1 : cols, ni = tall ? cols : 1;      // element strides of the short and the long side
-        GemmIn ga{x, x, mi, ni, mi, ni, count, count, m, m, n, batch};
-        GemmOut oa;
-        oa.y = A; oa.ldy = m; oa.batch_y = sq;
-        if ((rc = launch_gemm(ga, oa, EBS_F32, EBS_F32, st))) return rc;
-        GemmIn gb{A, A, m, 1, 1, m, sq, sq, m, m, m, batch};
-        GemmOut ob;
-        ob.y = B; ob.ldy = m; ob.batch_y = sq; ob.c = A; ob.alpha = coeff[2]; ob.beta = coeff[1];
-        if ((rc = launch_gemm(gb, ob, EBS_F32, EBS_F32, st))) return rc;
-        GemmIn gx = tall ? GemmIn{x, B, cols, 1, m, 1, count, sq, rows, cols, m, batch} : GemmIn{B, x, m, 1, 1, cols, sq, count, rows, cols, m, batch};
-        GemmOut ox;
-        ox.y = x2; ox.ldy = cols; ox.batch_y = count; ox.c = x; ox.alpha = 1.0f; ox.beta = coeff[0];
-        if ((rc = launch_gemm(gx, ox, EBS_F32, EBS_F32, st))) return rc;
-        float* t = x; x = x2; x2 = t;
+        // A 2^ea = X^T X or X X^T
+        const GemmOperand xs{x, b.ld, tall, 2, b.plane, 2 * b.plane}, as{A, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane}, bs{B, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane};
+        const int ea = 2 * ex[s] - 14;                          // entries of A are at most the square of X's bound: below 2^14
+        PlanesOut oa{A, nullptr, b.side_ld, b.side_plane, 2 * b.side_plane, 0, 0, 0, ldexpf(1.0f, ea - 2 * ex[s]), 0.0f};
+        if ((rc = launch_gemm_tile(xs, xs, GemmShape{m, m, n, batch}, oa, st))) return rc;
+        // B 2^eb = b A + c A^2  (A is symmetric: its rows are its columns)
+        PlanesOut ob{B, A, b.side_ld, b.side_plane, 2 * b.side_plane, b.side_ld, b.side_plane, 2 * b.side_plane, coeff[2] * ldexpf(1.0f, eb[s] - 2 * ea), coeff[1] * ldexpf(1.0f, eb[s] - ea)};
+        if ((rc = launch_gemm_tile(as, as, GemmShape{m, m, m, batch}, ob, st))) return rc;
+        // X 2^ex' = a X + B X or a X + X B
+        PlanesOut ox{x2, x, b.ld, b.plane, 2 * b.plane, b.ld, b.plane, 2 * b.plane, ldexpf(1.0f, ex[s + 1] - eb[s] - ex[s]), coeff[0] * ldexpf(1.0f, ex[s + 1] - ex[s])};
+        const GemmOperand xk{x, b.ld, false, 2, b.plane, 2 * b.plane}, xm{x, b.ld, true, 2, b.plane, 2 * b.plane};
+        if ((rc = tall ? launch_gemm_tile(xk, bs, GemmShape{rows, cols, m, batch}, ox, st) : launch_gemm_tile(bs, xm, GemmShape{rows, cols, m, batch}, ox, st))) return rc;
+        __half* t = x; x = x2; x2 = t;
     }
-    const long long total = count * batch, blocks = (total + 255) / 256;
+    const long long total = (long long)rows * cols * batch, blocks = (total + 255) / 256;
     const int grid = (int)(blocks < 148 * 16 ? blocks : 148 * 16);
-    if (dtype == EBS_F32) scale_out_kernel<float><<<grid, 256, 0, st>>>(x, total, scale, static_cast<float*>(out));
-    else if (dtype == EBS_F16) scale_out_kernel<__half><<<grid, 256, 0, st>>>(x, total, scale, static_cast<__half*>(out));
-    else scale_out_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(x, total, scale, static_cast<__nv_bfloat16*>(out));
+    const float last = scale * ldexpf(1.0f, -ex[steps]);
+    if (dtype == EBS_F32) scale_out_kernel<float><<<grid, 256, 0, st>>>(x, b.ld, b.plane, rows, cols, batch, last, static_cast<float*>(out));
+    else if (dtype == EBS_F16) scale_out_kernel<__half><<<grid, 256, 0, st>>>(x, b.ld, b.plane, rows, cols, batch, last, static_cast<__half*>(out));
+    else scale_out_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(x, b.ld, b.plane, rows, cols, batch, last, static_cast<__nv_bfloat16*>(out));
     return check_cuda(cudaGetLastError());
 }
 
