@@ -84,22 +84,24 @@ __device__ __forceinline__ float scale_pow2(float v, int e) {
     const int h = e >> 1;
     return v * __int_as_float((h + 127) << 23) * __int_as_float((e - h + 127) << 23);
 }
-static __device__ __noinline__ float fp32_dot(const GemmFp32& g, long long row, int col) {
+// (arguments by value: a reference would have the kernel's parameters copied to the stack)
+static __device__ __noinline__ float fp32_dot(const float* a, long long a_red, const float* b, long long b_red, int red) {
     float v = 0.0f;
-    for (int r = 0; r < g.red; ++r) v = fmaf(g.a[row * g.a_row + r * g.a_red], g.b[col * g.b_col + r * g.b_red], v);
+    for (int r = 0; r < red; ++r) v = fmaf(a[r * a_red], b[r * b_red], v);
     return v;
 }
 __device__ __forceinline__ float gemm_unscale(const GemmOut& o, long long row, int col, int row_exp, int col_exp, float v) {
     const int e = row_exp + col_exp;
     if (e < SCALE_NAN / 2) return scale_pow2(v, e);
     if (row_exp == SCALE_NAN || col_exp == SCALE_NAN) return __int_as_float(0x7fffffff);
-    return fp32_dot(o.fp32, row, col);
+    const GemmFp32& f = o.fp32;
+    return fp32_dot(f.a + row * f.a_row, f.a_red, f.b + col * f.b_col, f.b_red, f.red);
 }
 
 // One element: the path of ragged or unaligned outputs.
 template <typename T>
 __device__ __forceinline__ void gemm_store(const GemmOut& o, long long row, int col, float v) {
-    if (o.row_exp) v = gemm_unscale(o, row, col, o.row_exp[row], o.col_exp[col], v);
+    if (sizeof(T) == 4) v = gemm_unscale(o, row, col, o.row_exp[row], o.col_exp[col], v);
     v *= o.alpha;
     if (o.bias) v += to_f32(static_cast<const T*>(o.bias)[col]);
     if (o.z) static_cast<T*>(o.z)[row * o.ldz + col] = from_f32<T>(v);
@@ -130,7 +132,7 @@ template <typename T>
 __device__ __forceinline__ void gemm_store_pack(const GemmOut& o, long long row, int col, float (&v)[16 / sizeof(T)]) {
     constexpr int N = Pack<T>::N;
     float t[N];
-    if (o.row_exp) {
+    if (sizeof(T) == 4) {
         const int re = o.row_exp[row];
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = gemm_unscale(o, row, col + i, re, o.col_exp[col + i], v[i]);

@@ -8,7 +8,7 @@ namespace ebs {
 constexpr int GEMM_CHUNK = 4;                 // stages (of 64 reduction elements) summed in the tensor core at a time, split products
 
 struct TileArgs {
-    int red, out_rows, out_cols;
+    int red, out_rows, out_cols, batch;
     int split, stages;
     int a_mn, b_mn, bf16, packs;
     unsigned wait_limit;
@@ -19,5 +19,15 @@ struct TileArgs {
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmOut& out, int dtype, cudaStream_t st);
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st);
 unsigned long long gemm_tile_timeouts();
+int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmOut& out, int dtype, cudaStream_t st);
+int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st);
+unsigned long long gemm_pair_timeouts();
+
+// The kernel for a product, by its size.
+bool gemm_pair_pays(const GemmShape& s);
+template <class... A>
+inline int launch_gemm(const GemmOperand& a, const GemmOperand& b, const GemmShape& s, const A&... rest) {
+    return gemm_pair_pays(s) ? launch_gemm_pair(a, b, s, rest...) : launch_gemm_tile(a, b, s, rest...);
+}
 
 }  // namespace ebs

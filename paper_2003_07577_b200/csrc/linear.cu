@@ -186,7 +186,7 @@ static int product(const Prepared& a, const Matrix& am, const Prepared& b, const
         o.fp32.b_red = b.op.mn_major ? bm.ld : 1;
         o.fp32.red = red;
     }
-    return launch_gemm_tile(a.op, b.op, s, o, dtype, st);
+    return launch_gemm(a.op, b.op, s, o, dtype, st);
 }
 
 // ---------------------------------------------------------------------------------------------------- dz and dbias
