@@ -90,43 +90,107 @@ __device__ __forceinline__ void split_value(float x, int e, __half& hi, __half& 
     lo = __float2half_rn(v - __half2float(hi));
 }
 
-// Planes of a matrix whose reduction runs along its rows: one exponent a row, a warp a row.
+// Four neighbouring elements of a row, of which `left` exist: one 16-byte access where the rows allow it (VEC).
+template <bool VEC>
+__device__ __forceinline__ float4 load4(const float* p, int left) {
+    if (VEC && left >= 4) return *reinterpret_cast<const float4*>(p);
+    return make_float4(left > 0 ? p[0] : 0.0f, left > 1 ? p[1] : 0.0f, left > 2 ? p[2] : 0.0f, left > 3 ? p[3] : 0.0f);
+}
+__device__ __forceinline__ unsigned magnitude(const float4& v) {
+    const unsigned a = max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu);
+    return max(a, max(__float_as_uint(v.z) & 0x7fffffffu, __float_as_uint(v.w) & 0x7fffffffu));
+}
+// (the planes' rows are padded to whole groups of eight elements: what is written past the end of a row is padding)
+__device__ __forceinline__ void store_split4(__half* hi_plane, __half* lo_plane, const float4& v, int e0, int e1, int e2, int e3) {
+    __half hi[4], lo[4];
+    split_value(v.x, e0, hi[0], lo[0]);
+    split_value(v.y, e1, hi[1], lo[1]);
+    split_value(v.z, e2, hi[2], lo[2]);
+    split_value(v.w, e3, hi[3], lo[3]);
+    *reinterpret_cast<uint2*>(hi_plane) = *reinterpret_cast<const uint2*>(hi);
+    *reinterpret_cast<uint2*>(lo_plane) = *reinterpret_cast<const uint2*>(lo);
+}
+
+// Planes of a matrix whose reduction runs along its rows: one exponent a row.  A row is a warp's or (WIDE) a block's; its first
+// 16 elements a thread stay in registers between the search for the largest and the split.
+template <bool VEC, bool WIDE>
 __global__ void __launch_bounds__(256) split_rows_kernel(const float* __restrict__ src, long long ld, long long rows, int cols, __half* __restrict__ dst,
                                                          long long ldd, int* __restrict__ exps) {
-    const int lane = threadIdx.x & 31;
-    for (long long r = blockIdx.x * 8LL + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8LL) {
+    __shared__ unsigned part[8];
+    constexpr int T = WIDE ? 256 : 32;
+    const int t = WIDE ? threadIdx.x : threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long step = WIDE ? gridDim.x : gridDim.x * 8LL;
+    for (long long r = WIDE ? blockIdx.x : blockIdx.x * 8LL + warp; r < rows; r += step) {
         const float* x = src + r * ld;
+        float4 held[4];
         unsigned top = 0u;
-        for (int c = lane; c < cols; c += 32) top = max(top, __float_as_uint(x[c]) & 0x7fffffffu);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = (i * T + t) * 4;
+            held[i] = load4<VEC>(x + c, cols - c);
+            top = max(top, magnitude(held[i]));
+        }
+        for (int c = (4 * T + t) * 4; c < cols; c += 4 * T) top = max(top, magnitude(load4<VEC>(x + c, cols - c)));
         top = __reduce_max_sync(0xffffffffu, top);
+        if (WIDE) {
+            __syncthreads();                                  // (the previous row's reads are over)
+            if ((threadIdx.x & 31) == 0) part[warp] = top;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, part[i]);
+        }
         const int e = top < 0x7f800000u && top != 0u ? split_exponent(top) : 0;
-        if (lane == 0) exps[r] = split_record(top);
-        for (int c = lane; c < cols; c += 32) split_value(x[c], e, dst[r * ldd + c], dst[rows * ldd + r * ldd + c]);
+        if (t == 0) exps[r] = split_record(top);
+        __half *hi = dst + r * ldd, *lo = hi + rows * ldd;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = (i * T + t) * 4;
+            if (c < cols) store_split4(hi + c, lo + c, held[i], e, e, e, e);
+        }
+        for (int c = (4 * T + t) * 4; c < cols; c += 4 * T) store_split4(hi + c, lo + c, load4<VEC>(x + c, cols - c), e, e, e, e);
     }
 }
-// The largest magnitudes of the columns (their bits, in `top`, which starts at zero).
+// The largest magnitudes of the columns (their bits, in `top`, which starts at zero): 128 columns a block.
+template <bool VEC>
 __global__ void __launch_bounds__(256) column_top_kernel(const float* __restrict__ src, long long ld, long long rows, int cols, unsigned* __restrict__ top) {
-    __shared__ unsigned part[8][32];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), y = threadIdx.x >> 5;
-    unsigned m = 0u;
+    __shared__ unsigned part[8][128];
+    const int lane = threadIdx.x & 31, c = blockIdx.x * 128 + lane * 4, y = threadIdx.x >> 5;
+    unsigned m[4] = {0u, 0u, 0u, 0u};
     if (c < cols)
-        for (long long r = blockIdx.y * 8LL + y; r < rows; r += gridDim.y * 8LL) m = max(m, __float_as_uint(src[r * ld + c]) & 0x7fffffffu);
-    part[y][threadIdx.x & 31] = m;
+#pragma unroll 4
+        for (long long r = blockIdx.y * 8LL + y; r < rows; r += gridDim.y * 8LL) {
+            const float4 v = load4<VEC>(src + r * ld + c, cols - c);
+            m[0] = max(m[0], __float_as_uint(v.x) & 0x7fffffffu);
+            m[1] = max(m[1], __float_as_uint(v.y) & 0x7fffffffu);
+            m[2] = max(m[2], __float_as_uint(v.z) & 0x7fffffffu);
+            m[3] = max(m[3], __float_as_uint(v.w) & 0x7fffffffu);
+        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[y][lane * 4 + i] = m[i];
     __syncthreads();
-    if (y == 0 && c < cols) {
-        for (int i = 1; i < 8; ++i) m = max(m, part[i][threadIdx.x]);
-        atomicMax(top + c, m);
+    if (threadIdx.x < 128 && blockIdx.x * 128 + threadIdx.x < cols) {
+        unsigned v = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v = max(v, part[i][threadIdx.x]);
+        atomicMax(top + blockIdx.x * 128 + threadIdx.x, v);   // (a maximum does not depend on the order)
     }
 }
 // Planes of a matrix whose reduction runs across its rows: one exponent a column, from column_top_kernel.
+template <bool VEC>
 __global__ void __launch_bounds__(256) split_columns_kernel(const float* __restrict__ src, long long ld, long long rows, int cols, const unsigned* __restrict__ top,
                                                             __half* __restrict__ dst, long long ldd, int* __restrict__ exps) {
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), y = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, c = blockIdx.x * 128 + lane * 4, y = threadIdx.x >> 5;
     if (c >= cols) return;
-    const unsigned t = top[c];
-    const int e = t < 0x7f800000u && t != 0u ? split_exponent(t) : 0;
-    if (blockIdx.y == 0 && y == 0) exps[c] = split_record(t);
-    for (long long r = blockIdx.y * 8LL + y; r < rows; r += gridDim.y * 8LL) split_value(src[r * ld + c], e, dst[r * ldd + c], dst[rows * ldd + r * ldd + c]);
+    int e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned t = c + i < cols ? top[c + i] : 0u;
+        e[i] = t < 0x7f800000u && t != 0u ? split_exponent(t) : 0;
+        if (blockIdx.y == 0 && y == 0 && c + i < cols) exps[c + i] = split_record(t);
+    }
+#pragma unroll 4
+    for (long long r = blockIdx.y * 8LL + y; r < rows; r += gridDim.y * 8LL)
+        store_split4(dst + r * ldd + c, dst + (rows + r) * ldd + c, load4<VEC>(src + r * ld + c, cols - c), e[0], e[1], e[2], e[3]);
 }
 
 // An operand of a product: 16-bit rows as they are, or copied where their starts are not on 16 bytes; fp32 rows split.
@@ -140,6 +204,13 @@ struct Matrix {
     int cols;
 };
 static unsigned row_blocks(long long rows, int per) { const long long b = (rows + per - 1) / per; return (unsigned)(b < 2048 ? b : 2048); }
+
+// Row blocks (of at least 32 rows) for kernels that go down `across` blocks of columns: about eight blocks an SM.
+static unsigned column_blocks(long long rows, int across) {
+    long long b = (rows + 31) / 32, want = (8LL * gemm_sm_count() + across - 1) / across;
+    if (b > want) b = want;
+    return (unsigned)(b < 1 ? 1 : b > 65535 ? 65535 : b);
+}
 
 static int prepare_operand(const Matrix& m, int dtype, bool across, Carver& ws, bool run, cudaStream_t st, Prepared* out) {
     out->op = GemmOperand{m.p, m.ld, across};
@@ -161,13 +232,17 @@ static int prepare_operand(const Matrix& m, int dtype, bool across, Carver& ws, 
     out->exps = exps;
     if (!run) return EBS_OK;
     const float* src = static_cast<const float*>(m.p);
+    const bool vec = (m.ld & 3) == 0;
     if (!across) {
-        split_rows_kernel<<<row_blocks(m.rows, 8), 256, 0, st>>>(src, m.ld, m.rows, m.cols, planes, ldd, exps);
+        const bool wide = m.cols > 512;
+        const unsigned grid = row_blocks(m.rows, wide ? 1 : 8);
+        auto kern = wide ? (vec ? split_rows_kernel<true, true> : split_rows_kernel<false, true>) : (vec ? split_rows_kernel<true, false> : split_rows_kernel<false, false>);
+        kern<<<grid, 256, 0, st>>>(src, m.ld, m.rows, m.cols, planes, ldd, exps);
     } else {
         if (check_cuda(cudaMemsetAsync(top, 0, (size_t)m.cols * 4, st))) return EBS_ERR_CUDA;
-        const dim3 grid((m.cols + 31) / 32, row_blocks(m.rows, 64));
-        column_top_kernel<<<grid, 256, 0, st>>>(src, m.ld, m.rows, m.cols, top);
-        split_columns_kernel<<<grid, 256, 0, st>>>(src, m.ld, m.rows, m.cols, top, planes, ldd, exps);
+        const dim3 grid((m.cols + 127) / 128, column_blocks(m.rows, (m.cols + 127) / 128));
+        (vec ? column_top_kernel<true> : column_top_kernel<false>)<<<grid, 256, 0, st>>>(src, m.ld, m.rows, m.cols, top);
+        (vec ? split_columns_kernel<true> : split_columns_kernel<false>)<<<grid, 256, 0, st>>>(src, m.ld, m.rows, m.cols, top, planes, ldd, exps);
     }
     return check_cuda(cudaGetLastError());
 }
@@ -193,31 +268,94 @@ static int product(const Prepared& a, const Matrix& am, const Prepared& b, const
 // A half-precision dz is kept halved: the steepest slope (1.13) times the type's largest value would not fit.
 static float dz_store_scale(const ebs_linear_desc& d) { return d.dtype == EBS_F16 && d.act ? 0.5f : 1.0f; }
 
-// dz = dy * act'(z), stored times `store`, and the column sums of dz before its rounding: 32 columns a thread block, every row.
-template <typename T>
-__global__ void __launch_bounds__(256) linear_dz_kernel(const T* dy, long long ldy, const T* z, long long ldz, int m, int n, int act, float store, T* dz, long long lddz, T* dbias) {
-    __shared__ float part[8][33];
-    const int col = blockIdx.x * 32 + (threadIdx.x & 31), lane_row = threadIdx.x >> 5;
-    float sum = 0.0f;
+// dz = dy * act'(z), stored times `store`, and the column sums of dz before its rounding.  A block takes 32 packs of N columns and
+// the rows of one of gridDim.y chunks; the sums of a chunk go to `part`, or (one chunk) to dbias at once.
+template <typename T, int N>
+__global__ void __launch_bounds__(256) linear_dz_kernel(const T* __restrict__ dy, long long ldy, const T* __restrict__ z, long long ldz, int m, int n, int act, float store,
+                                                        T* __restrict__ dz, long long lddz, T* __restrict__ dbias, float* __restrict__ part) {
+    __shared__ float sums[8][32 * N + 4];
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, col = (blockIdx.x * 32 + lane) * N;
+    const long long r0 = (long long)m * blockIdx.y / gridDim.y, r1 = (long long)m * (blockIdx.y + 1) / gridDim.y;
+    float sum[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[e] = 0.0f;
     if (col < n) {
-        for (long long r = lane_row; r < m; r += 8) {
-            float v = to_f32(dy[r * ldy + col]);
-            if (act) v *= activation_slope(to_f32(z[r * ldz + col]), act);
-            if (dz) dz[r * lddz + col] = from_f32<T>(v * store);
-            sum += v;
+#pragma unroll 2
+        for (long long r = r0 + y; r < r1; r += 8) {
+            float v[N], zv[N];
+            const bool whole = N > 1 && col + N <= n;
+            if (whole) {
+                if constexpr (N > 1) load_pack(dy + r * ldy + col, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = col + e < n ? to_f32(dy[r * ldy + col + e]) : 0.0f;
+            }
+            if (act) {
+                if (whole) {
+                    if constexpr (N > 1) load_pack(z + r * ldz + col, zv);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) zv[e] = col + e < n ? to_f32(z[r * ldz + col + e]) : 0.0f;
+                }
+                switch (act) {
+#define EBS_SLOPE_CASE(A) case A: _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] *= activation_slope(zv[e], A); break;
+                    EBS_SLOPE_CASE(EBS_ACT_RELU) EBS_SLOPE_CASE(EBS_ACT_GELU) EBS_SLOPE_CASE(EBS_ACT_GELU_TANH) EBS_SLOPE_CASE(EBS_ACT_SILU)
+#undef EBS_SLOPE_CASE
+                    default: break;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum[e] += v[e];
+            if (dz) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] *= store;
+                if (N > 1) {                                  // (rows of dz are padded to whole packs)
+                    if constexpr (N > 1) store_pack(dz + r * lddz + col, v);
+                } else {
+                    dz[r * lddz + col] = from_f32<T>(v[0]);
+                }
+            }
         }
     }
-    part[lane_row][threadIdx.x & 31] = sum;
+    if (!dbias) return;
+#pragma unroll
+    for (int e = 0; e < N; ++e) sums[y][lane * N + e] = sum[e];
     __syncthreads();
-    if (lane_row == 0 && col < n && dbias) {
-        for (int i = 1; i < 8; ++i) sum += part[i][threadIdx.x];
-        dbias[col] = from_f32<T>(sum);
+    for (int i = threadIdx.x; i < 32 * N; i += 256) {
+        const int c = blockIdx.x * 32 * N + i;
+        if (c >= n) break;
+        float s = 0.0f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s += sums[q][i];
+        if (gridDim.y == 1) dbias[c] = from_f32<T>(s);
+        else part[(size_t)blockIdx.y * n + c] = s;
     }
 }
 template <typename T>
-static int launch_dz(const void* dy, const void* z, const ebs_linear_desc& d, void* dz, long long lddz, void* dbias, cudaStream_t st) {
-    linear_dz_kernel<T><<<(d.n + 31) / 32, 256, 0, st>>>(static_cast<const T*>(dy), d.ldy, static_cast<const T*>(z), d.ldz, d.m, d.n, d.act, dz_store_scale(d), static_cast<T*>(dz), lddz,
-                                                         static_cast<T*>(dbias));
+__global__ void __launch_bounds__(256) linear_dbias_kernel(const float* __restrict__ part, int chunks, int n, T* __restrict__ dbias) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= n) return;
+    float s = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < chunks; ++i) s += part[(size_t)i * n + c];
+    dbias[c] = from_f32<T>(s);
+}
+
+// Chunks of rows the sums are taken in, from the sizes alone: about four blocks an SM, at least 32 rows each.
+static int dz_chunks(const ebs_linear_desc& d) {
+    const int packs = d.dtype == EBS_F32 ? 128 : 256, across = (d.n + packs - 1) / packs;
+    long long c = (d.m + 31) / 32, want = (4LL * 148 + across - 1) / across;
+    return (int)(c < want ? c : want);
+}
+template <typename T>
+static int launch_dz(const void* dy, const void* z, const ebs_linear_desc& d, void* dz, long long lddz, void* dbias, float* part, cudaStream_t st) {
+    constexpr int N = Pack<T>::N;
+    const bool packs = d.ldy % N == 0 && (!d.act || d.ldz % N == 0);
+    const int chunks = dz_chunks(d), per = packs ? 32 * N : 32;
+    const dim3 grid((d.n + per - 1) / per, chunks);
+    auto kern = packs ? linear_dz_kernel<T, N> : linear_dz_kernel<T, 1>;
+    kern<<<grid, 256, 0, st>>>(static_cast<const T*>(dy), d.ldy, static_cast<const T*>(z), d.ldz, d.m, d.n, d.act, dz_store_scale(d), static_cast<T*>(dz), lddz, static_cast<T*>(dbias), part);
+    if (dbias && chunks > 1) linear_dbias_kernel<T><<<(d.n + 255) / 256, 256, 0, st>>>(part, chunks, d.n, static_cast<T*>(dbias));
     return check_cuda(cudaGetLastError());
 }
 
@@ -256,10 +394,11 @@ static int backward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws
             dm.p = dz;
             dm.ld = ld;
         }
+        float* part = dz_chunks(d) > 1 ? ws.take<float>((size_t)dz_chunks(d) * d.n) : nullptr;
         if (run) {
-            if (d.dtype == EBS_F32) rc = launch_dz<float>(t.dy, t.z, d, dz, dm.ld, t.dbias, st);
-            else if (d.dtype == EBS_F16) rc = launch_dz<__half>(t.dy, t.z, d, dz, dm.ld, t.dbias, st);
-            else rc = launch_dz<__nv_bfloat16>(t.dy, t.z, d, dz, dm.ld, t.dbias, st);
+            if (d.dtype == EBS_F32) rc = launch_dz<float>(t.dy, t.z, d, dz, dm.ld, t.dbias, part, st);
+            else if (d.dtype == EBS_F16) rc = launch_dz<__half>(t.dy, t.z, d, dz, dm.ld, t.dbias, part, st);
+            else rc = launch_dz<__nv_bfloat16>(t.dy, t.z, d, dz, dm.ld, t.dbias, part, st);
             if (rc) return rc;
         }
     }

@@ -10,29 +10,46 @@ static size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
 // Matrices are kept as two fp16 planes hi + lo (22 bits) times a power of two: X by 2^-ex, its Gram matrix A by 2^-ea and
 // B = b A + c A^2 by 2^-eb, chosen from bounds of the singular values so that no entry leaves fp16 (an entry is at most the
 // largest singular value).
-// X = G / (|G|_F + eps), one thread block a matrix, the sum of squares in 64 bits in a fixed order.
+// Sums of squares in 64 bits, a part of each matrix a thread block (blockIdx.y: the matrix), in an order that depends on sizes alone.
 template <typename T>
-__global__ void __launch_bounds__(1024) normalize_kernel(const T* g, int rows, int cols, float eps, float store, __half* x, long long ld, long long plane) {
-    __shared__ double part[1024];
-    const long long count = (long long)rows * cols;
-    g += blockIdx.x * count;
-    x += blockIdx.x * 2 * plane;
+__global__ void __launch_bounds__(256) sum_squares_kernel(const T* __restrict__ g, long long count, double* __restrict__ part) {
+    __shared__ double sums[8];
+    g += blockIdx.y * count;
     double s = 0.0;
-    for (long long i = threadIdx.x; i < count; i += 1024) { const double v = to_f32(g[i]); s += v * v; }
-    part[threadIdx.x] = s;
+#pragma unroll 4
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < count; i += gridDim.x * 256LL) { const double v = to_f32(g[i]); s += v * v; }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
     __syncthreads();
-    for (int o = 512; o > 0; o >>= 1) {
-        if (threadIdx.x < o) part[threadIdx.x] += part[threadIdx.x + o];
-        __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i) s += sums[i];
+        part[blockIdx.y * gridDim.x + blockIdx.x] = s;
     }
-    const double inv = store / (sqrt(part[0]) + (double)eps);
-    for (long long i = threadIdx.x; i < count; i += 1024) {
-        const long long at = i / cols * ld + i % cols;
-        const float v = (float)(to_f32(g[i]) * inv);
-        const __half hi = __float2half_rn(v);
-        x[at] = hi;
-        x[plane + at] = __float2half_rn(v - __half2float(hi));
-    }
+}
+// X = G / (|G|_F + eps), times `store`, as planes; parts: thread blocks of sum_squares_kernel a matrix.
+template <typename T>
+__global__ void __launch_bounds__(256) normalize_kernel(const T* __restrict__ g, int rows, int cols, float eps, float store, const double* __restrict__ part, int parts,
+                                                        __half* __restrict__ x, long long ld, long long plane) {
+    g += (long long)blockIdx.z * rows * cols;
+    x += blockIdx.z * 2 * plane;
+    double s = 0.0;
+    for (int i = 0; i < parts; ++i) s += part[blockIdx.z * parts + i];
+    const double inv = store / (sqrt(s) + (double)eps);
+    for (int r = blockIdx.y; r < rows; r += gridDim.y)
+        for (int c = blockIdx.x * 256 + threadIdx.x; c < cols; c += gridDim.x * 256) {
+            const float v = (float)(to_f32(g[(long long)r * cols + c]) * inv);
+            const __half hi = __float2half_rn(v);
+            x[r * ld + c] = hi;
+            x[plane + r * ld + c] = __float2half_rn(v - __half2float(hi));
+        }
+}
+template <typename T>
+static void launch_normalize(const void* g, int batch, int rows, int cols, float eps, float store, double* part, int parts, __half* x, long long ld, long long plane,
+                             cudaStream_t st) {
+    sum_squares_kernel<T><<<dim3(parts, batch), 256, 0, st>>>(static_cast<const T*>(g), (long long)rows * cols, part);
+    const dim3 grid((cols + 255) / 256, rows < 1024 ? rows : 1024, batch);
+    normalize_kernel<T><<<grid, 256, 0, st>>>(static_cast<const T*>(g), rows, cols, eps, store, part, parts, x, ld, plane);
 }
 template <typename T>
 __global__ void __launch_bounds__(256) scale_out_kernel(const __half* x, long long ld, long long plane, int rows, int cols, int batch, float scale, T* out) {
@@ -59,7 +76,8 @@ static int headroom(double v) { int e; frexp(v > 0.0 ? v : 1.0, &e); return 14 -
 
 struct OrthoBuffers {
     long long ld, plane, side_ld, side_plane;
-    size_t x, a, total;
+    size_t x, a, part, total;
+    int parts;                                                // sums of squares a matrix
 };
 static OrthoBuffers ortho_buffers(int batch, int rows, int cols) {
     const long long side = rows < cols ? rows : cols;
@@ -70,7 +88,10 @@ static OrthoBuffers ortho_buffers(int batch, int rows, int cols) {
     b.side_plane = b.side_ld * side;
     b.x = round256((size_t)batch * 2 * b.plane * 2);
     b.a = round256((size_t)batch * 2 * b.side_plane * 2);
-    b.total = 2 * b.x + 2 * b.a;
+    const long long parts = ((long long)rows * cols + 8191) / 8192;
+    b.parts = (int)(parts < 128 ? parts : 128);
+    b.part = round256((size_t)batch * b.parts * 8);
+    b.total = 2 * b.x + 2 * b.a + b.part;
     return b;
 }
 static int check_shape(int batch, int rows, int cols, int dtype, int steps) {
@@ -122,9 +143,10 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     __half* A = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x);
     __half* B = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x + b.a);
     const float first = ldexpf(1.0f, ex[0]);
-    if (dtype == EBS_F32) normalize_kernel<float><<<batch, 1024, 0, st>>>(static_cast<const float*>(g), rows, cols, eps, first, x, b.ld, b.plane);
-    else if (dtype == EBS_F16) normalize_kernel<__half><<<batch, 1024, 0, st>>>(static_cast<const __half*>(g), rows, cols, eps, first, x, b.ld, b.plane);
-    else normalize_kernel<__nv_bfloat16><<<batch, 1024, 0, st>>>(static_cast<const __nv_bfloat16*>(g), rows, cols, eps, first, x, b.ld, b.plane);
+    double* part = reinterpret_cast<double*>(static_cast<char*>(workspace) + 2 * b.x + 2 * b.a);
+    if (dtype == EBS_F32) launch_normalize<float>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
+    else if (dtype == EBS_F16) launch_normalize<__half>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
+    else launch_normalize<__nv_bfloat16>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
     if ((rc = check_cuda(cudaGetLastError()))) return rc;
     const bool tall = rows > cols;                            // then X X^T X is taken as X (X^T X): the smaller product
     const int m = tall ? cols : rows, n = tall ? rows : cols;
