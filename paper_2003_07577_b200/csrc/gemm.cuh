@@ -20,35 +20,83 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
 inline size_t element_size(int dtype) { return dtype == EBS_F32 ? 4 : 2; }
 inline bool real_dtype(int dtype) { return dtype == EBS_F32 || dtype == EBS_F16 || dtype == EBS_BF16; }
 
+// Elementary functions at the accuracy of the results' type: fp32 results take CUDA's functions, 16-bit results (rounding 2^-9 or 2^-12)
+// the hardware exponential and reciprocal (relative error about 2^-21).
+template <bool FAST> __device__ __forceinline__ float exp_of(float v) { return FAST ? __expf(v) : expf(v); }
+template <bool FAST> __device__ __forceinline__ float quotient(float a, float b) { return FAST ? __fdividef(a, b) : a / b; }
 // The logistic function of v and its complement, neither taken as a difference: both keep their relative accuracy.
+template <bool FAST>
 __device__ __forceinline__ void logistic(float v, float& s, float& rest) {
-    const float t = expf(-fabsf(v)), r = 1.0f / (1.0f + t), tr = t * r;
+    const float t = exp_of<FAST>(-fabsf(v)), r = quotient<FAST>(1.0f, 1.0f + t), tr = t * r;
     s = v >= 0.0f ? r : tr;
     rest = v >= 0.0f ? tr : r;
 }
+// (1 + erf(z / sqrt 2)) / 2, and exp(-z^2 / 2).  16-bit results: Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26, absolute
+// error 1.5e-7; the exponential serves both.
+template <bool FAST>
+__device__ __forceinline__ void normal_cdf(float z, float& cdf, float& bell) {
+    if (FAST) {
+        const float a = fabsf(z) * 0.70710678f, t = __fdividef(1.0f, fmaf(0.3275911f, a, 1.0f));
+        bell = __expf(-a * a);
+        const float half_tail = 0.5f * bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+        cdf = z >= 0.0f ? 1.0f - half_tail : half_tail;
+        if (z != z) cdf = z;
+    } else {
+        bell = expf(-0.5f * z * z);
+        cdf = 0.5f * (1.0f + erff(z * 0.70710678f));
+    }
+}
 // act(z) and act'(z) as include/ebs.h states them.  (1 + tanh u) / 2 is the logistic function of 2u.
+template <bool FAST>
 __device__ __forceinline__ float activation(float z, int act) {
+    float s, e;
     switch (act) {
         case EBS_ACT_RELU: return z > 0.0f ? z : 0.0f;
-        case EBS_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-        case EBS_ACT_GELU_TANH: return z / (1.0f + expf(-1.59576912f * (z + 0.044715f * z * z * z)));
-        case EBS_ACT_SILU: return z / (1.0f + expf(-z));
+        case EBS_ACT_GELU: normal_cdf<FAST>(z, s, e); return z * s;
+        case EBS_ACT_GELU_TANH: logistic<FAST>(1.59576912f * (z + 0.044715f * z * z * z), s, e); return z * s;
+        case EBS_ACT_SILU: logistic<FAST>(z, s, e); return z * s;
         default: return z;
     }
 }
+template <bool FAST>
 __device__ __forceinline__ float activation_slope(float z, int act) {
     float s, rest;
     switch (act) {
         case EBS_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-        case EBS_ACT_GELU: return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * (0.39894228f * expf(-0.5f * z * z));
+        case EBS_ACT_GELU: normal_cdf<FAST>(z, s, rest); return fmaf(z * 0.39894228f, rest, s);
         case EBS_ACT_GELU_TANH:
-            logistic(1.59576912f * (z + 0.044715f * z * z * z), s, rest);
+            logistic<FAST>(1.59576912f * (z + 0.044715f * z * z * z), s, rest);
             return s * (1.0f + z * rest * (1.59576912f * (1.0f + 0.134145f * z * z)));
         case EBS_ACT_SILU:
-            logistic(z, s, rest);
+            logistic<FAST>(z, s, rest);
             return s * (1.0f + z * rest);
         default: return 1.0f;
     }
+}
+
+// Kernels of one call start while the one before them still runs (programmatic launches): each waits here, before it touches memory, for
+// that one's end and results ...
+__device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+// ... and lets the next one start once all its own blocks run.  A block that holds tensor memory calls this after it got it: the next
+// kernel's blocks may take what is left.
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
+
+template <typename... P, typename... A>
+inline int launch_chained(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, A&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return check_cuda(cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...));
 }
 
 // Powers of two that fp32 operands are scaled by before they are split (linear.cu): one exponent a row or column.
@@ -105,7 +153,7 @@ __device__ __forceinline__ void gemm_store(const GemmOut& o, long long row, int 
     v *= o.alpha;
     if (o.bias) v += to_f32(static_cast<const T*>(o.bias)[col]);
     if (o.z) static_cast<T*>(o.z)[row * o.ldz + col] = from_f32<T>(v);
-    if (o.act) v = activation(v, o.act);
+    if (o.act) v = activation<sizeof(T) == 2>(v, o.act);
     if (o.residual) v += to_f32(static_cast<const T*>(o.residual)[row * o.ldr + col]);
     static_cast<T*>(o.y)[row * o.ldy + col] = from_f32<T>(v);
 }
@@ -127,34 +175,62 @@ __device__ __forceinline__ void store_pack(T* p, const float (&v)[16 / sizeof(T)
     for (int i = 0; i < Pack<T>::N; ++i) e[i] = from_f32<T>(v[i]);
     *reinterpret_cast<uint4*>(p) = u;
 }
-// 16 bytes of neighbouring columns of one row, every address 16-byte aligned.
+// Packs of neighbouring columns of one row, every address 16-byte aligned.  What a pack needs from memory is loaded ahead: what depends on
+// the columns once for all rows of a thread, what depends on the row before the sums arrive.
 template <typename T>
-__device__ __forceinline__ void gemm_store_pack(const GemmOut& o, long long row, int col, float (&v)[16 / sizeof(T)]) {
+struct GemmColumns {
+    float bias[Pack<T>::N];
+    int exp[sizeof(T) == 4 ? Pack<T>::N : 1];
+};
+struct GemmAhead {
+    uint4 residual;
+    int row_exp;
+};
+template <typename T>
+__device__ __forceinline__ void gemm_columns(const GemmOut& o, int col, GemmColumns<T>& c) {
+    if (o.bias) load_pack(static_cast<const T*>(o.bias) + col, c.bias);
+    else
+#pragma unroll
+        for (int i = 0; i < Pack<T>::N; ++i) c.bias[i] = 0.0f;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < Pack<T>::N; ++i) c.exp[i] = o.col_exp[col + i];
+    }
+}
+template <typename T>
+__device__ __forceinline__ void gemm_ahead(const GemmOut& o, long long row, int col, GemmAhead& a) {
+    if (o.residual) a.residual = *reinterpret_cast<const uint4*>(static_cast<const T*>(o.residual) + row * o.ldr + col);
+    if (sizeof(T) == 4) a.row_exp = o.row_exp[row];
+}
+template <typename T>
+__device__ __forceinline__ void gemm_store_pack(const GemmOut& o, long long row, int col, float (&v)[16 / sizeof(T)], const GemmColumns<T>& c, const GemmAhead& a) {
     constexpr int N = Pack<T>::N;
-    float t[N];
-    if (sizeof(T) == 4) {
-        const int re = o.row_exp[row];
+    constexpr bool FAST = sizeof(T) == 2;
+    if constexpr (sizeof(T) == 4) {
+        bool plain = true;
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = gemm_unscale(o, row, col + i, re, o.col_exp[col + i], v[i]);
+        for (int i = 0; i < N; ++i) plain = plain && a.row_exp + c.exp[i] < SCALE_NAN / 2;
+        if (plain) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = scale_pow2(v[i], a.row_exp + c.exp[i]);
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < N; ++i) v[i] = gemm_unscale(o, row, col + i, a.row_exp, o.col_exp[col + i], v[i]);
+        }
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] *= o.alpha;
-    if (o.bias) {
-        load_pack(static_cast<const T*>(o.bias) + col, t);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += t[i];
-    }
+    for (int i = 0; i < N; ++i) v[i] = fmaf(v[i], o.alpha, c.bias[i]);      // (alpha: a power of two, the product is exact)
     if (o.z) store_pack(static_cast<T*>(o.z) + row * o.ldz + col, v);
     switch (o.act) {                                        // (outside the loop: one branch a pack)
-#define EBS_ACT_CASE(A) case A: _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = activation(v[i], A); break;
+#define EBS_ACT_CASE(A) case A: _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = activation<FAST>(v[i], A); break;
         EBS_ACT_CASE(EBS_ACT_RELU) EBS_ACT_CASE(EBS_ACT_GELU) EBS_ACT_CASE(EBS_ACT_GELU_TANH) EBS_ACT_CASE(EBS_ACT_SILU)
 #undef EBS_ACT_CASE
         default: break;
     }
     if (o.residual) {
-        load_pack(static_cast<const T*>(o.residual) + row * o.ldr + col, t);
+        const T* t = reinterpret_cast<const T*>(&a.residual);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += t[i];
+        for (int i = 0; i < N; ++i) v[i] += to_f32(t[i]);
     }
     store_pack(static_cast<T*>(o.y) + row * o.ldy + col, v);
 }
@@ -168,11 +244,14 @@ inline bool packs_ok(const GemmOut& o, size_t size) {
 // each of `batch` (batch_stride apart), with the reduction along a row (mn_major = false: rows = the result's rows or columns) or
 // across rows (mn_major = true: rows = reduction).  Base and strides are multiples of 16 bytes.
 struct GemmOperand {
-    const void* p;
-    long long ld;
-    bool mn_major;
+    const void* p = nullptr;
+    long long ld = 0;
+    bool mn_major = false;
     int planes = 1;
     long long plane_stride = 0, batch_stride = 0;
+    GemmOperand() = default;
+    GemmOperand(const void* p_, long long ld_, bool mn_major_, int planes_ = 1, long long plane_stride_ = 0, long long batch_stride_ = 0)
+        : p(p_), ld(ld_), mn_major(mn_major_), planes(planes_), plane_stride(plane_stride_), batch_stride(batch_stride_) {}
 };
 
 }  // namespace ebs

@@ -12,6 +12,7 @@ namespace ebs {
 
 static __device__ unsigned long long g_gemm_pair_timeouts = 0ull;
 
+constexpr int PAIR_THREADS = 384;                                // three warpgroups: two that take sums out, one that fetches and issues (two of its warps idle)
 constexpr int PAIR_HALF = 128 * GEMM_ROW_BYTES;                  // 128 rows of 64 elements
 template <int PL> __host__ __device__ constexpr int pair_stage_bytes() { return 2 * PL * PAIR_HALF; }
 template <int PL> __host__ __device__ constexpr int pair_stages() { return PL == 1 ? 5 : 3; }
@@ -75,7 +76,7 @@ __device__ __forceinline__ void pair_tile(int t, int tiles_m, int tiles_n, int& 
 }
 
 template <class EPI, int PL>
-__global__ void __launch_bounds__(320, 1) gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+__global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                            const TileArgs g, const EPI epi) {
     extern __shared__ uint8_t smem_raw[];
     constexpr int S = pair_stages<PL>(), STAGE = pair_stage_bytes<PL>(), PC = pair_patch_columns<PL>(), PITCH = PC + 4;
@@ -103,8 +104,15 @@ __global__ void __launch_bounds__(320, 1) gemm_pair_kernel(const __grid_constant
     cluster_sync_all();                                           // the partner's barriers are ready too
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     const uint32_t tmem = uni(tmem_slot);
+    let_next_kernel_start();
+    wait_for_previous_kernel();
 
-    if (warp == 8) {
+    // Split products keep 128 sums a thread.  Registers are dealt anew among the warpgroups: 2 * 128 * 208 + 128 * 80 = 63488 of the
+    // 384 * 168 = 64512 the block was launched with.  (Each at the head of its warpgroup's own code: the compiler counts registers by
+    // what it can reach.)
+    if (warp >= 8) {
+      if (PL == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
+      if (warp == 8) {
         const bool leader = elect_one();
         int i = 0;                                                // stages filled so far
         bool ok = true;
@@ -132,8 +140,7 @@ __global__ void __launch_bounds__(320, 1) gemm_pair_kernel(const __grid_constant
                 __syncwarp();
             }
         }
-    } else if (warp == 9) {
-        if (rank == 0) {
+      } else if (warp == 9 && rank == 0) {
             const uint32_t leader = elect_one() ? 1u : 0u;
             const uint32_t idesc = gemm_idesc(256, 256, g.bf16, g.a_mn, g.b_mn);
             const uint32_t a_step = g.a_mn ? 2048 >> 4 : 32 >> 4, b_step = g.b_mn ? 2048 >> 4 : 32 >> 4;
@@ -165,8 +172,9 @@ __global__ void __launch_bounds__(320, 1) gemm_pair_kernel(const __grid_constant
                     c += last;
                 }
             }
-        }
+      }
     } else {
+        if (PL == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
         float* patch = reinterpret_cast<float*>(tiles + S * STAGE) + warp * 32 * PITCH;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * 128;
         constexpr int N = EPI::N, PER_ROW = PC / N, ROWS = 32 / PER_ROW;
@@ -176,17 +184,32 @@ __global__ void __launch_bounds__(320, 1) gemm_pair_kernel(const __grid_constant
             int batch, tm, tn;
             pair_tile(t, tiles_m, tiles_n, batch, tm, tn);
             const int row0 = tm * 256 + rank * 128 + (warp & 3) * 32, col0 = tn * 256 + (warp >> 2) * 128;
+            constexpr int STEPS = 32 / ROWS;
+            const int pack_col = (lane % PER_ROW) * N, pack_row = row0 + lane / PER_ROW;
+            typename EPI::Columns columns;
+            typename EPI::Ahead ahead[STEPS];
+            bool whole = false;
+            auto load_ahead = [&](int column) {                   // what the packs of these columns need, before the sums are there
+                const int col = col0 + column + pack_col;
+                whole = g.packs && col + N <= g.out_cols;
+                if (!whole) return;
+                epi.columns(col, columns);
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i)
+                    if (pack_row + i * ROWS < g.out_rows) epi.ahead(batch, pack_row + i * ROWS, col, ahead[i]);
+            };
             auto write = [&](int column) {                        // the patch's columns of this warp's rows
                 __syncwarp();
-#pragma unroll 1
-                for (int r = lane / PER_ROW; r < 32; r += ROWS) {
-                    const int row = row0 + r, col = col0 + column + (lane % PER_ROW) * N;
+                const int col = col0 + column + pack_col;
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) {
+                    const int row = pack_row + i * ROWS;
                     float v[N];
-                    const float* p = patch + r * PITCH + (lane % PER_ROW) * N;
+                    const float* p = patch + (lane / PER_ROW + i * ROWS) * PITCH + pack_col;
 #pragma unroll
                     for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(v + e) = *reinterpret_cast<const float4*>(p + e);
                     if (row >= g.out_rows || col >= g.out_cols) continue;
-                    if (g.packs && col + N <= g.out_cols) epi.pack(batch, row, col, v);
+                    if (whole) epi.pack(batch, row, col, v, columns, ahead[i]);
                     else
 #pragma unroll
                         for (int e = 0; e < N; ++e)
@@ -230,6 +253,7 @@ __global__ void __launch_bounds__(320, 1) gemm_pair_kernel(const __grid_constant
                         case 6: put(acc + 96); break;
                         default: put(acc + 112); break;
                     }
+                    load_ahead(j * 16);
                     write(j * 16);
                 }
             } else {
@@ -240,6 +264,7 @@ __global__ void __launch_bounds__(320, 1) gemm_pair_kernel(const __grid_constant
                 for (int j = 0; j < 128; j += 32) {
                     uint32_t v[32];
                     tmem_ld32_issue(lanes + (c & 1) * 256 + j, v);
+                    load_ahead(j);
                     tmem_ld32_wait(v);
                     if (j == 96) {
                         asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
@@ -295,18 +320,7 @@ static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmSha
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
     const int pairs = gemm_sm_count() / 2;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)), 1, 1);
-    cfg.blockDim = dim3(320, 1, 1);
-    cfg.dynamicSmemBytes = pair_smem_bytes<PL>();
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return check_cuda(cudaLaunchKernelEx(&cfg, kern, a, b, g, epi));
+    return launch_chained(kern, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), PAIR_THREADS, pair_smem_bytes<PL>(), st, 2, a, b, g, epi);
 }
 
 bool gemm_pair_pays(const GemmShape& s) {
@@ -322,6 +336,12 @@ int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape
 }
 int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st) {
     return launch_pair<PlanesOut, 2>(A, B, s, out, false, out.ld % 4 == 0, st);
+}
+int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const FinalOut& out, int dtype, cudaStream_t st) {
+    const bool packs = out.ld * (long long)element_size(dtype) % 16 == 0 && (out.batch * (long long)element_size(dtype)) % 16 == 0;
+    if (dtype == EBS_F32) return launch_pair<TypedFinal<float>, 2>(A, B, s, {out}, false, packs, st);
+    if (dtype == EBS_F16) return launch_pair<TypedFinal<__half>, 2>(A, B, s, {out}, false, packs, st);
+    return launch_pair<TypedFinal<__nv_bfloat16>, 2>(A, B, s, {out}, false, packs, st);
 }
 
 }  // namespace ebs

@@ -53,6 +53,8 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     const uint32_t tmem = uni(tmem_slot);
+    let_next_kernel_start();
+    wait_for_previous_kernel();
 
     float acc[PL == 2 ? TN / 2 : 1];                              // (split products: this thread's sums)
     if (warp == 8) {
@@ -169,36 +171,57 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     if (!skip) {
         const int outer0 = SWAP ? b0 : a0, inner0 = SWAP ? a0 : b0;
         const int o_begin = OUTER * part / split, o_end = OUTER * (part + 1) / split;
-        constexpr int N = EPI::N;
-        const bool packs = g.packs != 0;
-        for (int i = threadIdx.x; i < (o_end - o_begin) * (INNER / N); i += 320) {
-            const int o = o_begin + i / (INNER / N), n = (i % (INNER / N)) * N;
-            const int orow = outer0 + o, ocol = inner0 + n;
-            if (orow >= g.out_rows || ocol >= g.out_cols) continue;
-            float v[N];
-            const float* at = exchange + o * PITCH + n;
-            if (split == 1) {
+        constexpr int N = EPI::N, PER_ROW = INNER / N, STEP = 4;
+        // a thread keeps its pack of columns; 320 threads: rows STRIDE apart
+        constexpr int STRIDE = 320 / PER_ROW;
+        static_assert(PER_ROW <= 64 && STRIDE >= 1, "packs of a row");
+        const int n = (threadIdx.x % PER_ROW) * N, ocol = inner0 + n;
+        const bool whole = g.packs && ocol + N <= g.out_cols;
+        typename EPI::Columns columns;
+        if (whole) epi.columns(ocol, columns);
+        if (ocol < g.out_cols && (int)threadIdx.x < STRIDE * PER_ROW)
+            for (int first = o_begin + threadIdx.x / PER_ROW; first < o_end; first += STEP * STRIDE) {
+                typename EPI::Ahead ahead[STEP];
+                float v[STEP][N];
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[e] = at[e];
-            } else {
+                for (int i = 0; i < STEP; ++i) {
+                    const int o = first + i * STRIDE, orow = outer0 + o;
+                    if (whole && o < o_end && orow < g.out_rows) epi.ahead(batch, orow, ocol, ahead[i]);
+                }
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[e] = 0.0f;
-                for (int q = 0; q < split; ++q) {
-                    const uint32_t addr = cluster_addr(at, q);
+                for (int i = 0; i < STEP; ++i) {
+                    const int o = first + i * STRIDE;
+                    if (o >= o_end) continue;
+                    const float* at = exchange + o * PITCH + n;
+                    if (split == 1) {
 #pragma unroll
-                    for (int e = 0; e < N; e += 4) {
-                        float4 t;
-                        asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];\n" : "=f"(t.x), "=f"(t.y), "=f"(t.z), "=f"(t.w) : "r"(addr + 4 * e));
-                        v[e] += t.x; v[e + 1] += t.y; v[e + 2] += t.z; v[e + 3] += t.w;
+                        for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(&v[i][e]) = *reinterpret_cast<const float4*>(at + e);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < N; ++e) v[i][e] = 0.0f;
+#pragma unroll 4
+                        for (int q = 0; q < split; ++q) {
+                            const uint32_t addr = cluster_addr(at, q);
+#pragma unroll
+                            for (int e = 0; e < N; e += 4) {
+                                float4 t;
+                                asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];\n" : "=f"(t.x), "=f"(t.y), "=f"(t.z), "=f"(t.w) : "r"(addr + 4 * e));
+                                v[i][e] += t.x; v[i][e + 1] += t.y; v[i][e + 2] += t.z; v[i][e + 3] += t.w;
+                            }
+                        }
                     }
                 }
-            }
-            if (packs && ocol + N <= g.out_cols) epi.pack(batch, orow, ocol, v);
-            else
 #pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (ocol + e < g.out_cols) epi.one(batch, orow, ocol + e, v[e]);
-        }
+                for (int i = 0; i < STEP; ++i) {
+                    const int o = first + i * STRIDE, orow = outer0 + o;
+                    if (o >= o_end || orow >= g.out_rows) continue;
+                    if (whole) epi.pack(batch, orow, ocol, v[i], columns, ahead[i]);
+                    else
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            if (ocol + e < g.out_cols) epi.one(batch, orow, ocol + e, v[i][e]);
+                }
+            }
     }
     if (split > 1) cluster_sync_all();                            // no block leaves while another reads its sums
     if (gave_up) {
@@ -232,18 +255,8 @@ static int launch_tile(const CUtensorMap& a, const CUtensorMap& b, TileArgs g, c
         if (check_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024))) return EBS_ERR_CUDA;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((lanes + 127) / 128 * g.split), (unsigned)((columns + TN - 1) / TN), (unsigned)batch);
-    cfg.blockDim = dim3(320, 1, 1);
-    cfg.dynamicSmemBytes = (size_t)bytes;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)g.split;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return check_cuda(cudaLaunchKernelEx(&cfg, kern, a, b, g, epi));
+    const dim3 grid((unsigned)((lanes + 127) / 128 * g.split), (unsigned)((columns + TN - 1) / TN), (unsigned)batch);
+    return launch_chained(kern, grid, 320, (size_t)bytes, st, g.split, a, b, g, epi);
 }
 
 template <class EPI, int PL>
@@ -288,6 +301,12 @@ int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape
 
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st) {
     return launch_tile_form<PlanesOut, 2>(A, B, s, out, false, out.ld % 4 == 0, st);
+}
+int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const FinalOut& out, int dtype, cudaStream_t st) {
+    const bool packs = out.ld * (long long)element_size(dtype) % 16 == 0 && (out.batch * (long long)element_size(dtype)) % 16 == 0;
+    if (dtype == EBS_F32) return launch_tile_form<TypedFinal<float>, 2>(A, B, s, {out}, false, packs, st);
+    if (dtype == EBS_F16) return launch_tile_form<TypedFinal<__half>, 2>(A, B, s, {out}, false, packs, st);
+    return launch_tile_form<TypedFinal<__nv_bfloat16>, 2>(A, B, s, {out}, false, packs, st);
 }
 
 bool gemm_operand_map(const GemmOperand& o, int mn, int red, int batch, int box_mn, bool bf16, CUtensorMap* map) {

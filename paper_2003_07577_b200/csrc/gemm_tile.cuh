@@ -18,9 +18,11 @@ struct TileArgs {
 // D (rows x cols) = sum over red of A (rows x red) and B (cols x red); out is what becomes of it.
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmOut& out, int dtype, cudaStream_t st);
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st);
+int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const FinalOut& out, int dtype, cudaStream_t st);
 unsigned long long gemm_tile_timeouts();
 int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmOut& out, int dtype, cudaStream_t st);
 int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st);
+int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const FinalOut& out, int dtype, cudaStream_t st);
 unsigned long long gemm_pair_timeouts();
 
 // The kernel for a product, by its size.

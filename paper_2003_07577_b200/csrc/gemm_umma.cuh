@@ -89,8 +89,12 @@ int gemm_sm_count();
 template <typename T>
 struct LinearOut {
     static constexpr int N = Pack<T>::N;
+    using Columns = GemmColumns<T>;
+    using Ahead = GemmAhead;
     GemmOut o;
-    __device__ __forceinline__ void pack(int, long long row, int col, float (&v)[N]) const { gemm_store_pack<T>(o, row, col, v); }
+    __device__ __forceinline__ void columns(int col, Columns& c) const { gemm_columns<T>(o, col, c); }
+    __device__ __forceinline__ void ahead(int, long long row, int col, Ahead& a) const { gemm_ahead<T>(o, row, col, a); }
+    __device__ __forceinline__ void pack(int, long long row, int col, float (&v)[N], const Columns& c, const Ahead& a) const { gemm_store_pack<T>(o, row, col, v, c, a); }
     __device__ __forceinline__ void one(int, long long row, int col, float v) const { gemm_store<T>(o, row, col, v); }
 };
 
@@ -98,11 +102,20 @@ struct LinearOut {
 // caller's choice, folded into alpha and beta).  c and y: planes `plane` elements apart, matrices of a batch `batch` apart.
 struct PlanesOut {
     static constexpr int N = 4;
+    struct Columns {};
+    struct Ahead { uint2 hi, lo; };
     __half* y;
     const __half* c;
     long long ld, plane, batch;
     long long c_ld, c_plane, c_batch;
     float alpha, beta;
+    __device__ __forceinline__ void columns(int, Columns&) const {}
+    __device__ __forceinline__ void ahead(int b, long long row, int col, Ahead& a) const {
+        if (!c) return;
+        const __half* p = c + b * c_batch + row * c_ld + col;
+        a.hi = *reinterpret_cast<const uint2*>(p);
+        a.lo = *reinterpret_cast<const uint2*>(p + c_plane);
+    }
     __device__ __forceinline__ void one(int b, long long row, int col, float v) const {
         v *= alpha;
         if (c) {
@@ -114,13 +127,9 @@ struct PlanesOut {
         q[0] = hi;
         q[plane] = __float2half_rn(v - __half2float(hi));
     }
-    __device__ __forceinline__ void pack(int b, long long row, int col, float (&v)[N]) const {
-        __half hi[4], lo[4], ch[4], cl[4];
-        if (c) {
-            const __half* p = c + b * c_batch + row * c_ld + col;
-            *reinterpret_cast<uint2*>(ch) = *reinterpret_cast<const uint2*>(p);
-            *reinterpret_cast<uint2*>(cl) = *reinterpret_cast<const uint2*>(p + c_plane);
-        }
+    __device__ __forceinline__ void pack(int b, long long row, int col, float (&v)[N], const Columns&, const Ahead& a) const {
+        __half hi[4], lo[4];
+        const __half *ch = reinterpret_cast<const __half*>(&a.hi), *cl = reinterpret_cast<const __half*>(&a.lo);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float t = v[i] * alpha;
@@ -131,6 +140,42 @@ struct PlanesOut {
         __half* q = y + b * batch + row * ld + col;
         *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(hi);
         *reinterpret_cast<uint2*>(q + plane) = *reinterpret_cast<const uint2*>(lo);
+    }
+};
+
+// The last product of an orthogonalisation: v = alpha * sum + beta * (c_hi + c_lo), rounded to the caller's type.
+struct FinalOut {
+    void* y;
+    const __half* c;
+    long long ld, batch;
+    long long c_ld, c_plane, c_batch;
+    float alpha, beta;
+};
+template <typename T>
+struct TypedFinal {
+    static constexpr int N = Pack<T>::N;
+    struct Columns {};
+    struct Ahead { __align__(16) __half hi[N], lo[N]; };
+    FinalOut o;
+    __device__ __forceinline__ void columns(int, Columns&) const {}
+    __device__ __forceinline__ void ahead(int b, long long row, int col, Ahead& a) const {
+        const __half* p = o.c + b * o.c_batch + row * o.c_ld + col;
+        if constexpr (N == 8) {
+            *reinterpret_cast<uint4*>(a.hi) = *reinterpret_cast<const uint4*>(p);
+            *reinterpret_cast<uint4*>(a.lo) = *reinterpret_cast<const uint4*>(p + o.c_plane);
+        } else {
+            *reinterpret_cast<uint2*>(a.hi) = *reinterpret_cast<const uint2*>(p);
+            *reinterpret_cast<uint2*>(a.lo) = *reinterpret_cast<const uint2*>(p + o.c_plane);
+        }
+    }
+    __device__ __forceinline__ void pack(int b, long long row, int col, float (&v)[N], const Columns&, const Ahead& a) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = fmaf(o.beta, __half2float(a.hi[i]) + __half2float(a.lo[i]), v[i] * o.alpha);
+        store_pack(static_cast<T*>(o.y) + b * o.batch + row * o.ld + col, v);
+    }
+    __device__ __forceinline__ void one(int b, long long row, int col, float v) const {
+        const __half* p = o.c + b * o.c_batch + row * o.c_ld + col;
+        static_cast<T*>(o.y)[b * o.batch + row * o.ld + col] = from_f32<T>(fmaf(o.beta, __half2float(p[0]) + __half2float(p[o.c_plane]), v * o.alpha));
     }
 };
 

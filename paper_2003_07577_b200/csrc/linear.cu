@@ -70,17 +70,19 @@ static long long round8(long long v) { return (v + 7) & ~7LL; }
 
 // A copy of 16-bit rows whose stride is a multiple of 16 bytes.
 __global__ void __launch_bounds__(256) copy_rows_kernel(const uint16_t* __restrict__ src, long long ld, long long rows, int cols, uint16_t* __restrict__ dst, long long ldd) {
+    let_next_kernel_start();
+    wait_for_previous_kernel();
     for (long long r = blockIdx.y; r < rows; r += gridDim.y)
         for (int c = blockIdx.x * 256 + threadIdx.x; c < cols; c += gridDim.x * 256) dst[r * ldd + c] = src[r * ld + c];
 }
 
 // The power of two that brings values of magnitude up to the one with these bits below 2^15, and what is remembered of it: its
 // negated exponent, or what kind of row this is.
-__device__ __forceinline__ int split_exponent(unsigned top_bits) { return 141 - (int)(top_bits >> 23); }
+__device__ __forceinline__ int split_exponent(unsigned top_bits) { return top_bits < 0x7f800000u && top_bits != 0u ? 141 - (int)(top_bits >> 23) : 0; }
 __device__ __forceinline__ int split_record(unsigned top_bits) {
     if (top_bits > 0x7f800000u) return SCALE_NAN;
     if (top_bits == 0x7f800000u) return SCALE_INF;
-    return top_bits == 0u ? 0 : -split_exponent(top_bits);
+    return -split_exponent(top_bits);
 }
 // x = (hi + lo) 2^-e: both halves rounded to nearest, 22 bits where hi is a normal number and lo has its 11 bits (values within 2^-17
 // of the largest of the row), an absolute error of 2^-40 of the largest below.  Non-finite values are 0: their rows are flagged.
@@ -89,48 +91,63 @@ __device__ __forceinline__ void split_value(float x, int e, __half& hi, __half& 
     hi = __float2half_rn(v);
     lo = __float2half_rn(v - __half2float(hi));
 }
-
-// Four neighbouring elements of a row, of which `left` exist: one 16-byte access where the rows allow it (VEC).
-template <bool VEC>
-__device__ __forceinline__ float4 load4(const float* p, int left) {
-    if (VEC && left >= 4) return *reinterpret_cast<const float4*>(p);
+// Four neighbouring elements of a row, of which `left` exist: one 16-byte access where the rows allow it.
+__device__ __forceinline__ float4 load4(const float* p, int left, bool vec) {
+    if (vec && left >= 4) return *reinterpret_cast<const float4*>(p);
     return make_float4(left > 0 ? p[0] : 0.0f, left > 1 ? p[1] : 0.0f, left > 2 ? p[2] : 0.0f, left > 3 ? p[3] : 0.0f);
 }
-__device__ __forceinline__ unsigned magnitude(const float4& v) {
-    const unsigned a = max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu);
-    return max(a, max(__float_as_uint(v.z) & 0x7fffffffu, __float_as_uint(v.w) & 0x7fffffffu));
-}
+__device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 // (the planes' rows are padded to whole groups of eight elements: what is written past the end of a row is padding)
-__device__ __forceinline__ void store_split4(__half* hi_plane, __half* lo_plane, const float4& v, int e0, int e1, int e2, int e3) {
+__device__ __forceinline__ void store_split4(__half* hi_plane, __half* lo_plane, const float4& v, const int (&e)[4]) {
     __half hi[4], lo[4];
-    split_value(v.x, e0, hi[0], lo[0]);
-    split_value(v.y, e1, hi[1], lo[1]);
-    split_value(v.z, e2, hi[2], lo[2]);
-    split_value(v.w, e3, hi[3], lo[3]);
+    split_value(v.x, e[0], hi[0], lo[0]);
+    split_value(v.y, e[1], hi[1], lo[1]);
+    split_value(v.z, e[2], hi[2], lo[2]);
+    split_value(v.w, e[3], hi[3], lo[3]);
     *reinterpret_cast<uint2*>(hi_plane) = *reinterpret_cast<const uint2*>(hi);
     *reinterpret_cast<uint2*>(lo_plane) = *reinterpret_cast<const uint2*>(lo);
 }
 
-// Planes of a matrix whose reduction runs along its rows: one exponent a row.  A row is a warp's or (WIDE) a block's; its first
-// 16 elements a thread stay in registers between the search for the largest and the split.
-template <bool VEC, bool WIDE>
-__global__ void __launch_bounds__(256) split_rows_kernel(const float* __restrict__ src, long long ld, long long rows, int cols, __half* __restrict__ dst,
-                                                         long long ldd, int* __restrict__ exps) {
-    __shared__ unsigned part[8];
+// A matrix to split into planes.  across = 0: its reduction runs along a row, one exponent a row.  across = 1: down the rows, one
+// exponent a column; the largest magnitudes of the columns then come from column_tops, for each of `chunks` chunks of rows.
+struct SplitJob {
+    const float* src;
+    long long ld, rows;
+    int cols, across;
+    __half* dst;
+    long long ldd;
+    int* exps;
+    unsigned* tops;                        // [chunks][cols]
+    int chunks, vec;
+    unsigned blocks, first;                // thread blocks, and the first of them in the launch
+};
+constexpr int MAX_SPLIT_JOBS = 4;
+struct SplitJobs {
+    SplitJob job[MAX_SPLIT_JOBS];
+    int count;
+};
+
+// A row is a warp's or (WIDE) a block's; its first 16 elements a thread stay in registers between the search for the largest and the split.
+template <bool WIDE>
+__device__ __forceinline__ void split_rows(const SplitJob& j, unsigned block, unsigned* part) {
     constexpr int T = WIDE ? 256 : 32;
     const int t = WIDE ? threadIdx.x : threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long step = WIDE ? gridDim.x : gridDim.x * 8LL;
-    for (long long r = WIDE ? blockIdx.x : blockIdx.x * 8LL + warp; r < rows; r += step) {
-        const float* x = src + r * ld;
+    const long long step = WIDE ? j.blocks : j.blocks * 8LL;
+    for (long long r = WIDE ? block : block * 8LL + warp; r < j.rows; r += step) {
+        const float* x = j.src + r * j.ld;
         float4 held[4];
         unsigned top = 0u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int c = (i * T + t) * 4;
-            held[i] = load4<VEC>(x + c, cols - c);
-            top = max(top, magnitude(held[i]));
+            held[i] = load4(x + c, j.cols - c, j.vec);
         }
-        for (int c = (4 * T + t) * 4; c < cols; c += 4 * T) top = max(top, magnitude(load4<VEC>(x + c, cols - c)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(max(top, max(magnitude(held[i].x), magnitude(held[i].y))), max(magnitude(held[i].z), magnitude(held[i].w)));
+        for (int c = (4 * T + t) * 4; c < j.cols; c += 4 * T) {
+            const float4 v = load4(x + c, j.cols - c, j.vec);
+            top = max(max(top, max(magnitude(v.x), magnitude(v.y))), max(magnitude(v.z), magnitude(v.w)));
+        }
         top = __reduce_max_sync(0xffffffffu, top);
         if (WIDE) {
             __syncthreads();                                  // (the previous row's reads are over)
@@ -139,58 +156,88 @@ __global__ void __launch_bounds__(256) split_rows_kernel(const float* __restrict
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = max(top, part[i]);
         }
-        const int e = top < 0x7f800000u && top != 0u ? split_exponent(top) : 0;
-        if (t == 0) exps[r] = split_record(top);
-        __half *hi = dst + r * ldd, *lo = hi + rows * ldd;
+        const int e = split_exponent(top), es[4] = {e, e, e, e};
+        if (t == 0) j.exps[r] = split_record(top);
+        __half *hi = j.dst + r * j.ldd, *lo = hi + j.rows * j.ldd;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int c = (i * T + t) * 4;
-            if (c < cols) store_split4(hi + c, lo + c, held[i], e, e, e, e);
+            if (c < j.cols) store_split4(hi + c, lo + c, held[i], es);
         }
-        for (int c = (4 * T + t) * 4; c < cols; c += 4 * T) store_split4(hi + c, lo + c, load4<VEC>(x + c, cols - c), e, e, e, e);
+        for (int c = (4 * T + t) * 4; c < j.cols; c += 4 * T) store_split4(hi + c, lo + c, load4(x + c, j.cols - c, j.vec), es);
     }
 }
-// The largest magnitudes of the columns (their bits, in `top`, which starts at zero): 128 columns a block.
-template <bool VEC>
-__global__ void __launch_bounds__(256) column_top_kernel(const float* __restrict__ src, long long ld, long long rows, int cols, unsigned* __restrict__ top) {
-    __shared__ unsigned part[8][128];
-    const int lane = threadIdx.x & 31, c = blockIdx.x * 128 + lane * 4, y = threadIdx.x >> 5;
-    unsigned m[4] = {0u, 0u, 0u, 0u};
-    if (c < cols)
-#pragma unroll 4
-        for (long long r = blockIdx.y * 8LL + y; r < rows; r += gridDim.y * 8LL) {
-            const float4 v = load4<VEC>(src + r * ld + c, cols - c);
-            m[0] = max(m[0], __float_as_uint(v.x) & 0x7fffffffu);
-            m[1] = max(m[1], __float_as_uint(v.y) & 0x7fffffffu);
-            m[2] = max(m[2], __float_as_uint(v.z) & 0x7fffffffu);
-            m[3] = max(m[3], __float_as_uint(v.w) & 0x7fffffffu);
-        }
+__device__ __forceinline__ void tops_of_block(unsigned (&m)[4], unsigned (*part)[128], unsigned* out, int col0, int cols) {
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5;
 #pragma unroll
     for (int i = 0; i < 4; ++i) part[y][lane * 4 + i] = m[i];
     __syncthreads();
-    if (threadIdx.x < 128 && blockIdx.x * 128 + threadIdx.x < cols) {
+    if (threadIdx.x < 128 && col0 + (int)threadIdx.x < cols) {
         unsigned v = 0u;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v = max(v, part[i][threadIdx.x]);
-        atomicMax(top + blockIdx.x * 128 + threadIdx.x, v);   // (a maximum does not depend on the order)
+        out[threadIdx.x] = v;
     }
 }
-// Planes of a matrix whose reduction runs across its rows: one exponent a column, from column_top_kernel.
-template <bool VEC>
-__global__ void __launch_bounds__(256) split_columns_kernel(const float* __restrict__ src, long long ld, long long rows, int cols, const unsigned* __restrict__ top,
-                                                            __half* __restrict__ dst, long long ldd, int* __restrict__ exps) {
-    const int lane = threadIdx.x & 31, c = blockIdx.x * 128 + lane * 4, y = threadIdx.x >> 5;
-    if (c >= cols) return;
+// The largest magnitudes of 128 columns over one chunk of rows.
+__device__ __forceinline__ void column_tops(const SplitJob& j, unsigned block, unsigned (*part)[128]) {
+    const int across = (j.cols + 127) / 128, bx = (int)(block % across), by = (int)(block / across);
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, c = bx * 128 + lane * 4;
+    const long long r0 = j.rows * by / j.chunks, r1 = j.rows * (by + 1) / j.chunks;
+    unsigned m[4] = {0u, 0u, 0u, 0u};
+    if (c < j.cols)
+#pragma unroll 4
+        for (long long r = r0 + y; r < r1; r += 8) {
+            const float4 v = load4(j.src + r * j.ld + c, j.cols - c, j.vec);
+            m[0] = max(m[0], magnitude(v.x));
+            m[1] = max(m[1], magnitude(v.y));
+            m[2] = max(m[2], magnitude(v.z));
+            m[3] = max(m[3], magnitude(v.w));
+        }
+    tops_of_block(m, part, j.tops + (size_t)by * j.cols + bx * 128, bx * 128, j.cols);
+}
+__device__ __forceinline__ void split_columns(const SplitJob& j, unsigned block, unsigned (*part)[128]) {
+    const int across = (j.cols + 127) / 128, bx = (int)(block % across), by = (int)(block / across), down = (int)(j.blocks / across);
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, c = bx * 128 + lane * 4;
+    unsigned m[4] = {0u, 0u, 0u, 0u};
+    for (int k = y; k < j.chunks; k += 8)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < j.cols) m[i] = max(m[i], j.tops[(size_t)k * j.cols + c + i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[y][lane * 4 + i] = m[i];
+    __syncthreads();
     int e[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const unsigned t = c + i < cols ? top[c + i] : 0u;
-        e[i] = t < 0x7f800000u && t != 0u ? split_exponent(t) : 0;
-        if (blockIdx.y == 0 && y == 0 && c + i < cols) exps[c + i] = split_record(t);
+        unsigned t = 0u;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) t = max(t, part[q][lane * 4 + i]);
+        e[i] = split_exponent(t);
+        if (by == 0 && y == 0 && c + i < j.cols) j.exps[c + i] = split_record(t);
     }
+    if (c >= j.cols) return;
+    const long long r0 = j.rows * by / down, r1 = j.rows * (by + 1) / down;
 #pragma unroll 4
-    for (long long r = blockIdx.y * 8LL + y; r < rows; r += gridDim.y * 8LL)
-        store_split4(dst + r * ldd + c, dst + (rows + r) * ldd + c, load4<VEC>(src + r * ld + c, cols - c), e[0], e[1], e[2], e[3]);
+    for (long long r = r0 + y; r < r1; r += 8)
+        store_split4(j.dst + r * j.ldd + c, j.dst + (j.rows + r) * j.ldd + c, load4(j.src + r * j.ld + c, j.cols - c, j.vec), e);
+}
+
+__device__ __forceinline__ int job_of(const SplitJobs& s, unsigned block) {
+    int i = 0;
+    while (i + 1 < s.count && block >= s.job[i + 1].first) ++i;
+    return i;
+}
+// All splits of a call.
+__global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ SplitJobs jobs) {
+    __shared__ unsigned part[8][128];
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    const SplitJob& j = jobs.job[job_of(jobs, blockIdx.x)];
+    const unsigned block = blockIdx.x - j.first;
+    if (j.across) split_columns(j, block, part);
+    else if (j.cols > 512) split_rows<true>(j, block, part[0]);
+    else split_rows<false>(j, block, part[0]);
 }
 
 // An operand of a product: 16-bit rows as they are, or copied where their starts are not on 16 bytes; fp32 rows split.
@@ -203,48 +250,47 @@ struct Matrix {
     long long rows, ld;
     int cols;
 };
-static unsigned row_blocks(long long rows, int per) { const long long b = (rows + per - 1) / per; return (unsigned)(b < 2048 ? b : 2048); }
-
-// Row blocks (of at least 32 rows) for kernels that go down `across` blocks of columns: about eight blocks an SM.
-static unsigned column_blocks(long long rows, int across) {
-    long long b = (rows + 31) / 32, want = (8LL * gemm_sm_count() + across - 1) / across;
-    if (b > want) b = want;
-    return (unsigned)(b < 1 ? 1 : b > 65535 ? 65535 : b);
+// Chunks (of at least 32 rows) for work that goes down `across` blocks of columns: about four blocks an SM; from the sizes alone.
+static int row_chunks(long long rows, int across) {
+    const long long c = (rows + 31) / 32, want = (4LL * 148 + across - 1) / across;
+    return (int)(c < want ? c : want);
 }
-
-static int prepare_operand(const Matrix& m, int dtype, bool across, Carver& ws, bool run, cudaStream_t st, Prepared* out) {
-    out->op = GemmOperand{m.p, m.ld, across};
-    if (dtype != EBS_F32) {
-        if ((m.ld & 7) == 0) return EBS_OK;
-        const long long ldd = round8(m.cols);
-        uint16_t* copy = ws.take<uint16_t>((size_t)m.rows * ldd);
-        out->op.p = copy;
-        out->op.ld = ldd;
-        if (!run) return EBS_OK;
-        copy_rows_kernel<<<dim3((m.cols + 255) / 256, row_blocks(m.rows, 1)), 256, 0, st>>>(static_cast<const uint16_t*>(m.p), m.ld, m.rows, m.cols, copy, ldd);
-        return check_cuda(cudaGetLastError());
-    }
+// Describes the operand and takes its buffers; fp32: adds its split to the jobs.
+static Prepared plan_operand(const Matrix& m, int dtype, bool across, Carver& ws, SplitJobs* jobs) {
+    Prepared out;
+    out.op = GemmOperand{m.p, m.ld, across};
     const long long ldd = round8(m.cols);
-    __half* planes = ws.take<__half>(2 * (size_t)m.rows * ldd);
-    int* exps = ws.take<int>(across ? m.cols : m.rows);
-    unsigned* top = across ? ws.take<unsigned>(m.cols) : nullptr;
-    out->op = GemmOperand{planes, ldd, across, 2, m.rows * ldd, 2 * m.rows * ldd};
-    out->exps = exps;
-    if (!run) return EBS_OK;
-    const float* src = static_cast<const float*>(m.p);
-    const bool vec = (m.ld & 3) == 0;
-    if (!across) {
-        const bool wide = m.cols > 512;
-        const unsigned grid = row_blocks(m.rows, wide ? 1 : 8);
-        auto kern = wide ? (vec ? split_rows_kernel<true, true> : split_rows_kernel<false, true>) : (vec ? split_rows_kernel<true, false> : split_rows_kernel<false, false>);
-        kern<<<grid, 256, 0, st>>>(src, m.ld, m.rows, m.cols, planes, ldd, exps);
-    } else {
-        if (check_cuda(cudaMemsetAsync(top, 0, (size_t)m.cols * 4, st))) return EBS_ERR_CUDA;
-        const dim3 grid((m.cols + 127) / 128, column_blocks(m.rows, (m.cols + 127) / 128));
-        (vec ? column_top_kernel<true> : column_top_kernel<false>)<<<grid, 256, 0, st>>>(src, m.ld, m.rows, m.cols, top);
-        (vec ? split_columns_kernel<true> : split_columns_kernel<false>)<<<grid, 256, 0, st>>>(src, m.ld, m.rows, m.cols, top, planes, ldd, exps);
+    if (dtype != EBS_F32) {
+        if ((m.ld & 7) == 0) return out;
+        out.op.p = ws.take<uint16_t>((size_t)m.rows * ldd);
+        out.op.ld = ldd;
+        return out;
     }
-    return check_cuda(cudaGetLastError());
+    SplitJob j{static_cast<const float*>(m.p), m.ld, m.rows, m.cols, across, ws.take<__half>(2 * (size_t)m.rows * ldd), ldd, ws.take<int>(across ? m.cols : m.rows), nullptr, 0, (m.ld & 3) == 0, 0, 0};
+    if (across) {
+        const int blocks = (m.cols + 127) / 128;
+        j.chunks = row_chunks(m.rows, blocks);
+        j.tops = ws.take<unsigned>((size_t)j.chunks * m.cols);
+        j.blocks = (unsigned)(blocks * j.chunks);
+    } else {
+        const long long b = m.cols > 512 ? m.rows : (m.rows + 7) / 8;
+        j.blocks = (unsigned)(b < 2048 ? b : 2048);
+    }
+    out.op = GemmOperand{j.dst, ldd, across, 2, m.rows * ldd, 2 * m.rows * ldd};
+    out.exps = j.exps;
+    jobs->job[jobs->count++] = j;
+    return out;
+}
+static int copy_operand(const Matrix& m, const Prepared& p, cudaStream_t st) {
+    if (!p.op.p || p.op.planes == 2 || p.op.p == m.p) return EBS_OK;
+    const long long rows = m.rows < 4096 ? m.rows : 4096;
+    return launch_chained(copy_rows_kernel, dim3((m.cols + 255) / 256, (unsigned)rows), 256, 0, st, 1, static_cast<const uint16_t*>(m.p), m.ld, m.rows, m.cols,
+                          static_cast<uint16_t*>(const_cast<void*>(p.op.p)), p.op.ld);
+}
+static int launch_splits(SplitJobs& jobs, cudaStream_t st) {
+    unsigned blocks = 0;
+    for (int i = 0; i < jobs.count; ++i) { jobs.job[i].first = blocks; blocks += jobs.job[i].blocks; }
+    return blocks ? launch_chained(split_kernel, dim3(blocks), 256, 0, st, 1, jobs) : EBS_OK;
 }
 
 // One product with its operands prepared; a: its rows are the result's (across: its columns), likewise b for the result's columns.
@@ -268,95 +314,156 @@ static int product(const Prepared& a, const Matrix& am, const Prepared& b, const
 // A half-precision dz is kept halved: the steepest slope (1.13) times the type's largest value would not fit.
 static float dz_store_scale(const ebs_linear_desc& d) { return d.dtype == EBS_F16 && d.act ? 0.5f : 1.0f; }
 
-// dz = dy * act'(z), stored times `store`, and the column sums of dz before its rounding.  A block takes 32 packs of N columns and
-// the rows of one of gridDim.y chunks; the sums of a chunk go to `part`, or (one chunk) to dbias at once.
+struct DzArgs {
+    const void *dy, *z;
+    long long ldy, ldz, lddz;
+    int m, n, act;
+    float store;
+    void *dz, *dbias;
+    float* part;                           // [chunks][n]: column sums of dz
+    unsigned* tops;                        // [chunks][n]: largest magnitudes of dz (fp32, for the split)
+    int chunks;
+    unsigned blocks;                       // of this part of the launch; the column tops of `jobs` follow
+};
+
+// dz = dy * act'(z), stored times `store`, and the column sums of dz before its rounding.  A block takes 32 packs of N columns and the
+// rows of one chunk.  fp32: the column tops of dz here, those of other matrices (jobs with chunks) in further blocks.
 template <typename T, int N>
-__global__ void __launch_bounds__(256) linear_dz_kernel(const T* __restrict__ dy, long long ldy, const T* __restrict__ z, long long ldz, int m, int n, int act, float store,
-                                                        T* __restrict__ dz, long long lddz, T* __restrict__ dbias, float* __restrict__ part) {
+__global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ DzArgs g, const __grid_constant__ SplitJobs jobs) {
     __shared__ float sums[8][32 * N + 4];
-    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, col = (blockIdx.x * 32 + lane) * N;
-    const long long r0 = (long long)m * blockIdx.y / gridDim.y, r1 = (long long)m * (blockIdx.y + 1) / gridDim.y;
+    __shared__ unsigned part[8][128];
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    if (blockIdx.x >= g.blocks) {
+        const SplitJob& j = jobs.job[job_of(jobs, blockIdx.x)];
+        column_tops(j, blockIdx.x - j.first, part);
+        return;
+    }
+    const int across = (g.n + 32 * N - 1) / (32 * N), bx = (int)(blockIdx.x % across), by = (int)(blockIdx.x / across);
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, col = (bx * 32 + lane) * N;
+    const long long r0 = (long long)g.m * by / g.chunks, r1 = (long long)g.m * (by + 1) / g.chunks;
+    const T *dy = static_cast<const T*>(g.dy), *z = static_cast<const T*>(g.z);
+    T* dz = static_cast<T*>(g.dz);
     float sum[N];
+    unsigned top[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[e] = 0.0f;
-    if (col < n) {
-#pragma unroll 2
+    auto finish = [&](long long r, float (&v)[N], const float (&zv)[N]) {
+        switch (g.act) {
+#define EBS_SLOPE_CASE(A) case A: _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] *= activation_slope<sizeof(T) == 2>(zv[e], A); break;
+            EBS_SLOPE_CASE(EBS_ACT_RELU) EBS_SLOPE_CASE(EBS_ACT_GELU) EBS_SLOPE_CASE(EBS_ACT_GELU_TANH) EBS_SLOPE_CASE(EBS_ACT_SILU)
+#undef EBS_SLOPE_CASE
+            default: break;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            sum[e] += v[e];
+            if (sizeof(T) == 4) top[e] = max(top[e], magnitude(v[e]));
+            v[e] *= g.store;
+        }
+        if (!dz) return;
+        if constexpr (N > 1) store_pack(dz + r * g.lddz + col, v);          // (rows of dz are padded to whole packs)
+        else dz[r * g.lddz + col] = from_f32<T>(v[0]);
+    };
+    if (N > 1 && col + N <= g.n) {
+        if constexpr (N > 1) {
+            constexpr int U = 4;                              // rows under way: enough bytes in flight to cover the memory's latency
+            for (long long r = r0 + y; r < r1; r += 8 * U) {
+                uint4 a[U], b[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (r + 8 * u < r1) {
+                        a[u] = *reinterpret_cast<const uint4*>(dy + (r + 8 * u) * g.ldy + col);
+                        if (g.act) b[u] = *reinterpret_cast<const uint4*>(z + (r + 8 * u) * g.ldz + col);
+                    }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (r + 8 * u < r1) {
+                        float v[N], zv[N];
+#pragma unroll
+                        for (int e = 0; e < N; ++e) {
+                            v[e] = to_f32(reinterpret_cast<const T*>(&a[u])[e]);
+                            zv[e] = g.act ? to_f32(reinterpret_cast<const T*>(&b[u])[e]) : 0.0f;
+                        }
+                        finish(r + 8 * u, v, zv);
+                    }
+            }
+        }
+    } else if (col < g.n) {
+#pragma unroll 4
         for (long long r = r0 + y; r < r1; r += 8) {
             float v[N], zv[N];
-            const bool whole = N > 1 && col + N <= n;
-            if (whole) {
-                if constexpr (N > 1) load_pack(dy + r * ldy + col, v);
-            } else {
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[e] = col + e < n ? to_f32(dy[r * ldy + col + e]) : 0.0f;
+            for (int e = 0; e < N; ++e) {
+                v[e] = col + e < g.n ? to_f32(dy[r * g.ldy + col + e]) : 0.0f;
+                zv[e] = g.act && col + e < g.n ? to_f32(z[r * g.ldz + col + e]) : 0.0f;
             }
-            if (act) {
-                if (whole) {
-                    if constexpr (N > 1) load_pack(z + r * ldz + col, zv);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) zv[e] = col + e < n ? to_f32(z[r * ldz + col + e]) : 0.0f;
-                }
-                switch (act) {
-#define EBS_SLOPE_CASE(A) case A: _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] *= activation_slope(zv[e], A); break;
-                    EBS_SLOPE_CASE(EBS_ACT_RELU) EBS_SLOPE_CASE(EBS_ACT_GELU) EBS_SLOPE_CASE(EBS_ACT_GELU_TANH) EBS_SLOPE_CASE(EBS_ACT_SILU)
-#undef EBS_SLOPE_CASE
-                    default: break;
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < N; ++e) sum[e] += v[e];
-            if (dz) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) v[e] *= store;
-                if (N > 1) {                                  // (rows of dz are padded to whole packs)
-                    if constexpr (N > 1) store_pack(dz + r * lddz + col, v);
-                } else {
-                    dz[r * lddz + col] = from_f32<T>(v[0]);
-                }
+            finish(r, v, zv);
+        }
+    }
+    if (sizeof(T) == 4 && g.tops) {
+        if (N == 4) tops_of_block(top, part, g.tops + (size_t)by * g.n + bx * 128, bx * 128, g.n);
+        else {
+            part[y][lane] = top[0];
+            __syncthreads();
+            if (y == 0 && col < g.n) {
+                unsigned t = 0u;
+                for (int q = 0; q < 8; ++q) t = max(t, part[q][lane]);
+                g.tops[(size_t)by * g.n + col] = t;
             }
         }
     }
-    if (!dbias) return;
+    if (!g.dbias) return;
 #pragma unroll
     for (int e = 0; e < N; ++e) sums[y][lane * N + e] = sum[e];
     __syncthreads();
     for (int i = threadIdx.x; i < 32 * N; i += 256) {
-        const int c = blockIdx.x * 32 * N + i;
-        if (c >= n) break;
+        const int c = bx * 32 * N + i;
+        if (c >= g.n) break;
         float s = 0.0f;
 #pragma unroll
         for (int q = 0; q < 8; ++q) s += sums[q][i];
-        if (gridDim.y == 1) dbias[c] = from_f32<T>(s);
-        else part[(size_t)blockIdx.y * n + c] = s;
+        if (g.chunks == 1) static_cast<T*>(g.dbias)[c] = from_f32<T>(s);
+        else g.part[(size_t)by * g.n + c] = s;
+    }
+}
+// dbias from the chunks' sums: 32 columns a block, its eight warps take every eighth chunk.
+template <typename T>
+__global__ void __launch_bounds__(256) linear_dbias_kernel(const float* __restrict__ part, int chunks, int n, T* __restrict__ dbias) {
+    __shared__ float sums[8][33];
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    if (c < n)
+#pragma unroll 8
+        for (int i = y; i < chunks; i += 8) s += part[(size_t)i * n + c];
+    sums[y][lane] = s;
+    __syncthreads();
+    if (y == 0 && c < n) {
+        for (int q = 1; q < 8; ++q) s += sums[q][lane];
+        dbias[c] = from_f32<T>(s);
     }
 }
 template <typename T>
-__global__ void __launch_bounds__(256) linear_dbias_kernel(const float* __restrict__ part, int chunks, int n, T* __restrict__ dbias) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= n) return;
-    float s = 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < chunks; ++i) s += part[(size_t)i * n + c];
-    dbias[c] = from_f32<T>(s);
-}
-
-// Chunks of rows the sums are taken in, from the sizes alone: about four blocks an SM, at least 32 rows each.
-static int dz_chunks(const ebs_linear_desc& d) {
-    const int packs = d.dtype == EBS_F32 ? 128 : 256, across = (d.n + packs - 1) / packs;
-    long long c = (d.m + 31) / 32, want = (4LL * 148 + across - 1) / across;
-    return (int)(c < want ? c : want);
-}
-template <typename T>
-static int launch_dz(const void* dy, const void* z, const ebs_linear_desc& d, void* dz, long long lddz, void* dbias, float* part, cudaStream_t st) {
+static int launch_dz(DzArgs& g, SplitJobs& jobs, cudaStream_t st) {
     constexpr int N = Pack<T>::N;
-    const bool packs = d.ldy % N == 0 && (!d.act || d.ldz % N == 0);
-    const int chunks = dz_chunks(d), per = packs ? 32 * N : 32;
-    const dim3 grid((d.n + per - 1) / per, chunks);
-    auto kern = packs ? linear_dz_kernel<T, N> : linear_dz_kernel<T, 1>;
-    kern<<<grid, 256, 0, st>>>(static_cast<const T*>(dy), d.ldy, static_cast<const T*>(z), d.ldz, d.m, d.n, d.act, dz_store_scale(d), static_cast<T*>(dz), lddz, static_cast<T*>(dbias), part);
-    if (dbias && chunks > 1) linear_dbias_kernel<T><<<(d.n + 255) / 256, 256, 0, st>>>(part, chunks, d.n, static_cast<T*>(dbias));
-    return check_cuda(cudaGetLastError());
+    const bool packs = g.ldy % N == 0 && (!g.act || g.ldz % N == 0);
+    const int per = packs ? 32 * N : 32;
+    g.blocks = g.dz || g.dbias || g.tops ? (unsigned)((g.n + per - 1) / per * g.chunks) : 0u;
+    SplitJobs tops = {};
+    unsigned blocks = g.blocks;
+    for (int i = 0; i < jobs.count; ++i) {
+        if (!jobs.job[i].across || jobs.job[i].tops == g.tops) continue;
+        tops.job[tops.count] = jobs.job[i];
+        tops.job[tops.count++].first = blocks;
+        blocks += jobs.job[i].blocks;
+    }
+    int rc = EBS_OK;
+    if (blocks) rc = launch_chained(packs ? linear_dz_kernel<T, N> : linear_dz_kernel<T, 1>, dim3(blocks), 256, 0, st, 1, g, tops);
+    if (!rc && g.dbias && g.chunks > 1)
+        rc = launch_chained(linear_dbias_kernel<T>, dim3((g.n + 31) / 32), 256, 0, st, 1, (const float*)g.part, g.chunks, g.n, static_cast<T*>(g.dbias));
+    return rc;
 }
 
 // ---------------------------------------------------------------------------------------------------- the calls
@@ -368,16 +475,18 @@ struct LinearTensors {
 static int forward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws, bool run, cudaStream_t st) {
     if (d.m == 0) return EBS_OK;
     const Matrix xm{t.x, d.m, d.ldx, d.k}, wm{t.w, d.n, d.ldw, d.k};
-    Prepared x, w;
+    SplitJobs jobs = {};
+    const Prepared x = plan_operand(xm, d.dtype, false, ws, &jobs), w = plan_operand(wm, d.dtype, false, ws, &jobs);
+    if (!run) return EBS_OK;
     int rc;
-    if ((rc = prepare_operand(xm, d.dtype, false, ws, run, st, &x)) || (rc = prepare_operand(wm, d.dtype, false, ws, run, st, &w)) || !run) return rc;
+    if ((rc = launch_splits(jobs, st)) || (rc = copy_operand(xm, x, st)) || (rc = copy_operand(wm, w, st))) return rc;
     GemmOut o;
     o.bias = t.bias; o.residual = t.residual; o.z = t.keep; o.y = t.y; o.act = d.act;
     o.ldr = d.ldr; o.ldz = d.ldz; o.ldy = d.ldy;
     return product(x, xm, w, wm, d.k, o, d.dtype, st);
 }
 static int backward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws, bool run, cudaStream_t st) {
-    int rc;
+    int rc = EBS_OK;
     if (d.m == 0) {
         if (!run) return EBS_OK;
         const size_t size = element_size(d.dtype);
@@ -385,42 +494,51 @@ static int backward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws
         if (t.dbias && check_cuda(cudaMemsetAsync(t.dbias, 0, d.n * size, st))) return EBS_ERR_CUDA;
         return EBS_OK;
     }
+    const bool fp32 = d.dtype == EBS_F32, want_dx = t.dx || !run, want_dw = t.dw || !run;
+    const Matrix wm{t.w, d.n, d.ldw, d.k}, xm{t.x, d.m, d.ldx, d.k};
     Matrix dm{t.dy, d.m, d.ldy, d.n};
-    if (d.act || t.dbias || !run) {
-        void* dz = nullptr;
-        if (d.act) {
-            const long long ld = round8(d.n);
-            dz = d.dtype == EBS_F32 ? (void*)ws.take<float>((size_t)d.m * ld) : (void*)ws.take<uint16_t>((size_t)d.m * ld);
-            dm.p = dz;
-            dm.ld = ld;
-        }
-        float* part = dz_chunks(d) > 1 ? ws.take<float>((size_t)dz_chunks(d) * d.n) : nullptr;
-        if (run) {
-            if (d.dtype == EBS_F32) rc = launch_dz<float>(t.dy, t.z, d, dz, dm.ld, t.dbias, part, st);
-            else if (d.dtype == EBS_F16) rc = launch_dz<__half>(t.dy, t.z, d, dz, dm.ld, t.dbias, part, st);
-            else rc = launch_dz<__nv_bfloat16>(t.dy, t.z, d, dz, dm.ld, t.dbias, part, st);
-            if (rc) return rc;
-        }
+    DzArgs g = {t.dy, t.z, d.ldy, d.ldz, 0, d.m, d.n, d.act, dz_store_scale(d), nullptr, t.dbias, nullptr, nullptr, 0, 0};
+    // 16-bit columns come 256 a block, fp32 columns 128: the chunks of the sums follow the sizes, not the strides
+    g.chunks = row_chunks(d.m, (d.n + (fp32 ? 127 : 255)) / (fp32 ? 128 : 256));
+    if (d.act) {
+        g.lddz = round8(d.n);
+        g.dz = fp32 ? (void*)ws.take<float>((size_t)d.m * g.lddz) : (void*)ws.take<uint16_t>((size_t)d.m * g.lddz);
+        dm.p = g.dz;
+        dm.ld = g.lddz;
+        if (!want_dx && !want_dw) g.dz = nullptr;
     }
+    if (g.chunks > 1) g.part = ws.take<float>((size_t)g.chunks * d.n);
+    SplitJobs jobs = {};
+    Prepared rows, columns, w, x;                            // dz for dx and for dW, W, x
+    if (fp32) {
+        if (want_dw) {
+            columns = plan_operand(dm, d.dtype, true, ws, &jobs);
+            g.tops = jobs.job[0].tops;
+            g.chunks = jobs.job[0].chunks;                   // (the same number)
+        }
+        if (want_dx) rows = plan_operand(dm, d.dtype, false, ws, &jobs);
+    } else {
+        rows = columns = plan_operand(dm, d.dtype, false, ws, &jobs);
+        columns.op.mn_major = true;                          // one matrix, or one copy of it, serves both products
+    }
+    if (want_dx) w = plan_operand(wm, d.dtype, true, ws, &jobs);
+    if (want_dw) x = plan_operand(xm, d.dtype, true, ws, &jobs);
+    if (!run) return EBS_OK;
+    if (fp32) rc = launch_dz<float>(g, jobs, st);
+    else if (d.act || t.dbias) rc = d.dtype == EBS_F16 ? launch_dz<__half>(g, jobs, st) : launch_dz<__nv_bfloat16>(g, jobs, st);
+    if (rc || (rc = launch_splits(jobs, st))) return rc;
+    if (!fp32 && (t.dx || t.dw) && (rc = copy_operand(dm, rows, st))) return rc;
     GemmOut o;
     o.alpha = 1.0f / dz_store_scale(d);
-    Prepared g, other;
-    const bool shared = d.dtype != EBS_F32;                  // one 16-bit copy serves both products
-    if (shared && (rc = prepare_operand(dm, d.dtype, false, ws, run && (t.dx || t.dw), st, &g))) return rc;
-    if (t.dx || !run) {
-        const Matrix wm{t.w, d.n, d.ldw, d.k};
-        if (!shared && (rc = prepare_operand(dm, d.dtype, false, ws, run, st, &g))) return rc;
-        if ((rc = prepare_operand(wm, d.dtype, true, ws, run, st, &other))) return rc;
+    if (t.dx) {
+        if ((rc = copy_operand(wm, w, st))) return rc;
         o.y = t.dx; o.ldy = d.ldx;
-        if (run && (rc = product(g, dm, other, wm, d.n, o, d.dtype, st))) return rc;
+        if ((rc = product(rows, dm, w, wm, d.n, o, d.dtype, st))) return rc;
     }
-    if (t.dw || !run) {
-        const Matrix xm{t.x, d.m, d.ldx, d.k};
-        if (!shared) { if ((rc = prepare_operand(dm, d.dtype, true, ws, run, st, &g))) return rc; }
-        else g.op.mn_major = true;
-        if ((rc = prepare_operand(xm, d.dtype, true, ws, run, st, &other))) return rc;
+    if (t.dw) {
+        if ((rc = copy_operand(xm, x, st))) return rc;
         o.y = t.dw; o.ldy = d.ldw;
-        if (run && (rc = product(g, dm, other, xm, d.m, o, d.dtype, st))) return rc;
+        if ((rc = product(columns, dm, x, xm, d.m, o, d.dtype, st))) return rc;
     }
     return EBS_OK;
 }

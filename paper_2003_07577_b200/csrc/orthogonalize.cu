@@ -10,14 +10,31 @@ static size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
 // Matrices are kept as two fp16 planes hi + lo (22 bits) times a power of two: X by 2^-ex, its Gram matrix A by 2^-ea and
 // B = b A + c A^2 by 2^-eb, chosen from bounds of the singular values so that no entry leaves fp16 (an entry is at most the
 // largest singular value).
+// Elements i .. i + N - 1 of a dense matrix of `count`, one 16-byte access where they all exist and it is aligned.
+template <typename T>
+__device__ __forceinline__ void load_elements(const T* p, long long left, bool vec, float (&v)[Pack<T>::N]) {
+    if (vec && left >= Pack<T>::N) load_pack(p, v);
+    else
+#pragma unroll
+        for (int e = 0; e < Pack<T>::N; ++e) v[e] = e < left ? to_f32(p[e]) : 0.0f;
+}
 // Sums of squares in 64 bits, a part of each matrix a thread block (blockIdx.y: the matrix), in an order that depends on sizes alone.
 template <typename T>
-__global__ void __launch_bounds__(256) sum_squares_kernel(const T* __restrict__ g, long long count, double* __restrict__ part) {
+__global__ void __launch_bounds__(256) sum_squares_kernel(const T* __restrict__ g, long long count, int vec, double* __restrict__ part) {
     __shared__ double sums[8];
+    constexpr int N = Pack<T>::N;
+    let_next_kernel_start();
+    wait_for_previous_kernel();
     g += blockIdx.y * count;
     double s = 0.0;
+    const long long step = gridDim.x * 256LL * N;
 #pragma unroll 4
-    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < count; i += gridDim.x * 256LL) { const double v = to_f32(g[i]); s += v * v; }
+    for (long long i = (blockIdx.x * 256LL + threadIdx.x) * N; i < count; i += step) {
+        float v[N];
+        load_elements(g + i, count - i, vec, v);
+#pragma unroll
+        for (int e = 0; e < N; ++e) s = fma((double)v[e], (double)v[e], s);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
@@ -27,32 +44,72 @@ __global__ void __launch_bounds__(256) sum_squares_kernel(const T* __restrict__ 
         part[blockIdx.y * gridDim.x + blockIdx.x] = s;
     }
 }
+// The sum of a matrix's parts, the same in every thread of a block.
+__device__ __forceinline__ double total_of(const double* part, int parts) {
+    __shared__ double total;
+    if (threadIdx.x < 32) {
+        double s = 0.0;
+        for (int i = threadIdx.x; i < parts; i += 32) s += part[i];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (threadIdx.x == 0) total = s;
+    }
+    __syncthreads();
+    return total;
+}
 // X = G / (|G|_F + eps), times `store`, as planes; parts: thread blocks of sum_squares_kernel a matrix.
 template <typename T>
-__global__ void __launch_bounds__(256) normalize_kernel(const T* __restrict__ g, int rows, int cols, float eps, float store, const double* __restrict__ part, int parts,
+__global__ void __launch_bounds__(256) normalize_kernel(const T* __restrict__ g, int rows, int cols, int vec, float eps, float store, const double* __restrict__ part, int parts,
                                                         __half* __restrict__ x, long long ld, long long plane) {
-    g += (long long)blockIdx.z * rows * cols;
-    x += blockIdx.z * 2 * plane;
-    double s = 0.0;
-    for (int i = 0; i < parts; ++i) s += part[blockIdx.z * parts + i];
-    const double inv = store / (sqrt(s) + (double)eps);
-    for (int r = blockIdx.y; r < rows; r += gridDim.y)
-        for (int c = blockIdx.x * 256 + threadIdx.x; c < cols; c += gridDim.x * 256) {
-            const float v = (float)(to_f32(g[(long long)r * cols + c]) * inv);
-            const __half hi = __float2half_rn(v);
-            x[r * ld + c] = hi;
-            x[plane + r * ld + c] = __float2half_rn(v - __half2float(hi));
+    constexpr int N = Pack<T>::N;
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    g += (long long)blockIdx.y * rows * cols;
+    x += blockIdx.y * 2 * plane;
+    const double inv = store / (sqrt(total_of(part + (size_t)blockIdx.y * parts, parts)) + (double)eps);
+    const int per_row = (cols + N - 1) / N;
+    const long long items = (long long)per_row * rows, step = gridDim.x * 256LL;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < items; i += step) {
+        const int r = (int)(i / per_row), c = (int)(i - (long long)r * per_row) * N;
+        float v[N];
+        load_elements(g + (long long)r * cols + c, cols - c, vec, v);
+        __align__(16) __half hi[8], lo[8];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float s = (float)(v[e] * inv);
+            hi[e] = __float2half_rn(s);
+            lo[e] = __float2half_rn(s - __half2float(hi[e]));
         }
+        __half* to = x + r * ld + c;                          // (rows of the planes are padded to whole groups of eight)
+        if constexpr (N == 8) {
+            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi);
+            *reinterpret_cast<uint4*>(to + plane) = *reinterpret_cast<const uint4*>(lo);
+        } else {
+            *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(hi);
+            *reinterpret_cast<uint2*>(to + plane) = *reinterpret_cast<const uint2*>(lo);
+        }
+    }
+}
+static int blocks_for(long long items, int batch) {            // of 256 items, about eight an SM
+    const long long b = (items + 255) / 256, most = (8LL * 148 + batch - 1) / batch;
+    return (int)(b < most ? b : most);
 }
 template <typename T>
-static void launch_normalize(const void* g, int batch, int rows, int cols, float eps, float store, double* part, int parts, __half* x, long long ld, long long plane,
-                             cudaStream_t st) {
-    sum_squares_kernel<T><<<dim3(parts, batch), 256, 0, st>>>(static_cast<const T*>(g), (long long)rows * cols, part);
-    const dim3 grid((cols + 255) / 256, rows < 1024 ? rows : 1024, batch);
-    normalize_kernel<T><<<grid, 256, 0, st>>>(static_cast<const T*>(g), rows, cols, eps, store, part, parts, x, ld, plane);
+static int launch_normalize(const void* g, int batch, int rows, int cols, float eps, float store, double* part, int parts, __half* x, long long ld, long long plane,
+                            cudaStream_t st) {
+    constexpr int N = Pack<T>::N;
+    const long long count = (long long)rows * cols;
+    const int rc = launch_chained(sum_squares_kernel<T>, dim3(parts, batch), 256, 0, st, 1, static_cast<const T*>(g), count, (int)(count % N == 0), part);
+    if (rc) return rc;
+    const int vec = cols % N == 0;
+    return launch_chained(normalize_kernel<T>, dim3(blocks_for((long long)rows * ((cols + N - 1) / N), batch), batch), 256, 0, st, 1, static_cast<const T*>(g), rows, cols, vec, eps,
+                          store, (const double*)part, parts, x, ld, plane);
 }
+// out = scale * X, for no steps at all.
 template <typename T>
 __global__ void __launch_bounds__(256) scale_out_kernel(const __half* x, long long ld, long long plane, int rows, int cols, int batch, float scale, T* out) {
+    let_next_kernel_start();
+    wait_for_previous_kernel();
     const long long count = (long long)rows * cols, total = count * batch;
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < total; i += gridDim.x * 256LL) {
         const long long b = i / count, r = i % count, at = b * 2 * plane + r / cols * ld + r % cols;
@@ -88,8 +145,8 @@ static OrthoBuffers ortho_buffers(int batch, int rows, int cols) {
     b.side_plane = b.side_ld * side;
     b.x = round256((size_t)batch * 2 * b.plane * 2);
     b.a = round256((size_t)batch * 2 * b.side_plane * 2);
-    const long long parts = ((long long)rows * cols + 8191) / 8192;
-    b.parts = (int)(parts < 128 ? parts : 128);
+    const long long parts = ((long long)rows * cols + 4095) / 4096, most = (4LL * 148 + batch - 1) / batch;
+    b.parts = (int)(parts < most ? parts : most);
     b.part = round256((size_t)batch * b.parts * 8);
     b.total = 2 * b.x + 2 * b.a + b.part;
     return b;
@@ -144,10 +201,10 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     __half* B = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x + b.a);
     const float first = ldexpf(1.0f, ex[0]);
     double* part = reinterpret_cast<double*>(static_cast<char*>(workspace) + 2 * b.x + 2 * b.a);
-    if (dtype == EBS_F32) launch_normalize<float>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
-    else if (dtype == EBS_F16) launch_normalize<__half>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
-    else launch_normalize<__nv_bfloat16>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
-    if ((rc = check_cuda(cudaGetLastError()))) return rc;
+    if (dtype == EBS_F32) rc = launch_normalize<float>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
+    else if (dtype == EBS_F16) rc = launch_normalize<__half>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
+    else rc = launch_normalize<__nv_bfloat16>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
+    if (rc) return rc;
     const bool tall = rows > cols;                            // then X X^T X is taken as X (X^T X): the smaller product
     const int m = tall ? cols : rows, n = tall ? rows : cols;
     for (int s = 0; s < steps; ++s) {
@@ -159,19 +216,24 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
         // B 2^eb = b A + c A^2  (A is symmetric: its rows are its columns)
         PlanesOut ob{B, A, b.side_ld, b.side_plane, 2 * b.side_plane, b.side_ld, b.side_plane, 2 * b.side_plane, coeff[2] * ldexpf(1.0f, eb[s] - 2 * ea), coeff[1] * ldexpf(1.0f, eb[s] - ea)};
         if ((rc = launch_gemm(as, as, GemmShape{m, m, m, batch}, ob, st))) return rc;
-        // X 2^ex' = a X + B X or a X + X B
-        PlanesOut ox{x2, x, b.ld, b.plane, 2 * b.plane, b.ld, b.plane, 2 * b.plane, ldexpf(1.0f, ex[s + 1] - eb[s] - ex[s]), coeff[0] * ldexpf(1.0f, ex[s + 1] - ex[s])};
+        // X 2^ex' = a X + B X or a X + X B; the last one is the result
         const GemmOperand xk{x, b.ld, false, 2, b.plane, 2 * b.plane}, xm{x, b.ld, true, 2, b.plane, 2 * b.plane};
-        if ((rc = tall ? launch_gemm(xk, bs, GemmShape{rows, cols, m, batch}, ox, st) : launch_gemm(bs, xm, GemmShape{rows, cols, m, batch}, ox, st))) return rc;
+        const GemmOperand &left = tall ? xk : bs, &right = tall ? bs : xm;
+        const GemmShape shape{rows, cols, m, batch};
+        if (s == steps - 1) {
+            const float to = scale * ldexpf(1.0f, -eb[s] - ex[s]), from = scale * coeff[0] * ldexpf(1.0f, -ex[s]);
+            return launch_gemm(left, right, shape, FinalOut{out, x, cols, (long long)rows * cols, b.ld, b.plane, 2 * b.plane, to, from}, dtype, st);
+        }
+        PlanesOut ox{x2, x, b.ld, b.plane, 2 * b.plane, b.ld, b.plane, 2 * b.plane, ldexpf(1.0f, ex[s + 1] - eb[s] - ex[s]), coeff[0] * ldexpf(1.0f, ex[s + 1] - ex[s])};
+        if ((rc = launch_gemm(left, right, shape, ox, st))) return rc;
         __half* t = x; x = x2; x2 = t;
     }
-    const long long total = (long long)rows * cols * batch, blocks = (total + 255) / 256;
-    const int grid = (int)(blocks < 148 * 16 ? blocks : 148 * 16);
-    const float last = scale * ldexpf(1.0f, -ex[steps]);
-    if (dtype == EBS_F32) scale_out_kernel<float><<<grid, 256, 0, st>>>(x, b.ld, b.plane, rows, cols, batch, last, static_cast<float*>(out));
-    else if (dtype == EBS_F16) scale_out_kernel<__half><<<grid, 256, 0, st>>>(x, b.ld, b.plane, rows, cols, batch, last, static_cast<__half*>(out));
-    else scale_out_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(x, b.ld, b.plane, rows, cols, batch, last, static_cast<__nv_bfloat16*>(out));
-    return check_cuda(cudaGetLastError());
+    if (steps > 0) return EBS_OK;
+    const float last = scale * ldexpf(1.0f, -ex[0]);
+    const dim3 grid(blocks_for((long long)rows * cols * batch, 1));
+    if (dtype == EBS_F32) return launch_chained(scale_out_kernel<float>, grid, 256, 0, st, 1, (const __half*)x, b.ld, b.plane, rows, cols, batch, last, static_cast<float*>(out));
+    if (dtype == EBS_F16) return launch_chained(scale_out_kernel<__half>, grid, 256, 0, st, 1, (const __half*)x, b.ld, b.plane, rows, cols, batch, last, static_cast<__half*>(out));
+    return launch_chained(scale_out_kernel<__nv_bfloat16>, grid, 256, 0, st, 1, (const __half*)x, b.ld, b.plane, rows, cols, batch, last, static_cast<__nv_bfloat16*>(out));
 }
 
 }  // extern "C"
