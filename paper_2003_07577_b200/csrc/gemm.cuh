@@ -132,95 +132,110 @@ __device__ __forceinline__ float scale_pow2(float v, int e) {
     const int h = e >> 1;
     return v * __int_as_float((h + 127) << 23) * __int_as_float((e - h + 127) << 23);
 }
-// (arguments by value: a reference would have the kernel's parameters copied to the stack)
-static __device__ __noinline__ float fp32_dot(const float* a, long long a_red, const float* b, long long b_red, int red) {
-    float v = 0.0f;
-    for (int r = 0; r < red; ++r) v = fmaf(a[r * a_red], b[r * b_red], v);
-    return v;
-}
-__device__ __forceinline__ float gemm_unscale(const GemmOut& o, long long row, int col, int row_exp, int col_exp, float v) {
-    const int e = row_exp + col_exp;
-    if (e < SCALE_NAN / 2) return scale_pow2(v, e);
-    if (row_exp == SCALE_NAN || col_exp == SCALE_NAN) return __int_as_float(0x7fffffff);
-    const GemmFp32& f = o.fp32;
-    return fp32_dot(f.a + row * f.a_row, f.a_red, f.b + col * f.b_col, f.b_red, f.red);
-}
-
-// One element: the path of ragged or unaligned outputs.
-template <typename T>
-__device__ __forceinline__ void gemm_store(const GemmOut& o, long long row, int col, float v) {
-    if (sizeof(T) == 4) v = gemm_unscale(o, row, col, o.row_exp[row], o.col_exp[col], v);
-    v *= o.alpha;
-    if (o.bias) v += to_f32(static_cast<const T*>(o.bias)[col]);
-    if (o.z) static_cast<T*>(o.z)[row * o.ldz + col] = from_f32<T>(v);
-    if (o.act) v = activation<sizeof(T) == 2>(v, o.act);
-    if (o.residual) v += to_f32(static_cast<const T*>(o.residual)[row * o.ldr + col]);
-    static_cast<T*>(o.y)[row * o.ldy + col] = from_f32<T>(v);
-}
-
-// 16 bytes of elements.
+// 16 bytes of elements of a row, of which `left` exist; vec: they all do, and the address is a multiple of 16 bytes.
 template <typename T> struct Pack { static constexpr int N = 16 / sizeof(T); };
 template <typename T>
-__device__ __forceinline__ void load_pack(const T* p, float (&v)[16 / sizeof(T)]) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
+__device__ __forceinline__ uint4 load_raw(const T* p, int left, bool vec) {
+    uint4 u = make_uint4(0u, 0u, 0u, 0u);
+    if (vec) return *reinterpret_cast<const uint4*>(p);
+    T* e = reinterpret_cast<T*>(&u);
+#pragma unroll
+    for (int i = 0; i < Pack<T>::N; ++i)
+        if (i < left) e[i] = p[i];
+    return u;
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& u, float (&v)[16 / sizeof(T)]) {
     const T* e = reinterpret_cast<const T*>(&u);
 #pragma unroll
     for (int i = 0; i < Pack<T>::N; ++i) v[i] = to_f32(e[i]);
 }
 template <typename T>
-__device__ __forceinline__ void store_pack(T* p, const float (&v)[16 / sizeof(T)]) {
+__device__ __forceinline__ void load_pack(const T* p, float (&v)[16 / sizeof(T)]) {
+    unpack<T>(*reinterpret_cast<const uint4*>(p), v);
+}
+template <typename T>
+__device__ __forceinline__ void store_pack(T* p, const float (&v)[16 / sizeof(T)], int left = Pack<T>::N, bool vec = true) {
     uint4 u;
     T* e = reinterpret_cast<T*>(&u);
 #pragma unroll
     for (int i = 0; i < Pack<T>::N; ++i) e[i] = from_f32<T>(v[i]);
-    *reinterpret_cast<uint4*>(p) = u;
+    if (vec) *reinterpret_cast<uint4*>(p) = u;
+    else
+#pragma unroll
+        for (int i = 0; i < Pack<T>::N; ++i)
+            if (i < left) p[i] = e[i];
 }
-// Packs of neighbouring columns of one row, every address 16-byte aligned.  What a pack needs from memory is loaded ahead: what depends on
-// the columns once for all rows of a thread, what depends on the row before the sums arrive.
+
+// Packs of neighbouring columns of one row.  What a pack needs from memory is loaded ahead: what depends on the columns once for all
+// rows of a thread, what depends on the row before the sums arrive.
+constexpr int SCALE_PLAIN = 60;            // exponents up to this size multiply as floats: no product of two leaves the type's range
 template <typename T>
 struct GemmColumns {
-    float bias[Pack<T>::N];
+    uint4 bias;
     int exp[sizeof(T) == 4 ? Pack<T>::N : 1];
+    bool plain;
 };
 struct GemmAhead {
     uint4 residual;
     int row_exp;
 };
 template <typename T>
-__device__ __forceinline__ void gemm_columns(const GemmOut& o, int col, GemmColumns<T>& c) {
-    if (o.bias) load_pack(static_cast<const T*>(o.bias) + col, c.bias);
-    else
-#pragma unroll
-        for (int i = 0; i < Pack<T>::N; ++i) c.bias[i] = 0.0f;
+__device__ __forceinline__ void gemm_columns(const GemmOut& o, int col, int left, bool vec, GemmColumns<T>& c) {
+    c.bias = make_uint4(0u, 0u, 0u, 0u);
+    if (o.bias) c.bias = load_raw(static_cast<const T*>(o.bias) + col, left, vec);
     if constexpr (sizeof(T) == 4) {
+        c.plain = true;
 #pragma unroll
-        for (int i = 0; i < Pack<T>::N; ++i) c.exp[i] = o.col_exp[col + i];
-    }
-}
-template <typename T>
-__device__ __forceinline__ void gemm_ahead(const GemmOut& o, long long row, int col, GemmAhead& a) {
-    if (o.residual) a.residual = *reinterpret_cast<const uint4*>(static_cast<const T*>(o.residual) + row * o.ldr + col);
-    if (sizeof(T) == 4) a.row_exp = o.row_exp[row];
-}
-template <typename T>
-__device__ __forceinline__ void gemm_store_pack(const GemmOut& o, long long row, int col, float (&v)[16 / sizeof(T)], const GemmColumns<T>& c, const GemmAhead& a) {
-    constexpr int N = Pack<T>::N;
-    constexpr bool FAST = sizeof(T) == 2;
-    if constexpr (sizeof(T) == 4) {
-        bool plain = true;
-#pragma unroll
-        for (int i = 0; i < N; ++i) plain = plain && a.row_exp + c.exp[i] < SCALE_NAN / 2;
-        if (plain) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = scale_pow2(v[i], a.row_exp + c.exp[i]);
-        } else {
-#pragma unroll 1
-            for (int i = 0; i < N; ++i) v[i] = gemm_unscale(o, row, col + i, a.row_exp, o.col_exp[col + i], v[i]);
+        for (int i = 0; i < Pack<T>::N; ++i) {
+            c.exp[i] = i < left ? o.col_exp[col + i] : 0;
+            c.plain = c.plain && abs(c.exp[i]) <= SCALE_PLAIN;
         }
     }
+}
+template <typename T>
+__device__ __forceinline__ void gemm_ahead(const GemmOut& o, long long row, int col, int left, bool vec, GemmAhead& a) {
+    if (o.residual) a.residual = load_raw(static_cast<const T*>(o.residual) + row * o.ldr + col, left, vec);
+    if (sizeof(T) == 4) a.row_exp = o.row_exp[row];
+}
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
+static __device__ __noinline__ float gemm_unscale(const float* a, long long a_red, const float* b, long long b_red, int red, int row_exp, int col_exp, float v) {
+    const int e = row_exp + col_exp;
+    if (e < SCALE_NAN / 2) return scale_pow2(v, e);
+    if (row_exp == SCALE_NAN || col_exp == SCALE_NAN) return __int_as_float(0x7fffffff);
+    float s = 0.0f;
+    for (int r = 0; r < red; ++r) s = fmaf(a[r * a_red], b[r * b_red], s);
+    return s;
+}
+template <typename T>
+__device__ __forceinline__ void gemm_store_pack(const GemmOut& o, long long row, int col, int left, bool vec, float (&v)[16 / sizeof(T)], const GemmColumns<T>& c,
+                                                const GemmAhead& a) {
+    constexpr int N = Pack<T>::N;
+    constexpr bool FAST = sizeof(T) == 2;
+    float t[N];
+    if constexpr (sizeof(T) == 4) {
+        if (c.plain && abs(a.row_exp) <= SCALE_PLAIN) {
+            const float f = power_of_two(a.row_exp);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = fmaf(v[i], o.alpha, c.bias[i]);      // (alpha: a power of two, the product is exact)
-    if (o.z) store_pack(static_cast<T*>(o.z) + row * o.ldz + col, v);
+            for (int i = 0; i < N; ++i) v[i] *= f * power_of_two(c.exp[i]);
+        } else {
+            const GemmFp32& g = o.fp32;
+#pragma unroll 1
+            for (int i = 0; i < N; ++i) {
+                if (i >= left) break;
+                float s = 0.0f;
+#pragma unroll
+                for (int e = 0; e < N; ++e) s = e == i ? v[e] : s;                       // (registers have no index)
+                s = gemm_unscale(g.a + row * g.a_row, g.a_red, g.b + (col + i) * g.b_col, g.b_red, g.red, a.row_exp, o.col_exp[col + i], s);
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = e == i ? s : v[e];
+            }
+        }
+    }
+    unpack<T>(c.bias, t);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = fmaf(v[i], o.alpha, t[i]);           // (alpha: a power of two, the product is exact)
+    if (o.z) store_pack(static_cast<T*>(o.z) + row * o.ldz + col, v, left, vec);
     switch (o.act) {                                        // (outside the loop: one branch a pack)
 #define EBS_ACT_CASE(A) case A: _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = activation<FAST>(v[i], A); break;
         EBS_ACT_CASE(EBS_ACT_RELU) EBS_ACT_CASE(EBS_ACT_GELU) EBS_ACT_CASE(EBS_ACT_GELU_TANH) EBS_ACT_CASE(EBS_ACT_SILU)
@@ -228,11 +243,11 @@ __device__ __forceinline__ void gemm_store_pack(const GemmOut& o, long long row,
         default: break;
     }
     if (o.residual) {
-        const T* t = reinterpret_cast<const T*>(&a.residual);
+        unpack<T>(a.residual, t);
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += to_f32(t[i]);
+        for (int i = 0; i < N; ++i) v[i] += t[i];
     }
-    store_pack(static_cast<T*>(o.y) + row * o.ldy + col, v);
+    store_pack(static_cast<T*>(o.y) + row * o.ldy + col, v, left, vec);
 }
 // Whether every row of the outputs and of the residual starts on 16 bytes.
 inline bool packs_ok(const GemmOut& o, size_t size) {

@@ -65,10 +65,18 @@ __device__ __forceinline__ void tmem_ld32_wait(uint32_t (&v)[32]) {
 }
 
 // Tiles in bands of eight tile rows, column by column within a band: the tiles under way at a time share few rows and columns.
-__device__ __forceinline__ void pair_tile(int t, int tiles_m, int tiles_n, int& batch, int& tm, int& tn) {
-    const int per = tiles_m * tiles_n;
+// A symmetric result: only the tiles on and below the diagonal, row by row.
+__device__ __forceinline__ void pair_tile(int t, int tiles_m, int tiles_n, int symmetric, int& batch, int& tm, int& tn) {
+    const int per = symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n;
     batch = t / per;
     t -= batch * per;
+    if (symmetric) {
+        tm = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+        while (tm * (tm + 1) / 2 > t) --tm;
+        while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
+        tn = t - tm * (tm + 1) / 2;
+        return;
+    }
     const int band = t / (8 * tiles_n), first = band * 8, height = tiles_m - first < 8 ? tiles_m - first : 8;
     t -= band * 8 * tiles_n;
     tn = t / height;
@@ -87,7 +95,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x & 1), pairs = (int)(gridDim.x >> 1);
     const int nkb = (g.red + GEMM_BK - 1) / GEMM_BK, chunk = PL == 2 ? GEMM_CHUNK : nkb, chunks = (nkb + chunk - 1) / chunk;
-    const int tiles_m = (g.out_rows + 255) / 256, tiles_n = (g.out_cols + 255) / 256, count = tiles_m * tiles_n * g.batch;
+    const int tiles_m = (g.out_rows + 255) / 256, tiles_n = (g.out_cols + 255) / 256, count = (g.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n) * g.batch;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
@@ -118,7 +126,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
         bool ok = true;
         for (int t = (int)(blockIdx.x >> 1); t < count && ok; t += pairs) {
             int batch, tm, tn;
-            pair_tile(t, tiles_m, tiles_n, batch, tm, tn);
+            pair_tile(t, tiles_m, tiles_n, g.symmetric, batch, tm, tn);
             const int a0 = tm * 256 + rank * 128, b0 = tn * 256 + rank * 128;
             for (int kb = 0; kb < nkb; ++kb, ++i) {
                 const int s = i % S, k = kb * GEMM_BK;
@@ -182,25 +190,25 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
         bool ok = true;
         for (int t = (int)(blockIdx.x >> 1); t < count && ok; t += pairs) {
             int batch, tm, tn;
-            pair_tile(t, tiles_m, tiles_n, batch, tm, tn);
+            pair_tile(t, tiles_m, tiles_n, g.symmetric, batch, tm, tn);
             const int row0 = tm * 256 + rank * 128 + (warp & 3) * 32, col0 = tn * 256 + (warp >> 2) * 128;
             constexpr int STEPS = 32 / ROWS;
             const int pack_col = (lane % PER_ROW) * N, pack_row = row0 + lane / PER_ROW;
             typename EPI::Columns columns;
             typename EPI::Ahead ahead[STEPS];
-            bool whole = false;
             auto load_ahead = [&](int column) {                   // what the packs of these columns need, before the sums are there
-                const int col = col0 + column + pack_col;
-                whole = g.packs && col + N <= g.out_cols;
-                if (!whole) return;
-                epi.columns(col, columns);
+                const int col = col0 + column + pack_col, left = g.out_cols - col;
+                const bool vec = g.packs && left >= N;
+                if (left <= 0) return;
+                epi.columns(col, left, vec, columns);
 #pragma unroll
                 for (int i = 0; i < STEPS; ++i)
-                    if (pack_row + i * ROWS < g.out_rows) epi.ahead(batch, pack_row + i * ROWS, col, ahead[i]);
+                    if (pack_row + i * ROWS < g.out_rows) epi.ahead(batch, pack_row + i * ROWS, col, left, vec, ahead[i]);
             };
             auto write = [&](int column) {                        // the patch's columns of this warp's rows
                 __syncwarp();
-                const int col = col0 + column + pack_col;
+                const int col = col0 + column + pack_col, left = g.out_cols - col;
+                const bool vec = g.packs && left >= N;
 #pragma unroll
                 for (int i = 0; i < STEPS; ++i) {
                     const int row = pack_row + i * ROWS;
@@ -208,12 +216,21 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                     const float* p = patch + (lane / PER_ROW + i * ROWS) * PITCH + pack_col;
 #pragma unroll
                     for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(v + e) = *reinterpret_cast<const float4*>(p + e);
-                    if (row >= g.out_rows || col >= g.out_cols) continue;
-                    if (whole) epi.pack(batch, row, col, v, columns, ahead[i]);
-                    else
+                    if (row < g.out_rows && left > 0) epi.pack(batch, row, col, left, vec, v, columns, ahead[i]);
+                }
+                if (EPI::N == 4 && PL == 2 && g.symmetric && tm != tn) {
+                    // the mirror image: four rows of the patch along a row of the results
+                    const int mrow = col0 + column + lane % PC;
 #pragma unroll
-                        for (int e = 0; e < N; ++e)
-                            if (col + e < g.out_cols) epi.one(batch, row, col + e, v[e]);
+                    for (int i = 0; i < 32 * PC / 4 / 32; ++i) {
+                        const int r = (lane / PC + i * (32 / PC)) * 4, mcol = row0 + r, mleft = g.out_cols - mcol;
+                        float v[N];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = patch[(r + e) * PITCH + lane % PC];
+                        if (mrow >= g.out_rows || mleft <= 0) continue;
+                        epi.ahead(batch, mrow, mcol, mleft, mleft >= N, ahead[i % STEPS]);
+                        epi.pack(batch, mrow, mcol, mleft, mleft >= N, v, columns, ahead[i % STEPS]);
+                    }
                 }
                 __syncwarp();
             };
@@ -296,18 +313,20 @@ unsigned long long gemm_pair_timeouts() {
 
 template <class EPI, int PL>
 static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, bool packs, cudaStream_t st) {
+    const bool symmetric = s.symmetric && PL == 2 && EPI::N == 4;
     TileArgs g = {};
     g.red = s.red;
     g.out_rows = s.rows;
     g.out_cols = s.cols;
     g.batch = s.batch;
+    g.symmetric = symmetric;
     g.a_mn = A.mn_major;
     g.b_mn = B.mn_major;
     g.bf16 = bf16;
     g.packs = packs;
     g.wait_limit = device_wait_limit();
     g.test_flags = device_test_flags();
-    const long long tiles = (long long)((s.rows + 255) / 256) * ((s.cols + 255) / 256) * s.batch;
+    const long long side = (s.rows + 255) / 256, tiles = (symmetric ? side * (side + 1) / 2 : side * ((s.cols + 255) / 256)) * s.batch;
     if (tiles >= (1LL << 30)) return EBS_ERR_OVERFLOW;
     CUtensorMap a, b;
     if (!gemm_operand_map(A, s.rows, s.red, s.batch, 128, bf16, &a) || !gemm_operand_map(B, s.cols, s.red, s.batch, 128, bf16, &b)) return EBS_ERR_CUDA;

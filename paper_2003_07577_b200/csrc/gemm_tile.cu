@@ -176,17 +176,18 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
         constexpr int STRIDE = 320 / PER_ROW;
         static_assert(PER_ROW <= 64 && STRIDE >= 1, "packs of a row");
         const int n = (threadIdx.x % PER_ROW) * N, ocol = inner0 + n;
-        const bool whole = g.packs && ocol + N <= g.out_cols;
+        const int left = g.out_cols - ocol;
+        const bool vec = g.packs && left >= N;
         typename EPI::Columns columns;
-        if (whole) epi.columns(ocol, columns);
-        if (ocol < g.out_cols && (int)threadIdx.x < STRIDE * PER_ROW)
+        if (left > 0) epi.columns(ocol, left, vec, columns);
+        if (left > 0 && (int)threadIdx.x < STRIDE * PER_ROW)
             for (int first = o_begin + threadIdx.x / PER_ROW; first < o_end; first += STEP * STRIDE) {
                 typename EPI::Ahead ahead[STEP];
                 float v[STEP][N];
 #pragma unroll
                 for (int i = 0; i < STEP; ++i) {
                     const int o = first + i * STRIDE, orow = outer0 + o;
-                    if (whole && o < o_end && orow < g.out_rows) epi.ahead(batch, orow, ocol, ahead[i]);
+                    if (o < o_end && orow < g.out_rows) epi.ahead(batch, orow, ocol, left, vec, ahead[i]);
                 }
 #pragma unroll
                 for (int i = 0; i < STEP; ++i) {
@@ -215,11 +216,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
                 for (int i = 0; i < STEP; ++i) {
                     const int o = first + i * STRIDE, orow = outer0 + o;
                     if (o >= o_end || orow >= g.out_rows) continue;
-                    if (whole) epi.pack(batch, orow, ocol, v[i], columns, ahead[i]);
-                    else
-#pragma unroll
-                        for (int e = 0; e < N; ++e)
-                            if (ocol + e < g.out_cols) epi.one(batch, orow, ocol + e, v[i][e]);
+                    epi.pack(batch, orow, ocol, left, vec, v[i], columns, ahead[i]);
                 }
             }
     }

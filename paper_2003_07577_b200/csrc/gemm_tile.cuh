@@ -10,7 +10,7 @@ constexpr int GEMM_CHUNK = 4;                 // stages (of 64 reduction element
 struct TileArgs {
     int red, out_rows, out_cols, batch;
     int split, stages;
-    int a_mn, b_mn, bf16, packs;
+    int a_mn, b_mn, bf16, packs, symmetric;
     unsigned wait_limit;
     int test_flags;
 };

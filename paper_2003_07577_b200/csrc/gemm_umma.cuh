@@ -9,6 +9,8 @@
 
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "conv_frame.cuh"
 #include "conv_umma.cuh"
 #include "gemm.cuh"
@@ -81,9 +83,13 @@ bool gemm_operand_map(const GemmOperand& o, int mn, int red, int batch, int box_
 // Shape of a product D = A B over `red`; D has `rows` x `cols` (row-major results) as the caller sees them.
 struct GemmShape {
     int rows, cols, red, batch;
+    bool symmetric = false;                // the result is known to be symmetric: one half of it need not be summed
 };
 
 int gemm_sm_count();
+
+// What becomes of the sums, N neighbouring columns of a row at a time (`left` of them exist; vec: all do, at addresses of whole 16 bytes):
+// `columns` and `ahead` load what is needed, `pack` finishes and stores.
 
 // The results of a linear layer or of its gradients.
 template <typename T>
@@ -92,54 +98,50 @@ struct LinearOut {
     using Columns = GemmColumns<T>;
     using Ahead = GemmAhead;
     GemmOut o;
-    __device__ __forceinline__ void columns(int col, Columns& c) const { gemm_columns<T>(o, col, c); }
-    __device__ __forceinline__ void ahead(int, long long row, int col, Ahead& a) const { gemm_ahead<T>(o, row, col, a); }
-    __device__ __forceinline__ void pack(int, long long row, int col, float (&v)[N], const Columns& c, const Ahead& a) const { gemm_store_pack<T>(o, row, col, v, c, a); }
-    __device__ __forceinline__ void one(int, long long row, int col, float v) const { gemm_store<T>(o, row, col, v); }
+    __device__ __forceinline__ void columns(int col, int left, bool vec, Columns& c) const { gemm_columns<T>(o, col, left, vec, c); }
+    __device__ __forceinline__ void ahead(int, long long row, int col, int left, bool vec, Ahead& a) const { gemm_ahead<T>(o, row, col, left, vec, a); }
+    __device__ __forceinline__ void pack(int, long long row, int col, int left, bool vec, float (&v)[N], const Columns& c, const Ahead& a) const {
+        gemm_store_pack<T>(o, row, col, left, vec, v, c, a);
+    }
 };
+
+// Rows of a kept matrix: two fp16 planes hi + lo, rows padded to whole groups of eight elements (so that a pack is always whole).
+template <int N>
+struct PlanePack { __align__(2 * N) __half hi[N], lo[N]; };
+template <int N>
+__device__ __forceinline__ void load_planes(const __half* p, long long plane, PlanePack<N>& a) {
+    using V = typename std::conditional<N == 8, uint4, uint2>::type;
+    *reinterpret_cast<V*>(a.hi) = *reinterpret_cast<const V*>(p);
+    *reinterpret_cast<V*>(a.lo) = *reinterpret_cast<const V*>(p + plane);
+}
 
 // Results kept for further products: v = alpha * sum + beta * (c_hi + c_lo), as two fp16 planes hi + lo (value: times 2^-e of the
 // caller's choice, folded into alpha and beta).  c and y: planes `plane` elements apart, matrices of a batch `batch` apart.
 struct PlanesOut {
     static constexpr int N = 4;
     struct Columns {};
-    struct Ahead { uint2 hi, lo; };
+    using Ahead = PlanePack<4>;
     __half* y;
     const __half* c;
     long long ld, plane, batch;
     long long c_ld, c_plane, c_batch;
     float alpha, beta;
-    __device__ __forceinline__ void columns(int, Columns&) const {}
-    __device__ __forceinline__ void ahead(int b, long long row, int col, Ahead& a) const {
-        if (!c) return;
-        const __half* p = c + b * c_batch + row * c_ld + col;
-        a.hi = *reinterpret_cast<const uint2*>(p);
-        a.lo = *reinterpret_cast<const uint2*>(p + c_plane);
+    __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
+    __device__ __forceinline__ void ahead(int b, long long row, int col, int, bool, Ahead& a) const {
+        if (c) load_planes(c + b * c_batch + row * c_ld + col, c_plane, a);
     }
-    __device__ __forceinline__ void one(int b, long long row, int col, float v) const {
-        v *= alpha;
-        if (c) {
-            const __half* p = c + b * c_batch + row * c_ld + col;
-            v = fmaf(beta, __half2float(p[0]) + __half2float(p[c_plane]), v);
-        }
-        __half* q = y + b * batch + row * ld + col;
-        const __half hi = __float2half_rn(v);
-        q[0] = hi;
-        q[plane] = __float2half_rn(v - __half2float(hi));
-    }
-    __device__ __forceinline__ void pack(int b, long long row, int col, float (&v)[N], const Columns&, const Ahead& a) const {
-        __half hi[4], lo[4];
-        const __half *ch = reinterpret_cast<const __half*>(&a.hi), *cl = reinterpret_cast<const __half*>(&a.lo);
+    __device__ __forceinline__ void pack(int b, long long row, int col, int, bool, float (&v)[N], const Columns&, const Ahead& a) const {
+        PlanePack<4> o;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float t = v[i] * alpha;
-            if (c) t = fmaf(beta, __half2float(ch[i]) + __half2float(cl[i]), t);
-            hi[i] = __float2half_rn(t);
-            lo[i] = __float2half_rn(t - __half2float(hi[i]));
+            if (c) t = fmaf(beta, __half2float(a.hi[i]) + __half2float(a.lo[i]), t);
+            o.hi[i] = __float2half_rn(t);
+            o.lo[i] = __float2half_rn(t - __half2float(o.hi[i]));
         }
         __half* q = y + b * batch + row * ld + col;
-        *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(hi);
-        *reinterpret_cast<uint2*>(q + plane) = *reinterpret_cast<const uint2*>(lo);
+        *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(o.hi);
+        *reinterpret_cast<uint2*>(q + plane) = *reinterpret_cast<const uint2*>(o.lo);
     }
 };
 
@@ -155,27 +157,30 @@ template <typename T>
 struct TypedFinal {
     static constexpr int N = Pack<T>::N;
     struct Columns {};
-    struct Ahead { __align__(16) __half hi[N], lo[N]; };
+    using Ahead = PlanePack<N>;
     FinalOut o;
-    __device__ __forceinline__ void columns(int, Columns&) const {}
-    __device__ __forceinline__ void ahead(int b, long long row, int col, Ahead& a) const {
-        const __half* p = o.c + b * o.c_batch + row * o.c_ld + col;
-        if constexpr (N == 8) {
-            *reinterpret_cast<uint4*>(a.hi) = *reinterpret_cast<const uint4*>(p);
-            *reinterpret_cast<uint4*>(a.lo) = *reinterpret_cast<const uint4*>(p + o.c_plane);
-        } else {
-            *reinterpret_cast<uint2*>(a.hi) = *reinterpret_cast<const uint2*>(p);
-            *reinterpret_cast<uint2*>(a.lo) = *reinterpret_cast<const uint2*>(p + o.c_plane);
-        }
+    __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
+    __device__ __forceinline__ void ahead(int b, long long row, int col, int, bool, Ahead& a) const {
+        load_planes(o.c + b * o.c_batch + row * o.c_ld + col, o.c_plane, a);
     }
-    __device__ __forceinline__ void pack(int b, long long row, int col, float (&v)[N], const Columns&, const Ahead& a) const {
+    __device__ __forceinline__ void pack(int b, long long row, int col, int left, bool vec, float (&v)[N], const Columns&, const Ahead& a) const {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = fmaf(o.beta, __half2float(a.hi[i]) + __half2float(a.lo[i]), v[i] * o.alpha);
-        store_pack(static_cast<T*>(o.y) + b * o.batch + row * o.ld + col, v);
+        store_pack(static_cast<T*>(o.y) + b * o.batch + row * o.ld + col, v, left, vec);
     }
-    __device__ __forceinline__ void one(int b, long long row, int col, float v) const {
-        const __half* p = o.c + b * o.c_batch + row * o.c_ld + col;
-        static_cast<T*>(o.y)[b * o.batch + row * o.ld + col] = from_f32<T>(fmaf(o.beta, __half2float(p[0]) + __half2float(p[o.c_plane]), v * o.alpha));
+};
+
+// A part of the sums, for reduce_parts: fp32, the parts behind one another.
+struct PartialOut {
+    static constexpr int N = 4;
+    struct Columns {};
+    struct Ahead {};
+    float* y;                              // [part][batch][rows][ld], ld a multiple of four
+    long long ld, batch, part;
+    __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
+    __device__ __forceinline__ void ahead(int, long long, int, int, bool, Ahead&) const {}
+    __device__ __forceinline__ void pack(int b, long long row, int col, int, bool, float (&v)[N], const Columns&, const Ahead&) const {
+        *reinterpret_cast<float4*>(y + b * batch + row * ld + col) = make_float4(v[0], v[1], v[2], v[3]);
     }
 };
 

@@ -212,10 +212,10 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
         const GemmOperand xs{x, b.ld, tall, 2, b.plane, 2 * b.plane}, as{A, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane}, bs{B, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane};
         const int ea = 2 * ex[s] - 14;                          // entries of A are at most the square of X's bound: below 2^14
         PlanesOut oa{A, nullptr, b.side_ld, b.side_plane, 2 * b.side_plane, 0, 0, 0, ldexpf(1.0f, ea - 2 * ex[s]), 0.0f};
-        if ((rc = launch_gemm(xs, xs, GemmShape{m, m, n, batch}, oa, st))) return rc;
+        if ((rc = launch_gemm(xs, xs, GemmShape{m, m, n, batch, true}, oa, st))) return rc;
         // B 2^eb = b A + c A^2  (A is symmetric: its rows are its columns)
         PlanesOut ob{B, A, b.side_ld, b.side_plane, 2 * b.side_plane, b.side_ld, b.side_plane, 2 * b.side_plane, coeff[2] * ldexpf(1.0f, eb[s] - 2 * ea), coeff[1] * ldexpf(1.0f, eb[s] - ea)};
-        if ((rc = launch_gemm(as, as, GemmShape{m, m, m, batch}, ob, st))) return rc;
+        if ((rc = launch_gemm(as, as, GemmShape{m, m, m, batch, true}, ob, st))) return rc;
         // X 2^ex' = a X + B X or a X + X B; the last one is the result
         const GemmOperand xk{x, b.ld, false, 2, b.plane, 2 * b.plane}, xm{x, b.ld, true, 2, b.plane, 2 * b.plane};
         const GemmOperand &left = tall ? xk : bs, &right = tall ? bs : xm;
