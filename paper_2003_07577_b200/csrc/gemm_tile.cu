@@ -306,7 +306,7 @@ int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape
     return launch_tile_form<TypedFinal<__nv_bfloat16>, 2>(A, B, s, {out}, false, packs, st);
 }
 
-bool gemm_operand_map(const GemmOperand& o, int mn, int red, int batch, int box_mn, bool bf16, CUtensorMap* map) {
+bool encode_map(CUtensorMap* map, CUtensorMapDataType type, const void* p, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, bool narrow) {
     using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     static const Encode encode = [] {
@@ -317,14 +317,17 @@ bool gemm_operand_map(const GemmOperand& o, int mn, int red, int batch, int box_
                    ? reinterpret_cast<Encode>(fn)
                    : nullptr;
     }();
-    if (!encode) return false;
+    const cuuint32_t one[3] = {1, 1, 1};
+    return encode && encode(map, type, 3, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, narrow ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool gemm_operand_map(const GemmOperand& o, int mn, int red, int batch, int box_mn, bool bf16, CUtensorMap* map) {
     const cuuint64_t inner = o.mn_major ? mn : red, outer = o.mn_major ? red : mn;
     const long long slice = o.planes > 1 ? o.plane_stride : (batch > 1 ? o.batch_stride : o.ld * (long long)outer);
     const cuuint64_t dims[3] = {inner, outer, (cuuint64_t)batch * o.planes};
     const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)slice * 2};
-    const cuuint32_t box[3] = {64, o.mn_major ? 64u : (cuuint32_t)box_mn, 1}, one[3] = {1, 1, 1};
-    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(o.p), dims, strides, box, one,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint32_t box[3] = {64, o.mn_major ? 64u : (cuuint32_t)box_mn, 1};
+    return encode_map(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.p, dims, strides, box, false);
 }
 
 int gemm_sm_count() {

@@ -20,16 +20,24 @@ int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st);
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const FinalOut& out, int dtype, cudaStream_t st);
 unsigned long long gemm_tile_timeouts();
-int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmOut& out, int dtype, cudaStream_t st);
-int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st);
-int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const FinalOut& out, int dtype, cudaStream_t st);
+
+// How a product is run: the pair kernel, with its reduction in `split` parts that meet in `scratch` bytes of memory, or the tile kernel.
+struct GemmRoute {
+    bool pair = false;
+    int split = 1;
+    size_t scratch = 0;
+};
+GemmRoute gemm_route(const GemmShape& s, int planes);
+int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmRoute& r, float* scratch, const GemmOut& out, int dtype, cudaStream_t st);
+int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmRoute& r, float* scratch, const PlanesOut& out, cudaStream_t st);
+int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmRoute& r, float* scratch, const FinalOut& out, int dtype, cudaStream_t st);
 unsigned long long gemm_pair_timeouts();
 
-// The kernel for a product, by its size.
-bool gemm_pair_pays(const GemmShape& s);
+// scratch: gemm_route(s, planes).scratch bytes.
 template <class... A>
-inline int launch_gemm(const GemmOperand& a, const GemmOperand& b, const GemmShape& s, const A&... rest) {
-    return gemm_pair_pays(s) ? launch_gemm_pair(a, b, s, rest...) : launch_gemm_tile(a, b, s, rest...);
+inline int launch_gemm(const GemmOperand& a, const GemmOperand& b, const GemmShape& s, float* scratch, const A&... rest) {
+    const GemmRoute r = gemm_route(s, a.planes);
+    return r.pair ? launch_gemm_pair(a, b, s, r, scratch, rest...) : launch_gemm_tile(a, b, s, rest...);
 }
 
 }  // namespace ebs

@@ -76,7 +76,9 @@ __device__ __forceinline__ void umma_f16(uint32_t leader, uint32_t tmem_d, uint3
         : "memory");
 }
 
-// Host side: tensor map of an operand.  mn: its rows or columns in the result, red: the reduction; box_mn: rows a K-major box takes.
+// Host side: a three-dimensional tensor map, of 64-byte rows with their swizzle (narrow) or 128-byte ones.
+bool encode_map(CUtensorMap* map, CUtensorMapDataType type, const void* p, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, bool narrow);
+// Tensor map of an operand.  mn: its rows or columns in the result, red: the reduction; box_mn: rows a K-major box takes.
 // False: the driver has no tensor maps, or refused this one.
 bool gemm_operand_map(const GemmOperand& o, int mn, int red, int batch, int box_mn, bool bf16, CUtensorMap* map);
 
@@ -177,6 +179,7 @@ struct PartialOut {
     struct Ahead {};
     float* y;                              // [part][batch][rows][ld], ld a multiple of four
     long long ld, batch, part;
+    int parts;
     __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
     __device__ __forceinline__ void ahead(int, long long, int, int, bool, Ahead&) const {}
     __device__ __forceinline__ void pack(int b, long long row, int col, int, bool, float (&v)[N], const Columns&, const Ahead&) const {

@@ -294,8 +294,8 @@ static int launch_splits(SplitJobs& jobs, cudaStream_t st) {
 }
 
 // One product with its operands prepared; a: its rows are the result's (across: its columns), likewise b for the result's columns.
-static int product(const Prepared& a, const Matrix& am, const Prepared& b, const Matrix& bm, int red, GemmOut o, int dtype, cudaStream_t st) {
-    GemmShape s{(int)(a.op.mn_major ? am.cols : am.rows), (int)(b.op.mn_major ? bm.cols : bm.rows), red, 1};
+static int product(const Prepared& a, const Matrix& am, const Prepared& b, const Matrix& bm, int red, GemmOut o, int dtype, float* scratch, cudaStream_t st) {
+    const GemmShape s{(int)(a.op.mn_major ? am.cols : am.rows), (int)(b.op.mn_major ? bm.cols : bm.rows), red, 1};
     if (dtype == EBS_F32) {
         o.row_exp = a.exps;
         o.col_exp = b.exps;
@@ -307,7 +307,7 @@ static int product(const Prepared& a, const Matrix& am, const Prepared& b, const
         o.fp32.b_red = b.op.mn_major ? bm.ld : 1;
         o.fp32.red = red;
     }
-    return launch_gemm(a.op, b.op, s, o, dtype, st);
+    return launch_gemm(a.op, b.op, s, scratch, o, dtype, st);
 }
 
 // ---------------------------------------------------------------------------------------------------- dz and dbias
@@ -477,13 +477,15 @@ static int forward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws,
     const Matrix xm{t.x, d.m, d.ldx, d.k}, wm{t.w, d.n, d.ldw, d.k};
     SplitJobs jobs = {};
     const Prepared x = plan_operand(xm, d.dtype, false, ws, &jobs), w = plan_operand(wm, d.dtype, false, ws, &jobs);
+    const int planes = d.dtype == EBS_F32 ? 2 : 1;
+    float* scratch = ws.take<float>(gemm_route(GemmShape{d.m, d.n, d.k, 1}, planes).scratch / 4);
     if (!run) return EBS_OK;
     int rc;
     if ((rc = launch_splits(jobs, st)) || (rc = copy_operand(xm, x, st)) || (rc = copy_operand(wm, w, st))) return rc;
     GemmOut o;
     o.bias = t.bias; o.residual = t.residual; o.z = t.keep; o.y = t.y; o.act = d.act;
     o.ldr = d.ldr; o.ldz = d.ldz; o.ldy = d.ldy;
-    return product(x, xm, w, wm, d.k, o, d.dtype, st);
+    return product(x, xm, w, wm, d.k, o, d.dtype, scratch, st);
 }
 static int backward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws, bool run, cudaStream_t st) {
     int rc = EBS_OK;
@@ -523,6 +525,11 @@ static int backward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws
     }
     if (want_dx) w = plan_operand(wm, d.dtype, true, ws, &jobs);
     if (want_dw) x = plan_operand(xm, d.dtype, true, ws, &jobs);
+    size_t need = 0;                                          // the products run one after the other
+    const int planes = fp32 ? 2 : 1;
+    if (want_dx) need = gemm_route(GemmShape{d.m, d.k, d.n, 1}, planes).scratch;
+    if (want_dw) { const size_t b = gemm_route(GemmShape{d.n, d.k, d.m, 1}, planes).scratch; need = b > need ? b : need; }
+    float* scratch = ws.take<float>(need / 4);
     if (!run) return EBS_OK;
     if (fp32) rc = launch_dz<float>(g, jobs, st);
     else if (d.act || t.dbias) rc = d.dtype == EBS_F16 ? launch_dz<__half>(g, jobs, st) : launch_dz<__nv_bfloat16>(g, jobs, st);
@@ -533,12 +540,12 @@ static int backward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws
     if (t.dx) {
         if ((rc = copy_operand(wm, w, st))) return rc;
         o.y = t.dx; o.ldy = d.ldx;
-        if ((rc = product(rows, dm, w, wm, d.n, o, d.dtype, st))) return rc;
+        if ((rc = product(rows, dm, w, wm, d.n, o, d.dtype, scratch, st))) return rc;
     }
     if (t.dw) {
         if ((rc = copy_operand(xm, x, st))) return rc;
         o.y = t.dw; o.ldy = d.ldw;
-        if ((rc = product(columns, dm, x, xm, d.m, o, d.dtype, st))) return rc;
+        if ((rc = product(columns, dm, x, xm, d.m, o, d.dtype, scratch, st))) return rc;
     }
     return EBS_OK;
 }

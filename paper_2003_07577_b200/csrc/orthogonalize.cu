@@ -133,7 +133,7 @@ static int headroom(double v) { int e; frexp(v > 0.0 ? v : 1.0, &e); return 14 -
 
 struct OrthoBuffers {
     long long ld, plane, side_ld, side_plane;
-    size_t x, a, part, total;
+    size_t x, a, part, scratch, total;
     int parts;                                                // sums of squares a matrix
 };
 static OrthoBuffers ortho_buffers(int batch, int rows, int cols) {
@@ -148,7 +148,11 @@ static OrthoBuffers ortho_buffers(int batch, int rows, int cols) {
     const long long parts = ((long long)rows * cols + 4095) / 4096, most = (4LL * 148 + batch - 1) / batch;
     b.parts = (int)(parts < most ? parts : most);
     b.part = round256((size_t)batch * b.parts * 8);
-    b.total = 2 * b.x + 2 * b.a + b.part;
+    b.scratch = 0;                                            // of the products' partial sums; they run one after the other
+    const int m = (int)side, n = rows < cols ? cols : rows;
+    const GemmShape shapes[] = {{m, m, n, batch, true}, {m, m, m, batch, true}, {rows, cols, m, batch}};
+    for (const GemmShape& s : shapes) { const size_t need = round256(gemm_route(s, 2).scratch); b.scratch = need > b.scratch ? need : b.scratch; }
+    b.total = 2 * b.x + 2 * b.a + b.part + b.scratch;
     return b;
 }
 static int check_shape(int batch, int rows, int cols, int dtype, int steps) {
@@ -199,6 +203,7 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     __half* x2 = reinterpret_cast<__half*>(static_cast<char*>(workspace) + b.x);
     __half* A = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x);
     __half* B = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x + b.a);
+    float* scratch = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * b.x + 2 * b.a + b.part);
     const float first = ldexpf(1.0f, ex[0]);
     double* part = reinterpret_cast<double*>(static_cast<char*>(workspace) + 2 * b.x + 2 * b.a);
     if (dtype == EBS_F32) rc = launch_normalize<float>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
@@ -212,20 +217,20 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
         const GemmOperand xs{x, b.ld, tall, 2, b.plane, 2 * b.plane}, as{A, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane}, bs{B, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane};
         const int ea = 2 * ex[s] - 14;                          // entries of A are at most the square of X's bound: below 2^14
         PlanesOut oa{A, nullptr, b.side_ld, b.side_plane, 2 * b.side_plane, 0, 0, 0, ldexpf(1.0f, ea - 2 * ex[s]), 0.0f};
-        if ((rc = launch_gemm(xs, xs, GemmShape{m, m, n, batch, true}, oa, st))) return rc;
+        if ((rc = launch_gemm(xs, xs, GemmShape{m, m, n, batch, true}, scratch, oa, st))) return rc;
         // B 2^eb = b A + c A^2  (A is symmetric: its rows are its columns)
         PlanesOut ob{B, A, b.side_ld, b.side_plane, 2 * b.side_plane, b.side_ld, b.side_plane, 2 * b.side_plane, coeff[2] * ldexpf(1.0f, eb[s] - 2 * ea), coeff[1] * ldexpf(1.0f, eb[s] - ea)};
-        if ((rc = launch_gemm(as, as, GemmShape{m, m, m, batch, true}, ob, st))) return rc;
+        if ((rc = launch_gemm(as, as, GemmShape{m, m, m, batch, true}, scratch, ob, st))) return rc;
         // X 2^ex' = a X + B X or a X + X B; the last one is the result
         const GemmOperand xk{x, b.ld, false, 2, b.plane, 2 * b.plane}, xm{x, b.ld, true, 2, b.plane, 2 * b.plane};
         const GemmOperand &left = tall ? xk : bs, &right = tall ? bs : xm;
         const GemmShape shape{rows, cols, m, batch};
         if (s == steps - 1) {
             const float to = scale * ldexpf(1.0f, -eb[s] - ex[s]), from = scale * coeff[0] * ldexpf(1.0f, -ex[s]);
-            return launch_gemm(left, right, shape, FinalOut{out, x, cols, (long long)rows * cols, b.ld, b.plane, 2 * b.plane, to, from}, dtype, st);
+            return launch_gemm(left, right, shape, scratch, FinalOut{out, x, cols, (long long)rows * cols, b.ld, b.plane, 2 * b.plane, to, from}, dtype, st);
         }
         PlanesOut ox{x2, x, b.ld, b.plane, 2 * b.plane, b.ld, b.plane, 2 * b.plane, ldexpf(1.0f, ex[s + 1] - eb[s] - ex[s]), coeff[0] * ldexpf(1.0f, ex[s + 1] - ex[s])};
-        if ((rc = launch_gemm(left, right, shape, ox, st))) return rc;
+        if ((rc = launch_gemm(left, right, shape, scratch, ox, st))) return rc;
         __half* t = x; x = x2; x2 = t;
     }
     if (steps > 0) return EBS_OK;
