@@ -2,8 +2,8 @@
 //
 // The MMAs are M = 256, N = 256 over both blocks' shared and tensor memory (cta_group::2): each block fetches its 128 rows of A and half
 // of the 256 columns of B, so that an operand element crosses shared memory half as often as in a single block's 128 x 128 tile
-// (that one reads 128 bytes a clock, all there are).  Warp 8 of each block fetches by TMA, warp 9 of the even block issues, warps 0-7
-// of both take the sums of their 128 rows out of tensor memory (lanes 32 (w % 4), columns 128 (w / 4)) and write the results
+// (that one reads 128 bytes a clock, all there are).  Warp 16 of each block fetches by TMA, warp 17 of the even block issues, warps 0-15
+// of both take the sums of their 128 rows out of tensor memory (lanes 32 (w % 4), columns 64 (w / 4)) and write the results
 // through a patch of shared memory, so that neighbouring lanes write neighbouring bytes.  Two accumulators of 256 columns: the
 // MMAs of the next tile (split products: of the next GEMM_CHUNK stages, see gemm_tile.cu) run while one is taken out.
 #include "gemm_tile.cuh"
@@ -37,31 +37,44 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void*
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];\n" ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z) : "memory");
 }
 __device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;\n" ::: "memory"); }
-__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
 
-// CW, BUFFERS; TERMS: fp32 values a column; begin: the columns' terms of a tile; ahead: what a row needs from memory; finish: the values
-// into the buffer(s); planes: stores a buffer leads to.
+// A warp's ring of R buffers: a buffer is written again when the store that reads it, R stores back, is done with it.
+template <int R>
+struct RowRing {
+    uint8_t* base;
+    int lane, at = 0;
+    __device__ __forceinline__ uint8_t* next() {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;\n" ::"n"(R - 1) : "memory");
+        __syncwarp();
+        uint8_t* p = base + at * PAIR_BUFFER;
+        at = at + 1 == R ? 0 : at + 1;
+        return p;
+    }
+    // after every lane has written its row; one store is one group
+    __device__ __forceinline__ void store(const CUtensorMap* map, const uint8_t* buffer, int x, int y, int z, bool exists) {
+        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            if (exists) tma_store_3d(map, buffer, x, y, z);
+            tma_store_commit();
+        }
+    }
+};
+
+// CW: columns at a time; begin: the columns' terms of a tile; ahead: what a row needs from memory; finish: the values into buffers.
 template <class EPI> struct RowOut;
 
 template <typename T>
 struct RowOut<LinearOut<T>> {
-    static constexpr int CW = 64 / sizeof(T), BUFFERS = sizeof(T) == 2 ? 2 : 1, TERMS = sizeof(T) == 2 ? 1 : 2, N = Pack<T>::N;
+    static constexpr int CW = 64 / sizeof(T), N = Pack<T>::N;
     struct Ahead { uint4 residual[4]; };
-    // returns whether every column's exponent is an ordinary one
-    static __device__ __forceinline__ bool begin(const LinearOut<T>& e, float* terms, int col0, int cols, int lane) {
-        bool plain = true;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = i * 32 + lane, col = col0 + at;
-            terms[at] = e.o.bias && col < cols ? to_f32(static_cast<const T*>(e.o.bias)[col]) : 0.0f;
-            if (sizeof(T) == 4) {
-                const int x = col < cols ? e.o.col_exp[col] : 0;
-                plain = plain && abs(x) <= SCALE_PLAIN;
-                terms[128 + at] = power_of_two(abs(x) <= SCALE_PLAIN ? x : 0) * e.o.alpha;
-            }
+    static __device__ __forceinline__ void begin(const LinearOut<T>& e, float* terms, int at, int col, int cols) {
+        terms[at] = e.o.bias && col < cols ? to_f32(static_cast<const T*>(e.o.bias)[col]) : 0.0f;
+        if (sizeof(T) == 4) {                                 // (a factor of zero: an exponent that is not an ordinary one)
+            const int x = col < cols ? e.o.col_exp[col] : 0;
+            terms[64 + at] = abs(x) <= SCALE_PLAIN ? power_of_two(x) * e.o.alpha : 0.0f;
         }
-        return __all_sync(0xffffffffu, plain);
     }
     static __device__ __forceinline__ int row_term(const LinearOut<T>& e, long long row, bool exists) { return sizeof(T) == 4 && exists ? e.o.row_exp[row] : 0; }
     static __device__ __forceinline__ void ahead(const LinearOut<T>& e, int, long long row, int col, int left, Ahead& a) {
@@ -71,29 +84,38 @@ struct RowOut<LinearOut<T>> {
         for (int c = 0; c < 4; ++c)
             if (c * N < left) a.residual[c] = load_raw(p + c * N, left - c * N, left >= (c + 1) * N);
     }
-    // first: the pre-activations (if wanted) in buffer 0 (T of two bytes: 1), then the result in buffer 0
-    static __device__ __forceinline__ void scale(const LinearOut<T>& e, float (&v)[CW], const float* terms, long long row, int col, int left, int row_term, bool plain) {
+    static __device__ __forceinline__ void scale(const LinearOut<T>& e, float (&v)[CW], const float* terms, long long row, int col, int left, int row_term, uint8_t* buffer, int lane, bool exists) {
         if constexpr (sizeof(T) == 4) {
-            if (plain && abs(row_term) <= SCALE_PLAIN) {
+            float t[CW];
+            bool plain = abs(row_term) <= SCALE_PLAIN;
+#pragma unroll
+            for (int i = 0; i < CW; i += 4) {
+                *reinterpret_cast<float4*>(t + i) = *reinterpret_cast<const float4*>(terms + 64 + i);
+                plain = plain && t[i] != 0.0f && t[i + 1] != 0.0f && t[i + 2] != 0.0f && t[i + 3] != 0.0f;
+            }
+            if (plain) {
                 const float f = power_of_two(row_term);
 #pragma unroll
                 for (int i = 0; i < CW; i += 4) {
-                    const float4 t = *reinterpret_cast<const float4*>(terms + 128 + i), b = *reinterpret_cast<const float4*>(terms + i);
-                    v[i] = fmaf(v[i], f * t.x, b.x); v[i + 1] = fmaf(v[i + 1], f * t.y, b.y);
-                    v[i + 2] = fmaf(v[i + 2], f * t.z, b.z); v[i + 3] = fmaf(v[i + 3], f * t.w, b.w);
+                    const float4 b = *reinterpret_cast<const float4*>(terms + i);
+                    v[i] = fmaf(v[i], f * t[i], b.x); v[i + 1] = fmaf(v[i + 1], f * t[i + 1], b.y);
+                    v[i + 2] = fmaf(v[i + 2], f * t[i + 2], b.z); v[i + 3] = fmaf(v[i + 3], f * t[i + 3], b.w);
                 }
                 return;
             }
+            // rare: through this thread's row of the buffer, an element at a time
             const GemmFp32& g = e.o.fp32;
+            put_row<float>(buffer, lane, v);
 #pragma unroll 1
             for (int i = 0; i < CW && i < left; ++i) {
-                float s = 0.0f;
+                float* at = reinterpret_cast<float*>(row_chunk(buffer, lane, i >> 2)) + (i & 3);
+                const float s = exists ? gemm_unscale(g.a + row * g.a_row, g.a_red, g.b + (col + i) * g.b_col, g.b_red, g.red, row_term, e.o.col_exp[col + i], *at) : 0.0f;
+                *at = fmaf(s, e.o.alpha, terms[i]);
+            }
 #pragma unroll
-                for (int q = 0; q < CW; ++q) s = q == i ? v[q] : s;                      // (registers have no index)
-                s = gemm_unscale(g.a + row * g.a_row, g.a_red, g.b + (col + i) * g.b_col, g.b_red, g.red, row_term, e.o.col_exp[col + i], s);
-                s = fmaf(s, e.o.alpha, terms[i]);
-#pragma unroll
-                for (int q = 0; q < CW; ++q) v[q] = q == i ? s : v[q];
+            for (int c = 0; c < 4; ++c) {
+                const float4 q = *reinterpret_cast<const float4*>(row_chunk(buffer, lane, c));
+                v[4 * c] = q.x; v[4 * c + 1] = q.y; v[4 * c + 2] = q.z; v[4 * c + 3] = q.w;
             }
         } else {
 #pragma unroll
@@ -121,142 +143,112 @@ struct RowOut<LinearOut<T>> {
             }
         }
     }
-    // the buffer is free of earlier stores' reads when this is called
-    static __device__ __forceinline__ void finish(const LinearOut<T>& e, const CUtensorMap* y, const CUtensorMap* z, uint8_t* buffer, float (&v)[CW], const float* terms, int, int batch, int row0,
-                                                  int col, int left, int lane, int row_term, bool plain, const Ahead& a, bool store) {
-        scale(e, v, terms, row0 + lane, col, left, row_term, plain);
+    template <int R>
+    static __device__ __forceinline__ void finish(const LinearOut<T>& e, const CUtensorMap* y, const CUtensorMap* z, RowRing<R>& ring, float (&v)[CW], const float* terms, int, int rows, int batch, int row0,
+                                                  int col, int left, int row_term, const Ahead& a, bool exists) {
+        uint8_t* to = ring.next();
+        scale(e, v, terms, row0 + ring.lane, col, left, row_term, to, ring.lane, row0 + ring.lane < rows);
         if (e.o.z) {
-            uint8_t* to = buffer + (BUFFERS - 1) * PAIR_BUFFER;
-            put_row<T>(to, lane, v);
-            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-            __syncwarp();
-            if (lane == 0 && store) { tma_store_3d(z, to, col, row0, batch); tma_store_commit(); }
-            if (BUFFERS == 1) {
-                if (lane == 0) tma_store_wait_read();
-                __syncwarp();
-            }
+            put_row<T>(to, ring.lane, v);
+            ring.store(z, to, col, row0, batch, exists);
+            to = ring.next();
         }
         activate(e, v, a);
-        put_row<T>(buffer, lane, v);
-        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-        __syncwarp();
-        if (lane == 0 && store) { tma_store_3d(y, buffer, col, row0, batch); tma_store_commit(); }
+        put_row<T>(to, ring.lane, v);
+        ring.store(y, to, col, row0, batch, exists);
     }
 };
 
-// Rows of planes: hi in buffer 0, lo in buffer 1.
+// Rows of planes: a buffer for hi, one for lo.
 template <>
 struct RowOut<PlanesOut> {
-    static constexpr int CW = 32, BUFFERS = 2, TERMS = 0;
-    struct Ahead { uint4 hi[4], lo[4]; };
-    static __device__ __forceinline__ bool begin(const PlanesOut&, float*, int, int, int) { return true; }
+    static constexpr int CW = 32;
+    struct Ahead {};
+    static __device__ __forceinline__ void begin(const PlanesOut&, float*, int, int, int) {}
     static __device__ __forceinline__ int row_term(const PlanesOut&, long long, bool) { return 0; }
-    static __device__ __forceinline__ void ahead(const PlanesOut& e, int batch, long long row, int col, int left, Ahead& a) {
-        if (!e.c) return;
-        const __half* p = e.c + batch * e.c_batch + row * e.c_ld + col;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (c * 8 < left) {
-                a.hi[c] = *reinterpret_cast<const uint4*>(p + c * 8);
-                a.lo[c] = *reinterpret_cast<const uint4*>(p + e.c_plane + c * 8);
-            }
-    }
-    static __device__ __forceinline__ void finish(const PlanesOut& e, const CUtensorMap* y, const CUtensorMap*, uint8_t* buffer, float (&v)[CW], const float*, int mirror, int batch, int row0, int col,
-                                                  int left, int lane, int, bool, const Ahead& a, bool store) {
-        __half* image = e.y + batch * e.batch + (long long)col * e.ld + row0 + lane;
+    static __device__ __forceinline__ void ahead(const PlanesOut&, int, long long, int, int, Ahead&) {}
+    template <int R>
+    static __device__ __forceinline__ void matrix(__half* to, const PlanesOut& e, const CUtensorMap* y, RowRing<R>& ring, const float (&v)[CW], float factor, float on_diag, int mirror, int rows,
+                                                  int batch, int row0, int col, int left, bool exists) {
+        const int lane = ring.lane, diagonal = row0 + lane - col;             // the column of this row that lies on the diagonal
+        __half* image = to + batch * e.batch + (long long)col * e.ld + row0 + lane;
+        uint8_t* buffer = ring.next();
+        __align__(16) __half lo[CW];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            __align__(16) __half hi[8], lo[8];
-            float ch[8], cl[8];
-            if (e.c) { unpack<__half>(a.hi[c], ch); unpack<__half>(a.lo[c], cl); }
+            __align__(16) __half hi[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float t = v[c * 8 + i] * e.alpha;
-                if (e.c) t = fmaf(e.beta, ch[i] + cl[i], t);
-                hi[i] = __float2half_rn(t);
-                lo[i] = __float2half_rn(t - __half2float(hi[i]));
-            }
+            for (int i = 0; i < 8; ++i) PlanesOut::halves(v[c * 8 + i] * factor + (c * 8 + i == diagonal ? on_diag : 0.0f), hi[i], lo[c * 8 + i]);
             *row_chunk(buffer, lane, c) = *reinterpret_cast<const uint4*>(hi);
-            *row_chunk(buffer + PAIR_BUFFER, lane, c) = *reinterpret_cast<const uint4*>(lo);
-            if (mirror && row0 + lane < mirror) {                 // the image across the diagonal: 32 lanes write 64 bytes of a row
+            if (mirror && row0 + lane < rows) {                   // the image across the diagonal: 32 lanes write 64 bytes of a row
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (c * 8 + i < left) {
                         image[(c * 8 + i) * e.ld] = hi[i];
-                        image[(c * 8 + i) * e.ld + e.plane] = lo[i];
+                        image[(c * 8 + i) * e.ld + e.plane] = lo[c * 8 + i];
                     }
             }
         }
-        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-        __syncwarp();
-        if (lane == 0 && store) {
-            tma_store_3d(y, buffer, col, row0, 2 * batch);
-            tma_store_3d(y, buffer + PAIR_BUFFER, col, row0, 2 * batch + 1);
-            tma_store_commit();
-        }
+        ring.store(y, buffer, col, row0, 2 * batch, exists);
+        buffer = ring.next();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) *row_chunk(buffer, lane, c) = *reinterpret_cast<const uint4*>(lo + 8 * c);
+        ring.store(y, buffer, col, row0, 2 * batch + 1, exists);
+    }
+    template <int R>
+    static __device__ __forceinline__ void finish(const PlanesOut& e, const CUtensorMap* y, const CUtensorMap* y2, RowRing<R>& ring, float (&v)[CW], const float*, int mirror, int rows, int batch,
+                                                  int row0, int col, int left, int, const Ahead&, bool exists) {
+        matrix(e.y, e, y, ring, v, e.alpha, e.diag, mirror, rows, batch, row0, col, left, exists);
+        if (e.y2) matrix(e.y2, e, y2, ring, v, e.alpha2, e.diag2, mirror, rows, batch, row0, col, left, exists);
     }
 };
 
 template <typename T>
 struct RowOut<TypedFinal<T>> {
-    static constexpr int CW = 64 / sizeof(T), BUFFERS = 1, TERMS = 0, G = CW / 8;
-    struct Ahead { uint4 hi[G], lo[G]; };
-    static __device__ __forceinline__ bool begin(const TypedFinal<T>&, float*, int, int, int) { return true; }
+    static constexpr int CW = 64 / sizeof(T);
+    struct Ahead {};
+    static __device__ __forceinline__ void begin(const TypedFinal<T>&, float*, int, int, int) {}
     static __device__ __forceinline__ int row_term(const TypedFinal<T>&, long long, bool) { return 0; }
-    static __device__ __forceinline__ void ahead(const TypedFinal<T>& e, int batch, long long row, int col, int left, Ahead& a) {
-        const __half* p = e.o.c + batch * e.o.c_batch + row * e.o.c_ld + col;
+    static __device__ __forceinline__ void ahead(const TypedFinal<T>&, int, long long, int, int, Ahead&) {}
+    template <int R>
+    static __device__ __forceinline__ void finish(const TypedFinal<T>& e, const CUtensorMap* y, const CUtensorMap*, RowRing<R>& ring, float (&v)[CW], const float*, int, int rows, int batch, int row0, int col,
+                                                  int, int, const Ahead&, bool exists) {
 #pragma unroll
-        for (int c = 0; c < G; ++c)
-            if (c * 8 < left) {
-                a.hi[c] = *reinterpret_cast<const uint4*>(p + c * 8);
-                a.lo[c] = *reinterpret_cast<const uint4*>(p + e.o.c_plane + c * 8);
-            }
-    }
-    static __device__ __forceinline__ void finish(const TypedFinal<T>& e, const CUtensorMap* y, const CUtensorMap*, uint8_t* buffer, float (&v)[CW], const float*, int, int batch, int row0, int col,
-                                                  int, int lane, int, bool, const Ahead& a, bool store) {
-#pragma unroll
-        for (int c = 0; c < G; ++c) {
-            float ch[8], cl[8];
-            unpack<__half>(a.hi[c], ch);
-            unpack<__half>(a.lo[c], cl);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[c * 8 + i] = fmaf(e.o.beta, ch[i] + cl[i], v[c * 8 + i] * e.o.alpha);
-        }
-        put_row<T>(buffer, lane, v);
-        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-        __syncwarp();
-        if (lane == 0 && store) { tma_store_3d(y, buffer, col, row0, batch); tma_store_commit(); }
+        for (int i = 0; i < CW; ++i) v[i] *= e.o.alpha;
+        uint8_t* to = ring.next();
+        put_row<T>(to, ring.lane, v);
+        ring.store(y, to, col, row0, batch, exists);
     }
 };
 
 template <>
 struct RowOut<PartialOut> {
-    static constexpr int CW = 16, BUFFERS = 1, TERMS = 0;
+    static constexpr int CW = 16;
     struct Ahead {};
-    static __device__ __forceinline__ bool begin(const PartialOut&, float*, int, int, int) { return true; }
+    static __device__ __forceinline__ void begin(const PartialOut&, float*, int, int, int) {}
     static __device__ __forceinline__ int row_term(const PartialOut&, long long, bool) { return 0; }
     static __device__ __forceinline__ void ahead(const PartialOut&, int, long long, int, int, Ahead&) {}
-    static __device__ __forceinline__ void finish(const PartialOut&, const CUtensorMap* y, const CUtensorMap*, uint8_t* buffer, float (&v)[CW], const float*, int, int slice, int row0, int col, int,
-                                                  int lane, int, bool, const Ahead&, bool store) {
-        put_row<float>(buffer, lane, v);
-        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-        __syncwarp();
-        if (lane == 0 && store) { tma_store_3d(y, buffer, col, row0, slice); tma_store_commit(); }
+    template <int R>
+    static __device__ __forceinline__ void finish(const PartialOut&, const CUtensorMap* y, const CUtensorMap*, RowRing<R>& ring, float (&v)[CW], const float*, int, int, int slice, int row0, int col, int,
+                                                  int, const Ahead&, bool exists) {
+        uint8_t* to = ring.next();
+        put_row<float>(to, ring.lane, v);
+        ring.store(y, to, col, row0, slice, exists);
     }
 };
 
-constexpr int PAIR_THREADS = 384;                                // three warpgroups: two that take sums out, one that fetches and issues (two of its warps idle)
+constexpr int PAIR_EPI_WARPS = 16;                               // a quarter of the columns each four: fewer leave the memory and barrier latencies of small reductions in the open
+constexpr int PAIR_THREADS = (PAIR_EPI_WARPS + 4) * 32;          // and a warpgroup that fetches and issues (two of its warps idle)
 constexpr int PAIR_HALF = 128 * GEMM_ROW_BYTES;                  // 128 rows of 64 elements
 template <int PL> __host__ __device__ constexpr int pair_stage_bytes() { return 2 * PL * PAIR_HALF; }
 template <int PL> __host__ __device__ constexpr int pair_stages() { return PL == 1 ? 5 : 3; }
-// Per warp, behind the stages: 64-byte rows of results on their way out (one buffer, or two), the columns' terms as fp32.
-constexpr int PAIR_PATCH_COLUMNS = 16, PAIR_PATCH_PITCH = PAIR_PATCH_COLUMNS + 4;
-template <class EPI> __host__ __device__ constexpr int pair_warp_bytes() {
-    const int buffers = RowOut<EPI>::BUFFERS * PAIR_BUFFER, patch = 32 * PAIR_PATCH_PITCH * 4;
-    return (buffers > patch ? buffers : patch) + RowOut<EPI>::TERMS * 128 * 4;
-}
-template <class EPI, int PL> __host__ __device__ constexpr int pair_smem_bytes() {
-    return 1024 + pair_stages<PL>() * pair_stage_bytes<PL>() + 8 * pair_warp_bytes<EPI>();
+// Per warp, behind the stages: a ring of buffers of 64-byte rows of results on their way out.
+constexpr int PAIR_PATCH_COLUMNS = 8, PAIR_PATCH_PITCH = PAIR_PATCH_COLUMNS + 4;
+template <int PL> __host__ __device__ constexpr int pair_ring() { return PL == 1 ? 2 : 1; }
+constexpr int PAIR_TERMS = 4 * 2 * 64 * 4;                       // per column quarter: bias and factor of 64 columns
+constexpr int PAIR_BARRIERS = 256;
+template <int PL> __host__ __device__ constexpr int pair_smem_bytes() {
+    return pair_stages<PL>() * pair_stage_bytes<PL>() + PAIR_EPI_WARPS * pair_ring<PL>() * PAIR_BUFFER + PAIR_TERMS + PAIR_BARRIERS;
 }
 
 // A load into this block's shared memory that signals a barrier of either block of the pair.
@@ -333,12 +325,15 @@ template <class EPI, int PL>
 __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                            const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z, const TileArgs g,
                                                            const EPI epi) {
-    extern __shared__ uint8_t smem_raw[];
-    constexpr int S = pair_stages<PL>(), STAGE = pair_stage_bytes<PL>(), PC = PAIR_PATCH_COLUMNS, PITCH = PAIR_PATCH_PITCH;
-    __shared__ uint64_t full[S], empty[S], acc_full[2], acc_empty[2];
-    __shared__ uint32_t tmem_slot;
-    __shared__ volatile int abort_flag;
-    uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) uint8_t tiles[];            // (nothing static: the stages take all but a few hundred bytes)
+    constexpr int S = pair_stages<PL>(), STAGE = pair_stage_bytes<PL>(), PC = PAIR_PATCH_COLUMNS, PITCH = PAIR_PATCH_PITCH, R = pair_ring<PL>();
+    uint8_t* behind = tiles + S * STAGE;
+    float* all_terms = reinterpret_cast<float*>(behind + PAIR_EPI_WARPS * R * PAIR_BUFFER);
+    uint64_t* full = reinterpret_cast<uint64_t*>(behind + PAIR_EPI_WARPS * R * PAIR_BUFFER + PAIR_TERMS);
+    uint64_t *empty = full + S, *acc_full = empty + S, *acc_empty = acc_full + 2, *terms_there = acc_empty + 2, *terms_read = terms_there + 4;
+    uint32_t& tmem_slot = *reinterpret_cast<uint32_t*>(terms_read + 4);
+    volatile int& abort_flag = *reinterpret_cast<volatile int*>(terms_read + 5);
+    static_assert((2 * S + 12 + 2) * 8 <= PAIR_BARRIERS, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x & 1), pairs = (int)(gridDim.x >> 1);
     const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK, chunk = PL == 2 ? GEMM_CHUNK : blocks;
@@ -346,11 +341,12 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 16); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 2 * PAIR_EPI_WARPS); }
+        for (int q = 0; q < 4; ++q) { mbar_init(&terms_there[q], 4); mbar_init(&terms_read[q], 4); }
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
-    if (warp == 9) {
+    if (warp == PAIR_EPI_WARPS + 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
     }
@@ -362,12 +358,12 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     let_next_kernel_start();
     wait_for_previous_kernel();
 
-    // Split products keep 128 sums a thread.  Registers are dealt anew among the warpgroups: 2 * 128 * 208 + 128 * 80 = 63488 of the
-    // 384 * 168 = 64512 the block was launched with.  (Each at the head of its warpgroup's own code: the compiler counts registers by
+    // Split products keep 64 sums a thread.  Registers are dealt anew among the warpgroups: 4 * 128 * 104 + 128 * 56 = 60416 of the
+    // 640 * 96 = 61440 the block was launched with.  (Each at the head of its warpgroup's own code: the compiler counts registers by
     // what it can reach.)
-    if (warp >= 8) {
-      if (PL == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;\n");
-      if (warp == 8) {
+    if (warp >= PAIR_EPI_WARPS) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
+      if (warp == PAIR_EPI_WARPS) {
         const bool leader = elect_one();
         int i = 0;                                                // stages filled so far
         bool ok = true;
@@ -395,7 +391,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                 __syncwarp();
             }
         }
-      } else if (warp == 9 && rank == 0) {
+      } else if (warp == PAIR_EPI_WARPS + 1 && rank == 0) {
             const uint32_t leader = elect_one() ? 1u : 0u;
             const uint32_t idesc = gemm_idesc(256, 256, g.bf16, g.a_mn, g.b_mn);
             const uint32_t a_step = g.a_mn ? 2048 >> 4 : 32 >> 4, b_step = g.b_mn ? 2048 >> 4 : 32 >> 4;
@@ -431,39 +427,43 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
             }
       }
     } else {
-        if (PL == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;\n");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;\n");
         using Rows = RowOut<EPI>;
-        constexpr int CW = Rows::CW, WARP_BYTES = pair_warp_bytes<EPI>();
-        uint8_t* mine = tiles + S * STAGE + warp * (WARP_BYTES - Rows::TERMS * 512);
-        float* terms = reinterpret_cast<float*>(tiles + S * STAGE + 8 * (WARP_BYTES - Rows::TERMS * 512)) + warp * Rows::TERMS * 128;
-        float* patch = reinterpret_cast<float*>(mine);
-        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * 128;
+        constexpr int CW = Rows::CW;
+        RowRing<R> ring{behind + warp * R * PAIR_BUFFER, lane};
+        float* terms = all_terms + (warp >> 2) * 128;             // shared by the four warps of a column quarter
+        float* patch = reinterpret_cast<float*>(ring.base);
+        static_assert(R * PAIR_BUFFER >= 32 * PITCH * 4, "the patch lies in the ring");
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * 64;
         constexpr int N = EPI::N, PER_ROW = PC / N, ROWS = 32 / PER_ROW, STEPS = 32 / ROWS;
-        int c = 0;
+        int c = 0, done = 0;                                      // accumulators and tiles so far
         bool ok = true;
-        for (int t = (int)(blockIdx.x >> 1); t < count && ok; t += pairs) {
+        for (int t = (int)(blockIdx.x >> 1); t < count && ok; t += pairs, ++done) {
             int batch, tm, tn, part, kb0, kb1;
             pair_tile(t, tiles_m, tiles_n, g.symmetric, g.split, blocks, batch, tm, tn, part, kb0, kb1);
-            const int row0 = tm * 256 + rank * 128 + (warp & 3) * 32, col0 = tn * 256 + (warp >> 2) * 128;
+            const int row0 = tm * 256 + rank * 128 + (warp & 3) * 32, col0 = tn * 256 + (warp >> 2) * 64;
             const int slice = part * g.batch + batch;             // (parts: a matrix each)
             // rows by TMA
-            bool plain = false;
             int row_term = 0;
             if (g.packs) {
-                __syncwarp();                                     // (the terms of the tile before are read)
-                plain = Rows::begin(epi, terms, col0, g.out_cols, lane);
+                const int at = (warp & 3) * 16 + lane;
+                // (mbarriers, not a block barrier: a warp that gave up is not waited for without end)
+                if (done > 0) ok = mbar_wait_bounded(&terms_read[warp >> 2], (done - 1) & 1, &abort_flag, g.wait_limit);
+                if (!ok) break;
+                if (lane < 16) Rows::begin(epi, terms, at, col0 + at, g.out_cols);
                 row_term = Rows::row_term(epi, row0 + lane, row0 + lane < g.out_rows);
                 __syncwarp();
+                if (lane == 0) mbar_arrive(&terms_there[warp >> 2]);
+                ok = mbar_wait_bounded(&terms_there[warp >> 2], done & 1, &abort_flag, g.wait_limit);
+                if (!ok) break;
             }
             typename Rows::Ahead row_ahead;
             auto rows_ahead = [&](int column) {
                 if (row0 + lane < g.out_rows) Rows::ahead(epi, slice, row0 + lane, col0 + column, g.out_cols - col0 - column, row_ahead);
             };
             auto rows_out = [&](int column, float (&v)[CW]) {
-                if (lane == 0) tma_store_wait_read();             // the buffers' last stores have read them
-                __syncwarp();
                 const int col = col0 + column;
-                Rows::finish(epi, &map_y, &map_z, mine, v, terms + column, g.symmetric && tm != tn ? g.out_rows : 0, slice, row0, col, g.out_cols - col, lane, row_term, plain, row_ahead,
+                Rows::finish(epi, &map_y, &map_z, ring, v, terms + column, g.symmetric && tm != tn, g.out_rows, slice, row0, col, g.out_cols - col, row_term, row_ahead,
                              col < g.out_cols && row0 < g.out_rows);
             };
             // lanes that share rows, through a patch: outputs whose rows start anywhere
@@ -491,18 +491,18 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
             };
             auto put_patch = [&](const float* f) {
 #pragma unroll
-                for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(patch + lane * PITCH + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+                for (int e = 0; e < PC; e += 4) *reinterpret_cast<float4*>(patch + lane * PITCH + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
             };
             if constexpr (PL == 2) {
-                float acc[128];
+                float acc[64];
 #pragma unroll
-                for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
+                for (int j = 0; j < 64; ++j) acc[j] = 0.0f;
                 for (int kb = kb0; kb < kb1 && ok; kb += chunk, ++c) {
                     ok = mbar_wait_bounded(&acc_full[c & 1], (c >> 1) & 1, &abort_flag, g.wait_limit);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
 #pragma unroll
-                    for (int j = 0; j < 128; j += 32) {
+                    for (int j = 0; j < 64; j += 32) {
                         uint32_t v[32];
                         tmem_ld32_issue(lanes + (c & 1) * 256 + j, v);
                         tmem_ld32_wait(v);
@@ -513,23 +513,28 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                     if (lane == 0) mbar_arrive_cluster(cluster_addr(&acc_empty[c & 1], 0));
                 }
                 if (!ok) break;
+                if (g.packs) {
+#pragma unroll
+                    for (int j = 0; j < 64; j += CW) {
+                        rows_ahead(j);
+                        float v[CW];
+#pragma unroll
+                        for (int e = 0; e < CW; ++e) v[e] = acc[j + e];
+                        rows_out(j, v);
+                    }
+                } else {
 #pragma unroll 1
-                for (int j = 0; j < 128 / CW; ++j) {              // (registers have no index: one copy of the moves a position)
-                    if (g.packs) rows_ahead(j * CW);
-                    float v[CW];
+                    for (int j = 0; j < 64; j += PC) {            // (registers have no index: one copy of the moves a position)
+                        float v[PC];
 #pragma unroll
-                    for (int q = 0; q < 128 / CW; ++q)
-                        if (q == j) {
+                        for (int q = 0; q < 64; q += PC)
+                            if (q == j) {
 #pragma unroll
-                            for (int e = 0; e < CW; ++e) v[e] = acc[q * CW + e];
-                        }
-                    if (g.packs) rows_out(j * CW, v);
-                    else
-#pragma unroll
-                        for (int h = 0; h < CW; h += 16) {
-                            put_patch(v + h);
-                            patch_out(j * CW + h);
-                        }
+                                for (int e = 0; e < PC; ++e) v[e] = acc[q + e];
+                            }
+                        put_patch(v);
+                        patch_out(j);
+                    }
                 }
             } else {
                 if (g.packs) rows_ahead(0);
@@ -537,12 +542,12 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
 #pragma unroll 1
-                for (int j = 0; j < 128; j += 32) {
+                for (int j = 0; j < 64; j += 32) {
                     uint32_t raw[32];
                     tmem_ld32_issue(lanes + (c & 1) * 256 + j, raw);
                     if (g.packs && j > 0) rows_ahead(j);
                     tmem_ld32_wait(raw);
-                    if (j == 96) {
+                    if (j == 32) {
                         asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
                         if (lane == 0) mbar_arrive_cluster(cluster_addr(&acc_empty[c & 1], 0));
                     }
@@ -554,7 +559,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                         if (g.packs) rows_out(j + h, v);
                         else
 #pragma unroll
-                            for (int q = 0; q < CW; q += 16) {
+                            for (int q = 0; q < CW; q += PC) {
                                 put_patch(v + q);
                                 patch_out(j + h + q);
                             }
@@ -562,6 +567,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                 }
                 ++c;
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&terms_read[warp >> 2]);
         }
         if (lane == 0) tma_store_wait_all();
     }
@@ -572,7 +579,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     }
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     cluster_sync_all();                                           // no block leaves while the other's MMAs or arrivals reach it
-    if (warp == 9)
+    if (warp == PAIR_EPI_WARPS + 1)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512u) : "memory");
 }
 
@@ -597,7 +604,9 @@ static bool result_maps(const LinearOut<T>& e, const GemmShape& s, CUtensorMap* 
     const auto whole = [](const void* p, long long ld) { return !p || (((uintptr_t)p & 15) == 0 && (ld * sizeof(T)) % 16 == 0); };
     return whole(e.o.residual, e.o.ldr) && result_map<T>(e.o.y, s.rows, s.cols, e.o.ldy, 1, 0, y) && result_map<T>(e.o.z, s.rows, s.cols, e.o.ldz, 1, 0, z);
 }
-static bool result_maps(const PlanesOut& e, const GemmShape& s, CUtensorMap* y, CUtensorMap*) { return result_map<__half>(e.y, s.rows, s.cols, e.ld, 2LL * s.batch, e.plane, y); }
+static bool result_maps(const PlanesOut& e, const GemmShape& s, CUtensorMap* y, CUtensorMap* y2) {
+    return result_map<__half>(e.y, s.rows, s.cols, e.ld, 2LL * s.batch, e.plane, y) && result_map<__half>(e.y2, s.rows, s.cols, e.ld, 2LL * s.batch, e.plane, y2);
+}
 template <typename T>
 static bool result_maps(const TypedFinal<T>& e, const GemmShape& s, CUtensorMap* y, CUtensorMap*) {
     return result_map<T>(e.o.y, s.rows, s.cols, e.o.ld, s.batch, e.o.batch, y);
@@ -628,7 +637,7 @@ static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmSha
     g.packs = result_maps(epi, s, &y, &z);
     if (symmetric && !g.packs) return EBS_ERR_CUDA;               // (kept planes always have whole rows)
     auto kern = gemm_pair_kernel<EPI, PL>;
-    constexpr int bytes = pair_smem_bytes<EPI, PL>();
+    constexpr int bytes = pair_smem_bytes<PL>();
     static_assert(bytes <= 227 * 1024, "shared memory of a block");
     static bool attr_set[64] = {};
     int dev = 0;

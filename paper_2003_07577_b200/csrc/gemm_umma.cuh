@@ -107,67 +107,54 @@ struct LinearOut {
     }
 };
 
-// Rows of a kept matrix: two fp16 planes hi + lo, rows padded to whole groups of eight elements (so that a pack is always whole).
-template <int N>
-struct PlanePack { __align__(2 * N) __half hi[N], lo[N]; };
-template <int N>
-__device__ __forceinline__ void load_planes(const __half* p, long long plane, PlanePack<N>& a) {
-    using V = typename std::conditional<N == 8, uint4, uint2>::type;
-    *reinterpret_cast<V*>(a.hi) = *reinterpret_cast<const V*>(p);
-    *reinterpret_cast<V*>(a.lo) = *reinterpret_cast<const V*>(p + plane);
-}
-
-// Results kept for further products: v = alpha * sum + beta * (c_hi + c_lo), as two fp16 planes hi + lo (value: times 2^-e of the
-// caller's choice, folded into alpha and beta).  c and y: planes `plane` elements apart, matrices of a batch `batch` apart.
+// Results kept for further products, as two fp16 planes hi + lo (the value times a power of two of the caller's choice, folded into the
+// factors): alpha * sum + diag * (row == col), and a second matrix alpha2 * sum + diag2 * (row == col) of the same form where y2 is
+// set.  Rows are padded to whole groups of eight elements, so that a pack is always whole.
 struct PlanesOut {
     static constexpr int N = 4;
     struct Columns {};
-    using Ahead = PlanePack<4>;
+    struct Ahead {};
     __half* y;
-    const __half* c;
-    long long ld, plane, batch;
-    long long c_ld, c_plane, c_batch;
-    float alpha, beta;
+    __half* y2;
+    long long ld, plane, batch;            // of either: elements between rows, planes, matrices of a batch
+    float alpha, diag, alpha2, diag2;
     __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
-    __device__ __forceinline__ void ahead(int b, long long row, int col, int, bool, Ahead& a) const {
-        if (c) load_planes(c + b * c_batch + row * c_ld + col, c_plane, a);
+    __device__ __forceinline__ void ahead(int, long long, int, int, bool, Ahead&) const {}
+    static __device__ __forceinline__ void halves(float v, __half& hi, __half& lo) {
+        hi = __float2half_rn(v);
+        lo = __float2half_rn(v - __half2float(hi));
     }
-    __device__ __forceinline__ void pack(int b, long long row, int col, int, bool, float (&v)[N], const Columns&, const Ahead& a) const {
-        PlanePack<4> o;
+    __device__ __forceinline__ void store(__half* q, long long row, int col, const float (&v)[N], float factor, float on_diag) const {
+        __align__(8) __half hi[4], lo[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float t = v[i] * alpha;
-            if (c) t = fmaf(beta, __half2float(a.hi[i]) + __half2float(a.lo[i]), t);
-            o.hi[i] = __float2half_rn(t);
-            o.lo[i] = __float2half_rn(t - __half2float(o.hi[i]));
-        }
-        __half* q = y + b * batch + row * ld + col;
-        *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(o.hi);
-        *reinterpret_cast<uint2*>(q + plane) = *reinterpret_cast<const uint2*>(o.lo);
+        for (int i = 0; i < 4; ++i) halves(v[i] * factor + (row == col + i ? on_diag : 0.0f), hi[i], lo[i]);
+        *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(hi);
+        *reinterpret_cast<uint2*>(q + plane) = *reinterpret_cast<const uint2*>(lo);
+    }
+    __device__ __forceinline__ void pack(int b, long long row, int col, int, bool, float (&v)[N], const Columns&, const Ahead&) const {
+        const long long at = b * batch + row * ld + col;
+        store(y + at, row, col, v, alpha, diag);
+        if (y2) store(y2 + at, row, col, v, alpha2, diag2);
     }
 };
 
-// The last product of an orthogonalisation: v = alpha * sum + beta * (c_hi + c_lo), rounded to the caller's type.
+// The last product of an orthogonalisation: alpha * sum, rounded to the caller's type.
 struct FinalOut {
     void* y;
-    const __half* c;
     long long ld, batch;
-    long long c_ld, c_plane, c_batch;
-    float alpha, beta;
+    float alpha;
 };
 template <typename T>
 struct TypedFinal {
     static constexpr int N = Pack<T>::N;
     struct Columns {};
-    using Ahead = PlanePack<N>;
+    struct Ahead {};
     FinalOut o;
     __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
-    __device__ __forceinline__ void ahead(int b, long long row, int col, int, bool, Ahead& a) const {
-        load_planes(o.c + b * o.c_batch + row * o.c_ld + col, o.c_plane, a);
-    }
-    __device__ __forceinline__ void pack(int b, long long row, int col, int left, bool vec, float (&v)[N], const Columns&, const Ahead& a) const {
+    __device__ __forceinline__ void ahead(int, long long, int, int, bool, Ahead&) const {}
+    __device__ __forceinline__ void pack(int b, long long row, int col, int left, bool vec, float (&v)[N], const Columns&, const Ahead&) const {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = fmaf(o.beta, __half2float(a.hi[i]) + __half2float(a.lo[i]), v[i] * o.alpha);
+        for (int i = 0; i < N; ++i) v[i] *= o.alpha;
         store_pack(static_cast<T*>(o.y) + b * o.batch + row * o.ld + col, v, left, vec);
     }
 };

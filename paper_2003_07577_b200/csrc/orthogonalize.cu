@@ -7,9 +7,11 @@ namespace ebs {
 
 static size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-// Matrices are kept as two fp16 planes hi + lo (22 bits) times a power of two: X by 2^-ex, its Gram matrix A by 2^-ea and
-// B = b A + c A^2 by 2^-eb, chosen from bounds of the singular values so that no entry leaves fp16 (an entry is at most the
-// largest singular value).
+// A step is three products: the Gram matrix A of X, Q = a I + A (b I + c A), and X <- Q X.  What is added to a product lies on its
+// diagonal, so that no product reads anything beside its operands: A and b I + c A leave the first one together.  The first two are
+// symmetric; half of each is summed.
+// Matrices are kept as two fp16 planes hi + lo (22 bits) times a power of two each, chosen from bounds of the singular values so that
+// no entry leaves fp16 (an entry is at most the largest singular value).
 // Elements i .. i + N - 1 of a dense matrix of `count`, one 16-byte access where they all exist and it is aligned.
 template <typename T>
 __device__ __forceinline__ void load_elements(const T* p, long long left, bool vec, float (&v)[Pack<T>::N]) {
@@ -117,19 +119,27 @@ __global__ void __launch_bounds__(256) scale_out_kernel(const __half* x, long lo
     }
 }
 
-// The largest singular value a step can give from singular values in 0 .. s, and the largest of |b v + c v^2|, v in 0 .. s^2 (b A + c A^2).
-static void step_bounds(const float* c, double s, double* next, double* inner) {
-    double top = 0.0, in = 0.0;
+// For singular values in 0 .. s: the largest a step can give, and the largest entries of b + c v and a + b v + c v^2, v in 0 .. s^2.
+struct StepBounds {
+    double next, linear, square;
+};
+static StepBounds step_bounds(const float* c, double s) {
+    StepBounds b = {0.0, fabs(c[1]), fabs(c[0])};
     for (int j = 1; j <= 4096; ++j) {
-        const double v = s * j / 4096.0, v2 = v * v, q = fabs(v2 * (c[1] + v2 * (double)c[2])), p = fabs(v * (c[0] + v2 * (c[1] + v2 * (double)c[2])));
-        top = p > top ? p : top;
-        in = q > in ? q : in;
+        const double v = s * j / 4096.0, v2 = v * v, l = fabs(c[1] + v2 * (double)c[2]), q = fabs(c[0] + v2 * (c[1] + v2 * (double)c[2]));
+        b.next = fmax(b.next, v * q);
+        b.linear = fmax(b.linear, l);
+        b.square = fmax(b.square, q);
     }
-    *next = top;
-    *inner = in;
+    return b;
 }
 // The exponent e with v * 2^e in [2^13, 2^14): a factor of four below fp16's largest value for what roundings add to the bounds.
-static int headroom(double v) { int e; frexp(v > 0.0 ? v : 1.0, &e); return 14 - e; }
+// (At most 2^60: coefficients next to zero.)
+static int headroom(double v) {
+    int e;
+    frexp(v > 0x1p-46 ? v : 0x1p-46, &e);
+    return 14 - e;
+}
 
 struct OrthoBuffers {
     long long ld, plane, side_ld, side_plane;
@@ -152,7 +162,7 @@ static OrthoBuffers ortho_buffers(int batch, int rows, int cols) {
     const int m = (int)side, n = rows < cols ? cols : rows;
     const GemmShape shapes[] = {{m, m, n, batch, true}, {m, m, m, batch, true}, {rows, cols, m, batch}};
     for (const GemmShape& s : shapes) { const size_t need = round256(gemm_route(s, 2).scratch); b.scratch = need > b.scratch ? need : b.scratch; }
-    b.total = 2 * b.x + 2 * b.a + b.part + b.scratch;
+    b.total = 2 * b.x + 3 * b.a + b.part + b.scratch;
     return b;
 }
 static int check_shape(int batch, int rows, int cols, int dtype, int steps) {
@@ -180,17 +190,17 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     if (((uintptr_t)g & 15) || ((uintptr_t)out & 15) || ((uintptr_t)workspace & 15)) return EBS_ERR_INVALID_ARG;
     for (int i = 0; i < 3; ++i)
         if (!isfinite(coeff[i])) return EBS_ERR_INVALID_ARG;
-    // singular values before each step, and the exponents of X, A and B
+    // the singular values' bound before each step
     double bound = 1.0;
-    int ex[65], eb[64];
+    int ex[65], el[64], eq[64];                               // exponents of X, b I + c A, Q
     for (int i = 0; i <= steps; ++i) {
         if (!(bound < 0x1p20 && bound > 0x1p-20)) return EBS_ERR_UNSUPPORTED;
         ex[i] = headroom(bound);
         if (i == steps) break;
-        double next, inner;
-        step_bounds(coeff, bound, &next, &inner);
-        eb[i] = headroom(inner) < 60 ? headroom(inner) : 60;
-        bound = next;
+        const StepBounds b = step_bounds(coeff, bound);
+        el[i] = headroom(b.linear);
+        eq[i] = headroom(b.square);
+        bound = b.next;
     }
     const OrthoBuffers b = ortho_buffers(batch, rows, cols);
     if (workspace_bytes < b.total) return EBS_ERR_INVALID_ARG;
@@ -202,10 +212,11 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     __half* x = static_cast<__half*>(workspace);
     __half* x2 = reinterpret_cast<__half*>(static_cast<char*>(workspace) + b.x);
     __half* A = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x);
-    __half* B = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x + b.a);
-    float* scratch = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * b.x + 2 * b.a + b.part);
+    __half* L = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x + b.a);
+    __half* Q = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x + 2 * b.a);
+    float* scratch = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * b.x + 3 * b.a + b.part);
     const float first = ldexpf(1.0f, ex[0]);
-    double* part = reinterpret_cast<double*>(static_cast<char*>(workspace) + 2 * b.x + 2 * b.a);
+    double* part = reinterpret_cast<double*>(static_cast<char*>(workspace) + 2 * b.x + 3 * b.a);
     if (dtype == EBS_F32) rc = launch_normalize<float>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
     else if (dtype == EBS_F16) rc = launch_normalize<__half>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
     else rc = launch_normalize<__nv_bfloat16>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
@@ -213,23 +224,19 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     const bool tall = rows > cols;                            // then X X^T X is taken as X (X^T X): the smaller product
     const int m = tall ? cols : rows, n = tall ? rows : cols;
     for (int s = 0; s < steps; ++s) {
-        // A 2^ea = X^T X or X X^T
-        const GemmOperand xs{x, b.ld, tall, 2, b.plane, 2 * b.plane}, as{A, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane}, bs{B, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane};
         const int ea = 2 * ex[s] - 14;                          // entries of A are at most the square of X's bound: below 2^14
-        PlanesOut oa{A, nullptr, b.side_ld, b.side_plane, 2 * b.side_plane, 0, 0, 0, ldexpf(1.0f, ea - 2 * ex[s]), 0.0f};
+        const GemmOperand xs{x, b.ld, tall, 2, b.plane, 2 * b.plane}, as{A, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane}, ls{L, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane},
+            qs{Q, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane};
+        PlanesOut oa{A, L, b.side_ld, b.side_plane, 2 * b.side_plane, ldexpf(1.0f, ea - 2 * ex[s]), 0.0f, coeff[2] * ldexpf(1.0f, el[s] - 2 * ex[s]), coeff[1] * ldexpf(1.0f, el[s])};
         if ((rc = launch_gemm(xs, xs, GemmShape{m, m, n, batch, true}, scratch, oa, st))) return rc;
-        // B 2^eb = b A + c A^2  (A is symmetric: its rows are its columns)
-        PlanesOut ob{B, A, b.side_ld, b.side_plane, 2 * b.side_plane, b.side_ld, b.side_plane, 2 * b.side_plane, coeff[2] * ldexpf(1.0f, eb[s] - 2 * ea), coeff[1] * ldexpf(1.0f, eb[s] - ea)};
-        if ((rc = launch_gemm(as, as, GemmShape{m, m, m, batch, true}, scratch, ob, st))) return rc;
-        // X 2^ex' = a X + B X or a X + X B; the last one is the result
+        PlanesOut oq{Q, nullptr, b.side_ld, b.side_plane, 2 * b.side_plane, ldexpf(1.0f, eq[s] - ea - el[s]), coeff[0] * ldexpf(1.0f, eq[s]), 0.0f, 0.0f};
+        if ((rc = launch_gemm(as, ls, GemmShape{m, m, m, batch, true}, scratch, oq, st))) return rc;
+        // X <- Q X or X Q; the last one is the result
         const GemmOperand xk{x, b.ld, false, 2, b.plane, 2 * b.plane}, xm{x, b.ld, true, 2, b.plane, 2 * b.plane};
-        const GemmOperand &left = tall ? xk : bs, &right = tall ? bs : xm;
+        const GemmOperand &left = tall ? xk : qs, &right = tall ? qs : xm;
         const GemmShape shape{rows, cols, m, batch};
-        if (s == steps - 1) {
-            const float to = scale * ldexpf(1.0f, -eb[s] - ex[s]), from = scale * coeff[0] * ldexpf(1.0f, -ex[s]);
-            return launch_gemm(left, right, shape, scratch, FinalOut{out, x, cols, (long long)rows * cols, b.ld, b.plane, 2 * b.plane, to, from}, dtype, st);
-        }
-        PlanesOut ox{x2, x, b.ld, b.plane, 2 * b.plane, b.ld, b.plane, 2 * b.plane, ldexpf(1.0f, ex[s + 1] - eb[s] - ex[s]), coeff[0] * ldexpf(1.0f, ex[s + 1] - ex[s])};
+        if (s == steps - 1) return launch_gemm(left, right, shape, scratch, FinalOut{out, cols, (long long)rows * cols, scale * ldexpf(1.0f, -eq[s] - ex[s])}, dtype, st);
+        PlanesOut ox{x2, nullptr, b.ld, b.plane, 2 * b.plane, ldexpf(1.0f, ex[s + 1] - eq[s] - ex[s]), 0.0f, 0.0f, 0.0f};
         if ((rc = launch_gemm(left, right, shape, scratch, ox, st))) return rc;
         __half* t = x; x = x2; x2 = t;
     }
