@@ -22,12 +22,22 @@ inline bool real_dtype(int dtype) { return dtype == EBS_F32 || dtype == EBS_F16 
 
 // Elementary functions at the accuracy of the results' type: fp32 results take CUDA's functions, 16-bit results (rounding 2^-9 or 2^-12)
 // the hardware exponential and reciprocal (relative error about 2^-21).
-template <bool FAST> __device__ __forceinline__ float exp_of(float v) { return FAST ? __expf(v) : expf(v); }
-template <bool FAST> __device__ __forceinline__ float quotient(float a, float b) { return FAST ? __fdividef(a, b) : a / b; }
+__device__ __forceinline__ float fast_reciprocal(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float fast_exp(float v) {           // 2^(v log2 e)
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v * 1.44269504f));
+    return r;
+}
+template <bool FAST> __device__ __forceinline__ float exp_of(float v) { return FAST ? fast_exp(v) : expf(v); }
+template <bool FAST> __device__ __forceinline__ float reciprocal(float v) { return FAST ? fast_reciprocal(v) : 1.0f / v; }
 // The logistic function of v and its complement, neither taken as a difference: both keep their relative accuracy.
 template <bool FAST>
 __device__ __forceinline__ void logistic(float v, float& s, float& rest) {
-    const float t = exp_of<FAST>(-fabsf(v)), r = quotient<FAST>(1.0f, 1.0f + t), tr = t * r;
+    const float t = exp_of<FAST>(-fabsf(v)), r = reciprocal<FAST>(1.0f + t), tr = t * r;
     s = v >= 0.0f ? r : tr;
     rest = v >= 0.0f ? tr : r;
 }
@@ -36,11 +46,10 @@ __device__ __forceinline__ void logistic(float v, float& s, float& rest) {
 template <bool FAST>
 __device__ __forceinline__ void normal_cdf(float z, float& cdf, float& bell) {
     if (FAST) {
-        const float a = fabsf(z) * 0.70710678f, t = __fdividef(1.0f, fmaf(0.3275911f, a, 1.0f));
-        bell = __expf(-a * a);
+        const float a = fabsf(z) * 0.70710678f, t = fast_reciprocal(fmaf(0.3275911f, a, 1.0f));
+        bell = fast_exp(-a * a);
         const float half_tail = 0.5f * bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
         cdf = z >= 0.0f ? 1.0f - half_tail : half_tail;
-        if (z != z) cdf = z;
     } else {
         bell = expf(-0.5f * z * z);
         cdf = 0.5f * (1.0f + erff(z * 0.70710678f));

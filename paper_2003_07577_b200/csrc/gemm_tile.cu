@@ -266,8 +266,18 @@ static int launch_tile_form(const GemmOperand& A, const GemmOperand& B, const Ge
     const GemmOperand &la = swap ? B : A, &lb = swap ? A : B;
     const long long tiles = (long long)((lanes + 127) / 128) * ((columns + tn - 1) / tn) * s.batch;
     const int blocks = (s.red + GEMM_BK - 1) / GEMM_BK;
+    // Parts of the reduction (us, measured): a stage takes 0.32 (split products 0.9), two, four or eight parts 1.6, 2.2 and 4.0 to meet.
+    // 250 x 336 over 1024 bf16: 11.5, 10.9, 10.1 and 11.4 with 1, 2, 4 and 8 parts; 512 x 512 over 512 fp32: 14.0, 11.7, 9.5 and 18.0
+    // (eight parts of 16 tiles no longer run at once).
+    static const float meet[4] = {0.0f, 1.6f, 2.2f, 4.0f};
     g.split = 1;
-    while (g.split < 8 && tiles * g.split * 2 <= sms && blocks >= 4 * g.split) g.split *= 2;
+    float best = 0.0f;
+    for (int i = 0; i < 4; ++i) {
+        const int parts = 1 << i;
+        if (i > 0 && (tiles * parts > (i == 3 ? sms * 3 / 4 : sms) || blocks < parts)) break;
+        const float t = (PL == 2 ? 0.9f : 0.32f) * (float)((blocks + parts - 1) / parts) + meet[i];
+        if (i == 0 || t < best) { best = t; g.split = parts; }
+    }
     g.red = s.red;
     g.out_rows = s.rows;
     g.out_cols = s.cols;

@@ -33,6 +33,10 @@ int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape
 int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmRoute& r, float* scratch, const FinalOut& out, int dtype, cudaStream_t st);
 unsigned long long gemm_pair_timeouts();
 
+// y = x W^T for up to GEMM_ROWS rows of x, all operands as they are.
+constexpr int GEMM_ROWS = 8;
+int launch_gemm_rows(const void* x, long long ldx, const void* w, long long ldw, int m, int n, int k, const GemmOut& o, int dtype, cudaStream_t st);
+
 // scratch: gemm_route(s, planes).scratch bytes.
 template <class... A>
 inline int launch_gemm(const GemmOperand& a, const GemmOperand& b, const GemmShape& s, float* scratch, const A&... rest) {

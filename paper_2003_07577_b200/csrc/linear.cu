@@ -1,4 +1,6 @@
 // Real-valued layers: y = act(x W^T + bias) + residual and its gradients.  See include/ebs.h.
+#include <type_traits>
+
 #include "gemm_tile.cuh"
 
 namespace ebs {
@@ -32,6 +34,7 @@ static int complete(const ebs_linear_desc* in, ebs_linear_desc* d) {
     *d = *in;
     if (d->m < 0 || d->n < 1 || d->k < 1 || !real_dtype(d->dtype) || d->act < EBS_ACT_NONE || d->act > EBS_ACT_SILU)
         return EBS_ERR_INVALID_ARG;
+    if (d->m > (1 << 30) || d->n > (1 << 30) || d->k > (1 << 30)) return EBS_ERR_OVERFLOW;
     const long long limit = 1LL << 40;
     long long* ld[5] = {&d->ldx, &d->ldw, &d->ldy, &d->ldr, &d->ldz};
     for (int i = 0; i < 5; ++i) {
@@ -109,7 +112,8 @@ __device__ __forceinline__ void store_split4(__half* hi_plane, __half* lo_plane,
 }
 
 // A matrix to split into planes.  across = 0: its reduction runs along a row, one exponent a row.  across = 1: down the rows, one
-// exponent a column; the largest magnitudes of the columns then come from column_tops, for each of `chunks` chunks of rows.
+// exponent a column; the largest magnitudes of the columns then come from column_tops for each of `chunks` chunks of rows, and over the
+// chunks from linear_chunks_kernel (first row of `tops`).
 struct SplitJob {
     const float* src;
     long long ld, rows;
@@ -122,29 +126,31 @@ struct SplitJob {
     unsigned blocks, first;                // thread blocks, and the first of them in the launch
 };
 constexpr int MAX_SPLIT_JOBS = 4;
+constexpr int SPLIT_WIDE = 1280;           // columns from which on a block shares a row
 struct SplitJobs {
     SplitJob job[MAX_SPLIT_JOBS];
     int count;
 };
 
-// A row is a warp's or (WIDE) a block's; its first 16 elements a thread stay in registers between the search for the largest and the split.
-template <bool WIDE>
+// A row is a warp's or (WIDE) a block's; its first 4 * H elements a thread stay in registers between the search for the largest and the
+// split, all of them on their way at once.
+template <bool WIDE, int H>
 __device__ __forceinline__ void split_rows(const SplitJob& j, unsigned block, unsigned* part) {
     constexpr int T = WIDE ? 256 : 32;
     const int t = WIDE ? threadIdx.x : threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long step = WIDE ? j.blocks : j.blocks * 8LL;
     for (long long r = WIDE ? block : block * 8LL + warp; r < j.rows; r += step) {
         const float* x = j.src + r * j.ld;
-        float4 held[4];
+        float4 held[H];
         unsigned top = 0u;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < H; ++i) {
             const int c = (i * T + t) * 4;
             held[i] = load4(x + c, j.cols - c, j.vec);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = max(max(top, max(magnitude(held[i].x), magnitude(held[i].y))), max(magnitude(held[i].z), magnitude(held[i].w)));
-        for (int c = (4 * T + t) * 4; c < j.cols; c += 4 * T) {
+        for (int i = 0; i < H; ++i) top = max(max(top, max(magnitude(held[i].x), magnitude(held[i].y))), max(magnitude(held[i].z), magnitude(held[i].w)));
+        for (int c = (H * T + t) * 4; c < j.cols; c += 4 * T) {
             const float4 v = load4(x + c, j.cols - c, j.vec);
             top = max(max(top, max(magnitude(v.x), magnitude(v.y))), max(magnitude(v.z), magnitude(v.w)));
         }
@@ -160,11 +166,11 @@ __device__ __forceinline__ void split_rows(const SplitJob& j, unsigned block, un
         if (t == 0) j.exps[r] = split_record(top);
         __half *hi = j.dst + r * j.ldd, *lo = hi + j.rows * j.ldd;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < H; ++i) {
             const int c = (i * T + t) * 4;
             if (c < j.cols) store_split4(hi + c, lo + c, held[i], es);
         }
-        for (int c = (4 * T + t) * 4; c < j.cols; c += 4 * T) store_split4(hi + c, lo + c, load4(x + c, j.cols - c, j.vec), es);
+        for (int c = (H * T + t) * 4; c < j.cols; c += 4 * T) store_split4(hi + c, lo + c, load4(x + c, j.cols - c, j.vec), es);
     }
 }
 __device__ __forceinline__ void tops_of_block(unsigned (&m)[4], unsigned (*part)[128], unsigned* out, int col0, int cols) {
@@ -186,7 +192,7 @@ __device__ __forceinline__ void column_tops(const SplitJob& j, unsigned block, u
     const long long r0 = j.rows * by / j.chunks, r1 = j.rows * (by + 1) / j.chunks;
     unsigned m[4] = {0u, 0u, 0u, 0u};
     if (c < j.cols)
-#pragma unroll 4
+#pragma unroll 8
         for (long long r = r0 + y; r < r1; r += 8) {
             const float4 v = load4(j.src + r * j.ld + c, j.cols - c, j.vec);
             m[0] = max(m[0], magnitude(v.x));
@@ -196,29 +202,19 @@ __device__ __forceinline__ void column_tops(const SplitJob& j, unsigned block, u
         }
     tops_of_block(m, part, j.tops + (size_t)by * j.cols + bx * 128, bx * 128, j.cols);
 }
-__device__ __forceinline__ void split_columns(const SplitJob& j, unsigned block, unsigned (*part)[128]) {
+__device__ __forceinline__ void split_columns(const SplitJob& j, unsigned block) {
     const int across = (j.cols + 127) / 128, bx = (int)(block % across), by = (int)(block / across), down = (int)(j.blocks / across);
     const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, c = bx * 128 + lane * 4;
-    unsigned m[4] = {0u, 0u, 0u, 0u};
-    for (int k = y; k < j.chunks; k += 8)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < j.cols) m[i] = max(m[i], j.tops[(size_t)k * j.cols + c + i]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) part[y][lane * 4 + i] = m[i];
-    __syncthreads();
     int e[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        unsigned t = 0u;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) t = max(t, part[q][lane * 4 + i]);
+        const unsigned t = c + i < j.cols ? j.tops[c + i] : 0u;
         e[i] = split_exponent(t);
         if (by == 0 && y == 0 && c + i < j.cols) j.exps[c + i] = split_record(t);
     }
     if (c >= j.cols) return;
     const long long r0 = j.rows * by / down, r1 = j.rows * (by + 1) / down;
-#pragma unroll 4
+#pragma unroll 8
     for (long long r = r0 + y; r < r1; r += 8)
         store_split4(j.dst + r * j.ldd + c, j.dst + (j.rows + r) * j.ldd + c, load4(j.src + r * j.ld + c, j.cols - c, j.vec), e);
 }
@@ -228,16 +224,21 @@ __device__ __forceinline__ int job_of(const SplitJobs& s, unsigned block) {
     while (i + 1 < s.count && block >= s.job[i + 1].first) ++i;
     return i;
 }
-// All splits of a call.
+// Splits of a call: all in one launch, or (large matrices) those by rows and those by columns in one each -- the rows' registers
+// would cost the columns half their threads.
+template <bool ROWS, bool COLUMNS>
 __global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ SplitJobs jobs) {
-    __shared__ unsigned part[8][128];
+    __shared__ unsigned part[8];
     let_next_kernel_start();
     wait_for_previous_kernel();
     const SplitJob& j = jobs.job[job_of(jobs, blockIdx.x)];
     const unsigned block = blockIdx.x - j.first;
-    if (j.across) split_columns(j, block, part);
-    else if (j.cols > 512) split_rows<true>(j, block, part[0]);
-    else split_rows<false>(j, block, part[0]);
+    if (COLUMNS && (!ROWS || j.across)) split_columns(j, block);
+    if (ROWS && (!COLUMNS || !j.across)) {
+        if (j.cols > SPLIT_WIDE) split_rows<true, 4>(j, block, part);
+        else if (j.cols > 512) split_rows<false, 10>(j, block, part);
+        else split_rows<false, 4>(j, block, part);
+    }
 }
 
 // An operand of a product: 16-bit rows as they are, or copied where their starts are not on 16 bytes; fp32 rows split.
@@ -250,9 +251,9 @@ struct Matrix {
     long long rows, ld;
     int cols;
 };
-// Chunks (of at least 32 rows) for work that goes down `across` blocks of columns: about four blocks an SM; from the sizes alone.
+// Chunks (of at least 32 rows) for work that goes down `across` blocks of columns: about eight blocks an SM; from the sizes alone.
 static int row_chunks(long long rows, int across) {
-    const long long c = (rows + 31) / 32, want = (4LL * 148 + across - 1) / across;
+    const long long c = (rows + 31) / 32, want = (8LL * 148 + across - 1) / across;
     return (int)(c < want ? c : want);
 }
 // Describes the operand and takes its buffers; fp32: adds its split to the jobs.
@@ -273,8 +274,8 @@ static Prepared plan_operand(const Matrix& m, int dtype, bool across, Carver& ws
         j.tops = ws.take<unsigned>((size_t)j.chunks * m.cols);
         j.blocks = (unsigned)(blocks * j.chunks);
     } else {
-        const long long b = m.cols > 512 ? m.rows : (m.rows + 7) / 8;
-        j.blocks = (unsigned)(b < 2048 ? b : 2048);
+        const long long b = m.cols > SPLIT_WIDE ? m.rows : (m.rows + 7) / 8;
+        j.blocks = (unsigned)(b < 4096 ? b : 4096);
     }
     out.op = GemmOperand{j.dst, ldd, across, 2, m.rows * ldd, 2 * m.rows * ldd};
     out.exps = j.exps;
@@ -287,10 +288,26 @@ static int copy_operand(const Matrix& m, const Prepared& p, cudaStream_t st) {
     return launch_chained(copy_rows_kernel, dim3((m.cols + 255) / 256, (unsigned)rows), 256, 0, st, 1, static_cast<const uint16_t*>(m.p), m.ld, m.rows, m.cols,
                           static_cast<uint16_t*>(const_cast<void*>(p.op.p)), p.op.ld);
 }
-static int launch_splits(SplitJobs& jobs, cudaStream_t st) {
-    unsigned blocks = 0;
-    for (int i = 0; i < jobs.count; ++i) { jobs.job[i].first = blocks; blocks += jobs.job[i].blocks; }
-    return blocks ? launch_chained(split_kernel, dim3(blocks), 256, 0, st, 1, jobs) : EBS_OK;
+static int launch_splits(const SplitJobs& all, cudaStream_t st) {
+    long long elements = 0;
+    for (int i = 0; i < all.count; ++i) elements += all.job[i].rows * all.job[i].cols;
+    const bool together = elements < (1LL << 22);
+    for (int pass = 0; pass < (together ? 1 : 2); ++pass) {
+        SplitJobs jobs = {};
+        unsigned blocks = 0;
+        bool rows = false, columns = false;
+        for (int i = 0; i < all.count; ++i) {
+            if (!together && all.job[i].across != pass) continue;
+            (all.job[i].across ? columns : rows) = true;
+            jobs.job[jobs.count] = all.job[i];
+            jobs.job[jobs.count++].first = blocks;
+            blocks += all.job[i].blocks;
+        }
+        if (!blocks) continue;
+        const int rc = launch_chained(rows && columns ? split_kernel<true, true> : rows ? split_kernel<true, false> : split_kernel<false, true>, dim3(blocks), 256, 0, st, 1, jobs);
+        if (rc) return rc;
+    }
+    return EBS_OK;
 }
 
 // One product with its operands prepared; a: its rows are the result's (across: its columns), likewise b for the result's columns.
@@ -329,7 +346,7 @@ struct DzArgs {
 // dz = dy * act'(z), stored times `store`, and the column sums of dz before its rounding.  A block takes 32 packs of N columns and the
 // rows of one chunk.  fp32: the column tops of dz here, those of other matrices (jobs with chunks) in further blocks.
 template <typename T, int N>
-__global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ DzArgs g, const __grid_constant__ SplitJobs jobs) {
+__global__ void __launch_bounds__(256, 4) linear_dz_kernel(const __grid_constant__ DzArgs g, const __grid_constant__ SplitJobs jobs) {
     __shared__ float sums[8][32 * N + 4];
     __shared__ unsigned part[8][128];
     let_next_kernel_start();
@@ -359,7 +376,7 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ 
         for (int e = 0; e < N; ++e) {
             sum[e] += v[e];
             if (sizeof(T) == 4) top[e] = max(top[e], magnitude(v[e]));
-            v[e] *= g.store;
+            if (std::is_same<T, __half>::value) v[e] *= g.store;
         }
         if (!dz) return;
         if constexpr (N > 1) store_pack(dz + r * g.lddz + col, v);          // (rows of dz are padded to whole packs)
@@ -367,7 +384,7 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ 
     };
     if (N > 1 && col + N <= g.n) {
         if constexpr (N > 1) {
-            constexpr int U = 4;                              // rows under way: enough bytes in flight to cover the memory's latency
+            constexpr int U = 2;                              // rows under way: enough bytes in flight to cover the memory's latency
             for (long long r = r0 + y; r < r1; r += 8 * U) {
                 uint4 a[U], b[U];
 #pragma unroll
@@ -427,22 +444,39 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ 
         else g.part[(size_t)by * g.n + c] = s;
     }
 }
-// dbias from the chunks' sums: 32 columns a block, its eight warps take every eighth chunk.
+// dbias from the chunks' sums, 32 columns a block, its eight warps take every eighth chunk; behind those blocks the column tops of the jobs,
+// over their chunks likewise (into the first chunk's place).
 template <typename T>
-__global__ void __launch_bounds__(256) linear_dbias_kernel(const float* __restrict__ part, int chunks, int n, T* __restrict__ dbias) {
-    __shared__ float sums[8][33];
+__global__ void __launch_bounds__(256) linear_chunks_kernel(const float* __restrict__ part, int chunks, int n, T* __restrict__ dbias, unsigned blocks, const __grid_constant__ SplitJobs jobs) {
+    __shared__ unsigned words[8][33];
     let_next_kernel_start();
     wait_for_previous_kernel();
-    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    float s = 0.0f;
-    if (c < n)
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5;
+    if (blockIdx.x < blocks) {
+        const int c = blockIdx.x * 32 + lane;
+        float s = 0.0f;
+        if (c < n)
 #pragma unroll 8
-        for (int i = y; i < chunks; i += 8) s += part[(size_t)i * n + c];
-    sums[y][lane] = s;
-    __syncthreads();
-    if (y == 0 && c < n) {
-        for (int q = 1; q < 8; ++q) s += sums[q][lane];
-        dbias[c] = from_f32<T>(s);
+            for (int i = y; i < chunks; i += 8) s += part[(size_t)i * n + c];
+        words[y][lane] = __float_as_uint(s);
+        __syncthreads();
+        if (y == 0 && c < n) {
+            for (int q = 1; q < 8; ++q) s += __uint_as_float(words[q][lane]);
+            dbias[c] = from_f32<T>(s);
+        }
+        return;
+    }
+    const SplitJob& j = jobs.job[job_of(jobs, blockIdx.x)];
+    const int c = (int)(blockIdx.x - j.first) * 32 + lane;
+    unsigned t = 0u;
+    if (c < j.cols)
+#pragma unroll 8
+        for (int i = y; i < j.chunks; i += 8) t = max(t, j.tops[(size_t)i * j.cols + c]);
+    words[y][lane] = t;
+    __syncthreads();                                          // (every chunk of these columns is read)
+    if (y == 0 && c < j.cols) {
+        for (int q = 1; q < 8; ++q) t = max(t, words[q][lane]);
+        j.tops[c] = t;
     }
 }
 template <typename T>
@@ -461,8 +495,17 @@ static int launch_dz(DzArgs& g, SplitJobs& jobs, cudaStream_t st) {
     }
     int rc = EBS_OK;
     if (blocks) rc = launch_chained(packs ? linear_dz_kernel<T, N> : linear_dz_kernel<T, 1>, dim3(blocks), 256, 0, st, 1, g, tops);
-    if (!rc && g.dbias && g.chunks > 1)
-        rc = launch_chained(linear_dbias_kernel<T>, dim3((g.n + 31) / 32), 256, 0, st, 1, (const float*)g.part, g.chunks, g.n, static_cast<T*>(g.dbias));
+    if (rc) return rc;
+    const unsigned sums = g.dbias && g.chunks > 1 ? (unsigned)((g.n + 31) / 32) : 0u;
+    SplitJobs chunked = {};
+    blocks = sums;
+    for (int i = 0; i < jobs.count; ++i) {
+        if (!jobs.job[i].across || jobs.job[i].chunks < 2) continue;
+        chunked.job[chunked.count] = jobs.job[i];
+        chunked.job[chunked.count++].first = blocks;
+        blocks += (unsigned)((jobs.job[i].cols + 31) / 32);
+    }
+    if (blocks) rc = launch_chained(linear_chunks_kernel<T>, dim3(blocks), 256, 0, st, 1, (const float*)g.part, g.chunks, g.n, static_cast<T*>(g.dbias), sums, chunked);
     return rc;
 }
 
@@ -474,6 +517,10 @@ struct LinearTensors {
 // Runs the call, or (run = false) counts its workspace.
 static int forward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws, bool run, cudaStream_t st) {
     if (d.m == 0) return EBS_OK;
+    GemmOut o;
+    o.bias = t.bias; o.residual = t.residual; o.z = t.keep; o.y = t.y; o.act = d.act;
+    o.ldr = d.ldr; o.ldz = d.ldz; o.ldy = d.ldy;
+    if (d.m <= GEMM_ROWS) return run ? launch_gemm_rows(t.x, d.ldx, t.w, d.ldw, d.m, d.n, d.k, o, d.dtype, st) : EBS_OK;
     const Matrix xm{t.x, d.m, d.ldx, d.k}, wm{t.w, d.n, d.ldw, d.k};
     SplitJobs jobs = {};
     const Prepared x = plan_operand(xm, d.dtype, false, ws, &jobs), w = plan_operand(wm, d.dtype, false, ws, &jobs);
@@ -482,9 +529,6 @@ static int forward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws,
     if (!run) return EBS_OK;
     int rc;
     if ((rc = launch_splits(jobs, st)) || (rc = copy_operand(xm, x, st)) || (rc = copy_operand(wm, w, st))) return rc;
-    GemmOut o;
-    o.bias = t.bias; o.residual = t.residual; o.z = t.keep; o.y = t.y; o.act = d.act;
-    o.ldr = d.ldr; o.ldz = d.ldz; o.ldy = d.ldy;
     return product(x, xm, w, wm, d.k, o, d.dtype, scratch, st);
 }
 static int backward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws, bool run, cudaStream_t st) {
