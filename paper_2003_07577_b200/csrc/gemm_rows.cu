@@ -11,7 +11,7 @@ constexpr int ROWS_WARPS = 4;
 
 template <typename T, int M, int R, bool VEC>
 __global__ void __launch_bounds__(ROWS_WARPS * 32) gemm_rows_kernel(const T* __restrict__ x, long long ldx, const T* __restrict__ w, long long ldw, int m, int n, int k, const GemmOut o) {
-    constexpr int N = VEC ? Pack<T>::N : 1, U = 8 / R;            // U packs of R rows at a time: eight loads, twice
+    constexpr int N = VEC ? Pack<T>::N : 1, U = M <= 2 ? 8 / R : 4 / R;    // U packs of R rows at a time, twice
     let_next_kernel_start();
     wait_for_previous_kernel();
     const int lane = threadIdx.x & 31, row0 = (int)(blockIdx.x * ROWS_WARPS + (threadIdx.x >> 5)) * R;
@@ -24,6 +24,9 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32) gemm_rows_kernel(const T* __r
     const T* rows[R];                                             // (rows past the end: the last one once more)
 #pragma unroll
     for (int r = 0; r < R; ++r) rows[r] = w + (long long)(row0 + r < n ? row0 + r : n - 1) * ldw;
+    const T* xr[M];                                               // (rows of x past the last likewise)
+#pragma unroll
+    for (int i = 0; i < M; ++i) xr[i] = x + (long long)(i < m ? i : m - 1) * ldx;
     const int packs = k / N;
     auto load = [&](int p0, uint4 (&raw)[U][R]) {
 #pragma unroll
@@ -38,11 +41,21 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32) gemm_rows_kernel(const T* __r
             }
         }
     };
+    // every load of x before the first multiplication: one wait, not one a row
     auto multiply = [&](int p0, const uint4 (&raw)[U][R]) {
+        uint4 xs[U][M];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int p = p0 + u * 32;
-            if (p >= packs) break;
+            const int p = p0 + u * 32 < packs ? p0 + u * 32 : 0;
+#pragma unroll
+            for (int i = 0; i < M; ++i) {
+                if constexpr (VEC) xs[u][i] = *reinterpret_cast<const uint4*>(xr[i] + (size_t)p * N);
+                else xs[u][i].x = __float_as_uint(to_f32(xr[i][p]));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p0 + u * 32 >= packs) break;                      // (zero weights would turn an infinite x into NaN)
             float wv[R][N];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -51,10 +64,9 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32) gemm_rows_kernel(const T* __r
             }
 #pragma unroll
             for (int i = 0; i < M; ++i) {
-                if (i >= m) break;
                 float xv[N];
-                if constexpr (VEC) load_pack(x + i * ldx + (size_t)p * N, xv);
-                else xv[0] = to_f32(x[i * ldx + p]);
+                if constexpr (VEC) unpack<T>(xs[u][i], xv);
+                else xv[0] = __uint_as_float(xs[u][i].x);
 #pragma unroll
                 for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -74,8 +86,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32) gemm_rows_kernel(const T* __r
         const int c = packs * N + lane;
 #pragma unroll
         for (int i = 0; i < M; ++i) {
-            if (i >= m) break;
-            const float xv = to_f32(x[i * ldx + c]);
+            const float xv = to_f32(xr[i][c]);
 #pragma unroll
             for (int r = 0; r < R; ++r) acc[i][r] = fmaf(to_f32(rows[r][c]), xv, acc[i][r]);
         }
@@ -116,6 +127,7 @@ static int launch_rows(const void* x, long long ldx, const void* w, long long ld
 template <typename T>
 static int launch_rows_typed(const void* x, long long ldx, const void* w, long long ldw, int m, int n, int k, const GemmOut& o, cudaStream_t st) {
     if (m == 1) return launch_rows<T, 1>(x, ldx, w, ldw, m, n, k, o, st);
+    if (m == 2) return launch_rows<T, 2>(x, ldx, w, ldw, m, n, k, o, st);
     if (m <= 4) return launch_rows<T, 4>(x, ldx, w, ldw, m, n, k, o, st);
     return launch_rows<T, 8>(x, ldx, w, ldw, m, n, k, o, st);
 }

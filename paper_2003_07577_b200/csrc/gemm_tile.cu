@@ -32,6 +32,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     constexpr int COLS = PL * TN < 32 ? 32 : PL * TN;            // TMEM columns: one accumulator, or two taken in turn
     uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp >= 8 && lane == 0) asm volatile("prefetch.tensormap [%0];\n" ::"l"(warp == 8 ? &map_a : &map_b) : "memory");
     const int split = g.split, part = (int)(blockIdx.x % split);
     const int a0 = (int)(blockIdx.x / split) * 128, b0 = (int)blockIdx.y * TN, batch = (int)blockIdx.z;
     const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK;
@@ -57,6 +58,25 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     wait_for_previous_kernel();
 
     float acc[PL == 2 ? TN / 2 : 1];                              // (split products: this thread's sums)
+    // How the results are shared out at the end: warps 0-7, a thread keeps its pack of columns and takes rows STRIDE apart, what the next one
+    // needs from memory on its way.  One small loop: unrolled over eight rows the code of a tile's end, run once, took 2.5 us to arrive from
+    // the second-level cache (128 x 128 results; 9 us from memory).
+    constexpr int INNER = SWAP ? 128 : TN, OUTER = SWAP ? TN : 128, PITCH = INNER + 4;
+    constexpr int N = EPI::N, PER_ROW = INNER / N, STRIDE = 256 / PER_ROW;
+    static_assert(PER_ROW <= 64, "packs of a row");
+    const int outer0 = SWAP ? b0 : a0, inner0 = SWAP ? a0 : b0;
+    const int o_begin = OUTER * part / split, o_last = g.out_rows - outer0;
+    int o_end = OUTER * (part + 1) / split;
+    if (o_end > o_last) o_end = o_last;
+    const int pack = (threadIdx.x % PER_ROW) * N, ocol = inner0 + pack, left = g.out_cols - ocol, first = o_begin + (int)threadIdx.x / PER_ROW;
+    const bool vec = g.packs && left >= N, writes = warp < 8 && left > 0;
+    typename EPI::Columns columns;
+    typename EPI::Ahead next;
+    if (writes) {
+        epi.columns(ocol, left, vec, columns);
+        if (first < o_end) epi.ahead(batch, outer0 + first, ocol, left, vec, next);
+        epi.touch();
+    }
     if (warp == 8) {
         const bool leader = elect_one();
         for (int i = 0; i < nkb; ++i) {
@@ -115,12 +135,13 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
                 ok = mbar_wait_bounded(&acc_full[c & 1], (c >> 1) & 1, &abort_flag, g.wait_limit);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+                constexpr int W = TN / 2 < 32 ? TN / 2 : 32;
 #pragma unroll
-                for (int j = 0; j < TN / 2; j += 8) {
-                    uint32_t v[8];
-                    tmem_ld8(row + (c & 1) * TN + j, v);
+                for (int j = 0; j < TN / 2; j += W) {
+                    uint32_t v[W];
+                    tmem_load<W>(row + (c & 1) * TN + j, v);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) acc[j + e] += __uint_as_float(v[e]);
+                    for (int e = 0; e < W; ++e) acc[j + e] += __uint_as_float(v[e]);
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
                 if (lane == 0) mbar_arrive(&acc_empty[c & 1]);
@@ -134,10 +155,11 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     // exchange[outer][inner]: inner runs along a row of the results
     float* exchange = reinterpret_cast<float*>(tiles);
-    constexpr int INNER = SWAP ? 128 : TN, OUTER = SWAP ? TN : 128, PITCH = INNER + 4;
     if (warp < 8 && !abort_flag) {
         const uint32_t row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * (TN / 2);
         const int l = (warp & 3) * 32 + lane, n0 = (warp >> 2) * (TN / 2);
+        uint32_t raw[PL == 2 ? 1 : TN / 2];
+        if constexpr (PL == 1) tmem_load<TN / 2>(row, raw);
 #pragma unroll
         for (int j = 0; j < TN / 2; j += 8) {
             float f[8];
@@ -145,10 +167,8 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] = acc[j + e];
             } else {
-                uint32_t v[8];
-                tmem_ld8(row + j, v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = nkb > 0 ? __uint_as_float(v[e]) : 0.0f;
+                for (int e = 0; e < 8; ++e) f[e] = nkb > 0 ? __uint_as_float(raw[j + e]) : 0.0f;
             }
             if (SWAP) {
 #pragma unroll
@@ -168,57 +188,36 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
         asm volatile("ld.shared::cluster.s32 %0, [%1];\n" : "=r"(f) : "r"(cluster_addr((const void*)&abort_flag, q)));
         skip |= f != 0;
     }
-    if (!skip) {
-        const int outer0 = SWAP ? b0 : a0, inner0 = SWAP ? a0 : b0;
-        const int o_begin = OUTER * part / split, o_end = OUTER * (part + 1) / split;
-        constexpr int N = EPI::N, PER_ROW = INNER / N, STEP = 4;
-        // a thread keeps its pack of columns; 320 threads: rows STRIDE apart
-        constexpr int STRIDE = 320 / PER_ROW;
-        static_assert(PER_ROW <= 64 && STRIDE >= 1, "packs of a row");
-        const int n = (threadIdx.x % PER_ROW) * N, ocol = inner0 + n;
-        const int left = g.out_cols - ocol;
-        const bool vec = g.packs && left >= N;
-        typename EPI::Columns columns;
-        if (left > 0) epi.columns(ocol, left, vec, columns);
-        if (left > 0 && (int)threadIdx.x < STRIDE * PER_ROW)
-            for (int first = o_begin + threadIdx.x / PER_ROW; first < o_end; first += STEP * STRIDE) {
-                typename EPI::Ahead ahead[STEP];
-                float v[STEP][N];
+    if (!skip && writes) {
+#pragma unroll 1
+        for (int o = first; o < o_end; o += STRIDE) {
+            const typename EPI::Ahead here = next;
+            if (o + STRIDE < o_end) epi.ahead(batch, outer0 + o + STRIDE, ocol, left, vec, next);
+            float v[N];
+            const float* at = exchange + o * PITCH + pack;
+            if (split == 1) {
 #pragma unroll
-                for (int i = 0; i < STEP; ++i) {
-                    const int o = first + i * STRIDE, orow = outer0 + o;
-                    if (o < o_end && orow < g.out_rows) epi.ahead(batch, orow, ocol, left, vec, ahead[i]);
-                }
+                for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(&v[e]) = *reinterpret_cast<const float4*>(at + e);
+            } else {
+                float4 t[8][N / 4];                               // all parts on their way at once, added in their order
 #pragma unroll
-                for (int i = 0; i < STEP; ++i) {
-                    const int o = first + i * STRIDE;
-                    if (o >= o_end) continue;
-                    const float* at = exchange + o * PITCH + n;
-                    if (split == 1) {
+                for (int q = 0; q < 8; ++q)
 #pragma unroll
-                        for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(&v[i][e]) = *reinterpret_cast<const float4*>(at + e);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < N; ++e) v[i][e] = 0.0f;
-#pragma unroll 4
-                        for (int q = 0; q < split; ++q) {
-                            const uint32_t addr = cluster_addr(at, q);
-#pragma unroll
-                            for (int e = 0; e < N; e += 4) {
-                                float4 t;
-                                asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];\n" : "=f"(t.x), "=f"(t.y), "=f"(t.z), "=f"(t.w) : "r"(addr + 4 * e));
-                                v[i][e] += t.x; v[i][e + 1] += t.y; v[i][e + 2] += t.z; v[i][e + 3] += t.w;
-                            }
-                        }
+                    for (int e = 0; e < N / 4; ++e) {
+                        t[q][e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        if (q < split)
+                            asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];\n" : "=f"(t[q][e].x), "=f"(t[q][e].y), "=f"(t[q][e].z), "=f"(t[q][e].w) : "r"(cluster_addr(at, q) + 16 * e));
                     }
-                }
 #pragma unroll
-                for (int i = 0; i < STEP; ++i) {
-                    const int o = first + i * STRIDE, orow = outer0 + o;
-                    if (o >= o_end || orow >= g.out_rows) continue;
-                    epi.pack(batch, orow, ocol, left, vec, v[i], columns, ahead[i]);
+                for (int e = 0; e < N / 4; ++e) {
+                    float4 s = t[0][e];
+#pragma unroll
+                    for (int q = 1; q < 8; ++q) { s.x += t[q][e].x; s.y += t[q][e].y; s.z += t[q][e].z; s.w += t[q][e].w; }
+                    v[4 * e] = s.x; v[4 * e + 1] = s.y; v[4 * e + 2] = s.z; v[4 * e + 3] = s.w;
                 }
             }
+            epi.pack(batch, outer0 + o, ocol, left, vec, v, columns, here);
+        }
     }
     if (split > 1) cluster_sync_all();                            // no block leaves while another reads its sums
     if (gave_up) {

@@ -51,12 +51,43 @@ __device__ __forceinline__ uint32_t tile_desc_lo(uint32_t smem_addr, bool mn_maj
 }
 constexpr uint32_t TILE_DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);           // 8-row groups, descriptor version, 128-byte swizzle
 
-// 8 columns of this warp's 32 lanes.
+// Columns of this warp's 32 lanes out of tensor memory.
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
                  : "r"(taddr));
     asm volatile("tcgen05.wait::ld.sync.aligned;\n" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]) :: "memory");
+}
+__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+          "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
+          "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld32_wait(uint32_t (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;\n"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]),
+                   "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]),
+                   "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+                 :: "memory");
+}
+template <int W>
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&v)[W]) {
+    if constexpr (W == 8) tmem_ld8(taddr, v);
+    else if constexpr (W == 16) tmem_ld16(taddr, v);
+    else if constexpr (W == 32) { tmem_ld32_issue(taddr, v); tmem_ld32_wait(v); }
+    else {
+        uint32_t a[32], b[32];
+        tmem_ld32_issue(taddr, a);
+        tmem_ld32_issue(taddr + 32, b);
+        tmem_ld32_wait(a);
+        tmem_ld32_wait(b);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) { v[i] = a[i]; v[32 + i] = b[i]; }
+    }
 }
 
 // Instruction descriptor: fp32 sums, both operands fp16 (0) or bf16 (1).
@@ -91,7 +122,7 @@ struct GemmShape {
 int gemm_sm_count();
 
 // What becomes of the sums, N neighbouring columns of a row at a time (`left` of them exist; vec: all do, at addresses of whole 16 bytes):
-// `columns` and `ahead` load what is needed, `pack` finishes and stores.
+// `columns` and `ahead` load what is needed, `touch` reads the parameters that `pack` will use, which finishes and stores.
 
 // The results of a linear layer or of its gradients.
 template <typename T>
@@ -100,6 +131,7 @@ struct LinearOut {
     using Columns = GemmColumns<T>;
     using Ahead = GemmAhead;
     GemmOut o;
+    __device__ __forceinline__ void touch() const { asm volatile("" ::"l"(o.y), "l"(o.z), "l"(o.ldz), "l"(o.ldy), "f"(o.alpha), "r"(o.act)); }
     __device__ __forceinline__ void columns(int col, int left, bool vec, Columns& c) const { gemm_columns<T>(o, col, left, vec, c); }
     __device__ __forceinline__ void ahead(int, long long row, int col, int left, bool vec, Ahead& a) const { gemm_ahead<T>(o, row, col, left, vec, a); }
     __device__ __forceinline__ void pack(int, long long row, int col, int left, bool vec, float (&v)[N], const Columns& c, const Ahead& a) const {
@@ -118,6 +150,7 @@ struct PlanesOut {
     __half* y2;
     long long ld, plane, batch;            // of either: elements between rows, planes, matrices of a batch
     float alpha, diag, alpha2, diag2;
+    __device__ __forceinline__ void touch() const { asm volatile("" ::"l"(y), "l"(y2), "l"(plane), "f"(alpha), "f"(diag2)); }
     __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
     __device__ __forceinline__ void ahead(int, long long, int, int, bool, Ahead&) const {}
     static __device__ __forceinline__ void halves(float v, __half& hi, __half& lo) {
@@ -150,6 +183,7 @@ struct TypedFinal {
     struct Columns {};
     struct Ahead {};
     FinalOut o;
+    __device__ __forceinline__ void touch() const { asm volatile("" ::"l"(o.y), "l"(o.batch), "f"(o.alpha)); }
     __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
     __device__ __forceinline__ void ahead(int, long long, int, int, bool, Ahead&) const {}
     __device__ __forceinline__ void pack(int b, long long row, int col, int left, bool vec, float (&v)[N], const Columns&, const Ahead&) const {

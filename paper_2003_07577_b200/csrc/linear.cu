@@ -520,7 +520,7 @@ static int forward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws,
     GemmOut o;
     o.bias = t.bias; o.residual = t.residual; o.z = t.keep; o.y = t.y; o.act = d.act;
     o.ldr = d.ldr; o.ldz = d.ldz; o.ldy = d.ldy;
-    if (d.m <= GEMM_ROWS) return run ? launch_gemm_rows(t.x, d.ldx, t.w, d.ldw, d.m, d.n, d.k, o, d.dtype, st) : EBS_OK;
+    if (d.m <= (d.dtype == EBS_F32 ? 4 : 1)) return run ? launch_gemm_rows(t.x, d.ldx, t.w, d.ldw, d.m, d.n, d.k, o, d.dtype, st) : EBS_OK;
     const Matrix xm{t.x, d.m, d.ldx, d.k}, wm{t.w, d.n, d.ldw, d.k};
     SplitJobs jobs = {};
     const Prepared x = plan_operand(xm, d.dtype, false, ws, &jobs), w = plan_operand(wm, d.dtype, false, ws, &jobs);
