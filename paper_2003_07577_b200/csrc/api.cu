@@ -6,6 +6,7 @@
 namespace ebs {
 unsigned long long gemm_tile_timeouts();   // gemm_tile.cu
 unsigned long long gemm_pair_timeouts();   // gemm_pair.cu
+unsigned long long ortho_small_timeouts(); // orthogonalize_small.cu
 }
 
 namespace ebs {
@@ -51,7 +52,7 @@ const ConvVariant* conv_mma_variant(int w_bits, int a_bits, int variant) {
 unsigned long long conv_umma_timeouts() {
     return conv_umma_tile_timeouts() +
            conv_umma_strip_timeouts() + conv_umma_resident_timeouts() + conv_umma_pipe_timeouts() + fused_net_timeouts() +
-           gemm_tile_timeouts() + gemm_pair_timeouts();
+           gemm_tile_timeouts() + gemm_pair_timeouts() + ortho_small_timeouts();
 }
 
 // Polls a bounded device-side wait makes before it gives up (about 40 ns each), and test flags; process-wide,

@@ -17,6 +17,25 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// Two values as fp16 pairs hi + lo, both rounded to nearest: 22 bits (one conversion instruction a pair).
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t& hi, uint32_t& lo) {
+    const __half2 h = __floats2half2_rn(a, b);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = *reinterpret_cast<const uint32_t*>(&l);
+}
+// Two values in one 32-bit word of 16-bit elements.
+template <typename T> __device__ __forceinline__ uint32_t pair_word(float a, float b);
+template <> __device__ __forceinline__ uint32_t pair_word<__half>(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pair_word<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
 inline size_t element_size(int dtype) { return dtype == EBS_F32 ? 4 : 2; }
 inline bool real_dtype(int dtype) { return dtype == EBS_F32 || dtype == EBS_F16 || dtype == EBS_BF16; }
 
@@ -166,9 +185,9 @@ __device__ __forceinline__ void load_pack(const T* p, float (&v)[16 / sizeof(T)]
 template <typename T>
 __device__ __forceinline__ void store_pack(T* p, const float (&v)[16 / sizeof(T)], int left = Pack<T>::N, bool vec = true) {
     uint4 u;
-    T* e = reinterpret_cast<T*>(&u);
-#pragma unroll
-    for (int i = 0; i < Pack<T>::N; ++i) e[i] = from_f32<T>(v[i]);
+    if constexpr (sizeof(T) == 2) u = make_uint4(pair_word<T>(v[0], v[1]), pair_word<T>(v[2], v[3]), pair_word<T>(v[4], v[5]), pair_word<T>(v[6], v[7]));
+    else u = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    const T* e = reinterpret_cast<const T*>(&u);
     if (vec) *reinterpret_cast<uint4*>(p) = u;
     else
 #pragma unroll

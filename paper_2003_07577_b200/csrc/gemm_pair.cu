@@ -173,26 +173,30 @@ struct RowOut<PlanesOut> {
         const int lane = ring.lane, diagonal = row0 + lane - col;             // the column of this row that lies on the diagonal
         __half* image = to + batch * e.batch + (long long)col * e.ld + row0 + lane;
         uint8_t* buffer = ring.next();
-        __align__(16) __half lo[CW];
+        uint32_t lo[CW / 2];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            __align__(16) __half hi[8];
+            uint32_t hi[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) PlanesOut::halves(v[c * 8 + i] * factor + (c * 8 + i == diagonal ? on_diag : 0.0f), hi[i], lo[c * 8 + i]);
-            *row_chunk(buffer, lane, c) = *reinterpret_cast<const uint4*>(hi);
+            for (int i = 0; i < 4; ++i) {
+                const int at = c * 8 + 2 * i;
+                split_pair(v[at] * factor + (at == diagonal ? on_diag : 0.0f), v[at + 1] * factor + (at + 1 == diagonal ? on_diag : 0.0f), hi[i], lo[c * 4 + i]);
+            }
+            *row_chunk(buffer, lane, c) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
             if (mirror && row0 + lane < rows) {                   // the image across the diagonal: 32 lanes write 64 bytes of a row
+                const __half *h = reinterpret_cast<const __half*>(hi), *l = reinterpret_cast<const __half*>(lo + c * 4);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (c * 8 + i < left) {
-                        image[(c * 8 + i) * e.ld] = hi[i];
-                        image[(c * 8 + i) * e.ld + e.plane] = lo[c * 8 + i];
+                        image[(c * 8 + i) * e.ld] = h[i];
+                        image[(c * 8 + i) * e.ld + e.plane] = l[i];
                     }
             }
         }
         ring.store(y, buffer, col, row0, 2 * batch, exists);
         buffer = ring.next();
 #pragma unroll
-        for (int c = 0; c < 4; ++c) *row_chunk(buffer, lane, c) = *reinterpret_cast<const uint4*>(lo + 8 * c);
+        for (int c = 0; c < 4; ++c) *row_chunk(buffer, lane, c) = make_uint4(lo[4 * c], lo[4 * c + 1], lo[4 * c + 2], lo[4 * c + 3]);
         ring.store(y, buffer, col, row0, 2 * batch + 1, exists);
     }
     template <int R>

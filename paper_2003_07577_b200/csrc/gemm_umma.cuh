@@ -52,11 +52,17 @@ __device__ __forceinline__ uint32_t tile_desc_lo(uint32_t smem_addr, bool mn_maj
 constexpr uint32_t TILE_DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);           // 8-row groups, descriptor version, 128-byte swizzle
 
 // Columns of this warp's 32 lanes out of tensor memory.
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+__device__ __forceinline__ void tmem_ld8_issue(uint32_t taddr, uint32_t (&v)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
                  : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld8_wait(uint32_t (&v)[8]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;\n" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]) :: "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+    tmem_ld8_issue(taddr, v);
+    tmem_ld8_wait(v);
 }
 __device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&v)[32]) {
     asm volatile(
@@ -153,16 +159,15 @@ struct PlanesOut {
     __device__ __forceinline__ void touch() const { asm volatile("" ::"l"(y), "l"(y2), "l"(plane), "f"(alpha), "f"(diag2)); }
     __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
     __device__ __forceinline__ void ahead(int, long long, int, int, bool, Ahead&) const {}
-    static __device__ __forceinline__ void halves(float v, __half& hi, __half& lo) {
-        hi = __float2half_rn(v);
-        lo = __float2half_rn(v - __half2float(hi));
-    }
     __device__ __forceinline__ void store(__half* q, long long row, int col, const float (&v)[N], float factor, float on_diag) const {
-        __align__(8) __half hi[4], lo[4];
+        float t[4];
+        uint2 hi, lo;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) halves(v[i] * factor + (row == col + i ? on_diag : 0.0f), hi[i], lo[i]);
-        *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(hi);
-        *reinterpret_cast<uint2*>(q + plane) = *reinterpret_cast<const uint2*>(lo);
+        for (int i = 0; i < 4; ++i) t[i] = v[i] * factor + (row == col + i ? on_diag : 0.0f);
+        split_pair(t[0], t[1], hi.x, lo.x);
+        split_pair(t[2], t[3], hi.y, lo.y);
+        *reinterpret_cast<uint2*>(q) = hi;
+        *reinterpret_cast<uint2*>(q + plane) = lo;
     }
     __device__ __forceinline__ void pack(int b, long long row, int col, int, bool, float (&v)[N], const Columns&, const Ahead&) const {
         const long long at = b * batch + row * ld + col;

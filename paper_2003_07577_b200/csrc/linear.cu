@@ -89,11 +89,7 @@ __device__ __forceinline__ int split_record(unsigned top_bits) {
 }
 // x = (hi + lo) 2^-e: both halves rounded to nearest, 22 bits where hi is a normal number and lo has its 11 bits (values within 2^-17
 // of the largest of the row), an absolute error of 2^-40 of the largest below.  Non-finite values are 0: their rows are flagged.
-__device__ __forceinline__ void split_value(float x, int e, __half& hi, __half& lo) {
-    const float v = (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? 0.0f : scale_pow2(x, e);
-    hi = __float2half_rn(v);
-    lo = __float2half_rn(v - __half2float(hi));
-}
+__device__ __forceinline__ float scaled_finite(float x, int e) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? 0.0f : scale_pow2(x, e); }
 // Four neighbouring elements of a row, of which `left` exist: one 16-byte access where the rows allow it.
 __device__ __forceinline__ float4 load4(const float* p, int left, bool vec) {
     if (vec && left >= 4) return *reinterpret_cast<const float4*>(p);
@@ -102,13 +98,11 @@ __device__ __forceinline__ float4 load4(const float* p, int left, bool vec) {
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 // (the planes' rows are padded to whole groups of eight elements: what is written past the end of a row is padding)
 __device__ __forceinline__ void store_split4(__half* hi_plane, __half* lo_plane, const float4& v, const int (&e)[4]) {
-    __half hi[4], lo[4];
-    split_value(v.x, e[0], hi[0], lo[0]);
-    split_value(v.y, e[1], hi[1], lo[1]);
-    split_value(v.z, e[2], hi[2], lo[2]);
-    split_value(v.w, e[3], hi[3], lo[3]);
-    *reinterpret_cast<uint2*>(hi_plane) = *reinterpret_cast<const uint2*>(hi);
-    *reinterpret_cast<uint2*>(lo_plane) = *reinterpret_cast<const uint2*>(lo);
+    uint2 hi, lo;
+    split_pair(scaled_finite(v.x, e[0]), scaled_finite(v.y, e[1]), hi.x, lo.x);
+    split_pair(scaled_finite(v.z, e[2]), scaled_finite(v.w, e[3]), hi.y, lo.y);
+    *reinterpret_cast<uint2*>(hi_plane) = hi;
+    *reinterpret_cast<uint2*>(lo_plane) = lo;
 }
 
 // A matrix to split into planes.  across = 0: its reduction runs along a row, one exponent a row.  across = 1: down the rows, one

@@ -1,7 +1,7 @@
 // Newton-Schulz orthogonalisation of update matrices.  See include/ebs.h.
 #include <math.h>
 
-#include "gemm_tile.cuh"
+#include "orthogonalize.cuh"
 
 namespace ebs {
 
@@ -75,13 +75,9 @@ __global__ void __launch_bounds__(256) normalize_kernel(const T* __restrict__ g,
         const int r = (int)(i / per_row), c = (int)(i - (long long)r * per_row) * N;
         float v[N];
         load_elements(g + (long long)r * cols + c, cols - c, vec, v);
-        __align__(16) __half hi[8], lo[8];
+        __align__(16) uint32_t hi[N / 2], lo[N / 2];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float s = (float)(v[e] * inv);
-            hi[e] = __float2half_rn(s);
-            lo[e] = __float2half_rn(s - __half2float(hi[e]));
-        }
+        for (int e = 0; e < N; e += 2) split_pair((float)(v[e] * inv), (float)(v[e + 1] * inv), hi[e / 2], lo[e / 2]);
         __half* to = x + r * ld + c;                          // (rows of the planes are padded to whole groups of eight)
         if constexpr (N == 8) {
             *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi);
@@ -123,15 +119,21 @@ __global__ void __launch_bounds__(256) scale_out_kernel(const __half* x, long lo
 struct StepBounds {
     double next, linear, square;
 };
-static StepBounds step_bounds(const float* c, double s) {
-    StepBounds b = {0.0, fabs(c[1]), fabs(c[0])};
-    for (int j = 1; j <= 4096; ++j) {
-        const double v = s * j / 4096.0, v2 = v * v, l = fabs(c[1] + v2 * (double)c[2]), q = fabs(c[0] + v2 * (c[1] + v2 * (double)c[2]));
-        b.next = fmax(b.next, v * q);
-        b.linear = fmax(b.linear, l);
-        b.square = fmax(b.square, q);
-    }
-    return b;
+static StepBounds step_bounds(const float* coeff, double s) {
+    const double a = coeff[0], b = coeff[1], c = coeff[2], top = s * s;
+    StepBounds r = {0.0, fmax(fabs(b), fabs(b + c * top)), fmax(fabs(a), fabs(a + top * (b + c * top)))};
+    auto inner = [&](double u) { return u > 0.0 && u < top; };
+    auto step = [&](double u) { r.next = fmax(r.next, sqrt(u) * fabs(a + u * (b + c * u))); };      // u: a singular value squared
+    if (c != 0.0 && inner(-b / (2.0 * c))) r.square = fmax(r.square, fabs(a - b * b / (4.0 * c)));
+    step(top);                                                // the extremes: the end, and where a + 3 b u + 5 c u^2 = 0
+    const double disc = 9.0 * b * b - 20.0 * a * c;
+    if (c != 0.0 && disc >= 0.0)
+        for (int sign = -1; sign <= 1; sign += 2) {
+            const double u = (-3.0 * b + sign * sqrt(disc)) / (10.0 * c);
+            if (inner(u)) step(u);
+        }
+    if (b != 0.0 && inner(-a / (3.0 * b))) step(-a / (3.0 * b));   // (c = 0, or next to it)
+    return r;
 }
 // The exponent e with v * 2^e in [2^13, 2^14): a factor of four below fp16's largest value for what roundings add to the bounds.
 // (At most 2^60: coefficients next to zero.)
@@ -162,11 +164,11 @@ static OrthoBuffers ortho_buffers(int batch, int rows, int cols) {
     const int m = (int)side, n = rows < cols ? cols : rows;
     const GemmShape shapes[] = {{m, m, n, batch, true}, {m, m, m, batch, true}, {rows, cols, m, batch}};
     for (const GemmShape& s : shapes) { const size_t need = round256(gemm_route(s, 2).scratch); b.scratch = need > b.scratch ? need : b.scratch; }
-    b.total = 2 * b.x + 3 * b.a + b.part + b.scratch;
+    b.total = ortho_small_fits(rows, cols) ? 256 : 2 * b.x + 3 * b.a + b.part + b.scratch;      // (small matrices need none: any buffer will do)
     return b;
 }
 static int check_shape(int batch, int rows, int cols, int dtype, int steps) {
-    if (batch < 1 || rows < 1 || cols < 1 || !real_dtype(dtype) || steps < 0 || steps > 64) return EBS_ERR_INVALID_ARG;
+    if (batch < 1 || rows < 1 || cols < 1 || !real_dtype(dtype) || steps < 0 || steps > ORTHO_MAX_STEPS) return EBS_ERR_INVALID_ARG;
     if (batch > 65535 || (long long)rows * cols > (1LL << 36) / batch) return EBS_ERR_OVERFLOW;
     return EBS_OK;
 }
@@ -190,16 +192,24 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     if (((uintptr_t)g & 15) || ((uintptr_t)out & 15) || ((uintptr_t)workspace & 15)) return EBS_ERR_INVALID_ARG;
     for (int i = 0; i < 3; ++i)
         if (!isfinite(coeff[i])) return EBS_ERR_INVALID_ARG;
-    // the singular values' bound before each step
+    // the singular values' bound before each step; from it the exponents of X, A, b I + c A and Q, and the products' factors
+    OrthoFactors f = {};
     double bound = 1.0;
-    int ex[65], el[64], eq[64];                               // exponents of X, b I + c A, Q
-    for (int i = 0; i <= steps; ++i) {
-        if (!(bound < 0x1p20 && bound > 0x1p-20)) return EBS_ERR_UNSUPPORTED;
-        ex[i] = headroom(bound);
-        if (i == steps) break;
+    int ex = headroom(bound);
+    const float first = ldexpf(1.0f, ex);
+    float last = scale / first;
+    for (int i = 0; i < steps; ++i) {
         const StepBounds b = step_bounds(coeff, bound);
-        el[i] = headroom(b.linear);
-        eq[i] = headroom(b.square);
+        if (!(b.next < 0x1p20 && b.next > 0x1p-20)) return EBS_ERR_UNSUPPORTED;
+        const int ea = 2 * ex - 14, el = headroom(b.linear), eq = headroom(b.square), en = headroom(b.next);   // (an entry of A is at most the square of X's bound)
+        f.gram[i] = ldexpf(1.0f, ea - 2 * ex);
+        f.linear[i] = coeff[2] * ldexpf(1.0f, el - 2 * ex);
+        f.linear_diag[i] = coeff[1] * ldexpf(1.0f, el);
+        f.square[i] = ldexpf(1.0f, eq - ea - el);
+        f.square_diag[i] = coeff[0] * ldexpf(1.0f, eq);
+        f.next[i] = ldexpf(1.0f, en - eq - ex);
+        last = scale * ldexpf(1.0f, -eq - ex);
+        ex = en;
         bound = b.next;
     }
     const OrthoBuffers b = ortho_buffers(batch, rows, cols);
@@ -209,13 +219,13 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     if (pg != po && pg < po + bytes && po < pg + bytes) return EBS_ERR_INVALID_ARG;
     if ((pw < pg + bytes && pg < pw + b.total) || (pw < po + bytes && po < pw + b.total)) return EBS_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (ortho_small_fits(rows, cols)) return launch_ortho_small(g, out, batch, rows, cols, dtype, steps, eps, first, last, f, st);
     __half* x = static_cast<__half*>(workspace);
     __half* x2 = reinterpret_cast<__half*>(static_cast<char*>(workspace) + b.x);
     __half* A = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x);
     __half* L = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x + b.a);
     __half* Q = reinterpret_cast<__half*>(static_cast<char*>(workspace) + 2 * b.x + 2 * b.a);
     float* scratch = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * b.x + 3 * b.a + b.part);
-    const float first = ldexpf(1.0f, ex[0]);
     double* part = reinterpret_cast<double*>(static_cast<char*>(workspace) + 2 * b.x + 3 * b.a);
     if (dtype == EBS_F32) rc = launch_normalize<float>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
     else if (dtype == EBS_F16) rc = launch_normalize<__half>(g, batch, rows, cols, eps, first, part, b.parts, x, b.ld, b.plane, st);
@@ -224,24 +234,22 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
     const bool tall = rows > cols;                            // then X X^T X is taken as X (X^T X): the smaller product
     const int m = tall ? cols : rows, n = tall ? rows : cols;
     for (int s = 0; s < steps; ++s) {
-        const int ea = 2 * ex[s] - 14;                          // entries of A are at most the square of X's bound: below 2^14
         const GemmOperand xs{x, b.ld, tall, 2, b.plane, 2 * b.plane}, as{A, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane}, ls{L, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane},
             qs{Q, b.side_ld, false, 2, b.side_plane, 2 * b.side_plane};
-        PlanesOut oa{A, L, b.side_ld, b.side_plane, 2 * b.side_plane, ldexpf(1.0f, ea - 2 * ex[s]), 0.0f, coeff[2] * ldexpf(1.0f, el[s] - 2 * ex[s]), coeff[1] * ldexpf(1.0f, el[s])};
+        PlanesOut oa{A, L, b.side_ld, b.side_plane, 2 * b.side_plane, f.gram[s], 0.0f, f.linear[s], f.linear_diag[s]};
         if ((rc = launch_gemm(xs, xs, GemmShape{m, m, n, batch, true}, scratch, oa, st))) return rc;
-        PlanesOut oq{Q, nullptr, b.side_ld, b.side_plane, 2 * b.side_plane, ldexpf(1.0f, eq[s] - ea - el[s]), coeff[0] * ldexpf(1.0f, eq[s]), 0.0f, 0.0f};
+        PlanesOut oq{Q, nullptr, b.side_ld, b.side_plane, 2 * b.side_plane, f.square[s], f.square_diag[s], 0.0f, 0.0f};
         if ((rc = launch_gemm(as, ls, GemmShape{m, m, m, batch, true}, scratch, oq, st))) return rc;
         // X <- Q X or X Q; the last one is the result
         const GemmOperand xk{x, b.ld, false, 2, b.plane, 2 * b.plane}, xm{x, b.ld, true, 2, b.plane, 2 * b.plane};
         const GemmOperand &left = tall ? xk : qs, &right = tall ? qs : xm;
         const GemmShape shape{rows, cols, m, batch};
-        if (s == steps - 1) return launch_gemm(left, right, shape, scratch, FinalOut{out, cols, (long long)rows * cols, scale * ldexpf(1.0f, -eq[s] - ex[s])}, dtype, st);
-        PlanesOut ox{x2, nullptr, b.ld, b.plane, 2 * b.plane, ldexpf(1.0f, ex[s + 1] - eq[s] - ex[s]), 0.0f, 0.0f, 0.0f};
+        if (s == steps - 1) return launch_gemm(left, right, shape, scratch, FinalOut{out, cols, (long long)rows * cols, last}, dtype, st);
+        PlanesOut ox{x2, nullptr, b.ld, b.plane, 2 * b.plane, f.next[s], 0.0f, 0.0f, 0.0f};
         if ((rc = launch_gemm(left, right, shape, scratch, ox, st))) return rc;
         __half* t = x; x = x2; x2 = t;
     }
     if (steps > 0) return EBS_OK;
-    const float last = scale * ldexpf(1.0f, -ex[0]);
     const dim3 grid(blocks_for((long long)rows * cols * batch, 1));
     if (dtype == EBS_F32) return launch_chained(scale_out_kernel<float>, grid, 256, 0, st, 1, (const __half*)x, b.ld, b.plane, rows, cols, batch, last, static_cast<float*>(out));
     if (dtype == EBS_F16) return launch_chained(scale_out_kernel<__half>, grid, 256, 0, st, 1, (const __half*)x, b.ld, b.plane, rows, cols, batch, last, static_cast<__half*>(out));

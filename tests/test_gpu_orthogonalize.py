@@ -72,7 +72,9 @@ def check(got, ref, steps, coeff=COEFF, scale=1.0):
 
 
 SHAPES = [(1, 1, 1), (3, 1, 7), (2, 5, 1), (1, 2, 2), (6, 64, 576), (2, 576, 64), (3, 16, 144), (32, 16, 16), (1, 63, 65), (2, 129, 130), (1, 128, 128), (1, 257, 100),
-          (1, 512, 4608), (1, 1024, 777), (1, 8, 7057), (1, 3001, 5), (2, 200, 1000)]
+          (1, 512, 4608), (1, 1024, 777), (1, 8, 7057), (1, 3001, 5), (2, 200, 1000),
+          # the largest that stay in one thread block's shared memory, and one column more
+          (2, 64, 640), (1, 640, 64), (1, 64, 641), (2, 33, 768), (1, 33, 769), (1, 16, 2560), (1, 2561, 16), (2, 17, 1000), (200, 20, 30)]
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
