@@ -19,12 +19,20 @@ static __device__ unsigned long long g_gemm_tile_timeouts = 0ull;
 template <int TN, int PL>
 __host__ __device__ constexpr int tile_stage_bytes() { return PL * (128 + TN) * GEMM_ROW_BYTES; }
 
+// One launch: a product, or two that do not depend on each other.
+template <class EPI>
+struct TileLaunch {
+    CUtensorMap a[2], b[2];                                      // A: the operand on the 128 lanes, B: the one on the TN columns
+    TileArgs g[2];
+    EPI epi[2];
+    unsigned second;                                             // first thread block of the second product
+};
+
 template <class EPI, int TN, int PL, bool SWAP>
-__global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                           const TileArgs g, const EPI epi) {
-    // A is the operand on the 128 lanes, B the one on the TN columns; SWAP: lanes are the result's columns
+__global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant__ TileLaunch<EPI> launch) {
+    // SWAP: lanes are the result's columns
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full[8], empty[8], acc_full[2], acc_empty[2];
+    __shared__ uint64_t full[8], empty[8], acc_full[2], acc_empty[2], received;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     constexpr int STAGE = tile_stage_bytes<TN, PL>();
@@ -32,9 +40,20 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     constexpr int COLS = PL * TN < 32 ? 32 : PL * TN;            // TMEM columns: one accumulator, or two taken in turn
     uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (warp >= 8 && lane == 0) asm volatile("prefetch.tensormap [%0];\n" ::"l"(warp == 8 ? &map_a : &map_b) : "memory");
-    const int split = g.split, part = (int)(blockIdx.x % split);
-    const int a0 = (int)(blockIdx.x / split) * 128, b0 = (int)blockIdx.y * TN, batch = (int)blockIdx.z;
+    const int which = blockIdx.x >= launch.second;
+    const TileArgs g = launch.g[which];                           // (copies: an indexed parameter is a load at every use)
+    const EPI epi = launch.epi[which];
+    const CUtensorMap *map_a = &launch.a[which], *map_b = &launch.b[which];
+    if (warp >= 8 && lane == 0) asm volatile("prefetch.tensormap [%0];\n" ::"l"(warp == 8 ? map_a : map_b) : "memory");
+    // parts of a tile follow one another (a cluster), then tiles along the lanes, along the columns, of the batch
+    const int split = g.split;
+    int tile = (int)(blockIdx.x - (which ? launch.second : 0u));
+    if (tile >= g.blocks) return;                                 // (whole clusters of blocks; only where no block waits for another)
+    const int part = tile % split;
+    tile /= split;
+    const int a0 = tile % g.tiles_a * 128;
+    tile /= g.tiles_a;
+    const int b0 = tile % g.tiles_b * TN, batch = tile / g.tiles_b;
     const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK;
     const int kb0 = (int)((long long)blocks * part / split), kb1 = (int)((long long)blocks * (part + 1) / split);
     const int nkb = kb1 - kb0;
@@ -43,6 +62,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     if (threadIdx.x == 0) {
         for (int s = 0; s < g.stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 8); }
+        mbar_init(&received, 1);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
@@ -89,12 +109,12 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
                 for (int p = 0; p < PL; ++p) {
                     const uint32_t at = base + p * A_BYTES, bt = base + PL * A_BYTES + p * B_BYTES;
                     const int z = batch * PL + p;
-                    if (!g.a_mn) tma_load_3d(at, &map_a, k, a0, z, bar);
-                    else { tma_load_3d(at, &map_a, a0, k, z, bar); tma_load_3d(at + 8192, &map_a, a0 + 64, k, z, bar); }
-                    if (!g.b_mn) tma_load_3d(bt, &map_b, k, b0, z, bar);
+                    if (!g.a_mn) tma_load_3d(at, map_a, k, a0, z, bar);
+                    else { tma_load_3d(at, map_a, a0, k, z, bar); tma_load_3d(at + 8192, map_a, a0 + 64, k, z, bar); }
+                    if (!g.b_mn) tma_load_3d(bt, map_b, k, b0, z, bar);
                     else
 #pragma unroll
-                        for (int h = 0; h < (TN + 63) / 64; ++h) tma_load_3d(bt + h * 8192, &map_b, b0 + h * 64, k, z, bar);
+                        for (int h = 0; h < (TN + 63) / 64; ++h) tma_load_3d(bt + h * 8192, map_b, b0 + h * 64, k, z, bar);
                 }
             }
             __syncwarp();
@@ -179,14 +199,30 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
             }
         }
     }
+    // Parts: each block of the cluster sends every other one its share of the tile in one bulk copy and adds what it gets in block order.
+    // (Read out of the other blocks' memory by its own loads, the exchange took 3.6 us for 128 x 128 results in four parts.)
+    constexpr int EXCHANGE = OUTER * PITCH * 4;
+    const int share = EXCHANGE / split;                           // bytes
+    float* shares = reinterpret_cast<float*>(tiles + EXCHANGE);   // [part][OUTER / split][PITCH]
+    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
     if (split > 1) cluster_sync_all();
     else __syncthreads();
-    const bool gave_up = abort_flag != 0;
-    bool skip = gave_up;
-    for (int q = 0; q < split && split > 1; ++q) {                // (a part that gave up leaves no sums)
+    bool skip = abort_flag != 0;
+    for (int q = 0; q < split && split > 1; ++q) {                // (a part that gave up leaves no sums: no block of the cluster goes on)
         int f;
         asm volatile("ld.shared::cluster.s32 %0, [%1];\n" : "=r"(f) : "r"(cluster_addr((const void*)&abort_flag, q)));
         skip |= f != 0;
+    }
+    if (split > 1 && !skip) {
+        if (threadIdx.x == 288) {
+            mbar_expect_tx(&received, (uint32_t)EXCHANGE);
+            if ((g.test_flags & 2) == 0 || part != 0)             // (give-up test: one part's sums never come)
+                for (int q = 0; q < split; ++q)
+                    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(
+                                     cluster_addr(reinterpret_cast<uint8_t*>(shares) + part * share, q)), "r"(smem_u32(exchange) + q * share), "r"(share), "r"(cluster_addr(&received, q))
+                                 : "memory");
+        }
+        if (warp < 8) skip = !mbar_wait_bounded(&received, 0, &abort_flag, g.wait_limit);
     }
     if (!skip && writes) {
 #pragma unroll 1
@@ -194,33 +230,23 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
             const typename EPI::Ahead here = next;
             if (o + STRIDE < o_end) epi.ahead(batch, outer0 + o + STRIDE, ocol, left, vec, next);
             float v[N];
-            const float* at = exchange + o * PITCH + pack;
-            if (split == 1) {
+            const float* at = split == 1 ? exchange + o * PITCH + pack : shares + (o - o_begin) * PITCH + pack;
 #pragma unroll
-                for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(&v[e]) = *reinterpret_cast<const float4*>(at + e);
-            } else {
-                float4 t[8][N / 4];                               // all parts on their way at once, added in their order
+            for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(&v[e]) = *reinterpret_cast<const float4*>(at + e);
+#pragma unroll 1
+            for (int q = 1; q < split; ++q) {
+                at += share / 4;
 #pragma unroll
-                for (int q = 0; q < 8; ++q)
-#pragma unroll
-                    for (int e = 0; e < N / 4; ++e) {
-                        t[q][e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        if (q < split)
-                            asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];\n" : "=f"(t[q][e].x), "=f"(t[q][e].y), "=f"(t[q][e].z), "=f"(t[q][e].w) : "r"(cluster_addr(at, q) + 16 * e));
-                    }
-#pragma unroll
-                for (int e = 0; e < N / 4; ++e) {
-                    float4 s = t[0][e];
-#pragma unroll
-                    for (int q = 1; q < 8; ++q) { s.x += t[q][e].x; s.y += t[q][e].y; s.z += t[q][e].z; s.w += t[q][e].w; }
-                    v[4 * e] = s.x; v[4 * e + 1] = s.y; v[4 * e + 2] = s.z; v[4 * e + 3] = s.w;
+                for (int e = 0; e < N; e += 4) {
+                    const float4 t = *reinterpret_cast<const float4*>(at + e);
+                    v[e] += t.x; v[e + 1] += t.y; v[e + 2] += t.z; v[e + 3] += t.w;
                 }
             }
             epi.pack(batch, outer0 + o, ocol, left, vec, v, columns, here);
         }
     }
-    if (split > 1) cluster_sync_all();                            // no block leaves while another reads its sums
-    if (gave_up) {
+    if (split > 1) cluster_sync_all();                            // no block leaves while its sums are on their way
+    if (abort_flag) {
         giveup_drain();
         if (threadIdx.x == 0) atomicAdd(&g_gemm_tile_timeouts, 1ull);
     }
@@ -234,15 +260,75 @@ unsigned long long gemm_tile_timeouts() {
     return cudaMemcpyFromSymbol(&n, g_gemm_tile_timeouts, sizeof(n)) == cudaSuccess ? n : 0;
 }
 
+// The form of a product: which operand lies on the lanes, how wide a tile is, in how many parts its reduction is taken.
+struct TileForm {
+    bool swap;
+    int tn, split;
+};
+// tiles_beside: tiles of another product in the same launch.
+static TileForm tile_form(const GemmShape& s, bool a_mn, int planes, long long tiles_beside) {
+    TileForm f;
+    f.swap = s.rows <= 64 && !a_mn;
+    f.tn = f.swap ? (s.rows <= 16 ? 16 : s.rows <= 32 ? 32 : 64) : (s.cols <= 64 ? 64 : 128);
+    const int lanes = f.swap ? s.cols : s.rows, columns = f.swap ? s.rows : s.cols, sms = gemm_sm_count();
+    const long long tiles = (long long)((lanes + 127) / 128) * ((columns + f.tn - 1) / f.tn) * s.batch;
+    const int blocks = (s.red + GEMM_BK - 1) / GEMM_BK;
+    // Parts of the reduction (us, measured): a stage takes 0.32 (split products 0.9), two, four or eight parts 1.2, 1.6 and 2.4 to meet; eight
+    // parts of more than half the GPU's tiles no longer run at once.
+    static const float meet[4] = {0.0f, 1.2f, 1.6f, 2.4f};
+    f.split = 1;
+    float best = 0.0f;
+    for (int i = 0; i < 4; ++i) {
+        const int parts = 1 << i;
+        if (i > 0 && (tiles * parts + tiles_beside > (i == 3 ? sms * 3 / 4 : sms) || blocks < parts)) break;
+        const float t = (planes == 2 ? 0.9f : 0.32f) * (float)((blocks + parts - 1) / parts) + meet[i];
+        if (i == 0 || t < best) { best = t; f.split = parts; }
+    }
+    return f;
+}
+
+// Fills in one product of a launch; blocks: its thread blocks.
+template <class EPI>
+static int tile_product(TileLaunch<EPI>* l, int which, const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, bool packs, const TileForm& f,
+                        unsigned* blocks) {
+    TileArgs& g = l->g[which];
+    const int lanes = f.swap ? s.cols : s.rows, columns = f.swap ? s.rows : s.cols;
+    const GemmOperand &la = f.swap ? B : A, &lb = f.swap ? A : B;
+    g = {};
+    g.tiles_a = (lanes + 127) / 128;
+    g.tiles_b = (columns + f.tn - 1) / f.tn;
+    g.split = f.split;
+    g.red = s.red;
+    g.out_rows = s.rows;
+    g.out_cols = s.cols;
+    g.batch = s.batch;
+    g.a_mn = la.mn_major;
+    g.b_mn = lb.mn_major;
+    g.bf16 = bf16;
+    g.packs = packs;
+    g.wait_limit = device_wait_limit();
+    g.test_flags = device_test_flags();
+    l->epi[which] = epi;
+    const long long count = (long long)g.tiles_a * g.tiles_b * s.batch * f.split;
+    if (count >= (1LL << 30)) return EBS_ERR_OVERFLOW;
+    *blocks = (unsigned)count;
+    g.blocks = (int)count;
+    return gemm_operand_map(la, lanes, s.red, s.batch, 128, bf16, &l->a[which]) && gemm_operand_map(lb, columns, s.red, s.batch, f.tn, bf16, &l->b[which]) ? EBS_OK : EBS_ERR_CUDA;
+}
+
 template <class EPI, int TN, int PL, bool SWAP>
-static int launch_tile(const CUtensorMap& a, const CUtensorMap& b, TileArgs g, const EPI& epi, int batch, int lanes, int columns, cudaStream_t st) {
+static int launch_tile(TileLaunch<EPI>& l, unsigned blocks, int cluster, cudaStream_t st) {
     constexpr int STAGE = tile_stage_bytes<TN, PL>();
     constexpr int EXCHANGE = (SWAP ? TN * 132 : 128 * (TN + 4)) * 4;
     const int most = (220 * 1024) / STAGE;
-    g.stages = most < 8 ? most : 8;
-    const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK, mine = (blocks + g.split - 1) / g.split;
-    if (g.stages > mine) g.stages = mine;
-    const int bytes = (g.stages * STAGE > EXCHANGE ? g.stages * STAGE : EXCHANGE) + 1024;
+    int deepest = 1;
+    for (TileArgs& g : l.g) {
+        const int kb = (g.red + GEMM_BK - 1) / GEMM_BK, mine = (kb + g.split - 1) / g.split;
+        g.stages = most < 8 ? most : 8;
+        if (g.stages > mine) g.stages = mine;
+        if (g.stages > deepest) deepest = g.stages;
+    }
+    const int sums = cluster > 1 ? 2 * EXCHANGE : EXCHANGE, bytes = (deepest * STAGE > sums ? deepest * STAGE : sums) + 1024;
     auto kern = gemm_tile_kernel<EPI, TN, PL, SWAP>;
     static bool attr_set[64] = {};
     int dev = 0;
@@ -251,68 +337,77 @@ static int launch_tile(const CUtensorMap& a, const CUtensorMap& b, TileArgs g, c
         if (check_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024))) return EBS_ERR_CUDA;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    const dim3 grid((unsigned)((lanes + 127) / 128 * g.split), (unsigned)((columns + TN - 1) / TN), (unsigned)batch);
-    return launch_chained(kern, grid, 320, (size_t)bytes, st, g.split, a, b, g, epi);
+    return launch_chained(kern, dim3(blocks), 320, (size_t)bytes, st, cluster, l);
 }
-
 template <class EPI, int PL>
-static int launch_tile_form(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, bool packs, cudaStream_t st) {
-    const int sms = gemm_sm_count();
-    TileArgs g = {};
-    const bool swap = s.rows <= 64 && !A.mn_major;
-    const int tn = swap ? (s.rows <= 16 ? 16 : s.rows <= 32 ? 32 : 64) : (s.cols <= 64 ? 64 : 128);
-    const int lanes = swap ? s.cols : s.rows, columns = swap ? s.rows : s.cols;
-    const GemmOperand &la = swap ? B : A, &lb = swap ? A : B;
-    const long long tiles = (long long)((lanes + 127) / 128) * ((columns + tn - 1) / tn) * s.batch;
-    const int blocks = (s.red + GEMM_BK - 1) / GEMM_BK;
-    // Parts of the reduction (us, measured): a stage takes 0.32 (split products 0.9), two, four or eight parts 1.6, 2.2 and 4.0 to meet.
-    // 250 x 336 over 1024 bf16: 11.5, 10.9, 10.1 and 11.4 with 1, 2, 4 and 8 parts; 512 x 512 over 512 fp32: 14.0, 11.7, 9.5 and 18.0
-    // (eight parts of 16 tiles no longer run at once).
-    static const float meet[4] = {0.0f, 1.6f, 2.2f, 4.0f};
-    g.split = 1;
-    float best = 0.0f;
-    for (int i = 0; i < 4; ++i) {
-        const int parts = 1 << i;
-        if (i > 0 && (tiles * parts > (i == 3 ? sms * 3 / 4 : sms) || blocks < parts)) break;
-        const float t = (PL == 2 ? 0.9f : 0.32f) * (float)((blocks + parts - 1) / parts) + meet[i];
-        if (i == 0 || t < best) { best = t; g.split = parts; }
+static int launch_tile_form(TileLaunch<EPI>& l, unsigned blocks, const TileForm& f, cudaStream_t st) {
+    if (f.swap) {
+        if (f.tn == 16) return launch_tile<EPI, 16, PL, true>(l, blocks, f.split, st);
+        if (f.tn == 32) return launch_tile<EPI, 32, PL, true>(l, blocks, f.split, st);
+        return launch_tile<EPI, 64, PL, true>(l, blocks, f.split, st);
     }
-    g.red = s.red;
-    g.out_rows = s.rows;
-    g.out_cols = s.cols;
-    g.a_mn = la.mn_major;
-    g.b_mn = lb.mn_major;
-    g.bf16 = bf16;
-    g.packs = packs;
-    g.wait_limit = device_wait_limit();
-    g.test_flags = device_test_flags();
-    if ((columns + tn - 1) / tn > 65535 || s.batch > 65535) return EBS_ERR_OVERFLOW;
-    CUtensorMap a, b;
-    if (!gemm_operand_map(la, lanes, s.red, s.batch, 128, bf16, &a) || !gemm_operand_map(lb, columns, s.red, s.batch, tn, bf16, &b)) return EBS_ERR_CUDA;
-    if (swap) {
-        if (tn == 16) return launch_tile<EPI, 16, PL, true>(a, b, g, epi, s.batch, lanes, columns, st);
-        if (tn == 32) return launch_tile<EPI, 32, PL, true>(a, b, g, epi, s.batch, lanes, columns, st);
-        return launch_tile<EPI, 64, PL, true>(a, b, g, epi, s.batch, lanes, columns, st);
+    if (f.tn == 64) return launch_tile<EPI, 64, PL, false>(l, blocks, f.split, st);
+    return launch_tile<EPI, 128, PL, false>(l, blocks, f.split, st);
+}
+template <class EPI, int PL>
+static int launch_one(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, bool packs, cudaStream_t st) {
+    TileLaunch<EPI> l;
+    const TileForm f = tile_form(s, A.mn_major, PL, 0);
+    unsigned blocks = 0;
+    const int rc = tile_product(&l, 0, A, B, s, epi, bf16, packs, f, &blocks);
+    if (rc) return rc;
+    l.g[1] = l.g[0];
+    l.second = blocks;
+    return launch_tile_form<EPI, PL>(l, blocks, f, st);
+}
+template <class EPI, int PL>
+static int launch_two(const TileTask (&t)[2], const EPI (&epi)[2], bool bf16, const bool (&packs)[2], cudaStream_t st) {
+    // both in one launch where they have the same form
+    TileForm f[2];
+    for (int i = 0; i < 2; ++i) {
+        const GemmShape& other = t[1 - i].s;
+        f[i] = tile_form(t[i].s, t[i].a.mn_major, PL, (long long)((other.rows + 127) / 128) * ((other.cols + 127) / 128));
     }
-    if (tn == 64) return launch_tile<EPI, 64, PL, false>(a, b, g, epi, s.batch, lanes, columns, st);
-    return launch_tile<EPI, 128, PL, false>(a, b, g, epi, s.batch, lanes, columns, st);
+    if (f[0].swap != f[1].swap || f[0].tn != f[1].tn) {
+        const int rc = launch_one<EPI, PL>(t[0].a, t[0].b, t[0].s, epi[0], bf16, packs[0], st);
+        return rc ? rc : launch_one<EPI, PL>(t[1].a, t[1].b, t[1].s, epi[1], bf16, packs[1], st);
+    }
+    // a launch has one size of cluster: the other product takes as many parts, or one
+    const int cluster = f[0].split > f[1].split ? f[0].split : f[1].split;
+    for (TileForm& g : f) g.split = g.split * 2 >= cluster ? cluster : 1;
+    for (int i = 0; i < 2; ++i)
+        if ((t[i].s.red + GEMM_BK - 1) / GEMM_BK < f[i].split) f[i].split = 1;
+    TileLaunch<EPI> l;
+    unsigned first = 0, second = 0;
+    int rc = tile_product(&l, 0, t[0].a, t[0].b, t[0].s, epi[0], bf16, packs[0], f[0], &first);
+    if (!rc) rc = tile_product(&l, 1, t[1].a, t[1].b, t[1].s, epi[1], bf16, packs[1], f[1], &second);
+    if (rc) return rc;
+    l.second = (first + cluster - 1) / cluster * cluster;
+    TileForm both = f[0];
+    both.split = cluster;
+    return launch_tile_form<EPI, PL>(l, l.second + (second + cluster - 1) / cluster * cluster, both, st);
 }
 
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmOut& out, int dtype, cudaStream_t st) {
     const bool packs = packs_ok(out, element_size(dtype));
-    if (dtype == EBS_F32) return launch_tile_form<LinearOut<float>, 2>(A, B, s, {out}, false, packs, st);
-    if (dtype == EBS_F16) return launch_tile_form<LinearOut<__half>, 1>(A, B, s, {out}, false, packs, st);
-    return launch_tile_form<LinearOut<__nv_bfloat16>, 1>(A, B, s, {out}, true, packs, st);
+    if (dtype == EBS_F32) return launch_one<LinearOut<float>, 2>(A, B, s, {out}, false, packs, st);
+    if (dtype == EBS_F16) return launch_one<LinearOut<__half>, 1>(A, B, s, {out}, false, packs, st);
+    return launch_one<LinearOut<__nv_bfloat16>, 1>(A, B, s, {out}, true, packs, st);
 }
-
+int launch_gemm_tiles(const TileTask (&t)[2], const GemmOut (&out)[2], int dtype, cudaStream_t st) {
+    const bool packs[2] = {packs_ok(out[0], element_size(dtype)), packs_ok(out[1], element_size(dtype))};
+    if (dtype == EBS_F32) return launch_two<LinearOut<float>, 2>(t, {{out[0]}, {out[1]}}, false, packs, st);
+    if (dtype == EBS_F16) return launch_two<LinearOut<__half>, 1>(t, {{out[0]}, {out[1]}}, false, packs, st);
+    return launch_two<LinearOut<__nv_bfloat16>, 1>(t, {{out[0]}, {out[1]}}, true, packs, st);
+}
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st) {
-    return launch_tile_form<PlanesOut, 2>(A, B, s, out, false, out.ld % 4 == 0, st);
+    return launch_one<PlanesOut, 2>(A, B, s, out, false, out.ld % 4 == 0, st);
 }
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const FinalOut& out, int dtype, cudaStream_t st) {
     const bool packs = out.ld * (long long)element_size(dtype) % 16 == 0 && (out.batch * (long long)element_size(dtype)) % 16 == 0;
-    if (dtype == EBS_F32) return launch_tile_form<TypedFinal<float>, 2>(A, B, s, {out}, false, packs, st);
-    if (dtype == EBS_F16) return launch_tile_form<TypedFinal<__half>, 2>(A, B, s, {out}, false, packs, st);
-    return launch_tile_form<TypedFinal<__nv_bfloat16>, 2>(A, B, s, {out}, false, packs, st);
+    if (dtype == EBS_F32) return launch_one<TypedFinal<float>, 2>(A, B, s, {out}, false, packs, st);
+    if (dtype == EBS_F16) return launch_one<TypedFinal<__half>, 2>(A, B, s, {out}, false, packs, st);
+    return launch_one<TypedFinal<__nv_bfloat16>, 2>(A, B, s, {out}, false, packs, st);
 }
 
 bool encode_map(CUtensorMap* map, CUtensorMapDataType type, const void* p, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, bool narrow) {

@@ -9,7 +9,7 @@ constexpr int GEMM_CHUNK = 4;                 // stages (of 64 reduction element
 
 struct TileArgs {
     int red, out_rows, out_cols, batch;
-    int split, stages;
+    int tiles_a, tiles_b, blocks, split, stages;      // tile kernel: tiles along the lanes and the columns, thread blocks
     int a_mn, b_mn, bf16, packs, symmetric;
     unsigned wait_limit;
     int test_flags;
@@ -17,6 +17,12 @@ struct TileArgs {
 
 // D (rows x cols) = sum over red of A (rows x red) and B (cols x red); out is what becomes of it.
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmOut& out, int dtype, cudaStream_t st);
+// Two products that do not depend on each other, in one launch where their tiles have the same form.
+struct TileTask {
+    GemmOperand a, b;
+    GemmShape s;
+};
+int launch_gemm_tiles(const TileTask (&t)[2], const GemmOut (&out)[2], int dtype, cudaStream_t st);
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st);
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const FinalOut& out, int dtype, cudaStream_t st);
 unsigned long long gemm_tile_timeouts();

@@ -71,12 +71,31 @@ struct Carver {
 };
 static long long round8(long long v) { return (v + 7) & ~7LL; }
 
-// A copy of 16-bit rows whose stride is a multiple of 16 bytes.
-__global__ void __launch_bounds__(256) copy_rows_kernel(const uint16_t* __restrict__ src, long long ld, long long rows, int cols, uint16_t* __restrict__ dst, long long ldd) {
+// Copies of 16-bit rows whose stride is a multiple of 16 bytes: up to three matrices in one launch, 256 elements of a row a warp, all on
+// their way at once.
+struct CopyJobs {
+    const uint16_t* src[3];
+    uint16_t* dst[3];
+    long long ld[3], ldd[3], first[3], pieces;                // first: pieces of the matrices before
+    int cols[3], across[3], count;
+};
+__global__ void __launch_bounds__(256) copy_rows_kernel(const __grid_constant__ CopyJobs j) {
     let_next_kernel_start();
     wait_for_previous_kernel();
-    for (long long r = blockIdx.y; r < rows; r += gridDim.y)
-        for (int c = blockIdx.x * 256 + threadIdx.x; c < cols; c += gridDim.x * 256) dst[r * ldd + c] = src[r * ld + c];
+    const int lane = threadIdx.x & 31;
+    for (long long p = blockIdx.x * 8LL + (threadIdx.x >> 5); p < j.pieces; p += gridDim.x * 8LL) {
+        int i = 0;
+        while (i + 1 < j.count && p >= j.first[i + 1]) ++i;
+        const long long q = p - j.first[i], r = q / j.across[i];
+        const int c0 = (int)(q - r * j.across[i]) * 256 + lane;
+        const uint16_t* src = j.src[i] + r * j.ld[i];
+        uint16_t *dst = j.dst[i] + r * j.ldd[i], v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c0 + 32 * e < j.cols[i] ? src[c0 + 32 * e] : (uint16_t)0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c0 + 32 * e < j.cols[i]) dst[c0 + 32 * e] = v[e];
+    }
 }
 
 // The power of two that brings values of magnitude up to the one with these bits below 2^15, and what is remembered of it: its
@@ -106,8 +125,8 @@ __device__ __forceinline__ void store_split4(__half* hi_plane, __half* lo_plane,
 }
 
 // A matrix to split into planes.  across = 0: its reduction runs along a row, one exponent a row.  across = 1: down the rows, one
-// exponent a column; the largest magnitudes of the columns then come from column_tops for each of `chunks` chunks of rows, and over the
-// chunks from linear_chunks_kernel (first row of `tops`).
+// exponent a column; the largest magnitudes of the columns then come from column_tops for each of `chunks` chunks of rows, and where they are
+// many over the chunks from linear_chunks_kernel (first row of `tops`).
 struct SplitJob {
     const float* src;
     long long ld, rows;
@@ -116,10 +135,11 @@ struct SplitJob {
     long long ldd;
     int* exps;
     unsigned* tops;                        // [chunks][cols]
-    int chunks, vec;
+    int chunks, joined, vec;               // joined: chunks that are left when the matrix is split
     unsigned blocks, first;                // thread blocks, and the first of them in the launch
 };
 constexpr int MAX_SPLIT_JOBS = 4;
+constexpr int FEW_CHUNKS = 8;              // so many a split joins by itself: less than a launch costs
 constexpr int SPLIT_WIDE = 1280;           // columns from which on a block shares a row
 struct SplitJobs {
     SplitJob job[MAX_SPLIT_JOBS];
@@ -202,7 +222,10 @@ __device__ __forceinline__ void split_columns(const SplitJob& j, unsigned block)
     int e[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const unsigned t = c + i < j.cols ? j.tops[c + i] : 0u;
+        unsigned t = 0u;
+        if (c + i < j.cols)
+#pragma unroll 4
+            for (int q = 0; q < j.joined; ++q) t = max(t, j.tops[(size_t)q * j.cols + c + i]);
         e[i] = split_exponent(t);
         if (by == 0 && y == 0 && c + i < j.cols) j.exps[c + i] = split_record(t);
     }
@@ -261,10 +284,11 @@ static Prepared plan_operand(const Matrix& m, int dtype, bool across, Carver& ws
         out.op.ld = ldd;
         return out;
     }
-    SplitJob j{static_cast<const float*>(m.p), m.ld, m.rows, m.cols, across, ws.take<__half>(2 * (size_t)m.rows * ldd), ldd, ws.take<int>(across ? m.cols : m.rows), nullptr, 0, (m.ld & 3) == 0, 0, 0};
+    SplitJob j{static_cast<const float*>(m.p), m.ld, m.rows, m.cols, across, ws.take<__half>(2 * (size_t)m.rows * ldd), ldd, ws.take<int>(across ? m.cols : m.rows), nullptr, 0, 0, (m.ld & 3) == 0, 0, 0};
     if (across) {
         const int blocks = (m.cols + 127) / 128;
         j.chunks = row_chunks(m.rows, blocks);
+        j.joined = j.chunks > FEW_CHUNKS ? 1 : j.chunks;
         j.tops = ws.take<unsigned>((size_t)j.chunks * m.cols);
         j.blocks = (unsigned)(blocks * j.chunks);
     } else {
@@ -276,11 +300,21 @@ static Prepared plan_operand(const Matrix& m, int dtype, bool across, Carver& ws
     jobs->job[jobs->count++] = j;
     return out;
 }
-static int copy_operand(const Matrix& m, const Prepared& p, cudaStream_t st) {
-    if (!p.op.p || p.op.planes == 2 || p.op.p == m.p) return EBS_OK;
-    const long long rows = m.rows < 4096 ? m.rows : 4096;
-    return launch_chained(copy_rows_kernel, dim3((m.cols + 255) / 256, (unsigned)rows), 256, 0, st, 1, static_cast<const uint16_t*>(m.p), m.ld, m.rows, m.cols,
-                          static_cast<uint16_t*>(const_cast<void*>(p.op.p)), p.op.ld);
+static void add_copy(CopyJobs* j, const Matrix& m, const Prepared& p) {
+    if (!p.op.p || p.op.planes == 2 || p.op.p == m.p) return;
+    const int i = j->count++;
+    j->src[i] = static_cast<const uint16_t*>(m.p);
+    j->dst[i] = static_cast<uint16_t*>(const_cast<void*>(p.op.p));
+    j->ld[i] = m.ld;
+    j->ldd[i] = p.op.ld;
+    j->cols[i] = m.cols;
+    j->across[i] = (m.cols + 255) / 256;
+    j->first[i] = j->pieces;
+    j->pieces += m.rows * j->across[i];
+}
+static int launch_copies(const CopyJobs& j, cudaStream_t st) {
+    const long long blocks = (j.pieces + 7) / 8;
+    return j.count ? launch_chained(copy_rows_kernel, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), 256, 0, st, 1, j) : EBS_OK;
 }
 static int launch_splits(const SplitJobs& all, cudaStream_t st) {
     long long elements = 0;
@@ -304,21 +338,22 @@ static int launch_splits(const SplitJobs& all, cudaStream_t st) {
     return EBS_OK;
 }
 
-// One product with its operands prepared; a: its rows are the result's (across: its columns), likewise b for the result's columns.
-static int product(const Prepared& a, const Matrix& am, const Prepared& b, const Matrix& bm, int red, GemmOut o, int dtype, float* scratch, cudaStream_t st) {
-    const GemmShape s{(int)(a.op.mn_major ? am.cols : am.rows), (int)(b.op.mn_major ? bm.cols : bm.rows), red, 1};
-    if (dtype == EBS_F32) {
-        o.row_exp = a.exps;
-        o.col_exp = b.exps;
-        o.fp32.a = static_cast<const float*>(am.p);
-        o.fp32.b = static_cast<const float*>(bm.p);
-        o.fp32.a_row = a.op.mn_major ? 1 : am.ld;
-        o.fp32.a_red = a.op.mn_major ? am.ld : 1;
-        o.fp32.b_col = b.op.mn_major ? 1 : bm.ld;
-        o.fp32.b_red = b.op.mn_major ? bm.ld : 1;
-        o.fp32.red = red;
-    }
-    return launch_gemm(a.op, b.op, s, scratch, o, dtype, st);
+// A product of prepared operands; a: its rows are the result's (across: its columns), likewise b for the result's columns.
+static GemmShape product_shape(const Prepared& a, const Matrix& am, const Prepared& b, const Matrix& bm, int red) {
+    return GemmShape{(int)(a.op.mn_major ? am.cols : am.rows), (int)(b.op.mn_major ? bm.cols : bm.rows), red, 1};
+}
+static GemmOut product_out(const Prepared& a, const Matrix& am, const Prepared& b, const Matrix& bm, int red, GemmOut o, int dtype) {
+    if (dtype != EBS_F32) return o;
+    o.row_exp = a.exps;
+    o.col_exp = b.exps;
+    o.fp32.a = static_cast<const float*>(am.p);
+    o.fp32.b = static_cast<const float*>(bm.p);
+    o.fp32.a_row = a.op.mn_major ? 1 : am.ld;
+    o.fp32.a_red = a.op.mn_major ? am.ld : 1;
+    o.fp32.b_col = b.op.mn_major ? 1 : bm.ld;
+    o.fp32.b_red = b.op.mn_major ? bm.ld : 1;
+    o.fp32.red = red;
+    return o;
 }
 
 // ---------------------------------------------------------------------------------------------------- dz and dbias
@@ -494,7 +529,7 @@ static int launch_dz(DzArgs& g, SplitJobs& jobs, cudaStream_t st) {
     SplitJobs chunked = {};
     blocks = sums;
     for (int i = 0; i < jobs.count; ++i) {
-        if (!jobs.job[i].across || jobs.job[i].chunks < 2) continue;
+        if (!jobs.job[i].across || jobs.job[i].joined == jobs.job[i].chunks) continue;
         chunked.job[chunked.count] = jobs.job[i];
         chunked.job[chunked.count++].first = blocks;
         blocks += (unsigned)((jobs.job[i].cols + 31) / 32);
@@ -522,8 +557,11 @@ static int forward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws,
     float* scratch = ws.take<float>(gemm_route(GemmShape{d.m, d.n, d.k, 1}, planes).scratch / 4);
     if (!run) return EBS_OK;
     int rc;
-    if ((rc = launch_splits(jobs, st)) || (rc = copy_operand(xm, x, st)) || (rc = copy_operand(wm, w, st))) return rc;
-    return product(x, xm, w, wm, d.k, o, d.dtype, scratch, st);
+    CopyJobs copies = {};
+    add_copy(&copies, xm, x);
+    add_copy(&copies, wm, w);
+    if ((rc = launch_splits(jobs, st)) || (rc = launch_copies(copies, st))) return rc;
+    return launch_gemm(x.op, w.op, product_shape(x, xm, w, wm, d.k), scratch, product_out(x, xm, w, wm, d.k, o, d.dtype), d.dtype, st);
 }
 static int backward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws, bool run, cudaStream_t st) {
     int rc = EBS_OK;
@@ -572,19 +610,22 @@ static int backward(const ebs_linear_desc& d, const LinearTensors& t, Carver& ws
     if (fp32) rc = launch_dz<float>(g, jobs, st);
     else if (d.act || t.dbias) rc = d.dtype == EBS_F16 ? launch_dz<__half>(g, jobs, st) : launch_dz<__nv_bfloat16>(g, jobs, st);
     if (rc || (rc = launch_splits(jobs, st))) return rc;
-    if (!fp32 && (t.dx || t.dw) && (rc = copy_operand(dm, rows, st))) return rc;
-    GemmOut o;
-    o.alpha = 1.0f / dz_store_scale(d);
-    if (t.dx) {
-        if ((rc = copy_operand(wm, w, st))) return rc;
-        o.y = t.dx; o.ldy = d.ldx;
-        if ((rc = product(rows, dm, w, wm, d.n, o, d.dtype, scratch, st))) return rc;
-    }
-    if (t.dw) {
-        if ((rc = copy_operand(xm, x, st))) return rc;
-        o.y = t.dw; o.ldy = d.ldw;
-        if ((rc = product(columns, dm, x, xm, d.m, o, d.dtype, scratch, st))) return rc;
-    }
+    CopyJobs copies = {};
+    if (t.dx || t.dw) add_copy(&copies, dm, rows);
+    if (t.dx) add_copy(&copies, wm, w);
+    if (t.dw) add_copy(&copies, xm, x);
+    if ((rc = launch_copies(copies, st))) return rc;
+    GemmOut ox, ow;
+    ox.alpha = ow.alpha = 1.0f / dz_store_scale(d);
+    ox.y = t.dx; ox.ldy = d.ldx;
+    ow.y = t.dw; ow.ldy = d.ldw;
+    if (t.dx) ox = product_out(rows, dm, w, wm, d.n, ox, d.dtype);
+    if (t.dw) ow = product_out(columns, dm, x, xm, d.m, ow, d.dtype);
+    const GemmShape sx{d.m, d.k, d.n, 1}, sw{d.n, d.k, d.m, 1};
+    if (t.dx && t.dw && !gemm_route(sx, planes).pair && !gemm_route(sw, planes).pair)
+        return launch_gemm_tiles({{rows.op, w.op, sx}, {columns.op, x.op, sw}}, {ox, ow}, d.dtype, st);
+    if (t.dx && (rc = launch_gemm(rows.op, w.op, sx, scratch, ox, d.dtype, st))) return rc;
+    if (t.dw && (rc = launch_gemm(columns.op, x.op, sw, scratch, ow, d.dtype, st))) return rc;
     return EBS_OK;
 }
 static size_t linear_workspace(const ebs_linear_desc& d, bool back) {
