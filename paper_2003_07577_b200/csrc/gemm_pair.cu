@@ -69,11 +69,11 @@ template <typename T>
 struct RowOut<LinearOut<T>> {
     static constexpr int CW = 64 / sizeof(T), N = Pack<T>::N;
     struct Ahead { uint4 residual[4]; };
-    static __device__ __forceinline__ void begin(const LinearOut<T>& e, float* terms, int at, int col, int cols) {
+    static __device__ __forceinline__ void begin(const LinearOut<T>& e, float* terms, int columns, int at, int col, int cols) {
         terms[at] = e.o.bias && col < cols ? to_f32(static_cast<const T*>(e.o.bias)[col]) : 0.0f;
         if (sizeof(T) == 4) {                                 // (a factor of zero: an exponent that is not an ordinary one)
             const int x = col < cols ? e.o.col_exp[col] : 0;
-            terms[64 + at] = abs(x) <= SCALE_PLAIN ? power_of_two(x) * e.o.alpha : 0.0f;
+            terms[columns + at] = abs(x) <= SCALE_PLAIN ? power_of_two(x) * e.o.alpha : 0.0f;
         }
     }
     static __device__ __forceinline__ int row_term(const LinearOut<T>& e, long long row, bool exists) { return sizeof(T) == 4 && exists ? e.o.row_exp[row] : 0; }
@@ -84,13 +84,13 @@ struct RowOut<LinearOut<T>> {
         for (int c = 0; c < 4; ++c)
             if (c * N < left) a.residual[c] = load_raw(p + c * N, left - c * N, left >= (c + 1) * N);
     }
-    static __device__ __forceinline__ void scale(const LinearOut<T>& e, float (&v)[CW], const float* terms, long long row, int col, int left, int row_term, uint8_t* buffer, int lane, bool exists) {
+    static __device__ __forceinline__ void scale(const LinearOut<T>& e, float (&v)[CW], const float* terms, int columns, long long row, int col, int left, int row_term, uint8_t* buffer, int lane, bool exists) {
         if constexpr (sizeof(T) == 4) {
             float t[CW];
             bool plain = abs(row_term) <= SCALE_PLAIN;
 #pragma unroll
             for (int i = 0; i < CW; i += 4) {
-                *reinterpret_cast<float4*>(t + i) = *reinterpret_cast<const float4*>(terms + 64 + i);
+                *reinterpret_cast<float4*>(t + i) = *reinterpret_cast<const float4*>(terms + columns + i);
                 plain = plain && t[i] != 0.0f && t[i + 1] != 0.0f && t[i + 2] != 0.0f && t[i + 3] != 0.0f;
             }
             if (plain) {
@@ -144,10 +144,10 @@ struct RowOut<LinearOut<T>> {
         }
     }
     template <int R>
-    static __device__ __forceinline__ void finish(const LinearOut<T>& e, const CUtensorMap* y, const CUtensorMap* z, RowRing<R>& ring, float (&v)[CW], const float* terms, int, int rows, int batch, int row0,
+    static __device__ __forceinline__ void finish(const LinearOut<T>& e, const CUtensorMap* y, const CUtensorMap* z, RowRing<R>& ring, float (&v)[CW], const float* terms, int columns, int, int rows, int batch, int row0,
                                                   int col, int left, int row_term, const Ahead& a, bool exists) {
         uint8_t* to = ring.next();
-        scale(e, v, terms, row0 + ring.lane, col, left, row_term, to, ring.lane, row0 + ring.lane < rows);
+        scale(e, v, terms, columns, row0 + ring.lane, col, left, row_term, to, ring.lane, row0 + ring.lane < rows);
         if (e.o.z) {
             put_row<T>(to, ring.lane, v);
             ring.store(z, to, col, row0, batch, exists);
@@ -164,7 +164,7 @@ template <>
 struct RowOut<PlanesOut> {
     static constexpr int CW = 32;
     struct Ahead {};
-    static __device__ __forceinline__ void begin(const PlanesOut&, float*, int, int, int) {}
+    static __device__ __forceinline__ void begin(const PlanesOut&, float*, int, int, int, int) {}
     static __device__ __forceinline__ int row_term(const PlanesOut&, long long, bool) { return 0; }
     static __device__ __forceinline__ void ahead(const PlanesOut&, int, long long, int, int, Ahead&) {}
     template <int R>
@@ -200,7 +200,7 @@ struct RowOut<PlanesOut> {
         ring.store(y, buffer, col, row0, 2 * batch + 1, exists);
     }
     template <int R>
-    static __device__ __forceinline__ void finish(const PlanesOut& e, const CUtensorMap* y, const CUtensorMap* y2, RowRing<R>& ring, float (&v)[CW], const float*, int mirror, int rows, int batch,
+    static __device__ __forceinline__ void finish(const PlanesOut& e, const CUtensorMap* y, const CUtensorMap* y2, RowRing<R>& ring, float (&v)[CW], const float*, int, int mirror, int rows, int batch,
                                                   int row0, int col, int left, int, const Ahead&, bool exists) {
         matrix(e.y, e, y, ring, v, e.alpha, e.diag, mirror, rows, batch, row0, col, left, exists);
         if (e.y2) matrix(e.y2, e, y2, ring, v, e.alpha2, e.diag2, mirror, rows, batch, row0, col, left, exists);
@@ -211,11 +211,11 @@ template <typename T>
 struct RowOut<TypedFinal<T>> {
     static constexpr int CW = 64 / sizeof(T);
     struct Ahead {};
-    static __device__ __forceinline__ void begin(const TypedFinal<T>&, float*, int, int, int) {}
+    static __device__ __forceinline__ void begin(const TypedFinal<T>&, float*, int, int, int, int) {}
     static __device__ __forceinline__ int row_term(const TypedFinal<T>&, long long, bool) { return 0; }
     static __device__ __forceinline__ void ahead(const TypedFinal<T>&, int, long long, int, int, Ahead&) {}
     template <int R>
-    static __device__ __forceinline__ void finish(const TypedFinal<T>& e, const CUtensorMap* y, const CUtensorMap*, RowRing<R>& ring, float (&v)[CW], const float*, int, int rows, int batch, int row0, int col,
+    static __device__ __forceinline__ void finish(const TypedFinal<T>& e, const CUtensorMap* y, const CUtensorMap*, RowRing<R>& ring, float (&v)[CW], const float*, int, int, int rows, int batch, int row0, int col,
                                                   int, int, const Ahead&, bool exists) {
 #pragma unroll
         for (int i = 0; i < CW; ++i) v[i] *= e.o.alpha;
@@ -229,11 +229,11 @@ template <>
 struct RowOut<PartialOut> {
     static constexpr int CW = 16;
     struct Ahead {};
-    static __device__ __forceinline__ void begin(const PartialOut&, float*, int, int, int) {}
+    static __device__ __forceinline__ void begin(const PartialOut&, float*, int, int, int, int) {}
     static __device__ __forceinline__ int row_term(const PartialOut&, long long, bool) { return 0; }
     static __device__ __forceinline__ void ahead(const PartialOut&, int, long long, int, int, Ahead&) {}
     template <int R>
-    static __device__ __forceinline__ void finish(const PartialOut&, const CUtensorMap* y, const CUtensorMap*, RowRing<R>& ring, float (&v)[CW], const float*, int, int, int slice, int row0, int col, int,
+    static __device__ __forceinline__ void finish(const PartialOut&, const CUtensorMap* y, const CUtensorMap*, RowRing<R>& ring, float (&v)[CW], const float*, int, int, int, int slice, int row0, int col, int,
                                                   int, const Ahead&, bool exists) {
         uint8_t* to = ring.next();
         put_row<float>(to, ring.lane, v);
@@ -243,16 +243,17 @@ struct RowOut<PartialOut> {
 
 constexpr int PAIR_EPI_WARPS = 16;                               // a quarter of the columns each four: fewer leave the memory and barrier latencies of small reductions in the open
 constexpr int PAIR_THREADS = (PAIR_EPI_WARPS + 4) * 32;          // and a warpgroup that fetches and issues (two of its warps idle)
-constexpr int PAIR_HALF = 128 * GEMM_ROW_BYTES;                  // 128 rows of 64 elements
-template <int PL> __host__ __device__ constexpr int pair_stage_bytes() { return 2 * PL * PAIR_HALF; }
-template <int PL> __host__ __device__ constexpr int pair_stages() { return PL == 1 ? 5 : 3; }
+constexpr int PAIR_A = 128 * GEMM_ROW_BYTES;                     // a block's 128 rows of A: 64 elements each
+template <int TN> __host__ __device__ constexpr int pair_b() { return TN / 2 * GEMM_ROW_BYTES; }             // and its half of B
+template <int PL, int TN> __host__ __device__ constexpr int pair_stage_bytes() { return PL * (PAIR_A + pair_b<TN>()); }
+template <int PL, int TN> __host__ __device__ constexpr int pair_stages() { return 192 * 1024 / pair_stage_bytes<PL, TN>(); }      // 6 or 8, 3 or 4
 // Per warp, behind the stages: a ring of buffers of 64-byte rows of results on their way out.
 constexpr int PAIR_PATCH_COLUMNS = 8, PAIR_PATCH_PITCH = PAIR_PATCH_COLUMNS + 4;
-template <int PL> __host__ __device__ constexpr int pair_ring() { return PL == 1 ? 2 : 1; }
-constexpr int PAIR_TERMS = 4 * 2 * 64 * 4;                       // per column quarter: bias and factor of 64 columns
+constexpr int PAIR_RING = 1;
+constexpr int PAIR_TERMS = 4 * 2 * 64 * 4;                       // per column quarter: bias and factor of up to 64 columns
 constexpr int PAIR_BARRIERS = 256;
-template <int PL> __host__ __device__ constexpr int pair_smem_bytes() {
-    return pair_stages<PL>() * pair_stage_bytes<PL>() + PAIR_EPI_WARPS * pair_ring<PL>() * PAIR_BUFFER + PAIR_TERMS + PAIR_BARRIERS;
+template <int PL, int TN> __host__ __device__ constexpr int pair_smem_bytes() {
+    return pair_stages<PL, TN>() * pair_stage_bytes<PL, TN>() + PAIR_EPI_WARPS * PAIR_RING * PAIR_BUFFER + PAIR_TERMS + PAIR_BARRIERS;
 }
 
 // A load into this block's shared memory that signals a barrier of either block of the pair.
@@ -308,12 +309,13 @@ __device__ __forceinline__ void pair_tile(int t, int tiles_m, int tiles_n, int s
     tm = first + t - tn * height;
 }
 
-template <class EPI, int PL>
+template <class EPI, int PL, int TN>
 __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                            const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z, const TileArgs g,
                                                            const EPI epi) {
     extern __shared__ __align__(1024) uint8_t tiles[];            // (nothing static: the stages take all but a few hundred bytes)
-    constexpr int S = pair_stages<PL>(), STAGE = pair_stage_bytes<PL>(), PC = PAIR_PATCH_COLUMNS, PITCH = PAIR_PATCH_PITCH, R = pair_ring<PL>();
+    constexpr int S = pair_stages<PL, TN>(), STAGE = pair_stage_bytes<PL, TN>(), PC = PAIR_PATCH_COLUMNS, PITCH = PAIR_PATCH_PITCH, R = PAIR_RING;
+    constexpr int B_HALF = pair_b<TN>(), CQ = TN / 4;             // CQ: columns of a warp
     uint8_t* behind = tiles + S * STAGE;
     float* all_terms = reinterpret_cast<float*>(behind + PAIR_EPI_WARPS * R * PAIR_BUFFER);
     uint64_t* full = reinterpret_cast<uint64_t*>(behind + PAIR_EPI_WARPS * R * PAIR_BUFFER + PAIR_TERMS);
@@ -324,7 +326,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x & 1), pairs = (int)(gridDim.x >> 1);
     const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK, chunk = PL == 2 ? GEMM_CHUNK : blocks;
-    const int tiles_m = (g.out_rows + 255) / 256, tiles_n = (g.out_cols + 255) / 256, count = (g.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n) * g.batch * g.split;
+    const int tiles_m = (g.out_rows + 255) / 256, tiles_n = (g.out_cols + TN - 1) / TN, count = (g.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n) * g.batch * g.split;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
@@ -334,7 +336,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     if (warp == PAIR_EPI_WARPS + 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_slot)), "r"(2u * TN) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
@@ -357,7 +359,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
         for (int t = (int)(blockIdx.x >> 1); t < count && ok; t += pairs) {
             int batch, tm, tn, part, kb0, kb1;
             pair_tile(t, tiles_m, tiles_n, g.symmetric, g.split, blocks, batch, tm, tn, part, kb0, kb1);
-            const int a0 = tm * 256 + rank * 128, b0 = tn * 256 + rank * 128;
+            const int a0 = tm * 256 + rank * 128, b0 = tn * TN + rank * (TN / 2);
             for (int kb = kb0; kb < kb1; ++kb, ++i) {
                 const int s = i % S, k = kb * GEMM_BK;
                 ok = mbar_wait_warp(&empty[s], ((i / S) & 1) ^ 1, &abort_flag, g.wait_limit);
@@ -367,12 +369,14 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                     if (rank == 0) mbar_expect_tx(&full[s], 2 * STAGE);
 #pragma unroll
                     for (int p = 0; p < PL; ++p) {
-                        const uint32_t at = base + p * PAIR_HALF, bt = base + (PL + p) * PAIR_HALF;
+                        const uint32_t at = base + p * PAIR_A, bt = base + PL * PAIR_A + p * B_HALF;
                         const int z = batch * PL + p;
                         if (!g.a_mn) tma_load_3d_pair(at, &map_a, k, a0, z, bar);
                         else { tma_load_3d_pair(at, &map_a, a0, k, z, bar); tma_load_3d_pair(at + 8192, &map_a, a0 + 64, k, z, bar); }
                         if (!g.b_mn) tma_load_3d_pair(bt, &map_b, k, b0, z, bar);
-                        else { tma_load_3d_pair(bt, &map_b, b0, k, z, bar); tma_load_3d_pair(bt + 8192, &map_b, b0 + 64, k, z, bar); }
+                        else
+#pragma unroll
+                            for (int h = 0; h < TN / 128; ++h) tma_load_3d_pair(bt + h * 8192, &map_b, b0 + h * 64, k, z, bar);
                     }
                 }
                 __syncwarp();
@@ -380,7 +384,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
         }
       } else if (warp == PAIR_EPI_WARPS + 1 && rank == 0) {
             const uint32_t leader = elect_one() ? 1u : 0u;
-            const uint32_t idesc = gemm_idesc(256, 256, g.bf16, g.a_mn, g.b_mn);
+            const uint32_t idesc = gemm_idesc(256, TN, g.bf16, g.a_mn, g.b_mn);
             const uint32_t a_step = g.a_mn ? 2048 >> 4 : 32 >> 4, b_step = g.b_mn ? 2048 >> 4 : 32 >> 4;
             int i = 0, c = 0;                                     // stages and accumulators used so far
             bool ok = true;
@@ -395,15 +399,15 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
                     const bool last = in_chunk == chunk - 1 || kb == kb1 - 1;
                     if ((g.test_flags & 1) == 0) {                // (give-up test: nothing is ever issued)
-                        const uint32_t d = tmem + (uint32_t)((c & 1) * 256), base = smem_u32(tiles) + s * STAGE;
-                        const uint32_t ah = tile_desc_lo(base, g.a_mn), bh = tile_desc_lo(base + PL * PAIR_HALF, g.b_mn);
+                        const uint32_t d = tmem + (uint32_t)((c & 1) * TN), base = smem_u32(tiles) + s * STAGE;
+                        const uint32_t ah = tile_desc_lo(base, g.a_mn), bh = tile_desc_lo(base + PL * PAIR_A, g.b_mn);
 #pragma unroll
                         for (int k = 0; k < GEMM_BK / 16; ++k) {
                             const uint32_t a = ah + k * a_step, b = bh + k * b_step;
                             umma_f16_pair(leader, d, a, b, idesc, (in_chunk | k) != 0);
                             if (PL == 2) {
-                                umma_f16_pair(leader, d, a, b + (PAIR_HALF >> 4), idesc, 1u);
-                                umma_f16_pair(leader, d, a + (PAIR_HALF >> 4), b, idesc, 1u);
+                                umma_f16_pair(leader, d, a, b + (B_HALF >> 4), idesc, 1u);
+                                umma_f16_pair(leader, d, a + (PAIR_A >> 4), b, idesc, 1u);
                             }
                         }
                         umma_commit_both(leader, cluster_addr(&empty[s], 0), cluster_addr(&empty[s], 1));
@@ -418,26 +422,26 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
         using Rows = RowOut<EPI>;
         constexpr int CW = Rows::CW;
         RowRing<R> ring{behind + warp * R * PAIR_BUFFER, lane};
-        float* terms = all_terms + (warp >> 2) * 128;             // shared by the four warps of a column quarter
+        float* terms = all_terms + (warp >> 2) * 2 * CQ;             // shared by the four warps of a column quarter
         float* patch = reinterpret_cast<float*>(ring.base);
         static_assert(R * PAIR_BUFFER >= 32 * PITCH * 4, "the patch lies in the ring");
-        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * 64;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * CQ;
         constexpr int N = EPI::N, PER_ROW = PC / N, ROWS = 32 / PER_ROW, STEPS = 32 / ROWS;
         int c = 0, done = 0;                                      // accumulators and tiles so far
         bool ok = true;
         for (int t = (int)(blockIdx.x >> 1); t < count && ok; t += pairs, ++done) {
             int batch, tm, tn, part, kb0, kb1;
             pair_tile(t, tiles_m, tiles_n, g.symmetric, g.split, blocks, batch, tm, tn, part, kb0, kb1);
-            const int row0 = tm * 256 + rank * 128 + (warp & 3) * 32, col0 = tn * 256 + (warp >> 2) * 64;
+            const int row0 = tm * 256 + rank * 128 + (warp & 3) * 32, col0 = tn * TN + (warp >> 2) * CQ;
             const int slice = part * g.batch + batch;             // (parts: a matrix each)
             // rows by TMA
             int row_term = 0;
             if (g.packs) {
-                const int at = (warp & 3) * 16 + lane;
+                const int at = (warp & 3) * (CQ / 4) + lane;
                 // (mbarriers, not a block barrier: a warp that gave up is not waited for without end)
                 if (done > 0) ok = mbar_wait_bounded(&terms_read[warp >> 2], (done - 1) & 1, &abort_flag, g.wait_limit);
                 if (!ok) break;
-                if (lane < 16) Rows::begin(epi, terms, at, col0 + at, g.out_cols);
+                if (lane < CQ / 4) Rows::begin(epi, terms, CQ, at, col0 + at, g.out_cols);
                 row_term = Rows::row_term(epi, row0 + lane, row0 + lane < g.out_rows);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&terms_there[warp >> 2]);
@@ -450,7 +454,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
             };
             auto rows_out = [&](int column, float (&v)[CW]) {
                 const int col = col0 + column;
-                Rows::finish(epi, &map_y, &map_z, ring, v, terms + column, g.symmetric && tm != tn, g.out_rows, slice, row0, col, g.out_cols - col, row_term, row_ahead,
+                Rows::finish(epi, &map_y, &map_z, ring, v, terms + column, CQ, g.symmetric && tm != tn, g.out_rows, slice, row0, col, g.out_cols - col, row_term, row_ahead,
                              col < g.out_cols && row0 < g.out_rows);
             };
             // lanes that share rows, through a patch: outputs whose rows start anywhere
@@ -481,17 +485,17 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                 for (int e = 0; e < PC; e += 4) *reinterpret_cast<float4*>(patch + lane * PITCH + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
             };
             if constexpr (PL == 2) {
-                float acc[64];
+                float acc[CQ];
 #pragma unroll
-                for (int j = 0; j < 64; ++j) acc[j] = 0.0f;
+                for (int j = 0; j < CQ; ++j) acc[j] = 0.0f;
                 for (int kb = kb0; kb < kb1 && ok; kb += chunk, ++c) {
                     ok = mbar_wait_bounded(&acc_full[c & 1], (c >> 1) & 1, &abort_flag, g.wait_limit);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
 #pragma unroll
-                    for (int j = 0; j < 64; j += 32) {
+                    for (int j = 0; j < CQ; j += 32) {
                         uint32_t v[32];
-                        tmem_ld32_issue(lanes + (c & 1) * 256 + j, v);
+                        tmem_ld32_issue(lanes + (c & 1) * TN + j, v);
                         tmem_ld32_wait(v);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) acc[j + e] += __uint_as_float(v[e]);
@@ -502,7 +506,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                 if (!ok) break;
                 if (g.packs) {
 #pragma unroll
-                    for (int j = 0; j < 64; j += CW) {
+                    for (int j = 0; j < CQ; j += CW) {
                         rows_ahead(j);
                         float v[CW];
 #pragma unroll
@@ -511,10 +515,10 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                     }
                 } else {
 #pragma unroll 1
-                    for (int j = 0; j < 64; j += PC) {            // (registers have no index: one copy of the moves a position)
+                    for (int j = 0; j < CQ; j += PC) {            // (registers have no index: one copy of the moves a position)
                         float v[PC];
 #pragma unroll
-                        for (int q = 0; q < 64; q += PC)
+                        for (int q = 0; q < CQ; q += PC)
                             if (q == j) {
 #pragma unroll
                                 for (int e = 0; e < PC; ++e) v[e] = acc[q + e];
@@ -529,12 +533,12 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
 #pragma unroll 1
-                for (int j = 0; j < 64; j += 32) {
+                for (int j = 0; j < CQ; j += 32) {
                     uint32_t raw[32];
-                    tmem_ld32_issue(lanes + (c & 1) * 256 + j, raw);
+                    tmem_ld32_issue(lanes + (c & 1) * TN + j, raw);
                     if (g.packs && j > 0) rows_ahead(j);
                     tmem_ld32_wait(raw);
-                    if (j == 32) {
+                    if (j == CQ - 32) {
                         asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
                         if (lane == 0) mbar_arrive_cluster(cluster_addr(&acc_empty[c & 1], 0));
                     }
@@ -567,7 +571,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     cluster_sync_all();                                           // no block leaves while the other's MMAs or arrivals reach it
     if (warp == PAIR_EPI_WARPS + 1)
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512u) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(2u * TN) : "memory");
 }
 
 unsigned long long gemm_pair_timeouts() {
@@ -575,11 +579,12 @@ unsigned long long gemm_pair_timeouts() {
     return cudaMemcpyFromSymbol(&n, g_gemm_pair_timeouts, sizeof(n)) == cudaSuccess ? n : 0;
 }
 
-// Tensor map of outputs: matrices [rows][cols] of `slices`, 64 bytes by 32 rows a store.  False: rows that do not start on 16 bytes.
+// Tensor map of outputs: matrices [rows][cols] of `slices`, 64 bytes by 32 rows a store.  False: rows that do not start on 16 bytes, or end
+// inside 16 bytes (a store is clipped to whole 16 bytes: it would write past the end of each row).
 template <typename T>
-static bool result_map(const void* p, long long rows, long long cols, long long ld, long long slices, long long slice, CUtensorMap* map) {
+static bool result_map(const void* p, long long rows, long long cols, long long ld, long long slices, long long slice, CUtensorMap* map, bool padded = false) {
     if (!p) return true;
-    if (((uintptr_t)p & 15) != 0 || (ld * sizeof(T)) % 16 != 0 || (slice * sizeof(T)) % 16 != 0) return false;
+    if (((uintptr_t)p & 15) != 0 || (ld * sizeof(T)) % 16 != 0 || (slice * sizeof(T)) % 16 != 0 || (!padded && (cols * sizeof(T)) % 16 != 0)) return false;
     const CUtensorMapDataType type = std::is_same<T, float>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)slices};
     const cuuint64_t strides[2] = {(cuuint64_t)ld * sizeof(T), (cuuint64_t)(slices > 1 ? slice : ld * rows) * sizeof(T)};
@@ -592,19 +597,19 @@ static bool result_maps(const LinearOut<T>& e, const GemmShape& s, CUtensorMap* 
     return whole(e.o.residual, e.o.ldr) && result_map<T>(e.o.y, s.rows, s.cols, e.o.ldy, 1, 0, y) && result_map<T>(e.o.z, s.rows, s.cols, e.o.ldz, 1, 0, z);
 }
 static bool result_maps(const PlanesOut& e, const GemmShape& s, CUtensorMap* y, CUtensorMap* y2) {
-    return result_map<__half>(e.y, s.rows, s.cols, e.ld, 2LL * s.batch, e.plane, y) && result_map<__half>(e.y2, s.rows, s.cols, e.ld, 2LL * s.batch, e.plane, y2);
+    return result_map<__half>(e.y, s.rows, s.cols, e.ld, 2LL * s.batch, e.plane, y, true) && result_map<__half>(e.y2, s.rows, s.cols, e.ld, 2LL * s.batch, e.plane, y2, true);
 }
 template <typename T>
 static bool result_maps(const TypedFinal<T>& e, const GemmShape& s, CUtensorMap* y, CUtensorMap*) {
     return result_map<T>(e.o.y, s.rows, s.cols, e.o.ld, s.batch, e.o.batch, y);
 }
 static bool result_maps(const PartialOut& e, const GemmShape& s, CUtensorMap* y, CUtensorMap*) {
-    return result_map<float>(e.y, s.rows, s.cols, e.ld, (long long)s.batch * e.parts, e.batch, y);
+    return result_map<float>(e.y, s.rows, s.cols, e.ld, (long long)s.batch * e.parts, e.batch, y, true);
 }
 
-template <class EPI, int PL>
+template <class EPI, int PL, int TN>
 static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, int split, cudaStream_t st) {
-    const bool symmetric = s.symmetric && std::is_same<EPI, PlanesOut>::value;
+    const bool symmetric = s.symmetric && TN == 256 && std::is_same<EPI, PlanesOut>::value;
     TileArgs g = {};
     g.red = s.red;
     g.out_rows = s.rows;
@@ -617,14 +622,14 @@ static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmSha
     g.bf16 = bf16;
     g.wait_limit = device_wait_limit();
     g.test_flags = device_test_flags();
-    const long long side = (s.rows + 255) / 256, tiles = (symmetric ? side * (side + 1) / 2 : side * ((s.cols + 255) / 256)) * s.batch * split;
+    const long long side = (s.rows + 255) / 256, tiles = (symmetric ? side * (side + 1) / 2 : side * ((s.cols + TN - 1) / TN)) * s.batch * split;
     if (tiles >= (1LL << 30)) return EBS_ERR_OVERFLOW;
     CUtensorMap a, b, y{}, z{};
-    if (!gemm_operand_map(A, s.rows, s.red, s.batch, 128, bf16, &a) || !gemm_operand_map(B, s.cols, s.red, s.batch, 128, bf16, &b)) return EBS_ERR_CUDA;
+    if (!gemm_operand_map(A, s.rows, s.red, s.batch, 128, bf16, &a) || !gemm_operand_map(B, s.cols, s.red, s.batch, TN / 2, bf16, &b)) return EBS_ERR_CUDA;
     g.packs = result_maps(epi, s, &y, &z);
     if (symmetric && !g.packs) return EBS_ERR_CUDA;               // (kept planes always have whole rows)
-    auto kern = gemm_pair_kernel<EPI, PL>;
-    constexpr int bytes = pair_smem_bytes<PL>();
+    auto kern = gemm_pair_kernel<EPI, PL, TN>;
+    constexpr int bytes = pair_smem_bytes<PL, TN>();
     static_assert(bytes <= 227 * 1024, "shared memory of a block");
     static bool attr_set[64] = {};
     int dev = 0;
@@ -669,14 +674,14 @@ __global__ void __launch_bounds__(256) reduce_parts_kernel(const PartialOut in, 
 }
 template <class EPI, int PL>
 static int launch_pair_or_parts(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, bool packs, const GemmRoute& route, float* scratch, cudaStream_t st) {
-    if (route.split == 1) return launch_pair<EPI, PL>(A, B, s, epi, bf16, 1, st);
+    if (route.split == 1) return route.tn == 128 ? launch_pair<EPI, PL, 128>(A, B, s, epi, bf16, 1, st) : launch_pair<EPI, PL, 256>(A, B, s, epi, bf16, 1, st);
     PartialOut p;
     p.y = scratch;
     p.ld = (s.cols + 7) & ~7LL;
     p.batch = p.ld * s.rows;
     p.part = p.batch * s.batch;
     p.parts = route.split;
-    const int rc = launch_pair<PartialOut, PL>(A, B, s, p, bf16, route.split, st);
+    const int rc = launch_pair<PartialOut, PL, 256>(A, B, s, p, bf16, route.split, st);
     if (rc) return rc;
     const long long items = (long long)((s.cols + EPI::N - 1) / EPI::N) * s.rows, blocks = (items + 255) / 256;
     return launch_chained(reduce_parts_kernel<EPI>, dim3((unsigned)(blocks < 4096 ? blocks : 4096), s.batch), 256, 0, st, 1, p, route.split, s.rows, s.cols, (int)packs, epi);
@@ -701,10 +706,18 @@ int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape
 // The kernel for a product, from its sizes alone (and so the same for the workspace's count and for the call).
 GemmRoute gemm_route(const GemmShape& s, int planes) {
     GemmRoute r;
-    const long long side = (s.rows + 255) / 256, tiles = (s.symmetric ? side * (side + 1) / 2 : side * ((s.cols + 255) / 256)) * s.batch;
+    const long long side = (s.rows + 255) / 256, wide = (s.symmetric ? side * (side + 1) / 2 : side * ((s.cols + 255) / 256)) * s.batch;
+    const long long narrow = side * ((s.cols + 127) / 128) * s.batch;
     const int blocks = (s.red + GEMM_BK - 1) / GEMM_BK;
-    r.pair = s.rows > 128 && s.cols > 128 && tiles >= 32;
-    if (!r.pair && s.rows > 128 && s.cols > 128 && blocks >= 64) {
+    r.pair = s.rows > 128 && s.cols > 128 && wide >= 32;
+    if (r.pair) {
+        // Split products on tiles of 128 columns where 256 leave pairs idle (us with 256 and 128: 512 x 4608 over 512 23.3 and 13.9, 12544 x 256 over
+        // 1152 33.5 and 30.2, 2048 x 2048 over 2048 48.0 and 43.4) or the reduction is short and the last round fuller (12544 x 1152 over 256
+        // 37.1 and 33.2; 4096 x 4096 over 1024 78.4 and 81.4).  16-bit operands never: half the work per byte fetched (8192 x 4096 over 512 36.7
+        // and 55.4).
+        const long long w = (wide + 73) / 74 * 2, n = (narrow + 73) / 74;
+        if (planes == 2 && !s.symmetric && (wide <= 74 || (blocks <= 8 && n < w))) r.tn = 128;
+    } else if (s.rows > 128 && s.cols > 128 && blocks >= 64) {
         const long long all = side * ((s.cols + 255) / 256) * s.batch;
         r.split = (int)(74 / all);
         if (r.split > blocks / 8) r.split = blocks / 8;

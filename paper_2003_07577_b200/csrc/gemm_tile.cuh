@@ -27,10 +27,10 @@ int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const FinalOut& out, int dtype, cudaStream_t st);
 unsigned long long gemm_tile_timeouts();
 
-// How a product is run: the pair kernel, with its reduction in `split` parts that meet in `scratch` bytes of memory, or the tile kernel.
+// How a product is run: the pair kernel on tiles of 256 x tn, with its reduction in `split` parts that meet in `scratch` bytes of memory, or the tile kernel.
 struct GemmRoute {
     bool pair = false;
-    int split = 1;
+    int tn = 256, split = 1;                // columns of a tile, parts
     size_t scratch = 0;
 };
 GemmRoute gemm_route(const GemmShape& s, int planes);

@@ -192,6 +192,26 @@ def test_backward_strides(ebs, dtype, act, pads, m, n, k):
     check_backward(ebs, m, n, k, dtype, act, pads=pads)
 
 
+# sizes of the persistent pair kernel (32 tiles of 256 x 256 and more; fp32 on 128 columns too), of a reduction in parts, and of both
+# gradients in one launch; the result's rows start on 16 bytes (they leave by TMA, clipped at n) or anywhere
+LARGE = [(2049, 1283, 200, (0, 0, 5, 5, 5)), (2049, 1283, 200, (3, 5, 0, 2, 1)), (2304, 1152, 64, (0,) * 5), (4100, 2050, 330, (6, 6, 6, 6, 6)), (300, 260, 8200, (0, 0, 4, 4, 4)), (2304, 1160, 131, (5, 5, 0, 0, 0)),
+         (257, 129, 4104, (1, 0, 0, 0, 0)), (1531, 259, 517, (3, 0, 0, 0, 0))]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("m,n,k,pads", LARGE)
+def test_forward_large(ebs, dtype, m, n, k, pads):
+    check_forward(ebs, m, n, k, dtype, "gelu", pads=pads)
+    check_forward(ebs, m, n, k, dtype, "none", False, False, False, pads=pads)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("m,n,k,pads", LARGE)
+def test_backward_large(ebs, dtype, m, n, k, pads):
+    check_backward(ebs, m, n, k, dtype, "silu", pads=pads[:4])
+    check_backward(ebs, n, m, k, dtype, "none", pads=pads[:4], want=(1, 1, 0))
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_empty_batch(ebs, dtype):
     t = TYPES[dtype]
@@ -205,7 +225,7 @@ def test_empty_batch(ebs, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("m,n,k", [(3, 40, 200), (150, 200, 72)])
+@pytest.mark.parametrize("m,n,k", [(3, 40, 200), (7, 40, 200), (150, 200, 72), (2304, 1160, 72), (2100, 1200, 520), (300, 264, 8200)])
 def test_nan_and_infinity_reach_their_outputs_only(ebs, dtype, m, n, k):
     t, g = TYPES[dtype], gen(3)
     x, w = strided(m, k, k, t, g), strided(n, k, k, t, g)
@@ -226,7 +246,7 @@ def test_nan_and_infinity_reach_their_outputs_only(ebs, dtype, m, n, k):
         assert torch.equal(torch.isneginf(got), torch.isneginf(ref))
 
 
-@pytest.mark.parametrize("m", [4, 300])
+@pytest.mark.parametrize("m", [4, 300, 9000])
 def test_fp32_rows_of_very_different_size(ebs, m):
     """Rows (and columns) of 2^-60 beside rows of 2^60: every output keeps the accuracy of its own row and column."""
     g, n, k = gen(5), 72, 160
@@ -346,3 +366,27 @@ def test_offsets_beyond_32_bits(ebs):
     run_forward(ebs, x, w, None, None, "bf16", "none", y)
     ref, s = x.double() @ w.double().T, x.double().abs() @ w.double().abs().T
     assert ((y.double() - ref).abs() <= bound(t, ref, s, k)).all()
+
+
+@pytest.mark.parametrize("m,n,k,skip", [(40, 200, 400, 1), (200, 300, 2000, 1), (200, 300, 2000, 2), (4096, 2048, 256, 1), (300, 264, 8200, 1)])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_bounded_waits_give_up_and_recover(ebs, dtype, m, n, k, skip):
+    """Nothing is issued to the tensor core (skip 1), or one part of a split tile sends no sums (2): every wait runs out, the call returns, the
+    status says so once, and the next launch is right.  (One tile a part, a cluster a tile, a pair of blocks, a reduction in parts.)"""
+    t, g = TYPES[dtype], gen(11)
+    x, w = strided(m, k, k, t, g), strided(n, k, k, t, g, 1 / math.sqrt(k))
+    y, want = torch.empty((m, n), dtype=t, device="cuda"), torch.empty((m, n), dtype=t, device="cuda")
+    run_forward(ebs, x, w, None, None, dtype, "none", want)
+    assert ebs.ebs_check_device_status() == ebs.EBS_OK
+    before = ebs.ebs_device_wait_timeouts()
+    ebs.ebs_test_set_device_wait(64, skip)
+    try:
+        run_forward(ebs, x, w, None, None, dtype, "none", y)
+        torch.cuda.synchronize()
+    finally:
+        ebs.ebs_test_set_device_wait(0, 0)
+    assert ebs.ebs_device_wait_timeouts() > before
+    assert ebs.ebs_check_device_status() == ebs.EBS_ERR_TIMEOUT
+    assert ebs.ebs_check_device_status() == ebs.EBS_OK
+    run_forward(ebs, x, w, None, None, dtype, "none", y)
+    assert torch.equal(y, want)

@@ -154,3 +154,26 @@ def test_in_place_streams_and_replay(ebs, dtype, shape):
     ws.fill_(0xFF)
     graph.replay()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("shape", [(3, 64, 576), (2, 16, 2000), (1, 300, 500), (1, 2100, 2100)])
+def test_bounded_waits_give_up_and_recover(ebs, shape):
+    g = make(*shape, torch.bfloat16, 7)
+    want = run(ebs, g)
+    assert ebs.ebs_check_device_status() == ebs.EBS_OK
+    ebs.ebs_test_set_device_wait(64, 1)
+    try:
+        run(ebs, g)
+        torch.cuda.synchronize()
+    finally:
+        ebs.ebs_test_set_device_wait(0, 0)
+    assert ebs.ebs_check_device_status() == ebs.EBS_ERR_TIMEOUT
+    assert torch.equal(run(ebs, g), want)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,cols", [(2100, 2304), (2304, 2100), (512, 4608)])
+def test_large(ebs, dtype, rows, cols):
+    """Symmetric products on and below the diagonal with their mirror images; a reduction in parts."""
+    g = make(1, rows, cols, TYPES[dtype], 1)
+    check(run(ebs, g), iterate64(g, 5), 5)
