@@ -248,7 +248,6 @@ template <int TN> __host__ __device__ constexpr int pair_b() { return TN / 2 * G
 template <int PL, int TN> __host__ __device__ constexpr int pair_stage_bytes() { return PL * (PAIR_A + pair_b<TN>()); }
 template <int PL, int TN> __host__ __device__ constexpr int pair_stages() { return 192 * 1024 / pair_stage_bytes<PL, TN>(); }      // 6 or 8, 3 or 4
 // Per warp, behind the stages: a ring of buffers of 64-byte rows of results on their way out.
-constexpr int PAIR_PATCH_COLUMNS = 8, PAIR_PATCH_PITCH = PAIR_PATCH_COLUMNS + 4;
 constexpr int PAIR_RING = 1;
 constexpr int PAIR_TERMS = 4 * 2 * 64 * 4;                       // per column quarter: bias and factor of up to 64 columns
 constexpr int PAIR_BARRIERS = 256;
@@ -314,7 +313,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                                                            const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z, const TileArgs g,
                                                            const EPI epi) {
     extern __shared__ __align__(1024) uint8_t tiles[];            // (nothing static: the stages take all but a few hundred bytes)
-    constexpr int S = pair_stages<PL, TN>(), STAGE = pair_stage_bytes<PL, TN>(), PC = PAIR_PATCH_COLUMNS, PITCH = PAIR_PATCH_PITCH, R = PAIR_RING;
+    constexpr int S = pair_stages<PL, TN>(), STAGE = pair_stage_bytes<PL, TN>(), R = PAIR_RING;
     constexpr int B_HALF = pair_b<TN>(), CQ = TN / 4;             // CQ: columns of a warp
     uint8_t* behind = tiles + S * STAGE;
     float* all_terms = reinterpret_cast<float*>(behind + PAIR_EPI_WARPS * R * PAIR_BUFFER);
@@ -420,13 +419,11 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;\n");
         using Rows = RowOut<EPI>;
+        constexpr bool ELEMENTS = !std::is_same<EPI, PlanesOut>::value && !std::is_same<EPI, PartialOut>::value;      // (those always have whole rows)
         constexpr int CW = Rows::CW;
         RowRing<R> ring{behind + warp * R * PAIR_BUFFER, lane};
         float* terms = all_terms + (warp >> 2) * 2 * CQ;             // shared by the four warps of a column quarter
-        float* patch = reinterpret_cast<float*>(ring.base);
-        static_assert(R * PAIR_BUFFER >= 32 * PITCH * 4, "the patch lies in the ring");
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * CQ;
-        constexpr int N = EPI::N, PER_ROW = PC / N, ROWS = 32 / PER_ROW, STEPS = 32 / ROWS;
         int c = 0, done = 0;                                      // accumulators and tiles so far
         bool ok = true;
         for (int t = (int)(blockIdx.x >> 1); t < count && ok; t += pairs, ++done) {
@@ -457,32 +454,33 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                 Rows::finish(epi, &map_y, &map_z, ring, v, terms + column, CQ, g.symmetric && tm != tn, g.out_rows, slice, row0, col, g.out_cols - col, row_term, row_ahead,
                              col < g.out_cols && row0 < g.out_rows);
             };
-            // lanes that share rows, through a patch: outputs whose rows start anywhere
-            auto patch_out = [&](int column) {
-                __syncwarp();
-                const int pack_col = (lane % PER_ROW) * N, col = col0 + column + pack_col, left = g.out_cols - col;
-                typename EPI::Columns columns;
-                typename EPI::Ahead ahead[STEPS];
-                if (left > 0) {
-                    epi.columns(col, left, false, columns);
+            // Outputs whose rows start anywhere, 16 columns at a time: through the warp's buffer, then two rows an access, neighbouring lanes
+            // at neighbouring elements, eight accesses' loads under way.
+            auto elements_out = [&](int column, const float (&f)[16]) {
+                if constexpr (ELEMENTS) {
+                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < STEPS; ++i)
-                        if (row0 + lane / PER_ROW + i * ROWS < g.out_rows) epi.ahead(slice, row0 + lane / PER_ROW + i * ROWS, col, left, false, ahead[i]);
+                    for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(row_chunk(ring.base, lane, q)) = make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]);
+                    __syncwarp();
+                    const int cc = lane & 15, col = col0 + column + cc;
+                    if (col < g.out_cols) {
+                        typename EPI::Column terms_of;
+                        epi.column(col, terms_of);
+#pragma unroll 1
+                        for (int r0 = lane >> 4; r0 < 32; r0 += 16) {
+                            typename EPI::Place place[8];
 #pragma unroll
-                    for (int i = 0; i < STEPS; ++i) {
-                        const int r = lane / PER_ROW + i * ROWS;
-                        float v[N];
-                        const float* p = patch + r * PITCH + pack_col;
+                            for (int i = 0; i < 8; ++i)
+                                if (row0 + r0 + 2 * i < g.out_rows) epi.place(row0 + r0 + 2 * i, col, place[i]);
 #pragma unroll
-                        for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(v + e) = *reinterpret_cast<const float4*>(p + e);
-                        if (row0 + r < g.out_rows) epi.pack(slice, row0 + r, col, left, false, v, columns, ahead[i]);
+                            for (int i = 0; i < 8; ++i) {
+                                const int r = r0 + 2 * i;
+                                const float v = reinterpret_cast<const float*>(row_chunk(ring.base, r, cc >> 2))[cc & 3];
+                                if (row0 + r < g.out_rows) epi.one(batch, row0 + r, col, v, terms_of, place[i]);
+                            }
+                        }
                     }
                 }
-                __syncwarp();
-            };
-            auto put_patch = [&](const float* f) {
-#pragma unroll
-                for (int e = 0; e < PC; e += 4) *reinterpret_cast<float4*>(patch + lane * PITCH + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
             };
             if constexpr (PL == 2) {
                 float acc[CQ];
@@ -515,16 +513,15 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                     }
                 } else {
 #pragma unroll 1
-                    for (int j = 0; j < CQ; j += PC) {            // (registers have no index: one copy of the moves a position)
-                        float v[PC];
+                    for (int j = 0; j < CQ; j += 16) {            // (registers have no index: one copy of the moves a position)
+                        float v[16];
 #pragma unroll
-                        for (int q = 0; q < CQ; q += PC)
+                        for (int q = 0; q < CQ; q += 16)
                             if (q == j) {
 #pragma unroll
-                                for (int e = 0; e < PC; ++e) v[e] = acc[q + e];
+                                for (int e = 0; e < 16; ++e) v[e] = acc[q + e];
                             }
-                        put_patch(v);
-                        patch_out(j);
+                        elements_out(j, v);
                     }
                 }
             } else {
@@ -544,17 +541,20 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                     }
 #pragma unroll
                     for (int h = 0; h < 32; h += CW) {
+                        if (!g.packs) break;
                         float v[CW];
 #pragma unroll
                         for (int e = 0; e < CW; ++e) v[e] = __uint_as_float(raw[h + e]);
-                        if (g.packs) rows_out(j + h, v);
-                        else
-#pragma unroll
-                            for (int q = 0; q < CW; q += PC) {
-                                put_patch(v + q);
-                                patch_out(j + h + q);
-                            }
+                        rows_out(j + h, v);
                     }
+                    if (!g.packs)
+#pragma unroll
+                        for (int h = 0; h < 32; h += 16) {
+                            float v[16];
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(raw[h + e]);
+                            elements_out(j + h, v);
+                        }
                 }
                 ++c;
             }

@@ -138,6 +138,28 @@ struct LinearOut {
     using Ahead = GemmAhead;
     GemmOut o;
     __device__ __forceinline__ void touch() const { asm volatile("" ::"l"(o.y), "l"(o.z), "l"(o.ldz), "l"(o.ldy), "f"(o.alpha), "r"(o.act)); }
+    // an element at a time: what its column and its place need from memory, then the rest
+    struct Column { float bias; int exp; };
+    struct Place { float residual; int row_exp; };
+    __device__ __forceinline__ void column(int col, Column& c) const {
+        c.bias = o.bias ? to_f32(static_cast<const T*>(o.bias)[col]) : 0.0f;
+        if (sizeof(T) == 4) c.exp = o.col_exp[col];
+    }
+    __device__ __forceinline__ void place(long long row, int col, Place& p) const {
+        if (o.residual) p.residual = to_f32(static_cast<const T*>(o.residual)[row * o.ldr + col]);
+        if (sizeof(T) == 4) p.row_exp = o.row_exp[row];
+    }
+    __device__ __forceinline__ void one(int, long long row, int col, float v, const Column& c, const Place& p) const {
+        if (sizeof(T) == 4) {
+            if (abs(c.exp) <= SCALE_PLAIN && abs(p.row_exp) <= SCALE_PLAIN) v *= power_of_two(p.row_exp) * power_of_two(c.exp);
+            else v = gemm_unscale(o.fp32.a + row * o.fp32.a_row, o.fp32.a_red, o.fp32.b + col * o.fp32.b_col, o.fp32.b_red, o.fp32.red, p.row_exp, c.exp, v);
+        }
+        v = fmaf(v, o.alpha, c.bias);
+        if (o.z) static_cast<T*>(o.z)[row * o.ldz + col] = from_f32<T>(v);
+        if (o.act) v = activation<sizeof(T) == 2>(v, o.act);
+        if (o.residual) v += p.residual;
+        static_cast<T*>(o.y)[row * o.ldy + col] = from_f32<T>(v);
+    }
     __device__ __forceinline__ void columns(int col, int left, bool vec, Columns& c) const { gemm_columns<T>(o, col, left, vec, c); }
     __device__ __forceinline__ void ahead(int, long long row, int col, int left, bool vec, Ahead& a) const { gemm_ahead<T>(o, row, col, left, vec, a); }
     __device__ __forceinline__ void pack(int, long long row, int col, int left, bool vec, float (&v)[N], const Columns& c, const Ahead& a) const {
@@ -188,6 +210,13 @@ struct TypedFinal {
     struct Columns {};
     struct Ahead {};
     FinalOut o;
+    struct Column {};
+    struct Place {};
+    __device__ __forceinline__ void column(int, Column&) const {}
+    __device__ __forceinline__ void place(long long, int, Place&) const {}
+    __device__ __forceinline__ void one(int b, long long row, int col, float v, const Column&, const Place&) const {
+        static_cast<T*>(o.y)[b * o.batch + row * o.ld + col] = from_f32<T>(v * o.alpha);
+    }
     __device__ __forceinline__ void touch() const { asm volatile("" ::"l"(o.y), "l"(o.batch), "f"(o.alpha)); }
     __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
     __device__ __forceinline__ void ahead(int, long long, int, int, bool, Ahead&) const {}

@@ -372,10 +372,12 @@ struct DzArgs {
     unsigned blocks;                       // of this part of the launch; the column tops of `jobs` follow
 };
 
-// dz = dy * act'(z), stored times `store`, and the column sums of dz before its rounding.  A block takes 32 packs of N columns and the
-// rows of one chunk.  fp32: the column tops of dz here, those of other matrices (jobs with chunks) in further blocks.
-template <typename T, int N>
+// dz = dy * act'(z), stored times `store`, and the column sums of dz before its rounding.  A block takes 32 * N columns and the rows of one
+// chunk; a lane has N neighbouring columns (VEC: 16 bytes an access) or, where the rows start anywhere, every 32nd.  fp32: the column
+// tops of dz here, those of other matrices (jobs with chunks) in further blocks.
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(256, 4) linear_dz_kernel(const __grid_constant__ DzArgs g, const __grid_constant__ SplitJobs jobs) {
+    constexpr int N = Pack<T>::N, U = 2;                      // U rows under way: enough bytes in flight to cover the memory's latency
     __shared__ float sums[8][32 * N + 4];
     __shared__ unsigned part[8][128];
     let_next_kernel_start();
@@ -386,91 +388,83 @@ __global__ void __launch_bounds__(256, 4) linear_dz_kernel(const __grid_constant
         return;
     }
     const int across = (g.n + 32 * N - 1) / (32 * N), bx = (int)(blockIdx.x % across), by = (int)(blockIdx.x / across);
-    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, col = (bx * 32 + lane) * N;
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, col0 = bx * 32 * N;
+    auto local = [&](int e) { return VEC ? lane * N + e : lane + 32 * e; };              // column of element e in this block's
     const long long r0 = (long long)g.m * by / g.chunks, r1 = (long long)g.m * (by + 1) / g.chunks;
-    const T *dy = static_cast<const T*>(g.dy), *z = static_cast<const T*>(g.z);
-    T* dz = static_cast<T*>(g.dz);
+    const T *dy = static_cast<const T*>(g.dy) + col0, *z = static_cast<const T*>(g.z) + col0;
+    T* dz = static_cast<T*>(g.dz) + col0;
+    const int left = g.n - col0;
     float sum[N];
     unsigned top[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[e] = 0.0f;
-    auto finish = [&](long long r, float (&v)[N], const float (&zv)[N]) {
-        switch (g.act) {
-#define EBS_SLOPE_CASE(A) case A: _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] *= activation_slope<sizeof(T) == 2>(zv[e], A); break;
-            EBS_SLOPE_CASE(EBS_ACT_RELU) EBS_SLOPE_CASE(EBS_ACT_GELU) EBS_SLOPE_CASE(EBS_ACT_GELU_TANH) EBS_SLOPE_CASE(EBS_ACT_SILU)
-#undef EBS_SLOPE_CASE
-            default: break;
-        }
+    const bool whole = VEC && local(N - 1) < left;
+    auto load = [&](const T* row) {
+        uint4 u = make_uint4(0u, 0u, 0u, 0u);
+        if (whole) return *reinterpret_cast<const uint4*>(row + local(0));
+        T* t = reinterpret_cast<T*>(&u);
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            sum[e] += v[e];
-            if (sizeof(T) == 4) top[e] = max(top[e], magnitude(v[e]));
-            if (std::is_same<T, __half>::value) v[e] *= g.store;
-        }
-        if (!dz) return;
-        if constexpr (N > 1) store_pack(dz + r * g.lddz + col, v);          // (rows of dz are padded to whole packs)
-        else dz[r * g.lddz + col] = from_f32<T>(v[0]);
+        for (int e = 0; e < N; ++e)
+            if (local(e) < left) t[e] = row[local(e)];
+        return u;
     };
-    if (N > 1 && col + N <= g.n) {
-        if constexpr (N > 1) {
-            constexpr int U = 2;                              // rows under way: enough bytes in flight to cover the memory's latency
-            for (long long r = r0 + y; r < r1; r += 8 * U) {
-                uint4 a[U], b[U];
+    if (local(0) < left)
+        for (long long r = r0 + y; r < r1; r += 8 * U) {
+            uint4 a[U], b[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (r + 8 * u < r1) {
-                        a[u] = *reinterpret_cast<const uint4*>(dy + (r + 8 * u) * g.ldy + col);
-                        if (g.act) b[u] = *reinterpret_cast<const uint4*>(z + (r + 8 * u) * g.ldz + col);
-                    }
+            for (int u = 0; u < U; ++u)
+                if (r + 8 * u < r1) {
+                    a[u] = load(dy + (r + 8 * u) * g.ldy);
+                    if (g.act) b[u] = load(z + (r + 8 * u) * g.ldz);
+                }
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (r + 8 * u < r1) {
-                        float v[N], zv[N];
+            for (int u = 0; u < U; ++u) {
+                if (r + 8 * u >= r1) break;
+                float v[N], zv[N];
+                unpack<T>(a[u], v);
+                if (g.act) unpack<T>(b[u], zv);
+                switch (g.act) {
+#define EBS_SLOPE_CASE(A) case A: _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] *= activation_slope<sizeof(T) == 2>(zv[e], A); break;
+                    EBS_SLOPE_CASE(EBS_ACT_RELU) EBS_SLOPE_CASE(EBS_ACT_GELU) EBS_SLOPE_CASE(EBS_ACT_GELU_TANH) EBS_SLOPE_CASE(EBS_ACT_SILU)
+#undef EBS_SLOPE_CASE
+                    default: break;
+                }
 #pragma unroll
-                        for (int e = 0; e < N; ++e) {
-                            v[e] = to_f32(reinterpret_cast<const T*>(&a[u])[e]);
-                            zv[e] = g.act ? to_f32(reinterpret_cast<const T*>(&b[u])[e]) : 0.0f;
-                        }
-                        finish(r + 8 * u, v, zv);
-                    }
+                for (int e = 0; e < N; ++e) {
+                    sum[e] += v[e];
+                    if (sizeof(T) == 4) top[e] = max(top[e], magnitude(v[e]));
+                    if (std::is_same<T, __half>::value) v[e] *= g.store;
+                }
+                if (!g.dz) continue;
+                T* to = dz + (r + 8 * u) * g.lddz;
+                if (VEC) store_pack(to + local(0), v);        // (rows of dz are padded to whole packs)
+                else
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (local(e) < left) to[local(e)] = from_f32<T>(v[e]);
             }
         }
-    } else if (col < g.n) {
-#pragma unroll 4
-        for (long long r = r0 + y; r < r1; r += 8) {
-            float v[N], zv[N];
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                v[e] = col + e < g.n ? to_f32(dy[r * g.ldy + col + e]) : 0.0f;
-                zv[e] = g.act && col + e < g.n ? to_f32(z[r * g.ldz + col + e]) : 0.0f;
-            }
-            finish(r, v, zv);
-        }
-    }
     if (sizeof(T) == 4 && g.tops) {
-        if (N == 4) tops_of_block(top, part, g.tops + (size_t)by * g.n + bx * 128, bx * 128, g.n);
-        else {
-            part[y][lane] = top[0];
-            __syncthreads();
-            if (y == 0 && col < g.n) {
-                unsigned t = 0u;
-                for (int q = 0; q < 8; ++q) t = max(t, part[q][lane]);
-                g.tops[(size_t)by * g.n + col] = t;
-            }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[y][local(e) & 127] = top[e];
+        __syncthreads();
+        if (threadIdx.x < 128 && (int)threadIdx.x < left) {
+            unsigned t = 0u;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) t = max(t, part[q][threadIdx.x]);
+            g.tops[(size_t)by * g.n + col0 + threadIdx.x] = t;
         }
     }
     if (!g.dbias) return;
 #pragma unroll
-    for (int e = 0; e < N; ++e) sums[y][lane * N + e] = sum[e];
+    for (int e = 0; e < N; ++e) sums[y][local(e)] = sum[e];
     __syncthreads();
-    for (int i = threadIdx.x; i < 32 * N; i += 256) {
-        const int c = bx * 32 * N + i;
-        if (c >= g.n) break;
+    for (int i = threadIdx.x; i < 32 * N && i < left; i += 256) {
         float s = 0.0f;
 #pragma unroll
         for (int q = 0; q < 8; ++q) s += sums[q][i];
-        if (g.chunks == 1) static_cast<T*>(g.dbias)[c] = from_f32<T>(s);
-        else g.part[(size_t)by * g.n + c] = s;
+        if (g.chunks == 1) static_cast<T*>(g.dbias)[col0 + i] = from_f32<T>(s);
+        else g.part[(size_t)by * g.n + col0 + i] = s;
     }
 }
 // dbias from the chunks' sums, 32 columns a block, its eight warps take every eighth chunk; behind those blocks the column tops of the jobs,
@@ -511,9 +505,8 @@ __global__ void __launch_bounds__(256) linear_chunks_kernel(const float* __restr
 template <typename T>
 static int launch_dz(DzArgs& g, SplitJobs& jobs, cudaStream_t st) {
     constexpr int N = Pack<T>::N;
-    const bool packs = g.ldy % N == 0 && (!g.act || g.ldz % N == 0);
-    const int per = packs ? 32 * N : 32;
-    g.blocks = g.dz || g.dbias || g.tops ? (unsigned)((g.n + per - 1) / per * g.chunks) : 0u;
+    const bool vec = g.ldy % N == 0 && (!g.act || g.ldz % N == 0);
+    g.blocks = g.dz || g.dbias || g.tops ? (unsigned)((g.n + 32 * N - 1) / (32 * N) * g.chunks) : 0u;
     SplitJobs tops = {};
     unsigned blocks = g.blocks;
     for (int i = 0; i < jobs.count; ++i) {
@@ -523,7 +516,7 @@ static int launch_dz(DzArgs& g, SplitJobs& jobs, cudaStream_t st) {
         blocks += jobs.job[i].blocks;
     }
     int rc = EBS_OK;
-    if (blocks) rc = launch_chained(packs ? linear_dz_kernel<T, N> : linear_dz_kernel<T, 1>, dim3(blocks), 256, 0, st, 1, g, tops);
+    if (blocks) rc = launch_chained(vec ? linear_dz_kernel<T, true> : linear_dz_kernel<T, false>, dim3(blocks), 256, 0, st, 1, g, tops);
     if (rc) return rc;
     const unsigned sums = g.dbias && g.chunks > 1 ? (unsigned)((g.n + 31) / 32) : 0u;
     SplitJobs chunked = {};
