@@ -5,7 +5,7 @@
 // (that one reads 128 bytes a clock, all there are).  Warp 16 of each block fetches by TMA, warp 17 of the even block issues, warps 0-15
 // of both take the sums of their 128 rows out of tensor memory (lanes 32 (w % 4), columns 64 (w / 4)) and write the results
 // through a patch of shared memory, so that neighbouring lanes write neighbouring bytes.  Two accumulators of 256 columns: the
-// MMAs of the next tile (split products: of the next GEMM_CHUNK stages, see gemm_tile.cu) run while one is taken out.
+// MMAs of the next tile (split products: of the next few stages, see gemm_tile.cu) run while one is taken out.
 #include "gemm_tile.cuh"
 
 namespace ebs {
@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     static_assert((2 * S + 12 + 2) * 8 <= PAIR_BARRIERS, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x & 1), pairs = (int)(gridDim.x >> 1);
-    const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK, chunk = PL == 2 ? GEMM_CHUNK : blocks;
+    const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK, chunk = PL == 2 ? g.chunk : blocks;
     const int tiles_m = (g.out_rows + 255) / 256, tiles_n = (g.out_cols + TN - 1) / TN, count = (g.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n) * g.batch * g.split;
 
     if (threadIdx.x == 0) {
@@ -400,15 +400,15 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                     if ((g.test_flags & 1) == 0) {                // (give-up test: nothing is ever issued)
                         const uint32_t d = tmem + (uint32_t)((c & 1) * TN), base = smem_u32(tiles) + s * STAGE;
                         const uint32_t ah = tile_desc_lo(base, g.a_mn), bh = tile_desc_lo(base + PL * PAIR_A, g.b_mn);
+                        if (PL == 2)                              // (the small products first: each MMA truncates at the size of what is there)
 #pragma unroll
-                        for (int k = 0; k < GEMM_BK / 16; ++k) {
-                            const uint32_t a = ah + k * a_step, b = bh + k * b_step;
-                            umma_f16_pair(leader, d, a, b, idesc, (in_chunk | k) != 0);
-                            if (PL == 2) {
-                                umma_f16_pair(leader, d, a, b + (B_HALF >> 4), idesc, 1u);
+                            for (int k = 0; k < GEMM_BK / 16; ++k) {
+                                const uint32_t a = ah + k * a_step, b = bh + k * b_step;
+                                umma_f16_pair(leader, d, a, b + (B_HALF >> 4), idesc, (in_chunk | k) != 0);
                                 umma_f16_pair(leader, d, a + (PAIR_A >> 4), b, idesc, 1u);
                             }
-                        }
+#pragma unroll
+                        for (int k = 0; k < GEMM_BK / 16; ++k) umma_f16_pair(leader, d, ah + k * a_step, bh + k * b_step, idesc, PL == 2 || (in_chunk | k) != 0);
                         umma_commit_both(leader, cluster_addr(&empty[s], 0), cluster_addr(&empty[s], 1));
                         if (last) umma_commit_both(leader, cluster_addr(&acc_full[c & 1], 0), cluster_addr(&acc_full[c & 1], 1));
                     }
@@ -620,6 +620,7 @@ static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmSha
     g.a_mn = A.mn_major;
     g.b_mn = B.mn_major;
     g.bf16 = bf16;
+    g.chunk = s.chunk;
     g.wait_limit = device_wait_limit();
     g.test_flags = device_test_flags();
     const long long side = (s.rows + 255) / 256, tiles = (symmetric ? side * (side + 1) / 2 : side * ((s.cols + TN - 1) / TN)) * s.batch * split;

@@ -1,4 +1,4 @@
-// Products with a few rows: y = x W^T for up to eight rows of x, bound by the bytes of W.
+// Products with a few rows: y = x W^T for one row of x of 16-bit values, or up to four of fp32, bound by the bytes of W.
 //
 // A warp takes R rows of W over the whole reduction; its lanes run along them with 16-byte loads, the next ones on their way while these are
 // multiplied.  x comes from the first-level cache (it is the same for every warp); sums are fp32 multiply-adds: a weight is used once per row
@@ -127,9 +127,11 @@ static int launch_rows(const void* x, long long ldx, const void* w, long long ld
 template <typename T>
 static int launch_rows_typed(const void* x, long long ldx, const void* w, long long ldw, int m, int n, int k, const GemmOut& o, cudaStream_t st) {
     if (m == 1) return launch_rows<T, 1>(x, ldx, w, ldw, m, n, k, o, st);
-    if (m == 2) return launch_rows<T, 2>(x, ldx, w, ldw, m, n, k, o, st);
-    if (m <= 4) return launch_rows<T, 4>(x, ldx, w, ldw, m, n, k, o, st);
-    return launch_rows<T, 8>(x, ldx, w, ldw, m, n, k, o, st);
+    if constexpr (sizeof(T) == 4) {
+        if (m == 2) return launch_rows<T, 2>(x, ldx, w, ldw, m, n, k, o, st);
+        if (m <= 4) return launch_rows<T, 4>(x, ldx, w, ldw, m, n, k, o, st);
+    }
+    return EBS_ERR_UNSUPPORTED;                                   // (the caller asks for no other)
 }
 int launch_gemm_rows(const void* x, long long ldx, const void* w, long long ldw, int m, int n, int k, const GemmOut& o, int dtype, cudaStream_t st) {
     if (dtype == EBS_F32) return launch_rows_typed<float>(x, ldx, w, ldw, m, n, k, o, st);

@@ -3,7 +3,7 @@
 //
 // Warp 8 fetches operand tiles by TMA, warp 9 issues the MMAs, warps 0-7 take the sums out of tensor memory.
 //  - Split products (PL = 2: operands as two fp16 planes hi + lo): three MMAs a step, hi*hi + hi*lo + lo*hi.  The tensor core
-//    truncates when it adds to an accumulator, so that long sums drift by their length; every GEMM_CHUNK stages the accumulator
+//    truncates when it adds to an accumulator, so that long sums drift by their length; every few (GemmShape::chunk) stages the accumulator
 //    is therefore taken out and added up in registers, rounded to nearest, while the MMAs go on in a second one.
 //  - Few result rows (SWAP): the operand with many rows takes the 128 lanes, the few rows the N side of the MMA.  Such products
 //    are bound by the bytes of the large operand.
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK;
     const int kb0 = (int)((long long)blocks * part / split), kb1 = (int)((long long)blocks * (part + 1) / split);
     const int nkb = kb1 - kb0;
-    const int chunk = PL == 2 ? GEMM_CHUNK : (nkb > 0 ? nkb : 1);
+    const int chunk = PL == 2 ? g.chunk : (nkb > 0 ? nkb : 1);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < g.stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
@@ -132,15 +132,15 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
             const uint32_t d = tmem + (PL == 2 ? (uint32_t)((c & 1) * TN) : 0u);
             const uint32_t base = smem_u32(tiles) + s * STAGE;
             const uint32_t ah = tile_desc_lo(base, g.a_mn), bh = tile_desc_lo(base + PL * A_BYTES, g.b_mn);
+            if (PL == 2)                                          // (the small products first: each MMA truncates at the size of what is there)
 #pragma unroll
-            for (int k = 0; k < GEMM_BK / 16; ++k) {
-                const uint32_t a = ah + k * a_step, b = bh + k * b_step;
-                umma_f16(leader, d, a, b, idesc, (in_chunk | k) != 0);
-                if (PL == 2) {
-                    umma_f16(leader, d, a, b + (B_BYTES >> 4), idesc, 1u);
+                for (int k = 0; k < GEMM_BK / 16; ++k) {
+                    const uint32_t a = ah + k * a_step, b = bh + k * b_step;
+                    umma_f16(leader, d, a, b + (B_BYTES >> 4), idesc, (in_chunk | k) != 0);
                     umma_f16(leader, d, a + (A_BYTES >> 4), b, idesc, 1u);
                 }
-            }
+#pragma unroll
+            for (int k = 0; k < GEMM_BK / 16; ++k) umma_f16(leader, d, ah + k * a_step, bh + k * b_step, idesc, PL == 2 || (in_chunk | k) != 0);
             umma_commit_pred(leader, &empty[s]);
             if (in_chunk == chunk - 1 || i == nkb - 1) umma_commit_pred(leader, &acc_full[c & 1]);
         }
@@ -305,6 +305,7 @@ static int tile_product(TileLaunch<EPI>* l, int which, const GemmOperand& A, con
     g.a_mn = la.mn_major;
     g.b_mn = lb.mn_major;
     g.bf16 = bf16;
+    g.chunk = s.chunk;
     g.packs = packs;
     g.wait_limit = device_wait_limit();
     g.test_flags = device_test_flags();

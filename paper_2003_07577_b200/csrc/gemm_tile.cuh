@@ -5,12 +5,10 @@
 
 namespace ebs {
 
-constexpr int GEMM_CHUNK = 4;                 // stages (of 64 reduction elements) summed in the tensor core at a time, split products
-
 struct TileArgs {
     int red, out_rows, out_cols, batch;
     int tiles_a, tiles_b, blocks, split, stages;      // tile kernel: tiles along the lanes and the columns, thread blocks
-    int a_mn, b_mn, bf16, packs, symmetric;
+    int a_mn, b_mn, bf16, packs, symmetric, chunk;
     unsigned wait_limit;
     int test_flags;
 };
@@ -39,8 +37,7 @@ int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape
 int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmRoute& r, float* scratch, const FinalOut& out, int dtype, cudaStream_t st);
 unsigned long long gemm_pair_timeouts();
 
-// y = x W^T for up to GEMM_ROWS rows of x, all operands as they are.
-constexpr int GEMM_ROWS = 8;
+// y = x W^T for one row of x of 16-bit values, or up to four of fp32; all operands as they are.
 int launch_gemm_rows(const void* x, long long ldx, const void* w, long long ldw, int m, int n, int k, const GemmOut& o, int dtype, cudaStream_t st);
 
 // scratch: gemm_route(s, planes).scratch bytes.

@@ -119,10 +119,13 @@ bool encode_map(CUtensorMap* map, CUtensorMapDataType type, const void* p, const
 // False: the driver has no tensor maps, or refused this one.
 bool gemm_operand_map(const GemmOperand& o, int mn, int red, int batch, int box_mn, bool bf16, CUtensorMap* map);
 
+constexpr int GEMM_CHUNK = 4;              // stages of 64 reduction elements
+
 // Shape of a product D = A B over `red`; D has `rows` x `cols` (row-major results) as the caller sees them.
 struct GemmShape {
     int rows, cols, red, batch;
     bool symmetric = false;                // the result is known to be symmetric: one half of it need not be summed
+    int chunk = GEMM_CHUNK;                // stages summed in the tensor core at a time, split products
 };
 
 int gemm_sm_count();

@@ -143,13 +143,22 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const T* 
     for (int step = 0; step < p.steps && ok; ++step) {
         if (issues) {
             const uint32_t leader = elect_one() ? 1u : 0u;
-            for (int b = 0; b < p.blocks; ++b) {
-                const uint32_t d = uni(tmem + (uint32_t)((b >> 2) * mp)), h = uni(small_desc(smem_u32(xh) + b * plane, 16)), l = uni(small_desc(smem_u32(xl) + b * plane, 16));
+            // (of each sum the small products first: an MMA truncates at the size of what is there)
+            for (int b0 = 0; b0 < p.blocks; b0 += 4) {
+                const uint32_t d = uni(tmem + (uint32_t)((b0 >> 2) * mp));
+                const int b1 = b0 + 4 < p.blocks ? b0 + 4 : p.blocks;
+                for (int b = b0; b < b1; ++b) {
+                    const uint32_t h = uni(small_desc(smem_u32(xh) + b * plane, 16)), l = uni(small_desc(smem_u32(xl) + b * plane, 16));
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    umma_f16(leader, d, h + 2 * k, h + 2 * k, idesc_sym, ((b & 3) | k) != 0);
-                    umma_f16(leader, d, h + 2 * k, l + 2 * k, idesc_sym, 1u);
-                    umma_f16(leader, d, l + 2 * k, h + 2 * k, idesc_sym, 1u);
+                    for (int k = 0; k < 4; ++k) {
+                        umma_f16(leader, d, h + 2 * k, l + 2 * k, idesc_sym, ((b - b0) | k) != 0);
+                        umma_f16(leader, d, l + 2 * k, h + 2 * k, idesc_sym, 1u);
+                    }
+                }
+                for (int b = b0; b < b1; ++b) {
+                    const uint32_t h = uni(small_desc(smem_u32(xh) + b * plane, 16));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) umma_f16(leader, d, h + 2 * k, h + 2 * k, idesc_sym, 1u);
                 }
             }
             umma_commit_pred(leader, &done[0]);
@@ -189,9 +198,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const T* 
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (k >= k_steps) break;
-                umma_f16(leader, tmem + SMALL_Q_COL, a_h + 2 * k, l_h + 2 * k, idesc_sym, k != 0);
-                umma_f16(leader, tmem + SMALL_Q_COL, a_h + 2 * k, l_l + 2 * k, idesc_sym, 1u);
+                umma_f16(leader, tmem + SMALL_Q_COL, a_h + 2 * k, l_l + 2 * k, idesc_sym, k != 0);
                 umma_f16(leader, tmem + SMALL_Q_COL, a_l + 2 * k, l_h + 2 * k, idesc_sym, 1u);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (k >= k_steps) break;
+                umma_f16(leader, tmem + SMALL_Q_COL, a_h + 2 * k, l_h + 2 * k, idesc_sym, 1u);
             }
             umma_commit_pred(leader, &done[1]);
         }
@@ -225,9 +238,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const T* 
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {                     // 16 rows of a block: 2048 bytes
                     if (k >= k_steps) break;
-                    umma_f16(leader, d, q_h + 2 * k, h + 128 * k, idesc_x, k != 0);
-                    umma_f16(leader, d, q_l + 2 * k, h + 128 * k, idesc_x, 1u);
+                    umma_f16(leader, d, q_l + 2 * k, h + 128 * k, idesc_x, k != 0);
                     umma_f16(leader, d, q_h + 2 * k, l + 128 * k, idesc_x, 1u);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k >= k_steps) break;
+                    umma_f16(leader, d, q_h + 2 * k, h + 128 * k, idesc_x, 1u);
                 }
                 umma_commit_pred(leader, &done[2 + place]);
             }
