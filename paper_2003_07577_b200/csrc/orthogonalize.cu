@@ -208,6 +208,9 @@ int ebs_orthogonalize(const void* g, int batch, int rows, int cols, int dtype, i
         f.square[i] = ldexpf(1.0f, eq - ea - el);
         f.square_diag[i] = coeff[0] * ldexpf(1.0f, eq);
         f.next[i] = ldexpf(1.0f, en - eq - ex);
+        // (Q's bound is that of a quadratic polynomial, whose terms are at most a few times it: neither product leaves fp32's range)
+        f.quadratic[i] = (float)ldexp((double)coeff[2], eq - 2 * ea);
+        f.direct[i] = (float)ldexp((double)coeff[1], eq - ea);
         last = scale * ldexpf(1.0f, -eq - ex);
         ex = en;
         bound = b.next;

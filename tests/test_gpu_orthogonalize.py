@@ -177,3 +177,46 @@ def test_large(ebs, dtype, rows, cols):
     """Symmetric products on and below the diagonal with their mirror images; a reduction in parts."""
     g = make(1, rows, cols, TYPES[dtype], 1)
     check(run(ebs, g), iterate64(g, 5), 5)
+
+
+# one to eight blocks of a cluster: short sides up to 64 and up to 128, fewer and more columns than they hold, more matrices than run at once
+CLUSTERED = [(1, 65, 65), (1, 100, 300), (2, 128, 1152), (1, 1152, 128), (1, 127, 1537), (1, 128, 1600), (1, 2048, 80), (1, 80, 2049), (3, 96, 96), (1, 112, 129), (20, 66, 513),
+             (40, 128, 640), (1, 64, 4096), (1, 4097, 64), (1, 9, 4095), (18, 64, 576), (37, 64, 576), (75, 48, 200), (150, 64, 130)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("batch,rows,cols", CLUSTERED)
+def test_clusters(ebs, batch, rows, cols, dtype):
+    g = make(batch, rows, cols, TYPES[dtype], rows + cols)
+    check(run(ebs, g), iterate64(g, 5), 5)
+
+
+@pytest.mark.parametrize("shape", [(2, 128, 1152), (1, 300, 96), (9, 100, 640), (2, 64, 2000)])
+def test_clusters_give_up_in_place_and_replay(ebs, shape):
+    g = make(*shape, torch.float32, 8)
+    want = run(ebs, g)
+    same = g.clone()
+    run(ebs, same, out=same)
+    assert torch.equal(same, want)
+    ebs.ebs_test_set_device_wait(64, 1)
+    try:
+        run(ebs, g)
+        torch.cuda.synchronize()
+    finally:
+        ebs.ebs_test_set_device_wait(0, 0)
+    assert ebs.ebs_check_device_status() == ebs.EBS_ERR_TIMEOUT
+    out, ws = torch.empty_like(g), torch.zeros(ebs.ebs_orthogonalize_workspace_bytes(*shape, ebs.EBS_F32, 5), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(ebs, g, out=out, ws=ws)
+        run(ebs, out, out=out, ws=ws)
+    graph.replay()
+    assert torch.equal(out, run(ebs, want))
+
+
+@pytest.mark.parametrize("steps", [0, 1, 9])
+@pytest.mark.parametrize("shape", [(2, 90, 700), (1, 900, 128), (3, 30, 400)])
+def test_clusters_steps(ebs, shape, steps):
+    for coeff in ((1.5, -0.5, 0.0), COEFF):
+        g = make(*shape, torch.float32, 9)
+        check(run(ebs, g, steps=steps, coeff=coeff, scale=0.7), iterate64(g, steps, coeff, scale=0.7), steps, coeff, 0.7)
