@@ -361,9 +361,9 @@ int ebs_search_act_forward(const float *x_dev, size_t n, float alpha, const int 
  *   backward   dz = dy * act'(z)         dy, z [m][n] (z: what the forward call kept; unused without an activation)
  *              dx = dz W,  dW = dz^T x,  dbias = sum over the rows of dz        (residual's gradient is dy itself)
  *
- * All tensors have the element type `dtype` (EBS_F32, EBS_F16 or EBS_BF16); products are summed in fp32 (EBS_F32: from
- * operands kept to 22 bits), activation and residual are applied to the fp32 sums, and each output
- * is rounded once.  The backward call of a 16-bit type with an activation rounds dz to that type before the products,
+ * All tensors have the element type `dtype` (EBS_F32, EBS_F16 or EBS_BF16); products are summed in fp32, activation and
+ * residual are applied to the fp32 sums, and each output is rounded once.  EBS_F32: an operand is kept to 22 bits, or to
+ * 2^-40 of the largest magnitude that it has in the same sum, whichever is coarser (up to four rows forward: to all 24).  The backward call of a 16-bit type with an activation rounds dz to that type before the products,
  * not before the sum that gives dbias.
  *   EBS_ACT_RELU       z > 0 ? z : 0 (NaN gives 0, as in the convolution's epilogue); slope 1 where z > 0, else 0
  *   EBS_ACT_GELU       z/2 (1 + erf(z / sqrt 2))
@@ -376,7 +376,8 @@ int ebs_search_act_forward(const float *x_dev, size_t n, float alpha, const int 
  * 16-byte aligned, the strides need not be (strides whose rows all start on 16 bytes save a copy of that operand).
  * m = 0 is an empty batch: nothing is read, dW and dbias become zero.  No output may overlap another tensor of the call,
  * except that y may be the residual itself (same address and stride).
- * Results do not depend on anything but the arguments: sums are taken in a fixed order.
+ * Results do not depend on anything but the arguments: sums are taken in a fixed order, which goes by the sizes (a row's
+ * last bits may differ with the number of rows beside it).
  *
  * workspace_dev: ebs_linear_workspace_bytes(desc, backward) bytes of device memory (0 bytes: may be NULL).  A call leaves
  * nothing in it that another one reads; two calls whose GPU work overlaps need one each.
@@ -413,11 +414,12 @@ int ebs_linear_backward(const void *dy_dev, const void *x_dev, const void *w_dev
  *   out = scale * X
  * The iteration acts on the singular values alone, s <- a s + b s^3 + c s^5: with the coefficients 3.4445, -4.7750,
  * 2.0315 all but the smallest end in about 0.7 .. 1.2.  A zero matrix gives zero (eps > 0); a matrix with a NaN or an
- * infinity gives NaN throughout.  |G|_F is summed in 64 bits.  The products are summed in fp32 from operands kept to 22
+ * infinity gives NaN throughout (no steps: as the formula has it).  |G|_F is summed in 64 bits.  The products are summed in fp32 from operands kept to 22
  * bits, for every type: a steep polynomial multiplies early roundings by up to a^steps.
  * dtype (EBS_F32, EBS_F16, EBS_BF16) is the type of G and out.  steps 0 .. 64, coefficients and scale finite, eps >= 0;
  * EBS_ERR_UNSUPPORTED if the singular values could leave 2^-20 .. 2^20 under these coefficients.  coeff is a HOST array of
- * three floats.  out may be G itself, and may not overlap it otherwise; workspace_dev as above.
+ * three floats.  out may be G itself, and may not overlap it otherwise; workspace_dev as above.  The order of sums goes by
+ * the sizes: a matrix's last bits may differ with the number of matrices beside it.
  */
 size_t ebs_orthogonalize_workspace_bytes(int batch, int rows, int cols, int dtype, int steps);
 int ebs_orthogonalize(const void *g_dev, int batch, int rows, int cols, int dtype, int steps, const float *coeff, float eps,
