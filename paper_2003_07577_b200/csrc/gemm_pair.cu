@@ -282,8 +282,14 @@ __device__ __forceinline__ void umma_commit_both(uint32_t leader, uint32_t bar0,
         ::"r"(bar0), "r"(bar1), "r"(leader) : "memory");
 }
 // Tiles in bands of eight tile rows, column by column within a band: the tiles under way at a time share few rows and columns.
-// A symmetric result: only the tiles on and below the diagonal, row by row.
+// A symmetric result: only the tiles of the 256 x 256 squares on and below the diagonal, row by row.
 // Parts of the reduction of one tile follow one another.
+template <int TN>
+__host__ __device__ __forceinline__ int symmetric_tiles(int tiles_m, int tiles_n) {
+    constexpr int Q = 256 / TN;
+    return tiles_m * (tiles_m + 1) / 2 * Q - (tiles_m * Q - tiles_n);      // (the last square's second half need not exist)
+}
+template <int TN>
 __device__ __forceinline__ void pair_tile(int t, int tiles_m, int tiles_n, int symmetric, int split, int blocks, int& batch, int& tm, int& tn, int& part, int& kb0, int& kb1) {
     part = 0;
     if (split > 1) {
@@ -292,14 +298,16 @@ __device__ __forceinline__ void pair_tile(int t, int tiles_m, int tiles_n, int s
     }
     kb0 = (int)((long long)blocks * part / split);
     kb1 = (int)((long long)blocks * (part + 1) / split);
-    const int per = symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n;
+    const int per = symmetric ? symmetric_tiles<TN>(tiles_m, tiles_n) : tiles_m * tiles_n;
     batch = t / per;
     t -= batch * per;
     if (symmetric) {
-        tm = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
-        while (tm * (tm + 1) / 2 > t) --tm;
-        while ((tm + 1) * (tm + 2) / 2 <= t) ++tm;
-        tn = t - tm * (tm + 1) / 2;
+        constexpr int Q = 256 / TN;
+        const int square = t / Q;
+        tm = (int)((sqrtf(8.0f * square + 1.0f) - 1.0f) * 0.5f);
+        while (tm * (tm + 1) / 2 > square) --tm;
+        while ((tm + 1) * (tm + 2) / 2 <= square) ++tm;
+        tn = (square - tm * (tm + 1) / 2) * Q + t % Q;
         return;
     }
     const int band = t / (8 * tiles_n), first = band * 8, height = tiles_m - first < 8 ? tiles_m - first : 8;
@@ -325,7 +333,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x & 1), pairs = (int)(gridDim.x >> 1);
     const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK, chunk = PL == 2 ? g.chunk : blocks;
-    const int tiles_m = (g.out_rows + 255) / 256, tiles_n = (g.out_cols + TN - 1) / TN, count = (g.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n) * g.batch * g.split;
+    const int tiles_m = (g.out_rows + 255) / 256, tiles_n = (g.out_cols + TN - 1) / TN, count = (g.symmetric ? symmetric_tiles<TN>(tiles_m, tiles_n) : tiles_m * tiles_n) * g.batch * g.split;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
@@ -357,7 +365,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
         bool ok = true;
         for (int t = (int)(blockIdx.x >> 1); t < count && ok; t += pairs) {
             int batch, tm, tn, part, kb0, kb1;
-            pair_tile(t, tiles_m, tiles_n, g.symmetric, g.split, blocks, batch, tm, tn, part, kb0, kb1);
+            pair_tile<TN>(t, tiles_m, tiles_n, g.symmetric, g.split, blocks, batch, tm, tn, part, kb0, kb1);
             const int a0 = tm * 256 + rank * 128, b0 = tn * TN + rank * (TN / 2);
             for (int kb = kb0; kb < kb1; ++kb, ++i) {
                 const int s = i % S, k = kb * GEMM_BK;
@@ -389,7 +397,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
             bool ok = true;
             for (int t = (int)(blockIdx.x >> 1); t < count && ok; t += pairs) {
                 int batch, tm, tn, part, kb0, kb1;
-                pair_tile(t, tiles_m, tiles_n, g.symmetric, g.split, blocks, batch, tm, tn, part, kb0, kb1);
+                pair_tile<TN>(t, tiles_m, tiles_n, g.symmetric, g.split, blocks, batch, tm, tn, part, kb0, kb1);
                 for (int kb = kb0; kb < kb1 && ok; ++kb, ++i) {
                     const int s = i % S, in_chunk = (kb - kb0) % chunk;
                     if (in_chunk == 0 && c >= 2) ok = mbar_wait_cluster_warp(&acc_empty[c & 1], ((c >> 1) & 1) ^ 1, &abort_flag, g.wait_limit);
@@ -428,7 +436,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
         bool ok = true;
         for (int t = (int)(blockIdx.x >> 1); t < count && ok; t += pairs, ++done) {
             int batch, tm, tn, part, kb0, kb1;
-            pair_tile(t, tiles_m, tiles_n, g.symmetric, g.split, blocks, batch, tm, tn, part, kb0, kb1);
+            pair_tile<TN>(t, tiles_m, tiles_n, g.symmetric, g.split, blocks, batch, tm, tn, part, kb0, kb1);
             const int row0 = tm * 256 + rank * 128 + (warp & 3) * 32, col0 = tn * TN + (warp >> 2) * CQ;
             const int slice = part * g.batch + batch;             // (parts: a matrix each)
             // rows by TMA
@@ -451,7 +459,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
             };
             auto rows_out = [&](int column, float (&v)[CW]) {
                 const int col = col0 + column;
-                Rows::finish(epi, &map_y, &map_z, ring, v, terms + column, CQ, g.symmetric && tm != tn, g.out_rows, slice, row0, col, g.out_cols - col, row_term, row_ahead,
+                Rows::finish(epi, &map_y, &map_z, ring, v, terms + column, CQ, g.symmetric && tn / (256 / TN) != tm, g.out_rows, slice, row0, col, g.out_cols - col, row_term, row_ahead,
                              col < g.out_cols && row0 < g.out_rows);
             };
             // Outputs whose rows start anywhere, 16 columns at a time: through the warp's buffer, then two rows an access, neighbouring lanes
@@ -609,7 +617,7 @@ static bool result_maps(const PartialOut& e, const GemmShape& s, CUtensorMap* y,
 
 template <class EPI, int PL, int TN>
 static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, int split, cudaStream_t st) {
-    const bool symmetric = s.symmetric && TN == 256 && std::is_same<EPI, PlanesOut>::value;
+    const bool symmetric = s.symmetric && std::is_same<EPI, PlanesOut>::value;
     TileArgs g = {};
     g.red = s.red;
     g.out_rows = s.rows;
@@ -623,7 +631,7 @@ static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmSha
     g.chunk = s.chunk;
     g.wait_limit = device_wait_limit();
     g.test_flags = device_test_flags();
-    const long long side = (s.rows + 255) / 256, tiles = (symmetric ? side * (side + 1) / 2 : side * ((s.cols + TN - 1) / TN)) * s.batch * split;
+    const long long side = (s.rows + 255) / 256, across = (s.cols + TN - 1) / TN, tiles = (symmetric ? side * (side + 1) / 2 * (256 / TN) - (side * (256 / TN) - across) : side * across) * s.batch * split;
     if (tiles >= (1LL << 30)) return EBS_ERR_OVERFLOW;
     CUtensorMap a, b, y{}, z{};
     if (!gemm_operand_map(A, s.rows, s.red, s.batch, 128, bf16, &a) || !gemm_operand_map(B, s.cols, s.red, s.batch, TN / 2, bf16, &b)) return EBS_ERR_CUDA;
@@ -710,13 +718,18 @@ GemmRoute gemm_route(const GemmShape& s, int planes) {
     const long long side = (s.rows + 255) / 256, wide = (s.symmetric ? side * (side + 1) / 2 : side * ((s.cols + 255) / 256)) * s.batch;
     const long long narrow = side * ((s.cols + 127) / 128) * s.batch;
     const int blocks = (s.red + GEMM_BK - 1) / GEMM_BK;
-    r.pair = s.rows > 128 && s.cols > 128 && wide >= 32;
+    // (a symmetric result by half pays from fewer tiles on, where the tile kernel's whole one is more than a round)
+    const long long whole = (long long)((s.rows + 127) / 128) * ((s.cols + 127) / 128) * s.batch;
+    r.pair = s.rows > 128 && s.cols > 128 && (wide >= 32 || (s.symmetric && wide >= 20 && whole > 148));
     if (r.pair) {
         // Split products on tiles of 128 columns where 256 leave pairs idle (us with 256 and 128: 512 x 4608 over 512 23.3 and 13.9, 12544 x 256 over
         // 1152 33.5 and 30.2, 2048 x 2048 over 2048 48.0 and 43.4) or the reduction is short and the last round fuller (12544 x 1152 over 256
         // 37.1 and 33.2; 4096 x 4096 over 1024 78.4 and 81.4).  16-bit operands never: half the work per byte fetched (8192 x 4096 over 512 36.7
         // and 55.4).
         const long long w = (wide + 73) / 74 * 2, n = (narrow + 73) / 74;
+        // Symmetric ones where 256 leave half the pairs idle (an orthogonalisation of 2048 x 2048 739 and 480 us; three rounds of 128 instead of two of
+        // 256 do not pay: 3300 x 3300 2348 and 2467 us).
+        if (planes == 2 && s.symmetric && wide <= 37) r.tn = 128;
         if (planes == 2 && !s.symmetric && (wide <= 74 || (blocks <= 8 && n < w))) r.tn = 128;
     } else if (s.rows > 128 && s.cols > 128 && blocks >= 64) {
         const long long all = side * ((s.cols + 255) / 256) * s.batch;

@@ -273,14 +273,14 @@ static TileForm tile_form(const GemmShape& s, bool a_mn, int planes, long long t
     const int lanes = f.swap ? s.cols : s.rows, columns = f.swap ? s.rows : s.cols, sms = gemm_sm_count();
     const long long tiles = (long long)((lanes + 127) / 128) * ((columns + f.tn - 1) / f.tn) * s.batch;
     const int blocks = (s.red + GEMM_BK - 1) / GEMM_BK;
-    // Parts of the reduction (us, measured): a stage takes 0.32 (split products 0.9), two, four or eight parts 1.2, 1.6 and 2.4 to meet; eight
-    // parts of more than half the GPU's tiles no longer run at once.
+    // Parts of the reduction (us, measured): a stage takes 0.32 (split products 0.9), two, four or eight parts 1.2, 1.6 and 2.4 to meet; and
+    // clusters of eight and four fill only part of the GPU (36 of four no longer run at once: 768 x 768 orthogonalised in 321 us on 36, 202 on clusters of two).
     static const float meet[4] = {0.0f, 1.2f, 1.6f, 2.4f};
     f.split = 1;
     float best = 0.0f;
     for (int i = 0; i < 4; ++i) {
         const int parts = 1 << i;
-        if (i > 0 && (tiles * parts + tiles_beside > (i == 3 ? sms * 3 / 4 : sms) || blocks < parts)) break;
+        if (i > 0 && (tiles * parts + tiles_beside > (i == 3 ? sms * 3 / 4 : i == 2 ? sms * 7 / 8 : sms) || blocks < parts)) break;
         const float t = (planes == 2 ? 0.9f : 0.32f) * (float)((blocks + parts - 1) / parts) + meet[i];
         if (i == 0 || t < best) { best = t; f.split = parts; }
     }

@@ -220,3 +220,21 @@ def test_clusters_steps(ebs, shape, steps):
     for coeff in ((1.5, -0.5, 0.0), COEFF):
         g = make(*shape, torch.float32, 9)
         check(run(ebs, g, steps=steps, coeff=coeff, scale=0.7), iterate64(g, steps, coeff, scale=0.7), steps, coeff, 0.7)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 1921, 1950), (1, 1800, 1793), (1, 2048, 2049), (2, 1100, 1300), (1, 768, 770)])
+def test_symmetric_halves(ebs, dtype, shape):
+    """Symmetric products in squares of two tiles, the last square with one or two of them."""
+    g = make(*shape, TYPES[dtype], 2)
+    check(run(ebs, g), iterate64(g, 5), 5)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_nan_and_infinity_cross_a_cluster(ebs, bad):
+    g = make(3, 100, 640, torch.float32, 3)
+    clean = run(ebs, g)
+    g[1, 7, 639] = bad
+    out = run(ebs, g)
+    assert torch.isnan(out[1]).all()
+    assert torch.equal(out[0], clean[0]) and torch.equal(out[2], clean[2])
