@@ -366,27 +366,3 @@ def test_offsets_beyond_32_bits(ebs):
     run_forward(ebs, x, w, None, None, "bf16", "none", y)
     ref, s = x.double() @ w.double().T, x.double().abs() @ w.double().abs().T
     assert ((y.double() - ref).abs() <= bound(t, ref, s, k)).all()
-
-
-@pytest.mark.parametrize("m,n,k,skip", [(40, 200, 400, 1), (200, 300, 2000, 1), (200, 300, 2000, 2), (4096, 2048, 256, 1), (300, 264, 8200, 1)])
-@pytest.mark.parametrize("dtype", list(TYPES))
-def test_bounded_waits_give_up_and_recover(ebs, dtype, m, n, k, skip):
-    """Nothing is issued to the tensor core (skip 1), or one part of a split tile sends no sums (2): every wait runs out, the call returns, the
-    status says so once, and the next launch is right.  (One tile a part, a cluster a tile, a pair of blocks, a reduction in parts.)"""
-    t, g = TYPES[dtype], gen(11)
-    x, w = strided(m, k, k, t, g), strided(n, k, k, t, g, 1 / math.sqrt(k))
-    y, want = torch.empty((m, n), dtype=t, device="cuda"), torch.empty((m, n), dtype=t, device="cuda")
-    run_forward(ebs, x, w, None, None, dtype, "none", want)
-    assert ebs.ebs_check_device_status() == ebs.EBS_OK
-    before = ebs.ebs_device_wait_timeouts()
-    ebs.ebs_test_set_device_wait(64, skip)
-    try:
-        run_forward(ebs, x, w, None, None, dtype, "none", y)
-        torch.cuda.synchronize()
-    finally:
-        ebs.ebs_test_set_device_wait(0, 0)
-    assert ebs.ebs_device_wait_timeouts() > before
-    assert ebs.ebs_check_device_status() == ebs.EBS_ERR_TIMEOUT
-    assert ebs.ebs_check_device_status() == ebs.EBS_OK
-    run_forward(ebs, x, w, None, None, dtype, "none", y)
-    assert torch.equal(y, want)
