@@ -10,7 +10,7 @@ zero outside, the gradient of w_hat is that of w.  The update is momentum, ortho
 convolution takes this form on the matrix of its windows, a 1x1 convolution on its pixels.
 
 Buffers and call order only: the arithmetic is in the library's entry points (the clip mask and the momentum are element-wise
-torch operations).  Everything runs on the current stream, in buffers made once, so that a training step can be captured into a
+torch operations).  Everything runs on the weights' device and its current stream, in buffers made once, so that a training step can be captured into a
 CUDA graph and replayed; a second stream or thread needs an object of its own.
 """
 from __future__ import annotations
@@ -30,8 +30,8 @@ class SearchLinear:
 
     def __init__(self, weight: torch.Tensor, rows: int, bits: Sequence[int], coeff_w: Sequence[float], coeff_x: Sequence[float],
                  alpha: float, bias: Optional[torch.Tensor] = None, act: int = ebs.EBS_ACT_NONE, steps: int = 5):
-        if weight.dim() != 2:
-            raise ValueError("weight must be a matrix")
+        if weight.dim() != 2 or not weight.is_cuda or rows < 1:
+            raise ValueError("weight must be a matrix on a GPU, rows at least 1")
         n, k = weight.shape
         self._check("weight", weight, (n, k), weight.device)
         self._check("bias", bias, (n,), weight.device)
@@ -60,9 +60,10 @@ class SearchLinear:
         self._check("x", x, (self.rows, k), self.weight.device)
         self._check("residual", residual, (self.rows, n), self.weight.device)
         self.x = x
-        ebs.ebs_search_weight_forward(self.weight, self.bits, self.coeff_w, self.w_hat, self._scratch)
-        ebs.ebs_search_act_forward(x, self.alpha, self.bits, self.coeff_x, self.x_hat)
-        ebs.ebs_linear_forward(self.x_hat, self.w_hat, self.bias, residual, self.desc, self.y, self.z, self._workspace)
+        with torch.cuda.device(self.weight.device):
+            ebs.ebs_search_weight_forward(self.weight, self.bits, self.coeff_w, self.w_hat, self._scratch)
+            ebs.ebs_search_act_forward(x, self.alpha, self.bits, self.coeff_x, self.x_hat)
+            ebs.ebs_linear_forward(self.x_hat, self.w_hat, self.bias, residual, self.desc, self.y, self.z, self._workspace)
         return self.y
 
     def backward(self, dy: torch.Tensor) -> torch.Tensor:
@@ -71,14 +72,16 @@ class SearchLinear:
         if self.x is None:
             raise RuntimeError("backward() before forward()")
         self._check("dy", dy, (self.rows, self.weight.shape[0]), self.weight.device)
-        ebs.ebs_linear_backward(dy, self.x_hat, self.w_hat, self.z, self.desc, self.dx, self.dw, self.dbias, self._workspace)
+        with torch.cuda.device(self.weight.device):
+            ebs.ebs_linear_backward(dy, self.x_hat, self.w_hat, self.z, self.desc, self.dx, self.dw, self.dbias, self._workspace)
         return self.dx * ((self.x > 0) & (self.x < self.alpha))
 
     def step(self, rate: float, decay: float = 0.95) -> None:
         """w <- w - rate * orthogonalised(decay * momentum + dw); the bias takes a plain gradient step."""
         self.momentum.mul_(decay).add_(self.dw)
         n, k = self.weight.shape
-        ebs.ebs_orthogonalize(self.momentum, 1, n, k, ebs.EBS_F32, self.steps, COEFF, 1e-7, 1.0, self.update, self._workspace)
+        with torch.cuda.device(self.weight.device):
+            ebs.ebs_orthogonalize(self.momentum, 1, n, k, ebs.EBS_F32, self.steps, COEFF, 1e-7, 1.0, self.update, self._workspace)
         self.weight.sub_(self.update, alpha=rate)
         if self.bias is not None:
             self.bias.sub_(self.dbias, alpha=rate)

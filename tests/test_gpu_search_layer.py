@@ -106,6 +106,9 @@ def test_refusals(mods):
             layer.forward(bad)
     with pytest.raises(ValueError):
         layer.forward(x, x)
+    for weight, rows in ((torch.zeros((4, 8)), 2), (torch.zeros(8, device="cuda"), 2), (torch.zeros((4, 8), device="cuda"), 0)):
+        with pytest.raises(ValueError):
+            search.SearchLinear(weight, rows, [2], [1.0], [1.0], 1.0)
     with pytest.raises(ValueError):
         search.SearchLinear(torch.zeros((4, 8), dtype=torch.float64, device="cuda"), 2, [2], [1.0], [1.0], 1.0)
     layer.forward(x)
