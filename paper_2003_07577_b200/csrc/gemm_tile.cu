@@ -423,8 +423,16 @@ bool encode_map(CUtensorMap* map, CUtensorMapDataType type, const void* p, const
                    : nullptr;
     }();
     const cuuint32_t one[3] = {1, 1, 1};
-    return encode && encode(map, type, 3, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, narrow ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
-                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    if (!encode) return false;
+    for (int attempt = 0; attempt < 2; ++attempt) {
+        if (encode(map, type, 3, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, narrow ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS)
+            return true;
+        // a thread's first call: the driver wants a current context, which runtime calls make and this one does not
+        int dev = 0;
+        if (attempt || cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return false;
+    }
+    return false;
 }
 bool gemm_operand_map(const GemmOperand& o, int mn, int red, int batch, int box_mn, bool bf16, CUtensorMap* map) {
     const cuuint64_t inner = o.mn_major ? mn : red, outer = o.mn_major ? red : mn;

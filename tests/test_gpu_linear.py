@@ -7,6 +7,7 @@ and sums here are taken in blocks, so 2^-24 * (8 + sqrt(K)) * 4 * S is generous;
 a few 2^-24 of (1 + |z|).  The backward pass of a 16-bit type with an activation rounds dz first: u more of every product."""
 import math
 import os
+import threading
 
 import pytest
 import torch
@@ -366,3 +367,34 @@ def test_offsets_beyond_32_bits(ebs):
     run_forward(ebs, x, w, None, None, "bf16", "none", y)
     ref, s = x.double() @ w.double().T, x.double().abs() @ w.double().abs().T
     assert ((y.double() - ref).abs() <= bound(t, ref, s, k)).all()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("m,n,k", [(4096, 2048, 256), (40, 200, 400), (1, 300, 264)])
+def test_threads(ebs, dtype, m, n, k):
+    """Calls from threads that made no CUDA call before, at the same time on streams of their own."""
+    t, g = TYPES[dtype], gen(13)
+    x, w = strided(m, k, k, t, g), strided(n, k, k, t, g, 1 / math.sqrt(k))
+    want = torch.empty((m, n), dtype=t, device="cuda")
+    run_forward(ebs, x, w, None, None, dtype, "silu", want)
+    outs = [torch.zeros((m, n), dtype=t, device="cuda") for _ in range(4)]
+    d = ebs.linear_desc(m, n, k, *codes(ebs, dtype, "silu"))
+    spaces = [workspace(ebs, d, False) for _ in outs]
+    streams = [torch.cuda.Stream() for _ in outs]
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(i):
+        try:
+            for _ in range(20):
+                ebs.ebs_linear_forward(x, w, None, None, d, outs[i], None, spaces[i], streams[i])
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(outs))]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    torch.cuda.synchronize()
+    assert not errors and all(torch.equal(o, want) for o in outs)
