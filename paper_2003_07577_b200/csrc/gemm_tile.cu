@@ -265,24 +265,35 @@ struct TileForm {
     bool swap;
     int tn, split;
 };
-// tiles_beside: tiles of another product in the same launch.
-static TileForm tile_form(const GemmShape& s, bool a_mn, int planes, long long tiles_beside) {
+static long long tile_count(const GemmShape& s, const TileForm& f) {
+    const int lanes = f.swap ? s.cols : s.rows, columns = f.swap ? s.rows : s.cols;
+    return (long long)((lanes + 127) / 128) * ((columns + f.tn - 1) / f.tn) * s.batch;
+}
+// Parts of the reduction (us, measured): a stage takes 0.32 (split products 0.9), two, four or eight parts 1.2, 1.6 and 2.4 to meet.
+static float tile_time(const GemmShape& s, int planes, int log_parts) {
+    static const float meet[4] = {0.0f, 1.2f, 1.6f, 2.4f};
+    const int parts = 1 << log_parts, blocks = (s.red + GEMM_BK - 1) / GEMM_BK;
+    return (planes == 2 ? 0.9f : 0.32f) * (float)((blocks + parts - 1) / parts) + meet[log_parts];
+}
+// Thread blocks that run at once: clusters of eight and four fill only part of the GPU (36 of four no longer run at once: 768 x 768
+// orthogonalised in 321 us on 36, 202 on clusters of two).
+static int tile_blocks(int log_parts) {
+    const int sms = gemm_sm_count();
+    return log_parts == 3 ? sms * 3 / 4 : log_parts == 2 ? sms * 7 / 8 : sms;
+}
+static TileForm tile_form(const GemmShape& s, bool a_mn, int planes) {
     TileForm f;
     f.swap = s.rows <= 64 && !a_mn;
     f.tn = f.swap ? (s.rows <= 16 ? 16 : s.rows <= 32 ? 32 : 64) : (s.cols <= 64 ? 64 : 128);
-    const int lanes = f.swap ? s.cols : s.rows, columns = f.swap ? s.rows : s.cols, sms = gemm_sm_count();
-    const long long tiles = (long long)((lanes + 127) / 128) * ((columns + f.tn - 1) / f.tn) * s.batch;
+    const long long tiles = tile_count(s, f);
     const int blocks = (s.red + GEMM_BK - 1) / GEMM_BK;
-    // Parts of the reduction (us, measured): a stage takes 0.32 (split products 0.9), two, four or eight parts 1.2, 1.6 and 2.4 to meet; and
-    // clusters of eight and four fill only part of the GPU (36 of four no longer run at once: 768 x 768 orthogonalised in 321 us on 36, 202 on clusters of two).
-    static const float meet[4] = {0.0f, 1.2f, 1.6f, 2.4f};
     f.split = 1;
-    float best = 0.0f;
-    for (int i = 0; i < 4; ++i) {
+    float best = tile_time(s, planes, 0);
+    for (int i = 1; i < 4; ++i) {
         const int parts = 1 << i;
-        if (i > 0 && (tiles * parts + tiles_beside > (i == 3 ? sms * 3 / 4 : i == 2 ? sms * 7 / 8 : sms) || blocks < parts)) break;
-        const float t = (planes == 2 ? 0.9f : 0.32f) * (float)((blocks + parts - 1) / parts) + meet[i];
-        if (i == 0 || t < best) { best = t; f.split = parts; }
+        if (tiles * parts > tile_blocks(i) || blocks < parts) break;
+        const float t = tile_time(s, planes, i);
+        if (t < best) { best = t; f.split = parts; }
     }
     return f;
 }
@@ -353,7 +364,7 @@ static int launch_tile_form(TileLaunch<EPI>& l, unsigned blocks, const TileForm&
 template <class EPI, int PL>
 static int launch_one(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, bool packs, cudaStream_t st) {
     TileLaunch<EPI> l;
-    const TileForm f = tile_form(s, A.mn_major, PL, 0);
+    const TileForm f = tile_form(s, A.mn_major, PL);
     unsigned blocks = 0;
     const int rc = tile_product(&l, 0, A, B, s, epi, bf16, packs, f, &blocks);
     if (rc) return rc;
@@ -365,19 +376,36 @@ template <class EPI, int PL>
 static int launch_two(const TileTask (&t)[2], const EPI (&epi)[2], bool bf16, const bool (&packs)[2], cudaStream_t st) {
     // both in one launch where they have the same form
     TileForm f[2];
-    for (int i = 0; i < 2; ++i) {
-        const GemmShape& other = t[1 - i].s;
-        f[i] = tile_form(t[i].s, t[i].a.mn_major, PL, (long long)((other.rows + 127) / 128) * ((other.cols + 127) / 128));
-    }
+    for (int i = 0; i < 2; ++i) f[i] = tile_form(t[i].s, t[i].a.mn_major, PL);
     if (f[0].swap != f[1].swap || f[0].tn != f[1].tn) {
         const int rc = launch_one<EPI, PL>(t[0].a, t[0].b, t[0].s, epi[0], bf16, packs[0], st);
         return rc ? rc : launch_one<EPI, PL>(t[1].a, t[1].b, t[1].s, epi[1], bf16, packs[1], st);
     }
-    // a launch has one size of cluster: the other product takes as many parts, or one
-    const int cluster = f[0].split > f[1].split ? f[0].split : f[1].split;
-    for (TileForm& g : f) g.split = g.split * 2 >= cluster ? cluster : 1;
-    for (int i = 0; i < 2; ++i)
-        if ((t[i].s.red + GEMM_BK - 1) / GEMM_BK < f[i].split) f[i].split = 1;
+    // a launch has one size of cluster: each product is taken in as many parts, or whole; what ends first, from the sizes (parts chosen for
+    // each alone did not all run at once: gradients of 256 x 1024 -> 1000 fp32 45.5 us, so 25.8)
+    const long long tiles[2] = {tile_count(t[0].s, f[0]), tile_count(t[1].s, f[1])};
+    int cluster = 1;
+    float best = 0.0f;
+    for (int i = 0; i < 4; ++i)
+        for (int split = i ? 1 : 0; split < (i ? 4 : 1); ++split) {       // bit p: product p in parts
+            const int parts = 1 << i;
+            long long all = 0;
+            float time = 0.0f;
+            bool fits = true;
+            for (int p = 0; p < 2; ++p) {
+                const bool in_parts = split >> p & 1;
+                const float mine = tile_time(t[p].s, PL, in_parts ? i : 0);
+                fits = fits && (!in_parts || (t[p].s.red + GEMM_BK - 1) / GEMM_BK >= parts);
+                all += tiles[p] * (in_parts ? parts : 1);
+                time = mine > time ? mine : time;
+            }
+            if (i == 0) time *= (float)((all + tile_blocks(0) - 1) / tile_blocks(0));
+            else if (!fits || all > tile_blocks(i)) continue;
+            if (i && time >= best) continue;
+            best = time;
+            cluster = parts;
+            for (int p = 0; p < 2; ++p) f[p].split = split >> p & 1 ? parts : 1;
+        }
     TileLaunch<EPI> l;
     unsigned first = 0, second = 0;
     int rc = tile_product(&l, 0, t[0].a, t[0].b, t[0].s, epi[0], bf16, packs[0], f[0], &first);
