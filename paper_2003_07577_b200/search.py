@@ -39,7 +39,7 @@ class SearchLinear:
         self.bits, self.coeff_w, self.coeff_x = list(bits), list(coeff_w), list(coeff_x)
         self.alpha, self.act, self.steps = float(alpha), act, steps
         self.desc = ebs.linear_desc(rows, n, k, ebs.EBS_F32, act)
-        new = lambda *shape: torch.zeros(shape, device=weight.device)  # noqa: E731
+        new = lambda *shape: torch.zeros(shape, dtype=torch.float32, device=weight.device)  # noqa: E731
         self.w_hat, self.dw, self.momentum, self.update = new(n, k), new(n, k), new(n, k), new(n, k)
         self.dbias = None if bias is None else new(n)
         self.x_hat, self.dx, self.y, self.z = new(rows, k), new(rows, k), new(rows, n), new(rows, n)

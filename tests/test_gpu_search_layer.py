@@ -114,3 +114,30 @@ def test_refusals(mods):
     layer.forward(x)
     with pytest.raises(ValueError):
         layer.backward(x)
+
+
+def layer_of_dtype(mods, default):
+    """A step of a layer made under another default type: its buffers, then what it leaves in them."""
+    ebs, search = mods
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    w, b, x, dy = (torch.randn(s, generator=g, device="cuda", dtype=torch.float32) for s in ((40, 72), (40,), (20, 72), (20, 40)))
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(default)
+    try:
+        layer = search.SearchLinear(w, 20, [2, 4], [0.5, 0.5], [0.3, 0.7], 2.0, b, ebs.EBS_ACT_SILU)
+        own = [layer.w_hat, layer.dw, layer.momentum, layer.update, layer.dbias, layer.x_hat, layer.dx, layer.y, layer.z]
+        assert all(t.dtype == torch.float32 for t in own)    # (before any kernel writes to them)
+        layer.forward(x)
+        dx = layer.backward(dy)
+        layer.step(0.01)
+    finally:
+        torch.set_default_dtype(before)
+    return own + [dx, layer.weight, layer.bias]
+
+
+@pytest.mark.parametrize("default", [torch.float16, torch.bfloat16, torch.float64])
+def test_another_default_type(mods, default):
+    """The layer's buffers are fp32 whatever torch's default type is: the kernels write fp32 into them."""
+    for got, want in zip(layer_of_dtype(mods, default), layer_of_dtype(mods, torch.float32)):
+        assert got.dtype == torch.float32 and torch.equal(got, want)
