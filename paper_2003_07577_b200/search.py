@@ -74,7 +74,7 @@ class SearchLinear:
         self._check("dy", dy, (self.rows, self.weight.shape[0]), self.weight.device)
         with torch.cuda.device(self.weight.device):
             ebs.ebs_linear_backward(dy, self.x_hat, self.w_hat, self.z, self.desc, self.dx, self.dw, self.dbias, self._workspace)
-        return self.dx * ((self.x > 0) & (self.x < self.alpha))
+        return self.dx.masked_fill(~((self.x > 0) & (self.x < self.alpha)), 0.0)
 
     def step(self, rate: float, decay: float = 0.95) -> None:
         """w <- w - rate * orthogonalised(decay * momentum + dw); the bias takes a plain gradient step."""

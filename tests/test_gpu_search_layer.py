@@ -141,3 +141,18 @@ def test_another_default_type(mods, default):
     """The layer's buffers are fp32 whatever torch's default type is: the kernels write fp32 into them."""
     for got, want in zip(layer_of_dtype(mods, default), layer_of_dtype(mods, torch.float32)):
         assert got.dtype == torch.float32 and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_clipped_activations_have_no_gradient(mods, bad):
+    """Outside the clip range the gradient is zero, whatever the gradient of x_hat is there."""
+    ebs, _ = mods
+    layer, g = make(mods, 9, 16, 24, ebs.EBS_ACT_NONE)
+    x, dy = torch.randn((9, 24), generator=g, device="cuda"), torch.randn((9, 16), generator=g, device="cuda")
+    x[3, :4] = torch.tensor([-0.5, 3.0, 0.0, 2.0], device="cuda")
+    dy[3, 5] = bad
+    layer.forward(x)
+    dx = layer.backward(dy)
+    clipped = (x <= 0) | (x >= 2.0)
+    assert (dx[clipped] == 0).all()
+    assert not torch.isfinite(dx[3][~clipped[3]]).any() and torch.isfinite(dx[torch.arange(9, device="cuda") != 3]).all()
