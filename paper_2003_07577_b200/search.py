@@ -11,7 +11,8 @@ convolution takes this form on the matrix of its windows, a 1x1 convolution on i
 
 Buffers and call order only: the arithmetic is in the library's entry points (the clip mask and the momentum are element-wise
 torch operations).  Everything runs on the weights' device and its current stream, in buffers made once, so that a training step can be captured into a
-CUDA graph and replayed; a second stream or thread needs an object of its own.
+CUDA graph and replayed; a second stream or thread needs an object of its own.  Autograd sees none of it: the weights may be leaves that require
+gradients, backward() is the gradient.
 """
 from __future__ import annotations
 
@@ -54,6 +55,7 @@ class SearchLinear:
         if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device):
             raise ValueError(f"{name} must be dense fp32 {list(shape)} on {device}")
 
+    @torch.no_grad()
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x: fp32 [rows, k], left as it is until backward().  The result stays valid until the next call."""
         n, k = self.weight.shape
@@ -66,6 +68,7 @@ class SearchLinear:
             ebs.ebs_linear_forward(self.x_hat, self.w_hat, self.bias, residual, self.desc, self.y, self.z, self._workspace)
         return self.y
 
+    @torch.no_grad()
     def backward(self, dy: torch.Tensor) -> torch.Tensor:
         """Gradient with respect to the x of the last forward pass (that of its residual is dy); those of the weights (dw) and the
         bias (dbias) are kept for step()."""
@@ -76,6 +79,7 @@ class SearchLinear:
             ebs.ebs_linear_backward(dy, self.x_hat, self.w_hat, self.z, self.desc, self.dx, self.dw, self.dbias, self._workspace)
         return self.dx.masked_fill(~((self.x > 0) & (self.x < self.alpha)), 0.0)
 
+    @torch.no_grad()
     def step(self, rate: float, decay: float = 0.95) -> None:
         """w <- w - rate * orthogonalised(decay * momentum + dw); the bias takes a plain gradient step."""
         self.momentum.mul_(decay).add_(self.dw)

@@ -156,3 +156,20 @@ def test_clipped_activations_have_no_gradient(mods, bad):
     clipped = (x <= 0) | (x >= 2.0)
     assert (dx[clipped] == 0).all()
     assert not torch.isfinite(dx[3][~clipped[3]]).any() and torch.isfinite(dx[torch.arange(9, device="cuda") != 3]).all()
+
+
+def test_parameters(mods):
+    """Weights that are a module's parameters are trained as plain tensors are."""
+    ebs, search = mods
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    w, b, x, dy = (torch.randn(s, generator=g, device="cuda") for s in ((40, 72), (40,), (20, 72), (20, 40)))
+    results = []
+    for kind in (lambda t: t.clone(), lambda t: torch.nn.Parameter(t.clone())):
+        layer = search.SearchLinear(kind(w), 20, [2, 4], [0.5, 0.5], [0.3, 0.7], 2.0, kind(b), ebs.EBS_ACT_SILU)
+        for _ in range(2):
+            layer.forward(x)
+            layer.backward(dy)
+            layer.step(0.01)
+        results.append((layer.weight.detach(), layer.bias.detach(), layer.momentum))
+    assert all(torch.equal(p, q) for p, q in zip(*results))
