@@ -46,8 +46,10 @@ class SearchLinear:
         self.x_hat, self.dx, self.y, self.z = new(rows, k), new(rows, k), new(rows, n), new(rows, n)
         self.x = None
         self._scratch = torch.zeros(4, dtype=torch.int32, device=weight.device)
-        need = max(ebs.ebs_linear_workspace_bytes(self.desc, False), ebs.ebs_linear_workspace_bytes(self.desc, True),
-                   ebs.ebs_orthogonalize_workspace_bytes(1, n, k, ebs.EBS_F32, steps), 16)
+        need = [ebs.ebs_linear_workspace_bytes(self.desc, True), ebs.ebs_orthogonalize_workspace_bytes(1, n, k, ebs.EBS_F32, steps)]
+        if min(need) == 0:                                    # (what the entry points answer to arguments that they refuse)
+            raise ValueError("act, steps or sizes are out of range")
+        need = max(need + [ebs.ebs_linear_workspace_bytes(self.desc, False)])
         self._workspace = torch.empty(need, dtype=torch.uint8, device=weight.device)
 
     @staticmethod

@@ -173,3 +173,12 @@ def test_parameters(mods):
             layer.step(0.01)
         results.append((layer.weight.detach(), layer.bias.detach(), layer.momentum))
     assert all(torch.equal(p, q) for p, q in zip(*results))
+
+
+def test_refused_when_made(mods):
+    """What step() or backward() would refuse is refused before there is a state that they could leave half changed."""
+    ebs, search = mods
+    w = torch.zeros((8, 16), device="cuda")
+    for change in (dict(steps=65), dict(steps=-1), dict(act=5), dict(act=-1)):
+        with pytest.raises(ValueError):
+            search.SearchLinear(w, 4, [2], [1.0], [1.0], 1.0, **change)
