@@ -364,7 +364,8 @@ int ebs_search_act_forward(const float *x_dev, size_t n, float alpha, const int 
  * All tensors have the element type `dtype` (EBS_F32, EBS_F16 or EBS_BF16); products are summed in fp32, activation and
  * residual are applied to the fp32 sums, and each output is rounded once.  EBS_F32: an operand is kept to 22 bits, or to
  * 2^-40 of the largest magnitude that it has in the same sum, whichever is coarser (up to four rows forward: to all 24).  The backward call of a 16-bit type with an activation rounds dz to that type before the products,
- * not before the sum that gives dbias.
+ * not before the sum that gives dbias.  (EBS_F16 with EBS_ACT_GELU, EBS_ACT_GELU_TANH or EBS_ACT_SILU: dz / 2 is rounded, so
+ * that the steepest slope overflows nowhere; dz below 2^-13 is a multiple of 2^-23.)
  *   EBS_ACT_RELU       z > 0 ? z : 0 (NaN gives 0, as in the convolution's epilogue); slope 1 where z > 0, else 0
  *   EBS_ACT_GELU       z/2 (1 + erf(z / sqrt 2))
  *   EBS_ACT_GELU_TANH  z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))

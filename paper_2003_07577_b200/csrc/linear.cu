@@ -357,8 +357,9 @@ static GemmOut product_out(const Prepared& a, const Matrix& am, const Prepared& 
 }
 
 // ---------------------------------------------------------------------------------------------------- dz and dbias
-// A half-precision dz is kept halved: the steepest slope (1.13) times the type's largest value would not fit.
-static float dz_store_scale(const ebs_linear_desc& d) { return d.dtype == EBS_F16 && d.act ? 0.5f : 1.0f; }
+// A half-precision dz is kept halved where a slope may exceed one: the steepest (1.13) times the type's largest value would not fit.  That costs
+// dz below 2^-13 its last bit (multiples of 2^-23 instead of 2^-24); a rectified one is dy itself or zero and keeps all of them.
+static float dz_store_scale(const ebs_linear_desc& d) { return d.dtype == EBS_F16 && d.act > EBS_ACT_RELU ? 0.5f : 1.0f; }
 
 struct DzArgs {
     const void *dy, *z;

@@ -398,3 +398,28 @@ def test_threads(ebs, dtype, m, n, k):
         th.join()
     torch.cuda.synchronize()
     assert not errors and all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("m,n,k", [(24, 16, 24), (300, 264, 520)])
+def test_f16_gradients_next_to_zero(ebs, act, m, n, k):
+    """dy of a few times 2^-24.  None and ReLU: dz is dy or zero, no bit of it is lost.  The others keep half of dz (multiples of 2^-23)."""
+    t = torch.float16
+    dy = ((torch.arange(m * n, device="cuda").reshape(m, n) * 7 % 11 - 5).double() * 2.0 ** -24).to(t)
+    z = (torch.arange(m * n, device="cuda").reshape(m, n) * 5 % 13 - 6).to(t)
+    # one factor of 1024 in each sum: a result is one dz times 2^10
+    x, w = torch.zeros((m, k), dtype=t, device="cuda"), torch.zeros((n, k), dtype=t, device="cuda")
+    x[torch.arange(m), torch.arange(m) % k] = 1024
+    w[torch.arange(n), torch.arange(n) % k] = 1024
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    dt, ac = codes(ebs, "f16", act)
+    d = ebs.linear_desc(m, n, k, dt, ac)
+    ebs.ebs_linear_backward(dy, x, w, z, d, dx, dw, None, workspace(ebs, d, True))
+    z64 = z.double().requires_grad_(True)
+    dz = dy.double() * (z > 0 if act == "relu" else 1)
+    if act not in ("none", "relu"):
+        (dz,) = torch.autograd.grad(act64(z64, act), z64, dy.double())
+    # a kept dz is off by half a step: nothing, or 2^-24 (and by the slope's own 2^-21 of dy); terms a sum has at most: each is a kept dz times 2^10
+    step = 0.0 if act in ("none", "relu") else 2.0 ** -24 * (1 + 2.0 ** -10)
+    for got, ref, terms in ((dx, dz @ w.double(), (w != 0).double().sum(0).max()), (dw, dz.T @ x.double(), (x != 0).double().sum(0).max())):
+        assert ((got.double() - ref).abs() <= 2.0 ** -11 * ref.abs() + terms * 1024 * step).all()
