@@ -88,13 +88,16 @@ __device__ __forceinline__ float activation(float z, int act) {
 }
 template <bool FAST>
 __device__ __forceinline__ float activation_slope(float z, int act) {
-    float s, rest;
+    float s, rest, e;
     switch (act) {
         case EBS_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
         case EBS_ACT_GELU: normal_cdf<FAST>(z, s, rest); return fmaf(z * 0.39894228f, rest, s);
         case EBS_ACT_GELU_TANH:
             logistic<FAST>(1.59576912f * (z + 0.044715f * z * z * z), s, rest);
-            return s * (1.0f + z * rest * (1.59576912f * (1.0f + 0.134145f * z * z)));
+            // (s times rest is below 2^-149 from |z| = 20 on; the polynomial there would leave the type's range and make zero times infinity of it.
+            // z - z: zero, and NaN for an infinite z, as the other two give)
+            e = fminf(fmaxf(z, -20.0f), 20.0f) + (z - z);
+            return s * (1.0f + e * rest * (1.59576912f * (1.0f + 0.134145f * e * e)));
         case EBS_ACT_SILU:
             logistic<FAST>(z, s, rest);
             return s * (1.0f + z * rest);

@@ -423,3 +423,24 @@ def test_f16_gradients_next_to_zero(ebs, act, m, n, k):
     step = 0.0 if act in ("none", "relu") else 2.0 ** -24 * (1 + 2.0 ** -10)
     for got, ref, terms in ((dx, dz @ w.double(), (w != 0).double().sum(0).max()), (dw, dz.T @ x.double(), (x != 0).double().sum(0).max())):
         assert ((got.double() - ref).abs() <= 2.0 ** -11 * ref.abs() + terms * 1024 * step).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_slopes_far_out(ebs, act, dtype):
+    """|z| of 9 to the end of the type's range: the slope is 0 or 1 there to within what its exponential leaves, and no factor of it overflows."""
+    t = TYPES[dtype]
+    far = torch.tensor([9.0, 19.5, 20.0, 21.0, 1e3, 1e13, 2e13, 1e14, 5e18, 1e19, 2e19, 1e20, 1e30, 3e38], device="cuda")
+    z = torch.cat([far, -far]).to(t)
+    for rows in (1, 5):
+        zs = z.repeat(rows, 1)
+        n = z.numel()
+        dy, x, w = torch.ones_like(zs), torch.ones((rows, 8), dtype=t, device="cuda"), torch.eye(n, device="cuda").to(t)[:, :8].contiguous()
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(n, dtype=t, device="cuda")
+        d = ebs.linear_desc(rows, n, 8, *codes(ebs, dtype, act))
+        ebs.ebs_linear_backward(dy, x, w, zs, d, dx, dw, db, workspace(ebs, d, True))
+        # at |z| = 9 SiLU's slope is 9 e^-9 = 1.1e-3 off; the others' 2e-16 at most
+        off = 1.2e-3 if act == "silu" else 2.0 ** -21
+        want = rows * (z > 0).double()
+        assert ((db.double() - want).abs() <= rows * off).all() and ((dw.double() - want[:, None]).abs() <= rows * off).all()
+        assert ((dx.double() - (z[:8] > 0).double()).abs() <= off).all()
