@@ -370,8 +370,9 @@ int ebs_search_act_forward(const float *x_dev, size_t n, float alpha, const int 
  *   EBS_ACT_GELU       z/2 (1 + erf(z / sqrt 2))
  *   EBS_ACT_GELU_TANH  z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))
  *   EBS_ACT_SILU       z / (1 + exp(-z))
- * Infinities and NaN in x, W and dy reach exactly the outputs whose sums contain them.  (EBS_F32: an output with an infinity
- * in its row of x or column of the other operand is summed by itself, some hundred times slower.)
+ * Infinities and NaN in x, W and dy reach exactly the outputs whose sums contain them.  (EBS_F32: where a row of x or a column
+ * of the other operand holds an infinity, its outputs are found behind the others, from the operands: with one in every row
+ * 4096 x 4096 outputs over 4096 take 35 ms instead of 0.36, 4096 x 2048 over 131072 590 ms instead of 7.)
  *
  * Rows may be strided: ld* = elements from one row to the next (0: dense, that is k for x and W, n for the others); what
  * lies between the rows is neither read nor written.  dx has the stride of x, dW of W, dy of y.  Base addresses are

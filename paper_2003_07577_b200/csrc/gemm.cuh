@@ -132,7 +132,7 @@ inline int launch_chained(void (*kern)(P...), dim3 grid, int threads, size_t sme
 
 // Powers of two that fp32 operands are scaled by before they are split (linear.cu): one exponent a row or column.
 constexpr int SCALE_NAN = 1 << 20;         // the row holds a NaN: so do all its results
-constexpr int SCALE_INF = 1 << 21;         // it holds an infinity: its results are summed once more from the fp32 operands
+constexpr int SCALE_INF = 1 << 21;         // it holds an infinity: its results are found from the fp32 operands (finish_infinite)
 
 // fp32 operands of a split product, for rows and columns with infinities: a[i * a_row + r * a_red], b[j * b_col + r * b_red].
 struct GemmFp32 {
@@ -186,16 +186,16 @@ __device__ __forceinline__ void load_pack(const T* p, float (&v)[16 / sizeof(T)]
     unpack<T>(*reinterpret_cast<const uint4*>(p), v);
 }
 template <typename T>
-__device__ __forceinline__ void store_pack(T* p, const float (&v)[16 / sizeof(T)], int left = Pack<T>::N, bool vec = true) {
+__device__ __forceinline__ void store_pack(T* p, const float (&v)[16 / sizeof(T)], int left = Pack<T>::N, bool vec = true, unsigned holes = 0u) {
     uint4 u;
     if constexpr (sizeof(T) == 2) u = make_uint4(pair_word<T>(v[0], v[1]), pair_word<T>(v[2], v[3]), pair_word<T>(v[4], v[5]), pair_word<T>(v[6], v[7]));
     else u = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     const T* e = reinterpret_cast<const T*>(&u);
-    if (vec) *reinterpret_cast<uint4*>(p) = u;
+    if (vec && holes == 0u) *reinterpret_cast<uint4*>(p) = u;
     else
 #pragma unroll
         for (int i = 0; i < Pack<T>::N; ++i)
-            if (i < left) p[i] = e[i];
+            if (i < left && (holes >> i & 1u) == 0u) p[i] = e[i];
 }
 
 // Packs of neighbouring columns of one row.  What a pack needs from memory is loaded ahead: what depends on the columns once for all
@@ -230,43 +230,106 @@ __device__ __forceinline__ void gemm_ahead(const GemmOut& o, long long row, int 
     if (sizeof(T) == 4) a.row_exp = o.row_exp[row];
 }
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
-static __device__ __noinline__ float gemm_unscale(const float* a, long long a_red, const float* b, long long b_red, int red, int row_exp, int col_exp, float v) {
+// The sum v of a row and a column with these exponents.  A hole: one of them holds an infinity and none a NaN; finish_infinite has its result.
+__device__ __forceinline__ float unscale(float v, int row_exp, int col_exp, bool& hole) {
     const int e = row_exp + col_exp;
-    if (e < SCALE_NAN / 2) return scale_pow2(v, e);
-    if (row_exp == SCALE_NAN || col_exp == SCALE_NAN) return __int_as_float(0x7fffffff);
-    float s = 0.0f;
-    for (int r = 0; r < red; ++r) s = fmaf(a[r * a_red], b[r * b_red], s);
-    return s;
+    const bool nan = row_exp == SCALE_NAN || col_exp == SCALE_NAN;
+    hole = !nan && e >= SCALE_NAN / 2;
+    return nan ? __int_as_float(0x7fffffff) : hole ? 0.0f : scale_pow2(v, e);
 }
+// Results with an infinity in their row of a or column of b: rows row0 .. row0 + rows - 1, columns col0 .. col0 + cols - 1 of fp32 results, by
+// the block's first WARPS warps, which meet at named barrier BARRIER; masks: 64 words of shared memory.  Every term with an infinite factor is an infinity
+// or a NaN, so that the finite ones do not matter and a result is known from two bits: whether a term is plus (or a NaN), whether one is minus
+// infinity (or a NaN).  32 x 32 results at a time, the warps share the reduction; only where a value is not finite the 32 x 32 products of that place
+// are looked at.  (Summed one by one where the results leave, 4096 x 4096 over 4096 with an infinity in every row took 0.4 s and held up warps
+// whose waits are bounded.)
+template <int WARPS, int BARRIER>
+static __device__ __noinline__ void finish_infinite(const GemmOut o, long long row0, int rows, int col0, int cols, unsigned* masks) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const GemmFp32 g = o.fp32;
+    const int begin = (int)((long long)g.red * warp / WARPS), end = (int)((long long)g.red * (warp + 1) / WARPS);
+    auto meet = [&] { asm volatile("bar.sync %0, %1;\n" ::"n"(BARRIER), "n"(WARPS * 32) : "memory"); };
+    auto finite = [](float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; };
+#pragma unroll 1
+    for (int rb = 0; rb < rows; rb += 32)
+#pragma unroll 1
+        for (int cb = 0; cb < cols; cb += 32) {
+            const long long row = row0 + rb + lane;
+            const int col = col0 + cb + lane;
+            const bool row_there = rb + lane < rows, col_there = cb + lane < cols;
+            const int re = row_there ? o.row_exp[row] : 0, ce = col_there ? o.col_exp[col] : 0;
+            if (!__any_sync(0xffffffffu, re == SCALE_INF || ce == SCALE_INF)) continue;       // (the same in every warp)
+            meet();                                               // (the previous masks are read)
+            if (warp == 0) masks[lane] = masks[32 + lane] = 0u;
+            meet();
+            const float *a = g.a + row * g.a_row, *b = g.b + col * g.b_col;      // lanes: rows of a, columns of b
+            unsigned plus = 0u, minus = 0u;                       // of this lane's row, a bit a column
+#pragma unroll 1
+            for (int r = begin; r < end; r += 8) {
+                const float *at = a + r * g.a_red, *bt = b + r * g.b_red;
+                float av[8], bv[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i, at += g.a_red, bt += g.b_red) {
+                    const bool there = r + i < end;
+                    av[i] = there && row_there ? *at : 0.0f;
+                    bv[i] = there && col_there ? *bt : 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (!__any_sync(0xffffffffu, !finite(av[i]) || !finite(bv[i]))) continue;
+#pragma unroll 1
+                    for (int j = 0; j < 32; ++j) {
+                        const float bj = __shfl_sync(0xffffffffu, bv[i], j), p = av[i] * bj;
+                        const bool counts = !finite(av[i]) || !finite(bj), nan = p != p;
+                        plus |= (counts && (p > 0.0f || nan) ? 1u : 0u) << j;
+                        minus |= (counts && (p < 0.0f || nan) ? 1u : 0u) << j;
+                    }
+                }
+            }
+            if (plus) atomicOr(&masks[lane], plus);
+            if (minus) atomicOr(&masks[32 + lane], minus);
+            meet();
+#pragma unroll 1
+            for (int r = warp; r < 32; r += WARPS) {              // lanes: columns
+                const int x = __shfl_sync(0xffffffffu, re, r);
+                if (rb + r >= rows || !col_there || x == SCALE_NAN || ce == SCALE_NAN || (x != SCALE_INF && ce != SCALE_INF)) continue;
+                const bool p = masks[r] >> lane & 1u, m = masks[32 + r] >> lane & 1u;
+                const long long to = row0 + rb + r;
+                float v = __uint_as_float(p && m ? 0x7fffffffu : p ? 0x7f800000u : 0xff800000u);
+                v = fmaf(v, o.alpha, o.bias ? static_cast<const float*>(o.bias)[col] : 0.0f);
+                if (o.z) static_cast<float*>(o.z)[to * o.ldz + col] = v;
+                if (o.act) v = activation<false>(v, o.act);
+                if (o.residual) v += static_cast<const float*>(o.residual)[to * o.ldr + col];
+                static_cast<float*>(o.y)[to * o.ldy + col] = v;
+            }
+        }
+}
+// True: holes were left, elements that finish_infinite writes.
 template <typename T>
-__device__ __forceinline__ void gemm_store_pack(const GemmOut& o, long long row, int col, int left, bool vec, float (&v)[16 / sizeof(T)], const GemmColumns<T>& c,
+__device__ __forceinline__ bool gemm_store_pack(const GemmOut& o, long long row, int col, int left, bool vec, float (&v)[16 / sizeof(T)], const GemmColumns<T>& c,
                                                 const GemmAhead& a) {
     constexpr int N = Pack<T>::N;
     constexpr bool FAST = sizeof(T) == 2;
     float t[N];
+    unsigned holes = 0u;
     if constexpr (sizeof(T) == 4) {
         if (c.plain && abs(a.row_exp) <= SCALE_PLAIN) {
             const float f = power_of_two(a.row_exp);
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] *= f * power_of_two(c.exp[i]);
         } else {
-            const GemmFp32& g = o.fp32;
-#pragma unroll 1
+#pragma unroll
             for (int i = 0; i < N; ++i) {
-                if (i >= left) break;
-                float s = 0.0f;
-#pragma unroll
-                for (int e = 0; e < N; ++e) s = e == i ? v[e] : s;                       // (registers have no index)
-                s = gemm_unscale(g.a + row * g.a_row, g.a_red, g.b + (col + i) * g.b_col, g.b_red, g.red, a.row_exp, o.col_exp[col + i], s);
-#pragma unroll
-                for (int e = 0; e < N; ++e) v[e] = e == i ? s : v[e];
+                bool hole;
+                v[i] = unscale(v[i], a.row_exp, c.exp[i], hole);
+                holes |= (hole && i < left ? 1u : 0u) << i;
             }
         }
     }
     unpack<T>(c.bias, t);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = fmaf(v[i], o.alpha, t[i]);           // (alpha: a power of two, the product is exact)
-    if (o.z) store_pack(static_cast<T*>(o.z) + row * o.ldz + col, v, left, vec);
+    if (o.z) store_pack(static_cast<T*>(o.z) + row * o.ldz + col, v, left, vec, holes);
     switch (o.act) {                                        // (outside the loop: one branch a pack)
 #define EBS_ACT_CASE(A) case A: _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = activation<FAST>(v[i], A); break;
         EBS_ACT_CASE(EBS_ACT_RELU) EBS_ACT_CASE(EBS_ACT_GELU) EBS_ACT_CASE(EBS_ACT_GELU_TANH) EBS_ACT_CASE(EBS_ACT_SILU)
@@ -278,7 +341,8 @@ __device__ __forceinline__ void gemm_store_pack(const GemmOut& o, long long row,
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += t[i];
     }
-    store_pack(static_cast<T*>(o.y) + row * o.ldy + col, v, left, vec);
+    store_pack(static_cast<T*>(o.y) + row * o.ldy + col, v, left, vec, holes);
+    return holes != 0u;
 }
 // Whether every row of the outputs and of the residual starts on 16 bytes.
 inline bool packs_ok(const GemmOut& o, size_t size) {

@@ -67,6 +67,7 @@ template <class EPI> struct RowOut;
 
 template <typename T>
 struct RowOut<LinearOut<T>> {
+    static constexpr bool HOLES = LinearOut<T>::HOLES;
     static constexpr int CW = 64 / sizeof(T), N = Pack<T>::N;
     struct Ahead { uint4 residual[4]; };
     static __device__ __forceinline__ void begin(const LinearOut<T>& e, float* terms, int columns, int at, int col, int cols) {
@@ -84,7 +85,7 @@ struct RowOut<LinearOut<T>> {
         for (int c = 0; c < 4; ++c)
             if (c * N < left) a.residual[c] = load_raw(p + c * N, left - c * N, left >= (c + 1) * N);
     }
-    static __device__ __forceinline__ void scale(const LinearOut<T>& e, float (&v)[CW], const float* terms, int columns, long long row, int col, int left, int row_term, uint8_t* buffer, int lane, bool exists) {
+    static __device__ __forceinline__ void scale(const LinearOut<T>& e, float (&v)[CW], const float* terms, int columns, int col, int left, int row_term, uint8_t* buffer, int lane, bool exists, volatile int* holes) {
         if constexpr (sizeof(T) == 4) {
             float t[CW];
             bool plain = abs(row_term) <= SCALE_PLAIN;
@@ -103,14 +104,16 @@ struct RowOut<LinearOut<T>> {
                 }
                 return;
             }
-            // rare: through this thread's row of the buffer, an element at a time
-            const GemmFp32& g = e.o.fp32;
+            // rare: through this thread's row of the buffer, an element at a time.  A hole becomes zero without the bias: act(0) is zero, so that y
+            // gets the residual, which may be y itself and is read again by finish_infinite.
             put_row<float>(buffer, lane, v);
 #pragma unroll 1
             for (int i = 0; i < CW && i < left; ++i) {
                 float* at = reinterpret_cast<float*>(row_chunk(buffer, lane, i >> 2)) + (i & 3);
-                const float s = exists ? gemm_unscale(g.a + row * g.a_row, g.a_red, g.b + (col + i) * g.b_col, g.b_red, g.red, row_term, e.o.col_exp[col + i], *at) : 0.0f;
-                *at = fmaf(s, e.o.alpha, terms[i]);
+                bool hole = false;
+                const float s = exists ? unscale(*at, row_term, e.o.col_exp[col + i], hole) : 0.0f;
+                *at = hole ? 0.0f : fmaf(s, e.o.alpha, terms[i]);
+                if (hole) *holes = 1;
             }
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -145,9 +148,9 @@ struct RowOut<LinearOut<T>> {
     }
     template <int R>
     static __device__ __forceinline__ void finish(const LinearOut<T>& e, const CUtensorMap* y, const CUtensorMap* z, RowRing<R>& ring, float (&v)[CW], const float* terms, int columns, int, int rows, int batch, int row0,
-                                                  int col, int left, int row_term, const Ahead& a, bool exists) {
+                                                  int col, int left, int row_term, const Ahead& a, bool exists, volatile int* holes) {
         uint8_t* to = ring.next();
-        scale(e, v, terms, columns, row0 + ring.lane, col, left, row_term, to, ring.lane, row0 + ring.lane < rows);
+        scale(e, v, terms, columns, col, left, row_term, to, ring.lane, row0 + ring.lane < rows, holes);
         if (e.o.z) {
             put_row<T>(to, ring.lane, v);
             ring.store(z, to, col, row0, batch, exists);
@@ -162,6 +165,7 @@ struct RowOut<LinearOut<T>> {
 // Rows of planes: a buffer for hi, one for lo.
 template <>
 struct RowOut<PlanesOut> {
+    static constexpr bool HOLES = false;
     static constexpr int CW = 32;
     struct Ahead {};
     static __device__ __forceinline__ void begin(const PlanesOut&, float*, int, int, int, int) {}
@@ -201,7 +205,7 @@ struct RowOut<PlanesOut> {
     }
     template <int R>
     static __device__ __forceinline__ void finish(const PlanesOut& e, const CUtensorMap* y, const CUtensorMap* y2, RowRing<R>& ring, float (&v)[CW], const float*, int, int mirror, int rows, int batch,
-                                                  int row0, int col, int left, int, const Ahead&, bool exists) {
+                                                  int row0, int col, int left, int, const Ahead&, bool exists, volatile int*) {
         matrix(e.y, e, y, ring, v, e.alpha, e.diag, mirror, rows, batch, row0, col, left, exists);
         if (e.y2) matrix(e.y2, e, y2, ring, v, e.alpha2, e.diag2, mirror, rows, batch, row0, col, left, exists);
     }
@@ -209,6 +213,7 @@ struct RowOut<PlanesOut> {
 
 template <typename T>
 struct RowOut<TypedFinal<T>> {
+    static constexpr bool HOLES = false;
     static constexpr int CW = 64 / sizeof(T);
     struct Ahead {};
     static __device__ __forceinline__ void begin(const TypedFinal<T>&, float*, int, int, int, int) {}
@@ -216,7 +221,7 @@ struct RowOut<TypedFinal<T>> {
     static __device__ __forceinline__ void ahead(const TypedFinal<T>&, int, long long, int, int, Ahead&) {}
     template <int R>
     static __device__ __forceinline__ void finish(const TypedFinal<T>& e, const CUtensorMap* y, const CUtensorMap*, RowRing<R>& ring, float (&v)[CW], const float*, int, int, int rows, int batch, int row0, int col,
-                                                  int, int, const Ahead&, bool exists) {
+                                                  int, int, const Ahead&, bool exists, volatile int*) {
 #pragma unroll
         for (int i = 0; i < CW; ++i) v[i] *= e.o.alpha;
         uint8_t* to = ring.next();
@@ -227,6 +232,7 @@ struct RowOut<TypedFinal<T>> {
 
 template <>
 struct RowOut<PartialOut> {
+    static constexpr bool HOLES = false;
     static constexpr int CW = 16;
     struct Ahead {};
     static __device__ __forceinline__ void begin(const PartialOut&, float*, int, int, int, int) {}
@@ -234,7 +240,7 @@ struct RowOut<PartialOut> {
     static __device__ __forceinline__ void ahead(const PartialOut&, int, long long, int, int, Ahead&) {}
     template <int R>
     static __device__ __forceinline__ void finish(const PartialOut&, const CUtensorMap* y, const CUtensorMap*, RowRing<R>& ring, float (&v)[CW], const float*, int, int, int, int slice, int row0, int col, int,
-                                                  int, const Ahead&, bool exists) {
+                                                  int, const Ahead&, bool exists, volatile int*) {
         uint8_t* to = ring.next();
         put_row<float>(to, ring.lane, v);
         ring.store(y, to, col, row0, slice, exists);
@@ -329,6 +335,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     uint64_t *empty = full + S, *acc_full = empty + S, *acc_empty = acc_full + 2, *terms_there = acc_empty + 2, *terms_read = terms_there + 4;
     uint32_t& tmem_slot = *reinterpret_cast<uint32_t*>(terms_read + 4);
     volatile int& abort_flag = *reinterpret_cast<volatile int*>(terms_read + 5);
+    volatile int* holes = &abort_flag + 1;                        // results were left to finish_infinite
     static_assert((2 * S + 12 + 2) * 8 <= PAIR_BARRIERS, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x & 1), pairs = (int)(gridDim.x >> 1);
@@ -339,7 +346,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
         for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 2 * PAIR_EPI_WARPS); }
         for (int q = 0; q < 4; ++q) { mbar_init(&terms_there[q], 4); mbar_init(&terms_read[q], 4); }
-        abort_flag = 0;
+        abort_flag = *holes = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     if (warp == PAIR_EPI_WARPS + 1) {
@@ -460,7 +467,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
             auto rows_out = [&](int column, float (&v)[CW]) {
                 const int col = col0 + column;
                 Rows::finish(epi, &map_y, &map_z, ring, v, terms + column, CQ, g.symmetric && tn / (256 / TN) != tm, g.out_rows, slice, row0, col, g.out_cols - col, row_term, row_ahead,
-                             col < g.out_cols && row0 < g.out_rows);
+                             col < g.out_cols && row0 < g.out_rows, holes);
             };
             // Outputs whose rows start anywhere, 16 columns at a time: through the warp's buffer, then two rows an access, neighbouring lanes
             // at neighbouring elements, eight accesses' loads under way.
@@ -484,7 +491,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                             for (int i = 0; i < 8; ++i) {
                                 const int r = r0 + 2 * i;
                                 const float v = reinterpret_cast<const float*>(row_chunk(ring.base, r, cc >> 2))[cc & 3];
-                                if (row0 + r < g.out_rows) epi.one(batch, row0 + r, col, v, terms_of, place[i]);
+                                if (row0 + r < g.out_rows && epi.one(batch, row0 + r, col, v, terms_of, place[i])) *holes = 1;
                             }
                         }
                     }
@@ -576,6 +583,15 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
         giveup_drain();
         if (threadIdx.x == 0) atomicAdd(&g_gemm_pair_timeouts, 1ull);
     }
+    if constexpr (RowOut<EPI>::HOLES) {                           // (behind all waits, by the warps that have the registers)
+        if (*holes && !abort_flag && warp < PAIR_EPI_WARPS)
+            for (int t = (int)(blockIdx.x >> 1); t < count; t += pairs) {
+                int batch, tm, tn, part, kb0, kb1;
+                pair_tile<TN>(t, tiles_m, tiles_n, g.symmetric, g.split, blocks, batch, tm, tn, part, kb0, kb1);
+                const int row0 = tm * 256 + rank * 128, col0 = tn * TN;
+                finish_infinite<PAIR_EPI_WARPS, 1>(epi.o, row0, min(128, g.out_rows - row0), col0, min(TN, g.out_cols - col0), reinterpret_cast<unsigned*>(behind));
+            }
+    }
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     cluster_sync_all();                                           // no block leaves while the other's MMAs or arrivals reach it
     if (warp == PAIR_EPI_WARPS + 1)
@@ -651,34 +667,53 @@ static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmSha
     return launch_chained(kern, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), PAIR_THREADS, (size_t)bytes, st, 2, a, b, y, z, g, epi);
 }
 
-// Adds the parts of a product split over its reduction, in their order, and finishes the results: a thread a pack.
+// Adds the parts of a product split over its reduction, in their order, and finishes the results: a thread a pack.  Where there may be holes a block
+// takes 32 x 32 results at a time, what finish_infinite does, and its registers (a called function's count too) are bounded so that four blocks run.
 template <class EPI>
-__global__ void __launch_bounds__(256) reduce_parts_kernel(const PartialOut in, const int parts, const int rows, const int cols, const int packs, const EPI epi) {
+__global__ void __launch_bounds__(256, EPI::HOLES ? 4 : 0) reduce_parts_kernel(const PartialOut in, const int parts, const int rows, const int cols, const int packs, const EPI epi) {
     constexpr int N = EPI::N;
     let_next_kernel_start();
     wait_for_previous_kernel();
-    const int per_row = (cols + N - 1) / N, batch = (int)blockIdx.y;
-    const long long items = (long long)per_row * rows;
+    const int per_row = EPI::HOLES ? (cols + 31) / 32 : (cols + N - 1) / N, batch = (int)blockIdx.y;      // squares, or packs
+    const long long items = EPI::HOLES ? (long long)per_row * ((rows + 31) / 32) * 256 : (long long)per_row * rows;
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < items; i += gridDim.x * 256LL) {
-        const int row = (int)(i / per_row), col = (int)(i - (long long)row * per_row) * N, left = cols - col;
-        const bool vec = packs && left >= N;
-        typename EPI::Columns columns;
-        typename EPI::Ahead ahead;
-        epi.columns(col, left, vec, columns);
-        epi.ahead(batch, row, col, left, vec, ahead);
-        float v[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = 0.0f;
-        const float* p = in.y + batch * in.batch + row * in.ld + col;
-#pragma unroll 4
-        for (int q = 0; q < parts; ++q) {
-#pragma unroll
-            for (int e = 0; e < N; e += 4) {
-                const float4 t = *reinterpret_cast<const float4*>(p + q * in.part + e);
-                v[e] += t.x; v[e + 1] += t.y; v[e + 2] += t.z; v[e + 3] += t.w;
-            }
+        int row, col;
+        if constexpr (EPI::HOLES) {
+            static_assert(N == 4, "eight packs of 32 columns");
+            const int square = (int)(i >> 8);
+            row = square / per_row * 32 + (int)threadIdx.x / 8;
+            col = square % per_row * 32 + (int)threadIdx.x % 8 * N;
+        } else {
+            row = (int)(i / per_row);
+            col = (int)(i - (long long)row * per_row) * N;
         }
-        epi.pack(batch, row, col, left, vec, v, columns, ahead);
+        bool holes = false;
+        if (!EPI::HOLES || (row < rows && col < cols)) {
+            const int left = cols - col;
+            const bool vec = packs && left >= N;
+            typename EPI::Columns columns;
+            typename EPI::Ahead ahead;
+            epi.columns(col, left, vec, columns);
+            epi.ahead(batch, row, col, left, vec, ahead);
+            float v[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = 0.0f;
+            const float* p = in.y + batch * in.batch + row * in.ld + col;
+#pragma unroll 4
+            for (int q = 0; q < parts; ++q) {
+#pragma unroll
+                for (int e = 0; e < N; e += 4) {
+                    const float4 t = *reinterpret_cast<const float4*>(p + q * in.part + e);
+                    v[e] += t.x; v[e + 1] += t.y; v[e + 2] += t.z; v[e + 3] += t.w;
+                }
+            }
+            holes = epi.pack(batch, row, col, left, vec, v, columns, ahead);
+        }
+        if constexpr (EPI::HOLES) {
+            __shared__ unsigned masks[64];
+            const int row0 = row & ~31, col0 = col & ~31;
+            if (__syncthreads_or(holes)) finish_infinite<8, 0>(epi.o, row0, min(32, rows - row0), col0, min(32, cols - col0), masks);
+        }
     }
 }
 template <class EPI, int PL>
@@ -692,7 +727,7 @@ static int launch_pair_or_parts(const GemmOperand& A, const GemmOperand& B, cons
     p.parts = route.split;
     const int rc = launch_pair<PartialOut, PL, 256>(A, B, s, p, bf16, route.split, st);
     if (rc) return rc;
-    const long long items = (long long)((s.cols + EPI::N - 1) / EPI::N) * s.rows, blocks = (items + 255) / 256;
+    const long long items = (long long)((s.cols + EPI::N - 1) / EPI::N) * s.rows, blocks = EPI::HOLES ? (s.rows + 31LL) / 32 * ((s.cols + 31) / 32) : (items + 255) / 256;
     return launch_chained(reduce_parts_kernel<EPI>, dim3((unsigned)(blocks < 4096 ? blocks : 4096), s.batch), 256, 0, st, 1, p, route.split, s.rows, s.cols, (int)packs, epi);
 }
 

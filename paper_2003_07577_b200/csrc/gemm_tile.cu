@@ -224,6 +224,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
         }
         if (warp < 8) skip = !mbar_wait_bounded(&received, 0, &abort_flag, g.wait_limit);
     }
+    bool holes = false;
     if (!skip && writes) {
 #pragma unroll 1
         for (int o = first; o < o_end; o += STRIDE) {
@@ -242,8 +243,12 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
                     v[e] += t.x; v[e + 1] += t.y; v[e + 2] += t.z; v[e + 3] += t.w;
                 }
             }
-            epi.pack(batch, outer0 + o, ocol, left, vec, v, columns, here);
+            holes |= epi.pack(batch, outer0 + o, ocol, left, vec, v, columns, here);
         }
+    }
+    if constexpr (EPI::HOLES) {
+        __shared__ unsigned masks[64];
+        if (__syncthreads_or(holes)) finish_infinite<10, 0>(epi.o, outer0 + o_begin, o_end - o_begin, inner0, min(INNER, g.out_cols - inner0), masks);
     }
     if (split > 1) cluster_sync_all();                            // no block leaves while its sums are on their way
     if (abort_flag) {

@@ -131,12 +131,14 @@ struct GemmShape {
 int gemm_sm_count();
 
 // What becomes of the sums, N neighbouring columns of a row at a time (`left` of them exist; vec: all do, at addresses of whole 16 bytes):
-// `columns` and `ahead` load what is needed, `touch` reads the parameters that `pack` will use, which finishes and stores.
+// `columns` and `ahead` load what is needed, `touch` reads the parameters that `pack` will use, which finishes and stores.  HOLES: it may leave
+// elements (and then says so) whose results finish_infinite has.
 
 // The results of a linear layer or of its gradients.
 template <typename T>
 struct LinearOut {
     static constexpr int N = Pack<T>::N;
+    static constexpr bool HOLES = sizeof(T) == 4;
     using Columns = GemmColumns<T>;
     using Ahead = GemmAhead;
     GemmOut o;
@@ -152,21 +154,24 @@ struct LinearOut {
         if (o.residual) p.residual = to_f32(static_cast<const T*>(o.residual)[row * o.ldr + col]);
         if (sizeof(T) == 4) p.row_exp = o.row_exp[row];
     }
-    __device__ __forceinline__ void one(int, long long row, int col, float v, const Column& c, const Place& p) const {
+    __device__ __forceinline__ bool one(int, long long row, int col, float v, const Column& c, const Place& p) const {
         if (sizeof(T) == 4) {
+            bool hole = false;
             if (abs(c.exp) <= SCALE_PLAIN && abs(p.row_exp) <= SCALE_PLAIN) v *= power_of_two(p.row_exp) * power_of_two(c.exp);
-            else v = gemm_unscale(o.fp32.a + row * o.fp32.a_row, o.fp32.a_red, o.fp32.b + col * o.fp32.b_col, o.fp32.b_red, o.fp32.red, p.row_exp, c.exp, v);
+            else v = unscale(v, p.row_exp, c.exp, hole);
+            if (hole) return true;
         }
         v = fmaf(v, o.alpha, c.bias);
         if (o.z) static_cast<T*>(o.z)[row * o.ldz + col] = from_f32<T>(v);
         if (o.act) v = activation<sizeof(T) == 2>(v, o.act);
         if (o.residual) v += p.residual;
         static_cast<T*>(o.y)[row * o.ldy + col] = from_f32<T>(v);
+        return false;
     }
     __device__ __forceinline__ void columns(int col, int left, bool vec, Columns& c) const { gemm_columns<T>(o, col, left, vec, c); }
     __device__ __forceinline__ void ahead(int, long long row, int col, int left, bool vec, Ahead& a) const { gemm_ahead<T>(o, row, col, left, vec, a); }
-    __device__ __forceinline__ void pack(int, long long row, int col, int left, bool vec, float (&v)[N], const Columns& c, const Ahead& a) const {
-        gemm_store_pack<T>(o, row, col, left, vec, v, c, a);
+    __device__ __forceinline__ bool pack(int, long long row, int col, int left, bool vec, float (&v)[N], const Columns& c, const Ahead& a) const {
+        return gemm_store_pack<T>(o, row, col, left, vec, v, c, a);
     }
 };
 
@@ -175,6 +180,7 @@ struct LinearOut {
 // set.  Rows are padded to whole groups of eight elements, so that a pack is always whole.
 struct PlanesOut {
     static constexpr int N = 4;
+    static constexpr bool HOLES = false;
     struct Columns {};
     struct Ahead {};
     __half* y;
@@ -194,10 +200,11 @@ struct PlanesOut {
         *reinterpret_cast<uint2*>(q) = hi;
         *reinterpret_cast<uint2*>(q + plane) = lo;
     }
-    __device__ __forceinline__ void pack(int b, long long row, int col, int, bool, float (&v)[N], const Columns&, const Ahead&) const {
+    __device__ __forceinline__ bool pack(int b, long long row, int col, int, bool, float (&v)[N], const Columns&, const Ahead&) const {
         const long long at = b * batch + row * ld + col;
         store(y + at, row, col, v, alpha, diag);
         if (y2) store(y2 + at, row, col, v, alpha2, diag2);
+        return false;
     }
 };
 
@@ -210,6 +217,7 @@ struct FinalOut {
 template <typename T>
 struct TypedFinal {
     static constexpr int N = Pack<T>::N;
+    static constexpr bool HOLES = false;
     struct Columns {};
     struct Ahead {};
     FinalOut o;
@@ -217,16 +225,18 @@ struct TypedFinal {
     struct Place {};
     __device__ __forceinline__ void column(int, Column&) const {}
     __device__ __forceinline__ void place(long long, int, Place&) const {}
-    __device__ __forceinline__ void one(int b, long long row, int col, float v, const Column&, const Place&) const {
+    __device__ __forceinline__ bool one(int b, long long row, int col, float v, const Column&, const Place&) const {
         static_cast<T*>(o.y)[b * o.batch + row * o.ld + col] = from_f32<T>(v * o.alpha);
+        return false;
     }
     __device__ __forceinline__ void touch() const { asm volatile("" ::"l"(o.y), "l"(o.batch), "f"(o.alpha)); }
     __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
     __device__ __forceinline__ void ahead(int, long long, int, int, bool, Ahead&) const {}
-    __device__ __forceinline__ void pack(int b, long long row, int col, int left, bool vec, float (&v)[N], const Columns&, const Ahead&) const {
+    __device__ __forceinline__ bool pack(int b, long long row, int col, int left, bool vec, float (&v)[N], const Columns&, const Ahead&) const {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] *= o.alpha;
         store_pack(static_cast<T*>(o.y) + b * o.batch + row * o.ld + col, v, left, vec);
+        return false;
     }
 };
 

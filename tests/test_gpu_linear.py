@@ -444,3 +444,98 @@ def test_slopes_far_out(ebs, act, dtype):
         want = rows * (z > 0).double()
         assert ((db.double() - want).abs() <= rows * off).all() and ((dw.double() - want[:, None]).abs() <= rows * off).all()
         assert ((dx.double() - (z[:8] > 0).double()).abs() <= off).all()
+
+
+def sprinkle(t, g, rows, one_in):
+    """An infinity of either sign in one of `one_in` rows (or, rows = False, columns), at a place of its own."""
+    count, other = (t.shape[0], t.shape[1]) if rows else (t.shape[1], t.shape[0])
+    i = torch.arange(0, count, one_in, device="cuda")
+    at = torch.randint(0, other, (i.numel(),), generator=g, device="cuda")
+    v = torch.where(torch.rand(i.numel(), generator=g, device="cuda") < 0.5, math.inf, -math.inf).to(t.dtype)
+    if rows:
+        t[i, at] = v
+    else:
+        t[at, i] = v
+
+
+def same_where_not_finite(got, ref):
+    assert torch.equal(torch.isnan(got), torch.isnan(ref))
+    assert torch.equal(torch.isposinf(got), torch.isposinf(ref)) and torch.equal(torch.isneginf(got), torch.isneginf(ref))
+
+
+# few rows, one tile, clusters, parts through memory, pairs with rows on 16 bytes and anywhere
+INFINITE = [(7, 40, 200), (40, 37, 129), (200, 300, 2000), (300, 264, 8200), (300, 261, 4103), (2304, 1160, 72), (2304, 1161, 72), (2100, 1200, 520)]
+
+
+@pytest.mark.parametrize("one_in", [(1, 0), (0, 1), (1, 1), (5, 7), (33, 50)])
+@pytest.mark.parametrize("m,n,k", INFINITE)
+def test_fp32_infinities_in_many_rows(ebs, m, n, k, one_in):
+    """An infinity in every row of x, column of W, in both or in some: which results are infinite or NaN, and that the others and a residual in
+    place are what they are without."""
+    g = gen(17)
+    for act, in_place in (("none", True), ("relu", False), ("silu", True)):
+        x, w, r = strided(m, k, k, torch.float32, g), strided(n, k, k, torch.float32, g, 1 / math.sqrt(k)), strided(m, n, n, torch.float32, g)
+        b = torch.randn(n, generator=g, device="cuda")
+        w[:, ::9] = 0.0                                       # infinity times zero
+        if one_in[0]:
+            sprinkle(x, g, True, one_in[0])
+        if one_in[1]:
+            sprinkle(w, g, True, one_in[1])
+        x[1, 3] = math.nan
+        r[2, 4] = -math.inf
+        z64 = x.double() @ w.double().T + b.double()
+        y64 = act64(z64, act) + r.double()
+        y, z = r.clone(), torch.empty((m, n), device="cuda")
+        run_forward(ebs, x, w, b, y if in_place else r, "f32", act, y, z)
+        same_where_not_finite(z, z64)
+        same_where_not_finite(y, y64)
+        xs, ws = torch.where(torch.isfinite(x), x, torch.zeros_like(x)), torch.where(torch.isfinite(w), w, torch.zeros_like(w))
+        sums = xs.double().abs() @ ws.double().abs().T + b.double().abs()
+        ok = torch.isfinite(z64)
+        assert ((z.double() - z64).abs() <= bound(torch.float32, z64, sums, k))[ok].all()
+        ok = torch.isfinite(y64)
+        assert ((y.double() - y64).abs() <= bound(torch.float32, y64, 1.13 * sums, k) + 2.0 ** -23 * (act64(z64, act).abs() + r.double().abs()))[ok].all()
+    assert ebs.ebs_check_device_status() == ebs.EBS_OK
+
+
+@pytest.mark.parametrize("one_in", [(1, 0), (0, 1), (1, 1), (5, 7)])
+@pytest.mark.parametrize("m,n,k", INFINITE)
+def test_fp32_infinities_in_many_gradients(ebs, m, n, k, one_in):
+    g = gen(19)
+    x, w, dy, z = (strided(*s, torch.float32, g) for s in ((m, k, k), (n, k, k), (m, n, n), (m, n, n)))
+    w[::7] = 0.0
+    x[::7] = 0.0
+    if one_in[0]:
+        sprinkle(dy, g, True, one_in[0])
+    if one_in[1]:
+        sprinkle(x, g, False, one_in[1])
+        sprinkle(w, g, False, one_in[1])
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    for act in ("none", "gelu"):
+        d = ebs.linear_desc(m, n, k, *codes(ebs, "f32", act))
+        ebs.ebs_linear_backward(dy, x, w, z, d, dx, dw, None, workspace(ebs, d, True))
+        dz = dy.double()
+        if act == "gelu":
+            dz = dz * slope64(z.double())
+        same_where_not_finite(dx, dz @ w.double())
+        same_where_not_finite(dw, dz.T @ x.double())
+    assert ebs.ebs_check_device_status() == ebs.EBS_OK
+
+
+def slope64(z):
+    """GELU's derivative."""
+    return 0.5 * (1 + torch.erf(z * math.sqrt(0.5))) + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+
+
+@pytest.mark.parametrize("m,n,k", [(4096, 2048, 131112), (700, 520, 262150), (144, 16, 200001)])
+def test_fp32_infinities_along_long_reductions(ebs, m, n, k):
+    """One in every row of x: a result is that infinity with the sign of the weight it meets.  No wait runs out meanwhile."""
+    g = gen(23)
+    x, w = torch.randn((m, k), generator=g, device="cuda"), torch.randn((n, k), generator=g, device="cuda")
+    at = torch.randint(0, k, (m,), generator=g, device="cuda")
+    sign = torch.where(torch.rand(m, generator=g, device="cuda") < 0.5, 1.0, -1.0)
+    x[torch.arange(m, device="cuda"), at] = sign * math.inf
+    y = torch.zeros((m, n), device="cuda")
+    run_forward(ebs, x, w, None, None, "f32", "none", y)
+    assert torch.equal(y, w[:, at].T * sign[:, None] * math.inf)
+    assert ebs.ebs_check_device_status() == ebs.EBS_OK
