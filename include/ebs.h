@@ -420,6 +420,7 @@ int ebs_linear_backward(const void *dy_dev, const void *x_dev, const void *w_dev
  * infinity gives NaN throughout (no steps: as the formula has it).  |G|_F is summed in 64 bits.  The products are summed in fp32 from operands kept to 22
  * bits, for every type: a steep polynomial multiplies early roundings by up to a^steps.
  * dtype (EBS_F32, EBS_F16, EBS_BF16) is the type of G and out.  steps 0 .. 64, coefficients and scale finite, eps >= 0;
+ * at most 65535 matrices, 2^36 elements and 2^30 rows or columns;
  * EBS_ERR_UNSUPPORTED if the singular values could leave 2^-20 .. 2^20 under these coefficients.  coeff is a HOST array of
  * three floats.  out may be G itself, and may not overlap it otherwise; workspace_dev as above.  The order of sums goes by
  * the sizes: a matrix's last bits may differ with the number of matrices beside it.

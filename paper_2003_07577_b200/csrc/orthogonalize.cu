@@ -169,7 +169,8 @@ static OrthoBuffers ortho_buffers(int batch, int rows, int cols) {
 }
 static int check_shape(int batch, int rows, int cols, int dtype, int steps) {
     if (batch < 1 || rows < 1 || cols < 1 || !real_dtype(dtype) || steps < 0 || steps > ORTHO_MAX_STEPS) return EBS_ERR_INVALID_ARG;
-    if (batch > 65535 || (long long)rows * cols > (1LL << 36) / batch) return EBS_ERR_OVERFLOW;
+    // (a side of up to 2^30, as in a layer: tiles and stages are counted in 32 bits, rounded up)
+    if (batch > 65535 || rows > (1 << 30) || cols > (1 << 30) || (long long)rows * cols > (1LL << 36) / batch) return EBS_ERR_OVERFLOW;
     return EBS_OK;
 }
 

@@ -132,3 +132,11 @@ def test_fast_path_types(ebs):
         assert m.linear_forward(None, None, None, None, d, None, None, ws, None) == ebs.EBS_ERR_INVALID_ARG
     finally:
         ebs._fast = None
+
+
+def test_orthogonalize_sides_beyond_the_index_range(ebs):
+    """Tiles and stages of 32-bit counts: a side of more than 2^30 is refused, whichever it is, by the size query too."""
+    for rows, cols in (((1 << 30) + 1, 1), (1, (1 << 30) + 1), ((1 << 31) - 1, 1), (1, (1 << 31) - 1), ((1 << 31) - 64, 17), (8, (1 << 31) - 200)):
+        assert ortho(ebs, batch=1, rows=rows, cols=cols, ws_bytes=1 << 62) == ebs.EBS_ERR_OVERFLOW
+        assert ebs.ebs_orthogonalize_workspace_bytes(1, rows, cols, 0, 5) == 0
+    assert ebs.ebs_orthogonalize_workspace_bytes(1, 1 << 30, 1, 0, 5) > 0
