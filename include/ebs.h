@@ -362,7 +362,9 @@ int ebs_search_act_forward(const float *x_dev, size_t n, float alpha, const int 
  *              dx = dz W,  dW = dz^T x,  dbias = sum over the rows of dz        (residual's gradient is dy itself)
  *
  * All tensors have the element type `dtype` (EBS_F32, EBS_F16 or EBS_BF16); products are summed in fp32, activation and
- * residual are applied to the fp32 sums, and each output is rounded once.  EBS_F32: an operand is kept to 22 bits, or to
+ * residual are applied to the fp32 sums, and each output is rounded once.  The tensor cores truncate what they add up, 256 elements
+ * of a sum at a time (EBS_F32; an error of about 1.5e-6 of a sum of one sign) or up to 4096 (16-bit types; 2.6e-5, a twentieth of
+ * what EBS_F16 rounds); the rest of a sum is rounded to nearest.  EBS_F32: an operand is kept to 22 bits, or to
  * 2^-40 of the largest magnitude that it has in the same sum, whichever is coarser (up to four rows forward: to all 24).  The backward call of a 16-bit type with an activation rounds dz to that type before the products,
  * not before the sum that gives dbias.  (EBS_F16 with EBS_ACT_GELU, EBS_ACT_GELU_TANH or EBS_ACT_SILU: dz / 2 is rounded, so
  * that the steepest slope overflows nowhere; dz below 2^-13 is a multiple of 2^-23.)

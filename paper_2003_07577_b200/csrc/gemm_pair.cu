@@ -322,7 +322,8 @@ __device__ __forceinline__ void pair_tile(int t, int tiles_m, int tiles_n, int s
     tm = first + t - tn * height;
 }
 
-template <class EPI, int PL, int TN>
+// CHUNKS: sums leave tensor memory every g.chunk stages and go on in registers.
+template <class EPI, int PL, int TN, bool CHUNKS>
 __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                            const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z, const TileArgs g,
                                                            const EPI epi) {
@@ -339,7 +340,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     static_assert((2 * S + 12 + 2) * 8 <= PAIR_BARRIERS, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x & 1), pairs = (int)(gridDim.x >> 1);
-    const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK, chunk = PL == 2 ? g.chunk : blocks;
+    const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK, chunk = CHUNKS ? g.chunk : blocks;
     const int tiles_m = (g.out_rows + 255) / 256, tiles_n = (g.out_cols + TN - 1) / TN, count = (g.symmetric ? symmetric_tiles<TN>(tiles_m, tiles_n) : tiles_m * tiles_n) * g.batch * g.split;
 
     if (threadIdx.x == 0) {
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
     let_next_kernel_start();
     wait_for_previous_kernel();
 
-    // Split products keep 64 sums a thread.  Registers are dealt anew among the warpgroups: 4 * 128 * 104 + 128 * 56 = 60416 of the
+    // Sums taken in chunks are 64 a thread.  Registers are dealt anew among the warpgroups: 4 * 128 * 104 + 128 * 56 = 60416 of the
     // 640 * 96 = 61440 the block was launched with.  (Each at the head of its warpgroup's own code: the compiler counts registers by
     // what it can reach.)
     if (warp >= PAIR_EPI_WARPS) {
@@ -497,7 +498,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) gemm_pair_kernel(const __grid
                     }
                 }
             };
-            if constexpr (PL == 2) {
+            if constexpr (CHUNKS) {
                 float acc[CQ];
 #pragma unroll
                 for (int j = 0; j < CQ; ++j) acc[j] = 0.0f;
@@ -631,7 +632,7 @@ static bool result_maps(const PartialOut& e, const GemmShape& s, CUtensorMap* y,
     return result_map<float>(e.y, s.rows, s.cols, e.ld, (long long)s.batch * e.parts, e.batch, y, true);
 }
 
-template <class EPI, int PL, int TN>
+template <class EPI, int PL, int TN, bool CHUNKS>
 static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, int split, cudaStream_t st) {
     const bool symmetric = s.symmetric && std::is_same<EPI, PlanesOut>::value;
     TileArgs g = {};
@@ -644,7 +645,7 @@ static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmSha
     g.a_mn = A.mn_major;
     g.b_mn = B.mn_major;
     g.bf16 = bf16;
-    g.chunk = s.chunk;
+    g.chunk = PL == 2 ? s.chunk : GEMM_LONG;
     g.wait_limit = device_wait_limit();
     g.test_flags = device_test_flags();
     const long long side = (s.rows + 255) / 256, across = (s.cols + TN - 1) / TN, tiles = (symmetric ? side * (side + 1) / 2 * (256 / TN) - (side * (256 / TN) - across) : side * across) * s.batch * split;
@@ -653,7 +654,7 @@ static int launch_pair(const GemmOperand& A, const GemmOperand& B, const GemmSha
     if (!gemm_operand_map(A, s.rows, s.red, s.batch, 128, bf16, &a) || !gemm_operand_map(B, s.cols, s.red, s.batch, TN / 2, bf16, &b)) return EBS_ERR_CUDA;
     g.packs = result_maps(epi, s, &y, &z);
     if (symmetric && !g.packs) return EBS_ERR_CUDA;               // (kept planes always have whole rows)
-    auto kern = gemm_pair_kernel<EPI, PL, TN>;
+    auto kern = gemm_pair_kernel<EPI, PL, TN, CHUNKS>;
     constexpr int bytes = pair_smem_bytes<PL, TN>();
     static_assert(bytes <= 227 * 1024, "shared memory of a block");
     static bool attr_set[64] = {};
@@ -716,16 +717,28 @@ __global__ void __launch_bounds__(256, EPI::HOLES ? 4 : 0) reduce_parts_kernel(c
         }
     }
 }
+// (16-bit operands, and parts: tiles of 256 columns)
+template <class EPI, int PL>
+static int launch_pair_form(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, int tn, int split, cudaStream_t st) {
+    if constexpr (PL == 2) {
+        if constexpr (!std::is_same<EPI, PartialOut>::value)
+            if (tn == 128) return launch_pair<EPI, PL, 128, true>(A, B, s, epi, bf16, split, st);
+        return launch_pair<EPI, PL, 256, true>(A, B, s, epi, bf16, split, st);
+    } else {
+        const int stages = ((s.red + GEMM_BK - 1) / GEMM_BK + split - 1) / split;
+        return stages > GEMM_LONG ? launch_pair<EPI, PL, 256, true>(A, B, s, epi, bf16, split, st) : launch_pair<EPI, PL, 256, false>(A, B, s, epi, bf16, split, st);
+    }
+}
 template <class EPI, int PL>
 static int launch_pair_or_parts(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, bool packs, const GemmRoute& route, float* scratch, cudaStream_t st) {
-    if (route.split == 1) return route.tn == 128 ? launch_pair<EPI, PL, 128>(A, B, s, epi, bf16, 1, st) : launch_pair<EPI, PL, 256>(A, B, s, epi, bf16, 1, st);
+    if (route.split == 1) return launch_pair_form<EPI, PL>(A, B, s, epi, bf16, route.tn, 1, st);
     PartialOut p;
     p.y = scratch;
     p.ld = (s.cols + 7) & ~7LL;
     p.batch = p.ld * s.rows;
     p.part = p.batch * s.batch;
     p.parts = route.split;
-    const int rc = launch_pair<PartialOut, PL, 256>(A, B, s, p, bf16, route.split, st);
+    const int rc = launch_pair_form<PartialOut, PL>(A, B, s, p, bf16, 256, route.split, st);
     if (rc) return rc;
     const long long items = (long long)((s.cols + EPI::N - 1) / EPI::N) * s.rows, blocks = EPI::HOLES ? (s.rows + 31LL) / 32 * ((s.cols + 31) / 32) : (items + 255) / 256;
     return launch_chained(reduce_parts_kernel<EPI>, dim3((unsigned)(blocks < 4096 ? blocks : 4096), s.batch), 256, 0, st, 1, p, route.split, s.rows, s.cols, (int)packs, epi);

@@ -5,6 +5,7 @@
 //  - Split products (PL = 2: operands as two fp16 planes hi + lo): three MMAs a step, hi*hi + hi*lo + lo*hi.  The tensor core
 //    truncates when it adds to an accumulator, so that long sums drift by their length; every few (GemmShape::chunk) stages the accumulator
 //    is therefore taken out and added up in registers, rounded to nearest, while the MMAs go on in a second one.
+//  - Long sums of 16-bit operands leave the tensor core likewise, every GEMM_LONG stages.
 //  - Few result rows (SWAP): the operand with many rows takes the 128 lanes, the few rows the N side of the MMA.  Such products
 //    are bound by the bytes of the large operand.
 //  - Few tiles and a long reduction: up to eight thread blocks of a cluster take a part of the reduction each; the sums meet in
@@ -28,16 +29,16 @@ struct TileLaunch {
     unsigned second;                                             // first thread block of the second product
 };
 
-template <class EPI, int TN, int PL, bool SWAP>
+template <class EPI, int TN, int PL, bool SWAP, bool CHUNKS>
 __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant__ TileLaunch<EPI> launch) {
-    // SWAP: lanes are the result's columns
+    // SWAP: lanes are the result's columns.  CHUNKS: sums leave tensor memory every g.chunk stages and go on in registers
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full[8], empty[8], acc_full[2], acc_empty[2], received;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     constexpr int STAGE = tile_stage_bytes<TN, PL>();
     constexpr int A_BYTES = 128 * GEMM_ROW_BYTES, B_BYTES = TN * GEMM_ROW_BYTES;
-    constexpr int COLS = PL * TN < 32 ? 32 : PL * TN;            // TMEM columns: one accumulator, or two taken in turn
+    constexpr int COLS = (CHUNKS ? 2 : 1) * TN < 32 ? 32 : (CHUNKS ? 2 : 1) * TN;            // TMEM columns: one accumulator, or two taken in turn
     uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int which = blockIdx.x >= launch.second;
@@ -57,7 +58,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     const int blocks = (g.red + GEMM_BK - 1) / GEMM_BK;
     const int kb0 = (int)((long long)blocks * part / split), kb1 = (int)((long long)blocks * (part + 1) / split);
     const int nkb = kb1 - kb0;
-    const int chunk = PL == 2 ? g.chunk : (nkb > 0 ? nkb : 1);
+    const int chunk = CHUNKS ? g.chunk : (nkb > 0 ? nkb : 1);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < g.stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
@@ -77,7 +78,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     let_next_kernel_start();
     wait_for_previous_kernel();
 
-    float acc[PL == 2 ? TN / 2 : 1];                              // (split products: this thread's sums)
+    float acc[CHUNKS ? TN / 2 : 1];                               // (this thread's sums)
     // How the results are shared out at the end: warps 0-7, a thread keeps its pack of columns and takes rows STRIDE apart, what the next one
     // needs from memory on its way.  One small loop: unrolled over eight rows the code of a tile's end, run once, took 2.5 us to arrive from
     // the second-level cache (128 x 128 results; 9 us from memory).
@@ -125,11 +126,11 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
         const uint32_t a_step = g.a_mn ? 2048 >> 4 : 32 >> 4, b_step = g.b_mn ? 2048 >> 4 : 32 >> 4;
         for (int i = 0; i < nkb; ++i) {
             const int s = i % g.stages, c = i / chunk, in_chunk = i - c * chunk;
-            if (PL == 2 && in_chunk == 0 && c >= 2 && !mbar_wait_warp(&acc_empty[c & 1], ((c >> 1) & 1) ^ 1, &abort_flag, g.wait_limit)) break;
+            if (CHUNKS && in_chunk == 0 && c >= 2 && !mbar_wait_warp(&acc_empty[c & 1], ((c >> 1) & 1) ^ 1, &abort_flag, g.wait_limit)) break;
             if (!mbar_wait_warp(&full[s], (i / g.stages) & 1, &abort_flag, g.wait_limit)) break;
             asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
             if (g.test_flags & 1) continue;                       // (give-up test: nothing is ever issued)
-            const uint32_t d = tmem + (PL == 2 ? (uint32_t)((c & 1) * TN) : 0u);
+            const uint32_t d = tmem + (CHUNKS ? (uint32_t)((c & 1) * TN) : 0u);
             const uint32_t base = smem_u32(tiles) + s * STAGE;
             const uint32_t ah = tile_desc_lo(base, g.a_mn), bh = tile_desc_lo(base + PL * A_BYTES, g.b_mn);
             if (PL == 2)                                          // (the small products first: each MMA truncates at the size of what is there)
@@ -147,7 +148,7 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     } else {
         const uint32_t row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * (TN / 2);
         bool ok = true;
-        if (PL == 2) {
+        if (CHUNKS) {
 #pragma unroll
             for (int j = 0; j < TN / 2; ++j) acc[j] = 0.0f;
             const int chunks = (nkb + chunk - 1) / chunk;
@@ -178,12 +179,12 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
     if (warp < 8 && !abort_flag) {
         const uint32_t row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * (TN / 2);
         const int l = (warp & 3) * 32 + lane, n0 = (warp >> 2) * (TN / 2);
-        uint32_t raw[PL == 2 ? 1 : TN / 2];
-        if constexpr (PL == 1) tmem_load<TN / 2>(row, raw);
+        uint32_t raw[CHUNKS ? 1 : TN / 2];
+        if constexpr (!CHUNKS) tmem_load<TN / 2>(row, raw);
 #pragma unroll
         for (int j = 0; j < TN / 2; j += 8) {
             float f[8];
-            if (PL == 2) {
+            if (CHUNKS) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] = acc[j + e];
             } else {
@@ -321,7 +322,7 @@ static int tile_product(TileLaunch<EPI>* l, int which, const GemmOperand& A, con
     g.a_mn = la.mn_major;
     g.b_mn = lb.mn_major;
     g.bf16 = bf16;
-    g.chunk = s.chunk;
+    g.chunk = A.planes == 2 ? s.chunk : GEMM_LONG;
     g.packs = packs;
     g.wait_limit = device_wait_limit();
     g.test_flags = device_test_flags();
@@ -333,7 +334,7 @@ static int tile_product(TileLaunch<EPI>* l, int which, const GemmOperand& A, con
     return gemm_operand_map(la, lanes, s.red, s.batch, 128, bf16, &l->a[which]) && gemm_operand_map(lb, columns, s.red, s.batch, f.tn, bf16, &l->b[which]) ? EBS_OK : EBS_ERR_CUDA;
 }
 
-template <class EPI, int TN, int PL, bool SWAP>
+template <class EPI, int TN, int PL, bool SWAP, bool CHUNKS>
 static int launch_tile(TileLaunch<EPI>& l, unsigned blocks, int cluster, cudaStream_t st) {
     constexpr int STAGE = tile_stage_bytes<TN, PL>();
     constexpr int EXCHANGE = (SWAP ? TN * 132 : 128 * (TN + 4)) * 4;
@@ -346,7 +347,7 @@ static int launch_tile(TileLaunch<EPI>& l, unsigned blocks, int cluster, cudaStr
         if (g.stages > deepest) deepest = g.stages;
     }
     const int sums = cluster > 1 ? 2 * EXCHANGE : EXCHANGE, bytes = (deepest * STAGE > sums ? deepest * STAGE : sums) + 1024;
-    auto kern = gemm_tile_kernel<EPI, TN, PL, SWAP>;
+    auto kern = gemm_tile_kernel<EPI, TN, PL, SWAP, CHUNKS>;
     static bool attr_set[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
@@ -356,15 +357,25 @@ static int launch_tile(TileLaunch<EPI>& l, unsigned blocks, int cluster, cudaStr
     }
     return launch_chained(kern, dim3(blocks), 320, (size_t)bytes, st, cluster, l);
 }
+template <class EPI, int PL, bool CHUNKS>
+static int launch_tile_chunks(TileLaunch<EPI>& l, unsigned blocks, const TileForm& f, cudaStream_t st) {
+    if (f.swap) {
+        if (f.tn == 16) return launch_tile<EPI, 16, PL, true, CHUNKS>(l, blocks, f.split, st);
+        if (f.tn == 32) return launch_tile<EPI, 32, PL, true, CHUNKS>(l, blocks, f.split, st);
+        return launch_tile<EPI, 64, PL, true, CHUNKS>(l, blocks, f.split, st);
+    }
+    if (f.tn == 64) return launch_tile<EPI, 64, PL, false, CHUNKS>(l, blocks, f.split, st);
+    return launch_tile<EPI, 128, PL, false, CHUNKS>(l, blocks, f.split, st);
+}
 template <class EPI, int PL>
 static int launch_tile_form(TileLaunch<EPI>& l, unsigned blocks, const TileForm& f, cudaStream_t st) {
-    if (f.swap) {
-        if (f.tn == 16) return launch_tile<EPI, 16, PL, true>(l, blocks, f.split, st);
-        if (f.tn == 32) return launch_tile<EPI, 32, PL, true>(l, blocks, f.split, st);
-        return launch_tile<EPI, 64, PL, true>(l, blocks, f.split, st);
+    if constexpr (PL == 2) {
+        return launch_tile_chunks<EPI, PL, true>(l, blocks, f, st);
+    } else {
+        bool whole = true;
+        for (const TileArgs& g : l.g) whole = whole && ((g.red + GEMM_BK - 1) / GEMM_BK + g.split - 1) / g.split <= GEMM_LONG;
+        return whole ? launch_tile_chunks<EPI, PL, false>(l, blocks, f, st) : launch_tile_chunks<EPI, PL, true>(l, blocks, f, st);
     }
-    if (f.tn == 64) return launch_tile<EPI, 64, PL, false>(l, blocks, f.split, st);
-    return launch_tile<EPI, 128, PL, false>(l, blocks, f.split, st);
 }
 template <class EPI, int PL>
 static int launch_one(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const EPI& epi, bool bf16, bool packs, cudaStream_t st) {

@@ -539,3 +539,47 @@ def test_fp32_infinities_along_long_reductions(ebs, m, n, k):
     run_forward(ebs, x, w, None, None, "f32", "none", y)
     assert torch.equal(y, w[:, at].T * sign[:, None] * math.inf)
     assert ebs.ebs_check_device_status() == ebs.EBS_OK
+
+
+def one_sign(rows, cols, t, g):
+    """Values of 1/16 .. 1/4: columns of different size, so that the results' mantissas are spread."""
+    return ((torch.rand((rows, cols), generator=g, device="cuda") * 0.5 + 0.5) * 2.0 ** (torch.rand(cols, generator=g, device="cuda") - 3)).to(t)
+
+
+def long_bound(ref, t, terms):
+    """The tensor core adds 16 products at a time and truncates: each of the 256 additions of a sum of up to 4096 terms loses at most 2^-23 of what it
+    ends at, together 2^-15.  Such sums, `terms` / 4096 at most, are added in fp32 and rounded to nearest
+    (2^-24 each, and a few for parts that meet); the output is rounded once."""
+    return ref * (torch.finfo(t).eps / 2 + 2.0 ** -15 + (terms / 4096 + 16) * 2.0 ** -24)
+
+
+# rows of dy, n, k: tiles on few blocks, a cluster's parts, pairs, parts through memory; a reduction that ends inside a stage
+LONG = [(131072, 16, 144), (200711, 64, 577), (50176, 128, 1152), (200000, 300, 264), (32768, 2304, 2304), (8256, 2304, 2304), (8192, 2304, 2304), (70001, 5, 7)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("m,n,k", LONG)
+def test_long_sums_of_one_sign(ebs, m, n, k, dtype):
+    """Weight gradients over many rows, all terms of one sign: what the tensor core truncates does not add up along the reduction."""
+    t, g = TYPES[dtype], gen(29)
+    dy, x = one_sign(m, n, t, g), one_sign(m, k, t, g)
+    dw, db = torch.empty((n, k), dtype=t, device="cuda"), torch.empty(n, dtype=t, device="cuda")
+    d = ebs.linear_desc(m, n, k, *codes(ebs, dtype, "none"))
+    ebs.ebs_linear_backward(dy, x, None, None, d, None, dw, db, workspace(ebs, d, True))
+    some = torch.arange(0, n, max(1, n // 64), device="cuda")
+    ref = dy[:, some].double().T @ x.double()
+    assert ((dw[some].double() - ref).abs() <= long_bound(ref, t, m)).all()
+    ref = dy.double().sum(0)
+    assert ((db.double() - ref).abs() <= long_bound(ref, t, m)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(3, 200, 131080), (40, 200, 131080), (200, 300, 70000), (2304, 2304, 16456)])
+def test_long_products_of_one_sign(ebs, m, n, k, dtype):
+    t, g = TYPES[dtype], gen(31)
+    x, w = one_sign(m, k, t, g), one_sign(n, k, t, g)
+    y = torch.empty((m, n), dtype=t, device="cuda")
+    run_forward(ebs, x, w, None, None, dtype, "none", y)
+    some = torch.arange(0, m, max(1, m // 64), device="cuda")
+    ref = x[some].double() @ w.double().T
+    assert ((y[some].double() - ref).abs() <= long_bound(ref, t, k)).all()
