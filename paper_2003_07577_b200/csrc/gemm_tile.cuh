@@ -23,7 +23,6 @@ struct TileTask {
 int launch_gemm_tiles(const TileTask (&t)[2], const GemmOut (&out)[2], int dtype, cudaStream_t st);
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const PlanesOut& out, cudaStream_t st);
 int launch_gemm_tile(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const FinalOut& out, int dtype, cudaStream_t st);
-unsigned long long gemm_tile_timeouts();
 
 // How a product is run: the pair kernel on tiles of 256 x tn, with its reduction in `split` parts that meet in `scratch` bytes of memory, or the tile kernel.
 struct GemmRoute {
@@ -35,7 +34,6 @@ GemmRoute gemm_route(const GemmShape& s, int planes);
 int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmRoute& r, float* scratch, const GemmOut& out, int dtype, cudaStream_t st);
 int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmRoute& r, float* scratch, const PlanesOut& out, cudaStream_t st);
 int launch_gemm_pair(const GemmOperand& A, const GemmOperand& B, const GemmShape& s, const GemmRoute& r, float* scratch, const FinalOut& out, int dtype, cudaStream_t st);
-unsigned long long gemm_pair_timeouts();
 
 // y = x W^T for one row of x of 16-bit values, or up to four of fp32; all operands as they are.
 int launch_gemm_rows(const void* x, long long ldx, const void* w, long long ldw, int m, int n, int k, const GemmOut& o, int dtype, cudaStream_t st);

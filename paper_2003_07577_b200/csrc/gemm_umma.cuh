@@ -243,19 +243,11 @@ struct TypedFinal {
     }
 };
 
-// A part of the sums, for reduce_parts: fp32, the parts behind one another.
+// A part of the sums, for reduce_parts: fp32, the parts behind one another (the pair kernel alone writes them).
 struct PartialOut {
-    static constexpr int N = 4;
-    struct Columns {};
-    struct Ahead {};
     float* y;                              // [part][batch][rows][ld], ld a multiple of four
     long long ld, batch, part;
     int parts;
-    __device__ __forceinline__ void columns(int, int, bool, Columns&) const {}
-    __device__ __forceinline__ void ahead(int, long long, int, int, bool, Ahead&) const {}
-    __device__ __forceinline__ void pack(int b, long long row, int col, int, bool, float (&v)[N], const Columns&, const Ahead&) const {
-        *reinterpret_cast<float4*>(y + b * batch + row * ld + col) = make_float4(v[0], v[1], v[2], v[3]);
-    }
 };
 
 // ebs_test_set_device_wait's settings.
