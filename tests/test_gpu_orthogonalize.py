@@ -216,3 +216,14 @@ def test_nan_and_infinity_cross_a_cluster(ebs, bad):
     out = run(ebs, g)
     assert torch.isnan(out[1]).all()
     assert torch.equal(out[0], clean[0]) and torch.equal(out[2], clean[2])
+
+
+# A few steps, whose tolerance is far below what 11 bits leave: X and Q on matrices of full rank, A where one singular value is all of G
+FEW_STEPS = [(None, 2, COEFF), (None, 3, (1.875, -1.25, 0.375)), (1, 1, COEFF), (2, 2, COEFF)]
+
+
+@pytest.mark.parametrize("rank,steps,coeff", FEW_STEPS)
+@pytest.mark.parametrize("shape", [(1, 64, 576), (9, 576, 64), (1, 128, 1152), (2, 300, 700), (1, 700, 300), (1, 512, 1024), (1, 768, 770), (1, 2100, 1900)])
+def test_few_steps_keep_both_planes(ebs, shape, rank, steps, coeff):
+    g = make(*shape, torch.float32, 21, rank)
+    check(run(ebs, g, steps, coeff), iterate64(g, steps, coeff), steps, coeff)

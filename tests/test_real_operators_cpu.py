@@ -140,3 +140,42 @@ def test_orthogonalize_sides_beyond_the_index_range(ebs):
         assert ortho(ebs, batch=1, rows=rows, cols=cols, ws_bytes=1 << 62) == ebs.EBS_ERR_OVERFLOW
         assert ebs.ebs_orthogonalize_workspace_bytes(1, rows, cols, 0, 5) == 0
     assert ebs.ebs_orthogonalize_workspace_bytes(1, 1 << 30, 1, 0, 5) > 0
+
+
+def first_plane(t):
+    """What is left of a matrix kept as its first fp16 plane alone."""
+    scale = 2.0 ** 13 / 2.0 ** math.ceil(math.log2(float(t.abs().max())))
+    return (t * scale).half().double() / scale
+
+
+def orthogonalize_without(g, steps, coeff, matrix, step):
+    """The iteration in 64 bits, but for one matrix of one step that lost its second plane."""
+    a, b, c = coeff
+    x = g.double() / (g.double().norm() + 1e-7)
+    for i in range(steps):
+        lost = lambda name, t: first_plane(t) if (name, i) == (matrix, step) else t  # noqa: E731
+        s = x @ x.T
+        p = lost("A", s)
+        q = lost("Q", a * torch.eye(len(s), dtype=torch.float64) + b * p + c * (p @ p))
+        x = q @ lost("X", x)
+    return x.float()[None]
+
+
+def test_orthogonalize_tolerance_notices_a_lost_plane():
+    """The tolerance of the tests with a few steps (test_gpu_orthogonalize.py) passes the iteration and none that lost a plane."""
+    from test_gpu_orthogonalize import FEW_STEPS, check, iterate64
+    gen = torch.Generator().manual_seed(0)
+    noticed = set()
+    for rows, cols in ((64, 576), (128, 1152), (300, 700)):
+        for rank, steps, coeff in FEW_STEPS:
+            g = torch.randn((rows, cols), generator=gen) if rank is None else torch.randn((rows, rank), generator=gen) @ torch.randn((rank, cols), generator=gen)
+            ref = iterate64(g[None], steps, coeff)
+            check(orthogonalize_without(g, steps, coeff, None, 0), ref, steps, coeff)
+            for matrix in "XAQ":
+                for step in range(steps):
+                    try:
+                        check(orthogonalize_without(g, steps, coeff, matrix, step), ref, steps, coeff)
+                    except AssertionError:
+                        noticed.add((rows, matrix, rank))
+    for rows in (64, 128, 300):
+        assert {(rows, "X", None), (rows, "Q", None), (rows, "X", 1), (rows, "Q", 1), (rows, "A", 1)} <= noticed
