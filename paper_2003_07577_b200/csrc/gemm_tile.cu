@@ -124,26 +124,30 @@ __global__ void __launch_bounds__(320, 1) gemm_tile_kernel(const __grid_constant
         const uint32_t leader = elect_one() ? 1u : 0u;
         const uint32_t idesc = gemm_idesc(128, TN, g.bf16, g.a_mn, g.b_mn);
         const uint32_t a_step = g.a_mn ? 2048 >> 4 : 32 >> 4, b_step = g.b_mn ? 2048 >> 4 : 32 >> 4;
-        for (int i = 0; i < nkb; ++i) {
-            const int s = i % g.stages, c = i / chunk, in_chunk = i - c * chunk;
+        for (int i = 0, c = 0, in_chunk = 0; i < nkb; ++i) {
+            const int s = i % g.stages;
             if (CHUNKS && in_chunk == 0 && c >= 2 && !mbar_wait_warp(&acc_empty[c & 1], ((c >> 1) & 1) ^ 1, &abort_flag, g.wait_limit)) break;
             if (!mbar_wait_warp(&full[s], (i / g.stages) & 1, &abort_flag, g.wait_limit)) break;
             asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
-            if (g.test_flags & 1) continue;                       // (give-up test: nothing is ever issued)
+            const int first = in_chunk;
             const uint32_t d = tmem + (CHUNKS ? (uint32_t)((c & 1) * TN) : 0u);
+            uint64_t* out = &acc_full[c & 1];
+            const bool last = ++in_chunk == chunk || i == nkb - 1;
+            if (last) { in_chunk = 0; ++c; }
+            if (g.test_flags & 1) continue;                       // (give-up test: nothing is ever issued)
             const uint32_t base = smem_u32(tiles) + s * STAGE;
             const uint32_t ah = tile_desc_lo(base, g.a_mn), bh = tile_desc_lo(base + PL * A_BYTES, g.b_mn);
             if (PL == 2)                                          // (the small products first: each MMA truncates at the size of what is there)
 #pragma unroll
                 for (int k = 0; k < GEMM_BK / 16; ++k) {
                     const uint32_t a = ah + k * a_step, b = bh + k * b_step;
-                    umma_f16(leader, d, a, b + (B_BYTES >> 4), idesc, (in_chunk | k) != 0);
+                    umma_f16(leader, d, a, b + (B_BYTES >> 4), idesc, (first | k) != 0);
                     umma_f16(leader, d, a + (A_BYTES >> 4), b, idesc, 1u);
                 }
 #pragma unroll
-            for (int k = 0; k < GEMM_BK / 16; ++k) umma_f16(leader, d, ah + k * a_step, bh + k * b_step, idesc, PL == 2 || (in_chunk | k) != 0);
+            for (int k = 0; k < GEMM_BK / 16; ++k) umma_f16(leader, d, ah + k * a_step, bh + k * b_step, idesc, PL == 2 || (first | k) != 0);
             umma_commit_pred(leader, &empty[s]);
-            if (in_chunk == chunk - 1 || i == nkb - 1) umma_commit_pred(leader, &acc_full[c & 1]);
+            if (last) umma_commit_pred(leader, out);
         }
     } else {
         const uint32_t row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * (TN / 2);
