@@ -583,3 +583,12 @@ def test_long_products_of_one_sign(ebs, m, n, k, dtype):
     some = torch.arange(0, m, max(1, m // 64), device="cuda")
     ref = x[some].double() @ w.double().T
     assert ((y[some].double() - ref).abs() <= long_bound(ref, t, k)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(2304, 2304, 4168), (2304, 2305, 5000), (40, 200, 5000), (200, 72, 4097), (1, 300, 9000)])
+def test_long_products_with_every_part(ebs, m, n, k, dtype):
+    """Sums that leave the tensor core in chunks, behind bias, activation, residual and kept z, into rows on 16 bytes and anywhere."""
+    check_forward(ebs, m, n, k, dtype, "gelu")
+    check_forward(ebs, m, n, k, dtype, "silu", pads=(3, 0, 1, 2, 5))
+    check_forward(ebs, m, n, k, dtype, "none", False, True, False, in_place=True)

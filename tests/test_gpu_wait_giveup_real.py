@@ -65,3 +65,15 @@ def test_orthogonalize(ebs, shape):
     out = torch.empty_like(x)
     ws = torch.empty(ebs.ebs_orthogonalize_workspace_bytes(*shape, ebs.EBS_BF16, 5), dtype=torch.uint8, device="cuda")
     give_up_and_recover(ebs, lambda: ebs.ebs_orthogonalize(x, *shape, ebs.EBS_BF16, 5, COEFF, 1e-7, 1.0, out, ws), out, 1)
+
+
+# 16-bit sums in chunks: tiles, a cluster's parts, pairs, parts through memory
+@pytest.mark.parametrize("m,n,k", [(40, 20000, 4500), (40, 200, 40000), (4096, 2048, 4500), (300, 264, 200000)])
+def test_long_sums(ebs, m, n, k):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(13)
+    x, w = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((m, k), (n, k)))
+    y = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
+    d = ebs.linear_desc(m, n, k, ebs.EBS_BF16, ebs.EBS_ACT_NONE)
+    ws = torch.empty(max(ebs.ebs_linear_workspace_bytes(d, False), 16), dtype=torch.uint8, device="cuda")
+    give_up_and_recover(ebs, lambda: ebs.ebs_linear_forward(x, w, None, None, d, y, None, ws), y, 1)
