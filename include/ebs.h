@@ -432,6 +432,42 @@ int ebs_orthogonalize(const void *g_dev, int batch, int rows, int cols, int dtyp
                       float scale, void *out_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
+ * Clipping of all gradients of a network by their norm, before an update (the paper has no counterpart):
+ *   norm = sqrt(sum of g^2 over all tensors),  f = norm <= max_norm ? 1 : max_norm / norm,  out = f g
+ * The sum is taken in 64 bits (squares of 16 bytes of elements are added in fp32 first, where that is accurate to 2^-22 of
+ * their sum); f is rounded to fp32, f g to fp32 and to the tensor's type.  f = 1 leaves a tensor clipped in place as it is and
+ * copies any other.  An infinite norm gives f = 0 (infinite gradients become NaN, as 0 * inf has it) unless max_norm is infinite
+ * too, a NaN norm makes every gradient NaN.  norm_dev is one fp32 value; a norm beyond that type's range is stored as infinity, f is right all the same.
+ *
+ * A tensor has `rows` rows of `cols` elements of `dtype` (EBS_F32, EBS_F16, EBS_BF16), ld_* elements from one row to the next
+ * (0: dense); what lies between rows is neither read nor written.  Either size may be 0: an empty tensor.  Addresses are
+ * multiples of the element's size (rows whose places in `in` and `out` differ modulo 16 bytes are written an element at a time).
+ * out may be the gradient itself (same address and stride); no output may share an element with any other tensor.
+ *
+ * The tensors of a network are laid out once:
+ *   ebs_clip_plan       checks `count` tensors (HOST array) and writes their work list, *chunks records of
+ *                       EBS_CLIP_CHUNK_BYTES each, to plan_host, which holds *chunks records before the call; plan_host = NULL: only
+ *                       counts them.  Host arithmetic alone: the caller copies the list to the device, and it stays valid
+ *                       as long as the tensors' addresses do.
+ *   ebs_clip_gradients  plan_dev: the list in device memory, of exactly `chunks` records.  max_norm >= 0 (infinity: the norm alone,
+ *                       with copies where out is not the gradient).  workspace_dev: ebs_clip_workspace_bytes(chunks) bytes of device
+ *                       memory; a call leaves nothing in it that another one reads.
+ * Sums are taken in an order that goes by the plan alone.
+ */
+#define EBS_CLIP_CHUNK_BYTES 48
+typedef struct ebs_clip_tensor {
+    const void *in_dev;
+    void *out_dev;
+    long long rows, cols;
+    long long ld_in, ld_out;
+    int dtype;
+} ebs_clip_tensor;
+int ebs_clip_plan(const ebs_clip_tensor *tensors, int count, void *plan_host, long long *chunks);
+size_t ebs_clip_workspace_bytes(long long chunks);
+int ebs_clip_gradients(const void *plan_dev, long long chunks, float max_norm, float *norm_dev, void *workspace_dev,
+                       size_t workspace_bytes, void *stream);
+
+/*
  * Expected operation count of a layer during the search (Eq. 11):
  * FLOP(sum_i coeff_w[i] bits_w[i], sum_j coeff_x[j] bits_x[j]) with FLOP(M, K) = macs * M * K
  * (Sec. 4.3: s n c_o M K AND operations).  Host arithmetic in double; negative on bad arguments.

@@ -38,7 +38,9 @@ EXPORTS = [
     "ebs_graph_begin", "ebs_graph_end", "ebs_graph_launch", "ebs_graph_destroy",
     "ebs_linear_workspace_bytes", "ebs_linear_forward", "ebs_linear_backward",
     "ebs_orthogonalize_workspace_bytes", "ebs_orthogonalize",
+    "ebs_clip_plan", "ebs_clip_workspace_bytes", "ebs_clip_gradients",
 ]
+EBS_CLIP_CHUNK_BYTES = 48
 
 
 class ebs_conv_desc(ctypes.Structure):
@@ -59,6 +61,11 @@ class ebs_linear_desc(ctypes.Structure):
     _fields_ = [("m", ctypes.c_int), ("n", ctypes.c_int), ("k", ctypes.c_int), ("dtype", ctypes.c_int), ("act", ctypes.c_int),
                 ("ldx", ctypes.c_longlong), ("ldw", ctypes.c_longlong), ("ldy", ctypes.c_longlong),
                 ("ldr", ctypes.c_longlong), ("ldz", ctypes.c_longlong)]
+
+
+class ebs_clip_tensor(ctypes.Structure):
+    _fields_ = [("in_dev", ctypes.c_void_p), ("out_dev", ctypes.c_void_p), ("rows", ctypes.c_longlong), ("cols", ctypes.c_longlong),
+                ("ld_in", ctypes.c_longlong), ("ld_out", ctypes.c_longlong), ("dtype", ctypes.c_int)]
 
 
 class EbsError(RuntimeError):
@@ -142,6 +149,11 @@ def lib() -> ctypes.CDLL:
         L.ebs_orthogonalize_workspace_bytes.argtypes = [i, i, i, i, i]
         L.ebs_orthogonalize_workspace_bytes.restype = z
         L.ebs_orthogonalize.argtypes = [p, i, i, i, i, i, fp, f, f, p, p, z, p]
+        ll = ctypes.c_longlong
+        L.ebs_clip_plan.argtypes = [ctypes.POINTER(ebs_clip_tensor), i, p, ctypes.POINTER(ll)]
+        L.ebs_clip_workspace_bytes.argtypes = [ll]
+        L.ebs_clip_workspace_bytes.restype = z
+        L.ebs_clip_gradients.argtypes = [p, ll, f, p, p, z, p]
         _lib = L
     return _lib
 
@@ -157,7 +169,8 @@ def _native():
         L = lib()
         names = ("ebs_pack_acts", "ebs_pack_acts_s2d", "ebs_conv2d_mixed", "ebs_conv2d_mixed_variant", "ebs_dequant",
                  "ebs_global_avgpool", "ebs_maxpool_packed", "ebs_resnet_cifar_forward", "ebs_search_weight_forward",
-                 "ebs_search_act_forward", "ebs_graph_launch", "ebs_linear_forward", "ebs_linear_backward", "ebs_orthogonalize")
+                 "ebs_search_act_forward", "ebs_graph_launch", "ebs_linear_forward", "ebs_linear_backward", "ebs_orthogonalize",
+                 "ebs_clip_gradients")
         torch.cuda.init()                                  # the stream lookups below need torch's CUDA state
         _fastcall.bind({k: ctypes.cast(getattr(L, k), ctypes.c_void_p).value for k in names},
                        torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, ebs_conv_desc, ebs_epilogue, ebs_fused_head,
@@ -457,6 +470,66 @@ def ebs_orthogonalize(g_dev, batch: int, rows: int, cols: int, dtype: int, steps
     rc = (_fast or _native()).orthogonalize(g_dev, batch, rows, cols, dtype, steps, coeff, eps, scale, out_dev, workspace_dev, stream)
     if rc:
         _check(rc, "ebs_orthogonalize")
+
+
+class ClipPlan:
+    """The work list of ebs_clip_gradients for the tensors it was made of, which it keeps."""
+
+    def __init__(self, plan_dev: torch.Tensor, chunks: int, tensors):
+        self.plan_dev, self.chunks, self.tensors = plan_dev, chunks, tensors
+
+
+_REAL_TYPES = {torch.float32: EBS_F32, torch.float16: EBS_F16, torch.bfloat16: EBS_BF16}
+
+
+def _clip_rows(t: torch.Tensor):
+    """A tensor as rows of neighbouring elements: (rows, columns, stride of the rows)."""
+    if t.numel() == 0 or t.is_contiguous():
+        return 1, t.numel(), t.numel()
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("a tensor is dense, or a matrix whose rows are")
+    return t.shape[0], t.shape[1], t.stride(0)
+
+
+def ebs_clip_plan(tensors, plan_host: Optional[torch.Tensor] = None, chunks: int = 0) -> int:
+    """tensors: list of ebs_clip_tensor; returns the number of records (plan_host: uint8 host tensor they are written to)."""
+    arr, n = (ebs_clip_tensor * max(1, len(tensors)))(*tensors), ctypes.c_longlong(chunks)
+    _check(lib().ebs_clip_plan(arr, len(tensors), _ptr(plan_host), ctypes.byref(n)), "ebs_clip_plan")
+    return n.value
+
+
+def clip_plan(tensors, outs=None) -> ClipPlan:
+    """The plan that clips `tensors` into `outs` (None: in place), on the tensors' device."""
+    outs = tensors if outs is None else outs
+    if len(outs) != len(tensors):
+        raise ValueError("one output for each tensor")
+    records, device = [], None
+    for t, o in zip(tensors, outs):
+        if t.dtype not in _REAL_TYPES or o.dtype != t.dtype or o.shape != t.shape or o.device != t.device:
+            raise ValueError("gradients are fp32, fp16 or bf16, an output has its gradient's type, shape and device")
+        if not t.is_cuda or (device is not None and t.device != device):
+            raise ValueError("all gradients are on one GPU")
+        device = t.device
+        (rows, cols, ld), (rows_out, cols_out, ld_out) = _clip_rows(t), _clip_rows(o)
+        if rows != rows_out:                                   # (one of the two is dense, the other a matrix of strided rows)
+            rows, cols = t.shape
+            ld, ld_out = t.stride(0), o.stride(0)
+        records.append(ebs_clip_tensor(t.data_ptr(), o.data_ptr(), rows, cols, ld, ld_out, _REAL_TYPES[t.dtype]))
+    chunks = ebs_clip_plan(records)
+    host = torch.empty(max(1, chunks) * EBS_CLIP_CHUNK_BYTES, dtype=torch.uint8)
+    ebs_clip_plan(records, host, chunks)
+    return ClipPlan(host.to(device if device is not None else "cuda"), chunks, (list(tensors), list(outs)))
+
+
+def ebs_clip_workspace_bytes(plan) -> int:
+    """plan: a ClipPlan, or its number of records."""
+    return lib().ebs_clip_workspace_bytes(plan.chunks if isinstance(plan, ClipPlan) else plan)
+
+
+def ebs_clip_gradients(plan: ClipPlan, max_norm: float, norm_dev: torch.Tensor, workspace_dev: torch.Tensor, stream=None) -> None:
+    rc = (_fast or _native()).clip_gradients(plan.plan_dev, plan.chunks, max_norm, norm_dev, workspace_dev, stream)
+    if rc:
+        _check(rc, "ebs_clip_gradients")
 
 
 class CaptureStream:

@@ -1,0 +1,316 @@
+// Norm of all gradients of a network and their clipping.  See include/ebs.h.
+//
+// Bound by the bytes: one pass reads every gradient for the sum of squares, one reads it again and writes it.  The work list ("plan") cuts all
+// tensors into chunks of up to CLIP_CHUNK elements, a record each, so that a block learns from one 48-byte load what to do next, however many
+// tensors there are and whatever their sizes.  The second pass takes the chunks from the last to the first: what the first pass read last is still in
+// the second-level cache.
+//
+// The sum is taken in 64 bits.  A pack of 16 bytes is squared and added in fp32 first (relative error 2^-22 of the pack at most), unless that sum
+// leaves the range where neither an overflow nor a lost small square matters; then each square is taken in 64 bits.  Partial sums are added in
+// an order that goes by the plan alone.
+#include <algorithm>
+#include <cstring>
+#include <new>
+
+#include "tensors.cuh"
+
+namespace ebs {
+
+constexpr int CLIP_CHUNK = 8192;            // elements
+constexpr int CLIP_BLOCKS = 148 * 8;        // at most: a wave of blocks of 256 threads
+constexpr int CLIP_THREADS = 256;
+
+// rows = 1: the block's threads share the row; more: a warp takes a row.
+struct alignas(16) ClipChunk {
+    const void* in;
+    void* out;
+    long long ld_in, ld_out;
+    int rows, cols, dtype, pad;
+};
+static_assert(sizeof(ClipChunk) == EBS_CLIP_CHUNK_BYTES, "chunk record");
+
+__device__ __forceinline__ ClipChunk load_chunk(const ClipChunk* p) {
+    const uint4* q = reinterpret_cast<const uint4*>(p);
+    union { uint4 u[3]; ClipChunk c; } v;
+    v.u[0] = q[0]; v.u[1] = q[1]; v.u[2] = q[2];
+    return v.c;
+}
+
+// The sum of the squares of one pack.
+template <typename T>
+__device__ __forceinline__ void add_squares(const uint4& u, double& sum) {
+    constexpr int N = Pack<T>::N;
+    float v[N], s = 0.0f;
+    unpack<T>(u, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s = fmaf(v[i], v[i], s);
+    // (below 1e-28 a square of the pack may be lost that matters, above 1e37 one may be infinite that is not)
+    if (s >= 1e-28f && s <= 1e37f) sum += (double)s;
+    else if (((u.x | u.y | u.z | u.w) & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) != 0u)
+#pragma unroll 1
+        for (int i = 0; i < N; ++i) {
+            const double d = (double)to_f32(reinterpret_cast<const T*>(&u)[i]);
+            sum += d * d;
+        }
+}
+template <typename T>
+__device__ __forceinline__ void add_square(T x, double& sum) {
+    const double d = (double)to_f32(x);
+    sum += d * d;
+}
+// Elements before the first 16-byte boundary of a row (its elements lie on multiples of their size).
+template <typename T>
+__device__ __forceinline__ int head_of(const T* p, int cols) {
+    const int h = (int)((16u - ((unsigned)(uintptr_t)p & 15u)) & 15u) / (int)sizeof(T);
+    return h < cols ? h : cols;
+}
+constexpr int CLIP_UNROLL = 4;              // packs of a thread under way
+
+template <typename T>
+__device__ __forceinline__ void row_squares(const T* p, int cols, int t, int step, double& sum) {
+    constexpr int N = Pack<T>::N;
+    const int head = head_of(p, cols), packs = (cols - head) / N, tail = head + packs * N;
+    const uint4* q = reinterpret_cast<const uint4*>(p + head);
+    int i = t;
+    for (; i + (CLIP_UNROLL - 1) * step < packs; i += CLIP_UNROLL * step) {
+        uint4 u[CLIP_UNROLL];
+#pragma unroll
+        for (int j = 0; j < CLIP_UNROLL; ++j) u[j] = q[i + j * step];
+#pragma unroll
+        for (int j = 0; j < CLIP_UNROLL; ++j) add_squares<T>(u[j], sum);
+    }
+    for (; i < packs; i += step) add_squares<T>(q[i], sum);
+    if (t < head) add_square(p[t], sum);
+    if (tail + t < cols) add_square(p[tail + t], sum);        // (a head and a tail have fewer elements than a warp has lanes)
+}
+template <typename T>
+__device__ __forceinline__ void chunk_squares(const ClipChunk& c, double& sum) {
+    const T* p = static_cast<const T*>(c.in);
+    if (c.rows == 1) row_squares(p, c.cols, threadIdx.x, CLIP_THREADS, sum);
+    else
+        for (int r = threadIdx.x >> 5; r < c.rows; r += CLIP_THREADS / 32) row_squares(p + r * c.ld_in, c.cols, threadIdx.x & 31, 32, sum);
+}
+__device__ __forceinline__ double block_sum(double v) {
+    __shared__ double part[CLIP_THREADS / 32];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int i = 0; i < CLIP_THREADS / 32; ++i) v += part[i];
+    return v;
+}
+
+__global__ void __launch_bounds__(CLIP_THREADS) clip_norm_kernel(const ClipChunk* __restrict__ chunks, long long count, double* __restrict__ partial) {
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    double sum = 0.0;
+    for (long long i = blockIdx.x; i < count; i += gridDim.x) {
+        const ClipChunk c = load_chunk(chunks + i);
+        if (c.dtype == EBS_F32) chunk_squares<float>(c, sum);
+        else if (c.dtype == EBS_F16) chunk_squares<__half>(c, sum);
+        else chunk_squares<__nv_bfloat16>(c, sum);
+    }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+}
+
+template <typename T>
+__device__ __forceinline__ void scale_pack(uint4& u, float f) {
+    float v[Pack<T>::N];
+    unpack<T>(u, v);
+#pragma unroll
+    for (int i = 0; i < Pack<T>::N; ++i) v[i] *= f;
+    store_pack(reinterpret_cast<T*>(&u), v);
+}
+template <typename T>
+__device__ __forceinline__ void row_scale(const T* p, T* to, int cols, int t, int step, float f) {
+    constexpr int N = Pack<T>::N;
+    if ((((uintptr_t)p ^ (uintptr_t)to) & 15u) != 0) {        // in and out never on a boundary together
+        for (int i = t; i < cols; i += step) to[i] = from_f32<T>(to_f32(p[i]) * f);
+        return;
+    }
+    const int head = head_of(p, cols), packs = (cols - head) / N, tail = head + packs * N;
+    const uint4* q = reinterpret_cast<const uint4*>(p + head);
+    uint4* r = reinterpret_cast<uint4*>(to + head);
+    int i = t;
+    for (; i + (CLIP_UNROLL - 1) * step < packs; i += CLIP_UNROLL * step) {
+        uint4 u[CLIP_UNROLL];
+#pragma unroll
+        for (int j = 0; j < CLIP_UNROLL; ++j) u[j] = q[i + j * step];
+#pragma unroll
+        for (int j = 0; j < CLIP_UNROLL; ++j) {
+            scale_pack<T>(u[j], f);
+            r[i + j * step] = u[j];
+        }
+    }
+    for (; i < packs; i += step) {
+        uint4 u = q[i];
+        scale_pack<T>(u, f);
+        r[i] = u;
+    }
+    if (t < head) to[t] = from_f32<T>(to_f32(p[t]) * f);
+    if (tail + t < cols) to[tail + t] = from_f32<T>(to_f32(p[tail + t]) * f);
+}
+template <typename T>
+__device__ __forceinline__ void chunk_scale(const ClipChunk& c, float f) {
+    const T* p = static_cast<const T*>(c.in);
+    T* to = static_cast<T*>(c.out);
+    if (c.rows == 1) row_scale(p, to, c.cols, threadIdx.x, CLIP_THREADS, f);
+    else
+        for (int r = threadIdx.x >> 5; r < c.rows; r += CLIP_THREADS / 32) row_scale(p + r * c.ld_in, to + r * c.ld_out, c.cols, threadIdx.x & 31, 32, f);
+}
+
+__global__ void __launch_bounds__(CLIP_THREADS) clip_scale_kernel(const ClipChunk* __restrict__ chunks, long long count, const double* __restrict__ partial, int parts,
+                                                                  float max_norm, float* __restrict__ norm_out) {
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < parts; i += CLIP_THREADS) sum += partial[i];
+    const double norm = sqrt(block_sum(sum));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+    const float f = norm <= (double)max_norm ? 1.0f : (float)((double)max_norm / norm);      // (a NaN norm: NaN)
+    for (long long i = (long long)count - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
+        const ClipChunk c = load_chunk(chunks + i);
+        if (f == 1.0f && c.in == c.out) continue;
+        if (c.dtype == EBS_F32) chunk_scale<float>(c, f);
+        else if (c.dtype == EBS_F16) chunk_scale<__half>(c, f);
+        else chunk_scale<__nv_bfloat16>(c, f);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- the plan
+// A tensor with its strides filled in; rows that lie one behind the other are one row.
+static int complete_tensor(const ebs_clip_tensor& in, ebs_clip_tensor* t) {
+    *t = in;
+    if (t->rows < 0 || t->cols < 0 || !real_dtype(t->dtype)) return EBS_ERR_INVALID_ARG;
+    if (t->ld_in == 0) t->ld_in = t->cols;
+    if (t->ld_out == 0) t->ld_out = t->cols;
+    if (t->ld_in < t->cols || t->ld_out < t->cols) return EBS_ERR_INVALID_ARG;
+    const long long limit = 1LL << 40;
+    if (t->cols > limit || t->rows > limit) return EBS_ERR_OVERFLOW;
+    if (t->rows == 0 || t->cols == 0) {
+        t->rows = t->cols = 0;
+        return EBS_OK;
+    }
+    if (t->ld_in > limit / t->rows || t->ld_out > limit / t->rows) return EBS_ERR_OVERFLOW;
+    const uintptr_t size = element_size(t->dtype);
+    if (!t->in_dev || !t->out_dev || (uintptr_t)t->in_dev % size || (uintptr_t)t->out_dev % size) return EBS_ERR_INVALID_ARG;
+    if (t->in_dev == t->out_dev && t->ld_in != t->ld_out) return EBS_ERR_INVALID_ARG;
+    if (t->rows > 1 && t->ld_in == t->cols && t->ld_out == t->cols) {
+        t->cols *= t->rows;
+        t->ld_in = t->ld_out = t->cols;
+        t->rows = 1;
+    }
+    return EBS_OK;
+}
+static long long row_segments(const ebs_clip_tensor& t) { return (t.cols + CLIP_CHUNK - 1) / CLIP_CHUNK; }
+static long long rows_of_chunk(const ebs_clip_tensor& t) {
+    const long long r = CLIP_CHUNK / t.cols;
+    return t.rows == 1 || r < 1 ? 1 : r;
+}
+static long long tensor_chunks(const ebs_clip_tensor& t) {
+    if (t.rows == 0) return 0;
+    return (t.rows + rows_of_chunk(t) - 1) / rows_of_chunk(t) * row_segments(t);
+}
+// What a tensor reads or writes, in bytes.
+struct Extent {
+    uintptr_t begin, end, pitch, width;
+    int tensor;
+    bool out;
+};
+static bool share(const Extent& a, const Extent& b) {
+    if (a.pitch != b.pitch) return true;                        // (their extents meet: the caller knows)
+    const uintptr_t d = (b.begin - a.begin) % a.pitch;          // b begins behind a
+    return !(d >= a.width && a.pitch - d >= b.width);
+}
+
+}  // namespace ebs
+
+using namespace ebs;
+
+extern "C" {
+
+int ebs_clip_plan(const ebs_clip_tensor* tensors, int count, void* plan_host, long long* chunks) {
+    if (!chunks || count < 0 || (count && !tensors)) return EBS_ERR_INVALID_ARG;
+    long long total = 0;
+    for (int i = 0; i < count; ++i) {
+        ebs_clip_tensor t;
+        const int rc = complete_tensor(tensors[i], &t);
+        if (rc) return rc;
+        total += tensor_chunks(t);
+        if (total > (1LL << 31)) return EBS_ERR_OVERFLOW;
+    }
+    // no output may share an element with another tensor: extents in the order of their addresses
+    Extent* e = new (std::nothrow) Extent[2 * (size_t)count + 1];
+    if (!e) return EBS_ERR_OVERFLOW;
+    int n = 0;
+    for (int i = 0; i < count; ++i) {
+        ebs_clip_tensor t;
+        complete_tensor(tensors[i], &t);
+        if (t.rows == 0) continue;
+        const uintptr_t size = element_size(t.dtype);
+        for (int out = 0; out < 2; ++out) {
+            const uintptr_t p = (uintptr_t)(out ? t.out_dev : t.in_dev), ld = (uintptr_t)(out ? t.ld_out : t.ld_in);
+            e[n++] = Extent{p, p + ((uintptr_t)(t.rows - 1) * ld + (uintptr_t)t.cols) * size, ld * size, (uintptr_t)t.cols * size, i, out == 1};
+        }
+    }
+    std::sort(e, e + n, [](const Extent& a, const Extent& b) { return a.begin < b.begin; });
+    bool apart = true;
+    for (int i = 0; i < n && apart; ++i)
+        for (int j = i + 1; j < n && e[j].begin < e[i].end && apart; ++j) {
+            if (!e[i].out && !e[j].out) continue;
+            if (e[i].tensor == e[j].tensor && e[i].begin == e[j].begin) continue;             // (in place)
+            apart = !share(e[i], e[j]);
+        }
+    delete[] e;
+    if (!apart) return EBS_ERR_INVALID_ARG;
+    if (plan_host) {
+        if (*chunks < total) return EBS_ERR_INVALID_ARG;
+        char* to = static_cast<char*>(plan_host);
+        for (int i = 0; i < count; ++i) {
+            ebs_clip_tensor t;
+            complete_tensor(tensors[i], &t);
+            if (t.rows == 0) continue;
+            const long long size = (long long)element_size(t.dtype), step = rows_of_chunk(t);
+            for (long long r = 0; r < t.rows; r += step)
+                for (long long c = 0; c < t.cols; c += CLIP_CHUNK) {
+                    ClipChunk k = {};
+                    k.in = static_cast<const char*>(t.in_dev) + (r * t.ld_in + c) * size;
+                    k.out = static_cast<char*>(t.out_dev) + (r * t.ld_out + c) * size;
+                    k.ld_in = t.ld_in;
+                    k.ld_out = t.ld_out;
+                    k.rows = (int)(t.rows - r < step ? t.rows - r : step);
+                    k.cols = (int)(t.cols - c < CLIP_CHUNK ? t.cols - c : CLIP_CHUNK);
+                    k.dtype = t.dtype;
+                    memcpy(to, &k, sizeof(k));
+                    to += sizeof(k);
+                }
+        }
+    }
+    *chunks = total;
+    return EBS_OK;
+}
+
+size_t ebs_clip_workspace_bytes(long long chunks) {
+    if (chunks < 0 || chunks > (1LL << 31)) return 0;
+    return round256((size_t)(chunks < 1 ? 1 : chunks < CLIP_BLOCKS ? chunks : CLIP_BLOCKS) * sizeof(double));
+}
+
+int ebs_clip_gradients(const void* plan_dev, long long chunks, float max_norm, float* norm_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
+    if (chunks < 0 || chunks > (1LL << 31) || (chunks && !plan_dev) || !norm_dev || !workspace_dev || !(max_norm >= 0.0f)) return EBS_ERR_INVALID_ARG;
+    if (!aligned16(plan_dev) || ((uintptr_t)norm_dev & 3u) || !aligned16(workspace_dev) || workspace_bytes < ebs_clip_workspace_bytes(chunks)) return EBS_ERR_INVALID_ARG;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const ClipChunk* plan = static_cast<const ClipChunk*>(plan_dev);
+    double* partial = static_cast<double*>(workspace_dev);
+    const int blocks = (int)(chunks < CLIP_BLOCKS ? chunks : CLIP_BLOCKS);
+    if (blocks) {
+        const int rc = launch_chained(clip_norm_kernel, dim3((unsigned)blocks), CLIP_THREADS, 0, st, 1, plan, chunks, partial);
+        if (rc) return rc;
+    }
+    return launch_chained(clip_scale_kernel, dim3((unsigned)(blocks ? blocks : 1)), CLIP_THREADS, 0, st, 1, plan, chunks, (const double*)partial, blocks, max_norm, norm_dev);
+}
+
+}  // extern "C"

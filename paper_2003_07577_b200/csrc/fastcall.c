@@ -23,6 +23,9 @@ EACH_ENTRY(DECLARE_ENTRY)
 /* The real-valued operators: bound where `bind` is given their descriptor type and addresses. */
 #define EACH_REAL_ENTRY(X) X(ebs_linear_forward) X(ebs_linear_backward) X(ebs_orthogonalize)
 EACH_REAL_ENTRY(DECLARE_ENTRY)
+/* Those around layers of experts: bound where `bind` finds their addresses. */
+#define EACH_EXPERT_ENTRY(X) X(ebs_clip_gradients)
+EACH_EXPERT_ENTRY(DECLARE_ENTRY)
 
 /* Device or host address of a tensor argument; None is the null pointer. */
 static int as_ptr(PyObject *o, void **out) {
@@ -306,6 +309,18 @@ FAST(orthogonalize) {
     CALL(p_ebs_orthogonalize(g, i[0], i[1], i[2], i[3], i[4], c, eps, scale, out, ws, bytes, st));
 }
 
+FAST(clip_gradients) {
+    void *plan, *norm, *ws, *st;
+    size_t bytes;
+    float max_norm;
+    if (!arg_count(n, 6) || !bound(p_ebs_clip_gradients) || !as_ptr(a[0], &plan)) return NULL;
+    const long long chunks = PyLong_AsLongLong(a[1]);
+    if ((chunks == -1 && PyErr_Occurred()) || !as_float(a[2], &max_norm) || !as_ptr(a[3], &norm) || !as_workspace(a[4], &ws, &bytes) ||
+        !as_stream(a[5], &st))
+        return NULL;
+    CALL(p_ebs_clip_gradients(plan, chunks, max_norm, norm, ws, bytes, st));
+}
+
 /* same_bytes(structs, bytes): whether the concatenated contents of the structures are exactly `bytes`. */
 FAST(same_bytes) {
     if (!arg_count(n, 2)) return NULL;
@@ -362,6 +377,8 @@ static PyObject *bind(PyObject *self, PyObject *args) {
         if (!p_##name) return PyErr_Occurred() ? NULL : PyErr_Format(PyExc_ValueError, "null address: %s", #name);    \
     }
     EACH_ENTRY(BIND_ENTRY)
+#define BIND_IF_THERE(name) if (PyDict_GetItemString(addr, #name)) BIND_ENTRY(name)
+    EACH_EXPERT_ENTRY(BIND_IF_THERE)
     if (linear) {
         EACH_REAL_ENTRY(BIND_ENTRY)
         Py_INCREF(linear);
@@ -395,6 +412,7 @@ static PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, NULL},
                                 FAST_METHOD(linear_forward),
                                 FAST_METHOD(linear_backward),
                                 FAST_METHOD(orthogonalize),
+                                FAST_METHOD(clip_gradients),
                                 FAST_METHOD(same_bytes),
                                 FAST_METHOD(same_addresses),
                                 {NULL, NULL, 0, NULL}};

@@ -2,34 +2,12 @@
 #include <type_traits>
 
 #include "gemm_tile.cuh"
+#include "tensors.cuh"
 
 namespace ebs {
 
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-static size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
-
-// One tensor of a call: `rows` rows of `cols` elements, `ld` elements apart.
-struct Rows {
-    const void* p;
-    long long rows, cols, ld;
-    bool out;
-};
-
-// Whether two tensors share an element.  Rows of the same stride may interleave (column ranges of one buffer).
-static bool overlap(const Rows& a, const Rows& b, size_t size) {
-    if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0) return false;
-    const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
-    const uintptr_t ea = pa + ((a.rows - 1) * a.ld + a.cols) * size, eb = pb + ((b.rows - 1) * b.ld + b.cols) * size;
-    if (pa >= eb || pb >= ea) return false;
-    if (a.ld != b.ld) return true;
-    const long long pitch = a.ld * (long long)size;
-    long long d = ((long long)(pb - pa)) % pitch;
-    if (d < 0) d += pitch;
-    return !(d >= a.cols * (long long)size && pitch - d >= b.cols * (long long)size);
-}
-
 // The descriptor with its strides filled in, or an error.
-static int complete(const ebs_linear_desc* in, ebs_linear_desc* d) {
+int complete_linear(const ebs_linear_desc* in, ebs_linear_desc* d) {
     if (!in) return EBS_ERR_INVALID_ARG;
     *d = *in;
     if (d->m < 0 || d->n < 1 || d->k < 1 || !real_dtype(d->dtype) || d->act < EBS_ACT_NONE || d->act > EBS_ACT_SILU)
@@ -46,39 +24,8 @@ static int complete(const ebs_linear_desc* in, ebs_linear_desc* d) {
     return EBS_OK;
 }
 
-static int check_tensors(const Rows* t, int count, size_t size, const Rows* same_a, const Rows* same_b) {
-    for (int i = 0; i < count; ++i) {
-        if (!aligned16(t[i].p)) return EBS_ERR_INVALID_ARG;
-        for (int j = 0; j < i; ++j) {
-            if (!t[i].out && !t[j].out) continue;
-            if (((&t[i] == same_a && &t[j] == same_b) || (&t[j] == same_a && &t[i] == same_b)) && t[i].p == t[j].p && t[i].ld == t[j].ld) continue;
-            if (overlap(t[i], t[j], size)) return EBS_ERR_INVALID_ARG;
-        }
-    }
-    return EBS_OK;
-}
-
 // ---------------------------------------------------------------------------------------------------- operands
-// Takes buffers out of the workspace one behind the other; without a base it only counts.
-struct Carver {
-    char* base;
-    size_t used = 0;
-    template <typename T> T* take(size_t count) {
-        char* p = base ? base + used : nullptr;
-        used += round256(count * sizeof(T));
-        return reinterpret_cast<T*>(p);
-    }
-};
-static long long round8(long long v) { return (v + 7) & ~7LL; }
-
-// Copies of 16-bit rows whose stride is a multiple of 16 bytes: up to three matrices in one launch, 256 elements of a row a warp, all on
-// their way at once.
-struct CopyJobs {
-    const uint16_t* src[3];
-    uint16_t* dst[3];
-    long long ld[3], ldd[3], first[3], pieces;                // first: pieces of the matrices before
-    int cols[3], across[3], count;
-};
+// Copies of 16-bit rows: 256 elements of a row a warp, all on their way at once.
 __global__ void __launch_bounds__(256) copy_rows_kernel(const __grid_constant__ CopyJobs j) {
     let_next_kernel_start();
     wait_for_previous_kernel();
@@ -300,19 +247,22 @@ static Prepared plan_operand(const Matrix& m, int dtype, bool across, Carver& ws
     jobs->job[jobs->count++] = j;
     return out;
 }
+void add_copy_rows(CopyJobs* j, const void* src, void* dst, long long rows, int cols, long long ld, long long ldd) {
+    const int i = j->count++;
+    j->src[i] = static_cast<const uint16_t*>(src);
+    j->dst[i] = static_cast<uint16_t*>(dst);
+    j->ld[i] = ld;
+    j->ldd[i] = ldd;
+    j->cols[i] = cols;
+    j->across[i] = (cols + 255) / 256;
+    j->first[i] = j->pieces;
+    j->pieces += rows * j->across[i];
+}
 static void add_copy(CopyJobs* j, const Matrix& m, const Prepared& p) {
     if (!p.op.p || p.op.planes == 2 || p.op.p == m.p) return;
-    const int i = j->count++;
-    j->src[i] = static_cast<const uint16_t*>(m.p);
-    j->dst[i] = static_cast<uint16_t*>(const_cast<void*>(p.op.p));
-    j->ld[i] = m.ld;
-    j->ldd[i] = p.op.ld;
-    j->cols[i] = m.cols;
-    j->across[i] = (m.cols + 255) / 256;
-    j->first[i] = j->pieces;
-    j->pieces += m.rows * j->across[i];
+    add_copy_rows(j, m.p, const_cast<void*>(p.op.p), m.rows, m.cols, m.ld, p.op.ld);
 }
-static int launch_copies(const CopyJobs& j, cudaStream_t st) {
+int launch_copies(const CopyJobs& j, cudaStream_t st) {
     const long long blocks = (j.pieces + 7) / 8;
     return j.count ? launch_chained(copy_rows_kernel, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), 256, 0, st, 1, j) : EBS_OK;
 }
@@ -357,10 +307,6 @@ static GemmOut product_out(const Prepared& a, const Matrix& am, const Prepared& 
 }
 
 // ---------------------------------------------------------------------------------------------------- dz and dbias
-// A half-precision dz is kept halved where a slope may exceed one: the steepest (1.13) times the type's largest value would not fit.  That costs
-// dz below 2^-13 its last bit (multiples of 2^-23 instead of 2^-24); a rectified one is dy itself or zero and keeps all of them.
-static float dz_store_scale(const ebs_linear_desc& d) { return d.dtype == EBS_F16 && d.act > EBS_ACT_RELU ? 0.5f : 1.0f; }
-
 struct DzArgs {
     const void *dy, *z;
     long long ldy, ldz, lddz;
@@ -638,14 +584,14 @@ extern "C" {
 
 size_t ebs_linear_workspace_bytes(const ebs_linear_desc* desc, int backward) {
     ebs_linear_desc d;
-    if (complete(desc, &d)) return 0;
+    if (complete_linear(desc, &d)) return 0;
     return linear_workspace(d, backward != 0);
 }
 
 int ebs_linear_forward(const void* x, const void* w, const void* bias, const void* residual, const ebs_linear_desc* desc, void* y, void* z,
                        void* workspace, size_t workspace_bytes, void* stream) {
     ebs_linear_desc d;
-    const int rc = complete(desc, &d);
+    const int rc = complete_linear(desc, &d);
     if (rc) return rc;
     if (!w || (d.m > 0 && (!x || !y))) return EBS_ERR_INVALID_ARG;
     const size_t size = element_size(d.dtype), need = linear_workspace(d, false);
@@ -660,7 +606,7 @@ int ebs_linear_forward(const void* x, const void* w, const void* bias, const voi
 int ebs_linear_backward(const void* dy, const void* x, const void* w, const void* z, const ebs_linear_desc* desc, void* dx, void* dw, void* dbias,
                         void* workspace, size_t workspace_bytes, void* stream) {
     ebs_linear_desc d;
-    const int rc = complete(desc, &d);
+    const int rc = complete_linear(desc, &d);
     if (rc) return rc;
     if (!dx && !dw && !dbias && d.m > 0) return EBS_ERR_INVALID_ARG;
     if (d.m > 0 && (!dy || (dx && !w) || (dw && !x) || (d.act && !z))) return EBS_ERR_INVALID_ARG;
