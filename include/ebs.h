@@ -432,6 +432,45 @@ int ebs_orthogonalize(const void *g_dev, int batch, int rows, int cols, int dtyp
                       float scale, void *out_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
+ * Layers with weights of 4 bits, for answering: what a real-valued layer (or a layer of experts) becomes once it is trained.
+ * The paper's weights have one scale a layer and an integer product; here each `group` neighbouring weights of a row have a scale of
+ * their own, activations stay real, and the product is one of a few rows (tokens), bound by the weights' bytes.
+ *
+ *   pack      W [experts][n][k] of type w_dtype -> for each group of a row (the last one of a row may be shorter)
+ *               scale = max|w| * fl32(1/7), rounded to fp32 and to `dtype`,  code = floor(w / scale + 1/2) within -8 .. 7, exactly (codes of
+ *               a zero scale are 0).  A group with an infinity or a NaN (or whose scale overflows) stands for NaN throughout.
+ *   unpack    scale * code, rounded to w_dtype: what the packed weights stand for (a prompt of many rows multiplies them with
+ *               ebs_linear_forward or ebs_grouped_forward)
+ *   forward   y = act(x W_e^T + bias_e) + residual     x [m][k], bias [experts][n], residual and y [m][n], all of type `dtype`;
+ *               act as in ebs_linear_forward.  Rows offsets[e] .. offsets[e+1]-1 are expert e's; offsets_dev: int32
+ *               [experts + 1] in device memory, not decreasing; y keeps what it holds in rows that are no expert's.  NULL: one expert, all rows.
+ *               (Offsets out of order or out of 0 .. m lead to no access out of bounds; which expert's results rows then get is not defined.)
+ *
+ * Products of codes and activations are exact, their sums over up to 64 inputs are taken in fp32 by the tensor core (it truncates; 2^-21 of a sum of
+ * one sign at most), multiplied by the scale and added up in fp32.  EBS_F32 activations keep all their 24 bits.  Any number of rows is taken, up to
+ * 64 (EBS_F32: 32) at a time, each time with the expert's weights.  The order of sums goes by the sizes.  (Activations above 2^117 in EBS_F32 or
+ * EBS_BF16 may overflow before they meet the scale.)
+ *
+ * packed: ebs_q4_packed_bytes(desc) bytes, laid out for one kernel (its layout is not part of the interface).  ldw: elements
+ * between the rows of W (0: dense); experts follow one another, n rows each.  desc of the product: m, act, ldx, ldy, ldr (n, k and dtype as in
+ * the weights' descriptor).  Rows of x that start anywhere (ldx not a multiple of 16 bytes) are copied first: workspace_dev,
+ * ebs_linear_q4_workspace_bytes(desc, q4) bytes (0: may be NULL), used as in ebs_linear_forward.  y may be the residual itself; no output may
+ * overlap another tensor otherwise.
+ */
+typedef struct ebs_q4_desc {
+    int experts, n, k; /* weights [experts][n][k], each >= 1 */
+    int group;         /* weights of a row that share a scale: 32, 64 or 128 */
+    int dtype;         /* type of the scales and of the layer's activations: EBS_F32, EBS_F16, EBS_BF16 */
+} ebs_q4_desc;
+size_t ebs_q4_packed_bytes(const ebs_q4_desc *desc);
+int ebs_pack_weights_q4(const void *w_dev, int w_dtype, const ebs_q4_desc *desc, long long ldw, void *packed_dev, void *stream);
+int ebs_unpack_weights_q4(const void *packed_dev, const ebs_q4_desc *desc, void *w_dev, int w_dtype, long long ldw, void *stream);
+size_t ebs_linear_q4_workspace_bytes(const ebs_linear_desc *desc, const ebs_q4_desc *q4);
+int ebs_linear_q4_forward(const void *x_dev, const void *packed_dev, const void *bias_dev, const void *residual_dev,
+                          const int *offsets_dev, const ebs_linear_desc *desc, const ebs_q4_desc *q4, void *y_dev,
+                          void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
  * Clipping of all gradients of a network by their norm, before an update (the paper has no counterpart):
  *   norm = sqrt(sum of g^2 over all tensors),  f = norm <= max_norm ? 1 : max_norm / norm,  out = f g
  * The sum is taken in 64 bits (squares of 16 bytes of elements are added in fp32 first, where that is accurate to 2^-22 of

@@ -38,7 +38,8 @@ EXPORTS = [
     "ebs_graph_begin", "ebs_graph_end", "ebs_graph_launch", "ebs_graph_destroy",
     "ebs_linear_workspace_bytes", "ebs_linear_forward", "ebs_linear_backward",
     "ebs_orthogonalize_workspace_bytes", "ebs_orthogonalize",
-    "ebs_clip_plan", "ebs_clip_workspace_bytes", "ebs_clip_gradients",
+    "ebs_clip_plan", "ebs_clip_workspace_bytes", "ebs_clip_gradients", "ebs_q4_packed_bytes", "ebs_pack_weights_q4",
+    "ebs_unpack_weights_q4", "ebs_linear_q4_workspace_bytes", "ebs_linear_q4_forward",
 ]
 EBS_CLIP_CHUNK_BYTES = 48
 
@@ -61,6 +62,10 @@ class ebs_linear_desc(ctypes.Structure):
     _fields_ = [("m", ctypes.c_int), ("n", ctypes.c_int), ("k", ctypes.c_int), ("dtype", ctypes.c_int), ("act", ctypes.c_int),
                 ("ldx", ctypes.c_longlong), ("ldw", ctypes.c_longlong), ("ldy", ctypes.c_longlong),
                 ("ldr", ctypes.c_longlong), ("ldz", ctypes.c_longlong)]
+
+
+class ebs_q4_desc(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int), ("n", ctypes.c_int), ("k", ctypes.c_int), ("group", ctypes.c_int), ("dtype", ctypes.c_int)]
 
 
 class ebs_clip_tensor(ctypes.Structure):
@@ -154,6 +159,14 @@ def lib() -> ctypes.CDLL:
         L.ebs_clip_workspace_bytes.argtypes = [ll]
         L.ebs_clip_workspace_bytes.restype = z
         L.ebs_clip_gradients.argtypes = [p, ll, f, p, p, z, p]
+        QD = ctypes.POINTER(ebs_q4_desc)
+        L.ebs_q4_packed_bytes.argtypes = [QD]
+        L.ebs_q4_packed_bytes.restype = z
+        L.ebs_pack_weights_q4.argtypes = [p, i, QD, ll, p, p]
+        L.ebs_unpack_weights_q4.argtypes = [p, QD, p, i, ll, p]
+        L.ebs_linear_q4_workspace_bytes.argtypes = [LD, QD]
+        L.ebs_linear_q4_workspace_bytes.restype = z
+        L.ebs_linear_q4_forward.argtypes = [p, p, p, p, p, LD, QD, p, p, z, p]
         _lib = L
     return _lib
 
@@ -170,11 +183,11 @@ def _native():
         names = ("ebs_pack_acts", "ebs_pack_acts_s2d", "ebs_conv2d_mixed", "ebs_conv2d_mixed_variant", "ebs_dequant",
                  "ebs_global_avgpool", "ebs_maxpool_packed", "ebs_resnet_cifar_forward", "ebs_search_weight_forward",
                  "ebs_search_act_forward", "ebs_graph_launch", "ebs_linear_forward", "ebs_linear_backward", "ebs_orthogonalize",
-                 "ebs_clip_gradients")
+                 "ebs_clip_gradients", "ebs_pack_weights_q4", "ebs_unpack_weights_q4", "ebs_linear_q4_forward")
         torch.cuda.init()                                  # the stream lookups below need torch's CUDA state
         _fastcall.bind({k: ctypes.cast(getattr(L, k), ctypes.c_void_p).value for k in names},
                        torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, ebs_conv_desc, ebs_epilogue, ebs_fused_head,
-                       ebs_linear_desc)
+                       ebs_linear_desc, ebs_q4_desc)
         _fast = _fastcall
     return _fast
 
@@ -530,6 +543,37 @@ def ebs_clip_gradients(plan: ClipPlan, max_norm: float, norm_dev: torch.Tensor, 
     rc = (_fast or _native()).clip_gradients(plan.plan_dev, plan.chunks, max_norm, norm_dev, workspace_dev, stream)
     if rc:
         _check(rc, "ebs_clip_gradients")
+
+
+def q4_desc(n, k, group, dtype=EBS_F32, experts=1) -> ebs_q4_desc:
+    return ebs_q4_desc(experts, n, k, group, dtype)
+
+
+def ebs_q4_packed_bytes(desc: ebs_q4_desc) -> int:
+    return lib().ebs_q4_packed_bytes(ctypes.byref(desc))
+
+
+def ebs_pack_weights_q4(w_dev, w_dtype: int, desc: ebs_q4_desc, packed_dev, ldw: int = 0, stream=None) -> None:
+    rc = (_fast or _native()).pack_weights_q4(w_dev, w_dtype, desc, ldw, packed_dev, stream)
+    if rc:
+        _check(rc, "ebs_pack_weights_q4")
+
+
+def ebs_unpack_weights_q4(packed_dev, desc: ebs_q4_desc, w_dev, w_dtype: int, ldw: int = 0, stream=None) -> None:
+    rc = (_fast or _native()).unpack_weights_q4(packed_dev, desc, w_dev, w_dtype, ldw, stream)
+    if rc:
+        _check(rc, "ebs_unpack_weights_q4")
+
+
+def ebs_linear_q4_workspace_bytes(desc: ebs_linear_desc, q4: ebs_q4_desc) -> int:
+    return lib().ebs_linear_q4_workspace_bytes(ctypes.byref(desc), ctypes.byref(q4))
+
+
+def ebs_linear_q4_forward(x_dev, packed_dev, bias_dev, residual_dev, offsets_dev, desc: ebs_linear_desc, q4: ebs_q4_desc, y_dev,
+                          workspace_dev=None, stream=None) -> None:
+    rc = (_fast or _native()).linear_q4_forward(x_dev, packed_dev, bias_dev, residual_dev, offsets_dev, desc, q4, y_dev, workspace_dev, stream)
+    if rc:
+        _check(rc, "ebs_linear_q4_forward")
 
 
 class CaptureStream:

@@ -12,7 +12,7 @@
 
 #include "ebs.h"
 
-static PyObject *s_data_ptr, *s_cuda_stream, *s_nbytes, *f_raw_stream, *f_get_device, *t_desc, *t_epilogue, *t_head, *t_linear;
+static PyObject *s_data_ptr, *s_cuda_stream, *s_nbytes, *f_raw_stream, *f_get_device, *t_desc, *t_epilogue, *t_head, *t_linear, *t_q4;
 
 #define EACH_ENTRY(X)                                                                                                 \
     X(ebs_pack_acts) X(ebs_pack_acts_s2d) X(ebs_conv2d_mixed) X(ebs_conv2d_mixed_variant) X(ebs_dequant)              \
@@ -24,7 +24,7 @@ EACH_ENTRY(DECLARE_ENTRY)
 #define EACH_REAL_ENTRY(X) X(ebs_linear_forward) X(ebs_linear_backward) X(ebs_orthogonalize)
 EACH_REAL_ENTRY(DECLARE_ENTRY)
 /* Those around layers of experts: bound where `bind` finds their addresses. */
-#define EACH_EXPERT_ENTRY(X) X(ebs_clip_gradients)
+#define EACH_EXPERT_ENTRY(X) X(ebs_clip_gradients) X(ebs_pack_weights_q4) X(ebs_unpack_weights_q4) X(ebs_linear_q4_forward)
 EACH_EXPERT_ENTRY(DECLARE_ENTRY)
 
 /* Device or host address of a tensor argument; None is the null pointer. */
@@ -79,6 +79,10 @@ static int as_size(PyObject *o, size_t *out) {
 }
 /* A ctypes structure of the given type by value. */
 static int as_struct(PyObject *o, PyObject *type, void *out, size_t size) {
+    if (!type) {
+        PyErr_SetString(PyExc_RuntimeError, "structure type is not bound");
+        return 0;
+    }
     if (!PyObject_TypeCheck(o, (PyTypeObject *)type)) {
         PyErr_Format(PyExc_TypeError, "%s expected instead of %s", ((PyTypeObject *)type)->tp_name, Py_TYPE(o)->tp_name);
         return 0;
@@ -309,16 +313,56 @@ FAST(orthogonalize) {
     CALL(p_ebs_orthogonalize(g, i[0], i[1], i[2], i[3], i[4], c, eps, scale, out, ws, bytes, st));
 }
 
+static int as_long_long(PyObject *o, long long *out) {
+    *out = PyLong_AsLongLong(o);
+    return !(*out == -1 && PyErr_Occurred());
+}
 FAST(clip_gradients) {
     void *plan, *norm, *ws, *st;
     size_t bytes;
     float max_norm;
     if (!arg_count(n, 6) || !bound(p_ebs_clip_gradients) || !as_ptr(a[0], &plan)) return NULL;
-    const long long chunks = PyLong_AsLongLong(a[1]);
-    if ((chunks == -1 && PyErr_Occurred()) || !as_float(a[2], &max_norm) || !as_ptr(a[3], &norm) || !as_workspace(a[4], &ws, &bytes) ||
+    long long chunks;
+    if (!as_long_long(a[1], &chunks) || !as_float(a[2], &max_norm) || !as_ptr(a[3], &norm) || !as_workspace(a[4], &ws, &bytes) ||
         !as_stream(a[5], &st))
         return NULL;
     CALL(p_ebs_clip_gradients(plan, chunks, max_norm, norm, ws, bytes, st));
+}
+
+FAST(pack_weights_q4) {
+    void *w, *packed, *st;
+    int dtype;
+    long long ldw;
+    ebs_q4_desc q;
+    if (!arg_count(n, 6) || !bound(p_ebs_pack_weights_q4) || !as_ptr(a[0], &w) || !as_int(a[1], &dtype) || !as_struct(a[2], t_q4, &q, sizeof(q)) ||
+        !as_long_long(a[3], &ldw) || !as_ptr(a[4], &packed) || !as_stream(a[5], &st))
+        return NULL;
+    CALL(p_ebs_pack_weights_q4(w, dtype, &q, ldw, packed, st));
+}
+
+FAST(unpack_weights_q4) {
+    void *w, *packed, *st;
+    int dtype;
+    long long ldw;
+    ebs_q4_desc q;
+    if (!arg_count(n, 6) || !bound(p_ebs_unpack_weights_q4) || !as_ptr(a[0], &packed) || !as_struct(a[1], t_q4, &q, sizeof(q)) || !as_ptr(a[2], &w) ||
+        !as_int(a[3], &dtype) || !as_long_long(a[4], &ldw) || !as_stream(a[5], &st))
+        return NULL;
+    CALL(p_ebs_unpack_weights_q4(packed, &q, w, dtype, ldw, st));
+}
+
+FAST(linear_q4_forward) {
+    void *p[5], *y, *ws, *st;
+    size_t bytes;
+    ebs_linear_desc d;
+    ebs_q4_desc q;
+    if (!arg_count(n, 10) || !bound(p_ebs_linear_q4_forward)) return NULL;
+    for (int k = 0; k < 5; ++k)
+        if (!as_ptr(a[k], &p[k])) return NULL;
+    if (!as_struct(a[5], t_linear, &d, sizeof(d)) || !as_struct(a[6], t_q4, &q, sizeof(q)) || !as_ptr(a[7], &y) || !as_workspace(a[8], &ws, &bytes) ||
+        !as_stream(a[9], &st))
+        return NULL;
+    CALL(p_ebs_linear_q4_forward(p[0], p[1], p[2], p[3], p[4], &d, &q, y, ws, bytes, st));
 }
 
 /* same_bytes(structs, bytes): whether the concatenated contents of the structures are exactly `bytes`. */
@@ -362,12 +406,12 @@ FAST(same_addresses) {
     return same < 0 ? NULL : PyBool_FromLong(same);
 }
 
-/* bind(addresses, raw_stream, get_device, desc, epilogue, head[, linear]): library entry points by name, torch's raw current
- * stream of a device, torch's current device and the ctypes structure types (linear: with the real-valued operators). */
+/* bind(addresses, raw_stream, get_device, desc, epilogue, head[, linear[, q4]]): library entry points by name, torch's raw current
+ * stream of a device, torch's current device and the ctypes structure types (linear, q4: with the real-valued operators). */
 static PyObject *bind(PyObject *self, PyObject *args) {
-    PyObject *addr, *raw, *dev, *desc, *epi, *head, *linear = NULL;
-    if (!PyArg_ParseTuple(args, "O!OOO!O!O!|O!", &PyDict_Type, &addr, &raw, &dev, &PyType_Type, &desc, &PyType_Type, &epi,
-                          &PyType_Type, &head, &PyType_Type, &linear))
+    PyObject *addr, *raw, *dev, *desc, *epi, *head, *linear = NULL, *q4 = NULL;
+    if (!PyArg_ParseTuple(args, "O!OOO!O!O!|O!O!", &PyDict_Type, &addr, &raw, &dev, &PyType_Type, &desc, &PyType_Type, &epi,
+                          &PyType_Type, &head, &PyType_Type, &linear, &PyType_Type, &q4))
         return NULL;
 #define BIND_ENTRY(name)                                                                                              \
     {                                                                                                                 \
@@ -379,6 +423,10 @@ static PyObject *bind(PyObject *self, PyObject *args) {
     EACH_ENTRY(BIND_ENTRY)
 #define BIND_IF_THERE(name) if (PyDict_GetItemString(addr, #name)) BIND_ENTRY(name)
     EACH_EXPERT_ENTRY(BIND_IF_THERE)
+    if (q4) {
+        Py_INCREF(q4);
+        Py_XSETREF(t_q4, q4);
+    }
     if (linear) {
         EACH_REAL_ENTRY(BIND_ENTRY)
         Py_INCREF(linear);
@@ -413,6 +461,9 @@ static PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, NULL},
                                 FAST_METHOD(linear_backward),
                                 FAST_METHOD(orthogonalize),
                                 FAST_METHOD(clip_gradients),
+                                FAST_METHOD(pack_weights_q4),
+                                FAST_METHOD(unpack_weights_q4),
+                                FAST_METHOD(linear_q4_forward),
                                 FAST_METHOD(same_bytes),
                                 FAST_METHOD(same_addresses),
                                 {NULL, NULL, 0, NULL}};

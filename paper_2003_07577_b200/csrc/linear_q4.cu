@@ -1,0 +1,629 @@
+// Layers with weights of 4 bits and a scale for each group of them: packing, reading back, and the product with a few rows.  See include/ebs.h.
+//
+// The product is bound by the weights' bytes (half a byte a weight and the scales), and next by the instructions that turn codes into operands.  Weights lie in
+// tiles of 16 outputs x 64 inputs, 512 bytes, in the order in which the lanes of a warp need them for four mma.sync m16n8k16: one 16-byte
+// load a lane.  A word holds the eight codes (+ 8) of a lane for one MMA, those of operand register i in bits 4i .. 4i+3 and 16+4i .. 16+4i+3, so that a mask and the bits of
+// a power of two make two 16-bit numbers of them at once.  Codes and 16-bit activations multiply exactly; a tile's sum over 64 inputs (32, where
+// a group has no more) leaves the MMA in fp32 and is multiplied by its group's scale there.  fp32 activations go as three bf16 planes of
+// 8 bits each, which hold all 24.
+//
+// MMA k index (step s, half h, lane group t = lane % 4, element j) stands for input (s / 2) * 32 + t * 8 + (s % 2) * 4 + h * 2 + j of the 64: a lane's share
+// of a row of activations is two runs of eight neighbouring elements, which it loads from the row as it lies in memory.
+#include "gemm_tile.cuh"
+#include "tensors.cuh"
+
+namespace ebs {
+
+constexpr int Q4_ROWS = 16, Q4_K = 64, Q4_TILE_BYTES = 512;
+
+struct Q4Layout {
+    int tiles, kbs, groups;                // tiles of 16 outputs, of 64 inputs, groups of a row
+    size_t codes, scales;                  // bytes of all experts' codes (rounded up), of their scales
+};
+static Q4Layout q4_layout(const ebs_q4_desc& d) {
+    Q4Layout l;
+    l.tiles = (d.n + Q4_ROWS - 1) / Q4_ROWS;
+    l.kbs = (d.k + Q4_K - 1) / Q4_K;
+    l.groups = (d.k + d.group - 1) / d.group;
+    l.codes = round256((size_t)d.experts * l.tiles * l.kbs * Q4_TILE_BYTES);
+    l.scales = (size_t)d.experts * l.tiles * l.groups * Q4_ROWS * element_size(d.dtype);
+    return l;
+}
+static int check_q4(const ebs_q4_desc* d) {
+    if (!d || d->experts < 1 || d->n < 1 || d->k < 1 || !real_dtype(d->dtype)) return EBS_ERR_INVALID_ARG;
+    if (d->group != 32 && d->group != 64 && d->group != 128) return EBS_ERR_INVALID_ARG;
+    if (d->n > (1 << 30) || d->k > (1 << 30) || (double)d->experts * d->n * d->k > (double)(1LL << 40)) return EBS_ERR_OVERFLOW;
+    const Q4Layout l = q4_layout(*d);
+    if ((long long)d->experts * l.tiles * l.kbs >= (1LL << 34)) return EBS_ERR_OVERFLOW;
+    return EBS_OK;
+}
+
+// ---------------------------------------------------------------------------------------------------- packing
+// Input of element e (0 .. 7) of run r (0, 1) of a lane; its code lies in word 2 * r + e / 4 of the lane's four.
+__device__ __forceinline__ int q4_input(int r, int lane, int e) { return r * 32 + (lane & 3) * 8 + e; }
+
+// Eight neighbouring elements of a row, of which `left` exist.
+template <typename S>
+__device__ __forceinline__ void load8(const S* p, int left, bool vec, float (&v)[8]) {
+    if (vec && left >= 8) {
+        constexpr int N = Pack<S>::N;
+#pragma unroll
+        for (int i = 0; i < 8 / N; ++i) {
+            float t[N];
+            load_pack<S>(p + i * N, t);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[i * N + e] = t[e];
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? to_f32(p[e]) : 0.0f;
+}
+
+// floor(w / s + 1/2) within -8 .. 7, exactly: the quotient by the reciprocal is off by a rounding or two, the remainders of a
+// fused multiply-add tell on which side of a border w lies.  inv = 1 / s.
+__device__ __forceinline__ int q4_code(float w, float s, float inv) {
+    float c = fminf(fmaxf(floorf(fmaf(w, inv, 0.5f)), -8.0f), 7.0f);
+    if (c < 7.0f && fmaf(-(c + 0.5f), s, w) >= 0.0f) c += 1.0f;
+    else if (c > -8.0f && fmaf(-(c - 0.5f), s, w) < 0.0f) c -= 1.0f;
+    return (int)c;
+}
+
+template <typename S>
+struct Q4Pack {
+    const S* w;
+    uint4* codes;
+    void* scales;
+    long long ldw, units;                  // units: warps' pieces of work
+    int n, k, tiles, kbs, groups, vec;
+};
+// A warp packs 16 rows x KB tiles of 64 inputs, which hold whole groups of G: the largest magnitudes, scales and codes from one load.
+template <typename S, typename T, int G>
+__global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4Pack<S> g) {
+    constexpr int KB = G == 128 ? 2 : 1;
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    const int lane = threadIdx.x & 31, gid = lane >> 2;
+    const int across = (g.kbs + KB - 1) / KB;
+    for (long long u = blockIdx.x * 8LL + (threadIdx.x >> 5); u < g.units; u += gridDim.x * 8LL) {
+        const long long tile = u / across;                        // of all experts
+        const int kb0 = (int)(u - tile * across) * KB;
+        const long long expert = tile / g.tiles;
+        const int row0 = (int)(tile - expert * g.tiles) * Q4_ROWS;
+        uint32_t word[KB][4];
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) word[b][i] = 0x88888888u;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {                    // rows gid and gid + 8
+            const int row = row0 + gid + 8 * half;
+            const S* p = g.w + (expert * g.n + row) * g.ldw;
+            float v[KB][2][8];
+            unsigned top[KB][2];
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int c = (kb0 + b) * Q4_K + q4_input(r, lane, 0);
+                    load8<S>(p + c, row < g.n ? g.k - c : 0, g.vec, v[b][r]);
+                }
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    unsigned t = 0u;                              // (as integers: a NaN is larger than an infinity)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) t = max(t, __float_as_uint(v[b][r][e]) & 0x7fffffffu);
+                    t = max(t, __shfl_xor_sync(0xffffffffu, t, 1));
+                    top[b][r] = max(t, __shfl_xor_sync(0xffffffffu, t, 2));
+                }
+            if (G >= 64)
+#pragma unroll
+                for (int b = 0; b < KB; ++b) top[b][0] = top[b][1] = max(top[b][0], top[b][1]);
+            if (G == 128) top[0][0] = top[0][1] = top[KB - 1][0] = top[KB - 1][1] = max(top[0][0], top[KB - 1][0]);
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const T kept = from_f32<T>(__fmul_rn(__uint_as_float(top[b][r]), 1.0f / 7.0f));
+                    float s = to_f32(kept);
+                    const int group = ((kb0 + b) * Q4_K + r * 32) / G;
+                    if ((lane & 3) == 0 && (G == 32 || r == 0) && (G != 128 || b == 0) && group < g.groups)
+                        static_cast<T*>(g.scales)[(tile * g.groups + group) * Q4_ROWS + gid + 8 * half] = row < g.n ? kept : from_f32<T>(0.0f);
+                    if (!(s > 0.0f) || (__float_as_uint(s) & 0x7f800000u) == 0x7f800000u) continue;          // (codes of zero)
+                    const float up = s < 1e-30f ? 1.2676506e30f : 1.0f;                                      // 2^100: no reciprocal overflows, no remainder is lost
+                    s *= up;
+                    const float inv = 1.0f / s;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t c = (uint32_t)(q4_code(v[b][r][e] * up, s, inv) + 8);
+                        // register 2 * h + half of the MMA, element j
+                        const int at = 4 * (2 * ((e >> 1) & 1) + half) + 16 * (e & 1);
+                        word[b][2 * r + (e >> 2)] = (word[b][2 * r + (e >> 2)] & ~(15u << at)) | c << at;
+                    }
+                }
+        }
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+            if (kb0 + b < g.kbs) g.codes[(tile * g.kbs + kb0 + b) * 32 + lane] = make_uint4(word[b][0], word[b][1], word[b][2], word[b][3]);
+    }
+}
+
+template <typename D>
+struct Q4Unpack {
+    const uint4* codes;
+    const void* scales;
+    D* w;
+    long long ldw, units;
+    int n, k, tiles, kbs, groups, group, vec;
+};
+template <typename T, typename D>
+__global__ void __launch_bounds__(256) q4_unpack_kernel(const __grid_constant__ Q4Unpack<D> g) {
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    const int lane = threadIdx.x & 31, gid = lane >> 2;
+    for (long long u = blockIdx.x * 8LL + (threadIdx.x >> 5); u < g.units; u += gridDim.x * 8LL) {
+        const long long tile = u / g.kbs, expert = tile / g.tiles;
+        const int kb = (int)(u - tile * g.kbs), row0 = (int)(tile - expert * g.tiles) * Q4_ROWS;
+        const uint4 q = g.codes[u * 32 + lane];
+        const uint32_t word[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int row = row0 + gid + 8 * half, c = kb * Q4_K + q4_input(r, lane, 0);
+                if (row >= g.n || c >= g.k) continue;
+                const float s = to_f32(static_cast<const T*>(g.scales)[(tile * g.groups + (kb * Q4_K + r * 32) / g.group) * Q4_ROWS + gid + 8 * half]);
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = s * (float)((int)(word[2 * r + (e >> 2)] >> (4 * (2 * ((e >> 1) & 1) + half) + 16 * (e & 1)) & 15u) - 8);
+                D* to = g.w + (expert * g.n + row) * g.ldw + c;
+                constexpr int N = Pack<D>::N;
+                const int left = g.k - c;
+#pragma unroll
+                for (int i = 0; i < 8 / N; ++i) {
+                    float t[N];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) t[e] = v[i * N + e];
+                    store_pack(to + i * N, t, left - i * N, g.vec && left >= (i + 1) * N);
+                }
+            }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- the product
+__device__ __forceinline__ uint4 load_stream(const uint4* p) {      // read once: not kept in the first-level cache
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+// Operand registers of one MMA from a word of codes: the values code - 8.
+template <typename T> struct Q4Operand;
+template <> struct Q4Operand<__half> {
+    // 0x6400: 1024, whose last bit is 1, so that a code in the low bits adds itself, one four bits up 16 times itself
+    static __device__ __forceinline__ void make(uint32_t w, uint32_t (&a)[4]) {
+        const uint32_t v = w >> 8;
+        const __half2 low = __floats2half2_rn(-1032.0f, -1032.0f), sixteenth = __floats2half2_rn(0.0625f, 0.0625f), high = __floats2half2_rn(-72.0f, -72.0f);
+        auto bits = [](uint32_t x) { return *reinterpret_cast<__half2*>(&x); };
+        auto raw = [](__half2 x) { return *reinterpret_cast<uint32_t*>(&x); };
+        a[0] = raw(__hadd2(bits((w & 0x000f000fu) | 0x64006400u), low));
+        a[1] = raw(__hfma2(bits((w & 0x00f000f0u) | 0x64006400u), sixteenth, high));
+        a[2] = raw(__hadd2(bits((v & 0x000f000fu) | 0x64006400u), low));
+        a[3] = raw(__hfma2(bits((v & 0x00f000f0u) | 0x64006400u), sixteenth, high));
+    }
+    static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+};
+template <> struct Q4Operand<__nv_bfloat16> {
+    // 0x4300: 128, whose last bit is 1
+    static __device__ __forceinline__ void make(uint32_t w, uint32_t (&a)[4]) {
+        const __nv_bfloat162 low = __floats2bfloat162_rn(-136.0f, -136.0f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+            const __nv_bfloat162 v = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&x), low);
+            a[i] = *reinterpret_cast<const uint32_t*>(&v);
+        }
+    }
+    static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+};
+template <> struct Q4Operand<float> : Q4Operand<__nv_bfloat16> {};
+
+// A lane's activations of one row for 64 inputs: PL planes of two words for each of the four MMAs.
+template <typename T> struct Q4Acts {
+    static constexpr int PL = 1;
+    uint32_t b[1][8];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[0][i] = 0u;
+    }
+    // x: the lane's first element; left: elements of the row from there on
+    __device__ __forceinline__ void load(const T* x, int left, bool whole) {
+        if (whole) {
+            const uint4 u = *reinterpret_cast<const uint4*>(x), v = *reinterpret_cast<const uint4*>(x + 32);
+            b[0][0] = u.x; b[0][1] = u.y; b[0][2] = u.z; b[0][3] = u.w;
+            b[0][4] = v.x; b[0][5] = v.y; b[0][6] = v.z; b[0][7] = v.w;
+            return;
+        }
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int at = (i >> 2) * 32 + (i & 3) * 2;
+            b[0][i] = (at < left ? (uint32_t)p[at] : 0u) | (at + 1 < left ? (uint32_t)p[at + 1] << 16 : 0u);
+        }
+    }
+};
+template <> struct Q4Acts<float> {
+    static constexpr int PL = 3;
+    uint32_t b[3][8];                                               // the low bits first
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[p][i] = 0u;
+    }
+    // x = high + middle + low, each what the one before left cut to bf16: exact.  An infinity or a NaN is all in the first.
+    static __device__ __forceinline__ void planes(float x, uint32_t (&t)[3]) {
+        uint32_t bits = __float_as_uint(x);
+        const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
+        if (!finite && (bits & 0x007fffffu) != 0u) bits |= 0x00400000u;
+        const float r = finite ? x - __uint_as_float(bits & 0xffff0000u) : 0.0f;
+        t[2] = bits;
+        t[1] = __float_as_uint(r);
+        t[0] = __float_as_uint(r - __uint_as_float(t[1] & 0xffff0000u));
+    }
+    __device__ __forceinline__ void pair(int i, float x, float y) {
+        uint32_t s[3], t[3];
+        planes(x, s);
+        planes(y, t);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) b[p][i] = __byte_perm(s[p], t[p], 0x7632);       // the upper halves of both
+    }
+    __device__ __forceinline__ void load(const float* x, int left, bool whole) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = (i >> 1) * 32 + (i & 1) * 4;
+            float4 v;
+            if (whole) v = *reinterpret_cast<const float4*>(x + at);
+            else v = make_float4(at < left ? x[at] : 0.0f, at + 1 < left ? x[at + 1] : 0.0f, at + 2 < left ? x[at + 2] : 0.0f, at + 3 < left ? x[at + 3] : 0.0f);
+            pair(2 * i, v.x, v.y);
+            pair(2 * i + 1, v.z, v.w);
+        }
+    }
+};
+
+struct Q4Args {
+    const void *x, *scales, *bias, *residual;
+    const uint4* codes;
+    const int* offsets;
+    void* y;
+    long long ldx, ldr, ldy;
+    int m, n, k, experts, tiles, kbs, groups, group_shift, slots, act;
+};
+constexpr int Q4_WARPS = 8;
+
+// The `slot`-th piece of up to `most` rows of an expert, in the order of the experts: the expert, its rows.  Offsets that are out of order or
+// out of range are taken as the nearest ones that are not.
+__device__ __forceinline__ bool q4_slot(const Q4Args& g, int slot, int most, int& expert, int& row0, int& rows) {
+    if (!g.offsets) {
+        expert = 0;
+        row0 = slot * most;
+        rows = min(most, g.m - row0);
+        return rows > 0;
+    }
+    const int lane = threadIdx.x & 31;
+    for (int e0 = 0; e0 < g.experts; e0 += 32) {
+        const int e = e0 + lane;
+        int begin = 0, count = 0;
+        if (e < g.experts) {
+            begin = min(max(g.offsets[e], 0), g.m);
+            count = min(max(g.offsets[e + 1], begin), g.m) - begin;
+        }
+        const int pieces = (count + most - 1) / most;
+        int sum = pieces;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, slot < sum);
+        if (hit) {
+            const int l = __ffs(hit) - 1;
+            const int piece = slot - __shfl_sync(0xffffffffu, sum - pieces, l);
+            expert = e0 + l;
+            row0 = __shfl_sync(0xffffffffu, begin, l) + piece * most;
+            rows = min(most, __shfl_sync(0xffffffffu, count, l) - piece * most);
+            return true;
+        }
+        slot -= __shfl_sync(0xffffffffu, sum, 31);
+    }
+    return false;
+}
+
+// A block: 16 * MT outputs of up to 8 * NT rows; its warps share the reduction and add up in shared memory, in their order.
+template <typename T, int NT, int MT, bool G32>
+__global__ void __launch_bounds__(Q4_WARPS * 32) q4_kernel(const __grid_constant__ Q4Args g) {
+    extern __shared__ float sums[];                                 // [warp][row][16 * MT outputs]
+    constexpr int COLS = Q4_ROWS * MT, ROWS = 8 * NT, D = MT == 1 ? 4 : 2;
+    using Acts = Q4Acts<T>;
+    using Operand = Q4Operand<T>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    const int slot = (int)(blockIdx.x % (unsigned)g.slots), tile0 = (int)(blockIdx.x / (unsigned)g.slots) * MT;
+    int expert, row0, rows;
+    if (!q4_slot(g, slot, ROWS, expert, row0, rows)) return;
+    const int kb0 = (int)((long long)g.kbs * warp / Q4_WARPS), kb1 = (int)((long long)g.kbs * (warp + 1) / Q4_WARPS);
+    const T* x = static_cast<const T*>(g.x) + (long long)(row0 + gid) * g.ldx + tig * 8;
+    const uint4* codes[MT];
+    const T* scales[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const long long tile = (long long)expert * g.tiles + min(tile0 + t, g.tiles - 1);
+        codes[t] = g.codes + tile * g.kbs * 32 + lane;
+        scales[t] = static_cast<const T*>(g.scales) + tile * g.groups * Q4_ROWS + gid;
+    }
+    float acc[MT][NT][4];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][i][e] = 0.0f;
+
+    uint4 w[D][MT], next[D][MT];
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) next[d][t] = kb0 + d < kb1 ? load_stream(codes[t] + (long long)(kb0 + d) * 32) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 1
+    for (int kb = kb0; kb < kb1; kb += D) {
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                w[d][t] = next[d][t];
+                if (kb + D + d < kb1) next[d][t] = load_stream(codes[t] + (long long)(kb + D + d) * 32);
+            }
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            if (kb + d >= kb1) break;
+            const int k = (kb + d) * Q4_K, left = g.k - k - tig * 8;
+            const bool whole = k + Q4_K <= g.k;
+            Acts b[NT];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                if (gid + 8 * i < rows) b[i].load(x + (long long)(8 * i) * g.ldx + k, left, whole);
+                else b[i].zero();
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const uint32_t word[4] = {w[d][t].x, w[d][t].y, w[d][t].z, w[d][t].w};
+                uint32_t a[4][4];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) Operand::make(word[s], a[s]);
+#pragma unroll
+                for (int q = 0; q < (G32 ? 2 : 1); ++q) {
+                    const int group = G32 ? min((kb + d) * 2 + q, g.groups - 1) : (kb + d) >> g.group_shift;
+                    const float s0 = to_f32(scales[t][group * Q4_ROWS]), s1 = to_f32(scales[t][group * Q4_ROWS + 8]);
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int p = 0; p < Acts::PL; ++p)
+#pragma unroll
+                            for (int s = G32 ? 2 * q : 0; s < (G32 ? 2 * q + 2 : 4); ++s) Operand::mma(c, a[s], b[i].b[p][2 * s], b[i].b[p][2 * s + 1]);
+                        acc[t][i][0] = fmaf(c[0], s0, acc[t][i][0]);
+                        acc[t][i][1] = fmaf(c[1], s0, acc[t][i][1]);
+                        acc[t][i][2] = fmaf(c[2], s1, acc[t][i][2]);
+                        acc[t][i][3] = fmaf(c[3], s1, acc[t][i][3]);
+                    }
+                }
+            }
+        }
+    }
+    float* mine = sums + warp * ROWS * COLS;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine[(8 * i + 2 * tig + (e & 1)) * COLS + t * Q4_ROWS + gid + 8 * (e >> 1)] = acc[t][i][e];
+    __syncthreads();
+    const T* bias = g.bias ? static_cast<const T*>(g.bias) + (long long)expert * g.n : nullptr;
+    for (int i = threadIdx.x; i < rows * COLS; i += Q4_WARPS * 32) {
+        const int r = i / COLS, col = tile0 * Q4_ROWS + i % COLS;
+        if (col >= g.n) continue;
+        float v = 0.0f;
+#pragma unroll
+        for (int q = 0; q < Q4_WARPS; ++q) v += sums[q * ROWS * COLS + i];
+        if (bias) v += to_f32(bias[col]);
+        if (g.act) v = activation<sizeof(T) == 2>(v, g.act);
+        if (g.residual) v += to_f32(static_cast<const T*>(g.residual)[(long long)(row0 + r) * g.ldr + col]);
+        static_cast<T*>(g.y)[(long long)(row0 + r) * g.ldy + col] = from_f32<T>(v);
+    }
+}
+
+template <typename T, int NT, int MT, bool G32>
+static int launch_q4(const Q4Args& g, long long blocks, cudaStream_t st) {
+    constexpr int SMEM = Q4_WARPS * 8 * NT * Q4_ROWS * MT * 4;
+    auto kern = q4_kernel<T, NT, MT, G32>;
+    if (SMEM > 48 * 1024) {
+        static bool attr_set[64] = {};
+        int dev = 0;
+        cudaGetDevice(&dev);
+        if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+            if (check_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM))) return EBS_ERR_CUDA;
+            if (dev >= 0 && dev < 64) attr_set[dev] = true;
+        }
+    }
+    return launch_chained(kern, dim3((unsigned)blocks), Q4_WARPS * 32, SMEM, st, 1, g);
+}
+// Rows that a block takes at a time, in eights: from the rows an expert has in the mean, twice that so that most experts' weights are read once.
+static int q4_row_tiles(int m, int experts, int dtype) {
+    const long long rows = experts == 1 ? m : 2LL * ((m + experts - 1) / experts);
+    const int most = dtype == EBS_F32 ? 4 : 8;
+    int nt = 1;
+    while (nt < most && 8LL * nt < rows) nt *= 2;
+    return nt;
+}
+template <typename T, int NT, int MT>
+static int launch_q4_group(Q4Args& g, int group, cudaStream_t st) {
+    // pieces of rows: at most one for each expert that has rows, and one more for each full piece
+    const long long pieces = g.offsets ? (long long)(g.experts < g.m ? g.experts : g.m) + g.m / (8 * NT) : (g.m + 8LL * NT - 1) / (8 * NT);
+    const long long blocks = pieces * ((g.tiles + MT - 1) / MT);
+    if (blocks > 0x7fffffffLL) return EBS_ERR_OVERFLOW;
+    g.slots = (int)pieces;
+    return group == 32 ? launch_q4<T, NT, MT, true>(g, blocks, st) : launch_q4<T, NT, MT, false>(g, blocks, st);
+}
+template <typename T>
+static int launch_q4_rows(Q4Args& g, int group, int dtype, cudaStream_t st) {
+    switch (q4_row_tiles(g.m, g.offsets ? g.experts : 1, dtype)) {
+        case 1: return launch_q4_group<T, 1, 1>(g, group, st);
+        case 2: return launch_q4_group<T, 2, 1>(g, group, st);
+        case 4: return launch_q4_group<T, 4, 2>(g, group, st);
+        default:
+            if constexpr (sizeof(T) == 2) return launch_q4_group<T, 8, 2>(g, group, st);
+            else return EBS_ERR_UNSUPPORTED;
+    }
+}
+
+template <typename S, typename T>
+static int launch_pack_typed(const ebs_q4_desc& d, const void* w, long long ldw, void* packed, cudaStream_t st) {
+    const Q4Layout l = q4_layout(d);
+    const int kb = d.group == 128 ? 2 : 1;
+    Q4Pack<S> g{static_cast<const S*>(w), static_cast<uint4*>(packed), static_cast<char*>(packed) + l.codes, ldw, (long long)d.experts * l.tiles * ((l.kbs + kb - 1) / kb),
+                d.n, d.k, l.tiles, l.kbs, l.groups, ldw * (long long)sizeof(S) % 16 == 0};
+    const long long blocks = (g.units + 7) / 8;
+    const dim3 grid((unsigned)(blocks < 148 * 64 ? blocks : 148 * 64));
+    if (d.group == 32) return launch_chained(q4_pack_kernel<S, T, 32>, grid, 256, 0, st, 1, g);
+    if (d.group == 64) return launch_chained(q4_pack_kernel<S, T, 64>, grid, 256, 0, st, 1, g);
+    return launch_chained(q4_pack_kernel<S, T, 128>, grid, 256, 0, st, 1, g);
+}
+template <typename S>
+static int launch_pack(const ebs_q4_desc& d, const void* w, long long ldw, void* packed, cudaStream_t st) {
+    if (d.dtype == EBS_F32) return launch_pack_typed<S, float>(d, w, ldw, packed, st);
+    if (d.dtype == EBS_F16) return launch_pack_typed<S, __half>(d, w, ldw, packed, st);
+    return launch_pack_typed<S, __nv_bfloat16>(d, w, ldw, packed, st);
+}
+template <typename T, typename D>
+static int launch_unpack_typed(const ebs_q4_desc& d, const void* packed, void* w, long long ldw, cudaStream_t st) {
+    const Q4Layout l = q4_layout(d);
+    Q4Unpack<D> g{static_cast<const uint4*>(packed), static_cast<const char*>(packed) + l.codes, static_cast<D*>(w), ldw, (long long)d.experts * l.tiles * l.kbs, d.n, d.k,
+                  l.tiles, l.kbs, l.groups, d.group, ldw * (long long)sizeof(D) % 16 == 0};
+    const long long blocks = (g.units + 7) / 8;
+    return launch_chained(q4_unpack_kernel<T, D>, dim3((unsigned)(blocks < 148 * 64 ? blocks : 148 * 64)), 256, 0, st, 1, g);
+}
+template <typename D>
+static int launch_unpack(const ebs_q4_desc& d, const void* packed, void* w, long long ldw, cudaStream_t st) {
+    if (d.dtype == EBS_F32) return launch_unpack_typed<float, D>(d, packed, w, ldw, st);
+    if (d.dtype == EBS_F16) return launch_unpack_typed<__half, D>(d, packed, w, ldw, st);
+    return launch_unpack_typed<__nv_bfloat16, D>(d, packed, w, ldw, st);
+}
+
+// Checks of the two calls that bring weights to 4 bits and back; `from` and `to` in the order of the call.
+static int check_weights(const ebs_q4_desc* d, const void* w, int w_dtype, long long* ldw, const void* packed, bool packed_out) {
+    const int rc = check_q4(d);
+    if (rc) return rc;
+    if (!w || !packed || !real_dtype(w_dtype)) return EBS_ERR_INVALID_ARG;
+    if (*ldw == 0) *ldw = d->k;
+    if (*ldw < d->k) return EBS_ERR_INVALID_ARG;
+    const long long rows = (long long)d->experts * d->n;
+    if (*ldw > (1LL << 40) / rows) return EBS_ERR_OVERFLOW;
+    const size_t size = element_size(w_dtype);
+    const Q4Layout l = q4_layout(*d);
+    const long long bytes = (long long)((l.codes + l.scales) / size);
+    const Rows t[] = {{w, rows, d->k, *ldw, !packed_out}, {packed, 1, bytes, bytes, packed_out}};
+    return check_tensors(t, 2, size, nullptr, nullptr);
+}
+
+// The two descriptors of a product together, strides filled in; rows_copied: x goes through the workspace, since its rows start anywhere.
+static int check_product(const ebs_linear_desc* desc, const ebs_q4_desc* q, ebs_linear_desc* d, bool* rows_copied) {
+    int rc = check_q4(q);
+    if (rc || (rc = complete_linear(desc, d))) return rc;
+    if (d->n != q->n || d->k != q->k || d->dtype != q->dtype) return EBS_ERR_INVALID_ARG;
+    *rows_copied = d->m > 1 && d->ldx * (long long)element_size(d->dtype) % 16 != 0;
+    return EBS_OK;
+}
+static long long copied_stride(const ebs_linear_desc& d) { return round8(d.k); }
+
+}  // namespace ebs
+
+using namespace ebs;
+
+extern "C" {
+
+size_t ebs_q4_packed_bytes(const ebs_q4_desc* desc) {
+    if (check_q4(desc)) return 0;
+    const Q4Layout l = q4_layout(*desc);
+    return l.codes + round256(l.scales);
+}
+
+int ebs_pack_weights_q4(const void* w_dev, int w_dtype, const ebs_q4_desc* desc, long long ldw, void* packed_dev, void* stream) {
+    const int rc = check_weights(desc, w_dev, w_dtype, &ldw, packed_dev, true);
+    if (rc) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (w_dtype == EBS_F32) return launch_pack<float>(*desc, w_dev, ldw, packed_dev, st);
+    if (w_dtype == EBS_F16) return launch_pack<__half>(*desc, w_dev, ldw, packed_dev, st);
+    return launch_pack<__nv_bfloat16>(*desc, w_dev, ldw, packed_dev, st);
+}
+
+int ebs_unpack_weights_q4(const void* packed_dev, const ebs_q4_desc* desc, void* w_dev, int w_dtype, long long ldw, void* stream) {
+    const int rc = check_weights(desc, w_dev, w_dtype, &ldw, packed_dev, false);
+    if (rc) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (w_dtype == EBS_F32) return launch_unpack<float>(*desc, packed_dev, w_dev, ldw, st);
+    if (w_dtype == EBS_F16) return launch_unpack<__half>(*desc, packed_dev, w_dev, ldw, st);
+    return launch_unpack<__nv_bfloat16>(*desc, packed_dev, w_dev, ldw, st);
+}
+
+size_t ebs_linear_q4_workspace_bytes(const ebs_linear_desc* desc, const ebs_q4_desc* q4) {
+    ebs_linear_desc d;
+    bool copied;
+    if (check_product(desc, q4, &d, &copied)) return 0;
+    return copied ? round256((size_t)d.m * copied_stride(d) * element_size(d.dtype)) : 0;
+}
+
+int ebs_linear_q4_forward(const void* x_dev, const void* packed_dev, const void* bias_dev, const void* residual_dev, const int* offsets_dev, const ebs_linear_desc* desc,
+                          const ebs_q4_desc* q4, void* y_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
+    ebs_linear_desc d;
+    bool copied;
+    int rc = check_product(desc, q4, &d, &copied);
+    if (rc) return rc;
+    if (!packed_dev || (d.m > 0 && (!x_dev || !y_dev)) || (!offsets_dev && q4->experts != 1) || ((uintptr_t)offsets_dev & 3u)) return EBS_ERR_INVALID_ARG;
+    const size_t size = element_size(d.dtype), need = ebs_linear_q4_workspace_bytes(desc, q4);
+    if (need && (!workspace_dev || workspace_bytes < need)) return EBS_ERR_INVALID_ARG;
+    const Q4Layout l = q4_layout(*q4);
+    auto flat = [&](const void* p, size_t bytes, bool out) { return Rows{p, 1, (long long)(bytes / size), (long long)(bytes / size), out}; };
+    const Rows t[] = {{x_dev, d.m, d.k, d.ldx, false}, flat(packed_dev, l.codes + l.scales, false), flat(bias_dev, (size_t)q4->experts * d.n * size, false),
+                      {residual_dev, d.m, d.n, d.ldr, false}, {y_dev, d.m, d.n, d.ldy, true}, flat(need ? workspace_dev : nullptr, need, true)};
+    if (check_tensors(t, 6, size, &t[3], &t[4])) return EBS_ERR_INVALID_ARG;
+    if (offsets_dev) {
+        const uintptr_t o = (uintptr_t)offsets_dev, oe = o + ((size_t)q4->experts + 1) * 4, y = (uintptr_t)y_dev, w = (uintptr_t)workspace_dev;
+        if (d.m > 0 && o < y + ((size_t)(d.m - 1) * d.ldy + d.n) * size && y < oe) return EBS_ERR_INVALID_ARG;
+        if (need && o < w + need && w < oe) return EBS_ERR_INVALID_ARG;
+    }
+    if (d.m == 0) return EBS_OK;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Q4Args g{x_dev, static_cast<const char*>(packed_dev) + l.codes, bias_dev, residual_dev, static_cast<const uint4*>(packed_dev), offsets_dev, y_dev, d.ldx, d.ldr, d.ldy,
+             d.m, d.n, d.k, q4->experts, l.tiles, l.kbs, l.groups, q4->group == 128 ? 1 : 0, 0, d.act};
+    if (copied) {                                                  // (fp32 rows as twice as many 16-bit elements)
+        const int halves = (int)(size / 2);
+        CopyJobs jobs = {};
+        add_copy_rows(&jobs, x_dev, workspace_dev, d.m, d.k * halves, d.ldx * halves, copied_stride(d) * halves);
+        if ((rc = launch_copies(jobs, st))) return rc;
+        g.x = workspace_dev;
+        g.ldx = copied_stride(d);
+    }
+    if (d.dtype == EBS_F32) return launch_q4_rows<float>(g, q4->group, d.dtype, st);
+    if (d.dtype == EBS_F16) return launch_q4_rows<__half>(g, q4->group, d.dtype, st);
+    return launch_q4_rows<__nv_bfloat16>(g, q4->group, d.dtype, st);
+}
+
+}  // extern "C"
