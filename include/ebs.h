@@ -432,6 +432,27 @@ int ebs_orthogonalize(const void *g_dev, int batch, int rows, int cols, int dtyp
                       float scale, void *out_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
+ * Layers of experts: the real-valued layer above with weights of its own for each of several groups of rows, trained.  Rows
+ * offsets[e] .. offsets[e+1]-1 of x are expert e's; the sizes are known on the device only, so that nothing waits for them.
+ *
+ *   forward    z = x W_e^T + bias_e,  y = act(z) + residual      x [m][k], W [experts][n][k], bias [experts][n]
+ *   backward   dz = dy * act'(z),  dx = dz W_e,  dW_e = dz_e^T x_e,  dbias_e = sum over the expert's rows of dz
+ *
+ * Descriptor, tensors, activations, accuracy, strides, overlaps and workspace (ebs_grouped_workspace_bytes) are those of ebs_linear_forward
+ * and ebs_linear_backward, for EBS_F16 and EBS_BF16 (EBS_F32: EBS_ERR_UNSUPPORTED); desc->m counts all rows of the buffers.
+ * offsets_dev: int32 [experts + 1] in device memory, not decreasing, within 0 .. m.  Rows that are no expert's are neither read for a result nor written
+ * (padding at the end of a batch); an expert without rows gets dW_e = 0 and dbias_e = 0.  (Offsets out of order or out of 0 .. m lead to
+ * no access out of bounds; which results rows then get is not defined.)  No output may overlap the offsets.
+ */
+size_t ebs_grouped_workspace_bytes(const ebs_linear_desc *desc, int experts, int backward);
+int ebs_grouped_forward(const void *x_dev, const void *w_dev, const void *bias_dev, const void *residual_dev,
+                        const int *offsets_dev, int experts, const ebs_linear_desc *desc, void *y_dev, void *z_dev,
+                        void *workspace_dev, size_t workspace_bytes, void *stream);
+int ebs_grouped_backward(const void *dy_dev, const void *x_dev, const void *w_dev, const void *z_dev, const int *offsets_dev,
+                         int experts, const ebs_linear_desc *desc, void *dx_dev, void *dw_dev, void *dbias_dev,
+                         void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
  * Layers with weights of 4 bits, for answering: what a real-valued layer (or a layer of experts) becomes once it is trained.
  * The paper's weights have one scale a layer and an integer product; here each `group` neighbouring weights of a row have a scale of
  * their own, activations stay real, and the product is one of a few rows (tokens), bound by the weights' bytes.

@@ -40,6 +40,7 @@ EXPORTS = [
     "ebs_orthogonalize_workspace_bytes", "ebs_orthogonalize",
     "ebs_clip_plan", "ebs_clip_workspace_bytes", "ebs_clip_gradients", "ebs_q4_packed_bytes", "ebs_pack_weights_q4",
     "ebs_unpack_weights_q4", "ebs_linear_q4_workspace_bytes", "ebs_linear_q4_forward",
+    "ebs_grouped_workspace_bytes", "ebs_grouped_forward", "ebs_grouped_backward",
 ]
 EBS_CLIP_CHUNK_BYTES = 48
 
@@ -167,6 +168,10 @@ def lib() -> ctypes.CDLL:
         L.ebs_linear_q4_workspace_bytes.argtypes = [LD, QD]
         L.ebs_linear_q4_workspace_bytes.restype = z
         L.ebs_linear_q4_forward.argtypes = [p, p, p, p, p, LD, QD, p, p, z, p]
+        L.ebs_grouped_workspace_bytes.argtypes = [LD, i, i]
+        L.ebs_grouped_workspace_bytes.restype = z
+        L.ebs_grouped_forward.argtypes = [p, p, p, p, p, i, LD, p, p, p, z, p]
+        L.ebs_grouped_backward.argtypes = [p, p, p, p, p, i, LD, p, p, p, p, z, p]
         _lib = L
     return _lib
 
@@ -183,7 +188,8 @@ def _native():
         names = ("ebs_pack_acts", "ebs_pack_acts_s2d", "ebs_conv2d_mixed", "ebs_conv2d_mixed_variant", "ebs_dequant",
                  "ebs_global_avgpool", "ebs_maxpool_packed", "ebs_resnet_cifar_forward", "ebs_search_weight_forward",
                  "ebs_search_act_forward", "ebs_graph_launch", "ebs_linear_forward", "ebs_linear_backward", "ebs_orthogonalize",
-                 "ebs_clip_gradients", "ebs_pack_weights_q4", "ebs_unpack_weights_q4", "ebs_linear_q4_forward")
+                 "ebs_clip_gradients", "ebs_pack_weights_q4", "ebs_unpack_weights_q4", "ebs_linear_q4_forward",
+                 "ebs_grouped_forward", "ebs_grouped_backward")
         torch.cuda.init()                                  # the stream lookups below need torch's CUDA state
         _fastcall.bind({k: ctypes.cast(getattr(L, k), ctypes.c_void_p).value for k in names},
                        torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, ebs_conv_desc, ebs_epilogue, ebs_fused_head,
@@ -574,6 +580,24 @@ def ebs_linear_q4_forward(x_dev, packed_dev, bias_dev, residual_dev, offsets_dev
     rc = (_fast or _native()).linear_q4_forward(x_dev, packed_dev, bias_dev, residual_dev, offsets_dev, desc, q4, y_dev, workspace_dev, stream)
     if rc:
         _check(rc, "ebs_linear_q4_forward")
+
+
+def ebs_grouped_workspace_bytes(desc: ebs_linear_desc, experts: int, backward=False) -> int:
+    return lib().ebs_grouped_workspace_bytes(ctypes.byref(desc), experts, int(bool(backward)))
+
+
+def ebs_grouped_forward(x_dev, w_dev, bias_dev, residual_dev, offsets_dev, experts: int, desc: ebs_linear_desc, y_dev, z_dev=None,
+                        workspace_dev=None, stream=None) -> None:
+    rc = (_fast or _native()).grouped_forward(x_dev, w_dev, bias_dev, residual_dev, offsets_dev, experts, desc, y_dev, z_dev, workspace_dev, stream)
+    if rc:
+        _check(rc, "ebs_grouped_forward")
+
+
+def ebs_grouped_backward(dy_dev, x_dev, w_dev, z_dev, offsets_dev, experts: int, desc: ebs_linear_desc, dx_dev=None, dw_dev=None, dbias_dev=None,
+                         workspace_dev=None, stream=None) -> None:
+    rc = (_fast or _native()).grouped_backward(dy_dev, x_dev, w_dev, z_dev, offsets_dev, experts, desc, dx_dev, dw_dev, dbias_dev, workspace_dev, stream)
+    if rc:
+        _check(rc, "ebs_grouped_backward")
 
 
 class CaptureStream:

@@ -24,7 +24,8 @@ EACH_ENTRY(DECLARE_ENTRY)
 #define EACH_REAL_ENTRY(X) X(ebs_linear_forward) X(ebs_linear_backward) X(ebs_orthogonalize)
 EACH_REAL_ENTRY(DECLARE_ENTRY)
 /* Those around layers of experts: bound where `bind` finds their addresses. */
-#define EACH_EXPERT_ENTRY(X) X(ebs_clip_gradients) X(ebs_pack_weights_q4) X(ebs_unpack_weights_q4) X(ebs_linear_q4_forward)
+#define EACH_EXPERT_ENTRY(X) X(ebs_clip_gradients) X(ebs_pack_weights_q4) X(ebs_unpack_weights_q4) X(ebs_linear_q4_forward) \
+    X(ebs_grouped_forward) X(ebs_grouped_backward)
 EACH_EXPERT_ENTRY(DECLARE_ENTRY)
 
 /* Device or host address of a tensor argument; None is the null pointer. */
@@ -365,6 +366,35 @@ FAST(linear_q4_forward) {
     CALL(p_ebs_linear_q4_forward(p[0], p[1], p[2], p[3], p[4], &d, &q, y, ws, bytes, st));
 }
 
+FAST(grouped_forward) {
+    void *p[5], *y, *z, *ws, *st;
+    size_t bytes;
+    int experts;
+    ebs_linear_desc d;
+    if (!arg_count(n, 11) || !bound(p_ebs_grouped_forward)) return NULL;
+    for (int k = 0; k < 5; ++k)
+        if (!as_ptr(a[k], &p[k])) return NULL;
+    if (!as_int(a[5], &experts) || !as_struct(a[6], t_linear, &d, sizeof(d)) || !as_ptr(a[7], &y) || !as_ptr(a[8], &z) ||
+        !as_workspace(a[9], &ws, &bytes) || !as_stream(a[10], &st))
+        return NULL;
+    CALL(p_ebs_grouped_forward(p[0], p[1], p[2], p[3], p[4], experts, &d, y, z, ws, bytes, st));
+}
+
+FAST(grouped_backward) {
+    void *p[5], *out[3], *ws, *st;
+    size_t bytes;
+    int experts;
+    ebs_linear_desc d;
+    if (!arg_count(n, 12) || !bound(p_ebs_grouped_backward)) return NULL;
+    for (int k = 0; k < 5; ++k)
+        if (!as_ptr(a[k], &p[k])) return NULL;
+    if (!as_int(a[5], &experts) || !as_struct(a[6], t_linear, &d, sizeof(d))) return NULL;
+    for (int k = 0; k < 3; ++k)
+        if (!as_ptr(a[7 + k], &out[k])) return NULL;
+    if (!as_workspace(a[10], &ws, &bytes) || !as_stream(a[11], &st)) return NULL;
+    CALL(p_ebs_grouped_backward(p[0], p[1], p[2], p[3], p[4], experts, &d, out[0], out[1], out[2], ws, bytes, st));
+}
+
 /* same_bytes(structs, bytes): whether the concatenated contents of the structures are exactly `bytes`. */
 FAST(same_bytes) {
     if (!arg_count(n, 2)) return NULL;
@@ -464,6 +494,8 @@ static PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, NULL},
                                 FAST_METHOD(pack_weights_q4),
                                 FAST_METHOD(unpack_weights_q4),
                                 FAST_METHOD(linear_q4_forward),
+                                FAST_METHOD(grouped_forward),
+                                FAST_METHOD(grouped_backward),
                                 FAST_METHOD(same_bytes),
                                 FAST_METHOD(same_addresses),
                                 {NULL, NULL, 0, NULL}};

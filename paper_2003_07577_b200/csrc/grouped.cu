@@ -1,0 +1,664 @@
+// Layers of experts: products grouped by the rows of each expert, and their gradients.  See include/ebs.h.
+//
+// One persistent kernel, two forms.  Rows (forward and dx): tiles of 128 rows of one expert x TN outputs, over the reduction of the layer; the last tile
+// of an expert reads rows of the next one and leaves them out when it writes.  Weights (dW): tiles of 128 x TN of an expert's gradient over the
+// expert's own rows; what its last stage holds of other rows is cleared in shared memory before the tensor core reads it.  Offsets are read on the
+// device only: a block finds its tiles by scanning them, 32 experts at a time.
+//
+// Warp 8 fetches by TMA, warp 9 issues the MMAs, warps 0-7 take the sums of the finished tile out of tensor memory while the next one is
+// multiplied (two accumulators).  Sums of more than 4096 terms leave the tensor core on the way, which truncates what it adds.  Results go
+// through a patch of shared memory, so that neighbouring lanes write neighbouring bytes, and leave with ordinary stores: a row that is not the expert's
+// is not written.
+#include "gemm_tile.cuh"
+#include "tensors.cuh"
+
+namespace ebs {
+
+static __device__ unsigned long long g_grouped_timeouts = 0ull;
+
+struct GroupedArgs {
+    const int* offsets;
+    const void *bias, *residual;
+    void *y, *z;
+    long long ldy, ldr, ldz, y_expert;     // y_expert: elements between the results of two experts (weights)
+    int m, experts, rows, cols, red;       // rows: of a weight gradient
+    int tiles_n, b_mn, bf16, act, vec, bias_vec;
+    float alpha;
+    unsigned wait_limit;
+    int test_flags;
+};
+
+constexpr int GROUPED_THREADS = 320;
+constexpr int PATCH_PITCH = 80;                                  // bytes: 32 values of a row and 16 bytes, so that eight lanes' rows meet no bank twice
+constexpr int PATCH_BYTES = 32 * PATCH_PITCH;
+template <int TN> __host__ __device__ constexpr int grouped_stage_bytes() { return (128 + TN) * GEMM_ROW_BYTES; }
+template <int TN> __host__ __device__ constexpr int grouped_stages() { return TN == 256 ? 4 : TN == 128 ? 6 : 3; }
+template <int TN> __host__ __device__ constexpr int grouped_smem_bytes() { return grouped_stages<TN>() * grouped_stage_bytes<TN>() + 8 * PATCH_BYTES + 1024; }
+
+// Rows of expert e; offsets that are out of order or out of range are taken as the nearest ones that are not.
+__device__ __forceinline__ void expert_rows(const int* offsets, int m, int e, int& begin, int& count) {
+    begin = min(max(__ldg(offsets + e), 0), m);
+    count = min(max(__ldg(offsets + e + 1), begin), m) - begin;
+}
+struct GroupedTile {
+    int expert, a0, a_end, b0;             // first and end row on the lanes, first column
+    int red0, red_end;                     // weights: the expert's rows
+    int nkb;
+};
+// The tiles in their order; a warp asks for ever larger ones.
+template <bool DW>
+struct GroupedTiles {
+    int e0 = 0, before = 0;                // tiles of the experts below e0
+    __device__ __forceinline__ bool find(const GroupedArgs& g, int t, int tile_cols, GroupedTile& tile) {
+        if (DW) {
+            const int tiles_m = (g.rows + 127) / 128, per = tiles_m * g.tiles_n;
+            tile.expert = t / per;
+            if (tile.expert >= g.experts) return false;
+            t -= tile.expert * per;
+            int count;
+            expert_rows(g.offsets, g.m, tile.expert, tile.red0, count);
+            tile.red_end = tile.red0 + count;
+            tile.nkb = (count + GEMM_BK - 1) / GEMM_BK;
+            tile.a0 = t % tiles_m * 128;
+            tile.a_end = g.rows;
+            tile.b0 = t / tiles_m * tile_cols;
+            return true;
+        }
+        const int lane = threadIdx.x & 31;
+        for (; e0 < g.experts; e0 += 32) {
+            int begin = 0, count = 0;
+            if (e0 + lane < g.experts) expert_rows(g.offsets, g.m, e0 + lane, begin, count);
+            const int mine = (count + 127) / 128 * g.tiles_n;
+            int sum = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += v;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, t - before < sum);
+            if (hit) {
+                const int l = __ffs(hit) - 1, in = t - before - __shfl_sync(0xffffffffu, sum - mine, l);
+                begin = __shfl_sync(0xffffffffu, begin, l);
+                count = __shfl_sync(0xffffffffu, count, l);
+                const int tiles_m = (count + 127) / 128;
+                tile.expert = e0 + l;
+                tile.a0 = begin + in % tiles_m * 128;
+                tile.a_end = begin + count;
+                tile.b0 = in / tiles_m * tile_cols;
+                tile.red0 = tile.red_end = 0;
+                tile.nkb = (g.red + GEMM_BK - 1) / GEMM_BK;
+                return true;
+            }
+            before += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        return false;
+    }
+};
+
+// 32 values of this lane's row, through the warp's patch, to `rows` rows of 32 columns (`left` of them exist).
+template <typename T>
+__device__ __forceinline__ void store_patch(uint8_t* patch, const float (&v)[32], T* to, long long ld, int rows, int left, bool vec) {
+    const int lane = threadIdx.x & 31;
+    __syncwarp();                                                 // (what was there is read)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<uint4*>(patch + lane * PATCH_PITCH + c * 16) =
+            make_uint4(pair_word<T>(v[8 * c], v[8 * c + 1]), pair_word<T>(v[8 * c + 2], v[8 * c + 3]), pair_word<T>(v[8 * c + 4], v[8 * c + 5]), pair_word<T>(v[8 * c + 6], v[8 * c + 7]));
+    __syncwarp();
+    if (vec && left >= 32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 8 + (lane >> 2), c = lane & 3;
+            if (r < rows) *reinterpret_cast<uint4*>(to + r * ld + c * 8) = *reinterpret_cast<const uint4*>(patch + r * PATCH_PITCH + c * 16);
+        }
+    } else if (lane < left)
+        for (int r = 0; r < rows; ++r) to[r * ld + lane] = reinterpret_cast<const T*>(patch + r * PATCH_PITCH)[lane];
+}
+
+// The sums of 32 columns of the warp's rows on their way out: row0 the warp's first row, rows how many it has.
+template <typename T, bool DW>
+__device__ __forceinline__ void finish_columns(const GroupedArgs& g, const GroupedTile& tile, uint8_t* patch, float (&v)[32], int row0, int rows, int col, int left) {
+    const int lane = threadIdx.x & 31;
+    T* y = static_cast<T*>(g.y) + (DW ? tile.expert * g.y_expert : 0) + (long long)row0 * g.ldy + col;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] *= g.alpha;
+    if (!DW) {
+        if (g.bias) {
+            const T* b = static_cast<const T*>(g.bias) + (long long)tile.expert * g.cols + col;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float t[8];
+                unpack<T>(load_raw(b + 8 * c, left - 8 * c, g.bias_vec && left >= 8 * c + 8), t);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[8 * c + i] += t[i];
+            }
+        }
+        if (g.z) store_patch(patch, v, static_cast<T*>(g.z) + (long long)row0 * g.ldz + col, g.ldz, rows, left, g.vec);
+        switch (g.act) {
+#define EBS_ACT_CASE(A) case A: _Pragma("unroll") for (int i = 0; i < 32; ++i) v[i] = activation<true>(v[i], A); break;
+            EBS_ACT_CASE(EBS_ACT_RELU) EBS_ACT_CASE(EBS_ACT_GELU) EBS_ACT_CASE(EBS_ACT_GELU_TANH) EBS_ACT_CASE(EBS_ACT_SILU)
+#undef EBS_ACT_CASE
+            default: break;
+        }
+        if (g.residual && lane < rows) {
+            const T* r = static_cast<const T*>(g.residual) + (long long)(row0 + lane) * g.ldr + col;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float t[8];
+                unpack<T>(load_raw(r + 8 * c, left - 8 * c, g.vec && left >= 8 * c + 8), t);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[8 * c + i] += t[i];
+            }
+        }
+    }
+    store_patch(patch, v, y, g.ldy, rows, left, g.vec);
+}
+
+// DW: the form for weight gradients.  CHUNKS: sums leave tensor memory every GEMM_LONG stages and go on in registers.
+template <typename T, int TN, bool DW, bool CHUNKS>
+__global__ void __launch_bounds__(GROUPED_THREADS, TN == 64 ? 2 : 1) grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                                                     const __grid_constant__ GroupedArgs g) {
+    extern __shared__ uint8_t smem_raw[];
+    constexpr int S = grouped_stages<TN>(), STAGE = grouped_stage_bytes<TN>(), A_BYTES = 128 * GEMM_ROW_BYTES, CQ = TN / 2;
+    __shared__ uint64_t full[S], empty[S], acc_full[2], acc_empty[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp >= 8 && lane == 0) asm volatile("prefetch.tensormap [%0];\n" ::"l"(warp == 8 ? &map_a : &map_b) : "memory");
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 8); }
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_slot)), "r"(2u * TN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    const uint32_t tmem = uni(tmem_slot);
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+
+    GroupedTiles<DW> order;
+    GroupedTile tile;
+    bool ok = true;
+    if (warp == 8) {
+        const bool leader = elect_one();
+        int i = 0;                                                // stages filled so far
+        for (int t = (int)blockIdx.x; ok && order.find(g, t, TN, tile); t += (int)gridDim.x)
+            for (int kb = 0; kb < tile.nkb; ++kb, ++i) {
+                const int s = i % S, k = tile.red0 + kb * GEMM_BK;
+                ok = mbar_wait_warp(&empty[s], ((i / S) & 1) ^ 1, &abort_flag, g.wait_limit);
+                if (!ok) break;
+                if (leader) {
+                    const uint32_t at = smem_u32(tiles) + s * STAGE, bt = at + A_BYTES, bar = smem_u32(&full[s]);
+                    mbar_expect_tx(&full[s], STAGE);
+                    if (DW) { tma_load_3d(at, &map_a, tile.a0, k, 0, bar); tma_load_3d(at + 8192, &map_a, tile.a0 + 64, k, 0, bar); }
+                    else tma_load_3d(at, &map_a, k, tile.a0, 0, bar);
+                    if (!DW && !g.b_mn) tma_load_3d(bt, &map_b, k, tile.b0, tile.expert, bar);
+                    else
+#pragma unroll
+                        for (int h = 0; h < TN / 64; ++h) tma_load_3d(bt + h * 8192, &map_b, tile.b0 + h * 64, k, DW ? 0 : tile.expert, bar);
+                }
+                __syncwarp();
+            }
+    } else if (warp == 9) {
+        const uint32_t leader = elect_one() ? 1u : 0u;
+        const bool b_mn = DW || g.b_mn;
+        const uint32_t idesc = gemm_idesc(128, TN, g.bf16, DW, b_mn);
+        const uint32_t a_step = DW ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
+        int i = 0, c = 0;                                         // stages and accumulators used so far
+        for (int t = (int)blockIdx.x; ok && order.find(g, t, TN, tile); t += (int)gridDim.x)
+            for (int kb = 0, in_chunk = 0; kb < tile.nkb; ++kb, ++i) {
+                const int s = i % S;
+                if (in_chunk == 0 && c >= 2) ok = mbar_wait_warp(&acc_empty[c & 1], ((c >> 1) & 1) ^ 1, &abort_flag, g.wait_limit);
+                ok = ok && mbar_wait_warp(&full[s], (i / S) & 1, &abort_flag, g.wait_limit);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+                uint8_t* stage = tiles + s * STAGE;
+                int steps = GEMM_BK / 16;
+                if (DW && kb == tile.nkb - 1) {                   // rows of others behind the expert's last one: a row is 128 bytes of every block
+                    const int valid = tile.red_end - tile.red0 - kb * GEMM_BK;
+                    steps = (valid + 15) / 16;
+                    const int from = valid * 128, to = steps * 2048;
+                    if (from < to) {
+#pragma unroll
+                        for (int b = 0; b < STAGE / 8192; ++b)
+                            for (int o = from + lane * 16; o < to; o += 512) *reinterpret_cast<uint4*>(stage + b * 8192 + o) = make_uint4(0u, 0u, 0u, 0u);
+                        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                        __syncwarp();
+                    }
+                }
+                const uint32_t d = tmem + (uint32_t)((c & 1) * TN);
+                uint64_t* done = &acc_full[c & 1];
+                const int first = in_chunk;
+                const bool last = ++in_chunk == (CHUNKS ? GEMM_LONG : tile.nkb) || kb == tile.nkb - 1;
+                if (last) { in_chunk = 0; ++c; }
+                if (g.test_flags & 1) continue;                   // (give-up test: nothing is ever issued)
+                const uint32_t ah = tile_desc_lo(smem_u32(stage), DW), bh = tile_desc_lo(smem_u32(stage) + A_BYTES, b_mn);
+#pragma unroll
+                for (int k = 0; k < GEMM_BK / 16; ++k)
+                    if (k < steps) umma_f16(leader, d, ah + k * a_step, bh + k * b_step, idesc, (first | k) != 0);
+                umma_commit_pred(leader, &empty[s]);
+                if (last) umma_commit_pred(leader, done);
+            }
+    } else {
+        uint8_t* patch = tiles + S * STAGE + warp * PATCH_BYTES;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * CQ;
+        int c = 0;                                                // accumulators so far
+        for (int t = (int)blockIdx.x; ok && order.find(g, t, TN, tile); t += (int)gridDim.x) {
+            const int row0 = tile.a0 + (warp & 3) * 32, rows = min(tile.a_end - row0, 32);
+            const int col0 = tile.b0 + (warp >> 2) * CQ;
+            auto out = [&](float (&v)[32], int j) {
+                const int left = g.cols - col0 - j;
+                if (rows > 0 && left > 0) finish_columns<T, DW>(g, tile, patch, v, row0, rows, col0 + j, left);
+            };
+            if (CHUNKS) {
+                float acc[CQ];
+#pragma unroll
+                for (int j = 0; j < CQ; ++j) acc[j] = 0.0f;
+                for (int kb = 0; kb < tile.nkb && ok; kb += GEMM_LONG, ++c) {
+                    ok = mbar_wait_bounded(&acc_full[c & 1], (c >> 1) & 1, &abort_flag, g.wait_limit);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+                    if (rows > 0)
+#pragma unroll
+                        for (int j = 0; j < CQ; j += 32) {
+                            uint32_t v[32];
+                            tmem_load<32>(lanes + (c & 1) * TN + j, v);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) acc[j + e] += __uint_as_float(v[e]);
+                        }
+                    asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&acc_empty[c & 1]);
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int j = 0; j < CQ; j += 32) {
+                    float v[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = acc[j + e];
+                    out(v, j);
+                }
+            } else {
+                if (tile.nkb > 0) {
+                    ok = mbar_wait_bounded(&acc_full[c & 1], (c >> 1) & 1, &abort_flag, g.wait_limit);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+                }
+#pragma unroll 1
+                for (int j = 0; j < CQ; j += 32) {
+                    uint32_t raw[32];
+                    float v[32];
+                    if (tile.nkb > 0) tmem_load<32>(lanes + (c & 1) * TN + j, raw);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = tile.nkb > 0 ? __uint_as_float(raw[e]) : 0.0f;
+                    if (j + 32 == CQ && tile.nkb > 0) {           // all sums are in registers: the next tile but one may begin
+                        asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&acc_empty[c & 1]);
+                    }
+                    out(v, j);
+                }
+                c += tile.nkb > 0;
+            }
+        }
+    }
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
+    if (abort_flag) {
+        giveup_drain();
+        if (threadIdx.x == 0) atomicAdd(&g_grouped_timeouts, 1ull);
+    }
+    __syncthreads();
+    if (warp == 9)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(2u * TN) : "memory");
+}
+
+unsigned long long grouped_timeouts() {
+    unsigned long long n = 0;
+    return cudaMemcpyFromSymbol(&n, g_grouped_timeouts, sizeof(n)) == cudaSuccess ? n : 0;
+}
+
+// ---------------------------------------------------------------------------------------------------- dz and dbias
+// dz = dy * act'(z), stored times `store`, and the column sums of dz before its rounding, expert by expert.  A block has 256 columns of a chunk of rows; the
+// sums of the part of chunk c that is expert e's go to place c + e (no two parts share one: the next part has the next chunk or a later expert).
+struct GroupedDz {
+    const void *dy, *z;
+    void* dz;
+    float* part;
+    const int* offsets;
+    long long ldy, ldz, lddz;
+    int m, n, experts, act, chunk_rows, across, vec;
+    float store;
+};
+template <typename T>
+__global__ void __launch_bounds__(256, 4) grouped_dz_kernel(const __grid_constant__ GroupedDz g) {
+    __shared__ float sums[8][256 + 4];
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    const int bx = (int)(blockIdx.x % (unsigned)g.across), chunk = (int)(blockIdx.x / (unsigned)g.across);
+    const int lane = threadIdx.x & 31, y = threadIdx.x >> 5, col = bx * 256 + lane * 8, left = g.n - col;
+    const int c0 = chunk * g.chunk_rows, c1 = min(c0 + g.chunk_rows, g.m);
+    const T *dy = static_cast<const T*>(g.dy) + col, *z = static_cast<const T*>(g.z) + col;
+    T* dz = static_cast<T*>(g.dz) + col;
+    const bool vec = g.vec && left >= 8;
+    auto part_of = [&](int e, int begin, int end) {
+        const int r0 = max(begin, c0), r1 = min(end, c1);
+        float sum[8] = {};
+        for (int r = r0 + y; r < r1 && left > 0; r += 16) {       // two rows under way
+            uint4 a[2], b[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (r + 8 * u < r1) {
+                    a[u] = load_raw(dy + (r + 8 * u) * g.ldy, left, vec);
+                    if (g.act) b[u] = load_raw(z + (r + 8 * u) * g.ldz, left, vec);
+                }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (r + 8 * u >= r1) break;
+                float v[8], zv[8];
+                unpack<T>(a[u], v);
+                if (g.act) unpack<T>(b[u], zv);
+                switch (g.act) {
+#define EBS_SLOPE_CASE(A) case A: _Pragma("unroll") for (int i = 0; i < 8; ++i) v[i] *= activation_slope<true>(zv[i], A); break;
+                    EBS_SLOPE_CASE(EBS_ACT_RELU) EBS_SLOPE_CASE(EBS_ACT_GELU) EBS_SLOPE_CASE(EBS_ACT_GELU_TANH) EBS_SLOPE_CASE(EBS_ACT_SILU)
+#undef EBS_SLOPE_CASE
+                    default: break;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += v[i];
+                if (!g.dz) continue;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= g.store;
+                store_pack(dz + (r + 8 * u) * g.lddz, v);         // (its rows are padded to whole packs)
+            }
+        }
+        if (!g.part) return;
+        __syncthreads();                                          // (the sums before are read)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[y][lane * 8 + i] = sum[i];
+        __syncthreads();
+        if (bx * 256 + (int)threadIdx.x < g.n) {
+            float s = 0.0f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s += sums[q][threadIdx.x];
+            g.part[(long long)(chunk + e) * g.n + bx * 256 + threadIdx.x] = s;
+        }
+    };
+    for (int e0 = 0; e0 < g.experts; e0 += 32) {
+        int begin = 0, count = 0;
+        if (e0 + lane < g.experts) expert_rows(g.offsets, g.m, e0 + lane, begin, count);
+        unsigned hit = __ballot_sync(0xffffffffu, count > 0 && begin < c1 && begin + count > c0);
+        while (hit) {                                             // (the same in every warp)
+            const int l = __ffs(hit) - 1;
+            hit &= hit - 1;
+            const int b = __shfl_sync(0xffffffffu, begin, l);
+            part_of(e0 + l, b, b + __shfl_sync(0xffffffffu, count, l));
+        }
+    }
+}
+// dbias: an expert's chunks in their order, eight warps every eighth.
+template <typename T>
+__global__ void __launch_bounds__(256) grouped_dbias_kernel(const float* __restrict__ part, const int* __restrict__ offsets, int m, int n, int chunk_rows, int across, T* __restrict__ dbias) {
+    __shared__ float sums[8][33];
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    const int e = (int)(blockIdx.x / (unsigned)across), lane = threadIdx.x & 31, y = threadIdx.x >> 5, col = (int)(blockIdx.x % (unsigned)across) * 32 + lane;
+    int begin, count;
+    expert_rows(offsets, m, e, begin, count);
+    float s = 0.0f;
+    if (count > 0 && col < n) {
+        const int last = (begin + count - 1) / chunk_rows;
+#pragma unroll 4
+        for (int c = begin / chunk_rows + y; c <= last; c += 8) s += part[(long long)(c + e) * n + col];
+    }
+    sums[y][lane] = s;
+    __syncthreads();
+    if (y == 0 && col < n) {
+        for (int q = 1; q < 8; ++q) s += sums[q][lane];
+        dbias[(long long)e * n + col] = from_f32<T>(s);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- the calls
+struct GroupedOperand {
+    const void* p;
+    long long ld, expert;                  // elements between rows, between experts
+};
+// A 16-bit matrix as TMA wants it, copied to rows of whole 16 bytes where its own do not start on them.
+static GroupedOperand plan_rows(const void* p, long long rows, int cols, long long ld, Carver& ws, CopyJobs* jobs) {
+    if ((ld & 7) == 0) return {p, ld, 0};
+    const long long ldd = round8(cols);
+    void* to = ws.take<uint16_t>((size_t)rows * ldd);
+    if (p && to && rows > 0) add_copy_rows(jobs, p, to, rows, cols, ld, ldd);
+    return {to, ldd, 0};
+}
+
+template <typename T, int TN, bool DW, bool CHUNKS>
+static int launch_grouped(const CUtensorMap& a, const CUtensorMap& b, const GroupedArgs& g, long long tiles, cudaStream_t st) {
+    auto kern = grouped_kernel<T, TN, DW, CHUNKS>;
+    constexpr int SMEM = grouped_smem_bytes<TN>();
+    static bool attr_set[64] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+        if (check_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM))) return EBS_ERR_CUDA;
+        if (dev >= 0 && dev < 64) attr_set[dev] = true;
+    }
+    const long long at_once = (long long)gemm_sm_count() * (TN == 64 ? 2 : 1);
+    return launch_chained(kern, dim3((unsigned)(tiles < at_once ? tiles : at_once)), GROUPED_THREADS, (size_t)SMEM, st, 1, a, b, g);
+}
+// Columns of a tile: a tile of 256 feeds the tensor core at full rate; where there are not enough of them for the SMs, narrower ones.
+// Sums that go on in registers: 64 a thread.
+static int grouped_columns(long long row_tiles, int cols, bool chunks) {
+    const int sms = gemm_sm_count();
+    if (!chunks && row_tiles * ((cols + 255) / 256) >= sms) return 256;
+    return row_tiles * ((cols + 127) / 128) >= sms ? 128 : 64;
+}
+template <typename T, bool DW>
+static int launch_columns(int tn, const GemmOperand& a, int a_mn, int a_red, const GemmOperand& b, int b_cols, int b_red, int batch, GroupedArgs& g, long long row_tiles, bool chunks, cudaStream_t st) {
+    CUtensorMap ma, mb;
+    const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
+    if (!gemm_operand_map(a, a_mn, a_red, 1, 128, bf16, &ma) || !gemm_operand_map(b, b_cols, b_red, batch, tn, bf16, &mb)) return EBS_ERR_CUDA;
+    g.bf16 = bf16;
+    g.tiles_n = (g.cols + tn - 1) / tn;
+    g.wait_limit = device_wait_limit();
+    g.test_flags = device_test_flags();
+    const long long tiles = row_tiles * g.tiles_n;
+    if (tiles >= (1LL << 30)) return EBS_ERR_OVERFLOW;
+    if (tn == 256) return launch_grouped<T, 256, DW, false>(ma, mb, g, tiles, st);
+    if (tn == 128) return chunks ? launch_grouped<T, 128, DW, true>(ma, mb, g, tiles, st) : launch_grouped<T, 128, DW, false>(ma, mb, g, tiles, st);
+    return chunks ? launch_grouped<T, 64, DW, true>(ma, mb, g, tiles, st) : launch_grouped<T, 64, DW, false>(ma, mb, g, tiles, st);
+}
+// Row tiles there can be at most: one more than whole ones for each expert that has rows.
+static long long most_row_tiles(int m, int experts) { return m / 128 + (experts < m ? experts : m); }
+static long long expected_row_tiles(int m, int experts) {
+    const long long e = experts < m ? experts : m;
+    return e * ((m / e + 127) / 128);
+}
+
+struct GroupedTensors {
+    const void *x, *w, *bias, *residual, *dy, *z;
+    void *y, *keep, *dx, *dw, *dbias;
+    const int* offsets;
+};
+template <typename T>
+static int rows_product(const GroupedTensors& t, int m, int experts, int cols, int red, const GroupedOperand& a, const GroupedOperand& w, bool b_mn, GroupedArgs& g, cudaStream_t st) {
+    g.offsets = t.offsets;
+    g.m = m;
+    g.experts = experts;
+    g.cols = cols;
+    g.red = red;
+    g.b_mn = b_mn;
+    GemmOperand A(a.p, a.ld, false), B(w.p, w.ld, b_mn, 1, 0, w.expert);
+    const bool chunks = red > GEMM_LONG * GEMM_BK;
+    return launch_columns<T, false>(grouped_columns(expected_row_tiles(m, experts), cols, chunks), A, m, red, B, cols, red, experts, g, most_row_tiles(m, experts), chunks, st);
+}
+static bool rows_ok(const void* p, long long ld) { return !p || (ld & 7) == 0; }
+
+template <typename T>
+static int grouped_forward(const ebs_linear_desc& d, int experts, const GroupedTensors& t, Carver& ws, bool run, cudaStream_t st) {
+    if (d.m == 0) return EBS_OK;
+    CopyJobs copies = {};
+    const GroupedOperand x = plan_rows(t.x, d.m, d.k, d.ldx, ws, &copies);
+    GroupedOperand w = plan_rows(t.w, (long long)experts * d.n, d.k, d.ldw, ws, &copies);
+    w.expert = d.n * w.ld;
+    if (!run) return EBS_OK;
+    const int rc = launch_copies(copies, st);
+    if (rc) return rc;
+    GroupedArgs g = {};
+    g.bias = t.bias; g.residual = t.residual; g.y = t.y; g.z = t.keep;
+    g.ldy = d.ldy; g.ldr = d.ldr; g.ldz = d.ldz;
+    g.act = d.act;
+    g.alpha = 1.0f;
+    g.vec = rows_ok(t.y, d.ldy) && rows_ok(t.keep, d.ldz) && rows_ok(t.residual, d.ldr);
+    g.bias_vec = d.n % 8 == 0;
+    return rows_product<T>(t, d.m, experts, d.n, d.k, x, w, false, g, st);
+}
+template <typename T>
+static int grouped_backward(const ebs_linear_desc& d, int experts, const GroupedTensors& t, Carver& ws, bool run, cudaStream_t st) {
+    if (d.m == 0) {
+        if (!run) return EBS_OK;
+        if (t.dw && check_cuda(cudaMemset2DAsync(t.dw, d.ldw * 2, 0, (size_t)d.k * 2, (size_t)experts * d.n, st))) return EBS_ERR_CUDA;
+        if (t.dbias && check_cuda(cudaMemsetAsync(t.dbias, 0, (size_t)experts * d.n * 2, st))) return EBS_ERR_CUDA;
+        return EBS_OK;
+    }
+    CopyJobs copies = {};
+    GroupedOperand dz;
+    void* stored = nullptr;
+    if (d.act) {
+        dz = GroupedOperand{stored = ws.take<uint16_t>((size_t)d.m * round8(d.n)), round8(d.n), 0};
+        if (run && !t.dx && !t.dw) stored = nullptr;
+    } else dz = plan_rows(t.dx || t.dw || !run ? t.dy : nullptr, d.m, d.n, d.ldy, ws, &copies);
+    const GroupedOperand x = plan_rows(t.dw || !run ? t.x : nullptr, d.m, d.k, d.ldx, ws, &copies);
+    GroupedOperand w = plan_rows(t.dx || !run ? t.w : nullptr, (long long)experts * d.n, d.k, d.ldw, ws, &copies);
+    w.expert = d.n * w.ld;
+    const int across = (d.n + 255) / 256;
+    const long long want = (8LL * 148 + across - 1) / across;        // about eight blocks an SM, at least 32 rows each
+    const int chunk_rows = (int)((d.m + want - 1) / want > 32 ? (d.m + want - 1) / want : 32), chunks = (d.m + chunk_rows - 1) / chunk_rows;
+    float* part = ws.take<float>(((size_t)chunks + experts) * d.n);
+    if (!run) return EBS_OK;
+    int rc;
+    if (stored || t.dbias) {
+        if ((long long)chunks * across > 0x7fffffffLL || (long long)experts * ((d.n + 31) / 32) > 0x7fffffffLL) return EBS_ERR_OVERFLOW;
+        GroupedDz g{t.dy, t.z, stored, t.dbias ? part : nullptr, t.offsets, d.ldy, d.ldz, round8(d.n), d.m, d.n, experts, d.act, chunk_rows, across,
+                    (d.ldy & 7) == 0 && (!d.act || (d.ldz & 7) == 0), dz_store_scale(d)};
+        if ((rc = launch_chained(grouped_dz_kernel<T>, dim3((unsigned)(chunks * across)), 256, 0, st, 1, g))) return rc;
+        if (t.dbias && (rc = launch_chained(grouped_dbias_kernel<T>, dim3((unsigned)(experts * ((d.n + 31) / 32))), 256, 0, st, 1, (const float*)part, t.offsets, d.m, d.n, chunk_rows,
+                                            (d.n + 31) / 32, static_cast<T*>(t.dbias))))
+            return rc;
+    }
+    if ((rc = launch_copies(copies, st))) return rc;
+    if (t.dx) {
+        GroupedArgs g = {};
+        g.y = t.dx;
+        g.ldy = d.ldx;
+        g.alpha = 1.0f / dz_store_scale(d);
+        g.vec = rows_ok(t.dx, d.ldx);
+        if ((rc = rows_product<T>(t, d.m, experts, d.k, d.n, dz, w, true, g, st))) return rc;
+    }
+    if (t.dw) {
+        GroupedArgs g = {};
+        g.offsets = t.offsets;
+        g.m = d.m;
+        g.experts = experts;
+        g.rows = d.n;
+        g.cols = d.k;
+        g.y = t.dw;
+        g.ldy = d.ldw;
+        g.y_expert = d.n * d.ldw;
+        g.alpha = 1.0f / dz_store_scale(d);
+        g.vec = rows_ok(t.dw, d.ldw);
+        const long long row_tiles = (long long)experts * ((d.n + 127) / 128);
+        GemmOperand A(dz.p, dz.ld, true), B(x.p, x.ld, true);
+        const bool chunks = d.m > GEMM_LONG * GEMM_BK;
+        if ((rc = launch_columns<T, true>(grouped_columns(row_tiles, d.k, chunks), A, d.n, d.m, B, d.k, d.m, 1, g, row_tiles, chunks, st))) return rc;
+    }
+    return EBS_OK;
+}
+
+// The descriptor of a layer of experts, strides filled in.
+static int complete_grouped(const ebs_linear_desc* in, int experts, ebs_linear_desc* d) {
+    const int rc = complete_linear(in, d);
+    if (rc) return rc;
+    if (experts < 1) return EBS_ERR_INVALID_ARG;
+    if (d->dtype == EBS_F32) return EBS_ERR_UNSUPPORTED;
+    if ((double)experts * d->n * (double)d->ldw > (double)(1LL << 40) || (long long)experts * d->n > (1LL << 31) || d->m > (1 << 30) - 128) return EBS_ERR_OVERFLOW;
+    return EBS_OK;
+}
+static size_t grouped_workspace(const ebs_linear_desc& d, int experts, bool back) {
+    Carver count{nullptr};
+    const GroupedTensors none{};
+    if (back) grouped_backward<__half>(d, experts, none, count, false, nullptr);
+    else grouped_forward<__half>(d, experts, none, count, false, nullptr);
+    return count.used;
+}
+// Whether the offsets lie apart from what the call writes.
+static bool offsets_apart(const int* offsets, int experts, const Rows* t, int count, size_t size) {
+    const uintptr_t o = (uintptr_t)offsets, oe = o + ((size_t)experts + 1) * 4;
+    for (int i = 0; i < count; ++i) {
+        if (!t[i].out || !t[i].p || t[i].rows <= 0) continue;
+        const uintptr_t p = (uintptr_t)t[i].p;
+        if (o < p + ((size_t)(t[i].rows - 1) * t[i].ld + t[i].cols) * size && p < oe) return false;
+    }
+    return true;
+}
+
+}  // namespace ebs
+
+using namespace ebs;
+
+extern "C" {
+
+size_t ebs_grouped_workspace_bytes(const ebs_linear_desc* desc, int experts, int backward) {
+    ebs_linear_desc d;
+    if (complete_grouped(desc, experts, &d)) return 0;
+    return grouped_workspace(d, experts, backward != 0);
+}
+
+int ebs_grouped_forward(const void* x_dev, const void* w_dev, const void* bias_dev, const void* residual_dev, const int* offsets_dev, int experts, const ebs_linear_desc* desc, void* y_dev,
+                        void* z_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
+    ebs_linear_desc d;
+    const int rc = complete_grouped(desc, experts, &d);
+    if (rc) return rc;
+    if (!w_dev || !offsets_dev || ((uintptr_t)offsets_dev & 3u) || (d.m > 0 && (!x_dev || !y_dev))) return EBS_ERR_INVALID_ARG;
+    const size_t need = grouped_workspace(d, experts, false);
+    if (need && (!workspace_dev || workspace_bytes < need)) return EBS_ERR_INVALID_ARG;
+    const long long all = (long long)experts * d.n;
+    const Rows t[] = {{x_dev, d.m, d.k, d.ldx, false}, {w_dev, all, d.k, d.ldw, false}, {bias_dev, 1, all, all, false}, {residual_dev, d.m, d.n, d.ldr, false},
+                      {y_dev, d.m, d.n, d.ldy, true}, {z_dev, d.m, d.n, d.ldz, true}, {need ? workspace_dev : nullptr, 1, (long long)(need / 2), (long long)(need / 2), true}};
+    if (check_tensors(t, 7, 2, &t[3], &t[4]) || !offsets_apart(offsets_dev, experts, t, 7, 2)) return EBS_ERR_INVALID_ARG;
+    Carver ws{static_cast<char*>(workspace_dev)};
+    const GroupedTensors all_t{x_dev, w_dev, bias_dev, residual_dev, nullptr, nullptr, y_dev, z_dev, nullptr, nullptr, nullptr, offsets_dev};
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return d.dtype == EBS_F16 ? grouped_forward<__half>(d, experts, all_t, ws, true, st) : grouped_forward<__nv_bfloat16>(d, experts, all_t, ws, true, st);
+}
+
+int ebs_grouped_backward(const void* dy_dev, const void* x_dev, const void* w_dev, const void* z_dev, const int* offsets_dev, int experts, const ebs_linear_desc* desc, void* dx_dev,
+                         void* dw_dev, void* dbias_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
+    ebs_linear_desc d;
+    const int rc = complete_grouped(desc, experts, &d);
+    if (rc) return rc;
+    if (!dx_dev && !dw_dev && !dbias_dev && d.m > 0) return EBS_ERR_INVALID_ARG;
+    if (!offsets_dev || ((uintptr_t)offsets_dev & 3u)) return EBS_ERR_INVALID_ARG;
+    if (d.m > 0 && (!dy_dev || (dx_dev && !w_dev) || (dw_dev && !x_dev) || (d.act && !z_dev))) return EBS_ERR_INVALID_ARG;
+    const size_t need = grouped_workspace(d, experts, true);
+    if (need && (!workspace_dev || workspace_bytes < need)) return EBS_ERR_INVALID_ARG;
+    const long long all = (long long)experts * d.n;
+    const Rows t[] = {{dy_dev, d.m, d.n, d.ldy, false}, {x_dev, d.m, d.k, d.ldx, false}, {w_dev, all, d.k, d.ldw, false}, {d.act ? z_dev : nullptr, d.m, d.n, d.ldz, false},
+                      {dx_dev, d.m, d.k, d.ldx, true}, {dw_dev, all, d.k, d.ldw, true}, {dbias_dev, 1, all, all, true},
+                      {need ? workspace_dev : nullptr, 1, (long long)(need / 2), (long long)(need / 2), true}};
+    if (check_tensors(t, 8, 2, nullptr, nullptr) || !offsets_apart(offsets_dev, experts, t, 8, 2)) return EBS_ERR_INVALID_ARG;
+    Carver ws{static_cast<char*>(workspace_dev)};
+    const GroupedTensors all_t{x_dev, w_dev, nullptr, nullptr, dy_dev, z_dev, nullptr, nullptr, dx_dev, dw_dev, dbias_dev, offsets_dev};
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return d.dtype == EBS_F16 ? grouped_backward<__half>(d, experts, all_t, ws, true, st) : grouped_backward<__nv_bfloat16>(d, experts, all_t, ws, true, st);
+}
+
+}  // extern "C"
