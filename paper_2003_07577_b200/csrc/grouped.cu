@@ -1,11 +1,15 @@
 // Layers of experts: products grouped by the rows of each expert, and their gradients.  See include/ebs.h.
 //
-// One persistent kernel, two forms.  Rows (forward and dx): tiles of 128 rows of one expert x TN outputs, over the reduction of the layer; the last tile
-// of an expert reads rows of the next one and leaves them out when it writes.  Weights (dW): tiles of 128 x TN of an expert's gradient over the
+// One persistent kernel, two forms.  Rows (forward and dx): tiles of rows of one expert x TN outputs, over the reduction of the layer; the last tile
+// of an expert reads rows of the next one and leaves them out when it writes.  Weights (dW): tiles of an expert's gradient over the
 // expert's own rows; what its last stage holds of other rows is cleared in shared memory before the tensor core reads it.  Offsets are read on the
 // device only: a block finds its tiles by scanning them, 32 experts at a time.
 //
-// Warp 8 fetches by TMA, warp 9 issues the MMAs, warps 0-7 take the sums of the finished tile out of tensor memory while the next one is
+// PAIR: two thread blocks on two SMs take 256 x 256 results (cta_group::2), each fetches its 128 rows of A and half of the columns of B: 128 x 256 results of
+// one block read 192 bytes of shared memory a clock of the tensor core, which has 128 (16384 x 2048 -> 4096 over 16 experts, alone: 240 us, the tensor pipe 68% busy).
+// Without: a block takes 128 x 128 or 128 x 64, where there are few tiles.
+//
+// One warp fetches by TMA, one issues the MMAs, the first 8 (pair: 16) take the sums of the finished tile out of tensor memory while the next one is
 // multiplied (two accumulators).  Sums of more than 4096 terms leave the tensor core on the way, which truncates what it adds.  Results go
 // through a patch of shared memory, so that neighbouring lanes write neighbouring bytes, and leave with ordinary stores: a row that is not the expert's
 // is not written.
@@ -28,12 +32,17 @@ struct GroupedArgs {
     int test_flags;
 };
 
-constexpr int GROUPED_THREADS = 320;
-constexpr int PATCH_PITCH = 80;                                  // bytes: 32 values of a row and 16 bytes, so that eight lanes' rows meet no bank twice
-constexpr int PATCH_BYTES = 32 * PATCH_PITCH;
-template <int TN> __host__ __device__ constexpr int grouped_stage_bytes() { return (128 + TN) * GEMM_ROW_BYTES; }
-template <int TN> __host__ __device__ constexpr int grouped_stages() { return TN == 256 ? 4 : TN == 128 ? 6 : 3; }
-template <int TN> __host__ __device__ constexpr int grouped_smem_bytes() { return grouped_stages<TN>() * grouped_stage_bytes<TN>() + 8 * PATCH_BYTES + 1024; }
+// The forms by the columns of a tile: 256 a pair, 128 a block an SM, 64 two blocks an SM.
+template <int TN> struct GroupedForm {
+    static constexpr bool PAIR = TN == 256;
+    static constexpr int B_COLS = PAIR ? TN / 2 : TN;             // columns of B that a block fetches
+    static constexpr int EPI_WARPS = PAIR ? 16 : 8, THREADS = PAIR ? 640 : 320;        // (pair: whole warpgroups, whose registers are dealt anew)
+    static constexpr int STAGES = TN == 64 ? 3 : 6, STAGE = (128 + B_COLS) * GEMM_ROW_BYTES;
+    static constexpr int CQ = TN / (EPI_WARPS / 4);               // columns of a warp
+    static constexpr int PATCH = 32 * 64;                         // 32 rows of 64 bytes
+    static constexpr int SMEM = STAGES * STAGE + EPI_WARPS * PATCH + 1024;
+    static constexpr int ROWS = PAIR ? 256 : 128;                 // rows of a tile
+};
 
 // Rows of expert e; offsets that are out of order or out of range are taken as the nearest ones that are not.
 __device__ __forceinline__ void expert_rows(const int* offsets, int m, int e, int& begin, int& count) {
@@ -46,12 +55,12 @@ struct GroupedTile {
     int nkb;
 };
 // The tiles in their order; a warp asks for ever larger ones.
-template <bool DW>
+template <bool DW, int ROWS>
 struct GroupedTiles {
     int e0 = 0, before = 0;                // tiles of the experts below e0
     __device__ __forceinline__ bool find(const GroupedArgs& g, int t, int tile_cols, GroupedTile& tile) {
         if (DW) {
-            const int tiles_m = (g.rows + 127) / 128, per = tiles_m * g.tiles_n;
+            const int tiles_m = (g.rows + ROWS - 1) / ROWS, per = tiles_m * g.tiles_n;
             tile.expert = t / per;
             if (tile.expert >= g.experts) return false;
             t -= tile.expert * per;
@@ -59,7 +68,7 @@ struct GroupedTiles {
             expert_rows(g.offsets, g.m, tile.expert, tile.red0, count);
             tile.red_end = tile.red0 + count;
             tile.nkb = (count + GEMM_BK - 1) / GEMM_BK;
-            tile.a0 = t % tiles_m * 128;
+            tile.a0 = t % tiles_m * ROWS;
             tile.a_end = g.rows;
             tile.b0 = t / tiles_m * tile_cols;
             return true;
@@ -68,7 +77,7 @@ struct GroupedTiles {
         for (; e0 < g.experts; e0 += 32) {
             int begin = 0, count = 0;
             if (e0 + lane < g.experts) expert_rows(g.offsets, g.m, e0 + lane, begin, count);
-            const int mine = (count + 127) / 128 * g.tiles_n;
+            const int mine = (count + ROWS - 1) / ROWS * g.tiles_n;
             int sum = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -80,9 +89,9 @@ struct GroupedTiles {
                 const int l = __ffs(hit) - 1, in = t - before - __shfl_sync(0xffffffffu, sum - mine, l);
                 begin = __shfl_sync(0xffffffffu, begin, l);
                 count = __shfl_sync(0xffffffffu, count, l);
-                const int tiles_m = (count + 127) / 128;
+                const int tiles_m = (count + ROWS - 1) / ROWS;
                 tile.expert = e0 + l;
-                tile.a0 = begin + in % tiles_m * 128;
+                tile.a0 = begin + in % tiles_m * ROWS;
                 tile.a_end = begin + count;
                 tile.b0 = in / tiles_m * tile_cols;
                 tile.red0 = tile.red_end = 0;
@@ -95,6 +104,8 @@ struct GroupedTiles {
     }
 };
 
+// Chunk c (16 bytes) of row `row` of a patch; rows are 64 bytes, their chunks permuted so that eight lanes' rows meet no bank twice.
+__device__ __forceinline__ uint4* patch_chunk(uint8_t* patch, int row, int c) { return reinterpret_cast<uint4*>(patch + row * 64 + ((c ^ ((row >> 1) & 3)) << 4)); }
 // 32 values of this lane's row, through the warp's patch, to `rows` rows of 32 columns (`left` of them exist).
 template <typename T>
 __device__ __forceinline__ void store_patch(uint8_t* patch, const float (&v)[32], T* to, long long ld, int rows, int left, bool vec) {
@@ -102,17 +113,17 @@ __device__ __forceinline__ void store_patch(uint8_t* patch, const float (&v)[32]
     __syncwarp();                                                 // (what was there is read)
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-        *reinterpret_cast<uint4*>(patch + lane * PATCH_PITCH + c * 16) =
+        *patch_chunk(patch, lane, c) =
             make_uint4(pair_word<T>(v[8 * c], v[8 * c + 1]), pair_word<T>(v[8 * c + 2], v[8 * c + 3]), pair_word<T>(v[8 * c + 4], v[8 * c + 5]), pair_word<T>(v[8 * c + 6], v[8 * c + 7]));
     __syncwarp();
     if (vec && left >= 32) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = i * 8 + (lane >> 2), c = lane & 3;
-            if (r < rows) *reinterpret_cast<uint4*>(to + r * ld + c * 8) = *reinterpret_cast<const uint4*>(patch + r * PATCH_PITCH + c * 16);
+            if (r < rows) *reinterpret_cast<uint4*>(to + r * ld + c * 8) = *patch_chunk(patch, r, c);
         }
     } else if (lane < left)
-        for (int r = 0; r < rows; ++r) to[r * ld + lane] = reinterpret_cast<const T*>(patch + r * PATCH_PITCH)[lane];
+        for (int r = 0; r < rows; ++r) to[r * ld + lane] = reinterpret_cast<const T*>(patch_chunk(patch, r, lane >> 3))[lane & 7];
 }
 
 // The sums of 32 columns of the warp's rows on their way out: row0 the warp's first row, rows how many it has.
@@ -154,85 +165,146 @@ __device__ __forceinline__ void finish_columns(const GroupedArgs& g, const Group
     store_patch(patch, v, y, g.ldy, rows, left, g.vec);
 }
 
+__device__ __forceinline__ void tma_load_3d_of_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst), "l"(map),
+                 "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void umma_f16_of_pair(uint32_t leader, uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %3};\n\t"
+        "mov.b64 db, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, p;\n\t}\n"
+        :: "r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(TILE_DESC_HI), "r"(idesc), "r"(accumulate), "r"(leader)
+        : "memory");
+}
+// Completion of the pair's MMAs issued so far, on the barrier at this place in both blocks.
+__device__ __forceinline__ void umma_commit_pair(uint32_t leader, uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %2, 0;\n\t"
+        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t"
+        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}\n"
+        ::"r"(cluster_addr(bar, 0)), "r"(cluster_addr(bar, 1)), "r"(leader) : "memory");
+}
+
 // DW: the form for weight gradients.  CHUNKS: sums leave tensor memory every GEMM_LONG stages and go on in registers.
 template <typename T, int TN, bool DW, bool CHUNKS>
-__global__ void __launch_bounds__(GROUPED_THREADS, TN == 64 ? 2 : 1) grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                                                     const __grid_constant__ GroupedArgs g) {
+__global__ void __launch_bounds__(GroupedForm<TN>::THREADS, TN == 64 ? 2 : 1) grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                                                              const __grid_constant__ GroupedArgs g) {
     extern __shared__ uint8_t smem_raw[];
-    constexpr int S = grouped_stages<TN>(), STAGE = grouped_stage_bytes<TN>(), A_BYTES = 128 * GEMM_ROW_BYTES, CQ = TN / 2;
-    __shared__ uint64_t full[S], empty[S], acc_full[2], acc_empty[2];
+    using Form = GroupedForm<TN>;
+    constexpr bool PAIR = Form::PAIR;
+    constexpr int S = Form::STAGES, STAGE = Form::STAGE, A_BYTES = 128 * GEMM_ROW_BYTES, CQ = Form::CQ, EPI = Form::EPI_WARPS;
+    __shared__ uint64_t full[S], empty[S], acc_full[2], acc_empty[2], ready[S];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (warp >= 8 && lane == 0) asm volatile("prefetch.tensormap [%0];\n" ::"l"(warp == 8 ? &map_a : &map_b) : "memory");
+    const int rank = PAIR ? (int)(blockIdx.x & 1) : 0, step = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x, start = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
+    if (warp >= EPI && warp < EPI + 2 && lane == 0) asm volatile("prefetch.tensormap [%0];\n" ::"l"(warp == EPI ? &map_a : &map_b) : "memory");
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 8); }
+        for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); mbar_init(&ready[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], PAIR ? 2 * EPI : EPI); }
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
-    if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_slot)), "r"(2u * TN) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+    if (warp == EPI + 1) {
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_slot)), "r"(2u * TN) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_slot)), "r"(2u * TN) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
     __syncthreads();
+    if (PAIR) cluster_sync_all();                                 // the partner's barriers are ready too
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
     const uint32_t tmem = uni(tmem_slot);
     let_next_kernel_start();
     wait_for_previous_kernel();
 
-    GroupedTiles<DW> order;
+    GroupedTiles<DW, Form::ROWS> order;
     GroupedTile tile;
     bool ok = true;
-    if (warp == 8) {
+    // Rows of the last stage of a weight gradient that are the expert's; a remainder of 16 (an MMA's depth): the others of those 16 are cleared.
+    auto last_rows = [&] { return tile.red_end - tile.red0 - (tile.nkb - 1) * GEMM_BK; };
+    if (warp >= EPI) {
+      // Pair: registers are dealt anew among the warpgroups: 4 * 128 * 104 + 128 * 56 = 60416 of the 640 * 96 = 61440 the block was launched with.
+      if (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
+      if (warp == EPI) {
         const bool leader = elect_one();
         int i = 0;                                                // stages filled so far
-        for (int t = (int)blockIdx.x; ok && order.find(g, t, TN, tile); t += (int)gridDim.x)
+        for (int t = start; ok && order.find(g, t, TN, tile); t += step) {
+            const int a0 = tile.a0 + rank * 128, b0 = tile.b0 + rank * Form::B_COLS;
+            const bool tail = PAIR && DW && tile.nkb > 0 && (last_rows() & 15) != 0;
             for (int kb = 0; kb < tile.nkb; ++kb, ++i) {
                 const int s = i % S, k = tile.red0 + kb * GEMM_BK;
                 ok = mbar_wait_warp(&empty[s], ((i / S) & 1) ^ 1, &abort_flag, g.wait_limit);
                 if (!ok) break;
                 if (leader) {
-                    const uint32_t at = smem_u32(tiles) + s * STAGE, bt = at + A_BYTES, bar = smem_u32(&full[s]);
-                    mbar_expect_tx(&full[s], STAGE);
-                    if (DW) { tma_load_3d(at, &map_a, tile.a0, k, 0, bar); tma_load_3d(at + 8192, &map_a, tile.a0 + 64, k, 0, bar); }
-                    else tma_load_3d(at, &map_a, k, tile.a0, 0, bar);
-                    if (!DW && !g.b_mn) tma_load_3d(bt, &map_b, k, tile.b0, tile.expert, bar);
+                    const uint32_t at = smem_u32(tiles) + s * STAGE, bt = at + A_BYTES;
+                    // pair: both blocks' copies report to the first one, but for a last stage that each clears for itself
+                    const bool own = !PAIR || (tail && kb == tile.nkb - 1);
+                    const uint32_t to = PAIR ? cluster_addr(&full[s], own ? rank : 0) : smem_u32(&full[s]);
+                    if (own) mbar_expect_tx(&full[s], STAGE);
+                    else if (rank == 0) mbar_expect_tx(&full[s], 2 * STAGE);
+                    auto load = [&](uint32_t dst, const CUtensorMap* map, int x, int y, int z) {
+                        if (PAIR) tma_load_3d_of_pair(dst, map, x, y, z, to);
+                        else tma_load_3d(dst, map, x, y, z, to);
+                    };
+                    if (DW) { load(at, &map_a, a0, k, 0); load(at + 8192, &map_a, a0 + 64, k, 0); }
+                    else load(at, &map_a, k, a0, 0);
+                    if (!DW && !g.b_mn) load(bt, &map_b, k, b0, tile.expert);
                     else
 #pragma unroll
-                        for (int h = 0; h < TN / 64; ++h) tma_load_3d(bt + h * 8192, &map_b, tile.b0 + h * 64, k, DW ? 0 : tile.expert, bar);
+                        for (int h = 0; h < Form::B_COLS / 64; ++h) load(bt + h * 8192, &map_b, b0 + h * 64, k, DW ? 0 : tile.expert);
                 }
                 __syncwarp();
             }
-    } else if (warp == 9) {
+        }
+      } else if (warp == EPI + 1 && (rank == 0 || DW)) {          // (the second block of a pair only clears)
         const uint32_t leader = elect_one() ? 1u : 0u;
         const bool b_mn = DW || g.b_mn;
-        const uint32_t idesc = gemm_idesc(128, TN, g.bf16, DW, b_mn);
+        const uint32_t idesc = gemm_idesc(PAIR ? 256 : 128, TN, g.bf16, DW, b_mn);
         const uint32_t a_step = DW ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
-        int i = 0, c = 0;                                         // stages and accumulators used so far
-        for (int t = (int)blockIdx.x; ok && order.find(g, t, TN, tile); t += (int)gridDim.x)
+        int i = 0, c = 0;                                         // stages and accumulators so far
+        unsigned cleared = 0u;                                    // bit s: phase of what a pair reports of cleared stages in place s
+        for (int t = start; ok && order.find(g, t, TN, tile); t += step) {
             for (int kb = 0, in_chunk = 0; kb < tile.nkb; ++kb, ++i) {
                 const int s = i % S;
-                if (in_chunk == 0 && c >= 2) ok = mbar_wait_warp(&acc_empty[c & 1], ((c >> 1) & 1) ^ 1, &abort_flag, g.wait_limit);
-                ok = ok && mbar_wait_warp(&full[s], (i / S) & 1, &abort_flag, g.wait_limit);
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
                 uint8_t* stage = tiles + s * STAGE;
-                int steps = GEMM_BK / 16;
-                if (DW && kb == tile.nkb - 1) {                   // rows of others behind the expert's last one: a row is 128 bytes of every block
-                    const int valid = tile.red_end - tile.red0 - kb * GEMM_BK;
+                int steps = GEMM_BK / 16, valid = GEMM_BK;
+                if (DW && kb == tile.nkb - 1) {
+                    valid = last_rows();
                     steps = (valid + 15) / 16;
-                    const int from = valid * 128, to = steps * 2048;
-                    if (from < to) {
+                }
+                const bool tail = DW && (valid & 15) != 0;
+                if (rank != 0 && !tail) continue;
+                if (rank == 0 && in_chunk == 0 && c >= 2) ok = mbar_wait_cluster_warp(&acc_empty[c & 1], ((c >> 1) & 1) ^ 1, &abort_flag, g.wait_limit);
+                // (the second block's barriers count cleared stages alone)
+                ok = ok && mbar_wait_warp(&full[s], rank != 0 ? cleared >> s & 1u : (i / S) & 1, &abort_flag, g.wait_limit);
+                if (!ok) break;
+                if (tail) {                                       // a row is 128 bytes of every block of 64 columns
 #pragma unroll
-                        for (int b = 0; b < STAGE / 8192; ++b)
-                            for (int o = from + lane * 16; o < to; o += 512) *reinterpret_cast<uint4*>(stage + b * 8192 + o) = make_uint4(0u, 0u, 0u, 0u);
-                        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-                        __syncwarp();
+                    for (int b = 0; b < STAGE / 8192; ++b)
+                        for (int o = valid * 128 + lane * 16; o < steps * 2048; o += 512) *reinterpret_cast<uint4*>(stage + b * 8192 + o) = make_uint4(0u, 0u, 0u, 0u);
+                    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                    __syncwarp();
+                    if (PAIR) {
+                        if (rank == 0) ok = mbar_wait_cluster_warp(&ready[s], cleared >> s & 1u, &abort_flag, g.wait_limit);
+                        else if (lane == 0) mbar_arrive_cluster(cluster_addr(&ready[s], 0));
+                        cleared ^= 1u << s;
+                        if (!ok) break;
+                        if (rank != 0) continue;
                     }
                 }
+                asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
                 const uint32_t d = tmem + (uint32_t)((c & 1) * TN);
                 uint64_t* done = &acc_full[c & 1];
                 const int first = in_chunk;
@@ -242,16 +314,35 @@ __global__ void __launch_bounds__(GROUPED_THREADS, TN == 64 ? 2 : 1) grouped_ker
                 const uint32_t ah = tile_desc_lo(smem_u32(stage), DW), bh = tile_desc_lo(smem_u32(stage) + A_BYTES, b_mn);
 #pragma unroll
                 for (int k = 0; k < GEMM_BK / 16; ++k)
-                    if (k < steps) umma_f16(leader, d, ah + k * a_step, bh + k * b_step, idesc, (first | k) != 0);
-                umma_commit_pred(leader, &empty[s]);
-                if (last) umma_commit_pred(leader, done);
+                    if (k < steps) {
+                        if (PAIR) umma_f16_of_pair(leader, d, ah + k * a_step, bh + k * b_step, idesc, (first | k) != 0);
+                        else umma_f16(leader, d, ah + k * a_step, bh + k * b_step, idesc, (first | k) != 0);
+                    }
+                if (PAIR) {
+                    umma_commit_pair(leader, &empty[s]);
+                    if (last) umma_commit_pair(leader, done);
+                } else {
+                    umma_commit_pred(leader, &empty[s]);
+                    if (last) umma_commit_pred(leader, done);
+                }
             }
+        }
+      }
     } else {
-        uint8_t* patch = tiles + S * STAGE + warp * PATCH_BYTES;
+        if (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;\n");
+        uint8_t* patch = tiles + S * STAGE + warp * Form::PATCH;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * CQ;
         int c = 0;                                                // accumulators so far
-        for (int t = (int)blockIdx.x; ok && order.find(g, t, TN, tile); t += (int)gridDim.x) {
-            const int row0 = tile.a0 + (warp & 3) * 32, rows = min(tile.a_end - row0, 32);
+        auto taken = [&] {                                        // this warp has its part of accumulator c
+            asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) mbar_arrive_cluster(cluster_addr(&acc_empty[c & 1], 0));
+                else mbar_arrive(&acc_empty[c & 1]);
+            }
+        };
+        for (int t = start; ok && order.find(g, t, TN, tile); t += step) {
+            const int row0 = tile.a0 + rank * 128 + (warp & 3) * 32, rows = min(tile.a_end - row0, 32);
             const int col0 = tile.b0 + (warp >> 2) * CQ;
             auto out = [&](float (&v)[32], int j) {
                 const int left = g.cols - col0 - j;
@@ -273,9 +364,7 @@ __global__ void __launch_bounds__(GROUPED_THREADS, TN == 64 ? 2 : 1) grouped_ker
 #pragma unroll
                             for (int e = 0; e < 32; ++e) acc[j + e] += __uint_as_float(v[e]);
                         }
-                    asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&acc_empty[c & 1]);
+                    taken();
                 }
                 if (!ok) break;
 #pragma unroll
@@ -298,11 +387,7 @@ __global__ void __launch_bounds__(GROUPED_THREADS, TN == 64 ? 2 : 1) grouped_ker
                     if (tile.nkb > 0) tmem_load<32>(lanes + (c & 1) * TN + j, raw);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = tile.nkb > 0 ? __uint_as_float(raw[e]) : 0.0f;
-                    if (j + 32 == CQ && tile.nkb > 0) {           // all sums are in registers: the next tile but one may begin
-                        asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&acc_empty[c & 1]);
-                    }
+                    if (j + 32 == CQ && tile.nkb > 0) taken();    // all sums are in registers: the next tile but one may begin
                     out(v, j);
                 }
                 c += tile.nkb > 0;
@@ -315,9 +400,14 @@ __global__ void __launch_bounds__(GROUPED_THREADS, TN == 64 ? 2 : 1) grouped_ker
         giveup_drain();
         if (threadIdx.x == 0) atomicAdd(&g_grouped_timeouts, 1ull);
     }
-    __syncthreads();
-    if (warp == 9)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(2u * TN) : "memory");
+    if (PAIR) {
+        asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
+        cluster_sync_all();                                       // no block leaves while the other's MMAs or arrivals reach it
+        if (warp == EPI + 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(2u * TN) : "memory");
+    } else {
+        __syncthreads();
+        if (warp == EPI + 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(2u * TN) : "memory");
+    }
 }
 
 unsigned long long grouped_timeouts() {
@@ -443,7 +533,8 @@ static GroupedOperand plan_rows(const void* p, long long rows, int cols, long lo
 template <typename T, int TN, bool DW, bool CHUNKS>
 static int launch_grouped(const CUtensorMap& a, const CUtensorMap& b, const GroupedArgs& g, long long tiles, cudaStream_t st) {
     auto kern = grouped_kernel<T, TN, DW, CHUNKS>;
-    constexpr int SMEM = grouped_smem_bytes<TN>();
+    constexpr int SMEM = GroupedForm<TN>::SMEM;
+    static_assert(SMEM + 512 <= 227 * 1024, "shared memory of a block");
     static bool attr_set[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
@@ -451,36 +542,38 @@ static int launch_grouped(const CUtensorMap& a, const CUtensorMap& b, const Grou
         if (check_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM))) return EBS_ERR_CUDA;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    const long long at_once = (long long)gemm_sm_count() * (TN == 64 ? 2 : 1);
-    return launch_chained(kern, dim3((unsigned)(tiles < at_once ? tiles : at_once)), GROUPED_THREADS, (size_t)SMEM, st, 1, a, b, g);
+    constexpr int cluster = GroupedForm<TN>::PAIR ? 2 : 1;
+    const long long at_once = (long long)gemm_sm_count() * (TN == 64 ? 2 : 1) / cluster;
+    return launch_chained(kern, dim3((unsigned)(cluster * (tiles < at_once ? tiles : at_once))), GroupedForm<TN>::THREADS, (size_t)SMEM, st, cluster, a, b, g);
 }
-// Columns of a tile: a tile of 256 feeds the tensor core at full rate; where there are not enough of them for the SMs, narrower ones.
-// Sums that go on in registers: 64 a thread.
-static int grouped_columns(long long row_tiles, int cols, bool chunks) {
+// Columns of a tile; rows_of_pair, rows_of_block: how many times 256 and 128 rows there are to cover.  Pairs where there is a tile for each of them (a tile of 256 x 256
+// a pair takes less than 128 x 128 a block each), else tiles for every SM, else the narrowest ones.
+static int grouped_columns(long long rows_of_pair, long long rows_of_block, int cols) {
     const int sms = gemm_sm_count();
-    if (!chunks && row_tiles * ((cols + 255) / 256) >= sms) return 256;
-    return row_tiles * ((cols + 127) / 128) >= sms ? 128 : 64;
+    if (rows_of_pair * ((cols + 255) / 256) >= sms / 2) return 256;
+    return rows_of_block * ((cols + 127) / 128) >= sms ? 128 : 64;
 }
 template <typename T, bool DW>
 static int launch_columns(int tn, const GemmOperand& a, int a_mn, int a_red, const GemmOperand& b, int b_cols, int b_red, int batch, GroupedArgs& g, long long row_tiles, bool chunks, cudaStream_t st) {
+    // row_tiles: of the form that was chosen
     CUtensorMap ma, mb;
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
-    if (!gemm_operand_map(a, a_mn, a_red, 1, 128, bf16, &ma) || !gemm_operand_map(b, b_cols, b_red, batch, tn, bf16, &mb)) return EBS_ERR_CUDA;
+    if (!gemm_operand_map(a, a_mn, a_red, 1, 128, bf16, &ma) || !gemm_operand_map(b, b_cols, b_red, batch, tn == 256 ? 128 : tn, bf16, &mb)) return EBS_ERR_CUDA;
     g.bf16 = bf16;
     g.tiles_n = (g.cols + tn - 1) / tn;
     g.wait_limit = device_wait_limit();
     g.test_flags = device_test_flags();
     const long long tiles = row_tiles * g.tiles_n;
     if (tiles >= (1LL << 30)) return EBS_ERR_OVERFLOW;
-    if (tn == 256) return launch_grouped<T, 256, DW, false>(ma, mb, g, tiles, st);
+    if (tn == 256) return chunks ? launch_grouped<T, 256, DW, true>(ma, mb, g, tiles, st) : launch_grouped<T, 256, DW, false>(ma, mb, g, tiles, st);
     if (tn == 128) return chunks ? launch_grouped<T, 128, DW, true>(ma, mb, g, tiles, st) : launch_grouped<T, 128, DW, false>(ma, mb, g, tiles, st);
     return chunks ? launch_grouped<T, 64, DW, true>(ma, mb, g, tiles, st) : launch_grouped<T, 64, DW, false>(ma, mb, g, tiles, st);
 }
-// Row tiles there can be at most: one more than whole ones for each expert that has rows.
-static long long most_row_tiles(int m, int experts) { return m / 128 + (experts < m ? experts : m); }
-static long long expected_row_tiles(int m, int experts) {
+// Tiles of `tile` rows there can be at most: one more than whole ones for each expert that has rows; and how many there are where all have the same number.
+static long long most_row_tiles(int m, int experts, int tile) { return m / tile + (experts < m ? experts : m); }
+static long long expected_row_tiles(int m, int experts, int tile) {
     const long long e = experts < m ? experts : m;
-    return e * ((m / e + 127) / 128);
+    return e * ((m / e + tile - 1) / tile);
 }
 
 struct GroupedTensors {
@@ -498,7 +591,8 @@ static int rows_product(const GroupedTensors& t, int m, int experts, int cols, i
     g.b_mn = b_mn;
     GemmOperand A(a.p, a.ld, false), B(w.p, w.ld, b_mn, 1, 0, w.expert);
     const bool chunks = red > GEMM_LONG * GEMM_BK;
-    return launch_columns<T, false>(grouped_columns(expected_row_tiles(m, experts), cols, chunks), A, m, red, B, cols, red, experts, g, most_row_tiles(m, experts), chunks, st);
+    const int tn = grouped_columns(expected_row_tiles(m, experts, 256), expected_row_tiles(m, experts, 128), cols);
+    return launch_columns<T, false>(tn, A, m, red, B, cols, red, experts, g, most_row_tiles(m, experts, tn == 256 ? 256 : 128), chunks, st);
 }
 static bool rows_ok(const void* p, long long ld) { return !p || (ld & 7) == 0; }
 
@@ -575,10 +669,11 @@ static int grouped_backward(const ebs_linear_desc& d, int experts, const Grouped
         g.y_expert = d.n * d.ldw;
         g.alpha = 1.0f / dz_store_scale(d);
         g.vec = rows_ok(t.dw, d.ldw);
-        const long long row_tiles = (long long)experts * ((d.n + 127) / 128);
+        const long long pairs = (long long)experts * ((d.n + 255) / 256), blocks = (long long)experts * ((d.n + 127) / 128);
+        const int tn = grouped_columns(pairs, blocks, d.k);
         GemmOperand A(dz.p, dz.ld, true), B(x.p, x.ld, true);
         const bool chunks = d.m > GEMM_LONG * GEMM_BK;
-        if ((rc = launch_columns<T, true>(grouped_columns(row_tiles, d.k, chunks), A, d.n, d.m, B, d.k, d.m, 1, g, row_tiles, chunks, st))) return rc;
+        if ((rc = launch_columns<T, true>(tn, A, d.n, d.m, B, d.k, d.m, 1, g, tn == 256 ? pairs : blocks, chunks, st))) return rc;
     }
     return EBS_OK;
 }

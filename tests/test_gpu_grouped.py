@@ -146,9 +146,11 @@ def test_some_gradients(ebs, want, act):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-def test_wide_tiles(ebs, dtype):
-    """Enough tiles of 256 columns for every SM, several a block."""
-    layer(ebs, 7, [700, 1500, 0, 900, 129], 2056, 512, dtype, act=4, keep=True)
+@pytest.mark.parametrize("n,k", [(2056, 512), (520, 2100), (2300, 2056)])
+@pytest.mark.parametrize("counts", [[700, 1500, 0, 900, 129], [256, 512, 1024, 1280], [5, 300, 3, 17, 1, 2, 33, 64, 48, 2000, 9, 1, 1, 1, 1, 1]], ids=str)
+def test_wide_tiles(ebs, dtype, n, k, counts):
+    """Enough tiles of 256 columns for every pair of SMs, several a pair; experts of fewer rows than a stage one behind the other."""
+    layer(ebs, 7, counts, n, k, dtype, act=4, keep=True, spare=100)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
@@ -156,6 +158,9 @@ def test_long_sums(ebs, dtype):
     """Reductions that leave the tensor core on the way, in every product: input features, output features, rows."""
     layer(ebs, 8, [4097, 9000, 3], 72, 136, dtype, act=0)
     layer(ebs, 9, [40, 7], 4200, 4168, dtype, act=0)
+    layer(ebs, 10, [5001, 4200], 1100, 2100, dtype, act=0)               # pairs of blocks: dW's sums are long
+    layer(ebs, 11, [1500, 2000], 2056, 4200, dtype, act=0)               # y's
+    layer(ebs, 12, [1500, 2000], 4200, 2056, dtype, act=0)               # dx's
 
 
 def test_no_rows(ebs):
@@ -303,7 +308,7 @@ def test_elements_past_32_bits(ebs):
 
 
 # tiles of 64, 128 and 256 columns, sums in chunks
-@pytest.mark.parametrize("counts,n,k", [([40, 3], 64, 128), ([3000, 1000], 1000, 264), ([4000, 4000], 1500, 128), ([6000, 7], 72, 4200)])
+@pytest.mark.parametrize("counts,n,k", [([40, 3], 64, 128), ([3000, 1000], 1000, 264), ([3001, 1000], 2500, 2100), ([4000, 4000], 1500, 128), ([6000, 7], 72, 4200), ([6000, 2001], 2500, 4200)])
 def test_waits_that_give_up(ebs, counts, n, k):
     """Nothing is issued to the tensor core: every wait runs out, the calls return, the status says so once, and the next calls are right."""
     m, experts, t = sum(counts), len(counts), torch.bfloat16
