@@ -33,12 +33,6 @@ __device__ __forceinline__ void put_row(uint8_t* buffer, int lane, const float (
         store_pack(reinterpret_cast<T*>(row_chunk(buffer, lane, c)), t);
     }
 }
-__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void* src, int x, int y, int z) {
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];\n" ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z) : "memory");
-}
-__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;\n" ::: "memory"); }
-__device__ __forceinline__ void tma_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
-
 // A warp's ring of R buffers: a buffer is written again when the store that reads it, R stores back, is done with it.
 template <int R>
 struct RowRing {
@@ -261,32 +255,6 @@ template <int PL, int TN> __host__ __device__ constexpr int pair_smem_bytes() {
     return pair_stages<PL, TN>() * pair_stage_bytes<PL, TN>() + PAIR_EPI_WARPS * PAIR_RING * PAIR_BUFFER + PAIR_TERMS + PAIR_BARRIERS;
 }
 
-// A load into this block's shared memory that signals a barrier of either block of the pair.
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst), "l"(map),
-                 "r"(x), "r"(y), "r"(z), "r"(bar)
-                 : "memory");
-}
-__device__ __forceinline__ void umma_f16_pair(uint32_t leader, uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
-        "mov.b64 da, {%1, %3};\n\t"
-        "mov.b64 db, {%2, %3};\n\t"
-        "setp.ne.b32 p, %5, 0;\n\t"
-        "setp.ne.b32 q, %6, 0;\n\t"
-        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, p;\n\t}\n"
-        :: "r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(TILE_DESC_HI), "r"(idesc), "r"(accumulate), "r"(leader)
-        : "memory");
-}
-// Completion of the pair's MMAs issued so far, on the barrier at this place in both blocks.
-__device__ __forceinline__ void umma_commit_both(uint32_t leader, uint32_t bar0, uint32_t bar1) {
-    asm volatile(
-        "{\n\t.reg .pred q;\n\t"
-        "setp.ne.b32 q, %2, 0;\n\t"
-        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t"
-        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}\n"
-        ::"r"(bar0), "r"(bar1), "r"(leader) : "memory");
-}
 // Tiles in bands of eight tile rows, column by column within a band: the tiles under way at a time share few rows and columns.
 // A symmetric result: only the tiles of the 256 x 256 squares on and below the diagonal, row by row.
 // Parts of the reduction of one tile follow one another.
@@ -604,18 +572,6 @@ unsigned long long gemm_pair_timeouts() {
     return cudaMemcpyFromSymbol(&n, g_gemm_pair_timeouts, sizeof(n)) == cudaSuccess ? n : 0;
 }
 
-// Tensor map of outputs: matrices [rows][cols] of `slices`, 64 bytes by 32 rows a store.  False: rows that do not start on 16 bytes, or end
-// inside 16 bytes (a store is clipped to whole 16 bytes: it would write past the end of each row).
-template <typename T>
-static bool result_map(const void* p, long long rows, long long cols, long long ld, long long slices, long long slice, CUtensorMap* map, bool padded = false) {
-    if (!p) return true;
-    if (((uintptr_t)p & 15) != 0 || (ld * sizeof(T)) % 16 != 0 || (slice * sizeof(T)) % 16 != 0 || (!padded && (cols * sizeof(T)) % 16 != 0)) return false;
-    const CUtensorMapDataType type = std::is_same<T, float>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)slices};
-    const cuuint64_t strides[2] = {(cuuint64_t)ld * sizeof(T), (cuuint64_t)(slices > 1 ? slice : ld * rows) * sizeof(T)};
-    const cuuint32_t box[3] = {(cuuint32_t)(64 / sizeof(T)), 32, 1};
-    return encode_map(map, type, p, dims, strides, box, true);
-}
 template <typename T>
 static bool result_maps(const LinearOut<T>& e, const GemmShape& s, CUtensorMap* y, CUtensorMap* z) {
     const auto whole = [](const void* p, long long ld) { return !p || (((uintptr_t)p & 15) == 0 && (ld * sizeof(T)) % 16 == 0); };

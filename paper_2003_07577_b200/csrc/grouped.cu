@@ -26,7 +26,7 @@ struct GroupedArgs {
     void *y, *z;
     long long ldy, ldr, ldz, y_expert;     // y_expert: elements between the results of two experts (weights)
     int m, experts, rows, cols, red;       // rows: of a weight gradient
-    int tiles_n, b_mn, bf16, act, vec, bias_vec;
+    int tiles_n, b_mn, bf16, act, vec, bias_vec, tma;
     float alpha;
     unsigned wait_limit;
     int test_flags;
@@ -91,9 +91,13 @@ struct GroupedTiles {
                 count = __shfl_sync(0xffffffffu, count, l);
                 const int tiles_m = (count + ROWS - 1) / ROWS;
                 tile.expert = e0 + l;
-                tile.a0 = begin + in % tiles_m * ROWS;
+                // bands of 2048 rows, column by column within a band: the tiles under way at a time share few rows and columns (18944 rows of 4096 that
+                // are one expert's, 2048 columns: 249 us row by row of all, whose operand is larger than the second-level cache, 223 so)
+                constexpr int BAND = 2048 / ROWS;
+                const int band = in / (BAND * g.tiles_n), first = band * BAND, height = min(tiles_m - first, BAND), rest = in - first * g.tiles_n;
+                tile.a0 = begin + (first + rest % height) * ROWS;
                 tile.a_end = begin + count;
-                tile.b0 = in / tiles_m * tile_cols;
+                tile.b0 = rest / height * tile_cols;
                 tile.red0 = tile.red_end = 0;
                 tile.nkb = (g.red + GEMM_BK - 1) / GEMM_BK;
                 return true;
@@ -106,15 +110,26 @@ struct GroupedTiles {
 
 // Chunk c (16 bytes) of row `row` of a patch; rows are 64 bytes, their chunks permuted so that eight lanes' rows meet no bank twice.
 __device__ __forceinline__ uint4* patch_chunk(uint8_t* patch, int row, int c) { return reinterpret_cast<uint4*>(patch + row * 64 + ((c ^ ((row >> 1) & 3)) << 4)); }
-// 32 values of this lane's row, through the warp's patch, to `rows` rows of 32 columns (`left` of them exist).
+// 32 values of this lane's row, through the warp's patch, to `rows` rows of 32 columns (`left` of them exist) from `to` on: by one TMA store (map; x, row, z: where)
+// where all 32 rows are the expert's or the map ends where they do, else by the lanes.
 template <typename T>
-__device__ __forceinline__ void store_patch(uint8_t* patch, const float (&v)[32], T* to, long long ld, int rows, int left, bool vec) {
+__device__ __forceinline__ void store_patch(uint8_t* patch, const float (&v)[32], T* to, long long ld, int rows, int left, bool vec, bool by_tma, const CUtensorMap* map, int x, int row, int z) {
     const int lane = threadIdx.x & 31;
-    __syncwarp();                                                 // (what was there is read)
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");         // what was there is read
+    __syncwarp();
 #pragma unroll
     for (int c = 0; c < 4; ++c)
         *patch_chunk(patch, lane, c) =
             make_uint4(pair_word<T>(v[8 * c], v[8 * c + 1]), pair_word<T>(v[8 * c + 2], v[8 * c + 3]), pair_word<T>(v[8 * c + 4], v[8 * c + 5]), pair_word<T>(v[8 * c + 6], v[8 * c + 7]));
+    if (by_tma) {
+        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            tma_store_3d(map, patch, x, row, z);
+            tma_store_commit();
+        }
+        return;
+    }
     __syncwarp();
     if (vec && left >= 32) {
 #pragma unroll
@@ -128,7 +143,9 @@ __device__ __forceinline__ void store_patch(uint8_t* patch, const float (&v)[32]
 
 // The sums of 32 columns of the warp's rows on their way out: row0 the warp's first row, rows how many it has.
 template <typename T, bool DW>
-__device__ __forceinline__ void finish_columns(const GroupedArgs& g, const GroupedTile& tile, uint8_t* patch, float (&v)[32], int row0, int rows, int col, int left) {
+__device__ __forceinline__ void finish_columns(const GroupedArgs& g, const GroupedTile& tile, uint8_t* patch, float (&v)[32], int row0, int rows, int col, int left, const CUtensorMap* map_y,
+                                               const CUtensorMap* map_z) {
+    const bool by_tma = g.tma && (DW || rows == 32);
     const int lane = threadIdx.x & 31;
     T* y = static_cast<T*>(g.y) + (DW ? tile.expert * g.y_expert : 0) + (long long)row0 * g.ldy + col;
 #pragma unroll
@@ -144,7 +161,7 @@ __device__ __forceinline__ void finish_columns(const GroupedArgs& g, const Group
                 for (int i = 0; i < 8; ++i) v[8 * c + i] += t[i];
             }
         }
-        if (g.z) store_patch(patch, v, static_cast<T*>(g.z) + (long long)row0 * g.ldz + col, g.ldz, rows, left, g.vec);
+        if (g.z) store_patch(patch, v, static_cast<T*>(g.z) + (long long)row0 * g.ldz + col, g.ldz, rows, left, g.vec, by_tma, map_z, col, row0, 0);
         switch (g.act) {
 #define EBS_ACT_CASE(A) case A: _Pragma("unroll") for (int i = 0; i < 32; ++i) v[i] = activation<true>(v[i], A); break;
             EBS_ACT_CASE(EBS_ACT_RELU) EBS_ACT_CASE(EBS_ACT_GELU) EBS_ACT_CASE(EBS_ACT_GELU_TANH) EBS_ACT_CASE(EBS_ACT_SILU)
@@ -162,38 +179,13 @@ __device__ __forceinline__ void finish_columns(const GroupedArgs& g, const Group
             }
         }
     }
-    store_patch(patch, v, y, g.ldy, rows, left, g.vec);
-}
-
-__device__ __forceinline__ void tma_load_3d_of_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst), "l"(map),
-                 "r"(x), "r"(y), "r"(z), "r"(bar)
-                 : "memory");
-}
-__device__ __forceinline__ void umma_f16_of_pair(uint32_t leader, uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
-        "mov.b64 da, {%1, %3};\n\t"
-        "mov.b64 db, {%2, %3};\n\t"
-        "setp.ne.b32 p, %5, 0;\n\t"
-        "setp.ne.b32 q, %6, 0;\n\t"
-        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, p;\n\t}\n"
-        :: "r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(TILE_DESC_HI), "r"(idesc), "r"(accumulate), "r"(leader)
-        : "memory");
-}
-// Completion of the pair's MMAs issued so far, on the barrier at this place in both blocks.
-__device__ __forceinline__ void umma_commit_pair(uint32_t leader, uint64_t* bar) {
-    asm volatile(
-        "{\n\t.reg .pred q;\n\t"
-        "setp.ne.b32 q, %2, 0;\n\t"
-        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t"
-        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}\n"
-        ::"r"(cluster_addr(bar, 0)), "r"(cluster_addr(bar, 1)), "r"(leader) : "memory");
+    store_patch(patch, v, y, g.ldy, rows, left, g.vec, by_tma, map_y, col, row0, DW ? tile.expert : 0);
 }
 
 // DW: the form for weight gradients.  CHUNKS: sums leave tensor memory every GEMM_LONG stages and go on in registers.
 template <typename T, int TN, bool DW, bool CHUNKS>
 __global__ void __launch_bounds__(GroupedForm<TN>::THREADS, TN == 64 ? 2 : 1) grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                                                              const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z,
                                                                                               const __grid_constant__ GroupedArgs g) {
     extern __shared__ uint8_t smem_raw[];
     using Form = GroupedForm<TN>;
@@ -206,6 +198,7 @@ __global__ void __launch_bounds__(GroupedForm<TN>::THREADS, TN == 64 ? 2 : 1) gr
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)(blockIdx.x & 1) : 0, step = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x, start = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
     if (warp >= EPI && warp < EPI + 2 && lane == 0) asm volatile("prefetch.tensormap [%0];\n" ::"l"(warp == EPI ? &map_a : &map_b) : "memory");
+    if (warp == 0 && lane == 0 && g.tma) asm volatile("prefetch.tensormap [%0];\n" ::"l"(&map_y) : "memory");
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); mbar_init(&ready[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], PAIR ? 2 * EPI : EPI); }
@@ -255,7 +248,7 @@ __global__ void __launch_bounds__(GroupedForm<TN>::THREADS, TN == 64 ? 2 : 1) gr
                     if (own) mbar_expect_tx(&full[s], STAGE);
                     else if (rank == 0) mbar_expect_tx(&full[s], 2 * STAGE);
                     auto load = [&](uint32_t dst, const CUtensorMap* map, int x, int y, int z) {
-                        if (PAIR) tma_load_3d_of_pair(dst, map, x, y, z, to);
+                        if (PAIR) tma_load_3d_pair(dst, map, x, y, z, to);
                         else tma_load_3d(dst, map, x, y, z, to);
                     };
                     if (DW) { load(at, &map_a, a0, k, 0); load(at + 8192, &map_a, a0 + 64, k, 0); }
@@ -315,12 +308,12 @@ __global__ void __launch_bounds__(GroupedForm<TN>::THREADS, TN == 64 ? 2 : 1) gr
 #pragma unroll
                 for (int k = 0; k < GEMM_BK / 16; ++k)
                     if (k < steps) {
-                        if (PAIR) umma_f16_of_pair(leader, d, ah + k * a_step, bh + k * b_step, idesc, (first | k) != 0);
+                        if (PAIR) umma_f16_pair(leader, d, ah + k * a_step, bh + k * b_step, idesc, (first | k) != 0);
                         else umma_f16(leader, d, ah + k * a_step, bh + k * b_step, idesc, (first | k) != 0);
                     }
                 if (PAIR) {
-                    umma_commit_pair(leader, &empty[s]);
-                    if (last) umma_commit_pair(leader, done);
+                    umma_commit_both(leader, cluster_addr(&empty[s], 0), cluster_addr(&empty[s], 1));
+                    if (last) umma_commit_both(leader, cluster_addr(done, 0), cluster_addr(done, 1));
                 } else {
                     umma_commit_pred(leader, &empty[s]);
                     if (last) umma_commit_pred(leader, done);
@@ -346,7 +339,7 @@ __global__ void __launch_bounds__(GroupedForm<TN>::THREADS, TN == 64 ? 2 : 1) gr
             const int col0 = tile.b0 + (warp >> 2) * CQ;
             auto out = [&](float (&v)[32], int j) {
                 const int left = g.cols - col0 - j;
-                if (rows > 0 && left > 0) finish_columns<T, DW>(g, tile, patch, v, row0, rows, col0 + j, left);
+                if (rows > 0 && left > 0) finish_columns<T, DW>(g, tile, patch, v, row0, rows, col0 + j, left, &map_y, &map_z);
             };
             if (CHUNKS) {
                 float acc[CQ];
@@ -393,6 +386,7 @@ __global__ void __launch_bounds__(GroupedForm<TN>::THREADS, TN == 64 ? 2 : 1) gr
                 c += tile.nkb > 0;
             }
         }
+        if (lane == 0) tma_store_wait_all();
     }
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
@@ -531,7 +525,7 @@ static GroupedOperand plan_rows(const void* p, long long rows, int cols, long lo
 }
 
 template <typename T, int TN, bool DW, bool CHUNKS>
-static int launch_grouped(const CUtensorMap& a, const CUtensorMap& b, const GroupedArgs& g, long long tiles, cudaStream_t st) {
+static int launch_grouped(const CUtensorMap (&map)[4], const GroupedArgs& g, long long tiles, cudaStream_t st) {
     auto kern = grouped_kernel<T, TN, DW, CHUNKS>;
     constexpr int SMEM = GroupedForm<TN>::SMEM;
     static_assert(SMEM + 512 <= 227 * 1024, "shared memory of a block");
@@ -544,7 +538,7 @@ static int launch_grouped(const CUtensorMap& a, const CUtensorMap& b, const Grou
     }
     constexpr int cluster = GroupedForm<TN>::PAIR ? 2 : 1;
     const long long at_once = (long long)gemm_sm_count() * (TN == 64 ? 2 : 1) / cluster;
-    return launch_chained(kern, dim3((unsigned)(cluster * (tiles < at_once ? tiles : at_once))), GroupedForm<TN>::THREADS, (size_t)SMEM, st, cluster, a, b, g);
+    return launch_chained(kern, dim3((unsigned)(cluster * (tiles < at_once ? tiles : at_once))), GroupedForm<TN>::THREADS, (size_t)SMEM, st, cluster, map[0], map[1], map[2], map[3], g);
 }
 // Columns of a tile; rows_of_pair, rows_of_block: how many times 256 and 128 rows there are to cover.  Pairs where there is a tile for each of them (a tile of 256 x 256
 // a pair takes less than 128 x 128 a block each), else tiles for every SM, else the narrowest ones.
@@ -556,18 +550,20 @@ static int grouped_columns(long long rows_of_pair, long long rows_of_block, int 
 template <typename T, bool DW>
 static int launch_columns(int tn, const GemmOperand& a, int a_mn, int a_red, const GemmOperand& b, int b_cols, int b_red, int batch, GroupedArgs& g, long long row_tiles, bool chunks, cudaStream_t st) {
     // row_tiles: of the form that was chosen
-    CUtensorMap ma, mb;
+    CUtensorMap map[4] = {};
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
-    if (!gemm_operand_map(a, a_mn, a_red, 1, 128, bf16, &ma) || !gemm_operand_map(b, b_cols, b_red, batch, tn == 256 ? 128 : tn, bf16, &mb)) return EBS_ERR_CUDA;
+    if (!gemm_operand_map(a, a_mn, a_red, 1, 128, bf16, &map[0]) || !gemm_operand_map(b, b_cols, b_red, batch, tn == 256 ? 128 : tn, bf16, &map[1])) return EBS_ERR_CUDA;
     g.bf16 = bf16;
+    g.tma = DW ? result_map<T>(g.y, g.rows, g.cols, g.ldy, g.experts, g.y_expert, &map[2])
+               : result_map<T>(g.y, g.m, g.cols, g.ldy, 1, 0, &map[2]) && result_map<T>(g.z, g.m, g.cols, g.ldz, 1, 0, &map[3]);
     g.tiles_n = (g.cols + tn - 1) / tn;
     g.wait_limit = device_wait_limit();
     g.test_flags = device_test_flags();
     const long long tiles = row_tiles * g.tiles_n;
     if (tiles >= (1LL << 30)) return EBS_ERR_OVERFLOW;
-    if (tn == 256) return chunks ? launch_grouped<T, 256, DW, true>(ma, mb, g, tiles, st) : launch_grouped<T, 256, DW, false>(ma, mb, g, tiles, st);
-    if (tn == 128) return chunks ? launch_grouped<T, 128, DW, true>(ma, mb, g, tiles, st) : launch_grouped<T, 128, DW, false>(ma, mb, g, tiles, st);
-    return chunks ? launch_grouped<T, 64, DW, true>(ma, mb, g, tiles, st) : launch_grouped<T, 64, DW, false>(ma, mb, g, tiles, st);
+    if (tn == 256) return chunks ? launch_grouped<T, 256, DW, true>(map, g, tiles, st) : launch_grouped<T, 256, DW, false>(map, g, tiles, st);
+    if (tn == 128) return chunks ? launch_grouped<T, 128, DW, true>(map, g, tiles, st) : launch_grouped<T, 128, DW, false>(map, g, tiles, st);
+    return chunks ? launch_grouped<T, 64, DW, true>(map, g, tiles, st) : launch_grouped<T, 64, DW, false>(map, g, tiles, st);
 }
 // Tiles of `tile` rows there can be at most: one more than whole ones for each expert that has rows; and how many there are where all have the same number.
 static long long most_row_tiles(int m, int experts, int tile) { return m / tile + (experts < m ? experts : m); }
