@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4
                     float s = to_f32(kept);
                     const int group = ((kb0 + b) * Q4_K + r * 32) / G;
                     if ((lane & 3) == 0 && (G == 32 || r == 0) && (G != 128 || b == 0) && group < g.groups)
-                        static_cast<T*>(g.scales)[(tile * g.groups + group) * Q4_ROWS + gid + 8 * half] = row < g.n ? kept : from_f32<T>(0.0f);
+                        static_cast<T*>(g.scales)[(tile * g.groups + group) * Q4_ROWS + 2 * gid + half] = row < g.n ? kept : from_f32<T>(0.0f);
                     if (!(s > 0.0f) || (__float_as_uint(s) & 0x7f800000u) == 0x7f800000u) continue;          // (codes of zero)
                     const float up = s < 1e-30f ? 1.2676506e30f : 1.0f;                                      // 2^100: no reciprocal overflows, no remainder is lost
                     s *= up;
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(256) q4_unpack_kernel(const __grid_constant__ 
             for (int r = 0; r < 2; ++r) {
                 const int row = row0 + gid + 8 * half, c = kb * Q4_K + q4_input(r, lane, 0);
                 if (row >= g.n || c >= g.k) continue;
-                const float s = to_f32(static_cast<const T*>(g.scales)[(tile * g.groups + (kb * Q4_K + r * 32) / g.group) * Q4_ROWS + gid + 8 * half]);
+                const float s = to_f32(static_cast<const T*>(g.scales)[(tile * g.groups + (kb * Q4_K + r * 32) / g.group) * Q4_ROWS + 2 * gid + half]);
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = s * (float)((int)(word[2 * r + (e >> 2)] >> (4 * (2 * ((e >> 1) & 1) + half) + 16 * (e & 1)) & 15u) - 8);
@@ -213,8 +213,12 @@ template <> struct Q4Operand<__half> {
         a[3] = raw(__hfma2(bits((v & 0x00f000f0u) | 0x64006400u), sixteenth, high));
     }
     static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    static __device__ __forceinline__ void mma_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {       // the sum begins
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
     }
 };
 template <> struct Q4Operand<__nv_bfloat16> {
@@ -229,8 +233,12 @@ template <> struct Q4Operand<__nv_bfloat16> {
         }
     }
     static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    static __device__ __forceinline__ void mma_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {       // the sum begins
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
     }
 };
 template <> struct Q4Operand<float> : Q4Operand<__nv_bfloat16> {};
@@ -239,10 +247,6 @@ template <> struct Q4Operand<float> : Q4Operand<__nv_bfloat16> {};
 template <typename T> struct Q4Acts {
     static constexpr int PL = 1;
     uint32_t b[1][8];
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b[0][i] = 0u;
-    }
     // x: the lane's first element; left: elements of the row from there on
     __device__ __forceinline__ void load(const T* x, int left, bool whole) {
         if (whole) {
@@ -262,12 +266,6 @@ template <typename T> struct Q4Acts {
 template <> struct Q4Acts<float> {
     static constexpr int PL = 3;
     uint32_t b[3][8];                                               // the low bits first
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int p = 0; p < 3; ++p)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) b[p][i] = 0u;
-    }
     // x = high + middle + low, each what the one before left cut to bf16: exact.  An infinity or a NaN is all in the first.
     static __device__ __forceinline__ void planes(float x, uint32_t (&t)[3]) {
         uint32_t bits = __float_as_uint(x);
@@ -304,7 +302,7 @@ struct Q4Args {
     const int* offsets;
     void* y;
     long long ldx, ldr, ldy;
-    int m, n, k, experts, tiles, kbs, groups, group_shift, slots, act;
+    int m, n, k, experts, tiles, kbs, groups, slots, act;
 };
 constexpr int Q4_WARPS = 8;
 
@@ -346,11 +344,19 @@ __device__ __forceinline__ bool q4_slot(const Q4Args& g, int slot, int most, int
     return false;
 }
 
-// A block: 16 * MT outputs of up to 8 * NT rows; its warps share the reduction and add up in shared memory, in their order.
-template <typename T, int NT, int MT, bool G32>
+// The scales of outputs gid and gid + 8 of a tile.
+__device__ __forceinline__ float2 scale_pair(const float* p) { return *reinterpret_cast<const float2*>(p); }
+__device__ __forceinline__ float2 scale_pair(const __half* p) { return __half22float2(*reinterpret_cast<const __half2*>(p)); }
+__device__ __forceinline__ float2 scale_pair(const __nv_bfloat16* p) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p)); }
+
+// A block: 16 * MT outputs of up to 8 * NT rows; its warps share the reduction and add up in shared memory, in their order.  Columns of the MMA beyond the last row
+// take its activations again and are not written.
+template <typename T, int NT, int MT, int G>
 __global__ void __launch_bounds__(Q4_WARPS * 32) q4_kernel(const __grid_constant__ Q4Args g) {
     extern __shared__ float sums[];                                 // [warp][row][16 * MT outputs]
     constexpr int COLS = Q4_ROWS * MT, ROWS = 8 * NT, D = MT == 1 ? 4 : 2;
+    // tiles whose sum meets a scale: a group's two where that leaves the registers for it
+    constexpr int UNIT = G == 128 && NT <= 2 ? 2 : 1;
     using Acts = Q4Acts<T>;
     using Operand = Q4Operand<T>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
@@ -359,17 +365,19 @@ __global__ void __launch_bounds__(Q4_WARPS * 32) q4_kernel(const __grid_constant
     const int slot = (int)(blockIdx.x % (unsigned)g.slots), tile0 = (int)(blockIdx.x / (unsigned)g.slots) * MT;
     int expert, row0, rows;
     if (!q4_slot(g, slot, ROWS, expert, row0, rows)) return;
-    const int kb0 = (int)((long long)g.kbs * warp / Q4_WARPS), kb1 = (int)((long long)g.kbs * (warp + 1) / Q4_WARPS);
-    const T* x = static_cast<const T*>(g.x) + (long long)(row0 + gid) * g.ldx + tig * 8;
+    const int units = (g.kbs + UNIT - 1) / UNIT, kb0 = (int)((long long)units * warp / Q4_WARPS) * UNIT, kb1 = min((int)((long long)units * (warp + 1) / Q4_WARPS) * UNIT, g.kbs);
+    const T* x[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) x[i] = static_cast<const T*>(g.x) + (long long)(row0 + min(gid + 8 * i, rows - 1)) * g.ldx + tig * 8 + (long long)kb0 * Q4_K;
     const uint4* codes[MT];
     const T* scales[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         const long long tile = (long long)expert * g.tiles + min(tile0 + t, g.tiles - 1);
-        codes[t] = g.codes + tile * g.kbs * 32 + lane;
-        scales[t] = static_cast<const T*>(g.scales) + tile * g.groups * Q4_ROWS + gid;
+        codes[t] = g.codes + (tile * g.kbs + kb0) * 32 + lane;
+        scales[t] = static_cast<const T*>(g.scales) + tile * g.groups * Q4_ROWS + 2 * gid;
     }
-    float acc[MT][NT][4];
+    float acc[MT][NT][4], c[MT][NT][4];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -377,56 +385,77 @@ __global__ void __launch_bounds__(Q4_WARPS * 32) q4_kernel(const __grid_constant
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[t][i][e] = 0.0f;
 
-    uint4 w[D][MT], next[D][MT];
+    // one tile of 64 inputs; begin: its sum begins here, end: it meets its scale
+    auto multiply = [&](const uint4 (&w)[MT], int kb, const Acts (&b)[NT], bool begin, bool end) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const uint32_t word[4] = {w[t].x, w[t].y, w[t].z, w[t].w};
+            uint32_t a[4][4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) Operand::make(word[s], a[s]);
+#pragma unroll
+            for (int q = 0; q < (G == 32 ? 2 : 1); ++q) {
+                const int group = G == 32 ? min(kb * 2 + q, g.groups - 1) : G == 64 ? kb : kb >> 1;
+                float2 s = make_float2(0.0f, 0.0f);
+                if (end) s = scale_pair(scales[t] + group * Q4_ROWS);
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+#pragma unroll
+                    for (int p = 0; p < Acts::PL; ++p)
+#pragma unroll
+                        for (int r = G == 32 ? 2 * q : 0; r < (G == 32 ? 2 * q + 2 : 4); ++r) {
+                            if (p == 0 && r == (G == 32 ? 2 * q : 0) && begin) Operand::mma_first(c[t][i], a[r], b[i].b[p][2 * r], b[i].b[p][2 * r + 1]);
+                            else Operand::mma(c[t][i], a[r], b[i].b[p][2 * r], b[i].b[p][2 * r + 1]);
+                        }
+                    if (end) {
+                        acc[t][i][0] = fmaf(c[t][i][0], s.x, acc[t][i][0]);
+                        acc[t][i][1] = fmaf(c[t][i][1], s.x, acc[t][i][1]);
+                        acc[t][i][2] = fmaf(c[t][i][2], s.y, acc[t][i][2]);
+                        acc[t][i][3] = fmaf(c[t][i][3], s.y, acc[t][i][3]);
+                    }
+                }
+            }
+        }
+    };
+    const int whole = min(kb1, g.k / Q4_K);                         // tiles that are all there
+    uint4 next[D][MT];
 #pragma unroll
     for (int d = 0; d < D; ++d)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) next[d][t] = kb0 + d < kb1 ? load_stream(codes[t] + (long long)(kb0 + d) * 32) : make_uint4(0u, 0u, 0u, 0u);
+        for (int t = 0; t < MT; ++t)
+            if (kb0 + d < kb1) next[d][t] = load_stream(codes[t] + d * 32);
 #pragma unroll 1
     for (int kb = kb0; kb < kb1; kb += D) {
+        uint4 w[D][MT];
 #pragma unroll
         for (int d = 0; d < D; ++d)
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 w[d][t] = next[d][t];
-                if (kb + D + d < kb1) next[d][t] = load_stream(codes[t] + (long long)(kb + D + d) * 32);
+                if (kb + D + d < kb1) next[d][t] = load_stream(codes[t] + (D + d) * 32);
             }
+        if (kb + D <= whole) {
 #pragma unroll
-        for (int d = 0; d < D; ++d) {
-            if (kb + d >= kb1) break;
-            const int k = (kb + d) * Q4_K, left = g.k - k - tig * 8;
-            const bool whole = k + Q4_K <= g.k;
-            Acts b[NT];
+            for (int d = 0; d < D; ++d) {
+                Acts b[NT];
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                if (gid + 8 * i < rows) b[i].load(x + (long long)(8 * i) * g.ldx + k, left, whole);
-                else b[i].zero();
+                for (int i = 0; i < NT; ++i) b[i].load(x[i] + d * Q4_K, Q4_K, true);
+                multiply(w[d], kb + d, b, d % UNIT == 0, d % UNIT == UNIT - 1);
             }
+        } else {
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                const uint32_t word[4] = {w[d][t].x, w[d][t].y, w[d][t].z, w[d][t].w};
-                uint32_t a[4][4];
+            for (int d = 0; d < D; ++d) {
+                if (kb + d >= kb1) break;
+                Acts b[NT];
 #pragma unroll
-                for (int s = 0; s < 4; ++s) Operand::make(word[s], a[s]);
-#pragma unroll
-                for (int q = 0; q < (G32 ? 2 : 1); ++q) {
-                    const int group = G32 ? min((kb + d) * 2 + q, g.groups - 1) : (kb + d) >> g.group_shift;
-                    const float s0 = to_f32(scales[t][group * Q4_ROWS]), s1 = to_f32(scales[t][group * Q4_ROWS + 8]);
-#pragma unroll
-                    for (int i = 0; i < NT; ++i) {
-                        float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                        for (int p = 0; p < Acts::PL; ++p)
-#pragma unroll
-                            for (int s = G32 ? 2 * q : 0; s < (G32 ? 2 * q + 2 : 4); ++s) Operand::mma(c, a[s], b[i].b[p][2 * s], b[i].b[p][2 * s + 1]);
-                        acc[t][i][0] = fmaf(c[0], s0, acc[t][i][0]);
-                        acc[t][i][1] = fmaf(c[1], s0, acc[t][i][1]);
-                        acc[t][i][2] = fmaf(c[2], s1, acc[t][i][2]);
-                        acc[t][i][3] = fmaf(c[3], s1, acc[t][i][3]);
-                    }
-                }
+                for (int i = 0; i < NT; ++i) b[i].load(x[i] + d * Q4_K, g.k - (kb + d) * Q4_K - tig * 8, kb + d < whole);
+                multiply(w[d], kb + d, b, d % UNIT == 0, d % UNIT == UNIT - 1 || kb + d == kb1 - 1);
             }
         }
+#pragma unroll
+        for (int t = 0; t < MT; ++t) codes[t] += D * 32;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) x[i] += D * Q4_K;
     }
     float* mine = sums + warp * ROWS * COLS;
 #pragma unroll
@@ -450,10 +479,10 @@ __global__ void __launch_bounds__(Q4_WARPS * 32) q4_kernel(const __grid_constant
     }
 }
 
-template <typename T, int NT, int MT, bool G32>
+template <typename T, int NT, int MT, int G>
 static int launch_q4(const Q4Args& g, long long blocks, cudaStream_t st) {
     constexpr int SMEM = Q4_WARPS * 8 * NT * Q4_ROWS * MT * 4;
-    auto kern = q4_kernel<T, NT, MT, G32>;
+    auto kern = q4_kernel<T, NT, MT, G>;
     if (SMEM > 48 * 1024) {
         static bool attr_set[64] = {};
         int dev = 0;
@@ -480,7 +509,7 @@ static int launch_q4_group(Q4Args& g, int group, cudaStream_t st) {
     const long long blocks = pieces * ((g.tiles + MT - 1) / MT);
     if (blocks > 0x7fffffffLL) return EBS_ERR_OVERFLOW;
     g.slots = (int)pieces;
-    return group == 32 ? launch_q4<T, NT, MT, true>(g, blocks, st) : launch_q4<T, NT, MT, false>(g, blocks, st);
+    return group == 32 ? launch_q4<T, NT, MT, 32>(g, blocks, st) : group == 64 ? launch_q4<T, NT, MT, 64>(g, blocks, st) : launch_q4<T, NT, MT, 128>(g, blocks, st);
 }
 template <typename T>
 static int launch_q4_rows(Q4Args& g, int group, int dtype, cudaStream_t st) {
@@ -612,7 +641,7 @@ int ebs_linear_q4_forward(const void* x_dev, const void* packed_dev, const void*
     if (d.m == 0) return EBS_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     Q4Args g{x_dev, static_cast<const char*>(packed_dev) + l.codes, bias_dev, residual_dev, static_cast<const uint4*>(packed_dev), offsets_dev, y_dev, d.ldx, d.ldr, d.ldy,
-             d.m, d.n, d.k, q4->experts, l.tiles, l.kbs, l.groups, q4->group == 128 ? 1 : 0, 0, d.act};
+             d.m, d.n, d.k, q4->experts, l.tiles, l.kbs, l.groups, 0, d.act};
     if (copied) {                                                  // (fp32 rows as twice as many 16-bit elements)
         const int halves = (int)(size / 2);
         CopyJobs jobs = {};
