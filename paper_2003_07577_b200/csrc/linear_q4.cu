@@ -352,7 +352,7 @@ __device__ __forceinline__ float2 scale_pair(const __nv_bfloat16* p) { return __
 // A block: 16 * MT outputs of up to 8 * NT rows; its warps share the reduction and add up in shared memory, in their order.  Columns of the MMA beyond the last row
 // take its activations again and are not written.
 template <typename T, int NT, int MT, int G>
-__global__ void __launch_bounds__(Q4_WARPS * 32) q4_kernel(const __grid_constant__ Q4Args g) {
+__global__ void __launch_bounds__(Q4_WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : NT <= 2 ? 2 : 1) q4_kernel(const __grid_constant__ Q4Args g) {
     extern __shared__ float sums[];                                 // [warp][row][16 * MT outputs]
     constexpr int COLS = Q4_ROWS * MT, ROWS = 8 * NT, D = MT == 1 ? 4 : 2;
     // tiles whose sum meets a scale: a group's two where that leaves the registers for it
@@ -418,22 +418,14 @@ __global__ void __launch_bounds__(Q4_WARPS * 32) q4_kernel(const __grid_constant
         }
     };
     const int whole = min(kb1, g.k / Q4_K);                         // tiles that are all there
-    uint4 next[D][MT];
+    uint4 w[D][MT];                                                 // D tiles under way: a place is loaded anew when it is used
 #pragma unroll
     for (int d = 0; d < D; ++d)
 #pragma unroll
         for (int t = 0; t < MT; ++t)
-            if (kb0 + d < kb1) next[d][t] = load_stream(codes[t] + d * 32);
+            if (kb0 + d < kb1) w[d][t] = load_stream(codes[t] + d * 32);
 #pragma unroll 1
     for (int kb = kb0; kb < kb1; kb += D) {
-        uint4 w[D][MT];
-#pragma unroll
-        for (int d = 0; d < D; ++d)
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                w[d][t] = next[d][t];
-                if (kb + D + d < kb1) next[d][t] = load_stream(codes[t] + (D + d) * 32);
-            }
         if (kb + D <= whole) {
 #pragma unroll
             for (int d = 0; d < D; ++d) {
@@ -441,6 +433,9 @@ __global__ void __launch_bounds__(Q4_WARPS * 32) q4_kernel(const __grid_constant
 #pragma unroll
                 for (int i = 0; i < NT; ++i) b[i].load(x[i] + d * Q4_K, Q4_K, true);
                 multiply(w[d], kb + d, b, d % UNIT == 0, d % UNIT == UNIT - 1);
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    if (kb + D + d < kb1) w[d][t] = load_stream(codes[t] + (D + d) * 32);
             }
         } else {
 #pragma unroll
@@ -451,6 +446,7 @@ __global__ void __launch_bounds__(Q4_WARPS * 32) q4_kernel(const __grid_constant
                 for (int i = 0; i < NT; ++i) b[i].load(x[i] + d * Q4_K, g.k - (kb + d) * Q4_K - tig * 8, kb + d < whole);
                 multiply(w[d], kb + d, b, d % UNIT == 0, d % UNIT == UNIT - 1 || kb + d == kb1 - 1);
             }
+            break;                                                  // (the warp's last tiles)
         }
 #pragma unroll
         for (int t = 0; t < MT; ++t) codes[t] += D * 32;
