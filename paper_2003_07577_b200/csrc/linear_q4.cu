@@ -198,6 +198,12 @@ __device__ __forceinline__ uint4 load_stream(const uint4* p) {      // read once
     asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
+// (w & mask) | bits in one instruction (the compiler makes two of it: the two constants do not fit one).
+__device__ __forceinline__ uint32_t masked(uint32_t w, uint32_t mask, uint32_t bits) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;\n" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+    return r;
+}
 // Operand registers of one MMA from a word of codes: the values code - 8.
 template <typename T> struct Q4Operand;
 template <> struct Q4Operand<__half> {
@@ -207,10 +213,10 @@ template <> struct Q4Operand<__half> {
         const __half2 low = __floats2half2_rn(-1032.0f, -1032.0f), sixteenth = __floats2half2_rn(0.0625f, 0.0625f), high = __floats2half2_rn(-72.0f, -72.0f);
         auto bits = [](uint32_t x) { return *reinterpret_cast<__half2*>(&x); };
         auto raw = [](__half2 x) { return *reinterpret_cast<uint32_t*>(&x); };
-        a[0] = raw(__hadd2(bits((w & 0x000f000fu) | 0x64006400u), low));
-        a[1] = raw(__hfma2(bits((w & 0x00f000f0u) | 0x64006400u), sixteenth, high));
-        a[2] = raw(__hadd2(bits((v & 0x000f000fu) | 0x64006400u), low));
-        a[3] = raw(__hfma2(bits((v & 0x00f000f0u) | 0x64006400u), sixteenth, high));
+        a[0] = raw(__hadd2(bits(masked(w, 0x000f000fu, 0x64006400u)), low));
+        a[1] = raw(__hfma2(bits(masked(w, 0x00f000f0u, 0x64006400u)), sixteenth, high));
+        a[2] = raw(__hadd2(bits(masked(v, 0x000f000fu, 0x64006400u)), low));
+        a[3] = raw(__hfma2(bits(masked(v, 0x00f000f0u, 0x64006400u)), sixteenth, high));
     }
     static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
@@ -227,7 +233,7 @@ template <> struct Q4Operand<__nv_bfloat16> {
         const __nv_bfloat162 low = __floats2bfloat162_rn(-136.0f, -136.0f);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t x = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+            const uint32_t x = masked(w >> (4 * i), 0x000f000fu, 0x43004300u);
             const __nv_bfloat162 v = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&x), low);
             a[i] = *reinterpret_cast<const uint32_t*>(&v);
         }
