@@ -474,9 +474,9 @@ int ebs_grouped_backward(const void *dy_dev, const void *x_dev, const void *w_de
  *
  * packed: ebs_q4_packed_bytes(desc) bytes, laid out for one kernel (its layout is not part of the interface).  ldw: elements
  * between the rows of W (0: dense); experts follow one another, n rows each.  desc of the product: m, act, ldx, ldy, ldr (n, k and dtype as in
- * the weights' descriptor).  Rows of x that start anywhere (ldx not a multiple of 16 bytes) are copied first: workspace_dev,
- * ebs_linear_q4_workspace_bytes(desc, q4) bytes (0: may be NULL), used as in ebs_linear_forward.  y may be the residual itself; no output may
- * overlap another tensor otherwise.
+ * the weights' descriptor).  Rows of x that start anywhere (ldx not a multiple of 16 bytes) are copied first, EBS_F32 rows brought into planes
+ * where the weights are many: workspace_dev, ebs_linear_q4_workspace_bytes(desc, q4) bytes (0: may be NULL), used as in ebs_linear_forward.
+ * y may be the residual itself; no output may overlap another tensor otherwise.
  */
 typedef struct ebs_q4_desc {
     int experts, n, k; /* weights [experts][n][k], each >= 1 */

@@ -249,12 +249,29 @@ template <> struct Q4Operand<__nv_bfloat16> {
 };
 template <> struct Q4Operand<float> : Q4Operand<__nv_bfloat16> {};
 
-// A lane's activations of one row for 64 inputs: PL planes of two words for each of the four MMAs.
-template <typename T> struct Q4Acts {
+// fp32 x = high + middle + low, each what the one before left cut to bf16 (the upper half of its word): exact.  An infinity or a NaN is all in the first.  The low bits first.
+__device__ __forceinline__ void q4_planes(float x, uint32_t (&t)[3]) {
+    uint32_t bits = __float_as_uint(x);
+    const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
+    if (!finite && (bits & 0x007fffffu) != 0u) bits |= 0x00400000u;
+    const float r = finite ? x - __uint_as_float(bits & 0xffff0000u) : 0.0f;
+    t[2] = bits;
+    t[1] = __float_as_uint(r);
+    t[0] = __float_as_uint(r - __uint_as_float(t[1] & 0xffff0000u));
+}
+__device__ __forceinline__ void q4_planes(float x, float y, uint32_t (&b)[3]) {
+    uint32_t s[3], t[3];
+    q4_planes(x, s);
+    q4_planes(y, t);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) b[p] = __byte_perm(s[p], t[p], 0x7632);
+}
+// A lane's activations of one row for 64 inputs: PL planes of two words for each of the four MMAs.  x: the lane's first element; left: elements of the row from there on.
+template <typename T, bool PREPARED> struct Q4Acts {
+    using X = T;
     static constexpr int PL = 1;
     uint32_t b[1][8];
-    // x: the lane's first element; left: elements of the row from there on
-    __device__ __forceinline__ void load(const T* x, int left, bool whole) {
+    __device__ __forceinline__ void load(const T* x, long long, int left, bool whole) {
         if (whole) {
             const uint4 u = *reinterpret_cast<const uint4*>(x), v = *reinterpret_cast<const uint4*>(x + 32);
             b[0][0] = u.x; b[0][1] = u.y; b[0][2] = u.z; b[0][3] = u.w;
@@ -269,48 +286,72 @@ template <typename T> struct Q4Acts {
         }
     }
 };
-template <> struct Q4Acts<float> {
+template <> struct Q4Acts<float, false> {
+    using X = float;
     static constexpr int PL = 3;
-    uint32_t b[3][8];                                               // the low bits first
-    // x = high + middle + low, each what the one before left cut to bf16: exact.  An infinity or a NaN is all in the first.
-    static __device__ __forceinline__ void planes(float x, uint32_t (&t)[3]) {
-        uint32_t bits = __float_as_uint(x);
-        const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
-        if (!finite && (bits & 0x007fffffu) != 0u) bits |= 0x00400000u;
-        const float r = finite ? x - __uint_as_float(bits & 0xffff0000u) : 0.0f;
-        t[2] = bits;
-        t[1] = __float_as_uint(r);
-        t[0] = __float_as_uint(r - __uint_as_float(t[1] & 0xffff0000u));
-    }
-    __device__ __forceinline__ void pair(int i, float x, float y) {
-        uint32_t s[3], t[3];
-        planes(x, s);
-        planes(y, t);
-#pragma unroll
-        for (int p = 0; p < 3; ++p) b[p][i] = __byte_perm(s[p], t[p], 0x7632);       // the upper halves of both
-    }
-    __device__ __forceinline__ void load(const float* x, int left, bool whole) {
+    uint32_t b[3][8];
+    __device__ __forceinline__ void load(const float* x, long long, int left, bool whole) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int at = (i >> 1) * 32 + (i & 1) * 4;
             float4 v;
             if (whole) v = *reinterpret_cast<const float4*>(x + at);
             else v = make_float4(at < left ? x[at] : 0.0f, at + 1 < left ? x[at + 1] : 0.0f, at + 2 < left ? x[at + 2] : 0.0f, at + 3 < left ? x[at + 3] : 0.0f);
-            pair(2 * i, v.x, v.y);
-            pair(2 * i + 1, v.z, v.w);
+            uint32_t t[3], u[3];
+            q4_planes(v.x, v.y, t);
+            q4_planes(v.z, v.w, u);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) { b[p][2 * i] = t[p]; b[p][2 * i + 1] = u[p]; }
         }
     }
 };
+// (planes of whole tiles, q4_planes_kernel)
+template <> struct Q4Acts<float, true> {
+    using X = uint16_t;
+    static constexpr int PL = 3;
+    uint32_t b[3][8];
+    __device__ __forceinline__ void load(const uint16_t* x, long long plane, int, bool) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            const uint4 u = *reinterpret_cast<const uint4*>(x + p * plane), v = *reinterpret_cast<const uint4*>(x + p * plane + 32);
+            b[p][0] = u.x; b[p][1] = u.y; b[p][2] = u.z; b[p][3] = u.w;
+            b[p][4] = v.x; b[p][5] = v.y; b[p][6] = v.z; b[p][7] = v.w;
+        }
+    }
+};
+// Planes of fp32 rows, each padded with zeros to whole tiles of 64: [plane][row][ldd].  A thread takes eight elements.
+__global__ void __launch_bounds__(256) q4_planes_kernel(const float* __restrict__ x, long long ldx, int k, int ldd, long long packs, uint16_t* __restrict__ to) {
+    let_next_kernel_start();
+    wait_for_previous_kernel();
+    const int across = ldd / 8;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < packs; i += gridDim.x * 256LL) {
+        const long long row = i / across;
+        const int c = (int)(i - row * across) * 8;
+        float v[8];
+        load8<float>(x + row * ldx + c, k - c, (ldx & 3) == 0, v);
+        uint4 out[3];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            uint32_t t[3];
+            q4_planes(v[2 * h], v[2 * h + 1], t);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) reinterpret_cast<uint32_t*>(&out[p])[h] = t[p];
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(to + (p * (packs / across) + row) * ldd + c) = out[p];
+    }
+}
+
+constexpr int q4_mt(int nt) { return nt >= 4 ? 2 : 1; }             // tiles of 16 outputs a block takes: with many rows their activations serve two
 
 struct Q4Args {
     const void *x, *scales, *bias, *residual;
     const uint4* codes;
     const int* offsets;
     void* y;
-    long long ldx, ldr, ldy;
+    long long ldx, ldr, ldy, plane;        // plane: elements between the planes of prepared activations
     int m, n, k, experts, tiles, kbs, groups, slots, act;
 };
-constexpr int Q4_WARPS = 8;
 
 // The `slot`-th piece of up to `most` rows of an expert, in the order of the experts: the expert, its rows.  Offsets that are out of order or
 // out of range are taken as the nearest ones that are not.
@@ -355,15 +396,17 @@ __device__ __forceinline__ float2 scale_pair(const float* p) { return *reinterpr
 __device__ __forceinline__ float2 scale_pair(const __half* p) { return __half22float2(*reinterpret_cast<const __half2*>(p)); }
 __device__ __forceinline__ float2 scale_pair(const __nv_bfloat16* p) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p)); }
 
-// A block: 16 * MT outputs of up to 8 * NT rows; its warps share the reduction and add up in shared memory, in their order.  Columns of the MMA beyond the last row
+// A block: 16 * MT outputs of up to 8 * NT rows; its WARPS warps share the reduction and add up in shared memory, in their order.  Columns of the MMA beyond the last row
 // take its activations again and are not written.
-template <typename T, int NT, int MT, int G>
-__global__ void __launch_bounds__(Q4_WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 : NT <= 2 ? 2 : 1) q4_kernel(const __grid_constant__ Q4Args g) {
+template <typename T, int NT, int WARPS> constexpr int q4_blocks() { return NT == 1 && sizeof(T) == 2 ? 32 / WARPS : NT >= 4 ? 8 / WARPS : 16 / WARPS; }      // of an SM
+template <typename T, bool PREPARED, int NT, int MT, int G, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, (q4_blocks<T, NT, WARPS>())) q4_kernel(const __grid_constant__ Q4Args g) {
     extern __shared__ float sums[];                                 // [warp][row][16 * MT outputs]
     constexpr int COLS = Q4_ROWS * MT, ROWS = 8 * NT, D = MT == 1 ? 4 : 2;
     // tiles whose sum meets a scale: a group's two where that leaves the registers for it
     constexpr int UNIT = G == 128 && NT <= 2 ? 2 : 1;
-    using Acts = Q4Acts<T>;
+    using Acts = Q4Acts<T, PREPARED>;
+    using X = typename Acts::X;
     using Operand = Q4Operand<T>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
     let_next_kernel_start();
@@ -371,10 +414,10 @@ __global__ void __launch_bounds__(Q4_WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 :
     const int slot = (int)(blockIdx.x % (unsigned)g.slots), tile0 = (int)(blockIdx.x / (unsigned)g.slots) * MT;
     int expert, row0, rows;
     if (!q4_slot(g, slot, ROWS, expert, row0, rows)) return;
-    const int units = (g.kbs + UNIT - 1) / UNIT, kb0 = (int)((long long)units * warp / Q4_WARPS) * UNIT, kb1 = min((int)((long long)units * (warp + 1) / Q4_WARPS) * UNIT, g.kbs);
-    const T* x[NT];
+    const int units = (g.kbs + UNIT - 1) / UNIT, kb0 = (int)((long long)units * warp / WARPS) * UNIT, kb1 = min((int)((long long)units * (warp + 1) / WARPS) * UNIT, g.kbs);
+    const X* x[NT];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) x[i] = static_cast<const T*>(g.x) + (long long)(row0 + min(gid + 8 * i, rows - 1)) * g.ldx + tig * 8 + (long long)kb0 * Q4_K;
+    for (int i = 0; i < NT; ++i) x[i] = static_cast<const X*>(g.x) + (long long)(row0 + min(gid + 8 * i, rows - 1)) * g.ldx + tig * 8 + (long long)kb0 * Q4_K;
     const uint4* codes[MT];
     const T* scales[MT];
 #pragma unroll
@@ -391,39 +434,67 @@ __global__ void __launch_bounds__(Q4_WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 :
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[t][i][e] = 0.0f;
 
-    // one tile of 64 inputs; begin: its sum begins here, end: it meets its scale
-    auto multiply = [&](const uint4 (&w)[MT], int kb, const Acts (&b)[NT], bool begin, bool end) {
+    // one tile of 64 inputs, `ahead` of the pointers; begin: its sum begins here, end: it meets its scale
+    auto multiply = [&](const uint4 (&w)[MT], int kb, int ahead, bool whole, bool begin, bool end) {
+        constexpr int Q = G == 32 ? 2 : 1, R = 4 / Q;
+        auto load = [&](Acts& b, int i) { b.load(x[i] + ahead * Q4_K, g.plane, g.k - kb * Q4_K - tig * 8, whole); };
+        auto scale_of = [&](int t, int q) { return scale_pair(scales[t] + (G == 32 ? min(kb * 2 + q, g.groups - 1) : G == 64 ? kb : kb >> 1) * Q4_ROWS); };
+        auto sum = [&](const uint32_t (&a)[4][4], const Acts& b, const float2& s, int t, int i, int q) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            const uint32_t word[4] = {w[t].x, w[t].y, w[t].z, w[t].w};
-            uint32_t a[4][4];
+            for (int p = 0; p < Acts::PL; ++p)
 #pragma unroll
-            for (int s = 0; s < 4; ++s) Operand::make(word[s], a[s]);
-#pragma unroll
-            for (int q = 0; q < (G == 32 ? 2 : 1); ++q) {
-                const int group = G == 32 ? min(kb * 2 + q, g.groups - 1) : G == 64 ? kb : kb >> 1;
-                float2 s = make_float2(0.0f, 0.0f);
-                if (end) s = scale_pair(scales[t] + group * Q4_ROWS);
-#pragma unroll
-                for (int i = 0; i < NT; ++i) {
-#pragma unroll
-                    for (int p = 0; p < Acts::PL; ++p)
-#pragma unroll
-                        for (int r = G == 32 ? 2 * q : 0; r < (G == 32 ? 2 * q + 2 : 4); ++r) {
-                            if (p == 0 && r == (G == 32 ? 2 * q : 0) && begin) Operand::mma_first(c[t][i], a[r], b[i].b[p][2 * r], b[i].b[p][2 * r + 1]);
-                            else Operand::mma(c[t][i], a[r], b[i].b[p][2 * r], b[i].b[p][2 * r + 1]);
-                        }
-                    if (end) {
-                        acc[t][i][0] = fmaf(c[t][i][0], s.x, acc[t][i][0]);
-                        acc[t][i][1] = fmaf(c[t][i][1], s.x, acc[t][i][1]);
-                        acc[t][i][2] = fmaf(c[t][i][2], s.y, acc[t][i][2]);
-                        acc[t][i][3] = fmaf(c[t][i][3], s.y, acc[t][i][3]);
-                    }
+                for (int r = R * q; r < R * q + R; ++r) {
+                    if (p == 0 && r == R * q && begin) Operand::mma_first(c[t][i], a[r], b.b[p][2 * r], b.b[p][2 * r + 1]);
+                    else Operand::mma(c[t][i], a[r], b.b[p][2 * r], b.b[p][2 * r + 1]);
                 }
+            if (end) {
+                acc[t][i][0] = fmaf(c[t][i][0], s.x, acc[t][i][0]);
+                acc[t][i][1] = fmaf(c[t][i][1], s.x, acc[t][i][1]);
+                acc[t][i][2] = fmaf(c[t][i][2], s.y, acc[t][i][2]);
+                acc[t][i][3] = fmaf(c[t][i][3], s.y, acc[t][i][3]);
+            }
+        };
+        if constexpr (NT <= 2) {                                    // (activations first: 8192 -> 28672 27 us, operands first 32)
+            Acts b[NT];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) load(b[i], i);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const uint32_t word[4] = {w[t].x, w[t].y, w[t].z, w[t].w};
+                uint32_t a[4][4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) Operand::make(word[r], a[r]);
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    float2 s = make_float2(0.0f, 0.0f);
+                    if (end) s = scale_of(t, q);
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) sum(a, b[i], s, t, i, q);
+                }
+            }
+        } else {                                                    // (operands first: they stay, a row's activations come and go)
+            uint32_t a[MT][4][4];
+            float2 s[MT][Q];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const uint32_t word[4] = {w[t].x, w[t].y, w[t].z, w[t].w};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) Operand::make(word[r], a[t][r]);
+#pragma unroll
+                for (int q = 0; q < Q; ++q) s[t][q] = end ? scale_of(t, q) : make_float2(0.0f, 0.0f);
+            }
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                Acts b;
+                load(b, i);
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) sum(a[t], b, s[t][q], t, i, q);
             }
         }
     };
-    const int whole = min(kb1, g.k / Q4_K);                         // tiles that are all there
+    const int whole = PREPARED ? kb1 : min(kb1, g.k / Q4_K);        // tiles that are all there
     uint4 w[D][MT];                                                 // D tiles under way: a place is loaded anew when it is used
 #pragma unroll
     for (int d = 0; d < D; ++d)
@@ -435,10 +506,7 @@ __global__ void __launch_bounds__(Q4_WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 :
         if (kb + D <= whole) {
 #pragma unroll
             for (int d = 0; d < D; ++d) {
-                Acts b[NT];
-#pragma unroll
-                for (int i = 0; i < NT; ++i) b[i].load(x[i] + d * Q4_K, Q4_K, true);
-                multiply(w[d], kb + d, b, d % UNIT == 0, d % UNIT == UNIT - 1);
+                multiply(w[d], kb + d, d, true, d % UNIT == 0, d % UNIT == UNIT - 1);
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
                     if (kb + D + d < kb1) w[d][t] = load_stream(codes[t] + (D + d) * 32);
@@ -447,12 +515,9 @@ __global__ void __launch_bounds__(Q4_WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 :
 #pragma unroll
             for (int d = 0; d < D; ++d) {
                 if (kb + d >= kb1) break;
-                Acts b[NT];
-#pragma unroll
-                for (int i = 0; i < NT; ++i) b[i].load(x[i] + d * Q4_K, g.k - (kb + d) * Q4_K - tig * 8, kb + d < whole);
-                multiply(w[d], kb + d, b, d % UNIT == 0, d % UNIT == UNIT - 1 || kb + d == kb1 - 1);
+                multiply(w[d], kb + d, d, kb + d < whole, d % UNIT == 0, d % UNIT == UNIT - 1 || kb + d == kb1 - 1);
             }
-            break;                                                  // (the warp's last tiles)
+            break;                                                  // (the warp's last tiles: no more than D, since at most the last one is not whole)
         }
 #pragma unroll
         for (int t = 0; t < MT; ++t) codes[t] += D * 32;
@@ -468,12 +533,12 @@ __global__ void __launch_bounds__(Q4_WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 :
             for (int e = 0; e < 4; ++e) mine[(8 * i + 2 * tig + (e & 1)) * COLS + t * Q4_ROWS + gid + 8 * (e >> 1)] = acc[t][i][e];
     __syncthreads();
     const T* bias = g.bias ? static_cast<const T*>(g.bias) + (long long)expert * g.n : nullptr;
-    for (int i = threadIdx.x; i < rows * COLS; i += Q4_WARPS * 32) {
+    for (int i = threadIdx.x; i < rows * COLS; i += WARPS * 32) {
         const int r = i / COLS, col = tile0 * Q4_ROWS + i % COLS;
         if (col >= g.n) continue;
         float v = 0.0f;
 #pragma unroll
-        for (int q = 0; q < Q4_WARPS; ++q) v += sums[q * ROWS * COLS + i];
+        for (int q = 0; q < WARPS; ++q) v += sums[q * ROWS * COLS + i];
         if (bias) v += to_f32(bias[col]);
         if (g.act) v = activation<sizeof(T) == 2>(v, g.act);
         if (g.residual) v += to_f32(static_cast<const T*>(g.residual)[(long long)(row0 + r) * g.ldr + col]);
@@ -481,10 +546,33 @@ __global__ void __launch_bounds__(Q4_WARPS * 32, NT == 1 && sizeof(T) == 2 ? 4 :
     }
 }
 
-template <typename T, int NT, int MT, int G>
-static int launch_q4(const Q4Args& g, long long blocks, cudaStream_t st) {
-    constexpr int SMEM = Q4_WARPS * 8 * NT * Q4_ROWS * MT * 4;
-    auto kern = q4_kernel<T, NT, MT, G>;
+// How a product is run, from its sizes alone.
+struct Q4Route {
+    int nt;                                // rows that a block takes at a time, in eights: from those an expert has in the mean, twice that so that most experts' weights are read once
+    bool prepared, copied, wide;           // x goes through the workspace as planes (fp32) or as it is, since its rows start anywhere; wide: 16 warps share a tile's reduction
+    long long pieces, blocks;              // pieces of rows: at most one for each expert that has rows, and one more for each full piece
+    size_t workspace;
+};
+static Q4Route q4_route(const ebs_linear_desc& d, const ebs_q4_desc& q) {
+    Q4Route r = {};
+    const long long rows = q.experts == 1 ? d.m : 2LL * (((long long)d.m + q.experts - 1) / q.experts);
+    const int most = d.dtype == EBS_F32 ? 4 : 8, tiles = (d.n + Q4_ROWS - 1) / Q4_ROWS, kbs = (d.k + Q4_K - 1) / Q4_K;
+    r.nt = 1;
+    while (r.nt < most && 8LL * r.nt < rows) r.nt *= 2;
+    r.pieces = q.experts > 1 ? (long long)(q.experts < d.m ? q.experts : d.m) + d.m / (8 * r.nt) : (d.m + 8LL * r.nt - 1) / (8 * r.nt);
+    r.blocks = r.pieces * ((tiles + q4_mt(r.nt) - 1) / q4_mt(r.nt));
+    // (4096 -> 14336 of four rows, 57344 tiles: 30.4 us split where they are used, 19.0 with the launch that prepares them, which costs 2)
+    r.prepared = d.dtype == EBS_F32 && r.blocks * kbs >= 8192;
+    r.copied = !r.prepared && d.m > 1 && d.ldx * (long long)element_size(d.dtype) % 16 != 0;
+// (14336 -> 4096: 15.6 us with 8 warps a tile, of which two blocks an SM have work, 9.9 with 16)
+    r.wide = r.nt == 1 && r.blocks < 148 * 3 && kbs >= 32;
+    r.workspace = r.prepared ? round256((size_t)d.m * kbs * Q4_K * 3 * 2) : r.copied ? round256((size_t)d.m * round8(d.k) * element_size(d.dtype)) : 0;
+    return r;
+}
+template <typename T, bool PREPARED, int NT, int G, int WARPS>
+static int launch_q4(const Q4Args& g, const Q4Route& r, cudaStream_t st) {
+    constexpr int SMEM = WARPS * 8 * NT * Q4_ROWS * q4_mt(NT) * 4;
+    auto kern = q4_kernel<T, PREPARED, NT, q4_mt(NT), G, WARPS>;
     if (SMEM > 48 * 1024) {
         static bool attr_set[64] = {};
         int dev = 0;
@@ -494,33 +582,22 @@ static int launch_q4(const Q4Args& g, long long blocks, cudaStream_t st) {
             if (dev >= 0 && dev < 64) attr_set[dev] = true;
         }
     }
-    return launch_chained(kern, dim3((unsigned)blocks), Q4_WARPS * 32, SMEM, st, 1, g);
+    return launch_chained(kern, dim3((unsigned)r.blocks), WARPS * 32, SMEM, st, 1, g);
 }
-// Rows that a block takes at a time, in eights: from the rows an expert has in the mean, twice that so that most experts' weights are read once.
-static int q4_row_tiles(int m, int experts, int dtype) {
-    const long long rows = experts == 1 ? m : 2LL * ((m + experts - 1) / experts);
-    const int most = dtype == EBS_F32 ? 4 : 8;
-    int nt = 1;
-    while (nt < most && 8LL * nt < rows) nt *= 2;
-    return nt;
+template <typename T, bool PREPARED, int NT, int WARPS = 8>
+static int launch_q4_group(const Q4Args& g, const Q4Route& r, int group, cudaStream_t st) {
+    return group == 32 ? launch_q4<T, PREPARED, NT, 32, WARPS>(g, r, st) : group == 64 ? launch_q4<T, PREPARED, NT, 64, WARPS>(g, r, st) : launch_q4<T, PREPARED, NT, 128, WARPS>(g, r, st);
 }
-template <typename T, int NT, int MT>
-static int launch_q4_group(Q4Args& g, int group, cudaStream_t st) {
-    // pieces of rows: at most one for each expert that has rows, and one more for each full piece
-    const long long pieces = g.offsets ? (long long)(g.experts < g.m ? g.experts : g.m) + g.m / (8 * NT) : (g.m + 8LL * NT - 1) / (8 * NT);
-    const long long blocks = pieces * ((g.tiles + MT - 1) / MT);
-    if (blocks > 0x7fffffffLL) return EBS_ERR_OVERFLOW;
-    g.slots = (int)pieces;
-    return group == 32 ? launch_q4<T, NT, MT, 32>(g, blocks, st) : group == 64 ? launch_q4<T, NT, MT, 64>(g, blocks, st) : launch_q4<T, NT, MT, 128>(g, blocks, st);
-}
-template <typename T>
-static int launch_q4_rows(Q4Args& g, int group, int dtype, cudaStream_t st) {
-    switch (q4_row_tiles(g.m, g.offsets ? g.experts : 1, dtype)) {
-        case 1: return launch_q4_group<T, 1, 1>(g, group, st);
-        case 2: return launch_q4_group<T, 2, 1>(g, group, st);
-        case 4: return launch_q4_group<T, 4, 2>(g, group, st);
+template <typename T, bool PREPARED>
+static int launch_q4_rows(Q4Args& g, const Q4Route& r, int group, cudaStream_t st) {
+    if (r.blocks > 0x7fffffffLL) return EBS_ERR_OVERFLOW;
+    g.slots = (int)r.pieces;
+    switch (r.nt) {
+        case 1: return r.wide ? launch_q4_group<T, PREPARED, 1, 16>(g, r, group, st) : launch_q4_group<T, PREPARED, 1>(g, r, group, st);
+        case 2: return launch_q4_group<T, PREPARED, 2>(g, r, group, st);
+        case 4: return launch_q4_group<T, PREPARED, 4>(g, r, group, st);
         default:
-            if constexpr (sizeof(T) == 2) return launch_q4_group<T, 8, 2>(g, group, st);
+            if constexpr (sizeof(T) == 2) return launch_q4_group<T, PREPARED, 8>(g, r, group, st);
             else return EBS_ERR_UNSUPPORTED;
     }
 }
@@ -574,15 +651,12 @@ static int check_weights(const ebs_q4_desc* d, const void* w, int w_dtype, long 
     return check_tensors(t, 2, size, nullptr, nullptr);
 }
 
-// The two descriptors of a product together, strides filled in; rows_copied: x goes through the workspace, since its rows start anywhere.
-static int check_product(const ebs_linear_desc* desc, const ebs_q4_desc* q, ebs_linear_desc* d, bool* rows_copied) {
+// The two descriptors of a product together, strides filled in.
+static int check_product(const ebs_linear_desc* desc, const ebs_q4_desc* q, ebs_linear_desc* d) {
     int rc = check_q4(q);
     if (rc || (rc = complete_linear(desc, d))) return rc;
-    if (d->n != q->n || d->k != q->k || d->dtype != q->dtype) return EBS_ERR_INVALID_ARG;
-    *rows_copied = d->m > 1 && d->ldx * (long long)element_size(d->dtype) % 16 != 0;
-    return EBS_OK;
+    return d->n != q->n || d->k != q->k || d->dtype != q->dtype ? EBS_ERR_INVALID_ARG : EBS_OK;
 }
-static long long copied_stride(const ebs_linear_desc& d) { return round8(d.k); }
 
 }  // namespace ebs
 
@@ -616,16 +690,13 @@ int ebs_unpack_weights_q4(const void* packed_dev, const ebs_q4_desc* desc, void*
 
 size_t ebs_linear_q4_workspace_bytes(const ebs_linear_desc* desc, const ebs_q4_desc* q4) {
     ebs_linear_desc d;
-    bool copied;
-    if (check_product(desc, q4, &d, &copied)) return 0;
-    return copied ? round256((size_t)d.m * copied_stride(d) * element_size(d.dtype)) : 0;
+    return check_product(desc, q4, &d) ? 0 : q4_route(d, *q4).workspace;
 }
 
 int ebs_linear_q4_forward(const void* x_dev, const void* packed_dev, const void* bias_dev, const void* residual_dev, const int* offsets_dev, const ebs_linear_desc* desc,
                           const ebs_q4_desc* q4, void* y_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
     ebs_linear_desc d;
-    bool copied;
-    int rc = check_product(desc, q4, &d, &copied);
+    int rc = check_product(desc, q4, &d);
     if (rc) return rc;
     if (!packed_dev || (d.m > 0 && (!x_dev || !y_dev)) || (!offsets_dev && q4->experts != 1) || ((uintptr_t)offsets_dev & 3u)) return EBS_ERR_INVALID_ARG;
     const size_t size = element_size(d.dtype), need = ebs_linear_q4_workspace_bytes(desc, q4);
@@ -642,19 +713,28 @@ int ebs_linear_q4_forward(const void* x_dev, const void* packed_dev, const void*
     }
     if (d.m == 0) return EBS_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    Q4Args g{x_dev, static_cast<const char*>(packed_dev) + l.codes, bias_dev, residual_dev, static_cast<const uint4*>(packed_dev), offsets_dev, y_dev, d.ldx, d.ldr, d.ldy,
+    const Q4Route r = q4_route(d, *q4);
+    Q4Args g{x_dev, static_cast<const char*>(packed_dev) + l.codes, bias_dev, residual_dev, static_cast<const uint4*>(packed_dev), offsets_dev, y_dev, d.ldx, d.ldr, d.ldy, 0,
              d.m, d.n, d.k, q4->experts, l.tiles, l.kbs, l.groups, 0, d.act};
-    if (copied) {                                                  // (fp32 rows as twice as many 16-bit elements)
+    if (r.prepared || r.copied) {
+        g.x = workspace_dev;
+        g.ldx = r.prepared ? (long long)l.kbs * Q4_K : round8(d.k);
+    }
+    if (r.prepared) {
+        const long long packs = d.m * (g.ldx / 8), blocks = (packs + 255) / 256;
+        g.plane = d.m * g.ldx;
+        if ((rc = launch_chained(q4_planes_kernel, dim3((unsigned)(blocks < 1184 ? blocks : 1184)), 256, 0, st, 1, static_cast<const float*>(x_dev), d.ldx, d.k, (int)g.ldx, packs,
+                                 static_cast<uint16_t*>(workspace_dev))))
+            return rc;
+    } else if (r.copied) {                                         // (fp32 rows as twice as many 16-bit elements)
         const int halves = (int)(size / 2);
         CopyJobs jobs = {};
-        add_copy_rows(&jobs, x_dev, workspace_dev, d.m, d.k * halves, d.ldx * halves, copied_stride(d) * halves);
+        add_copy_rows(&jobs, x_dev, workspace_dev, d.m, d.k * halves, d.ldx * halves, g.ldx * halves);
         if ((rc = launch_copies(jobs, st))) return rc;
-        g.x = workspace_dev;
-        g.ldx = copied_stride(d);
     }
-    if (d.dtype == EBS_F32) return launch_q4_rows<float>(g, q4->group, d.dtype, st);
-    if (d.dtype == EBS_F16) return launch_q4_rows<__half>(g, q4->group, d.dtype, st);
-    return launch_q4_rows<__nv_bfloat16>(g, q4->group, d.dtype, st);
+    if (d.dtype == EBS_F32) return r.prepared ? launch_q4_rows<float, true>(g, r, q4->group, st) : launch_q4_rows<float, false>(g, r, q4->group, st);
+    if (d.dtype == EBS_F16) return launch_q4_rows<__half, false>(g, r, q4->group, st);
+    return launch_q4_rows<__nv_bfloat16, false>(g, r, q4->group, st);
 }
 
 }  // extern "C"
