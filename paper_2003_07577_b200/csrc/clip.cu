@@ -1,8 +1,8 @@
 // Norm of all gradients of a network and their clipping.  See include/ebs.h.
 //
 // Bound by the bytes: one pass reads every gradient for the sum of squares, one reads it again and writes it.  The work list ("plan") cuts all
-// tensors into chunks of up to CLIP_CHUNK elements, a record each, so that a block learns from one 48-byte load what to do next, however many
-// tensors there are and whatever their sizes.  The second pass takes the chunks from the last to the first: what the first pass read last is still in
+// tensors into chunks, a record each, so that a block learns from one 48-byte load what to do next, however many tensors there are and whatever their
+// sizes; the next record is on its way while a chunk is read.  The second pass takes the chunks from the last to the first: what the first pass read last is still in
 // the second-level cache.
 //
 // The sum is taken in 64 bits.  A pack of 16 bytes is squared and added in fp32 first (relative error 2^-22 of the pack at most), unless that sum
@@ -16,9 +16,11 @@
 
 namespace ebs {
 
-constexpr int CLIP_CHUNK = 8192;            // elements
-constexpr int CLIP_BLOCKS = 148 * 8;        // at most: a wave of blocks of 256 threads
+constexpr int CLIP_BLOCKS = 148 * 4;        // at most: a wave of blocks of 256 threads
 constexpr int CLIP_THREADS = 256;
+constexpr int CLIP_UNROLL = 8;              // packs of a thread under way: 32 KB a block (four, and records loaded when they are needed: 1.07 GB read at 3.4 TB/s)
+// Bytes of a chunk of one row: as many as the block has under way; a network of a few MB is cut finer, so that every SM has some.
+constexpr long long CLIP_CHUNK = CLIP_THREADS * 16 * CLIP_UNROLL, CLIP_CHUNK_SMALL = CLIP_THREADS * 16, CLIP_SMALL = 8 << 20;
 
 // rows = 1: the block's threads share the row; more: a warp takes a row.
 struct alignas(16) ClipChunk {
@@ -31,27 +33,46 @@ static_assert(sizeof(ClipChunk) == EBS_CLIP_CHUNK_BYTES, "chunk record");
 
 __device__ __forceinline__ ClipChunk load_chunk(const ClipChunk* p) {
     const uint4* q = reinterpret_cast<const uint4*>(p);
-    union { uint4 u[3]; ClipChunk c; } v;
-    v.u[0] = q[0]; v.u[1] = q[1]; v.u[2] = q[2];
-    return v.c;
+    const uint4 a = q[0], b = q[1], d = q[2];
+    auto wide = [](uint32_t low, uint32_t high) { return (long long)((unsigned long long)high << 32 | low); };
+    ClipChunk c;
+    c.in = reinterpret_cast<const void*>(wide(a.x, a.y));
+    c.out = reinterpret_cast<void*>(wide(a.z, a.w));
+    c.ld_in = wide(b.x, b.y);
+    c.ld_out = wide(b.z, b.w);
+    c.rows = (int)d.x;
+    c.cols = (int)d.y;
+    c.dtype = (int)d.z;
+    return c;
 }
 
 // The sum of the squares of one pack.
 template <typename T>
-__device__ __forceinline__ void add_squares(const uint4& u, double& sum) {
+__device__ __noinline__ double squares_of(const uint4 u) {
+    double sum = 0.0;
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = __uint_as_float(w[i]), b = 0.0f;
+        if (sizeof(T) == 2) {
+            a = to_f32(reinterpret_cast<const T*>(&w[i])[0]);
+            b = to_f32(reinterpret_cast<const T*>(&w[i])[1]);
+        }
+        sum += (double)a * (double)a + (double)b * (double)b;
+    }
+    return sum;
+}
+// In fp32; false: it is left out, for squares_of (below 1e-28 a square of the pack may be lost that matters, above 1e37 one may be infinite that is not).
+template <typename T>
+__device__ __forceinline__ bool add_squares(const uint4& u, double& sum) {
     constexpr int N = Pack<T>::N;
     float v[N], s = 0.0f;
     unpack<T>(u, v);
 #pragma unroll
     for (int i = 0; i < N; ++i) s = fmaf(v[i], v[i], s);
-    // (below 1e-28 a square of the pack may be lost that matters, above 1e37 one may be infinite that is not)
-    if (s >= 1e-28f && s <= 1e37f) sum += (double)s;
-    else if (((u.x | u.y | u.z | u.w) & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) != 0u)
-#pragma unroll 1
-        for (int i = 0; i < N; ++i) {
-            const double d = (double)to_f32(reinterpret_cast<const T*>(&u)[i]);
-            sum += d * d;
-        }
+    const bool fits = s >= 1e-28f && s <= 1e37f;
+    sum += (double)(fits ? s : 0.0f);
+    return fits || ((u.x | u.y | u.z | u.w) & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) == 0u;
 }
 template <typename T>
 __device__ __forceinline__ void add_square(T x, double& sum) {
@@ -64,24 +85,29 @@ __device__ __forceinline__ int head_of(const T* p, int cols) {
     const int h = (int)((16u - ((unsigned)(uintptr_t)p & 15u)) & 15u) / (int)sizeof(T);
     return h < cols ? h : cols;
 }
-constexpr int CLIP_UNROLL = 4;              // packs of a thread under way
-
 template <typename T>
 __device__ __forceinline__ void row_squares(const T* p, int cols, int t, int step, double& sum) {
     constexpr int N = Pack<T>::N;
     const int head = head_of(p, cols), packs = (cols - head) / N, tail = head + packs * N;
+    // (a head and a tail have fewer elements than a warp has lanes)
+    const T first = t < head ? p[t] : from_f32<T>(0.0f), last = tail + t < cols ? p[tail + t] : from_f32<T>(0.0f);
     const uint4* q = reinterpret_cast<const uint4*>(p + head);
-    int i = t;
-    for (; i + (CLIP_UNROLL - 1) * step < packs; i += CLIP_UNROLL * step) {
+    for (int i = t; i < packs; i += CLIP_UNROLL * step) {
         uint4 u[CLIP_UNROLL];
 #pragma unroll
-        for (int j = 0; j < CLIP_UNROLL; ++j) u[j] = q[i + j * step];
+        for (int j = 0; j < CLIP_UNROLL; ++j) u[j] = i + j * step < packs ? q[i + j * step] : make_uint4(0u, 0u, 0u, 0u);
+        unsigned left_out = 0u;
 #pragma unroll
-        for (int j = 0; j < CLIP_UNROLL; ++j) add_squares<T>(u[j], sum);
+        for (int j = 0; j < CLIP_UNROLL; ++j) left_out |= (add_squares<T>(u[j], sum) ? 0u : 1u) << j;
+        if (left_out)                                             // (rare: read again, so that nothing is kept for it)
+#pragma unroll 1
+            for (int j = 0; j < CLIP_UNROLL; ++j)
+                if (left_out >> j & 1u) sum += squares_of<T>(q[i + j * step]);
     }
-    for (; i < packs; i += step) add_squares<T>(q[i], sum);
-    if (t < head) add_square(p[t], sum);
-    if (tail + t < cols) add_square(p[tail + t], sum);        // (a head and a tail have fewer elements than a warp has lanes)
+    if (t < N) {
+        add_square(first, sum);
+        add_square(last, sum);
+    }
 }
 template <typename T>
 __device__ __forceinline__ void chunk_squares(const ClipChunk& c, double& sum) {
@@ -103,12 +129,14 @@ __device__ __forceinline__ double block_sum(double v) {
     return v;
 }
 
-__global__ void __launch_bounds__(CLIP_THREADS) clip_norm_kernel(const ClipChunk* __restrict__ chunks, long long count, double* __restrict__ partial) {
+__global__ void __launch_bounds__(CLIP_THREADS, 4) clip_norm_kernel(const ClipChunk* __restrict__ chunks, long long count, double* __restrict__ partial) {
     let_next_kernel_start();
     wait_for_previous_kernel();
     double sum = 0.0;
+    ClipChunk next = load_chunk(chunks + blockIdx.x);             // (no more blocks than chunks)
     for (long long i = blockIdx.x; i < count; i += gridDim.x) {
-        const ClipChunk c = load_chunk(chunks + i);
+        const ClipChunk c = next;
+        if (i + gridDim.x < count) next = load_chunk(chunks + i + gridDim.x);
         if (c.dtype == EBS_F32) chunk_squares<float>(c, sum);
         else if (c.dtype == EBS_F16) chunk_squares<__half>(c, sum);
         else chunk_squares<__nv_bfloat16>(c, sum);
@@ -135,13 +163,14 @@ __device__ __forceinline__ void row_scale(const T* p, T* to, int cols, int t, in
     const int head = head_of(p, cols), packs = (cols - head) / N, tail = head + packs * N;
     const uint4* q = reinterpret_cast<const uint4*>(p + head);
     uint4* r = reinterpret_cast<uint4*>(to + head);
+    constexpr int U = CLIP_UNROLL / 2;                        // (with the bytes written as many are under way)
     int i = t;
-    for (; i + (CLIP_UNROLL - 1) * step < packs; i += CLIP_UNROLL * step) {
-        uint4 u[CLIP_UNROLL];
+    for (; i + (U - 1) * step < packs; i += U * step) {
+        uint4 u[U];
 #pragma unroll
-        for (int j = 0; j < CLIP_UNROLL; ++j) u[j] = q[i + j * step];
+        for (int j = 0; j < U; ++j) u[j] = q[i + j * step];
 #pragma unroll
-        for (int j = 0; j < CLIP_UNROLL; ++j) {
+        for (int j = 0; j < U; ++j) {
             scale_pack<T>(u[j], f);
             r[i + j * step] = u[j];
         }
@@ -163,17 +192,20 @@ __device__ __forceinline__ void chunk_scale(const ClipChunk& c, float f) {
         for (int r = threadIdx.x >> 5; r < c.rows; r += CLIP_THREADS / 32) row_scale(p + r * c.ld_in, to + r * c.ld_out, c.cols, threadIdx.x & 31, 32, f);
 }
 
-__global__ void __launch_bounds__(CLIP_THREADS) clip_scale_kernel(const ClipChunk* __restrict__ chunks, long long count, const double* __restrict__ partial, int parts,
+__global__ void __launch_bounds__(CLIP_THREADS, 4) clip_scale_kernel(const ClipChunk* __restrict__ chunks, long long count, const double* __restrict__ partial, int parts,
                                                                   float max_norm, float* __restrict__ norm_out) {
     let_next_kernel_start();
     wait_for_previous_kernel();
+    ClipChunk next = {};
+    if (blockIdx.x < count) next = load_chunk(chunks + count - 1 - blockIdx.x);
     double sum = 0.0;
     for (int i = threadIdx.x; i < parts; i += CLIP_THREADS) sum += partial[i];
     const double norm = sqrt(block_sum(sum));
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     const float f = norm <= (double)max_norm ? 1.0f : (float)((double)max_norm / norm);      // (a NaN norm: NaN)
     for (long long i = (long long)count - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
-        const ClipChunk c = load_chunk(chunks + i);
+        const ClipChunk c = next;
+        if (i >= gridDim.x) next = load_chunk(chunks + i - gridDim.x);
         if (f == 1.0f && c.in == c.out) continue;
         if (c.dtype == EBS_F32) chunk_scale<float>(c, f);
         else if (c.dtype == EBS_F16) chunk_scale<__half>(c, f);
@@ -206,14 +238,20 @@ static int complete_tensor(const ebs_clip_tensor& in, ebs_clip_tensor* t) {
     }
     return EBS_OK;
 }
-static long long row_segments(const ebs_clip_tensor& t) { return (t.cols + CLIP_CHUNK - 1) / CLIP_CHUNK; }
-static long long rows_of_chunk(const ebs_clip_tensor& t) {
-    const long long r = CLIP_CHUNK / t.cols;
-    return t.rows == 1 || r < 1 ? 1 : r;
+// How a tensor is cut: rows that a chunk takes (a warp each, whole eights), or pieces of one row for the whole block.
+struct Cut {
+    long long rows, cols;
+};
+static Cut cut_of(const ebs_clip_tensor& t, bool small) {
+    const long long size = (long long)element_size(t.dtype), chunk = (small ? CLIP_CHUNK_SMALL : CLIP_CHUNK) / size;
+    if (t.rows == 1 || t.cols * size > 16384) return {1, chunk};
+    const long long r = chunk / t.cols & ~7LL;
+    return {r < 8 ? 8 : r, t.cols};
 }
-static long long tensor_chunks(const ebs_clip_tensor& t) {
+static long long tensor_chunks(const ebs_clip_tensor& t, bool small) {
     if (t.rows == 0) return 0;
-    return (t.rows + rows_of_chunk(t) - 1) / rows_of_chunk(t) * row_segments(t);
+    const Cut c = cut_of(t, small);
+    return (t.rows + c.rows - 1) / c.rows * ((t.cols + c.cols - 1) / c.cols);
 }
 // What a tensor reads or writes, in bytes.
 struct Extent {
@@ -235,12 +273,19 @@ extern "C" {
 
 int ebs_clip_plan(const ebs_clip_tensor* tensors, int count, void* plan_host, long long* chunks) {
     if (!chunks || count < 0 || (count && !tensors)) return EBS_ERR_INVALID_ARG;
-    long long total = 0;
+    long long total = 0, bytes = 0;
     for (int i = 0; i < count; ++i) {
         ebs_clip_tensor t;
         const int rc = complete_tensor(tensors[i], &t);
         if (rc) return rc;
-        total += tensor_chunks(t);
+        bytes += t.rows * t.cols * (long long)element_size(t.dtype);
+        if (bytes > (1LL << 42)) return EBS_ERR_OVERFLOW;
+    }
+    const bool small = bytes <= CLIP_SMALL;
+    for (int i = 0; i < count; ++i) {
+        ebs_clip_tensor t;
+        complete_tensor(tensors[i], &t);
+        total += tensor_chunks(t, small);
         if (total > (1LL << 31)) return EBS_ERR_OVERFLOW;
     }
     // no output may share an element with another tensor: extents in the order of their addresses
@@ -274,16 +319,17 @@ int ebs_clip_plan(const ebs_clip_tensor* tensors, int count, void* plan_host, lo
             ebs_clip_tensor t;
             complete_tensor(tensors[i], &t);
             if (t.rows == 0) continue;
-            const long long size = (long long)element_size(t.dtype), step = rows_of_chunk(t);
-            for (long long r = 0; r < t.rows; r += step)
-                for (long long c = 0; c < t.cols; c += CLIP_CHUNK) {
+            const long long size = (long long)element_size(t.dtype);
+            const Cut cut = cut_of(t, small);
+            for (long long r = 0; r < t.rows; r += cut.rows)
+                for (long long c = 0; c < t.cols; c += cut.cols) {
                     ClipChunk k = {};
                     k.in = static_cast<const char*>(t.in_dev) + (r * t.ld_in + c) * size;
                     k.out = static_cast<char*>(t.out_dev) + (r * t.ld_out + c) * size;
                     k.ld_in = t.ld_in;
                     k.ld_out = t.ld_out;
-                    k.rows = (int)(t.rows - r < step ? t.rows - r : step);
-                    k.cols = (int)(t.cols - c < CLIP_CHUNK ? t.cols - c : CLIP_CHUNK);
+                    k.rows = (int)(t.rows - r < cut.rows ? t.rows - r : cut.rows);
+                    k.cols = (int)(t.cols - c < cut.cols ? t.cols - c : cut.cols);
                     k.dtype = t.dtype;
                     memcpy(to, &k, sizeof(k));
                     to += sizeof(k);

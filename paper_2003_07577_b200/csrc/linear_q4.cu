@@ -62,11 +62,25 @@ __device__ __forceinline__ void load8(const S* p, int left, bool vec, float (&v)
 
 // floor(w / s + 1/2) within -8 .. 7, exactly: the quotient by the reciprocal is off by a rounding or two, the remainders of a
 // fused multiply-add tell on which side of a border w lies.  inv = 1 / s.
-__device__ __forceinline__ int q4_code(float w, float s, float inv) {
+__device__ __noinline__ int q4_code_exact(float w, float s, float inv) {
     float c = fminf(fmaxf(floorf(fmaf(w, inv, 0.5f)), -8.0f), 7.0f);
     if (c < 7.0f && fmaf(-(c + 0.5f), s, w) >= 0.0f) c += 1.0f;
     else if (c > -8.0f && fmaf(-(c - 0.5f), s, w) < 0.0f) c -= 1.0f;
     return (int)c;
+}
+// The codes of eight weights, in the low four bits of each word, exactly too: a number of this size added leaves the quotient rounded in the low bits.  Where one lies within 2^-16 of a
+// border (the quotient is off by less), or the quotients leave the codes' range (a scale of few bits), each is found by its remainders.
+__device__ __forceinline__ void q4_codes(const float (&v)[8], float s, float inv, bool wide, uint32_t (&code)[8]) {
+    float far = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float q = v[e] * inv, r = q + 12582912.0f;                 // 1.5 * 2^23
+        code[e] = __float_as_uint(r);
+        far = fmaxf(far, fabsf(q - (r - 12582912.0f)));
+    }
+    if (far > 0.5f - 0x1p-16f || wide)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) code[e] = (uint32_t)q4_code_exact(v[e], s, inv);
 }
 
 template <typename S>
@@ -132,15 +146,20 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4
                     if ((lane & 3) == 0 && (G == 32 || r == 0) && (G != 128 || b == 0) && group < g.groups)
                         static_cast<T*>(g.scales)[(tile * g.groups + group) * Q4_ROWS + 2 * gid + half] = row < g.n ? kept : from_f32<T>(0.0f);
                     if (!(s > 0.0f) || (__float_as_uint(s) & 0x7f800000u) == 0x7f800000u) continue;          // (codes of zero)
-                    const float up = s < 1e-30f ? 1.2676506e30f : 1.0f;                                      // 2^100: no reciprocal overflows, no remainder is lost
-                    s *= up;
+                    if (s < 1e-30f) {                                        // times 2^100: no reciprocal overflows, no remainder is lost
+                        s *= 1.2676506e30f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[b][r][e] *= 1.2676506e30f;
+                        top[b][r] = __float_as_uint(__uint_as_float(top[b][r]) * 1.2676506e30f);
+                    }
                     const float inv = 1.0f / s;
+                    uint32_t code[8];
+                    q4_codes(v[b][r], s, inv, __uint_as_float(top[b][r]) * inv > 7.4f, code);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const uint32_t c = (uint32_t)(q4_code(v[b][r][e] * up, s, inv) + 8);
-                        // register 2 * h + half of the MMA, element j
+                        // register 2 * h + half of the MMA, element j; the code + 8 is the code with its sign bit turned
                         const int at = 4 * (2 * ((e >> 1) & 1) + half) + 16 * (e & 1);
-                        word[b][2 * r + (e >> 2)] = (word[b][2 * r + (e >> 2)] & ~(15u << at)) | c << at;
+                        word[b][2 * r + (e >> 2)] ^= (code[e] & 15u) << at;
                     }
                 }
         }

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-CHUNK = 8192
+CHUNK = 16384
 P = [0x10000000000 + (i << 36) for i in range(8)]      # aligned, far apart, never dereferenced
 
 
@@ -37,7 +37,7 @@ def covered(ebs, tensors):
     for w in words.tolist():
         rows, cols, dtype = w[4] & 0xffffffff, w[4] >> 32, w[5] & 0xffffffff
         size = 4 if dtype == 0 else 2
-        assert rows >= 1 and 1 <= cols <= CHUNK and rows * cols <= CHUNK
+        assert rows >= 1 and 1 <= cols <= CHUNK and (rows == 1 or cols * size <= 16384)
         for r in range(rows):
             for c in range(cols):
                 seen.append((w[0] + (r * w[2] + c) * size, w[1] + (r * w[3] + c) * size, dtype))
