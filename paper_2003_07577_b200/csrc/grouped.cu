@@ -32,16 +32,20 @@ struct GroupedArgs {
     int test_flags;
 };
 
-// The forms by the columns of a tile: 256 a pair, 128 a block an SM, 64 two blocks an SM.
-template <int TN> struct GroupedForm {
-    static constexpr bool PAIR = TN == 256;
-    static constexpr int B_COLS = PAIR ? TN / 2 : TN;             // columns of B that a block fetches
+// The forms: 256 a pair's 256 x 256 results, 128 and 64 so many columns of 128 rows, one and two blocks an SM, FEW_ROWS 64 columns of 32 rows, two blocks an SM with seven stages of
+// little more than the weights.  (The tensor core still takes 128 rows: those behind the 32 are whatever lies there, and so are the lanes of sums that nobody reads.)
+constexpr int FEW_ROWS = 32;
+template <int F> struct GroupedForm {
+    static constexpr bool PAIR = F == 256;
+    static constexpr int TN = F == FEW_ROWS ? 64 : F;
+    static constexpr int A_ROWS = F == FEW_ROWS ? 32 : 128, B_COLS = PAIR ? TN / 2 : TN;             // rows of A and columns of B that a block fetches
     static constexpr int EPI_WARPS = PAIR ? 16 : 8, THREADS = PAIR ? 640 : 320;        // (pair: whole warpgroups, whose registers are dealt anew)
-    static constexpr int STAGES = TN == 64 ? 3 : 6, STAGE = (128 + B_COLS) * GEMM_ROW_BYTES;
+    static constexpr int STAGES = F == FEW_ROWS ? 7 : F == 64 ? 3 : 6, A_BYTES = A_ROWS * GEMM_ROW_BYTES, STAGE = A_BYTES + B_COLS * GEMM_ROW_BYTES;
     static constexpr int CQ = TN / (EPI_WARPS / 4);               // columns of a warp
     static constexpr int PATCH = 32 * 64;                         // 32 rows of 64 bytes
-    static constexpr int SMEM = STAGES * STAGE + EPI_WARPS * PATCH + 1024;
-    static constexpr int ROWS = PAIR ? 256 : 128;                 // rows of a tile
+    static constexpr int SMEM = STAGES * STAGE + EPI_WARPS * PATCH + 1024, BLOCKS = TN == 64 ? 2 : 1;
+    static constexpr int ROWS = PAIR ? 256 : A_ROWS;              // rows of a tile
+    static_assert(B_COLS * GEMM_ROW_BYTES + EPI_WARPS * PATCH >= (128 - A_ROWS) * GEMM_ROW_BYTES, "what the tensor core reads behind the last stage's rows is this block's memory");
 };
 
 // Rows of expert e; offsets that are out of order or out of range are taken as the nearest ones that are not.
@@ -183,14 +187,15 @@ __device__ __forceinline__ void finish_columns(const GroupedArgs& g, const Group
 }
 
 // DW: the form for weight gradients.  CHUNKS: sums leave tensor memory every GEMM_LONG stages and go on in registers.
-template <typename T, int TN, bool DW, bool CHUNKS>
-__global__ void __launch_bounds__(GroupedForm<TN>::THREADS, TN == 64 ? 2 : 1) grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+template <typename T, int F, bool DW, bool CHUNKS>
+__global__ void __launch_bounds__(GroupedForm<F>::THREADS, GroupedForm<F>::BLOCKS) grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                                                               const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z,
                                                                                               const __grid_constant__ GroupedArgs g) {
     extern __shared__ uint8_t smem_raw[];
-    using Form = GroupedForm<TN>;
+    using Form = GroupedForm<F>;
     constexpr bool PAIR = Form::PAIR;
-    constexpr int S = Form::STAGES, STAGE = Form::STAGE, A_BYTES = 128 * GEMM_ROW_BYTES, CQ = Form::CQ, EPI = Form::EPI_WARPS;
+    constexpr int TN = Form::TN, S = Form::STAGES, STAGE = Form::STAGE, A_BYTES = Form::A_BYTES, CQ = Form::CQ, EPI = Form::EPI_WARPS;
+    static_assert(!DW || Form::A_ROWS == 128, "rows of a weight gradient are its lanes");
     __shared__ uint64_t full[S], empty[S], acc_full[2], acc_empty[2], ready[S];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
@@ -335,7 +340,7 @@ __global__ void __launch_bounds__(GroupedForm<TN>::THREADS, TN == 64 ? 2 : 1) gr
             }
         };
         for (int t = start; ok && order.find(g, t, TN, tile); t += step) {
-            const int row0 = tile.a0 + rank * 128 + (warp & 3) * 32, rows = min(tile.a_end - row0, 32);
+            const int row0 = tile.a0 + rank * 128 + (warp & 3) * 32, rows = min(min(tile.a_end, tile.a0 + Form::ROWS) - row0, 32);
             const int col0 = tile.b0 + (warp >> 2) * CQ;
             auto out = [&](float (&v)[32], int j) {
                 const int left = g.cols - col0 - j;
@@ -524,11 +529,12 @@ static GroupedOperand plan_rows(const void* p, long long rows, int cols, long lo
     return {to, ldd, 0};
 }
 
-template <typename T, int TN, bool DW, bool CHUNKS>
+template <typename T, int F, bool DW, bool CHUNKS>
 static int launch_grouped(const CUtensorMap (&map)[4], const GroupedArgs& g, long long tiles, cudaStream_t st) {
-    auto kern = grouped_kernel<T, TN, DW, CHUNKS>;
-    constexpr int SMEM = GroupedForm<TN>::SMEM;
-    static_assert(SMEM + 512 <= 227 * 1024, "shared memory of a block");
+    using Form = GroupedForm<F>;
+    auto kern = grouped_kernel<T, F, DW, CHUNKS>;
+    constexpr int SMEM = Form::SMEM;
+    static_assert(Form::BLOCKS * (SMEM + 512 + 1024) <= 228 * 1024, "shared memory of an SM: the blocks', what is static in them, and 1 KB that each takes besides");
     static bool attr_set[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
@@ -536,9 +542,9 @@ static int launch_grouped(const CUtensorMap (&map)[4], const GroupedArgs& g, lon
         if (check_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM))) return EBS_ERR_CUDA;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    constexpr int cluster = GroupedForm<TN>::PAIR ? 2 : 1;
-    const long long at_once = (long long)gemm_sm_count() * (TN == 64 ? 2 : 1) / cluster;
-    return launch_chained(kern, dim3((unsigned)(cluster * (tiles < at_once ? tiles : at_once))), GroupedForm<TN>::THREADS, (size_t)SMEM, st, cluster, map[0], map[1], map[2], map[3], g);
+    constexpr int cluster = Form::PAIR ? 2 : 1;
+    const long long at_once = (long long)gemm_sm_count() * Form::BLOCKS / cluster;
+    return launch_chained(kern, dim3((unsigned)(cluster * (tiles < at_once ? tiles : at_once))), Form::THREADS, (size_t)SMEM, st, cluster, map[0], map[1], map[2], map[3], g);
 }
 // Columns of a tile; rows_of_pair, rows_of_block: how many times 256 and 128 rows there are to cover.  Pairs where there is a tile for each of them (a tile of 256 x 256
 // a pair takes less than 128 x 128 a block each), else tiles for every SM, else the narrowest ones.
@@ -547,12 +553,13 @@ static int grouped_columns(long long rows_of_pair, long long rows_of_block, int 
     if (rows_of_pair * ((cols + 255) / 256) >= sms / 2) return 256;
     return rows_of_block * ((cols + 127) / 128) >= sms ? 128 : 64;
 }
+// row_tiles: of the form that was chosen.
 template <typename T, bool DW>
-static int launch_columns(int tn, const GemmOperand& a, int a_mn, int a_red, const GemmOperand& b, int b_cols, int b_red, int batch, GroupedArgs& g, long long row_tiles, bool chunks, cudaStream_t st) {
-    // row_tiles: of the form that was chosen
+static int launch_form(int form, const GemmOperand& a, int a_mn, int a_red, const GemmOperand& b, int b_cols, int b_red, int batch, GroupedArgs& g, long long row_tiles, bool chunks, cudaStream_t st) {
     CUtensorMap map[4] = {};
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
-    if (!gemm_operand_map(a, a_mn, a_red, 1, 128, bf16, &map[0]) || !gemm_operand_map(b, b_cols, b_red, batch, tn == 256 ? 128 : tn, bf16, &map[1])) return EBS_ERR_CUDA;
+    const int tn = form == FEW_ROWS ? 64 : form;
+    if (!gemm_operand_map(a, a_mn, a_red, 1, form == FEW_ROWS ? FEW_ROWS : 128, bf16, &map[0]) || !gemm_operand_map(b, b_cols, b_red, batch, tn == 256 ? 128 : tn, bf16, &map[1])) return EBS_ERR_CUDA;
     g.bf16 = bf16;
     g.tma = DW ? result_map<T>(g.y, g.rows, g.cols, g.ldy, g.experts, g.y_expert, &map[2])
                : result_map<T>(g.y, g.m, g.cols, g.ldy, 1, 0, &map[2]) && result_map<T>(g.z, g.m, g.cols, g.ldz, 1, 0, &map[3]);
@@ -561,9 +568,14 @@ static int launch_columns(int tn, const GemmOperand& a, int a_mn, int a_red, con
     g.test_flags = device_test_flags();
     const long long tiles = row_tiles * g.tiles_n;
     if (tiles >= (1LL << 30)) return EBS_ERR_OVERFLOW;
-    if (tn == 256) return chunks ? launch_grouped<T, 256, DW, true>(map, g, tiles, st) : launch_grouped<T, 256, DW, false>(map, g, tiles, st);
-    if (tn == 128) return chunks ? launch_grouped<T, 128, DW, true>(map, g, tiles, st) : launch_grouped<T, 128, DW, false>(map, g, tiles, st);
-    return chunks ? launch_grouped<T, 64, DW, true>(map, g, tiles, st) : launch_grouped<T, 64, DW, false>(map, g, tiles, st);
+    switch (form) {
+        case 256: return chunks ? launch_grouped<T, 256, DW, true>(map, g, tiles, st) : launch_grouped<T, 256, DW, false>(map, g, tiles, st);
+        case 128: return chunks ? launch_grouped<T, 128, DW, true>(map, g, tiles, st) : launch_grouped<T, 128, DW, false>(map, g, tiles, st);
+        case FEW_ROWS:
+            if constexpr (!DW) return chunks ? launch_grouped<T, FEW_ROWS, DW, true>(map, g, tiles, st) : launch_grouped<T, FEW_ROWS, DW, false>(map, g, tiles, st);
+            return EBS_ERR_UNSUPPORTED;
+        default: return chunks ? launch_grouped<T, 64, DW, true>(map, g, tiles, st) : launch_grouped<T, 64, DW, false>(map, g, tiles, st);
+    }
 }
 // Tiles of `tile` rows there can be at most: one more than whole ones for each expert that has rows; and how many there are where all have the same number.
 static long long most_row_tiles(int m, int experts, int tile) { return m / tile + (experts < m ? experts : m); }
@@ -587,8 +599,9 @@ static int rows_product(const GroupedTensors& t, int m, int experts, int cols, i
     g.b_mn = b_mn;
     GemmOperand A(a.p, a.ld, false), B(w.p, w.ld, b_mn, 1, 0, w.expert);
     const bool chunks = red > GEMM_LONG * GEMM_BK;
-    const int tn = grouped_columns(expected_row_tiles(m, experts, 256), expected_row_tiles(m, experts, 128), cols);
-    return launch_columns<T, false>(tn, A, m, red, B, cols, red, experts, g, most_row_tiles(m, experts, tn == 256 ? 256 : 128), chunks, st);
+    // few rows an expert: bound by the bytes of the weights
+    const int form = m <= FEW_ROWS * (long long)(experts < m ? experts : m) ? FEW_ROWS : grouped_columns(expected_row_tiles(m, experts, 256), expected_row_tiles(m, experts, 128), cols);
+    return launch_form<T, false>(form, A, m, red, B, cols, red, experts, g, most_row_tiles(m, experts, form == 256 ? 256 : form == FEW_ROWS ? FEW_ROWS : 128), chunks, st);
 }
 static bool rows_ok(const void* p, long long ld) { return !p || (ld & 7) == 0; }
 
@@ -669,7 +682,7 @@ static int grouped_backward(const ebs_linear_desc& d, int experts, const Grouped
         const int tn = grouped_columns(pairs, blocks, d.k);
         GemmOperand A(dz.p, dz.ld, true), B(x.p, x.ld, true);
         const bool chunks = d.m > GEMM_LONG * GEMM_BK;
-        if ((rc = launch_columns<T, true>(tn, A, d.n, d.m, B, d.k, d.m, 1, g, tn == 256 ? pairs : blocks, chunks, st))) return rc;
+        if ((rc = launch_form<T, true>(tn, A, d.n, d.m, B, d.k, d.m, 1, g, tn == 256 ? pairs : blocks, chunks, st))) return rc;
     }
     return EBS_OK;
 }

@@ -120,6 +120,14 @@ def test_sizes(ebs, dtype, n, k):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("counts", [[1, 0, 2, 24, 31, 32, 33, 5, 0, 0, 1, 1], [40, 1, 0, 7, 0, 3, 1], [96, 1, 1, 1, 1, 1, 1, 1, 1, 1]], ids=str)
+@pytest.mark.parametrize("n,k,ldy", [(256, 1024, 0), (100, 520, 0), (72, 8, 75), (64, 4200, 0)])
+def test_few_rows(ebs, dtype, counts, n, k, ldy):
+    """At most 32 rows an expert in the mean: tiles of 32 rows, experts with more of them among the others."""
+    layer(ebs, 13, counts, n, k, dtype, act=4, residual=True, keep=True, spare=2, first=1, ldy=ldy)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("act", range(5))
 @pytest.mark.parametrize("bias,residual,keep", [(False, False, False), (True, True, True), (False, True, False)])
 def test_activations(ebs, dtype, act, bias, residual, keep):
