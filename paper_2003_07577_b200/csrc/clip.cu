@@ -19,6 +19,7 @@ namespace ebs {
 constexpr int CLIP_BLOCKS = 148 * 4;        // at most: a wave of blocks of 256 threads
 constexpr int CLIP_THREADS = 256;
 constexpr int CLIP_UNROLL = 8;              // packs of a thread under way: 32 KB a block (four, and records loaded when they are needed: 1.07 GB read at 3.4 TB/s)
+constexpr int CLIP_NARROW = 512;            // bytes of a row that a warp's lanes would not fill: the block takes the rows' elements one by one
 // Bytes of a chunk of one row: as many as the block has under way; a network of a few MB is cut finer, so that every SM has some.
 constexpr long long CLIP_CHUNK = CLIP_THREADS * 16 * CLIP_UNROLL, CLIP_CHUNK_SMALL = CLIP_THREADS * 16, CLIP_SMALL = 8 << 20;
 
@@ -113,7 +114,19 @@ template <typename T>
 __device__ __forceinline__ void chunk_squares(const ClipChunk& c, double& sum) {
     const T* p = static_cast<const T*>(c.in);
     if (c.rows == 1) row_squares(p, c.cols, threadIdx.x, CLIP_THREADS, sum);
-    else
+    else if (c.cols * (int)sizeof(T) < CLIP_NARROW) {
+        const unsigned cols = (unsigned)c.cols, all = (unsigned)c.rows * cols;
+        for (unsigned i = threadIdx.x; i < all; i += CLIP_UNROLL * CLIP_THREADS) {
+            T v[CLIP_UNROLL];
+#pragma unroll
+            for (unsigned j = 0; j < CLIP_UNROLL; ++j) {
+                const unsigned at = i + j * CLIP_THREADS;
+                v[j] = at < all ? p[at / cols * c.ld_in + at % cols] : from_f32<T>(0.0f);
+            }
+#pragma unroll
+            for (int j = 0; j < CLIP_UNROLL; ++j) add_square(v[j], sum);
+        }
+    } else
         for (int r = threadIdx.x >> 5; r < c.rows; r += CLIP_THREADS / 32) row_squares(p + r * c.ld_in, c.cols, threadIdx.x & 31, 32, sum);
 }
 __device__ __forceinline__ double block_sum(double v) {
@@ -188,7 +201,22 @@ __device__ __forceinline__ void chunk_scale(const ClipChunk& c, float f) {
     const T* p = static_cast<const T*>(c.in);
     T* to = static_cast<T*>(c.out);
     if (c.rows == 1) row_scale(p, to, c.cols, threadIdx.x, CLIP_THREADS, f);
-    else
+    else if (c.cols * (int)sizeof(T) < CLIP_NARROW) {
+        const unsigned cols = (unsigned)c.cols, all = (unsigned)c.rows * cols;
+        for (unsigned i = threadIdx.x; i < all; i += CLIP_UNROLL * CLIP_THREADS) {
+            T v[CLIP_UNROLL];
+#pragma unroll
+            for (unsigned j = 0; j < CLIP_UNROLL; ++j) {
+                const unsigned at = i + j * CLIP_THREADS;
+                if (at < all) v[j] = p[at / cols * c.ld_in + at % cols];
+            }
+#pragma unroll
+            for (unsigned j = 0; j < CLIP_UNROLL; ++j) {
+                const unsigned at = i + j * CLIP_THREADS;
+                if (at < all) to[at / cols * c.ld_out + at % cols] = from_f32<T>(to_f32(v[j]) * f);
+            }
+        }
+    } else
         for (int r = threadIdx.x >> 5; r < c.rows; r += CLIP_THREADS / 32) row_scale(p + r * c.ld_in, to + r * c.ld_out, c.cols, threadIdx.x & 31, 32, f);
 }
 

@@ -141,7 +141,16 @@ __device__ __forceinline__ void store_patch(uint8_t* patch, const float (&v)[32]
             const int r = i * 8 + (lane >> 2), c = lane & 3;
             if (r < rows) *reinterpret_cast<uint4*>(to + r * ld + c * 8) = *patch_chunk(patch, r, c);
         }
+    } else if ((ld & 1) == 0) {                                   // two elements a lane, two rows an access
+        const int c = (lane & 15) * 2;
+#pragma unroll 8
+        for (int r = lane >> 4; r < rows; r += 2) {
+            const uint32_t* from = reinterpret_cast<const uint32_t*>(patch_chunk(patch, r, c >> 3)) + ((c & 7) >> 1);
+            if (c + 1 < left) *reinterpret_cast<uint32_t*>(to + r * ld + c) = *from;
+            else if (c < left) to[r * ld + c] = *reinterpret_cast<const T*>(from);
+        }
     } else if (lane < left)
+#pragma unroll 8
         for (int r = 0; r < rows; ++r) to[r * ld + lane] = reinterpret_cast<const T*>(patch_chunk(patch, r, lane >> 3))[lane & 7];
 }
 

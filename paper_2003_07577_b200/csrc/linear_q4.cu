@@ -34,7 +34,7 @@ static int check_q4(const ebs_q4_desc* d) {
     if (d->group != 32 && d->group != 64 && d->group != 128) return EBS_ERR_INVALID_ARG;
     if (d->n > (1 << 30) || d->k > (1 << 30) || (double)d->experts * d->n * d->k > (double)(1LL << 40)) return EBS_ERR_OVERFLOW;
     const Q4Layout l = q4_layout(*d);
-    if ((long long)d->experts * l.tiles * l.kbs >= (1LL << 34)) return EBS_ERR_OVERFLOW;
+    if ((long long)d->experts * l.tiles * l.kbs >= (1LL << 31)) return EBS_ERR_OVERFLOW;
     return EBS_OK;
 }
 
@@ -88,22 +88,29 @@ struct Q4Pack {
     const S* w;
     uint4* codes;
     void* scales;
-    long long ldw, units;                  // units: warps' pieces of work
+    long long ldw;
+    unsigned units;                        // warps' pieces of work
     int n, k, tiles, kbs, groups, vec;
 };
+// Eight rows of a piece of weights as the lanes of a warp have them, for matrices whose rows start anywhere: in memory the lanes take neighbouring elements, here their own eight (an element
+// a lane in 32 places of memory takes 32 accesses: 4.6 million weights of rows of 198 fp16 values packed and read back in 36 us).
+template <typename S, int COLS> struct Q4Stage { S row[8][COLS + 16 / sizeof(S)]; };
+
 // A warp packs 16 rows x KB tiles of 64 inputs, which hold whole groups of G: the largest magnitudes, scales and codes from one load.
 template <typename S, typename T, int G>
 __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4Pack<S> g) {
     constexpr int KB = G == 128 ? 2 : 1;
     let_next_kernel_start();
     wait_for_previous_kernel();
+    __shared__ __align__(16) Q4Stage<S, KB * Q4_K> stages[8];
     const int lane = threadIdx.x & 31, gid = lane >> 2;
-    const int across = (g.kbs + KB - 1) / KB;
-    for (long long u = blockIdx.x * 8LL + (threadIdx.x >> 5); u < g.units; u += gridDim.x * 8LL) {
+    Q4Stage<S, KB * Q4_K>& stage = stages[threadIdx.x >> 5];
+    const unsigned across = (unsigned)((g.kbs + KB - 1) / KB);
+    for (unsigned u = blockIdx.x * 8u + (threadIdx.x >> 5); u < g.units; u += gridDim.x * 8u) {
         const long long tile = u / across;                        // of all experts
-        const int kb0 = (int)(u - tile * across) * KB;
-        const long long expert = tile / g.tiles;
-        const int row0 = (int)(tile - expert * g.tiles) * Q4_ROWS;
+        const int kb0 = (int)(u % across) * KB;
+        const long long expert = (unsigned)tile / (unsigned)g.tiles;
+        const int row0 = (int)((unsigned)tile % (unsigned)g.tiles) * Q4_ROWS;
         uint32_t word[KB][4];
 #pragma unroll
         for (int b = 0; b < KB; ++b)
@@ -115,12 +122,24 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4
             const S* p = g.w + (expert * g.n + row) * g.ldw;
             float v[KB][2][8];
             unsigned top[KB][2];
+            if (!g.vec) {
+                __syncwarp();                                     // (what was there is read)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2 * KB; ++h) {
+                        const int at = row0 + 8 * half + i, c = kb0 * Q4_K + h * 32 + lane;
+                        stage.row[i][h * 32 + lane] = at < g.n && c < g.k ? g.w[(expert * g.n + at) * g.ldw + c] : from_f32<S>(0.0f);
+                    }
+                __syncwarp();
+            }
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const int c = (kb0 + b) * Q4_K + q4_input(r, lane, 0);
-                    load8<S>(p + c, row < g.n ? g.k - c : 0, g.vec, v[b][r]);
+                    const int c = b * Q4_K + q4_input(r, lane, 0), left = g.k - kb0 * Q4_K - c;
+                    if (g.vec) load8<S>(p + kb0 * Q4_K + c, row < g.n ? left : 0, true, v[b][r]);
+                    else load8<S>(&stage.row[gid][c], 8, true, v[b][r]);
                 }
 #pragma unroll
             for (int b = 0; b < KB; ++b)
@@ -174,40 +193,55 @@ struct Q4Unpack {
     const uint4* codes;
     const void* scales;
     D* w;
-    long long ldw, units;
+    long long ldw;
+    unsigned units;
     int n, k, tiles, kbs, groups, group, vec;
 };
 template <typename T, typename D>
 __global__ void __launch_bounds__(256) q4_unpack_kernel(const __grid_constant__ Q4Unpack<D> g) {
+    __shared__ __align__(16) Q4Stage<D, Q4_K> stages[8];
     let_next_kernel_start();
     wait_for_previous_kernel();
+    constexpr int N = Pack<D>::N;
     const int lane = threadIdx.x & 31, gid = lane >> 2;
-    for (long long u = blockIdx.x * 8LL + (threadIdx.x >> 5); u < g.units; u += gridDim.x * 8LL) {
-        const long long tile = u / g.kbs, expert = tile / g.tiles;
-        const int kb = (int)(u - tile * g.kbs), row0 = (int)(tile - expert * g.tiles) * Q4_ROWS;
-        const uint4 q = g.codes[u * 32 + lane];
+    Q4Stage<D, Q4_K>& stage = stages[threadIdx.x >> 5];
+    for (unsigned u = blockIdx.x * 8u + (threadIdx.x >> 5); u < g.units; u += gridDim.x * 8u) {
+        const long long tile = u / (unsigned)g.kbs, expert = (unsigned)tile / (unsigned)g.tiles;
+        const int kb = (int)(u % (unsigned)g.kbs), row0 = (int)((unsigned)tile % (unsigned)g.tiles) * Q4_ROWS;
+        const uint4 q = g.codes[(long long)u * 32 + lane];
         const uint32_t word[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int half = 0; half < 2; ++half) {
+            if (!g.vec) __syncwarp();                             // (what was there is read)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const int row = row0 + gid + 8 * half, c = kb * Q4_K + q4_input(r, lane, 0);
                 if (row >= g.n || c >= g.k) continue;
                 const float s = to_f32(static_cast<const T*>(g.scales)[(tile * g.groups + (kb * Q4_K + r * 32) / g.group) * Q4_ROWS + 2 * gid + half]);
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = s * (float)((int)(word[2 * r + (e >> 2)] >> (4 * (2 * ((e >> 1) & 1) + half) + 16 * (e & 1)) & 15u) - 8);
-                D* to = g.w + (expert * g.n + row) * g.ldw + c;
-                constexpr int N = Pack<D>::N;
-                const int left = g.k - c;
+                D* to = g.vec ? g.w + (expert * g.n + row) * g.ldw + c : &stage.row[gid][c - kb * Q4_K];
+                const int left = g.vec ? g.k - c : 8;
 #pragma unroll
                 for (int i = 0; i < 8 / N; ++i) {
                     float t[N];
 #pragma unroll
-                    for (int e = 0; e < N; ++e) t[e] = v[i * N + e];
-                    store_pack(to + i * N, t, left - i * N, g.vec && left >= (i + 1) * N);
+                    for (int e = 0; e < N; ++e) {
+                        const int j = i * N + e;
+                        t[e] = s * (float)((int)(word[2 * r + (j >> 2)] >> (4 * (2 * ((j >> 1) & 1) + half) + 16 * (j & 1)) & 15u) - 8);
+                    }
+                    store_pack(to + i * N, t, left - i * N, left >= (i + 1) * N);
                 }
             }
+            if (!g.vec) {
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int at = row0 + 8 * half + i, c = kb * Q4_K + h * 32 + lane;
+                        if (at < g.n && c < g.k) g.w[(expert * g.n + at) * g.ldw + c] = stage.row[i][h * 32 + lane];
+                    }
+            }
+        }
     }
 }
 
@@ -568,7 +602,8 @@ __global__ void __launch_bounds__(WARPS * 32, (q4_blocks<T, NT, WARPS>())) q4_ke
 // How a product is run, from its sizes alone.
 struct Q4Route {
     int nt;                                // rows that a block takes at a time, in eights: from those an expert has in the mean, twice that so that most experts' weights are read once
-    bool prepared, copied, wide;           // x goes through the workspace as planes (fp32) or as it is, since its rows start anywhere; wide: 16 warps share a tile's reduction
+    bool prepared, copied;                 // x goes through the workspace as planes (fp32) or as it is, since its rows start anywhere
+    int warps;                             // that share a tile's reduction
     long long pieces, blocks;              // pieces of rows: at most one for each expert that has rows, and one more for each full piece
     size_t workspace;
 };
@@ -584,7 +619,8 @@ static Q4Route q4_route(const ebs_linear_desc& d, const ebs_q4_desc& q) {
     r.prepared = d.dtype == EBS_F32 && r.blocks * kbs >= 8192;
     r.copied = !r.prepared && d.m > 1 && d.ldx * (long long)element_size(d.dtype) % 16 != 0;
 // (14336 -> 4096: 15.6 us with 8 warps a tile, of which two blocks an SM have work, 9.9 with 16)
-    r.wide = r.nt == 1 && r.blocks < 148 * 3 && kbs >= 32;
+    // Short reductions: two, whose blocks are many at a time (58 experts of 64 -> 8435 fp32, nine rows: 36 us with eight).
+    r.warps = r.nt == 1 && r.blocks < 148 * 3 && kbs >= 32 ? 16 : r.nt <= 2 && kbs <= 4 ? 2 : 8;
     r.workspace = r.prepared ? round256((size_t)d.m * kbs * Q4_K * 3 * 2) : r.copied ? round256((size_t)d.m * round8(d.k) * element_size(d.dtype)) : 0;
     return r;
 }
@@ -612,8 +648,8 @@ static int launch_q4_rows(Q4Args& g, const Q4Route& r, int group, cudaStream_t s
     if (r.blocks > 0x7fffffffLL) return EBS_ERR_OVERFLOW;
     g.slots = (int)r.pieces;
     switch (r.nt) {
-        case 1: return r.wide ? launch_q4_group<T, PREPARED, 1, 16>(g, r, group, st) : launch_q4_group<T, PREPARED, 1>(g, r, group, st);
-        case 2: return launch_q4_group<T, PREPARED, 2>(g, r, group, st);
+        case 1: return r.warps == 16 ? launch_q4_group<T, PREPARED, 1, 16>(g, r, group, st) : r.warps == 2 ? launch_q4_group<T, PREPARED, 1, 2>(g, r, group, st) : launch_q4_group<T, PREPARED, 1>(g, r, group, st);
+        case 2: return r.warps == 2 ? launch_q4_group<T, PREPARED, 2, 2>(g, r, group, st) : launch_q4_group<T, PREPARED, 2>(g, r, group, st);
         case 4: return launch_q4_group<T, PREPARED, 4>(g, r, group, st);
         default:
             if constexpr (sizeof(T) == 2) return launch_q4_group<T, PREPARED, 8>(g, r, group, st);
@@ -625,10 +661,10 @@ template <typename S, typename T>
 static int launch_pack_typed(const ebs_q4_desc& d, const void* w, long long ldw, void* packed, cudaStream_t st) {
     const Q4Layout l = q4_layout(d);
     const int kb = d.group == 128 ? 2 : 1;
-    Q4Pack<S> g{static_cast<const S*>(w), static_cast<uint4*>(packed), static_cast<char*>(packed) + l.codes, ldw, (long long)d.experts * l.tiles * ((l.kbs + kb - 1) / kb),
+    Q4Pack<S> g{static_cast<const S*>(w), static_cast<uint4*>(packed), static_cast<char*>(packed) + l.codes, ldw, (unsigned)(d.experts * (long long)l.tiles * ((l.kbs + kb - 1) / kb)),
                 d.n, d.k, l.tiles, l.kbs, l.groups, ldw * (long long)sizeof(S) % 16 == 0};
-    const long long blocks = (g.units + 7) / 8;
-    const dim3 grid((unsigned)(blocks < 148 * 64 ? blocks : 148 * 64));
+    const unsigned blocks = (g.units + 7u) / 8u;
+    const dim3 grid(blocks < 148 * 64 ? blocks : 148 * 64);
     if (d.group == 32) return launch_chained(q4_pack_kernel<S, T, 32>, grid, 256, 0, st, 1, g);
     if (d.group == 64) return launch_chained(q4_pack_kernel<S, T, 64>, grid, 256, 0, st, 1, g);
     return launch_chained(q4_pack_kernel<S, T, 128>, grid, 256, 0, st, 1, g);
@@ -642,10 +678,10 @@ static int launch_pack(const ebs_q4_desc& d, const void* w, long long ldw, void*
 template <typename T, typename D>
 static int launch_unpack_typed(const ebs_q4_desc& d, const void* packed, void* w, long long ldw, cudaStream_t st) {
     const Q4Layout l = q4_layout(d);
-    Q4Unpack<D> g{static_cast<const uint4*>(packed), static_cast<const char*>(packed) + l.codes, static_cast<D*>(w), ldw, (long long)d.experts * l.tiles * l.kbs, d.n, d.k,
+    Q4Unpack<D> g{static_cast<const uint4*>(packed), static_cast<const char*>(packed) + l.codes, static_cast<D*>(w), ldw, (unsigned)(d.experts * (long long)l.tiles * l.kbs), d.n, d.k,
                   l.tiles, l.kbs, l.groups, d.group, ldw * (long long)sizeof(D) % 16 == 0};
-    const long long blocks = (g.units + 7) / 8;
-    return launch_chained(q4_unpack_kernel<T, D>, dim3((unsigned)(blocks < 148 * 64 ? blocks : 148 * 64)), 256, 0, st, 1, g);
+    const unsigned blocks = (g.units + 7u) / 8u;
+    return launch_chained(q4_unpack_kernel<T, D>, dim3(blocks < 148 * 64 ? blocks : 148 * 64), 256, 0, st, 1, g);
 }
 template <typename D>
 static int launch_unpack(const ebs_q4_desc& d, const void* packed, void* w, long long ldw, cudaStream_t st) {
