@@ -154,12 +154,49 @@ __device__ __forceinline__ void store_patch(uint8_t* patch, const float (&v)[32]
         for (int r = 0; r < rows; ++r) to[r * ld + lane] = reinterpret_cast<const T*>(patch_chunk(patch, r, lane >> 3))[lane & 7];
 }
 
+// The other way: this lane's row of 32 columns, fetched by the lanes side by side.
+template <typename T>
+__device__ __forceinline__ void load_patch(uint8_t* patch, const T* from, long long ld, int rows, int left, bool vec, uint4 (&row)[4]) {
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");         // what was there is read
+    __syncwarp();
+    if (vec && left >= 32) {
+        uint4 u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i * 8 + (lane >> 2) < rows) u[i] = *reinterpret_cast<const uint4*>(from + (i * 8 + (lane >> 2)) * ld + (lane & 3) * 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i * 8 + (lane >> 2) < rows) *patch_chunk(patch, i * 8 + (lane >> 2), lane & 3) = u[i];
+    } else if ((ld & 1) == 0) {                                   // two elements a lane, two rows an access, all on their way at once
+        const int c = (lane & 15) * 2;
+        uint32_t u[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = 2 * i + (lane >> 4);
+            u[i] = 0u;
+            if (r < rows && c + 1 < left) u[i] = *reinterpret_cast<const uint32_t*>(from + r * ld + c);
+            else if (r < rows && c < left) *reinterpret_cast<T*>(&u[i]) = from[r * ld + c];
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = 2 * i + (lane >> 4);
+            reinterpret_cast<uint32_t*>(patch_chunk(patch, r, c >> 3))[(c & 7) >> 1] = u[i];
+        }
+    } else if (lane < left)
+#pragma unroll 16
+        for (int r = 0; r < rows; ++r) reinterpret_cast<T*>(patch_chunk(patch, r, lane >> 3))[lane & 7] = from[r * ld + lane];
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 4; ++c) row[c] = *patch_chunk(patch, lane, c);      // (columns and rows that do not exist: whatever is there)
+    __syncwarp();
+}
+
 // The sums of 32 columns of the warp's rows on their way out: row0 the warp's first row, rows how many it has.
 template <typename T, bool DW>
 __device__ __forceinline__ void finish_columns(const GroupedArgs& g, const GroupedTile& tile, uint8_t* patch, float (&v)[32], int row0, int rows, int col, int left, const CUtensorMap* map_y,
                                                const CUtensorMap* map_z) {
     const bool by_tma = g.tma && (DW || rows == 32);
-    const int lane = threadIdx.x & 31;
     T* y = static_cast<T*>(g.y) + (DW ? tile.expert * g.y_expert : 0) + (long long)row0 * g.ldy + col;
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] *= g.alpha;
@@ -181,12 +218,13 @@ __device__ __forceinline__ void finish_columns(const GroupedArgs& g, const Group
 #undef EBS_ACT_CASE
             default: break;
         }
-        if (g.residual && lane < rows) {
-            const T* r = static_cast<const T*>(g.residual) + (long long)(row0 + lane) * g.ldr + col;
+        if (g.residual) {
+            uint4 r[4];
+            load_patch(patch, static_cast<const T*>(g.residual) + (long long)row0 * g.ldr + col, g.ldr, rows, left, g.vec, r);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 float t[8];
-                unpack<T>(load_raw(r + 8 * c, left - 8 * c, g.vec && left >= 8 * c + 8), t);
+                unpack<T>(r[c], t);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[8 * c + i] += t[i];
             }
@@ -438,6 +476,7 @@ struct GroupedDz {
 template <typename T>
 __global__ void __launch_bounds__(256, 4) grouped_dz_kernel(const __grid_constant__ GroupedDz g) {
     __shared__ float sums[8][256 + 4];
+    __shared__ int owner[9];
     let_next_kernel_start();
     wait_for_previous_kernel();
     const int bx = (int)(blockIdx.x % (unsigned)g.across), chunk = (int)(blockIdx.x / (unsigned)g.across);
@@ -446,6 +485,23 @@ __global__ void __launch_bounds__(256, 4) grouped_dz_kernel(const __grid_constan
     const T *dy = static_cast<const T*>(g.dy) + col, *z = static_cast<const T*>(g.z) + col;
     T* dz = static_cast<T*>(g.dz) + col;
     const bool vec = g.vec && left >= 8;
+    // dz of one row's eight columns, out and left in v
+    auto row_dz = [&](const uint4& a, const uint4& b, int r, float (&v)[8]) {
+        float zv[8];
+        unpack<T>(a, v);
+        if (g.act) unpack<T>(b, zv);
+        switch (g.act) {
+#define EBS_SLOPE_CASE(A) case A: _Pragma("unroll") for (int i = 0; i < 8; ++i) v[i] *= activation_slope<true>(zv[i], A); break;
+            EBS_SLOPE_CASE(EBS_ACT_RELU) EBS_SLOPE_CASE(EBS_ACT_GELU) EBS_SLOPE_CASE(EBS_ACT_GELU_TANH) EBS_SLOPE_CASE(EBS_ACT_SILU)
+#undef EBS_SLOPE_CASE
+            default: break;
+        }
+        if (!g.dz) return;
+        float t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = v[i] * g.store;
+        store_pack(dz + r * g.lddz, t);                           // (its rows are padded to whole packs)
+    };
     auto part_of = [&](int e, int begin, int end) {
         const int r0 = max(begin, c0), r1 = min(end, c1);
         float sum[8] = {};
@@ -460,21 +516,10 @@ __global__ void __launch_bounds__(256, 4) grouped_dz_kernel(const __grid_constan
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 if (r + 8 * u >= r1) break;
-                float v[8], zv[8];
-                unpack<T>(a[u], v);
-                if (g.act) unpack<T>(b[u], zv);
-                switch (g.act) {
-#define EBS_SLOPE_CASE(A) case A: _Pragma("unroll") for (int i = 0; i < 8; ++i) v[i] *= activation_slope<true>(zv[i], A); break;
-                    EBS_SLOPE_CASE(EBS_ACT_RELU) EBS_SLOPE_CASE(EBS_ACT_GELU) EBS_SLOPE_CASE(EBS_ACT_GELU_TANH) EBS_SLOPE_CASE(EBS_ACT_SILU)
-#undef EBS_SLOPE_CASE
-                    default: break;
-                }
+                float v[8];
+                row_dz(a[u], b[u], r + 8 * u, v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[i] += v[i];
-                if (!g.dz) continue;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= g.store;
-                store_pack(dz + (r + 8 * u) * g.lddz, v);         // (its rows are padded to whole packs)
             }
         }
         if (!g.part) return;
@@ -489,6 +534,12 @@ __global__ void __launch_bounds__(256, 4) grouped_dz_kernel(const __grid_constan
             g.part[(long long)(chunk + e) * g.n + bx * 256 + threadIdx.x] = s;
         }
     };
+    // Chunks of eight rows, where experts have few: a warp a row, whoever's it is (one expert after another, 65 rows of 29 experts of 3060 columns took 33 us).
+    const bool by_row = g.chunk_rows == 8;
+    if (by_row) {
+        if (threadIdx.x < 9) owner[threadIdx.x] = -1;
+        __syncthreads();
+    }
     for (int e0 = 0; e0 < g.experts; e0 += 32) {
         int begin = 0, count = 0;
         if (e0 + lane < g.experts) expert_rows(g.offsets, g.m, e0 + lane, begin, count);
@@ -496,9 +547,34 @@ __global__ void __launch_bounds__(256, 4) grouped_dz_kernel(const __grid_constan
         while (hit) {                                             // (the same in every warp)
             const int l = __ffs(hit) - 1;
             hit &= hit - 1;
-            const int b = __shfl_sync(0xffffffffu, begin, l);
-            part_of(e0 + l, b, b + __shfl_sync(0xffffffffu, count, l));
+            const int b = __shfl_sync(0xffffffffu, begin, l), e = b + __shfl_sync(0xffffffffu, count, l);
+            if (!by_row) part_of(e0 + l, b, e);
+            else if (y == 0 && lane < 8 && c0 + lane >= b && c0 + lane < min(e, c1)) owner[lane] = e0 + l;
         }
+    }
+    if (!by_row) return;
+    __syncthreads();
+    float v[8] = {};
+    if (owner[y] >= 0 && left > 0) {
+        const int r = c0 + y;
+        const uint4 a = load_raw(dy + r * g.ldy, left, vec);
+        uint4 b = make_uint4(0u, 0u, 0u, 0u);
+        if (g.act) b = load_raw(z + r * g.ldz, left, vec);
+        row_dz(a, b, r, v);
+    }
+    if (!g.part) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[y][lane * 8 + i] = v[i];
+    __syncthreads();
+    if (bx * 256 + (int)threadIdx.x >= g.n) return;
+    float s = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        if (owner[q] < 0) continue;
+        s += sums[q][threadIdx.x];
+        if (owner[q + 1] == owner[q]) continue;
+        g.part[(long long)(chunk + owner[q]) * g.n + bx * 256 + threadIdx.x] = s;
+        s = 0.0f;
     }
 }
 // dbias: an expert's chunks in their order, eight warps every eighth.
@@ -555,12 +631,28 @@ static int launch_grouped(const CUtensorMap (&map)[4], const GroupedArgs& g, lon
     const long long at_once = (long long)gemm_sm_count() * Form::BLOCKS / cluster;
     return launch_chained(kern, dim3((unsigned)(cluster * (tiles < at_once ? tiles : at_once))), Form::THREADS, (size_t)SMEM, st, cluster, map[0], map[1], map[2], map[3], g);
 }
-// Columns of a tile; rows_of_pair, rows_of_block: how many times 256 and 128 rows there are to cover.  Pairs where there is a tile for each of them (a tile of 256 x 256
-// a pair takes less than 128 x 128 a block each), else tiles for every SM, else the narrowest ones.
-static int grouped_columns(long long rows_of_pair, long long rows_of_block, int cols) {
-    const int sms = gemm_sm_count();
-    if (rows_of_pair * ((cols + 255) / 256) >= sms / 2) return 256;
-    return rows_of_block * ((cols + 127) / 128) >= sms ? 128 : 64;
+// Tiles of `tile` rows there can be at most: one more than whole ones for each expert that has rows; and how many there are where all have the same number.
+static long long most_row_tiles(int m, int experts, int tile) { return m / tile + (experts < m ? experts : m); }
+static long long expected_row_tiles(int m, int experts, int tile) {
+    const long long e = experts < m ? experts : m;
+    return e * ((m / e + tile - 1) / tile);
+}
+// The form that ends first.  us a stage of 64 terms: of a tile alone on its SM (or pair), and of an SM's where two share it; and for a tile's results.  row_tiles(rows): tiles of that many.
+// FEW_ROWS where experts have few (it is bound by the weights' bytes then), or where the others leave SMs without a tile.
+template <class F>
+static int grouped_form(const F& row_tiles, int cols, long long stages, bool weights, bool few_rows) {
+    struct { int form, rows, cols, blocks; float stage, shared; } const forms[] = {
+        {256, 256, 256, 74, 0.30f, 0.30f}, {128, 128, 128, 148, 0.16f, 0.16f}, {64, 128, 64, 296, 0.13f, 0.24f}, {FEW_ROWS, FEW_ROWS, 64, 296, 0.12f, 0.24f}};
+    if (few_rows) return FEW_ROWS;
+    int best = 64;
+    float least = 0.0f;
+    for (const auto& f : forms) {
+        const long long tiles = row_tiles(f.rows) * ((cols + f.cols - 1) / f.cols);
+        if (f.form == FEW_ROWS && (weights || tiles > 148)) continue;
+        const float time = (float)((tiles + f.blocks - 1) / f.blocks) * ((float)stages * (tiles > 148 ? f.shared : f.stage) + 1.5f);
+        if (least == 0.0f || time < least) { least = time; best = f.form; }
+    }
+    return best;
 }
 // row_tiles: of the form that was chosen.
 template <typename T, bool DW>
@@ -586,13 +678,6 @@ static int launch_form(int form, const GemmOperand& a, int a_mn, int a_red, cons
         default: return chunks ? launch_grouped<T, 64, DW, true>(map, g, tiles, st) : launch_grouped<T, 64, DW, false>(map, g, tiles, st);
     }
 }
-// Tiles of `tile` rows there can be at most: one more than whole ones for each expert that has rows; and how many there are where all have the same number.
-static long long most_row_tiles(int m, int experts, int tile) { return m / tile + (experts < m ? experts : m); }
-static long long expected_row_tiles(int m, int experts, int tile) {
-    const long long e = experts < m ? experts : m;
-    return e * ((m / e + tile - 1) / tile);
-}
-
 struct GroupedTensors {
     const void *x, *w, *bias, *residual, *dy, *z;
     void *y, *keep, *dx, *dw, *dbias;
@@ -608,8 +693,8 @@ static int rows_product(const GroupedTensors& t, int m, int experts, int cols, i
     g.b_mn = b_mn;
     GemmOperand A(a.p, a.ld, false), B(w.p, w.ld, b_mn, 1, 0, w.expert);
     const bool chunks = red > GEMM_LONG * GEMM_BK;
-    // few rows an expert: bound by the bytes of the weights
-    const int form = m <= FEW_ROWS * (long long)(experts < m ? experts : m) ? FEW_ROWS : grouped_columns(expected_row_tiles(m, experts, 256), expected_row_tiles(m, experts, 128), cols);
+    const int form = grouped_form([&](int rows) { return expected_row_tiles(m, experts, rows); }, cols, (red + GEMM_BK - 1) / GEMM_BK, false,
+                                  m <= FEW_ROWS * (long long)(experts < m ? experts : m));
     return launch_form<T, false>(form, A, m, red, B, cols, red, experts, g, most_row_tiles(m, experts, form == 256 ? 256 : form == FEW_ROWS ? FEW_ROWS : 128), chunks, st);
 }
 static bool rows_ok(const void* p, long long ld) { return !p || (ld & 7) == 0; }
@@ -652,8 +737,8 @@ static int grouped_backward(const ebs_linear_desc& d, int experts, const Grouped
     GroupedOperand w = plan_rows(t.dx || !run ? t.w : nullptr, (long long)experts * d.n, d.k, d.ldw, ws, &copies);
     w.expert = d.n * w.ld;
     const int across = (d.n + 255) / 256;
-    const long long want = (8LL * 148 + across - 1) / across;        // about eight blocks an SM, at least 32 rows each
-    const int chunk_rows = (int)((d.m + want - 1) / want > 32 ? (d.m + want - 1) / want : 32), chunks = (d.m + chunk_rows - 1) / chunk_rows;
+    const long long want = (8LL * 148 + across - 1) / across, share = (d.m + want - 1) / want;        // about eight blocks an SM, at least 32 rows each, or eight
+    const int chunk_rows = d.m < 32LL * experts && share <= 8 ? 8 : (int)(share > 32 ? share : 32), chunks = (d.m + chunk_rows - 1) / chunk_rows;
     float* part = ws.take<float>(((size_t)chunks + experts) * d.n);
     if (!run) return EBS_OK;
     int rc;
@@ -687,11 +772,11 @@ static int grouped_backward(const ebs_linear_desc& d, int experts, const Grouped
         g.y_expert = d.n * d.ldw;
         g.alpha = 1.0f / dz_store_scale(d);
         g.vec = rows_ok(t.dw, d.ldw);
-        const long long pairs = (long long)experts * ((d.n + 255) / 256), blocks = (long long)experts * ((d.n + 127) / 128);
-        const int tn = grouped_columns(pairs, blocks, d.k);
+        const auto row_tiles = [&](int rows) { return (long long)experts * ((d.n + rows - 1) / rows); };
+        const int form = grouped_form(row_tiles, d.k, ((d.m + experts - 1) / experts + GEMM_BK - 1) / GEMM_BK, true, false);
         GemmOperand A(dz.p, dz.ld, true), B(x.p, x.ld, true);
         const bool chunks = d.m > GEMM_LONG * GEMM_BK;
-        if ((rc = launch_form<T, true>(tn, A, d.n, d.m, B, d.k, d.m, 1, g, tn == 256 ? pairs : blocks, chunks, st))) return rc;
+        if ((rc = launch_form<T, true>(form, A, d.n, d.m, B, d.k, d.m, 1, g, row_tiles(form == 256 ? 256 : 128), chunks, st))) return rc;
     }
     return EBS_OK;
 }
