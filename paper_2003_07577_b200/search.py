@@ -91,3 +91,24 @@ class SearchLinear:
         self.weight.sub_(self.update, alpha=rate)
         if self.bias is not None:
             self.bias.sub_(self.dbias, alpha=rate)
+
+
+class GradientClip:
+    """Clips the gradients that layers (SearchLinear, ExpertLinear: their dw and dbias) keep between backward() and step(), in place and together: by the norm over all
+    of them.  The work list is laid out once for the layers' buffers; a call can be captured with the step around it."""
+
+    def __init__(self, layers):
+        grads = [g for layer in layers for g in (layer.dw, layer.dbias) if g is not None]
+        if not grads:
+            raise ValueError("no layer")
+        self.device = grads[0].device
+        with torch.cuda.device(self.device):
+            self.plan = ebs.clip_plan(grads)
+        self.norm = torch.zeros(1, dtype=torch.float32, device=self.device)
+        self._workspace = torch.empty(ebs.ebs_clip_workspace_bytes(self.plan), dtype=torch.uint8, device=self.device)
+
+    def __call__(self, max_norm: float) -> torch.Tensor:
+        """The norm before clipping, fp32 [1]; stays valid until the next call."""
+        with torch.cuda.device(self.device):
+            ebs.ebs_clip_gradients(self.plan, max_norm, self.norm, self._workspace)
+        return self.norm
