@@ -32,7 +32,7 @@ struct GroupedArgs {
     int test_flags;
 };
 
-// The forms: 256 a pair's 256 x 256 results, 128 and 64 so many columns of 128 rows, one and two blocks an SM, FEW_ROWS 64 columns of 32 rows, two blocks an SM with seven stages of
+// The forms: 256 a pair's 256 x 256 results, 128 and 64 so many columns of 128 rows, one and two blocks an SM, FEW_ROWS 64 columns of 32 rows, two blocks an SM with eight stages of
 // little more than the weights.  (The tensor core still takes 128 rows: those behind the 32 are whatever lies there, and so are the lanes of sums that nobody reads.)
 constexpr int FEW_ROWS = 32;
 template <int F> struct GroupedForm {
@@ -40,10 +40,11 @@ template <int F> struct GroupedForm {
     static constexpr int TN = F == FEW_ROWS ? 64 : F;
     static constexpr int A_ROWS = F == FEW_ROWS ? 32 : 128, B_COLS = PAIR ? TN / 2 : TN;             // rows of A and columns of B that a block fetches
     static constexpr int EPI_WARPS = PAIR ? 16 : 8, THREADS = PAIR ? 640 : 320;        // (pair: whole warpgroups, whose registers are dealt anew)
-    static constexpr int STAGES = F == FEW_ROWS ? 7 : F == 64 ? 3 : 6, A_BYTES = A_ROWS * GEMM_ROW_BYTES, STAGE = A_BYTES + B_COLS * GEMM_ROW_BYTES;
+    static constexpr int STAGES = F == FEW_ROWS ? 8 : F == 64 ? 4 : 6, A_BYTES = A_ROWS * GEMM_ROW_BYTES, STAGE = A_BYTES + B_COLS * GEMM_ROW_BYTES;
     static constexpr int CQ = TN / (EPI_WARPS / 4);               // columns of a warp
     static constexpr int PATCH = 32 * 64;                         // 32 rows of 64 bytes
-    static constexpr int SMEM = STAGES * STAGE + EPI_WARPS * PATCH + 1024, BLOCKS = TN == 64 ? 2 : 1;
+    static constexpr int BARRIERS = 256;
+    static constexpr int SMEM = STAGES * STAGE + EPI_WARPS * PATCH + BARRIERS, BLOCKS = TN == 64 ? 2 : 1;
     static constexpr int ROWS = PAIR ? 256 : A_ROWS;              // rows of a tile
     static_assert(B_COLS * GEMM_ROW_BYTES + EPI_WARPS * PATCH >= (128 - A_ROWS) * GEMM_ROW_BYTES, "what the tensor core reads behind the last stage's rows is this block's memory");
 };
@@ -183,9 +184,15 @@ __device__ __forceinline__ void load_patch(uint8_t* patch, const T* from, long l
             const int r = 2 * i + (lane >> 4);
             reinterpret_cast<uint32_t*>(patch_chunk(patch, r, c >> 3))[(c & 7) >> 1] = u[i];
         }
-    } else if (lane < left)
-#pragma unroll 16
-        for (int r = 0; r < rows; ++r) reinterpret_cast<T*>(patch_chunk(patch, r, lane >> 3))[lane & 7] = from[r * ld + lane];
+    } else
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+            T u[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) u[i] = h + i < rows && lane < left ? from[(h + i) * ld + lane] : from_f32<T>(0.0f);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) reinterpret_cast<T*>(patch_chunk(patch, h + i, lane >> 3))[lane & 7] = u[i];
+        }
     __syncwarp();
 #pragma unroll
     for (int c = 0; c < 4; ++c) row[c] = *patch_chunk(patch, lane, c);      // (columns and rows that do not exist: whatever is there)
@@ -238,15 +245,16 @@ template <typename T, int F, bool DW, bool CHUNKS>
 __global__ void __launch_bounds__(GroupedForm<F>::THREADS, GroupedForm<F>::BLOCKS) grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                                                               const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z,
                                                                                               const __grid_constant__ GroupedArgs g) {
-    extern __shared__ uint8_t smem_raw[];
+    extern __shared__ __align__(1024) uint8_t tiles[];            // (nothing static: two blocks' stages take an SM's memory but for a KB)
     using Form = GroupedForm<F>;
     constexpr bool PAIR = Form::PAIR;
     constexpr int TN = Form::TN, S = Form::STAGES, STAGE = Form::STAGE, A_BYTES = Form::A_BYTES, CQ = Form::CQ, EPI = Form::EPI_WARPS;
     static_assert(!DW || Form::A_ROWS == 128, "rows of a weight gradient are its lanes");
-    __shared__ uint64_t full[S], empty[S], acc_full[2], acc_empty[2], ready[S];
-    __shared__ uint32_t tmem_slot;
-    __shared__ volatile int abort_flag;
-    uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t* full = reinterpret_cast<uint64_t*>(tiles + S * STAGE + EPI * Form::PATCH);
+    uint64_t *empty = full + S, *ready = empty + S, *acc_full = ready + S, *acc_empty = acc_full + 2;
+    uint32_t& tmem_slot = *reinterpret_cast<uint32_t*>(acc_empty + 2);
+    volatile int& abort_flag = *reinterpret_cast<volatile int*>(acc_empty + 3);
+    static_assert((3 * S + 4 + 2) * 8 <= Form::BARRIERS, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)(blockIdx.x & 1) : 0, step = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x, start = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
     if (warp >= EPI && warp < EPI + 2 && lane == 0) asm volatile("prefetch.tensormap [%0];\n" ::"l"(warp == EPI ? &map_a : &map_b) : "memory");
@@ -619,7 +627,7 @@ static int launch_grouped(const CUtensorMap (&map)[4], const GroupedArgs& g, lon
     using Form = GroupedForm<F>;
     auto kern = grouped_kernel<T, F, DW, CHUNKS>;
     constexpr int SMEM = Form::SMEM;
-    static_assert(Form::BLOCKS * (SMEM + 512 + 1024) <= 228 * 1024, "shared memory of an SM: the blocks', what is static in them, and 1 KB that each takes besides");
+    static_assert(Form::BLOCKS * (SMEM + 1024) <= 228 * 1024 && SMEM <= 227 * 1024, "shared memory of an SM: the blocks' and 1 KB that each takes besides");
     static bool attr_set[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
@@ -642,13 +650,13 @@ static long long expected_row_tiles(int m, int experts, int tile) {
 template <class F>
 static int grouped_form(const F& row_tiles, int cols, long long stages, bool weights, bool few_rows) {
     struct { int form, rows, cols, blocks; float stage, shared; } const forms[] = {
-        {256, 256, 256, 74, 0.30f, 0.30f}, {128, 128, 128, 148, 0.16f, 0.16f}, {64, 128, 64, 296, 0.13f, 0.24f}, {FEW_ROWS, FEW_ROWS, 64, 296, 0.12f, 0.24f}};
+        {256, 256, 256, 74, 0.30f, 0.30f}, {128, 128, 128, 148, 0.18f, 0.18f}, {64, 128, 64, 296, 0.26f, 0.30f}, {FEW_ROWS, FEW_ROWS, 64, 296, 0.14f, 0.24f}};
     if (few_rows) return FEW_ROWS;
     int best = 64;
     float least = 0.0f;
     for (const auto& f : forms) {
         const long long tiles = row_tiles(f.rows) * ((cols + f.cols - 1) / f.cols);
-        if (f.form == FEW_ROWS && (weights || tiles > 148)) continue;
+        if (f.form == FEW_ROWS && (weights || tiles > 296)) continue;
         const float time = (float)((tiles + f.blocks - 1) / f.blocks) * ((float)stages * (tiles > 148 ? f.shared : f.stage) + 1.5f);
         if (least == 0.0f || time < least) { least = time; best = f.form; }
     }
@@ -738,7 +746,7 @@ static int grouped_backward(const ebs_linear_desc& d, int experts, const Grouped
     w.expert = d.n * w.ld;
     const int across = (d.n + 255) / 256;
     const long long want = (8LL * 148 + across - 1) / across, share = (d.m + want - 1) / want;        // about eight blocks an SM, at least 32 rows each, or eight
-    const int chunk_rows = d.m < 32LL * experts && share <= 8 ? 8 : (int)(share > 32 ? share : 32), chunks = (d.m + chunk_rows - 1) / chunk_rows;
+    const int chunk_rows = share <= 8 && (d.m < 32LL * experts || (d.m + 31) / 32 * across < 148) ? 8 : (int)(share > 32 ? share : 32), chunks = (d.m + chunk_rows - 1) / chunk_rows;
     float* part = ws.take<float>(((size_t)chunks + experts) * d.n);
     if (!run) return EBS_OK;
     int rc;
