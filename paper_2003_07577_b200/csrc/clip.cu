@@ -19,11 +19,11 @@ namespace ebs {
 constexpr int CLIP_BLOCKS = 148 * 4;        // at most: a wave of blocks of 256 threads
 constexpr int CLIP_THREADS = 256;
 constexpr int CLIP_UNROLL = 8;              // packs of a thread under way: 32 KB a block (four, and records loaded when they are needed: 1.07 GB read at 3.4 TB/s)
-constexpr int CLIP_NARROW = 512;            // bytes of a row that a warp's lanes would not fill: the block takes the rows' elements one by one
+constexpr int CLIP_NARROW = 512;            // bytes of a row that a warp's lanes would not fill
 // Bytes of a chunk of one row: as many as the block has under way; a network of a few MB is cut finer, so that every SM has some.
 constexpr long long CLIP_CHUNK = CLIP_THREADS * 16 * CLIP_UNROLL, CLIP_CHUNK_SMALL = CLIP_THREADS * 16, CLIP_SMALL = 8 << 20;
 
-// rows = 1: the block's threads share the row; more: a warp takes a row.
+// rows = 1: the block's threads share the row; more: a warp takes a row, or, of narrow rows, the threads their pieces of 16 bytes.
 struct alignas(16) ClipChunk {
     const void* in;
     void* out;
@@ -110,24 +110,56 @@ __device__ __forceinline__ void row_squares(const T* p, int cols, int t, int ste
         add_square(last, sum);
     }
 }
+// Several rows that start anywhere, as the 16-byte pieces of memory that they lie in: piece `at` of all is one of a row's `pieces` (as many as its elements can touch); its
+// first element is element `start` of the row, which may lie before the row's first one.  (23 layers of 1792 x 64 and 64 x 1792 bf16, rows of 65 and 1793: an element a thread 44 us, so 31.  Wide rows
+// not: pieces at their ends cost more than lanes without work, 73 MB of padded fp16 rows 85 us instead of 46.)
+template <typename T>
+struct Piece {
+    const T* row;
+    int r, start;
+};
+template <typename T> __device__ __forceinline__ unsigned pieces_of(int cols) { return (unsigned)(cols + 2 * Pack<T>::N - 2) / (unsigned)Pack<T>::N; }
+template <typename T>
+__device__ __forceinline__ Piece<T> piece_at(const ClipChunk& c, unsigned pieces, unsigned at) {
+    Piece<T> q;
+    q.r = (int)(at / pieces);
+    q.row = static_cast<const T*>(c.in) + q.r * c.ld_in;
+    q.start = (int)(at - (unsigned)q.r * pieces) * Pack<T>::N - (int)((unsigned)(uintptr_t)q.row & 15u) / (int)sizeof(T);
+    return q;
+}
+// Zero where there is no element of the row.
+template <typename T>
+__device__ __forceinline__ uint4 load_piece(const Piece<T>& q, int cols) {
+    constexpr int N = Pack<T>::N;
+    if (q.start >= 0 && q.start + N <= cols) return *reinterpret_cast<const uint4*>(q.row + q.start);
+    uint4 u = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (q.start + e >= 0 && q.start + e < cols) reinterpret_cast<T*>(&u)[e] = q.row[q.start + e];
+    return u;
+}
+template <typename T>
+__device__ __forceinline__ void rows_squares(const ClipChunk& c, double& sum) {
+    const unsigned pieces = pieces_of<T>(c.cols), all = (unsigned)c.rows * pieces;
+    for (unsigned i = threadIdx.x; i < all; i += CLIP_UNROLL * CLIP_THREADS) {
+        uint4 u[CLIP_UNROLL];
+#pragma unroll
+        for (unsigned j = 0; j < CLIP_UNROLL; ++j) u[j] = i + j * CLIP_THREADS < all ? load_piece(piece_at<T>(c, pieces, i + j * CLIP_THREADS), c.cols) : make_uint4(0u, 0u, 0u, 0u);
+        unsigned left_out = 0u;
+#pragma unroll
+        for (int j = 0; j < CLIP_UNROLL; ++j) left_out |= (add_squares<T>(u[j], sum) ? 0u : 1u) << j;
+        if (left_out)
+#pragma unroll 1
+            for (unsigned j = 0; j < CLIP_UNROLL; ++j)
+                if (left_out >> j & 1u) sum += squares_of<T>(load_piece(piece_at<T>(c, pieces, i + j * CLIP_THREADS), c.cols));
+    }
+}
 template <typename T>
 __device__ __forceinline__ void chunk_squares(const ClipChunk& c, double& sum) {
-    const T* p = static_cast<const T*>(c.in);
-    if (c.rows == 1) row_squares(p, c.cols, threadIdx.x, CLIP_THREADS, sum);
-    else if (c.cols * (int)sizeof(T) < CLIP_NARROW) {
-        const unsigned cols = (unsigned)c.cols, all = (unsigned)c.rows * cols;
-        for (unsigned i = threadIdx.x; i < all; i += CLIP_UNROLL * CLIP_THREADS) {
-            T v[CLIP_UNROLL];
-#pragma unroll
-            for (unsigned j = 0; j < CLIP_UNROLL; ++j) {
-                const unsigned at = i + j * CLIP_THREADS;
-                v[j] = at < all ? p[at / cols * c.ld_in + at % cols] : from_f32<T>(0.0f);
-            }
-#pragma unroll
-            for (int j = 0; j < CLIP_UNROLL; ++j) add_square(v[j], sum);
-        }
-    } else
-        for (int r = threadIdx.x >> 5; r < c.rows; r += CLIP_THREADS / 32) row_squares(p + r * c.ld_in, c.cols, threadIdx.x & 31, 32, sum);
+    if (c.rows == 1) row_squares(static_cast<const T*>(c.in), c.cols, threadIdx.x, CLIP_THREADS, sum);
+    else if (c.cols * (int)sizeof(T) < CLIP_NARROW) rows_squares<T>(c, sum);
+    else
+        for (int r = threadIdx.x >> 5; r < c.rows; r += CLIP_THREADS / 32) row_squares(static_cast<const T*>(c.in) + r * c.ld_in, c.cols, threadIdx.x & 31, 32, sum);
 }
 __device__ __forceinline__ double block_sum(double v) {
     __shared__ double part[CLIP_THREADS / 32];
@@ -197,27 +229,35 @@ __device__ __forceinline__ void row_scale(const T* p, T* to, int cols, int t, in
     if (tail + t < cols) to[tail + t] = from_f32<T>(to_f32(p[tail + t]) * f);
 }
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const ClipChunk& c, float f) {
-    const T* p = static_cast<const T*>(c.in);
-    T* to = static_cast<T*>(c.out);
-    if (c.rows == 1) row_scale(p, to, c.cols, threadIdx.x, CLIP_THREADS, f);
-    else if (c.cols * (int)sizeof(T) < CLIP_NARROW) {
-        const unsigned cols = (unsigned)c.cols, all = (unsigned)c.rows * cols;
-        for (unsigned i = threadIdx.x; i < all; i += CLIP_UNROLL * CLIP_THREADS) {
-            T v[CLIP_UNROLL];
+__device__ __forceinline__ void rows_scale(const ClipChunk& c, float f) {
+    constexpr int N = Pack<T>::N, U = CLIP_UNROLL / 2;
+    const unsigned pieces = pieces_of<T>(c.cols), all = (unsigned)c.rows * pieces;
+    for (unsigned i = threadIdx.x; i < all; i += U * CLIP_THREADS) {
+        uint4 u[U];
 #pragma unroll
-            for (unsigned j = 0; j < CLIP_UNROLL; ++j) {
-                const unsigned at = i + j * CLIP_THREADS;
-                if (at < all) v[j] = p[at / cols * c.ld_in + at % cols];
-            }
+        for (unsigned j = 0; j < U; ++j)
+            if (i + j * CLIP_THREADS < all) u[j] = load_piece(piece_at<T>(c, pieces, i + j * CLIP_THREADS), c.cols);
 #pragma unroll
-            for (unsigned j = 0; j < CLIP_UNROLL; ++j) {
-                const unsigned at = i + j * CLIP_THREADS;
-                if (at < all) to[at / cols * c.ld_out + at % cols] = from_f32<T>(to_f32(v[j]) * f);
-            }
+        for (unsigned j = 0; j < U; ++j) {
+            if (i + j * CLIP_THREADS >= all) break;
+            const Piece<T> q = piece_at<T>(c, pieces, i + j * CLIP_THREADS);
+            T* to = static_cast<T*>(c.out) + q.r * c.ld_out;
+            scale_pack<T>(u[j], f);
+            if (q.start >= 0 && q.start + N <= c.cols && (((uintptr_t)(to + q.start)) & 15u) == 0) *reinterpret_cast<uint4*>(to + q.start) = u[j];
+            else
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (q.start + e >= 0 && q.start + e < c.cols) to[q.start + e] = reinterpret_cast<const T*>(&u[j])[e];
         }
-    } else
-        for (int r = threadIdx.x >> 5; r < c.rows; r += CLIP_THREADS / 32) row_scale(p + r * c.ld_in, to + r * c.ld_out, c.cols, threadIdx.x & 31, 32, f);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void chunk_scale(const ClipChunk& c, float f) {
+    if (c.rows == 1) row_scale(static_cast<const T*>(c.in), static_cast<T*>(c.out), c.cols, threadIdx.x, CLIP_THREADS, f);
+    else if (c.cols * (int)sizeof(T) < CLIP_NARROW) rows_scale<T>(c, f);
+    else
+        for (int r = threadIdx.x >> 5; r < c.rows; r += CLIP_THREADS / 32)
+            row_scale(static_cast<const T*>(c.in) + r * c.ld_in, static_cast<T*>(c.out) + r * c.ld_out, c.cols, threadIdx.x & 31, 32, f);
 }
 
 __global__ void __launch_bounds__(CLIP_THREADS, 4) clip_scale_kernel(const ClipChunk* __restrict__ chunks, long long count, const double* __restrict__ partial, int parts,
@@ -266,7 +306,7 @@ static int complete_tensor(const ebs_clip_tensor& in, ebs_clip_tensor* t) {
     }
     return EBS_OK;
 }
-// How a tensor is cut: rows that a chunk takes (a warp each, whole eights), or pieces of one row for the whole block.
+// How a tensor is cut: whole rows, eights of them where a warp takes one, or pieces of one.
 struct Cut {
     long long rows, cols;
 };
