@@ -1,6 +1,6 @@
 // Norm of all gradients of a network and their clipping.  See include/ebs.h.
 //
-// Bound by the bytes: one pass reads every gradient for the sum of squares, one reads it again and writes it.  The work list ("plan") cuts all
+// Bound by the bytes: one pass reads every gradient for the sum of squares, one reads it again and writes it (537 million bf16: 154 us, 7.0 TB/s, and 333 us, 6.4 TB/s).  The work list ("plan") cuts all
 // tensors into chunks, a record each, so that a block learns from one 48-byte load what to do next, however many tensors there are and whatever their
 // sizes; the next record is on its way while a chunk is read.  The second pass takes the chunks from the last to the first: what the first pass read last is still in
 // the second-level cache.
