@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4
         for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) word[b][i] = 0x88888888u;
-#pragma unroll
+#pragma unroll 1
         for (int half = 0; half < 2; ++half) {                    // rows gid and gid + 8
             const int row = row0 + gid + 8 * half;
             const S* p = g.w + (expert * g.n + row) * g.ldw;
@@ -620,8 +620,10 @@ static Q4Route q4_route(const ebs_linear_desc& d, const ebs_q4_desc& q) {
     r.prepared = d.dtype == EBS_F32 && r.blocks * kbs >= 8192;
     r.copied = !r.prepared && d.m > 1 && d.ldx * (long long)element_size(d.dtype) % 16 != 0;
 // (14336 -> 4096: 15.6 us with 8 warps a tile, of which two blocks an SM have work, 9.9 with 16)
-    // Short reductions: two, whose blocks are many at a time (58 experts of 64 -> 8435 fp32, nine rows: 36 us with eight).
-    r.warps = r.nt == 1 && r.blocks < 148 * 3 && kbs >= 32 ? 16 : r.nt <= 2 && kbs <= 4 ? 2 : 8;
+    // Short reductions: two, whose blocks are many at a time (58 experts of 64 -> 8435 fp32, nine rows: 36 us with eight, 14 with two).  Four where their blocks fill the SMs
+    // (12 rows of two experts of 3392 -> 23270 38 us with eight, 29 with four; 4096 -> 14336, three quarters of a round, 9.6 and 10.9).
+    const int four = r.nt == 1 && d.dtype != EBS_F32 ? 148 * 8 : 148 * 4;
+    r.warps = r.nt == 1 && r.blocks < 148 * 3 && kbs >= 32 ? 16 : r.nt > 2 ? 8 : kbs <= 4 ? 2 : r.blocks >= four ? 4 : 8;
     r.workspace = r.prepared ? round256((size_t)d.m * kbs * Q4_K * 3 * 2) : r.copied ? round256((size_t)d.m * round8(d.k) * element_size(d.dtype)) : 0;
     return r;
 }
@@ -649,8 +651,19 @@ static int launch_q4_rows(Q4Args& g, const Q4Route& r, int group, cudaStream_t s
     if (r.blocks > 0x7fffffffLL) return EBS_ERR_OVERFLOW;
     g.slots = (int)r.pieces;
     switch (r.nt) {
-        case 1: return r.warps == 16 ? launch_q4_group<T, PREPARED, 1, 16>(g, r, group, st) : r.warps == 2 ? launch_q4_group<T, PREPARED, 1, 2>(g, r, group, st) : launch_q4_group<T, PREPARED, 1>(g, r, group, st);
-        case 2: return r.warps == 2 ? launch_q4_group<T, PREPARED, 2, 2>(g, r, group, st) : launch_q4_group<T, PREPARED, 2>(g, r, group, st);
+        case 1:
+            switch (r.warps) {
+                case 16: return launch_q4_group<T, PREPARED, 1, 16>(g, r, group, st);
+                case 2: return launch_q4_group<T, PREPARED, 1, 2>(g, r, group, st);
+                case 4: return launch_q4_group<T, PREPARED, 1, 4>(g, r, group, st);
+                default: return launch_q4_group<T, PREPARED, 1>(g, r, group, st);
+            }
+        case 2:
+            switch (r.warps) {
+                case 2: return launch_q4_group<T, PREPARED, 2, 2>(g, r, group, st);
+                case 4: return launch_q4_group<T, PREPARED, 2, 4>(g, r, group, st);
+                default: return launch_q4_group<T, PREPARED, 2>(g, r, group, st);
+            }
         case 4: return launch_q4_group<T, PREPARED, 4>(g, r, group, st);
         default:
             if constexpr (sizeof(T) == 2) return launch_q4_group<T, PREPARED, 8>(g, r, group, st);
