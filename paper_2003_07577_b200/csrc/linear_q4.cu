@@ -91,21 +91,21 @@ struct Q4Pack {
     void* scales;
     long long ldw;
     unsigned units;                        // warps' pieces of work
-    int n, k, tiles, kbs, groups, vec;
+    int n, k, tiles, kbs, groups;
 };
 // Eight rows of a piece of weights as the lanes of a warp have them, for matrices whose rows start anywhere: in memory the lanes take neighbouring elements, here their own eight (an element
 // a lane in 32 places of memory takes 32 accesses: 4.6 million weights of rows of 198 fp16 values packed and read back in 36 us).
 template <typename S, int COLS> struct Q4Stage { S row[8][COLS + 16 / sizeof(S)]; };
 
 // A warp packs 16 rows x KB tiles of 64 inputs, which hold whole groups of G: the largest magnitudes, scales and codes from one load.
-template <typename S, typename T, int G>
+template <typename S, typename T, int G, bool VEC>
 __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4Pack<S> g) {
     constexpr int KB = G == 128 ? 2 : 1;
     let_next_kernel_start();
     wait_for_previous_kernel();
-    __shared__ __align__(16) Q4Stage<S, KB * Q4_K> stages[8];
+    __shared__ __align__(16) Q4Stage<S, KB * Q4_K> stages[VEC ? 1 : 8];
     const int lane = threadIdx.x & 31, gid = lane >> 2;
-    Q4Stage<S, KB * Q4_K>& stage = stages[threadIdx.x >> 5];
+    Q4Stage<S, KB * Q4_K>& stage = stages[VEC ? 0 : threadIdx.x >> 5];
     const unsigned across = (unsigned)((g.kbs + KB - 1) / KB);
     for (unsigned u = blockIdx.x * 8u + (threadIdx.x >> 5); u < g.units; u += gridDim.x * 8u) {
         const long long tile = u / across;                        // of all experts
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4
             const S* p = g.w + (expert * g.n + row) * g.ldw;
             float v[KB][2][8];
             unsigned top[KB][2];
-            if (!g.vec) {
+            if (!VEC) {
                 __syncwarp();                                     // (what was there is read)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const int c = b * Q4_K + q4_input(r, lane, 0), left = g.k - kb0 * Q4_K - c;
-                    if (g.vec) load8<S>(p + kb0 * Q4_K + c, row < g.n ? left : 0, true, v[b][r]);
+                    if (VEC) load8<S>(p + kb0 * Q4_K + c, row < g.n ? left : 0, true, v[b][r]);
                     else load8<S>(&stage.row[gid][c], 8, true, v[b][r]);
                 }
 #pragma unroll
@@ -196,16 +196,16 @@ struct Q4Unpack {
     D* w;
     long long ldw;
     unsigned units;
-    int n, k, tiles, kbs, groups, group, vec;
+    int n, k, tiles, kbs, groups, shift;       // groups of 2^shift inputs
 };
-template <typename T, typename D>
+template <typename T, typename D, bool VEC>
 __global__ void __launch_bounds__(256) q4_unpack_kernel(const __grid_constant__ Q4Unpack<D> g) {
-    __shared__ __align__(16) Q4Stage<D, Q4_K> stages[8];
+    __shared__ __align__(16) Q4Stage<D, Q4_K> stages[VEC ? 1 : 8];
     let_next_kernel_start();
     wait_for_previous_kernel();
     constexpr int N = Pack<D>::N;
     const int lane = threadIdx.x & 31, gid = lane >> 2;
-    Q4Stage<D, Q4_K>& stage = stages[threadIdx.x >> 5];
+    Q4Stage<D, Q4_K>& stage = stages[VEC ? 0 : threadIdx.x >> 5];
     for (unsigned u = blockIdx.x * 8u + (threadIdx.x >> 5); u < g.units; u += gridDim.x * 8u) {
         const long long tile = u / (unsigned)g.kbs, expert = (unsigned)tile / (unsigned)g.tiles;
         const int kb = (int)(u % (unsigned)g.kbs), row0 = (int)((unsigned)tile % (unsigned)g.tiles) * Q4_ROWS;
@@ -213,14 +213,14 @@ __global__ void __launch_bounds__(256) q4_unpack_kernel(const __grid_constant__ 
         const uint32_t word[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            if (!g.vec) __syncwarp();                             // (what was there is read)
+            if (!VEC) __syncwarp();                             // (what was there is read)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const int row = row0 + gid + 8 * half, c = kb * Q4_K + q4_input(r, lane, 0);
                 if (row >= g.n || c >= g.k) continue;
-                const float s = to_f32(static_cast<const T*>(g.scales)[(tile * g.groups + (kb * Q4_K + r * 32) / g.group) * Q4_ROWS + 2 * gid + half]);
-                D* to = g.vec ? g.w + (expert * g.n + row) * g.ldw + c : &stage.row[gid][c - kb * Q4_K];
-                const int left = g.vec ? g.k - c : 8;
+                const float s = to_f32(static_cast<const T*>(g.scales)[(tile * g.groups + ((kb * Q4_K + r * 32) >> g.shift)) * Q4_ROWS + 2 * gid + half]);
+                D* to = VEC ? g.w + (expert * g.n + row) * g.ldw + c : &stage.row[gid][c - kb * Q4_K];
+                const int left = VEC ? g.k - c : 8;
 #pragma unroll
                 for (int i = 0; i < 8 / N; ++i) {
                     float t[N];
@@ -229,10 +229,10 @@ __global__ void __launch_bounds__(256) q4_unpack_kernel(const __grid_constant__ 
                         const int j = i * N + e;
                         t[e] = s * (float)((int)(word[2 * r + (j >> 2)] >> (4 * (2 * ((j >> 1) & 1) + half) + 16 * (j & 1)) & 15u) - 8);
                     }
-                    store_pack(to + i * N, t, left - i * N, left >= (i + 1) * N);
+                    store_pack(to + i * N, t, left - i * N, left >= 8);
                 }
             }
-            if (!g.vec) {
+            if (!VEC) {
                 __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -676,12 +676,13 @@ static int launch_pack_typed(const ebs_q4_desc& d, const void* w, long long ldw,
     const Q4Layout l = q4_layout(d);
     const int kb = d.group == 128 ? 2 : 1;
     Q4Pack<S> g{static_cast<const S*>(w), static_cast<uint4*>(packed), static_cast<char*>(packed) + l.codes, ldw, (unsigned)(d.experts * (long long)l.tiles * ((l.kbs + kb - 1) / kb)),
-                d.n, d.k, l.tiles, l.kbs, l.groups, ldw * (long long)sizeof(S) % 16 == 0};
+                d.n, d.k, l.tiles, l.kbs, l.groups};
     const unsigned blocks = (g.units + 7u) / 8u;
     const dim3 grid(blocks < 148 * 64 ? blocks : 148 * 64);
-    if (d.group == 32) return launch_chained(q4_pack_kernel<S, T, 32>, grid, 256, 0, st, 1, g);
-    if (d.group == 64) return launch_chained(q4_pack_kernel<S, T, 64>, grid, 256, 0, st, 1, g);
-    return launch_chained(q4_pack_kernel<S, T, 128>, grid, 256, 0, st, 1, g);
+    const bool vec = ldw * (long long)sizeof(S) % 16 == 0;
+    if (d.group == 32) return launch_chained(vec ? q4_pack_kernel<S, T, 32, true> : q4_pack_kernel<S, T, 32, false>, grid, 256, 0, st, 1, g);
+    if (d.group == 64) return launch_chained(vec ? q4_pack_kernel<S, T, 64, true> : q4_pack_kernel<S, T, 64, false>, grid, 256, 0, st, 1, g);
+    return launch_chained(vec ? q4_pack_kernel<S, T, 128, true> : q4_pack_kernel<S, T, 128, false>, grid, 256, 0, st, 1, g);
 }
 template <typename S>
 static int launch_pack(const ebs_q4_desc& d, const void* w, long long ldw, void* packed, cudaStream_t st) {
@@ -693,9 +694,11 @@ template <typename T, typename D>
 static int launch_unpack_typed(const ebs_q4_desc& d, const void* packed, void* w, long long ldw, cudaStream_t st) {
     const Q4Layout l = q4_layout(d);
     Q4Unpack<D> g{static_cast<const uint4*>(packed), static_cast<const char*>(packed) + l.codes, static_cast<D*>(w), ldw, (unsigned)(d.experts * (long long)l.tiles * l.kbs), d.n, d.k,
-                  l.tiles, l.kbs, l.groups, d.group, ldw * (long long)sizeof(D) % 16 == 0};
+                  l.tiles, l.kbs, l.groups, d.group == 32 ? 5 : d.group == 64 ? 6 : 7};
     const unsigned blocks = (g.units + 7u) / 8u;
-    return launch_chained(q4_unpack_kernel<T, D>, dim3(blocks < 148 * 64 ? blocks : 148 * 64), 256, 0, st, 1, g);
+    const dim3 grid(blocks < 148 * 64 ? blocks : 148 * 64);
+    if (ldw * (long long)sizeof(D) % 16 == 0) return launch_chained(q4_unpack_kernel<T, D, true>, grid, 256, 0, st, 1, g);
+    return launch_chained(q4_unpack_kernel<T, D, false>, grid, 256, 0, st, 1, g);
 }
 template <typename D>
 static int launch_unpack(const ebs_q4_desc& d, const void* packed, void* w, long long ldw, cudaStream_t st) {
