@@ -61,27 +61,19 @@ __device__ __forceinline__ void load8(const S* p, int left, bool vec, float (&v)
     for (int e = 0; e < 8; ++e) v[e] = e < left ? to_f32(p[e]) : 0.0f;
 }
 
-// floor(w / s + 1/2) within -8 .. 7, exactly: the quotient by the reciprocal is off by a rounding or two, the remainders of a
-// fused multiply-add tell on which side of a border w lies.  inv = 1 / s.
-__device__ __noinline__ int q4_code_exact(float w, float s, float inv) {
-    float c = fminf(fmaxf(floorf(fmaf(w, inv, 0.5f)), -8.0f), 7.0f);
-    if (c < 7.0f && fmaf(-(c + 0.5f), s, w) >= 0.0f) c += 1.0f;
-    else if (c > -8.0f && fmaf(-(c - 0.5f), s, w) < 0.0f) c -= 1.0f;
-    return (int)c;
-}
-// The codes of eight weights, in the low four bits of each word, exactly too: a number of this size added leaves the quotient rounded in the low bits.  Where one lies within 2^-16 of a
-// border (the quotient is off by less), or the quotients leave the codes' range (a scale of few bits), each is found by its remainders.
+// floor(w / s + 1/2) of eight weights, exactly, in the low bits of each word.  The quotient by the reciprocal (inv = 1 / s) is off by less than 2^-19; with 2^-16 taken off first its floor (a
+// sum with 1.5 * 2^23, rounded down) is the code or one less, and the sign of a fused multiply-add's remainder tells which.  (Only those near a border by their remainders, the rest rounded:
+// fp32 weights the same, but half of the warps have one such 16-bit weight, and 235 million bf16 ones took 385 us.)  wide: quotients may leave -8 .. 7 (a scale of few bits).
 __device__ __forceinline__ void q4_codes(const float (&v)[8], float s, float inv, bool wide, uint32_t (&code)[8]) {
-    float far = 0.0f;
+    constexpr float WHOLE = 12582912.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float q = v[e] * inv, r = q + 12582912.0f;                 // 1.5 * 2^23
-        code[e] = __float_as_uint(r);
-        far = fmaxf(far, fabsf(q - (r - 12582912.0f)));
+        const float r = __fadd_rd(fmaf(v[e], inv, 0.5f - 0x1p-16f), WHOLE), left = fmaf(-((r - WHOLE) + 0.5f), s, v[e]);
+        code[e] = __float_as_uint(r) + 1u - (__float_as_uint(left) >> 31);
     }
-    if (far > 0.5f - 0x1p-16f || wide)
+    if (wide)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) code[e] = (uint32_t)q4_code_exact(v[e], s, inv);
+        for (int e = 0; e < 8; ++e) code[e] = (uint32_t)min(max((int)(code[e] - __float_as_uint(WHOLE)), -8), 7);
 }
 
 template <typename S>
@@ -173,14 +165,16 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4
                         top[b][r] = __float_as_uint(__uint_as_float(top[b][r]) * 1.2676506e30f);
                     }
                     const float inv = 1.0f / s;
-                    uint32_t code[8];
+                    uint32_t code[8], part[2] = {0u, 0u};
                     q4_codes(v[b][r], s, inv, __uint_as_float(top[b][r]) * inv > 7.4f, code);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         // register 2 * h + half of the MMA, element j; the code + 8 is the code with its sign bit turned
-                        const int at = 4 * (2 * ((e >> 1) & 1) + half) + 16 * (e & 1);
-                        word[b][2 * r + (e >> 2)] ^= (code[e] & 15u) << at;
+                        const int at = 8 * ((e >> 1) & 1) + 16 * (e & 1);
+                        part[e >> 2] |= (code[e] << at) & (15u << at);
                     }
+                    word[b][2 * r] ^= part[0] << (4 * half);
+                    word[b][2 * r + 1] ^= part[1] << (4 * half);
                 }
         }
 #pragma unroll
