@@ -92,7 +92,8 @@ template <typename S, int COLS> struct Q4Stage { S row[8][COLS + 16 / sizeof(S)]
 // A warp packs 16 rows x KB tiles of 64 inputs, which hold whole groups of G: the largest magnitudes, scales and codes from one load.
 template <typename S, typename T, int G, bool VEC>
 __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4Pack<S> g) {
-    constexpr int KB = G == 128 ? 2 : 1;
+    constexpr int KB = G == 128 ? 2 : 1, N = Pack<S>::N, W = 8 / N;
+    constexpr bool AHEAD = VEC && sizeof(S) == 2;
     let_next_kernel_start();
     wait_for_previous_kernel();
     __shared__ __align__(16) Q4Stage<S, KB * Q4_K> stages[VEC ? 1 : 8];
@@ -109,12 +110,11 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4
         for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) word[b][i] = 0x88888888u;
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {                    // rows gid and gid + 8
+        // All loads of a row before the first is used; of 16-bit weights the second half's (rows gid + 8) before the first half's codes are found.
+        uint4 raw[KB][2][W], next[KB][2][W];
+        const auto load = [&](int half, uint4 (&raw)[KB][2][W]) {
             const int row = row0 + gid + 8 * half;
-            const S* p = g.w + (expert * g.n + row) * g.ldw;
-            float v[KB][2][8];
-            unsigned top[KB][2];
+            const S* p = g.w + (expert * g.n + row) * g.ldw + kb0 * Q4_K;
             if (!VEC) {
                 __syncwarp();                                     // (what was there is read)
 #pragma unroll
@@ -125,15 +125,41 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4
                         stage.row[i][h * 32 + lane] = at < g.n && c < g.k ? g.w[(expert * g.n + at) * g.ldw + c] : from_f32<S>(0.0f);
                     }
                 __syncwarp();
+                p = stage.row[gid];
             }
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const int c = b * Q4_K + q4_input(r, lane, 0), left = g.k - kb0 * Q4_K - c;
-                    if (VEC) load8<S>(p + kb0 * Q4_K + c, row < g.n ? left : 0, true, v[b][r]);
-                    else load8<S>(&stage.row[gid][c], 8, true, v[b][r]);
+                    const int c = b * Q4_K + q4_input(r, lane, 0), left = !VEC ? 8 : row < g.n ? g.k - kb0 * Q4_K - c : 0;
+#pragma unroll
+                    for (int i = 0; i < W; ++i) raw[b][r][i] = left >= 8 ? reinterpret_cast<const uint4*>(p + c)[i] : make_uint4(0u, 0u, 0u, 0u);
+                    if (left > 0 && left < 8)
+#pragma unroll
+                        for (int e = 0; e < 7; ++e)
+                            if (e < left) reinterpret_cast<S*>(&raw[b][r][e / N])[e % N] = p[c + e];
                 }
+        };
+        load(0, raw);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {                    // rows gid and gid + 8
+            const int row = row0 + gid + 8 * half;
+            float v[KB][2][8];
+            unsigned top[KB][2];
+            if (AHEAD && half == 0) load(1, next);
+            if (!AHEAD && half == 1) load(1, raw);
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        float t[N];
+                        unpack<S>(raw[b][r][i], t);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) v[b][r][i * N + e] = t[e];
+                        if (AHEAD) raw[b][r][i] = next[b][r][i];
+                    }
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
