@@ -1,7 +1,7 @@
 // Layers with weights of 4 bits and a scale for each group of them: packing, reading back, and the product with a few rows.  See include/ebs.h.
 //
-// The product is bound by the weights' bytes (half a byte a weight and the scales), and next by the instructions that turn codes into operands (one row through 8192 -> 28672 bf16: 28 us,
-// 4.2 TB/s, the logic pipe 62% busy; packing 134 million fp32 weights 150 us, 4 TB/s).  Weights lie in
+// The product is bound by the weights' bytes (half a byte a weight and the scales), and next by the instructions that turn codes into operands (one row through 8192 -> 28672 bf16: 27 us,
+// 4.4 TB/s, the logic pipe 62% busy; packing 134 million fp32 weights 114 us, 5.3 TB/s).  Weights lie in
 // tiles of 16 outputs x 64 inputs, 512 bytes, in the order in which the lanes of a warp need them for four mma.sync m16n8k16: one 16-byte
 // load a lane.  A word holds the eight codes (+ 8) of a lane for one MMA, those of operand register i in bits 4i .. 4i+3 and 16+4i .. 16+4i+3, so that a mask and the bits of
 // a power of two make two 16-bit numbers of them at once.  Codes and 16-bit activations multiply exactly; a tile's sum over 64 inputs (32, where
@@ -63,7 +63,7 @@ __device__ __forceinline__ void load8(const S* p, int left, bool vec, float (&v)
 
 // floor(w / s + 1/2) of eight weights, exactly, in the low bits of each word.  The quotient by the reciprocal (inv = 1 / s) is off by less than 2^-19; with 2^-16 taken off first its floor (a
 // sum with 1.5 * 2^23, rounded down) is the code or one less, and the sign of a fused multiply-add's remainder tells which.  (Only those near a border by their remainders, the rest rounded:
-// fp32 weights the same, but half of the warps have one such 16-bit weight, and 235 million bf16 ones took 385 us.)  wide: quotients may leave -8 .. 7 (a scale of few bits).
+// fp32 weights the same, but two of five of a warp's loads of bf16 weights hold one such, and 235 million took 385 us, so 287.)  wide: quotients may leave -8 .. 7 (a scale of few bits).
 __device__ __forceinline__ void q4_codes(const float (&v)[8], float s, float inv, bool wide, uint32_t (&code)[8]) {
     constexpr float WHOLE = 12582912.0f;
 #pragma unroll
@@ -110,7 +110,8 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __grid_constant__ Q4
         for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) word[b][i] = 0x88888888u;
-        // All loads of a row before the first is used; of 16-bit weights the second half's (rows gid + 8) before the first half's codes are found.
+        // All loads of a row before the first is used (a branch a load: 140 us, so 114); of 16-bit weights the second half's (rows gid + 8) before the first half's codes are found (235 million
+        // bf16 287 us, so 214).
         uint4 raw[KB][2][W], next[KB][2][W];
         const auto load = [&](int half, uint4 (&raw)[KB][2][W]) {
             const int row = row0 + gid + 8 * half;
