@@ -507,7 +507,18 @@ def _clip_rows(t: torch.Tensor):
         return 1, t.numel(), t.numel()
     if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError("a tensor is dense, or a matrix whose rows are")
+    if t.stride(0) < t.shape[1]:                               # (an expanded matrix; 0 would mean dense to the library)
+        raise ValueError("the rows of a matrix share memory: clip the tensor that was expanded, or a copy")
     return t.shape[0], t.shape[1], t.stride(0)
+
+
+def _clip_record(t: torch.Tensor, o: torch.Tensor) -> ebs_clip_tensor:
+    """A gradient and its output, of the same type and shape."""
+    (rows, cols, ld), (rows_out, cols_out, ld_out) = _clip_rows(t), _clip_rows(o)
+    if rows != rows_out:                                       # (one of the two is dense, the other a matrix of strided rows)
+        rows, cols = t.shape
+        ld, ld_out = t.stride(0), o.stride(0)
+    return ebs_clip_tensor(t.data_ptr(), o.data_ptr(), rows, cols, ld, ld_out, _REAL_TYPES[t.dtype])
 
 
 def ebs_clip_plan(tensors, plan_host: Optional[torch.Tensor] = None, chunks: int = 0) -> int:
@@ -529,11 +540,7 @@ def clip_plan(tensors, outs=None) -> ClipPlan:
         if not t.is_cuda or (device is not None and t.device != device):
             raise ValueError("all gradients are on one GPU")
         device = t.device
-        (rows, cols, ld), (rows_out, cols_out, ld_out) = _clip_rows(t), _clip_rows(o)
-        if rows != rows_out:                                   # (one of the two is dense, the other a matrix of strided rows)
-            rows, cols = t.shape
-            ld, ld_out = t.stride(0), o.stride(0)
-        records.append(ebs_clip_tensor(t.data_ptr(), o.data_ptr(), rows, cols, ld, ld_out, _REAL_TYPES[t.dtype]))
+        records.append(_clip_record(t, o))
     chunks = ebs_clip_plan(records)
     host = torch.empty(max(1, chunks) * EBS_CLIP_CHUNK_BYTES, dtype=torch.uint8)
     ebs_clip_plan(records, host, chunks)
