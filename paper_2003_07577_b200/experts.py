@@ -72,10 +72,11 @@ class ExpertLinear:
 
     @torch.no_grad()
     def backward(self, dy: torch.Tensor) -> torch.Tensor:
-        """Gradient with respect to the x of the last forward pass; those of the weights (dw) and biases (dbias) are kept for step()."""
+        """Gradient with respect to the x of the last forward pass, zero in rows that are no expert's; those of the weights (dw) and biases (dbias) are kept for step()."""
         if self.x is None:
             raise RuntimeError("backward() before forward()")
         _check("dy", dy, (self.rows, self.weight.shape[1]), self.dtype, self.device)
+        self.dx.zero_()                                       # (the library leaves rows that are no expert's: they may have been one's in the step before)
         with torch.cuda.device(self.device):
             ebs.ebs_grouped_backward(dy, self.x, self.w, self.z if self.act else None, self.offsets, self.experts, self.desc, self.dx, self.dw, self.dbias, self._workspace)
         return self.dx
@@ -125,7 +126,8 @@ class QuantizedExperts:
 
     @torch.no_grad()
     def answer(self, x: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
-        """x: [m, k] with m <= rows, offsets: int32 [experts + 1] within 0 .. m.  The result stays valid until the next call."""
+        """x: [m, k] with m <= rows, offsets: int32 [experts + 1] within 0 .. m.  The result stays valid until the next call; its rows that are no
+        expert's hold whatever was there."""
         m = x.shape[0]
         if x.dim() != 2 or m > self.rows:
             raise ValueError(f"x has up to {self.rows} rows")
