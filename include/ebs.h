@@ -468,7 +468,7 @@ int ebs_grouped_backward(const void *dy_dev, const void *x_dev, const void *w_de
  *               (Offsets out of order or out of 0 .. m lead to no access out of bounds; which expert's results rows then get is not defined.)
  *
  * Products of codes and activations are exact, their sums over up to 64 inputs are taken in fp32 by the tensor core (it truncates; 2^-21 of a sum of
- * one sign at most), multiplied by the scale and added up in fp32.  EBS_F32 activations keep all their 24 bits.  Any number of rows is taken, up to
+ * one sign at most; 16-bit types with groups of 128: up to 128 inputs and 2^-20), multiplied by the scale and added up in fp32.  EBS_F32 activations keep all their 24 bits.  Any number of rows is taken, up to
  * 64 (EBS_F32: 32) at a time, each time with the expert's weights.  The order of sums goes by the sizes.  (Activations above 2^117 in EBS_F32 or
  * EBS_BF16 may overflow before they meet the scale.)
  *

@@ -5,7 +5,7 @@
 // tiles of 16 outputs x 64 inputs, 512 bytes, in the order in which the lanes of a warp need them for four mma.sync m16n8k16: one 16-byte
 // load a lane.  A word holds the eight codes (+ 8) of a lane for one MMA, those of operand register i in bits 4i .. 4i+3 and 16+4i .. 16+4i+3, so that a mask and the bits of
 // a power of two make two 16-bit numbers of them at once.  Codes and 16-bit activations multiply exactly; a tile's sum over 64 inputs (32, where
-// a group has no more) leaves the MMA in fp32 and is multiplied by its group's scale there.  fp32 activations go as three bf16 planes of
+// a group has no more; with few rows of 16-bit activations two tiles', where it has 128) leaves the MMA in fp32 and is multiplied by its group's scale there.  fp32 activations go as three bf16 planes of
 // 8 bits each, which hold all 24.
 //
 // MMA k index (step s, half h, lane group t = lane % 4, element j) stands for input (s / 2) * 32 + t * 8 + (s % 2) * 4 + h * 2 + j of the 64: a lane's share
@@ -478,8 +478,9 @@ template <typename T, bool PREPARED, int NT, int MT, int G, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, (q4_blocks<T, NT, WARPS>())) q4_kernel(const __grid_constant__ Q4Args g) {
     extern __shared__ float sums[];                                 // [warp][row][16 * MT outputs]
     constexpr int COLS = Q4_ROWS * MT, ROWS = 8 * NT, D = MT == 1 ? 4 : 2;
-    // tiles whose sum meets a scale: a group's two where that leaves the registers for it
-    constexpr int UNIT = G == 128 && NT <= 2 ? 2 : 1;
+    // Tiles whose sum meets a scale: a group's two where that leaves the registers for it, and of 16-bit types alone.  Eight steps of the tensor core cut 2^-20 of a sum of one sign at
+    // most, and those types round 2^-12 or 2^-9 of it; three planes make 24 steps, the second tile's on top of the whole first one's sum: 2^-20 seen, 2^-22 with a scale each.
+    constexpr int UNIT = G == 128 && NT <= 2 && sizeof(T) == 2 ? 2 : 1;
     using Acts = Q4Acts<T, PREPARED>;
     using X = typename Acts::X;
     using Operand = Q4Operand<T>;
@@ -637,7 +638,7 @@ static Q4Route q4_route(const ebs_linear_desc& d, const ebs_q4_desc& q) {
     while (r.nt < most && 8LL * r.nt < rows) r.nt *= 2;
     r.pieces = q.experts > 1 ? (long long)(q.experts < d.m ? q.experts : d.m) + d.m / (8 * r.nt) : (d.m + 8LL * r.nt - 1) / (8 * r.nt);
     r.blocks = r.pieces * ((tiles + q4_mt(r.nt) - 1) / q4_mt(r.nt));
-    // (4096 -> 14336 of four rows, 57344 tiles: 30.4 us split where they are used, 19.0 with the launch that prepares them, which costs 2)
+    // (4096 -> 14336 of four rows, 57344 tiles: 30.4 us split where they are used, 19.4 with the launch that prepares them, which costs 2)
     r.prepared = d.dtype == EBS_F32 && r.blocks * kbs >= 8192;
     r.copied = !r.prepared && d.m > 1 && d.ldx * (long long)element_size(d.dtype) % 16 != 0;
 // (14336 -> 4096: 15.6 us with 8 warps a tile, of which two blocks an SM have work, 9.9 with 16)
