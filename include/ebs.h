@@ -502,7 +502,8 @@ int ebs_linear_q4_forward(const void *x_dev, const void *packed_dev, const void 
  * A tensor has `rows` rows of `cols` elements of `dtype` (EBS_F32, EBS_F16, EBS_BF16), ld_* elements from one row to the next
  * (0: dense); what lies between rows is neither read nor written.  Either size may be 0: an empty tensor.  Addresses are
  * multiples of the element's size (rows whose places in `in` and `out` differ modulo 16 bytes are written an element at a time).
- * out may be the gradient itself (same address and stride); no output may share an element with any other tensor.
+ * out may be the gradient itself (same address and stride); no output may share an element with any other tensor (matrices of
+ * different strides that reach into one another count as sharing one).
  *
  * The tensors of a network are laid out once:
  *   ebs_clip_plan       checks `count` tensors (HOST array) and writes their work list, *chunks records of

@@ -321,15 +321,16 @@ static long long tensor_chunks(const ebs_clip_tensor& t, bool small) {
     const Cut c = cut_of(t, small);
     return (t.rows + c.rows - 1) / c.rows * ((t.cols + c.cols - 1) / c.cols);
 }
-// What a tensor reads or writes, in bytes.
+// What a tensor reads or writes, in bytes; pitch: 0 for one row.
 struct Extent {
     uintptr_t begin, end, pitch, width;
     int tensor;
     bool out;
 };
 static bool share(const Extent& a, const Extent& b) {
-    if (a.pitch != b.pitch) return true;                        // (their extents meet: the caller knows)
-    const uintptr_t d = (b.begin - a.begin) % a.pitch;          // b begins behind a
+    // (their extents meet, b begins behind a: the caller knows; matrices of different strides are not looked at further)
+    if (a.pitch == 0 || (b.pitch != 0 && a.pitch != b.pitch)) return true;
+    const uintptr_t d = (b.begin - a.begin) % a.pitch;
     return !(d >= a.width && a.pitch - d >= b.width);
 }
 
@@ -367,7 +368,7 @@ int ebs_clip_plan(const ebs_clip_tensor* tensors, int count, void* plan_host, lo
         const uintptr_t size = element_size(t.dtype);
         for (int out = 0; out < 2; ++out) {
             const uintptr_t p = (uintptr_t)(out ? t.out_dev : t.in_dev), ld = (uintptr_t)(out ? t.ld_out : t.ld_in);
-            e[n++] = Extent{p, p + ((uintptr_t)(t.rows - 1) * ld + (uintptr_t)t.cols) * size, ld * size, (uintptr_t)t.cols * size, i, out == 1};
+            e[n++] = Extent{p, p + ((uintptr_t)(t.rows - 1) * ld + (uintptr_t)t.cols) * size, t.rows > 1 ? ld * size : 0, (uintptr_t)t.cols * size, i, out == 1};
         }
     }
     std::sort(e, e + n, [](const Extent& a, const Extent& b) { return a.begin < b.begin; });
