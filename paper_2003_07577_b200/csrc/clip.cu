@@ -20,7 +20,7 @@ constexpr int CLIP_BLOCKS = 148 * 4;        // at most: a wave of blocks of 256 
 constexpr int CLIP_THREADS = 256;
 constexpr int CLIP_UNROLL = 8;              // packs of a thread under way: 32 KB a block (four, and records loaded when they are needed: 1.07 GB read at 3.4 TB/s)
 constexpr int CLIP_NARROW = 512;            // bytes of a row that a warp's lanes would not fill
-// Bytes of a chunk of one row: as many as the block has under way; a network of a few MB is cut finer, so that every SM has some.
+// Bytes of a chunk of pieces of one row or of narrow rows: as many as the block has under way; a network of a few MB is cut finer, so that every SM has some.
 constexpr long long CLIP_CHUNK = CLIP_THREADS * 16 * CLIP_UNROLL, CLIP_CHUNK_SMALL = CLIP_THREADS * 16, CLIP_SMALL = 8 << 20;
 
 // rows = 1: the block's threads share the row; more: a warp takes a row, or, of narrow rows, the threads their pieces of 16 bytes.
@@ -306,19 +306,21 @@ static int complete_tensor(const ebs_clip_tensor& in, ebs_clip_tensor* t) {
     }
     return EBS_OK;
 }
-// How a tensor is cut: whole rows, eights of them where a warp takes one, or pieces of one.
+// How a tensor of a network of `bytes` is cut: whole rows, eights of them where a warp takes one, or pieces of one.  Strided rows of 6 to 16 KB go one by one where the network has no
+// eight of them for every SM: 512 rows of 16 KB 10.0 us in eights, 8.2 one by one, 1024 of 8 KB 12.8 and 9.6, 1024 of 16 KB 20.2 and 11.7; 4096 of 8 KB 14.8 and 23.5, 1900 of 4.4 KB 10.1 and 12.4.
 struct Cut {
     long long rows, cols;
 };
-static Cut cut_of(const ebs_clip_tensor& t, bool small) {
-    const long long size = (long long)element_size(t.dtype), chunk = (small ? CLIP_CHUNK_SMALL : CLIP_CHUNK) / size;
-    if (t.rows == 1 || t.cols * size > 16384) return {1, chunk};
+static Cut cut_of(const ebs_clip_tensor& t, long long bytes) {
+    const long long size = (long long)element_size(t.dtype), chunk = (bytes <= CLIP_SMALL ? CLIP_CHUNK_SMALL : CLIP_CHUNK) / size, row = t.cols * size;
+    if (t.rows == 1 || row > 16384) return {1, chunk};
+    if (row > 6144 && bytes < 148 * 8 * row) return {1, t.cols};
     const long long r = chunk / t.cols & ~7LL;
     return {r < 8 ? 8 : r, t.cols};
 }
-static long long tensor_chunks(const ebs_clip_tensor& t, bool small) {
+static long long tensor_chunks(const ebs_clip_tensor& t, long long bytes) {
     if (t.rows == 0) return 0;
-    const Cut c = cut_of(t, small);
+    const Cut c = cut_of(t, bytes);
     return (t.rows + c.rows - 1) / c.rows * ((t.cols + c.cols - 1) / c.cols);
 }
 // What a tensor reads or writes, in bytes; pitch: 0 for one row.
@@ -350,11 +352,10 @@ int ebs_clip_plan(const ebs_clip_tensor* tensors, int count, void* plan_host, lo
         bytes += t.rows * t.cols * (long long)element_size(t.dtype);
         if (bytes > (1LL << 42)) return EBS_ERR_OVERFLOW;
     }
-    const bool small = bytes <= CLIP_SMALL;
     for (int i = 0; i < count; ++i) {
         ebs_clip_tensor t;
         complete_tensor(tensors[i], &t);
-        total += tensor_chunks(t, small);
+        total += tensor_chunks(t, bytes);
         if (total > (1LL << 31)) return EBS_ERR_OVERFLOW;
     }
     // no output may share an element with another tensor: extents in the order of their addresses
@@ -389,7 +390,7 @@ int ebs_clip_plan(const ebs_clip_tensor* tensors, int count, void* plan_host, lo
             complete_tensor(tensors[i], &t);
             if (t.rows == 0) continue;
             const long long size = (long long)element_size(t.dtype);
-            const Cut cut = cut_of(t, small);
+            const Cut cut = cut_of(t, bytes);
             for (long long r = 0; r < t.rows; r += cut.rows)
                 for (long long c = 0; c < t.cols; c += cut.cols) {
                     ClipChunk k = {};
