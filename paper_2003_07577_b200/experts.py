@@ -128,9 +128,9 @@ class QuantizedExperts:
     def answer(self, x: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
         """x: [m, k] with m <= rows, offsets: int32 [experts + 1] within 0 .. m.  The result stays valid until the next call; its rows that are no
         expert's hold whatever was there."""
-        m = x.shape[0]
-        if x.dim() != 2 or m > self.rows:
+        if x.dim() != 2 or x.shape[0] > self.rows:
             raise ValueError(f"x has up to {self.rows} rows")
+        m = x.shape[0]
         _check("x", x, (m, self.k), self.dtype, self.device)
         _check("offsets", offsets, (self.experts + 1,), torch.int32, self.device)
         y = self.y[:m]

@@ -47,3 +47,12 @@ def test_gradient_of_rows_that_are_no_experts_is_zero(mods, dtype, act, captured
         theirs[first:first + sum(counts)] = True
         assert not layer.dx[~theirs].any(), (first, counts)
         assert (layer.dx[theirs] != 0).any(dim=1).all()
+
+
+def test_answers_refuse_what_has_no_rows(mods):
+    _, ex = mods
+    served = ex.QuantizedExperts(torch.zeros(2, 8, 32, device="cuda"), 4, torch.float16, group=32)
+    o = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for shape in ((), (32,), (1, 2, 32), (5, 32), (4, 31)):
+        with pytest.raises(ValueError):
+            served.answer(torch.zeros(shape, dtype=torch.float16, device="cuda"), o)
