@@ -460,7 +460,7 @@ int ebs_grouped_backward(const void *dy_dev, const void *x_dev, const void *w_de
  *   pack      W [experts][n][k] of type w_dtype -> for each group of a row (the last one of a row may be shorter)
  *               scale = max|w| * fl32(1/7), rounded to fp32 and to `dtype`,  code = floor(w / scale + 1/2) within -8 .. 7, exactly (codes of
  *               a zero scale are 0).  A group with an infinity or a NaN (or whose scale overflows) stands for NaN throughout.
- *   unpack    scale * code, rounded to w_dtype: what the packed weights stand for (a prompt of many rows multiplies them with
+ *   unpack    scale * code, rounded to fp32 and to w_dtype: what the packed weights stand for (a prompt of many rows multiplies them with
  *               ebs_linear_forward or ebs_grouped_forward)
  *   forward   y = act(x W_e^T + bias_e) + residual     x [m][k], bias [experts][n], residual and y [m][n], all of type `dtype`;
  *               act as in ebs_linear_forward.  Rows offsets[e] .. offsets[e+1]-1 are expert e's; offsets_dev: int32
@@ -468,8 +468,8 @@ int ebs_grouped_backward(const void *dy_dev, const void *x_dev, const void *w_de
  *               (Offsets out of order or out of 0 .. m lead to no access out of bounds; which expert's results rows then get is not defined.)
  *
  * Products of codes and activations are exact, their sums over up to 64 inputs are taken in fp32 by the tensor core (it truncates; 2^-21 of a sum of
- * one sign at most; 16-bit types with groups of 128: up to 128 inputs and 2^-20), multiplied by the scale and added up in fp32.  EBS_F32 activations keep all their 24 bits.  Any number of rows is taken, up to
- * 64 (EBS_F32: 32) at a time, each time with the expert's weights.  The order of sums goes by the sizes.  (Activations above 2^117 in EBS_F32 or
+ * one sign at most; 16-bit types with groups of 128: up to 128 inputs and 2^-20), multiplied by the scale and added up in fp32.
+ * EBS_F32 activations keep all their 24 bits (below 2^-110: multiples of 2^-133).  Any number of rows is taken, up to 64 (EBS_F32: 32) at a time, each time with the expert's weights.  The order of sums goes by the sizes.  (Activations above 2^117 in EBS_F32 or
  * EBS_BF16 may overflow before they meet the scale.)
  *
  * packed: ebs_q4_packed_bytes(desc) bytes, laid out for one kernel (its layout is not part of the interface).  ldw: elements

@@ -2,8 +2,8 @@
 //
 // Bound by the bytes: one pass reads every gradient for the sum of squares, one reads it again and writes it (537 million bf16: 154 us, 7.0 TB/s, and 333 us, 6.4 TB/s).  The work list ("plan") cuts all
 // tensors into chunks, a record each, so that a block learns from one 48-byte load what to do next, however many tensors there are and whatever their
-// sizes; the next record is on its way while a chunk is read.  The second pass takes the chunks from the last to the first: what the first pass read last is still in
-// the second-level cache.
+// sizes; the next record is on its way while a chunk is read.  The second pass takes the chunks from the last to the first, so that it begins with what the
+// second-level cache has (from the first to the last: 73 MB of padded fp16 rows, again and again, 42.5 us instead of 37.4, 134 MB 75.0 and 68.8, 268 MB 142.8 and 138.3, 1.07 GB the same).
 //
 // The sum is taken in 64 bits.  A pack of 16 bytes is squared and added in fp32 first (relative error 2^-22 of the pack at most), unless that sum
 // leaves the range where neither an overflow nor a lost small square matters; then each square is taken in 64 bits.  Partial sums are added in

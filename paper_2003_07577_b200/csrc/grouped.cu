@@ -11,8 +11,8 @@
 //
 // One warp fetches by TMA, one issues the MMAs, the first 8 (pair: 16) take the sums of the finished tile out of tensor memory while the next one is
 // multiplied (two accumulators).  Sums of more than 4096 terms leave the tensor core on the way, which truncates what it adds.  Results go
-// through a patch of shared memory, so that neighbouring lanes write neighbouring bytes, and leave with ordinary stores: a row that is not the expert's
-// is not written.
+// through a patch of shared memory, 32 rows at a time, and leave by TMA where all 32 are the expert's; else, and where rows do not start on 16 bytes, neighbouring lanes write
+// neighbouring bytes with ordinary stores: a row that is not the expert's is not written.
 #include "gemm_tile.cuh"
 #include "tensors.cuh"
 

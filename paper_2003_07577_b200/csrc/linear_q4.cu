@@ -1,7 +1,7 @@
 // Layers with weights of 4 bits and a scale for each group of them: packing, reading back, and the product with a few rows.  See include/ebs.h.
 //
-// The product is bound by the weights' bytes (half a byte a weight and the scales), and next by the instructions that turn codes into operands (one row through 8192 -> 28672 bf16: 27 us,
-// 4.4 TB/s, the logic pipe 62% busy; packing 134 million fp32 weights 114 us, 5.3 TB/s).  Weights lie in
+// The product is bound by the weights' bytes (half a byte a weight and the scales), and next by the instructions that turn codes into operands (one row through 8192 -> 28672 bf16: 27 to 29 us,
+// 4.1 to 4.4 TB/s, the logic pipe 62% busy; packing 134 million fp32 weights 114 us, 5.3 TB/s).  Weights lie in
 // tiles of 16 outputs x 64 inputs, 512 bytes, in the order in which the lanes of a warp need them for four mma.sync m16n8k16: one 16-byte
 // load a lane.  A word holds the eight codes (+ 8) of a lane for one MMA, those of operand register i in bits 4i .. 4i+3 and 16+4i .. 16+4i+3, so that a mask and the bits of
 // a power of two make two 16-bit numbers of them at once.  Codes and 16-bit activations multiply exactly; a tile's sum over 64 inputs (32, where
